@@ -1,0 +1,524 @@
+"""What stands around the linear layers in a private training step, case by case: layer norms (whose
+weights are clipped per sample as the linear layers' are), attention, and the optimizer that takes
+the private gradient. Each runs in its plain form or through the library's entry points.
+
+A case:
+  op       layer_norm, layer_norm_grad     B samples of T tokens of width d; add: a residual stream goes
+                                           through (added before the norm, its gradient after it)
+           attention, attention_grad       H heads of width D, Hkv of them for keys and values; Tk keys;
+                                           lens: full (no lengths given) or ragged (every sample its own)
+           adamw                           tensors of a stack of `n` blocks of width d, biases and norms too
+                                           (stack "block"), or one rank's contiguous share of their flattened
+                                           gradient ("shard"); states of 32 or 8 bits; copy: 16-bit weights
+                                           written beside the 32-bit ones
+  dtype    of activations, or of the gradient that the optimizer reads
+"""
+import math
+
+import torch
+
+own = False
+
+DTYPES = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+EPS = 1e-5                                            # layer norm
+LR, BETA1, BETA2, ADAM_EPS, DECAY, GRAD_SCALE, STEP = 3e-4, 0.9, 0.95, 1e-8, 0.1, 1.0 / 16, 7
+BLOCK, FP8_MAX = 256, 448                             # 8-bit states: values to a scale, the format's largest value
+
+
+def _norm(op, dtype, B, T, d, add, name=None):
+    c = dict(op=op, dtype=dtype, B=B, T=T, d=d, add=add)
+    return dict(c, name=name) if name else c
+
+
+def _attn(op, dtype, B, T, H, Hkv, D, causal, lens="full", Tk=0, name=None):
+    c = dict(op=op, dtype=dtype, B=B, T=T, Tk=Tk or T, H=H, Hkv=Hkv, D=D, causal=causal, lens=lens)
+    return dict(c, name=name) if name else c
+
+
+def _adamw(dtype, bits, stack, d, n, ranks, copy, name=None):
+    c = dict(op="adamw", dtype=dtype, bits=bits, stack=stack, d=d, n=n, ranks=ranks, copy=copy)
+    return dict(c, name=name) if name else c
+
+
+def listed():
+    return [
+        # the smallest call, all latency: the 16-wide fp32 layer's input of a user's first test
+        _norm("layer_norm", "f32", 4, 8, 16, False, name="norm_tiny_f32"),
+        # one of the large GPT stack's 72 norms, with the residual stream going through
+        _norm("layer_norm", "bf16", 8, 512, 1280, True, name="norm_gpt_large"),
+        # backward of one of the small GPT stack's norms: 16 samples of 256 tokens, a clipped gradient for each
+        _norm("layer_norm_grad", "bf16", 16, 256, 768, True, name="norm_grad_gpt_small"),
+        # backward at the width of the 12288-wide block, few long samples
+        _norm("layer_norm_grad", "bf16", 4, 2048, 12288, False, name="norm_grad_wide"),
+        # attention of the small GPT stack, one layer
+        _attn("attention", "bf16", 16, 256, 12, 12, 64, True, name="attention_gpt_small"),
+        # few long documents, 4096 tokens
+        _attn("attention", "bf16", 2, 4096, 12, 12, 64, True, name="attention_long"),
+        # image patches plus one class token: 197 tokens, no mask
+        _attn("attention", "f16", 32, 197, 12, 12, 64, False, name="attention_patches_197"),
+        # backward, the large GPT stack: 512 tokens, 20 heads
+        _attn("attention_grad", "bf16", 8, 512, 20, 20, 64, True, name="attention_grad_gpt_large"),
+        # backward at the 12288-wide block: 96 heads of 128, one worker's four samples of 2048 tokens
+        _attn("attention_grad", "bf16", 4, 2048, 96, 96, 128, True, name="attention_grad_wide"),
+        # backward of a batch of unequal lengths, heads of 56 that share keys and values two by two
+        _attn("attention_grad", "f16", 18, 591, 14, 7, 56, True, "ragged", name="attention_grad_ragged"),
+        # all 148 tensors of the small GPT stack in one step, odd sizes among them, 16-bit weights beside
+        _adamw("f32", 32, "block", 768, 12, 1, True, name="adamw_gpt_small"),
+        # one of eight shards of the 12288-wide block, states in 8 bits
+        _adamw("f32", 8, "shard", 12288, 1, 8, False, name="adamw_8bit_shard"),
+    ]
+
+
+def _spread(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    """One more case of the ranges above."""
+    while True:
+        op = rng.choice(["layer_norm", "layer_norm_grad", "attention", "attention", "attention_grad", "attention_grad", "adamw"])
+        dtype = rng.choice(["bf16", "bf16", "f16", "f32"])
+        if op == "adamw":
+            stack = rng.choice(["block", "shard"])
+            c = _adamw(dtype, rng.choice([32, 8]), stack, _spread(rng, 10, 4096), rng.randint(1, 12),
+                       rng.choice([1, 2, 4, 8]) if stack == "shard" else 1, rng.random() < 0.5)
+            if work(c)["bytes"] < 3.6e9:
+                return c
+        elif op.startswith("layer_norm"):
+            d = _spread(rng, 16, 16384)
+            if rng.random() < 0.7:
+                d = 8 * -(-d // 8)
+            c = _norm(op, dtype, _spread(rng, 1, 64), _spread(rng, 1, 4096), d, rng.random() < 0.5)
+            if work(c)["bytes"] < 6e8:
+                return c
+        else:
+            B, T, Hkv = _spread(rng, 1, 64), _spread(rng, 1, 4096), _spread(rng, 1, 24)
+            H = Hkv * rng.choice([1, 1, 1, 2, 4, 8])
+            D = rng.choice([64, 64, 128, 8 * rng.randint(1, 16)])
+            Tk = T if rng.random() < 0.75 else _spread(rng, 1, 4096)
+            if dtype == "f32":                        # 32-bit networks are small ones
+                B, T, Tk, H, Hkv = min(B, 8), -(-T // 32), -(-Tk // 32), -(-Hkv // 4), -(-Hkv // 4)
+            c = _attn(op, dtype, B, T, H, Hkv, D, rng.random() < 0.6, rng.choice(["full", "full", "ragged"]), Tk)
+            if B * H * T * Tk <= 4e8 and B * H * D * (T + Tk) <= 4e8:
+                return c
+
+
+def _stack_shapes(d, n):
+    """Of n blocks of width d: four weights and biases (d to 3d, d to d, d to 4d, 4d to d) and two norms' gains and
+    biases, then a last norm and a head to an odd number of classes."""
+    block = [(d, 3 * d), (3 * d,), (d, d), (d,), (d, 4 * d), (4 * d,), (4 * d, d), (d,), (d,), (d,), (d,), (d,)]
+    return block * n + [(d,), (d,), (d, 5), (5,)]
+
+
+def _sizes(case):
+    """Numbers of values of the tensors that one step updates."""
+    sizes = [math.prod(s) for s in _stack_shapes(case["d"], case["n"])]
+    return sizes if case["stack"] == "block" else [max(1, sum(sizes) // case["ranks"])]
+
+
+# ---------------------------------------------------------------------------------------------- inputs
+
+def _generator(seed):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    return gen
+
+
+def _prepare_norm(case, gen):
+    B, T, d, dt = case["B"], case["T"], case["d"], DTYPES[case["dtype"]]
+    kw = dict(generator=gen, device="cuda")
+    s = dict(x=(torch.randn((B, T, d), **kw) * 2 + torch.randn((1, 1, d), **kw)).to(dt),
+             gain=1 + 0.2 * torch.randn(d, **kw), bias=0.2 * torch.randn(d, **kw))
+    if case["op"] == "layer_norm":
+        s["add"] = torch.randn((B, T, d), **kw).to(dt) if case["add"] else None
+        s["sum"] = torch.empty_like(s["x"]) if case["add"] else None
+        s["y"] = torch.empty_like(s["x"])
+        s["mean"], s["rstd"] = torch.empty((B, T), device="cuda"), torch.empty((B, T), device="cuda")
+        return s
+    x = s["x"].float()
+    s["mean"] = x.mean(-1)
+    s["rstd"] = (x.var(-1, unbiased=False) + EPS).rsqrt()
+    s["dy"] = (torch.randn((B, T, d), **kw) * 0.01).to(dt)
+    s["add"] = (torch.randn((B, T, d), **kw) * 0.01).to(dt) if case["add"] else None
+    s["dx"] = torch.empty_like(s["x"])
+    s["kept"] = torch.empty((B, 2, d), device="cuda")             # per-sample gradients of gain and bias
+    s["sqnorm"] = torch.empty(B, device="cuda")
+    return s
+
+
+def _lens(n, most, gen):
+    """Lengths of a padded batch: most of them long, one of them full, one of one token (none at all in large batches)."""
+    lens = (most * torch.rand(n, generator=gen, device="cuda") ** 0.5).ceil().to(torch.int32)
+    lens[0] = most
+    if n > 2:
+        lens[1] = 1
+    if n > 8:
+        lens[2] = 0
+    return lens
+
+
+def _prepare_attention(case, gen):
+    B, T, Tk, H, Hkv, D, dt = case["B"], case["T"], case["Tk"], case["H"], case["Hkv"], case["D"], DTYPES[case["dtype"]]
+    kw = dict(generator=gen, device="cuda")
+
+    def projections():                               # as the projection writes them: one row holds all heads of a token
+        if T == Tk:
+            packed = torch.randn((B, T, H + 2 * Hkv, D), **kw).to(dt)
+            return packed[:, :, :H], packed[:, :, H:H + Hkv], packed[:, :, H + Hkv:]
+        q, kv = torch.randn((B, T, H, D), **kw).to(dt), torch.randn((B, Tk, 2 * Hkv, D), **kw).to(dt)
+        return q, kv[:, :, :Hkv], kv[:, :, Hkv:]
+
+    q, k, v = projections()
+    s = dict(q=q, k=k, v=v, scale=1.0 / math.sqrt(D), q_len=None, k_len=None)
+    if case["lens"] == "ragged":
+        s["k_len"] = _lens(B, Tk, gen)
+        s["q_len"] = s["k_len"] if T == Tk else _lens(B, T, gen)
+    s["o"] = torch.empty((B, T, H, D), dtype=dt, device="cuda")
+    s["lse"] = torch.empty((B, H, T), device="cuda")
+    if case["op"] == "attention_grad":
+        o, lse = _plain_attention(s, case)
+        s["o"].copy_(o)
+        s["lse"].copy_(lse)
+        s["do"] = (torch.randn((B, T, H, D), **kw) * 0.01).to(dt)
+        s["dq"], s["dk"], s["dv"] = projections()     # the projection's gradient has its layout
+    return s
+
+
+def _prepare_adamw(case, gen):
+    kw = dict(generator=gen, device="cuda")
+    sizes = _sizes(case)
+    total, blocks = sum(sizes), [-(-n // BLOCK) for n in sizes]
+    s = dict(sizes=sizes, param=0.02 * torch.randn(total, **kw))
+    # clipped sum plus noise: most of a value is noise
+    s["grad"] = (0.6 * torch.randn(total, **kw) + 0.3).to(DTYPES[case["dtype"]])
+    s["m"], s["v"] = 0.05 * torch.randn(total, **kw), (0.05 * torch.randn(total, **kw)).square() + 1e-4
+    s["copy"] = torch.empty(total, dtype=torch.bfloat16, device="cuda") if case["copy"] else None
+    s["t"] = {}                                       # the flattened model: every tensor a view at its running offset
+    if case["bits"] == 8:
+        m, v = s["m"].split(sizes), s["v"].split(sizes)
+        s["m"], s["v"] = (torch.empty(total, dtype=torch.float8_e4m3fn, device="cuda") for _ in range(2))
+        s["m_scale"], s["v_scale"] = (torch.empty(sum(blocks), device="cuda") for _ in range(2))
+        s["t"] = {k: list(s[k].split(blocks)) for k in ("m_scale", "v_scale")}
+        list(map(_encode, m, s["m"].split(sizes), s["t"]["m_scale"], [STEP - 1] * len(sizes)))
+        list(map(_encode, map(torch.sqrt, v), s["v"].split(sizes), s["t"]["v_scale"], [STEP - 1] * len(sizes)))
+    s["t"] |= {k: list(s[k].split(sizes)) for k in ("param", "grad", "m", "v", "copy") if s[k] is not None}
+    # weights decay, biases and norms do not
+    s["decay"] = [DECAY if case["stack"] == "shard" or len(shape) == 2 else 0.0 for shape in _stack_shapes(case["d"], case["n"])][:len(sizes)]
+    return s
+
+
+def prepare(case, seed):
+    gen = _generator(seed)
+    make = {"l": _prepare_norm, "a": _prepare_attention}[case["op"][0]] if case["op"] != "adamw" else _prepare_adamw
+    s = make(case, gen)
+    s["case"] = case
+    if own:
+        s["plan"] = _plan(s, case)
+    return s
+
+
+# ---------------------------------------------------------------------------------------------- plain forms
+
+def _plain_norm(s):
+    x = s["x"].float()
+    if s["add"] is not None:
+        s["sum"].copy_(x + s["add"].float())          # the stream is kept in the activations' type, and normalised as kept
+        x = s["sum"].float()
+    mean = x.mean(-1)
+    x = x - mean[..., None]
+    rstd = (x.square().mean(-1) + EPS).rsqrt()
+    y = (x * rstd[..., None] * s["gain"] + s["bias"]).to(s["x"].dtype)
+    return dict(y=y, mean=mean, rstd=rstd, sum=s["sum"])
+
+
+def _plain_norm_grad(s):
+    x, dy = s["x"].float(), s["dy"].float()
+    x = (x - s["mean"][..., None]) * s["rstd"][..., None]
+    kept = torch.stack(((dy * x).sum(1), dy.sum(1)), 1)
+    g = dy * s["gain"]
+    dx = (g - g.mean(-1, keepdim=True) - x * (g * x).mean(-1, keepdim=True)) * s["rstd"][..., None]
+    if s["add"] is not None:
+        dx = dx + s["add"].float()
+    return dict(dx=dx.to(s["x"].dtype), kept=kept, sqnorm=kept.square().sum((1, 2)))
+
+
+def _allowed(s, case):
+    """[B or 1, 1, T, Tk]: the keys that a row sees; None where it sees all."""
+    T, Tk, B = case["T"], case["Tk"], case["B"]
+    if not case["causal"] and s["k_len"] is None:
+        return None
+    i, j = torch.arange(T, device="cuda")[:, None], torch.arange(Tk, device="cuda")
+    n = torch.full((1,), T, device="cuda") if s["q_len"] is None else s["q_len"]
+    m = torch.full((1,), Tk, device="cuda") if s["k_len"] is None else s["k_len"]
+    n, m = n[:, None, None], m[:, None, None]
+    seen = (i < n) & (j < m)
+    if case["causal"]:
+        seen = seen & (j <= i + (m - n))
+    return seen[:, None]
+
+
+def _heads(x, Hkv, kind=torch.float32):
+    """[B, T, H, D] as [B, Hkv, heads that share a key, T, D]."""
+    B, T, H, D = x.shape
+    return x.to(kind).permute(0, 2, 1, 3).reshape(B, Hkv, H // Hkv, T, D)
+
+
+def _scores(s, case, kind=torch.float32):
+    """Scaled products, masked, [B, H, T, Tk], and the operands that they come from."""
+    q, k = _heads(s["q"], case["Hkv"], kind), _heads(s["k"], case["Hkv"], kind)
+    scores = torch.matmul(q, k.transpose(-1, -2)) * s["scale"]
+    scores = scores.reshape(case["B"], case["H"], case["T"], case["Tk"])
+    seen = _allowed(s, case)
+    return (scores if seen is None else scores.masked_fill_(~seen, -math.inf)), q, k
+
+
+def _plain_attention(s, case, kind=torch.float32):
+    scores, _, _ = _scores(s, case, kind)
+    most = scores.amax(-1, keepdim=True)
+    most = torch.where(torch.isinf(most), torch.zeros_like(most), most)        # rows that see nothing
+    p = scores.sub_(most).exp_()
+    total = p.sum(-1, keepdim=True)
+    lse = (total.log() + most).squeeze(-1)
+    p /= torch.where(total == 0, torch.ones_like(total), total)
+    v = _heads(s["v"], case["Hkv"], kind)
+    o = torch.matmul(p.reshape(*v.shape[:2], -1, case["T"], case["Tk"]), v)
+    o = o.reshape(case["B"], case["H"], case["T"], case["D"]).permute(0, 2, 1, 3)
+    return o.to(s["q"].dtype if kind is torch.float32 else kind).contiguous(), lse
+
+
+def _plain_attention_grad(s, case):
+    scores, q, k = _scores(s, case)
+    lse = torch.where(torch.isinf(s["lse"]), torch.zeros_like(s["lse"]), s["lse"])
+    p = scores.sub_(lse[..., None]).exp_()
+    do, v = _heads(s["do"], case["Hkv"]), _heads(s["v"], case["Hkv"])
+    delta = (s["do"].float() * s["o"].float()).sum(-1).permute(0, 2, 1)
+    p = p.reshape(*q.shape[:4], case["Tk"])
+    dv = torch.matmul(p.transpose(-1, -2), do).sum(2)
+    ds = torch.matmul(do, v.transpose(-1, -2)).sub_(delta.reshape(*q.shape[:4], 1)).mul_(p).mul_(s["scale"])
+    dk = torch.matmul(ds.transpose(-1, -2), q).sum(2)
+    dq = torch.matmul(ds, k).reshape(case["B"], case["H"], case["T"], case["D"])
+    back = lambda x: x.permute(0, 2, 1, 3).to(s["q"].dtype).contiguous()  # noqa: E731
+    return dict(dq=back(dq), dk=back(dk), dv=back(dv))
+
+
+def _blocked(x):
+    """[n] as [blocks, 256], zeros behind the end."""
+    return torch.nn.functional.pad(x, (0, -x.numel() % BLOCK)).reshape(-1, BLOCK)
+
+
+def _decode(code, scale):
+    return (_blocked(code.to(scale.dtype)) * scale[:, None]).reshape(-1)[:code.numel()]
+
+
+def _dither(n, step):
+    """In [0, 1), evenly spread over the elements at a step and over the steps of an element: the fractional part of
+    element * (sqrt(2) - 1) + step * (golden ratio - 1), in 32-bit integers."""
+    h = (torch.arange(n, device="cuda") * 0x6A09E667 + step * 0x9E3779B1) & 0xFFFFFFFF
+    return (h >> 8).float() * 2.0 ** -24
+
+
+def _encode(x, code, scale, step):
+    """Values in 8 bits (sign, 4 bits of exponent, 3 of fraction) in units of their block's largest / 448, rounded up where
+    the rest is above one minus the dither, so that an average's small changes are not lost; not to zero from above it."""
+    b = _blocked(x)
+    scale.copy_(b.abs().amax(1) / FP8_MAX)
+    a = b.abs() / torch.where(scale > 0, scale, 1)[:, None]
+    unit = torch.ldexp(torch.ones_like(a), (torch.frexp(a).exponent - 1).clamp(min=-6) - 3)
+    c = (a / unit + _blocked(_dither(x.numel(), step))).floor() * unit
+    c = torch.where(a > 0, c.clamp(2.0 ** -9, FP8_MAX), 0.0) * b.sign()
+    code.copy_(c.reshape(-1)[:x.numel()])
+
+
+def _plain_adamw_one(decay, param, grad, m, v, copy, m_scale, v_scale):
+    g = grad.float() * GRAD_SCALE
+    m32, v32 = (m, v) if m_scale is None else (_decode(m, m_scale), _decode(v, v_scale).square())
+    m32 = BETA1 * m32 + (1 - BETA1) * g
+    v32 = BETA2 * v32 + (1 - BETA2) * g * g
+    step = m32 / (1 - BETA1 ** STEP) / ((v32 / (1 - BETA2 ** STEP)).sqrt() + ADAM_EPS)
+    param.copy_(param * (1 - LR * decay) - LR * step)
+    if m_scale is None:
+        m.copy_(m32)
+        v.copy_(v32)
+    else:                                             # the second state's root is what is kept in 8 bits
+        _encode(m32, m, m_scale, STEP)
+        _encode(v32.sqrt(), v, v_scale, STEP)
+    if copy is not None:
+        copy.copy_(param)
+
+
+def _adamw_outputs(s):
+    return {k: s[k] for k in ("param", "copy", "m", "v", "m_scale", "v_scale") if k in s}
+
+
+def _plain_adamw(s):
+    t, none = s["t"], [None] * len(s["sizes"])
+    columns = [t.get(k, none) for k in ("param", "grad", "m", "v", "copy", "m_scale", "v_scale")]
+    list(map(_plain_adamw_one, s["decay"], *columns))
+
+
+# ---------------------------------------------------------------------------------------------- the library's calls
+
+def _plan(s, case):
+    """What a program that trains keeps from step to step."""
+    from paper_2311_11822_amd import block
+    if case["op"] == "adamw":
+        t = s["t"]
+        return block.AdamW(t["param"], t["grad"], t["m"], t["v"], s["decay"], t.get("copy"), t.get("m_scale"), t.get("v_scale"))
+    if case["op"].startswith("layer_norm"):
+        return block.LayerNorm(s["gain"], s["bias"], EPS)
+    return block.Attention(s["q"], s["k"], s["v"], s["o"], case["causal"], s["scale"], s["q_len"], s["k_len"])
+
+
+def _own_norm(s, case):
+    if case["op"] == "layer_norm":
+        s["plan"].forward(s["x"], s["y"], s["mean"], s["rstd"], s["add"], s["sum"])
+        return dict(y=s["y"], mean=s["mean"], rstd=s["rstd"], sum=s["sum"])
+    s["plan"].backward(s["x"], s["dy"], s["mean"], s["rstd"], s["dx"], s["kept"], s["sqnorm"], s["add"])
+    return dict(dx=s["dx"], kept=s["kept"], sqnorm=s["sqnorm"])
+
+
+def _own_attention(s, case):
+    if case["op"] == "attention":
+        s["plan"].forward(s["q"], s["k"], s["v"], s["o"], s["lse"])
+        return dict(o=s["o"], lse=s["lse"])
+    s["plan"].backward(s["q"], s["k"], s["v"], s["o"], s["lse"], s["do"], s["dq"], s["dk"], s["dv"])
+    return dict(dq=s["dq"], dk=s["dk"], dv=s["dv"])
+
+
+def run(state):
+    s, case = state, state["case"]
+    if case["op"] == "adamw":
+        if own:
+            s["plan"].step(STEP, LR, BETA1, BETA2, ADAM_EPS, GRAD_SCALE)
+        else:
+            _plain_adamw(s)
+        return _adamw_outputs(s)
+    if case["op"].startswith("layer_norm"):
+        return _own_norm(s, case) if own else _plain_norm(s) if case["op"] == "layer_norm" else _plain_norm_grad(s)
+    if own:
+        return _own_attention(s, case)
+    if case["op"] == "attention":
+        o, lse = _plain_attention(s, case)
+        return dict(o=o, lse=lse)
+    return _plain_attention_grad(s, case)
+
+
+# ---------------------------------------------------------------------------------------------- costs
+
+def work(case):
+    """Each input read once, each output written once; of attention's products the pairs that a causal mask leaves
+    (of ragged lengths: as of full ones, since they are drawn with the inputs); backward: its five products."""
+    e = 4 if case["dtype"] == "f32" else 2
+    if case["op"] == "adamw":
+        n = sum(_sizes(case))
+        states = 16 if case["bits"] == 32 else 4 + 16 / BLOCK
+        return {"bytes": int(n * (8 + e + states + 2 * case["copy"])), "flops": 16 * n}
+    if case["op"].startswith("layer_norm"):
+        B, rows, d = case["B"], case["B"] * case["T"], case["d"]
+        if case["op"] == "layer_norm":
+            return {"bytes": (4 if case["add"] else 2) * rows * d * e + 8 * rows + 8 * d, "flops": 9 * rows * d}
+        return {"bytes": (4 if case["add"] else 3) * rows * d * e + 8 * rows + 4 * d + 8 * B * d + 4 * B, "flops": 16 * rows * d}
+    B, T, Tk, H, Hkv, D = (case[k] for k in ("B", "T", "Tk", "H", "Hkv", "D"))
+    full = T * Tk
+    if case["causal"]:                                # row i sees keys up to i + Tk - T
+        seen = min(T, Tk)
+        full = seen * (seen + 1) // 2 + (seen * (Tk - T) if Tk > T else 0)
+    mine, shared = B * T * H * D * e, B * Tk * Hkv * D * e
+    if case["op"] == "attention":
+        return {"bytes": 2 * mine + 2 * shared + 4 * B * H * T, "flops": 4 * B * H * D * full}
+    return {"bytes": 4 * mine + 4 * shared + 4 * B * H * T, "flops": 10 * B * H * D * full}
+
+
+# ---------------------------------------------------------------------------------------------- 64 bits
+
+def _exact_norm(s, case):
+    x, gain, bias = s["x"].double(), s["gain"].double(), s["bias"].double()
+    if case["op"] == "layer_norm":
+        if s["add"] is not None:
+            x = (x + s["add"].double()).to(s["x"].dtype).double()
+        mean, var = x.mean(-1), x.var(-1, unbiased=False)
+        rstd = 1 / (var + EPS).sqrt()
+        y = gain * (x - mean.unsqueeze(-1)) * rstd.unsqueeze(-1) + bias
+        return dict(y=y, mean=mean, rstd=rstd, sum=x if s["add"] is not None else None)
+    # the Jacobian of one row: (diag(1) - 1 1'/d - h h'/d) * rstd, with h the normalised row
+    dy, rstd = s["dy"].double(), s["rstd"].double().unsqueeze(-1)
+    h = (x - s["mean"].double().unsqueeze(-1)) * rstd
+    u = dy * gain
+    d = case["d"]
+    dx = rstd * (u - u.sum(-1, keepdim=True) / d - h * (u * h).sum(-1, keepdim=True) / d)
+    if s["add"] is not None:
+        dx = dx + s["add"].double()
+    kept = torch.cat((torch.einsum("btd,btd->bd", dy, h)[:, None], dy.sum(1, keepdim=True)), 1)
+    return dict(dx=dx, kept=kept, sqnorm=(kept ** 2).sum(dim=(1, 2)))
+
+
+def _exact_attention(s, case):
+    B, T, Tk, H, G = case["B"], case["T"], case["Tk"], case["H"], case["H"] // case["Hkv"]
+    if B * H * T * Tk > 5e8:
+        return None
+    scale = s["scale"]
+    q, k, v = (s[n].double().transpose(1, 2) for n in ("q", "k", "v"))
+    k, v = (x.repeat_interleave(G, dim=1) for x in (k, v))
+    logits = scale * (q @ k.mT)
+    rows, keys = torch.arange(T, device="cuda").view(1, 1, T, 1), torch.arange(Tk, device="cuda").view(1, 1, 1, Tk)
+    n = (torch.full((B,), T, device="cuda") if s["q_len"] is None else s["q_len"]).view(B, 1, 1, 1)
+    m = (torch.full((B,), Tk, device="cuda") if s["k_len"] is None else s["k_len"]).view(B, 1, 1, 1)
+    hidden = (rows >= n) | (keys >= m)
+    if case["causal"]:
+        hidden = hidden | (keys - m > rows - n)
+    logits.masked_fill_(hidden, -math.inf)
+    lse = torch.logsumexp(logits, -1)
+    p = torch.softmax(logits, -1)
+    p.masked_fill_(hidden, 0.0)                       # rows that see nothing
+    if case["op"] == "attention":
+        return dict(o=(p @ v).transpose(1, 2).contiguous(), lse=lse)
+    do = s["do"].double().transpose(1, 2)
+    dp = do @ v.mT
+    ds = scale * p * (dp - (p * dp).sum(-1, keepdim=True))
+    share = lambda x: x.view(B, case["Hkv"], G, Tk, -1).sum(2).transpose(1, 2).contiguous()  # noqa: E731
+    return dict(dq=(ds @ k).transpose(1, 2).contiguous(), dk=share(ds.mT @ q), dv=share(p.mT @ do))
+
+
+def _exact_adamw_one(s, i):
+    t = s["t"]
+    w, g = t["param"][i].double(), t["grad"][i].double() * GRAD_SCALE
+    m, v = t["m"][i].double(), t["v"][i].double()
+    n = w.numel()
+
+    def spread(scale):                                # a value for each block as one for each element
+        return scale.double().repeat_interleave(BLOCK)[:n]
+
+    def in_8_bits(x):
+        """Codes and scales: x over its unit lies between two whole numbers; the dither says which."""
+        whole = x.new_zeros(-(-n // BLOCK) * BLOCK)
+        whole[:n] = x.abs()
+        scale = whole.view(-1, BLOCK).max(1).values / FP8_MAX
+        y = x.abs() / spread(scale).clamp(min=1e-300)
+        unit = 2.0 ** (y.clamp(min=2.0 ** -6).log2().floor() - 3)
+        h = (torch.arange(n, device="cuda") * 0x6A09E667 + STEP * 0x9E3779B1) % 2 ** 32 // 256
+        low, rest = (y / unit).floor(), (y / unit) % 1
+        code = unit * (low + (rest + h / 2.0 ** 24 >= 1))
+        return torch.sign(x) * code.clamp(max=FP8_MAX).maximum(torch.where(y > 0, 2.0 ** -9, 0.0)), scale
+
+    if "m_scale" in t:
+        m = m * spread(t["m_scale"][i])
+        v = (v * spread(t["v_scale"][i])) ** 2
+    m, v = m + (1 - BETA1) * (g - m), v + (1 - BETA2) * (g * g - v)
+    change = (m / (1 - BETA1 ** STEP)) / ((v / (1 - BETA2 ** STEP)) ** 0.5 + ADAM_EPS) + s["decay"][i] * w
+    w = w - LR * change
+    if "m_scale" not in t:
+        return w, m, v
+    (mc, ms), (vc, vs) = in_8_bits(m), in_8_bits(v ** 0.5)
+    return w, mc, vc, ms, vs
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    if case["op"].startswith("layer_norm"):
+        return _exact_norm(s, case)
+    if case["op"] != "adamw":
+        return _exact_attention(s, case)
+    parts = list(zip(*(_exact_adamw_one(s, i) for i in range(len(s["sizes"])))))
+    names = ("param", "m", "v", "m_scale", "v_scale")
+    out = {k: torch.cat(part) for k, part in zip(names, parts)}
+    return dict(out, copy=out["param"] if case["copy"] else None)
