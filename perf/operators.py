@@ -291,10 +291,10 @@ def _plain_attention_grad(s, case):
     lse = torch.where(torch.isinf(s["lse"]), torch.zeros_like(s["lse"]), s["lse"])
     p = scores.sub_(lse[..., None]).exp_()
     do, v = _heads(s["do"], case["Hkv"]), _heads(s["v"], case["Hkv"])
-    delta = (s["do"].float() * s["o"].float()).sum(-1).permute(0, 2, 1)
     p = p.reshape(*q.shape[:4], case["Tk"])
     dv = torch.matmul(p.transpose(-1, -2), do).sum(2)
-    ds = torch.matmul(do, v.transpose(-1, -2)).sub_(delta.reshape(*q.shape[:4], 1)).mul_(p).mul_(s["scale"])
+    ds = torch.matmul(do, v.transpose(-1, -2))
+    ds = ds.sub_((p * ds).sum(-1, keepdim=True)).mul_(p).mul_(s["scale"])
     dk = torch.matmul(ds.transpose(-1, -2), q).sum(2)
     dq = torch.matmul(ds, k).reshape(case["B"], case["H"], case["T"], case["D"])
     back = lambda x: x.permute(0, 2, 1, 3).to(s["q"].dtype).contiguous()  # noqa: E731
