@@ -200,7 +200,7 @@ def _prepare_adamw(case, gen):
         s["m_scale"], s["v_scale"] = (torch.empty(sum(blocks), device="cuda") for _ in range(2))
         s["t"] = {k: list(s[k].split(blocks)) for k in ("m_scale", "v_scale")}
         list(map(_encode, m, s["m"].split(sizes), s["t"]["m_scale"], [STEP - 1] * len(sizes)))
-        list(map(_encode, map(torch.sqrt, v), s["v"].split(sizes), s["t"]["v_scale"], [STEP - 1] * len(sizes)))
+        list(map(_encode, map(torch.sqrt, v), s["v"].split(sizes), s["t"]["v_scale"], [STEP - 1] * len(sizes), [True] * len(sizes)))
     s["t"] |= {k: list(s[k].split(sizes)) for k in ("param", "grad", "m", "v", "copy") if s[k] is not None}
     # weights decay, biases and norms do not
     s["decay"] = [DECAY if case["stack"] == "shard" or len(shape) == 2 else 0.0 for shape in _stack_shapes(case["d"], case["n"])][:len(sizes)]
@@ -317,14 +317,18 @@ def _dither(n, step):
     return (h >> 8).float() * 2.0 ** -24
 
 
-def _encode(x, code, scale, step):
+def _encode(x, code, scale, step, of_square=False):
     """Values in 8 bits (sign, 4 bits of exponent, 3 of fraction) in units of their block's largest / 448, rounded up where
-    the rest is above one minus the dither, so that an average's small changes are not lost; not to zero from above it."""
+    the rest is above one minus the dither, so that an average's small changes are not lost; not to zero from above it.
+    of_square: the square is the average, and its rest is what counts."""
     b = _blocked(x)
     scale.copy_(b.abs().amax(1) / FP8_MAX)
     a = b.abs() / torch.where(scale > 0, scale, 1)[:, None]
     unit = torch.ldexp(torch.ones_like(a), (torch.frexp(a).exponent - 1).clamp(min=-6) - 3)
-    c = (a / unit + _blocked(_dither(x.numel(), step))).floor() * unit
+    a_units = a / unit
+    low = a_units.floor()
+    rest = (a_units - low) * (a_units + low) / (2 * low + 1) if of_square else a_units - low
+    c = (low + (rest + _blocked(_dither(x.numel(), step))).floor()) * unit
     c = torch.where(a > 0, c.clamp(2.0 ** -9, FP8_MAX), 0.0) * b.sign()
     code.copy_(c.reshape(-1)[:x.numel()])
 
@@ -341,7 +345,7 @@ def _plain_adamw_one(decay, param, grad, m, v, copy, m_scale, v_scale):
         v.copy_(v32)
     else:                                             # the second state's root is what is kept in 8 bits
         _encode(m32, m, m_scale, STEP)
-        _encode(v32.sqrt(), v, v_scale, STEP)
+        _encode(v32.sqrt(), v, v_scale, STEP, True)
     if copy is not None:
         copy.copy_(param)
 
@@ -488,7 +492,7 @@ def _exact_adamw_one(s, i):
     def spread(scale):                                # a value for each block as one for each element
         return scale.double().repeat_interleave(BLOCK)[:n]
 
-    def in_8_bits(x):
+    def in_8_bits(x, power):
         """Codes and scales: x over its unit lies between two whole numbers; the dither says which."""
         whole = x.new_zeros(-(-n // BLOCK) * BLOCK)
         whole[:n] = x.abs()
@@ -496,7 +500,8 @@ def _exact_adamw_one(s, i):
         y = x.abs() / spread(scale).clamp(min=1e-300)
         unit = 2.0 ** (y.clamp(min=2.0 ** -6).log2().floor() - 3)
         h = (torch.arange(n, device="cuda") * 0x6A09E667 + STEP * 0x9E3779B1) % 2 ** 32 // 256
-        low, rest = (y / unit).floor(), (y / unit) % 1
+        low = (y / unit).floor()
+        rest = ((y / unit) ** power - low ** power) / ((low + 1) ** power - low ** power)
         code = unit * (low + (rest + h / 2.0 ** 24 >= 1))
         return torch.sign(x) * code.clamp(max=FP8_MAX).maximum(torch.where(y > 0, 2.0 ** -9, 0.0)), scale
 
@@ -508,7 +513,7 @@ def _exact_adamw_one(s, i):
     w = w - LR * change
     if "m_scale" not in t:
         return w, m, v
-    (mc, ms), (vc, vs) = in_8_bits(m), in_8_bits(v ** 0.5)
+    (mc, ms), (vc, vs) = in_8_bits(m, 1), in_8_bits(v ** 0.5, 2)
     return w, mc, vc, ms, vs
 
 
