@@ -403,6 +403,120 @@ dp_status dp_clipped_grad_launches(const dp_layer* layers, int n_layers, dp_dtyp
 int64_t dp_ghost_tile_order(int T, int B, int32_t* sample, int32_t* token_row0, int32_t* token_col0,
                             int32_t* slot, int64_t capacity);
 
+/*
+ * What stands around the linear layers in a private training step: layer norms, whose gain and bias are clipped per sample as the
+ * linear layers' weights are; attention; and the optimizer that takes the private gradient.  Sums and statistics are fp32; what is
+ * stored in 16 bits is rounded once, to nearest even.
+ */
+
+/*
+ * Layer norm over the last axis:  y = (s - mean) * rstd * gain + bias,  rstd = 1 / sqrt(var + eps),  with s = x + add where a
+ * residual stream goes through (its sum is written, and normalised as written), else s = x.
+ *   x, y       device, [B, T, d] of type dt; any d from 1 to 32768 (wider: DP_ERR_UNSUPPORTED)
+ *   add, sum   device, [B, T, d] of type dt, both or neither NULL; sum may be x or add
+ *   gain, bias device, [d] fp32, or NULL: ones, zeros
+ *   mean, rstd device, [B * T] fp32, kept for the backward pass, or NULL
+ * The [B, T, d] arrays are 16-byte aligned; eps >= 0.
+ */
+dp_status dp_layer_norm(const void* x, const void* add, dp_dtype dt, int B, int T, int d, const float* gain, const float* bias,
+                        float eps, void* sum, void* y, float* mean, float* rstd, void* stream);
+
+/*
+ * Backward pass of dp_layer_norm, with h = (x - mean) * rstd and u = dy * gain:
+ *   dx = (u - mean_d(u) - h * mean_d(u h)) * rstd  (+ add: the gradient that reaches x beside the norm),
+ *   kept[i] = (sum_t dy h, sum_t dy): sample i's gradients of gain and bias, [B, 2, d] fp32,
+ *   sqnorm_out[i] = ||kept[i]||^2, one more row of sqnorm.
+ * Once the clip factors are known, dp_clipped_bias_grad(kept, B, 2 * d, C, grad, ...) adds the clipped gradients up, gain's
+ * and bias's one behind the other, as for biases.  (Without clipping: B = 1 and T = all rows give the plain sum in kept.)
+ *   x          what was normalised (dp_layer_norm's sum, where there was one)
+ *   dx         may be dy or add; NULL: not wanted (then add is NULL too)
+ *   kept, sqnorm_out   both or neither NULL
+ *   ws         device scratch, >= dp_layer_norm_workspace_bytes(...), 16-byte aligned; not used without kept
+ */
+size_t dp_layer_norm_workspace_bytes(dp_dtype dt, int B, int T, int d);
+dp_status dp_layer_norm_backward(const void* x, const void* dy, const void* add, dp_dtype dt, int B, int T, int d, const float* gain,
+                                 const float* mean, const float* rstd, void* dx, float* kept, float* sqnorm_out, void* ws,
+                                 size_t ws_bytes, void* stream);
+
+/*
+ * Attention of Tq queries over Tk keys, H heads of width D:  o_i = sum_j p_ij v_j,  p_ij = exp(scale q_i . k_j - lse_i)
+ * over the keys j that row i sees, lse_i = log sum_j exp(scale q_i . k_j).
+ *   Heads: H_kv divides H; query heads h share key head h / (H / H_kv).
+ *   Layout: element strides of sample, token and head, for q, k, v and o; columns are adjacent.  Packed projections ([B, T, 3 * H * D] and
+ *     the like) need no copies.  Strides are >= 0 and, for 16-bit types, multiples of 8; a token stride is from D to 2^23 (of one
+ *     token: whatever).
+ *   Lengths: q_len[b] queries and k_len[b] keys of sample b are there (device, [B] int32; NULL: all; values are held to 0 .. T).
+ *     What lies behind them is not read.
+ *   causal = 1: the ends are aligned; row i sees keys up to i + (keys there) - (queries there).
+ * Rows that see no key, and rows that are not there, are zeros, with lse = -infinity.  What a row does not see does not reach
+ * it, infinities and NaN included.
+ * D is at most 128 and, for 16-bit types, a multiple of 8.  16-bit types run on the matrix cores, with probabilities rounded to the
+ * type before their product with v; DP_F32 runs on the vector units, for small networks.  scale is positive and finite.
+ */
+typedef struct {
+  int32_t B, H, H_kv, Tq, Tk, D;
+  int32_t causal;
+  float scale;
+  int64_t q_stride[3], k_stride[3], v_stride[3], o_stride[3];   /* sample, token, head */
+  const int32_t* q_len;
+  const int32_t* k_len;
+} dp_attention_shape;
+
+/*
+ *   shape     HOST
+ *   q, k, v, o   device, of type dt, 16-byte aligned
+ *   lse       device, [B, H, Tq] fp32, kept for the backward pass
+ */
+dp_status dp_attention(const dp_attention_shape* shape, dp_dtype dt, const void* q, const void* k, const void* v, void* o, float* lse,
+                       void* stream);
+
+/*
+ * Backward pass, which forms the probabilities again from lse:
+ *   dv_j = sum_i p_ij do_i,  ds_ij = p_ij (do_i . v_j - do_i . o_i),  dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,
+ * dk and dv summed over the query heads that share a key head.  Every element of dq, dk and dv that the shape reaches is written (zeros
+ * where a row is not there); p and ds are rounded to the type before their products (16-bit types).
+ *   o, lse    dp_attention's;  dout  the gradient of o, in o's strides
+ *   dq, dk, dv   in the strides of q, k and v; they do not overlap each other nor an input
+ *   ws        device scratch, >= dp_attention_backward_workspace_bytes(...), 16-byte aligned
+ */
+size_t dp_attention_backward_workspace_bytes(const dp_attention_shape* shape, dp_dtype dt);
+dp_status dp_attention_backward(const dp_attention_shape* shape, dp_dtype dt, const void* q, const void* k, const void* v,
+                                const void* o, const float* lse, const void* dout, void* dq, void* dk, void* dv, void* ws,
+                                size_t ws_bytes, void* stream);
+
+/*
+ * One AdamW step over many tensors (for a rank that holds one shard of the flattened gradient: one tensor), in place:
+ *   g = grad_scale * grad;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2;
+ *   param = param (1 - lr * weight_decay) - lr * m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps).
+ * grad_scale is what the sum over samples of the private gradient lacks: 1 over the (expected) batch size.
+ *   tensors     HOST array; param fp32 [n]; grad [n] of type grad_dt; n = 0: nothing to do.  Elements need no more than their own
+ *               alignment; where all of a tensor's arrays are aligned to four elements they are moved four at a time.
+ *   state_bits  32: m and v are fp32 [n].
+ *               8: m and the root of v are e4m3 numbers (sign, 4 bits of exponent, 3 of fraction; largest 448), one byte each [n], in units of
+ *               m_scale and v_scale, fp32 [ceil(n / 256)]: the largest magnitude of each 256 values, over 448.  A value is
+ *               rounded up where its place between its neighbours (v's: between their squares) is at least 1 - f, f the fractional part of e (sqrt(2) - 1) + step (golden ratio - 1) for
+ *               element e (in 32-bit integers: (e * 0x6A09E667 + step * 0x9E3779B1) >> 8, over 2^24), so that slow averages do
+ *               move; one above zero is not rounded to zero.  All-zero bytes and scales are zero states.
+ *               An infinite or undefined state makes those of its 256 undefined.
+ *   copy_dt     DP_BF16 or DP_F16: the new param is also written to copy [n], rounded to nearest even; DP_F32: copy is not used
+ *   step        counts from 1
+ * Tensors travel in kernel arguments, up to 128 to a launch.
+ */
+typedef struct {
+  float* param;
+  const void* grad;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  void* copy;
+  uint64_t n;
+  float weight_decay;
+  int32_t reserved;
+} dp_adamw_tensor;
+dp_status dp_adamw_multi(const dp_adamw_tensor* tensors, int n_tensors, dp_dtype grad_dt, int state_bits, dp_dtype copy_dt, double lr,
+                         double beta1, double beta2, double eps, double grad_scale, uint64_t step, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

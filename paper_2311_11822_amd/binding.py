@@ -34,6 +34,17 @@ class dp_layer(C.Structure):
                 ("d_out", C.c_int32), ("path", C.c_int32)]
 
 
+class dp_attention_shape(C.Structure):
+    _fields_ = [*((k, C.c_int32) for k in ("B", "H", "H_kv", "Tq", "Tk", "D", "causal")), ("scale", C.c_float),
+                *((k, C.c_int64 * 3) for k in ("q_stride", "k_stride", "v_stride", "o_stride")), ("q_len", C.c_void_p),
+                ("k_len", C.c_void_p)]
+
+
+class dp_adamw_tensor(C.Structure):
+    _fields_ = [*((k, C.c_void_p) for k in ("param", "grad", "m", "v", "m_scale", "v_scale", "copy")), ("n", C.c_uint64),
+                ("weight_decay", C.c_float), ("reserved", C.c_int32)]
+
+
 _vp, _i, _f, _u64, _sz = C.c_void_p, C.c_int, C.c_float, C.c_uint64, C.c_size_t
 _PROTOS = {
     "dp_status_string": (C.c_char_p, [_i]),
@@ -70,6 +81,14 @@ _PROTOS = {
                                       C.POINTER(_u64), _i, _u64, _u64, _f, _u64, _u64, _vp, _vp, _vp, _sz, _i, _vp]),
     "dp_clipped_grad_tile_order": (C.c_int64, [_i, _i, _vp, _vp, C.c_int64]),
     "dp_clipped_grad_launches": (_i, [_vp, _i, _i, _i, _i, _vp]),
+    "dp_layer_norm": (_i, [_vp, _vp, _i, _i, _i, _i, _vp, _vp, _f, _vp, _vp, _vp, _vp, _vp]),
+    "dp_layer_norm_workspace_bytes": (_sz, [_i, _i, _i, _i]),
+    "dp_layer_norm_backward": (_i, [_vp, _vp, _vp, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "dp_attention": (_i, [C.POINTER(dp_attention_shape), _i, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "dp_attention_backward_workspace_bytes": (_sz, [C.POINTER(dp_attention_shape), _i]),
+    "dp_attention_backward": (_i, [C.POINTER(dp_attention_shape), _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "dp_adamw_multi": (_i, [C.POINTER(dp_adamw_tensor), _i, _i, _i, _i, C.c_double, C.c_double, C.c_double, C.c_double, C.c_double,
+                           _u64, _vp]),
     "dp_ghost_tile_order": (C.c_int64, [_i, _i, _vp, _vp, _vp, _vp, C.c_int64]),
 }
 EXPORTS = tuple(_PROTOS)
@@ -122,7 +141,8 @@ def _check(status: int, where: str) -> None:
 
 def _call(name: str, *args) -> None:
     """Library call `name`; device pointers as tensors, addresses or None, host arrays as ctypes arrays, the stream last."""
-    status = getattr(_pycall, name)(*args) if _pycall else None
+    native = getattr(_pycall, name, None)
+    status = native(*args) if native else None
     if status is None:                     # something that the native conversion leaves to ctypes
         fn = getattr(lib, name)
         status = fn(*[_ptr(x) if t is _vp else x for x, t in zip(args[:-1], fn.argtypes)],
@@ -303,6 +323,50 @@ def dp_layerwise_clipped_grad(layers, dt, B, R, mode, stability, grads, grad_off
         offs = grad_offset if isinstance(grad_offset, C.Array) else (C.c_uint64 * len(grad_offset))(*grad_offset)
     _call("dp_layerwise_clipped_grad", arr, len(arr), dt, B, _f32(R), mode, stability, gp, offs, accumulate, shard_offset,
           shard_count, sigma, seed, step, sqnorm_out, C_out, ws, _nbytes(ws), layers_per_pass, stream)
+
+
+def dp_layer_norm(x, add, dt, B, T, d, gain, bias, eps, sum, y, mean, rstd, stream=None) -> None:
+    _call("dp_layer_norm", x, add, dt, B, T, d, gain, bias, eps, sum, y, mean, rstd, stream)
+
+
+def dp_layer_norm_workspace_bytes(dt, B, T, d) -> int:
+    return lib.dp_layer_norm_workspace_bytes(dt, B, T, d)
+
+
+def dp_layer_norm_backward(x, dy, add, dt, B, T, d, gain, mean, rstd, dx, kept, sqnorm_out, ws, stream=None) -> None:
+    _call("dp_layer_norm_backward", x, dy, add, dt, B, T, d, gain, mean, rstd, dx, kept, sqnorm_out, ws, _nbytes(ws), stream)
+
+
+def attention_shape(B, H, H_kv, Tq, Tk, D, causal, scale, q_stride, k_stride, v_stride, o_stride, q_len=None, k_len=None):
+    """Strides: (sample, token, head), in elements.  The lengths are held by address: they live as long as the shape is used."""
+    three = C.c_int64 * 3
+    return dp_attention_shape(B, H, H_kv, Tq, Tk, D, int(causal), scale, three(*q_stride), three(*k_stride), three(*v_stride),
+                              three(*o_stride), _ptr(q_len), _ptr(k_len))
+
+
+def dp_attention(shape, dt, q, k, v, o, lse, stream=None) -> None:
+    _call("dp_attention", C.byref(shape), dt, q, k, v, o, lse, stream)
+
+
+def dp_attention_backward_workspace_bytes(shape, dt) -> int:
+    return lib.dp_attention_backward_workspace_bytes(C.byref(shape), dt)
+
+
+def dp_attention_backward(shape, dt, q, k, v, o, lse, dout, dq, dk, dv, ws, stream=None) -> None:
+    _call("dp_attention_backward", C.byref(shape), dt, q, k, v, o, lse, dout, dq, dk, dv, ws, _nbytes(ws), stream)
+
+
+def adamw_tensors(tensors: Sequence) -> "C.Array[dp_adamw_tensor]":
+    """tensors: sequence of (param, grad, m, v, m_scale, v_scale, copy, n, weight_decay)."""
+    arr = (dp_adamw_tensor * len(tensors))()
+    for k, (*arrays, n, decay) in enumerate(tensors):
+        arr[k] = dp_adamw_tensor(*[_ptr(x) for x in arrays], n, decay, 0)
+    return arr
+
+
+def dp_adamw_multi(tensors, grad_dt, state_bits, copy_dt, lr, beta1, beta2, eps, grad_scale, step, stream=None) -> None:
+    arr = tensors if isinstance(tensors, C.Array) else adamw_tensors(tensors)
+    _call("dp_adamw_multi", arr, len(arr), grad_dt, state_bits, copy_dt, lr, beta1, beta2, eps, grad_scale, step, stream)
 
 
 def dp_clipped_grad_tile_order(d_in: int, d_out: int):

@@ -1,0 +1,168 @@
+"""What stands around the linear layers of a transformer block in a private training step: layer norm, attention and the
+optimizer.  Each object holds what a program keeps from step to step (parameters, layouts, workspaces) and checks the
+tensors that it is given; all arithmetic is the library's."""
+from __future__ import annotations
+
+from typing import Optional, Sequence
+
+import torch
+
+from . import binding as dp
+
+_TYPES = {torch.float32: dp.DP_F32, torch.bfloat16: dp.DP_BF16, torch.float16: dp.DP_F16}
+
+
+def _dtype(x: torch.Tensor) -> int:
+    if x.dtype not in _TYPES:
+        raise TypeError(f"float32, bfloat16 or float16, not {x.dtype}")
+    return _TYPES[x.dtype]
+
+
+def _same(name: str, x: Optional[torch.Tensor], shape, dtype, device) -> None:
+    if x is not None and (tuple(x.shape) != tuple(shape) or x.dtype != dtype or x.device != device or not x.is_contiguous()):
+        raise ValueError(f"{name}: contiguous {tuple(shape)} of {dtype} on {device}, not {tuple(x.shape)} of {x.dtype} on {x.device}")
+
+
+class LayerNorm:
+    """gain, bias: [d] float32, or None (ones, zeros)."""
+
+    def __init__(self, gain: Optional[torch.Tensor], bias: Optional[torch.Tensor], eps: float = 1e-5):
+        self.gain, self.bias, self.eps = gain, bias, eps
+        self._ws = {}                  # by shape and stream: calls on different streams do not share a workspace
+
+    def _check(self, x, others, floats):
+        if x.dim() != 3 or not x.is_contiguous():
+            raise ValueError("x: contiguous [B, T, d]")
+        B, T, d = x.shape
+        for name, p in (("gain", self.gain), ("bias", self.bias)):
+            _same(name, p, (d,), torch.float32, x.device)
+        for name, t in others:
+            _same(name, t, x.shape, x.dtype, x.device)
+        for name, t, shape in floats:
+            if t is not None and (t.numel() != shape or t.dtype != torch.float32 or t.device != x.device or not t.is_contiguous()):
+                raise ValueError(f"{name}: {shape} contiguous float32 values on {x.device}")
+        return _dtype(x), B, T, d
+
+    def forward(self, x, y, mean=None, rstd=None, add=None, sum=None, stream=None) -> None:
+        """x, y: [B, T, d]; mean, rstd: [B, T], kept for backward; add: joins x before the norm, the sum goes to `sum`."""
+        dt, B, T, d = self._check(x, (("y", y), ("add", add), ("sum", sum)), (("mean", mean, x.shape[0] * x.shape[1]),
+                                                                            ("rstd", rstd, x.shape[0] * x.shape[1])))
+        dp.dp_layer_norm(x, add, dt, B, T, d, self.gain, self.bias, self.eps, sum, y, mean, rstd, stream)
+
+    def backward(self, x, dy, mean, rstd, dx, kept=None, sqnorm=None, add=None, stream=None) -> None:
+        """dx: [B, T, d] or None; kept: [B, 2, d], per-sample gradients of gain and bias, and sqnorm: [B], their squared norms;
+        add: the gradient that reaches x beside the norm."""
+        rows = x.shape[0] * x.shape[1]
+        dt, B, T, d = self._check(x, (("dy", dy), ("dx", dx), ("add", add)),
+                                  (("mean", mean, rows), ("rstd", rstd, rows), ("kept", kept, 2 * x.shape[0] * x.shape[2]),
+                                   ("sqnorm", sqnorm, x.shape[0])))
+        ws, stream = None, dp._stream(stream)
+        if kept is not None:
+            key = (dt, B, T, d, x.device, stream)
+            ws = self._ws.get(key)
+            if ws is None:
+                n = dp.dp_layer_norm_workspace_bytes(dt, B, T, d)
+                if n == 0:
+                    raise dp.DpError(dp.DP_ERR_UNSUPPORTED, "dp_layer_norm_workspace_bytes")
+                ws = self._ws[key] = torch.empty(n, dtype=torch.uint8, device=x.device)
+        dp.dp_layer_norm_backward(x, dy, add, dt, B, T, d, self.gain, mean, rstd, dx, kept, sqnorm, ws, stream)
+
+    @staticmethod
+    def clipped_gradient(kept, C, grad, accumulate=0, stream=None) -> None:
+        """grad: [2, d] float32, gain's and bias's, (+)= sum_i C[i] kept[i]."""
+        _same("grad", grad, kept.shape[1:], torch.float32, kept.device)
+        dp.dp_clipped_bias_grad(kept, kept.shape[0], kept[0].numel(), C, grad, accumulate, stream)
+
+
+class Attention:
+    """The layout of attention calls, from tensors as they will be given: q [B, Tq, H, D], k and v [B, Tk, H_kv, D], o [B, Tq, H, D],
+    views of packed projections among them.  q_len, k_len: [B] int32 on the device, or None."""
+
+    def __init__(self, q, k, v, o, causal: bool, scale: float, q_len=None, k_len=None):
+        self.device, self.dtype, self.dt = q.device, q.dtype, _dtype(q)
+        if q.dim() != 4 or k.dim() != 4:
+            raise ValueError("q, k: four axes")
+        B, Tq, H, D = q.shape
+        Tk, H_kv = k.shape[1:3]
+        for name, n in (("q_len", q_len), ("k_len", k_len)):
+            _same(name, n, (B,), torch.int32, q.device)
+        self.q_len, self.k_len = q_len, k_len             # held: the shape has their addresses
+        self.layout = {"q": (tuple(q.shape), q.stride()), "k": ((B, Tk, H_kv, D), k.stride()), "v": ((B, Tk, H_kv, D), v.stride()),
+                       "o": (tuple(q.shape), o.stride())}
+        self.rows = (B, H, Tq)
+        for name, t in (("q", q), ("k", k), ("v", v), ("o", o)):
+            self._check(name, t, name)
+            if t.shape[3] > 1 and t.stride(3) != 1:
+                raise ValueError(f"{name}: columns of a head are adjacent")
+        # an axis of one entry has whatever stride; none is needed of it
+        strides = [[st if n > 1 else 0 for n, st in zip(t.shape[:3], t.stride()[:3])] for t in (q, k, v, o)]
+        self.shape = dp.attention_shape(B, H, H_kv, Tq, Tk, D, causal, scale, *strides, q_len, k_len)
+        self._ws = {}
+
+    def _check(self, name, t, like):
+        shape, strides = self.layout[like]
+        if t.dtype != self.dtype or t.device != self.device or tuple(t.shape) != shape or t.stride() != strides:
+            raise ValueError(f"{name}: {shape} in strides {strides}, {self.dtype} on {self.device}")
+
+    def _check_lse(self, lse):
+        _same("lse", lse, self.rows, torch.float32, self.device)
+
+    def forward(self, q, k, v, o, lse, stream=None) -> None:
+        """o in its strides; lse: [B, H, Tq] float32, kept for backward."""
+        for name, t in (("q", q), ("k", k), ("v", v), ("o", o)):
+            self._check(name, t, name)
+        self._check_lse(lse)
+        dp.dp_attention(self.shape, self.dt, q, k, v, o, lse, stream)
+
+    def backward(self, q, k, v, o, lse, do, dq, dk, dv, stream=None) -> None:
+        """do in o's strides; dq, dk, dv in those of q, k and v."""
+        for name, t, like in (("q", q, "q"), ("k", k, "k"), ("v", v, "v"), ("o", o, "o"), ("do", do, "o"), ("dq", dq, "q"),
+                              ("dk", dk, "k"), ("dv", dv, "v")):
+            self._check(name, t, like)
+        self._check_lse(lse)
+        stream = dp._stream(stream)
+        ws = self._ws.get(stream)
+        if ws is None:                                    # calls on different streams do not share a workspace
+            n = dp.dp_attention_backward_workspace_bytes(self.shape, self.dt)
+            if n == 0:
+                raise dp.DpError(dp.DP_ERR_UNSUPPORTED, "dp_attention_backward_workspace_bytes")
+            ws = self._ws[stream] = torch.empty(n, dtype=torch.uint8, device=self.device)
+        dp.dp_attention_backward(self.shape, self.dt, q, k, v, o, lse, do, dq, dk, dv, ws, stream)
+
+
+class AdamW:
+    """Lists of tensors that are updated together.  param: float32; grad: one type; m, v: float32, or torch.float8_e4m3fn with m_scale and
+    v_scale ([ceil(n / 256)] float32; v then holds roots); copy: 16-bit tensors that take the new parameters, or None; decay: a
+    factor for each tensor, or one for all.  The tensors are held: their addresses go to the library."""
+
+    def __init__(self, param: Sequence, grad: Sequence, m: Sequence, v: Sequence, decay, copy: Optional[Sequence] = None,
+                 m_scale: Optional[Sequence] = None, v_scale: Optional[Sequence] = None):
+        n = len(param)
+        decay = [float(decay)] * n if isinstance(decay, (int, float)) else list(decay)
+        if n == 0 or any(len(x) != n for x in (grad, m, v, decay)) or any(x is not None and len(x) != n for x in (copy, m_scale, v_scale)):
+            raise ValueError("lists of one length, of a tensor at least")
+        self.bits = 8 if m[0].dtype == torch.float8_e4m3fn else 32
+        if self.bits == 8 and (m_scale is None or v_scale is None):
+            raise ValueError("8-bit states have scales")
+        state = torch.float8_e4m3fn if self.bits == 8 else torch.float32
+        self.grad_dt = _dtype(grad[0])
+        self.copy_dt = _dtype(copy[0]) if copy is not None else dp.DP_F32
+        if copy is not None and self.copy_dt == dp.DP_F32:
+            raise TypeError("copy: 16-bit tensors")
+        device = param[0].device
+        none = [None] * n
+        self.held = list(zip(param, grad, m, v, m_scale if self.bits == 8 else none, v_scale if self.bits == 8 else none,
+                             copy if copy is not None else none))
+        kinds = (torch.float32, grad[0].dtype, state, state, torch.float32, torch.float32, copy[0].dtype if copy is not None else None)
+        for tensors in self.held:
+            size = tensors[0].numel()
+            for k, (name, t, kind) in enumerate(zip(("param", "grad", "m", "v", "m_scale", "v_scale", "copy"), tensors, kinds)):
+                want = -(-size // 256) if k in (4, 5) else size
+                if t is not None and (t.dtype != kind or t.device != device or t.numel() != want or not t.is_contiguous()):
+                    raise ValueError(f"{name}: contiguous, {want} values of {kind} on {device}")
+        self.tensors = dp.adamw_tensors([(*tensors, tensors[0].numel(), d) for tensors, d in zip(self.held, decay)])
+
+    def step(self, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, grad_scale: float = 1.0,
+             stream=None) -> None:
+        """step counts from 1; grad_scale: what makes the gradient's sum over samples a mean."""
+        dp.dp_adamw_multi(self.tensors, self.grad_dt, self.bits, self.copy_dt, lr, beta1, beta2, eps, grad_scale, step, stream)

@@ -1,0 +1,351 @@
+// What the attention kernels share: arguments, the order of their workgroups, key and value tiles on their way into LDS, and the
+// row-wise form in fp32.
+//
+// Operands on the matrix cores.  A wave holds its 32 rows of one side (queries; in the key gradients, keys) as the second
+// operand in registers, and the tiles of the other side go through LDS.  A product's 32 x 32 result has that side's index in
+// the register (8 (r / 4) + 4 (lane / 32) + r % 4) and the wave's own row in the lane (lane % 32), so that
+//  * a softmax over keys is a reduction within a lane and one exchange between its halves, and maxima, sums and their
+//    corrections are one value a lane;
+//  * sixteen such values, rounded to 16 bits, are the second operand of the next product as they lie: lane half h holds
+//    rows 4 h .. 4 h + 3 and 8 + 4 h .. 8 + 4 h + 3 of every 16.  A sum does not care for its order, so the first operand is
+//    read in the same one (two transposing LDS reads, of rows 4 h and 8 + 4 h on), and no probability passes through LDS.
+//
+// LDS holds rows of a head (DP columns of 16 bits) as they come from memory, 16-byte chunks XOR-swizzled by row such that eight
+// rows' reads of one column and the transposing reads of four rows fall on different banks.
+#pragma once
+
+#include "dp_internal.h"
+#include "lds_dma.h"
+
+namespace dpbk {
+
+struct AttnSide {                 // element strides of sample, token and head
+  int64_t sample, token, head;
+};
+
+struct AttnArgs {
+  const void *q, *k, *v, *o, *dout;
+  void *out, *dq, *dk, *dv;
+  float* lse;                     // [B, H, Tq]
+  float *lse2, *delta;            // backward: lse in units of log 2 (+inf: the row counts for nothing), rows' sums of do * o
+  const int32_t *q_len, *k_len;   // [B] or null
+  int B, H, H_kv, share;          // share: query heads to a key head
+  int Tq, Tk, D;
+  int causal;
+  float scale, scale2;            // scale2: scale * log2(e)
+  AttnSide qs, ks, vs, os;
+  int heads, blocks;              // of the launch: (sample, head) pairs and their blocks of rows
+  int spread;                     // 1: a pair's blocks on one XCD
+  unsigned first;                 // number of the launch's first workgroup
+};
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+template <int DP>
+struct HeadTile {
+  static constexpr int CHUNKS = DP / 8, ROW_BYTES = 2 * DP;
+  __device__ static unsigned swizzle(unsigned row) {
+    return DP == 128 ? (row & 7) << 1 : DP == 64 ? row & 6 : (row >> 2) & 3;
+  }
+};
+
+// Valid rows of sample b: a length beyond the tensor's, or below zero, counts as the nearest that is none.
+__device__ __forceinline__ int valid_rows(const int32_t* len, int b, int T) { return len ? min(max(len[b], 0), T) : T; }
+
+// (sample and head, block) of workgroup id.  With `spread` the blocks of a pair go to one XCD (id % 8), whose L2 then holds its
+// keys and values; ids past the last pair come out at or past a.heads.
+__device__ __forceinline__ void attn_unit(const AttnArgs& a, unsigned id, int& pair, int& block) {
+  if (a.spread) {
+    const unsigned i = id >> 3;
+    pair = (int)(i / (unsigned)a.blocks * 8 + (id & 7));
+    block = (int)(i % (unsigned)a.blocks);
+  } else {
+    pair = (int)(id / (unsigned)a.blocks);
+    block = (int)(id % (unsigned)a.blocks);
+  }
+  pair = __builtin_amdgcn_readfirstlane(pair);    // (the divisions run on the vector side)
+  block = __builtin_amdgcn_readfirstlane(block);
+}
+
+// ROWS rows of a head from memory to LDS, one 16-byte chunk a lane and load, NW waves.  Rows past the descriptor's size and columns from D on
+// arrive as zeros.
+template <int DP, int ROWS, int NW>
+struct TileLoader {
+  static constexpr int CHUNKS = HeadTile<DP>::CHUNKS, LOADS = ROWS * CHUNKS / (64 * NW);
+  static_assert(LOADS * 64 * NW == ROWS * CHUNKS, "whole loads");
+  unsigned off[LOADS];
+  uint64_t base;
+  unsigned row_bytes;
+  __device__ __forceinline__ void init(const void* head, int64_t token_stride, int D, int wave, int lane) {
+    base = reinterpret_cast<uint64_t>(head);
+    row_bytes = (unsigned)(2 * token_stride);
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const unsigned id = (i * NW + wave) * 64 + lane, row = id / CHUNKS, chunk = (id % CHUNKS) ^ HeadTile<DP>::swizzle(row);
+      off[i] = (int)chunk * 8 < D ? row * row_bytes + chunk * 16 : OOB;
+    }
+  }
+  // Rows row0 .. row0 + ROWS - 1 of which those below `end` are there.
+  __device__ __forceinline__ void load(int row0, int end, unsigned lds, int wave) const {
+    i32x4 r = make_rsrc(reinterpret_cast<const void*>(base + (uint64_t)row0 * row_bytes), min(max(end - row0, 0), ROWS) * row_bytes);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) r[i] = __builtin_amdgcn_readfirstlane(r[i]);
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) load_to_lds(r, off[i], 0, lds + (i * NW + wave) * 1024);
+  }
+};
+
+// All loads into LDS issued so far have landed, here and (after the barrier) in the other waves.
+__device__ __forceinline__ void tiles_landed() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// Operand of rows row0 + lane % 32 (row0: a multiple of 32), columns 16 ks + 8 (lane / 32) .. + 7.
+template <int DP>
+__device__ __forceinline__ bf16x8 read_rows(unsigned lds, int row0, int ks, int lane) {
+  const unsigned row = lane & 31, chunk = (2 * ks + (lane >> 5)) ^ HeadTile<DP>::swizzle(row);
+  return *(__attribute__((address_space(3))) const bf16x8*)(uintptr_t)(lds + row0 * HeadTile<DP>::ROW_BYTES +
+                                                                      row * HeadTile<DP>::ROW_BYTES + chunk * 16);
+}
+
+// Transposed operand: columns 32 cb + lane % 32, rows row0 + 4 h .. + 3 and row0 + 8 + 4 h .. + 3 with h = lane / 32.
+template <int DP>
+__device__ __forceinline__ bf16x8 read_columns(unsigned lds, int row0, int cb, int lane) {
+  const int s = lane & 15, blk = lane >> 4;
+  const unsigned row = 4 * (blk >> 1) + (s >> 2), chunk = 4 * cb + 2 * (blk & 1) + ((s & 3) >> 1);
+  Frag f;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    f.h[i] = lds_read_tr(lds + row0 * HeadTile<DP>::ROW_BYTES + (row + 8 * i) * HeadTile<DP>::ROW_BYTES +
+                         (chunk ^ HeadTile<DP>::swizzle(row + 8 * i)) * 16 + 8 * (s & 1));
+  return f.v;
+}
+
+// The wave's own operand from memory: row `row` (zeros where !there), columns 16 ks + 8 (lane / 32) .. + 7.
+template <int DP>
+__device__ __forceinline__ void load_own(bf16x8 (&f)[DP / 16], const uint16_t* head, int64_t token_stride, int row, bool there,
+                                         int D, int lane) {
+#pragma unroll
+  for (int ks = 0; ks < DP / 16; ++ks) {
+    const int col = 16 * ks + 8 * (lane >> 5);
+    uint4 w = make_uint4(0, 0, 0, 0);
+    if (there && col < D) w = *reinterpret_cast<const uint4*>(head + row * token_stride + col);
+    f[ks] = __builtin_bit_cast(bf16x8, w);
+  }
+}
+
+// Eight values rounded to nearest even.
+template <bool F16>
+__device__ __forceinline__ bf16x8 round8(const f32x16& x, int first) {
+  if constexpr (F16) {
+    f16x8 y;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = (_Float16)x[first + i];
+    return __builtin_bit_cast(bf16x8, y);
+  } else {
+    bf16x8 y;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = (__bf16)x[first + i];
+    return y;
+  }
+}
+
+// The other half's value (lane ^ 32).
+__device__ __forceinline__ float other_half(float x, int lane) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(lane < 32 ? r[1] : r[0]);
+}
+
+__device__ __forceinline__ f32x16 zeros16() {
+  f32x16 z;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) z[r] = 0.f;
+  return z;
+}
+
+// A 32-row result (columns by register, the wave's rows by lane) times f, rounded, to memory: four columns of a row are eight bytes.
+// Rows with there == false get zeros; rows from `rows` on are not in the tensor.
+template <bool F16, int DP>
+__device__ __forceinline__ void store_rows16(const f32x16 (&acc)[DP / 32], float f, bool there, uint16_t* head, int64_t token_stride,
+                                             int row, int rows, int D, int lane) {
+  if (row >= rows) return;
+  uint16_t* p = head + row * token_stride;
+#pragma unroll
+  for (int cb = 0; cb < DP / 32; ++cb)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int col = 32 * cb + 8 * g + 4 * (lane >> 5);
+      uint16_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = there ? acc[cb][4 * g + i] * f : 0.f;
+        w[i] = F16 ? __builtin_bit_cast(uint16_t, (_Float16)x) : __builtin_bit_cast(uint16_t, (__bf16)x);
+      }
+      if (col < D) *reinterpret_cast<uint2*>(p + col) = make_uint2(w[0] | (uint32_t)w[1] << 16, w[2] | (uint32_t)w[3] << 16);
+    }
+}
+
+// Whether some value is an infinity or no number.
+template <int N>
+__device__ __forceinline__ bool not_finite(const f32x16 (&acc)[N]) {
+  float t = 0.f;
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) t = fmaf(acc[n][r], 0.f, t);
+  return t != 0.f;
+}
+
+// ---- One row by one wave, in fp32 throughout: what the 32-bit type runs on, and what a 16-bit row is formed by again where a value that
+// it does not see (a later token's, under a causal mask) is an infinity or no number and has spoilt its tile's products.
+// A lane takes one of 64 keys for the scores, and columns lane and lane + 64 for the sums.
+
+template <class E>
+__device__ __forceinline__ float widen(E x) {
+  return (float)x;
+}
+template <class E>
+__device__ __forceinline__ E narrow(float x) {
+  return (E)x;
+}
+
+template <class E>
+__device__ __forceinline__ float dot_rows(const E* x, const E* y, int D) {
+  float s = 0.f;
+  for (int d = 0; d < D; ++d) s = fmaf(widen(x[d]), widen(y[d]), s);
+  return s;
+}
+
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) x = fmaxf(x, __shfl_xor(x, off));
+  return x;
+}
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off);
+  return x;
+}
+
+// acc += sum_j w_j rows[j], j < n <= 64 (w_j in lane j).
+template <class E>
+__device__ __forceinline__ void add_rows(float (&acc)[2], float w, const E* rows, int64_t stride, int n, int D, int lane) {
+  for (int j = 0; j < n; ++j) {
+    const float wj = __shfl(w, j);
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+      if (lane + 64 * c < D) acc[c] = fmaf(wj, widen(rows[j * stride + lane + 64 * c]), acc[c]);
+  }
+}
+
+template <class E>
+__device__ __forceinline__ void store_row(const float (&acc)[2], float f, E* row, int D, int lane) {
+#pragma unroll
+  for (int c = 0; c < 2; ++c)
+    if (lane + 64 * c < D) row[lane + 64 * c] = narrow<E>(acc[c] * f);
+}
+
+template <class E>
+struct AttnRows {
+  const AttnArgs& a;
+  int b, h, lane, n_q, n_k;
+  __device__ AttnRows(const AttnArgs& args, int b_, int h_, int lane_) : a(args), b(b_), h(h_), lane(lane_) {
+    n_q = valid_rows(a.q_len, b, a.Tq);
+    n_k = valid_rows(a.k_len, b, a.Tk);
+  }
+  __device__ const E* query(const void* t, const AttnSide& s, int head) const { return (const E*)t + b * s.sample + head * s.head; }
+  __device__ int keys_of(int i) const {         // row i sees keys below this
+    return i >= n_q ? 0 : a.causal ? min(max(i + n_k - n_q + 1, 0), n_k) : n_k;
+  }
+
+  __device__ void forward(int i) const {
+    const E *q = query(a.q, a.qs, h) + i * a.qs.token, *k = query(a.k, a.ks, h / a.share), *v = query(a.v, a.vs, h / a.share);
+    const int n = keys_of(i);
+    float most = -INFINITY, total = 0.f, acc[2] = {0.f, 0.f};
+    for (int j0 = 0; j0 < n; j0 += 64) {
+      const float s = j0 + lane < n ? a.scale2 * dot_rows(q, k + (j0 + lane) * a.ks.token, a.D) : -INFINITY;
+      const float top = fmaxf(most, wave_max(s)), ref = top == -INFINITY ? 0.f : top;
+      const float p = exp2f(s - ref), fix = exp2f(most - ref);
+      most = top;
+      total = total * fix + wave_sum(p);
+#pragma unroll
+      for (int c = 0; c < 2; ++c) acc[c] *= fix;
+      add_rows(acc, p, v + j0 * a.vs.token, a.vs.token, min(64, n - j0), a.D, lane);
+    }
+    store_row(acc, total != 0.f ? 1.f / total : 0.f, (E*)a.out + b * a.os.sample + h * a.os.head + i * a.os.token, a.D, lane);
+    if (lane == 0) a.lse[((int64_t)b * a.H + h) * a.Tq + i] = total != 0.f ? most * kLn2 + logf(total) : -INFINITY;
+  }
+
+  // Probability and its gradient of one (query, key) pair.
+  __device__ void pair(const E* q, const E* dout, const E* k, const E* v, float lse2, float delta, float& p, float& ds) const {
+    p = exp2f(fmaf(a.scale2, dot_rows(q, k, a.D), -lse2));
+    ds = p * (dot_rows(dout, v, a.D) - delta);
+  }
+
+  __device__ void query_gradient(int i) const {
+    const E *q = query(a.q, a.qs, h) + i * a.qs.token, *k = query(a.k, a.ks, h / a.share), *v = query(a.v, a.vs, h / a.share);
+    const E *dout = query(a.dout, a.os, h) + i * a.os.token, *o = query(a.o, a.os, h) + i * a.os.token;
+    const int n = keys_of(i);
+    const int64_t at = ((int64_t)b * a.H + h) * a.Tq + i;
+    const float lse = a.lse[at], lse2 = n == 0 || lse == -INFINITY ? INFINITY : lse * kLog2e;
+    const float delta = n == 0 ? 0.f : dot_rows(dout, o, a.D);
+    float acc[2] = {0.f, 0.f};
+    for (int j0 = 0; j0 < n; j0 += 64) {
+      float p = 0.f, ds = 0.f;
+      if (j0 + lane < n) pair(q, dout, k + (j0 + lane) * a.ks.token, v + (j0 + lane) * a.vs.token, lse2, delta, p, ds);
+      add_rows(acc, ds, k + j0 * a.ks.token, a.ks.token, min(64, n - j0), a.D, lane);
+    }
+    store_row(acc, a.scale, (E*)a.dq + b * a.qs.sample + h * a.qs.head + i * a.qs.token, a.D, lane);
+    if (lane == 0) {
+      a.lse2[at] = lse2;
+      a.delta[at] = delta;
+    }
+  }
+
+  // h: a key head.
+  __device__ void key_gradient(int j) const {
+    const E *k = query(a.k, a.ks, h) + j * a.ks.token, *v = query(a.v, a.vs, h) + j * a.vs.token;
+    float dk[2] = {0.f, 0.f}, dv[2] = {0.f, 0.f};
+    const int from = a.causal ? max(j - (n_k - n_q), 0) : 0;
+    for (int hq = h * a.share; j < n_k && hq < (h + 1) * a.share; ++hq) {
+      const E *q = query(a.q, a.qs, hq), *dout = query(a.dout, a.os, hq);
+      const int64_t at = ((int64_t)b * a.H + hq) * a.Tq;
+      for (int i0 = from; i0 < n_q; i0 += 64) {
+        float p = 0.f, ds = 0.f;
+        const int i = i0 + lane;
+        if (i < n_q) pair(q + i * a.qs.token, dout + i * a.os.token, k, v, a.lse2[at + i], a.delta[at + i], p, ds);
+        add_rows(dv, p, dout + i0 * a.os.token, a.os.token, min(64, n_q - i0), a.D, lane);
+        add_rows(dk, ds, q + i0 * a.qs.token, a.qs.token, min(64, n_q - i0), a.D, lane);
+      }
+    }
+    store_row(dk, a.scale, (E*)a.dk + b * a.ks.sample + h * a.ks.head + j * a.ks.token, a.D, lane);
+    store_row(dv, 1.f, (E*)a.dv + b * a.vs.sample + h * a.vs.head + j * a.vs.token, a.D, lane);
+  }
+};
+
+template <bool F16>
+struct Half {
+  typedef __bf16 T;
+};
+template <>
+struct Half<true> {
+  typedef _Float16 T;
+};
+
+// Launches `blocks` of a.heads pairs, in runs below the grid's limit.
+template <class K>
+dp_status launch_attention(K kernel, AttnArgs a, int threads, int lds, hipStream_t s) {
+  // A pair's blocks stay on one XCD where the pairs fill the eight of them (padded up to a multiple of eight).
+  a.spread = a.blocks > 1 && (a.heads % 8 == 0 || a.heads >= 64);
+  const int64_t n = (int64_t)(a.spread ? (a.heads + 7) / 8 * 8 : a.heads) * a.blocks;
+  return launch_in_runs(n, [&](dim3 grid, int first) {
+    AttnArgs run = a;
+    run.first = (unsigned)first;
+    hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, s, run);
+  });
+}
+
+dp_status launch_attention_forward(const AttnArgs& a, dp_dtype dt, hipStream_t s);
+dp_status launch_attention_backward(const AttnArgs& a, dp_dtype dt, hipStream_t s);
+
+}  // namespace dpbk

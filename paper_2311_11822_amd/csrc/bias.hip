@@ -7,6 +7,7 @@
 #include <type_traits>
 
 #include "dp_internal.h"
+#include "train.h"
 
 namespace dpbk {
 
@@ -327,6 +328,12 @@ dp_status launch_bias_norm(const void* g, dp_dtype dt, int B, int T, int p, floa
   if (hipGetLastError() != hipSuccess) return DP_ERR_HIP;
   hipLaunchKernelGGL(bias_sqnorm_kernel, dim3(B), dim3(kSqThreads), 0, s, colsum, p, sqnorm_out);
   return hip_status(hipGetLastError());
+}
+
+dp_status launch_row_sqnorm(const float* rows, int B, int p, float* sqnorm, hipStream_t s) {
+  return launch_in_runs(B, [&](dim3 grid, int first) {
+    hipLaunchKernelGGL(bias_sqnorm_kernel, grid, dim3(kSqThreads), 0, s, rows + (size_t)first * p, p, sqnorm + first);
+  });
 }
 
 dp_status launch_clipped_bias_grad(const float* colsum, int B, int p, const float* C, float* grad_b,

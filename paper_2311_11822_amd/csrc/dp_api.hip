@@ -417,7 +417,7 @@ const char* dp_status_string(dp_status s) {
   return "unknown status";
 }
 
-int dp_version(void) { return 100; }
+int dp_version(void) { return 200; }
 
 dp_path dp_choose_path(int64_t T, int64_t d_in, int64_t d_out) {
   if (T <= 0 || d_in <= 0 || d_out <= 0) return DP_PATH_GHOST;
