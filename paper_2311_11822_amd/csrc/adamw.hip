@@ -9,9 +9,14 @@
 // parts of multiples of sqrt(2) - 1 and of the golden ratio, in 32-bit integers.  The root's rest is taken between the squares of its
 // neighbours, so that v is rounded without a bias (between the roots themselves v came out 3.5 % too large after 2000 steps with beta2 =
 // 0.999).  A value above zero is not rounded to zero: m / sqrt(v) stays bounded.
+//
+// Every operation is rounded on its own, none fused: what is computed is defined to the bit (a code at the edge of its dither does not
+// depend on how a compiler fuses, and plain fp32 code elsewhere reproduces a step).
 #include <type_traits>
 
 #include "train.h"
+
+#pragma clang fp contract(off)
 
 namespace dpbk {
 
@@ -124,7 +129,7 @@ __device__ __forceinline__ uint32_t encode(const float (&x)[4], const float (&di
   for (int i = 0; i < 4; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off));
-  scale = __uint_as_float(top) / 448.f;
+  scale = __uint_as_float(top) * (1.f / 448.f);
   const float unit = scale > 0.f ? scale : 1.f;
   float c[4];
 #pragma unroll
@@ -172,7 +177,7 @@ struct Block {
       m[i] = a.beta1 * m[i] + a.rest1 * gi;
       v[i] = a.beta2 * v[i] + a.rest2 * gi * gi;
       root[i] = sqrtf(v[i]);
-      w[i] = w[i] * t.keep - a.step_size * m[i] / (root[i] * a.root_scale + a.eps);
+      w[i] = w[i] * t.keep - a.lr * (m[i] * a.fix1 / (sqrtf(v[i] * a.fix2) + a.eps));
     }
     store4<VEC>(w, t.param, at, lane, left);
     if constexpr (COPY != DP_F32) {

@@ -61,10 +61,6 @@ __global__ void __launch_bounds__(64 * NW, 2) attention_query_grad_kernel(const 
     if (lse2 == -INFINITY) lse2 = INFINITY;
   }
   if (lane_end == 0) delta = 0.f;
-  if (lane < 32 && row < a.Tq) {
-    a.lse2[at] = lse2;
-    a.delta[at] = delta;
-  }
 
   f32x16 dq[DP / 32];
 #pragma unroll
@@ -78,21 +74,46 @@ __global__ void __launch_bounds__(64 * NW, 2) attention_query_grad_kernel(const 
     }
     if (j0 >= own_end) continue;
     const bool mask = j0 + kKeys > (a.causal ? min(n_k, own0 + shift + 1) : n_k);
+    // Probabilities and do v' of 32 keys.
+    auto products = [&](int kb, f32x16& p, f32x16& dp) {
+      p = dp = zeros16();
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      f32x16 s = zeros16(), dp = zeros16();
-#pragma unroll
-      for (int ks = 0; ks < DP / 16; ++ks) s = mfma16<F16>(read_rows<DP>(kt, 32 * kb, ks, lane), qf[ks], s);
+      for (int ks = 0; ks < DP / 16; ++ks) p = mfma16<F16>(read_rows<DP>(kt, 32 * kb, ks, lane), qf[ks], p);
 #pragma unroll
       for (int ks = 0; ks < DP / 16; ++ks) dp = mfma16<F16>(read_rows<DP>(vt, 32 * kb, ks, lane), df[ks], dp);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale2, -lse2)) * (dp[r] - delta);
-      if (mask) {                                 // a select: what is not seen may be no number
-        const int seen = lane_end - j0 - 32 * kb - 4 * (lane >> 5);
+      for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(p[r], a.scale2, -lse2));
+    };
+    auto hide = [&](int kb, f32x16& x) {          // a select: what is not seen may be no number
+      const int seen = lane_end - j0 - 32 * kb - 4 * (lane >> 5);
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (8 * (r >> 2) + (r & 3) >= seen) s[r] = 0.f;
+      for (int r = 0; r < 16; ++r)
+        if (8 * (r >> 2) + (r & 3) >= seen) x[r] = 0.f;
+    };
+    if (own_end <= kKeys) {
+      // All that these rows see is at hand: delta from the probabilities, free of o's rounding, which counts where few keys share a
+      // row (2-norm of dq's error against 64 bits, fp16, 18 x 591 tokens: 3.1e-4 with o's alone).
+      float sum = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        f32x16 p, dp;
+        products(kb, p, dp);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) p[r] *= dp[r];
+        hide(kb, p);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum += p[r];
       }
+      sum += other_half(sum, lane);
+      if (lane_end > 1) delta = sum;
+    }
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      f32x16 s, dp;
+      products(kb, s, dp);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] *= dp[r] - delta;
+      if (mask) hide(kb, s);
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) {
         const bf16x8 ds = round8<F16>(s, 8 * ks);
@@ -100,6 +121,10 @@ __global__ void __launch_bounds__(64 * NW, 2) attention_query_grad_kernel(const 
         for (int cb = 0; cb < DP / 32; ++cb) dq[cb] = mfma16<F16>(read_columns<DP>(kt, 32 * kb + 16 * ks, cb, lane), ds, dq[cb]);
       }
     }
+  }
+  if (lane < 32 && row < a.Tq) {
+    a.lse2[at] = lse2;
+    a.delta[at] = delta;
   }
   store_rows16<F16, DP>(dq, a.scale, lane_end > 0, static_cast<uint16_t*>(a.dq) + b * a.qs.sample + h * a.qs.head, a.qs.token, row,
                         a.Tq, a.D, lane);

@@ -45,7 +45,7 @@ struct AdamArgs {
   int n_tensors;
   unsigned first;                        // number of the launch's first workgroup
   float grad_scale, beta1, beta2, rest1, rest2;      // rest: 1 - beta
-  float step_size, root_scale, eps;      // lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
+  float lr, fix1, fix2, eps;             // fix: 1 / (1 - beta^t)
   uint32_t dither;                       // step * 0x9E3779B1
   unsigned begin[kAdamTensors];          // first workgroup of a tensor
   AdamTensor t[kAdamTensors];

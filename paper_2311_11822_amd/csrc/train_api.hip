@@ -194,8 +194,9 @@ dp_status dp_adamw_multi(const dp_adamw_tensor* tensors, int n_tensors, dp_dtype
   a.beta2 = (float)beta2;
   a.rest1 = (float)(1. - beta1);
   a.rest2 = (float)(1. - beta2);
-  a.step_size = (float)(lr / (1. - pow(beta1, (double)step)));
-  a.root_scale = (float)(1. / sqrt(1. - pow(beta2, (double)step)));
+  a.lr = (float)lr;
+  a.fix1 = 1.f / (float)(1. - pow(beta1, (double)step));
+  a.fix2 = 1.f / (float)(1. - pow(beta2, (double)step));
   a.eps = (float)eps;
   a.dither = (uint32_t)step * 0x9E3779B1u;
   int64_t blocks = 0;
