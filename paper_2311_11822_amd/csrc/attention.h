@@ -27,7 +27,7 @@ struct AttnArgs {
   const void *q, *k, *v, *o, *dout;
   void *out, *dq, *dk, *dv;
   float* lse;                     // [B, H, Tq]
-  float *lse2, *delta;            // backward: lse in units of log 2 (+inf: the row counts for nothing), rows' sums of do * o
+  float *lse2, *delta;            // backward, [B, H, Tq]: lse in units of log 2 (+inf: the row counts for nothing), and -delta
   const int32_t *q_len, *k_len;   // [B] or null
   int B, H, H_kv, share;          // share: query heads to a key head
   int Tq, Tk, D;
@@ -44,8 +44,10 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f
 template <int DP>
 struct HeadTile {
   static constexpr int CHUNKS = DP / 8, ROW_BYTES = 2 * DP;
+  // A 128-bit read takes sixteen lanes at a time, rows of sixteen different row % 16 here, and a transposing one four rows of 64 bytes: the
+  // first must differ in all of row % 16 that one line of the banks holds, the second in the 64-byte group.
   __device__ static unsigned swizzle(unsigned row) {
-    return DP == 128 ? (row & 7) << 1 : DP == 64 ? row & 6 : (row >> 2) & 3;
+    return DP == 128 ? (row & 3) << 2 | ((row >> 2) & 3) : DP == 64 ? (row & 2) << 1 | ((row >> 2) & 3) : (row >> 2) & 3;
   }
 };
 
@@ -53,16 +55,14 @@ struct HeadTile {
 __device__ __forceinline__ int valid_rows(const int32_t* len, int b, int T) { return len ? min(max(len[b], 0), T) : T; }
 
 // (sample and head, block) of workgroup id.  With `spread` the blocks of a pair go to one XCD (id % 8), whose L2 then holds its
-// keys and values; ids past the last pair come out at or past a.heads.
+// keys and values; ids past the last pair come out at or past a.heads.  Every other pair has its blocks in the opposite order:
+// workgroups go to compute units in turn, and under a causal mask a unit would otherwise get the longest block of every pair.
 __device__ __forceinline__ void attn_unit(const AttnArgs& a, unsigned id, int& pair, int& block) {
-  if (a.spread) {
-    const unsigned i = id >> 3;
-    pair = (int)(i / (unsigned)a.blocks * 8 + (id & 7));
-    block = (int)(i % (unsigned)a.blocks);
-  } else {
-    pair = (int)(id / (unsigned)a.blocks);
-    block = (int)(id % (unsigned)a.blocks);
-  }
+  const unsigned i = a.spread ? id >> 3 : id;
+  const int turn = (int)(i / (unsigned)a.blocks);
+  pair = a.spread ? turn * 8 + (int)(id & 7) : turn;
+  block = (int)(i % (unsigned)a.blocks);
+  if (turn & 1) block = a.blocks - 1 - block;
   pair = __builtin_amdgcn_readfirstlane(pair);    // (the divisions run on the vector side)
   block = __builtin_amdgcn_readfirstlane(block);
 }
@@ -71,8 +71,10 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, unsigned id, int& p
 // arrive as zeros.
 template <int DP, int ROWS, int NW>
 struct TileLoader {
-  static constexpr int CHUNKS = HeadTile<DP>::CHUNKS, LOADS = ROWS * CHUNKS / (64 * NW);
-  static_assert(LOADS * 64 * NW == ROWS * CHUNKS, "whole loads");
+  static constexpr int CHUNKS = HeadTile<DP>::CHUNKS, WAVE_LOADS = ROWS * CHUNKS / 64, LOADS = (WAVE_LOADS + NW - 1) / NW;
+  static_assert(WAVE_LOADS * 64 == ROWS * CHUNKS, "whole loads");
+  // Every wave makes the same number of loads: where they are more than a tile needs, some are made twice.
+  __device__ static int slot(int i, int wave) { return WAVE_LOADS % NW == 0 ? i * NW + wave : (i * NW + wave) % WAVE_LOADS; }
   unsigned off[LOADS];
   uint64_t base;
   unsigned row_bytes;
@@ -81,7 +83,7 @@ struct TileLoader {
     row_bytes = (unsigned)(2 * token_stride);
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      const unsigned id = (i * NW + wave) * 64 + lane, row = id / CHUNKS, chunk = (id % CHUNKS) ^ HeadTile<DP>::swizzle(row);
+      const unsigned id = slot(i, wave) * 64 + lane, row = id / CHUNKS, chunk = (id % CHUNKS) ^ HeadTile<DP>::swizzle(row);
       off[i] = (int)chunk * 8 < D ? row * row_bytes + chunk * 16 : OOB;
     }
   }
@@ -91,35 +93,49 @@ struct TileLoader {
 #pragma unroll
     for (int i = 0; i < 3; ++i) r[i] = __builtin_amdgcn_readfirstlane(r[i]);
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) load_to_lds(r, off[i], 0, lds + (i * NW + wave) * 1024);
+    for (int i = 0; i < LOADS; ++i) load_to_lds(r, off[i], 0, lds + slot(i, wave) * 1024);
   }
 };
 
-// All loads into LDS issued so far have landed, here and (after the barrier) in the other waves.
+// All loads into LDS but the LATER last ones have landed, here and (after the barrier) in the other waves; and every wave is
+// through with its reads so far.
+template <int LATER = 0>
 __device__ __forceinline__ void tiles_landed() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LATER) : "memory");
 }
 
-// Operand of rows row0 + lane % 32 (row0: a multiple of 32), columns 16 ks + 8 (lane / 32) .. + 7.
+// Where in LDS a lane finds its operands of a tile that begins at `lds`, worked out once: a tile elsewhere is a constant in the instruction.
 template <int DP>
-__device__ __forceinline__ bf16x8 read_rows(unsigned lds, int row0, int ks, int lane) {
-  const unsigned row = lane & 31, chunk = (2 * ks + (lane >> 5)) ^ HeadTile<DP>::swizzle(row);
-  return *(__attribute__((address_space(3))) const bf16x8*)(uintptr_t)(lds + row0 * HeadTile<DP>::ROW_BYTES +
-                                                                      row * HeadTile<DP>::ROW_BYTES + chunk * 16);
-}
-
-// Transposed operand: columns 32 cb + lane % 32, rows row0 + 4 h .. + 3 and row0 + 8 + 4 h .. + 3 with h = lane / 32.
-template <int DP>
-__device__ __forceinline__ bf16x8 read_columns(unsigned lds, int row0, int cb, int lane) {
-  const int s = lane & 15, blk = lane >> 4;
-  const unsigned row = 4 * (blk >> 1) + (s >> 2), chunk = 4 * cb + 2 * (blk & 1) + ((s & 3) >> 1);
-  Frag f;
+struct TileReader {
+  static constexpr int KS = DP / 16, CB = DP / 32, ROW_BYTES = HeadTile<DP>::ROW_BYTES;
+  unsigned row_at[KS], column_at[CB][2];
+  __device__ __forceinline__ void init(unsigned lds, int lane) {
+    const unsigned row = lane & 31;
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-    f.h[i] = lds_read_tr(lds + row0 * HeadTile<DP>::ROW_BYTES + (row + 8 * i) * HeadTile<DP>::ROW_BYTES +
-                         (chunk ^ HeadTile<DP>::swizzle(row + 8 * i)) * 16 + 8 * (s & 1));
-  return f.v;
-}
+    for (int ks = 0; ks < KS; ++ks)
+      row_at[ks] = lds + row * ROW_BYTES + ((2 * ks + (lane >> 5)) ^ HeadTile<DP>::swizzle(row)) * 16;
+    const int s = lane & 15, blk = lane >> 4;
+    const unsigned first = 4 * (blk >> 1) + (s >> 2);
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const unsigned chunk = 4 * cb + 2 * (blk & 1) + ((s & 3) >> 1);
+        column_at[cb][i] = lds + (first + 8 * i) * ROW_BYTES + (chunk ^ HeadTile<DP>::swizzle(first + 8 * i)) * 16 + 8 * (s & 1);
+      }
+  }
+  // Rows row0 + lane % 32 (row0: a multiple of 32), columns 16 ks + 8 (lane / 32) .. + 7 of the tile at byte `tile`.
+  __device__ __forceinline__ bf16x8 rows(int tile, int row0, int ks) const {
+    return *(__attribute__((address_space(3))) const bf16x8*)(uintptr_t)(row_at[ks] + tile + row0 * ROW_BYTES);
+  }
+  // Transposed: columns 32 cb + lane % 32, rows row0 + 4 h .. + 3 and row0 + 8 + 4 h .. + 3 with h = lane / 32 (row0: of 16).
+  __device__ __forceinline__ bf16x8 columns(int tile, int row0, int cb) const {
+    Frag f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) f.h[i] = lds_read_tr(column_at[cb][i] + tile + row0 * ROW_BYTES);
+    return f.v;
+  }
+};
 
 // The wave's own operand from memory: row `row` (zeros where !there), columns 16 ks + 8 (lane / 32) .. + 7.
 template <int DP>
@@ -298,7 +314,7 @@ struct AttnRows {
     store_row(acc, a.scale, (E*)a.dq + b * a.qs.sample + h * a.qs.head + i * a.qs.token, a.D, lane);
     if (lane == 0) {
       a.lse2[at] = lse2;
-      a.delta[at] = delta;
+      a.delta[at] = -delta;
     }
   }
 
@@ -313,7 +329,7 @@ struct AttnRows {
       for (int i0 = from; i0 < n_q; i0 += 64) {
         float p = 0.f, ds = 0.f;
         const int i = i0 + lane;
-        if (i < n_q) pair(q + i * a.qs.token, dout + i * a.os.token, k, v, a.lse2[at + i], a.delta[at + i], p, ds);
+        if (i < n_q) pair(q + i * a.qs.token, dout + i * a.os.token, k, v, a.lse2[at + i], -a.delta[at + i], p, ds);
         add_rows(dv, p, dout + i0 * a.os.token, a.os.token, min(64, n_q - i0), a.D, lane);
         add_rows(dk, ds, q + i0 * a.qs.token, a.qs.token, min(64, n_q - i0), a.D, lane);
       }

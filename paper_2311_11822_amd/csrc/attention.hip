@@ -1,18 +1,26 @@
 // Attention, forward: o_i = sum_j p_ij v_j with p_ij = exp(scale q_i k_j - lse_i) over the keys j that row i sees, in one pass over keys and
 // values with a running maximum and sum.
+#include <type_traits>
+
 #include "attention.h"
 
 namespace dpbk {
 
 namespace {
 
+#ifndef FWD_OCC
+#define FWD_OCC(DP) (DP <= 64 ? 3 : 2)
+#endif
+#ifndef FWD_PIPE
+#define FWD_PIPE (DP > 64)
+#endif
 constexpr int kKeys = 64;                         // of a tile
 constexpr float kLazy = 8.f;                      // a maximum may be passed by 2^8 before sums are expressed in a new one
 
-template <bool F16, int DP, int NW>
-__global__ void __launch_bounds__(64 * NW, DP <= 64 && NW == 4 ? 3 : 2) attention_kernel(const AttnArgs a) {
+template <bool F16, int DP, int NW, bool PIPE>
+__global__ void __launch_bounds__(64 * NW, FWD_OCC(DP)) attention_kernel(const AttnArgs a) {
   extern __shared__ __align__(1024) char smem[];
-  constexpr int TILE = kKeys * HeadTile<DP>::ROW_BYTES, STAGE = 2 * TILE;
+  constexpr int TILE = kKeys * HeadTile<DP>::ROW_BYTES;
   int pair, block;
   attn_unit(a, a.first + blockIdx.x, pair, block);
   if (pair >= a.heads) return;
@@ -33,33 +41,45 @@ __global__ void __launch_bounds__(64 * NW, DP <= 64 && NW == 4 ? 3 : 2) attentio
   TileLoader<DP, kKeys, NW> k_tiles, v_tiles;
   k_tiles.init(static_cast<const uint16_t*>(a.k) + b * a.ks.sample + h / a.share * a.ks.head, a.ks.token, a.D, wave, lane);
   v_tiles.init(static_cast<const uint16_t*>(a.v) + b * a.vs.sample + h / a.share * a.vs.head, a.vs.token, a.D, wave, lane);
+  constexpr int KS = DP / 16, CB = DP / 32;
+  constexpr int V = 2 * TILE;                     // two stages of keys, then two of values
   if (end > 0) {
     k_tiles.load(0, n_k, lds, wave);
-    v_tiles.load(0, n_k, lds + TILE, wave);
+    if (PIPE) k_tiles.load(kKeys, n_k, lds + TILE, wave);
+    v_tiles.load(0, n_k, lds + V, wave);
   }
-  bf16x8 qf[DP / 16];
+  bf16x8 qf[KS];
   load_own<DP>(qf, q, a.qs.token, row, row < n_q, a.D, lane);
+  TileReader<DP> read;
+  read.init(lds, lane);
 
-  f32x16 o[DP / 32];
+  f32x16 o[CB];
 #pragma unroll
-  for (int cb = 0; cb < DP / 32; ++cb) o[cb] = zeros16();
+  for (int cb = 0; cb < CB; ++cb) o[cb] = zeros16();
   float most = -3.4028235e38f, total = 0.f;       // of scale2 * score; total: of this half's keys
-  for (int j0 = 0, stage = 0; j0 < end; j0 += kKeys, stage ^= 1) {
-    tiles_landed();
-    const unsigned kt = lds + stage * STAGE, vt = kt + TILE;
-    if (j0 + kKeys < end) {
-      k_tiles.load(j0 + kKeys, n_k, lds + (stage ^ 1) * STAGE, wave);
-      v_tiles.load(j0 + kKeys, n_k, lds + (stage ^ 1) * STAGE + TILE, wave);
-    }
-    if (j0 >= own_end) continue;
-    f32x16 s[2];
+  auto scores = [&](f32x16 (&to)[2], int tile) {
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
-      s[kb] = zeros16();
+      to[kb] = zeros16();
 #pragma unroll
-      for (int ks = 0; ks < DP / 16; ++ks) s[kb] = mfma16<F16>(read_rows<DP>(kt, 32 * kb, ks, lane), qf[ks], s[kb]);
+      for (int ks = 0; ks < KS; ++ks) to[kb] = mfma16<F16>(read.rows(tile, 32 * kb, ks), qf[ks], to[kb]);
     }
-    if (j0 + kKeys > (a.causal ? min(n_k, own0 + shift + 1) : n_k)) {
+  };
+  const int all_see = a.causal ? min(n_k, own0 + shift + 1) : n_k;       // keys that each of the wave's rows sees
+  // One tile, in stage STAGE.  PIPE: s has its scores, and next gets those of the tile behind it (behind the last one: of what LDS holds,
+  // and not used).
+  auto step = [&](f32x16 (&s)[2], f32x16 (&next)[2], int j0, auto stage_tag) {
+    constexpr int STAGE = decltype(stage_tag)::value, HERE = STAGE * TILE, THERE = TILE - HERE;
+    tiles_landed();
+    if (PIPE) {
+      if (j0 + 2 * kKeys < end) k_tiles.load(j0 + 2 * kKeys, n_k, lds + HERE, wave);
+    } else {
+      if (j0 + kKeys < end) k_tiles.load(j0 + kKeys, n_k, lds + THERE, wave);
+    }
+    if (j0 + kKeys < end) v_tiles.load(j0 + kKeys, n_k, lds + V + THERE, wave);
+    if (j0 >= own_end) return;
+    if (!PIPE) scores(s, HERE);
+    if (j0 + kKeys > all_see) {
       const int seen = lane_end - j0 - 4 * (lane >> 5);
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -74,14 +94,15 @@ __global__ void __launch_bounds__(64 * NW, DP <= 64 && NW == 4 ? 3 : 2) attentio
       for (int r = 0; r < 16; ++r) top = fmaxf(top, s[kb][r]);
     top = fmaxf(top, other_half(top, lane)) * a.scale2;
     if (__any(top > most + kLazy)) {
-      const float next = fmaxf(most, top), fix = __builtin_amdgcn_exp2f(most - next);
-      most = next;
+      const float higher = fmaxf(most, top), fix = __builtin_amdgcn_exp2f(most - higher);
+      most = higher;
       total *= fix;
 #pragma unroll
-      for (int cb = 0; cb < DP / 32; ++cb)
+      for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[cb][r] *= fix;
     }
+    if (PIPE) scores(next, THERE);
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -93,7 +114,20 @@ __global__ void __launch_bounds__(64 * NW, DP <= 64 && NW == 4 ? 3 : 2) attentio
     for (int ks = 0; ks < kKeys / 16; ++ks) {
       const bf16x8 p = round8<F16>(s[ks >> 1], 8 * (ks & 1));
 #pragma unroll
-      for (int cb = 0; cb < DP / 32; ++cb) o[cb] = mfma16<F16>(read_columns<DP>(vt, 16 * ks, cb, lane), p, o[cb]);
+      for (int cb = 0; cb < CB; ++cb) o[cb] = mfma16<F16>(read.columns(V + HERE, 16 * ks, cb), p, o[cb]);
+    }
+  };
+  if (end > 0) {
+    f32x16 s[2], t[2];
+    if (PIPE) {
+      tiles_landed();
+      scores(s, 0);                               // (the next barrier says that all waves are through with these keys)
+    }
+    for (int j0 = 0;;) {
+      step(s, t, j0, std::integral_constant<int, 0>{});
+      if ((j0 += kKeys) >= end) break;
+      step(t, s, j0, std::integral_constant<int, 1>{});
+      if ((j0 += kKeys) >= end) break;
     }
   }
   total += other_half(total, lane);
@@ -123,7 +157,7 @@ dp_status launch(AttnArgs a, hipStream_t s) {
   a.heads = a.B * a.H;
   a.blocks = (a.Tq + 32 * NW - 1) / (32 * NW);
   constexpr int LDS = 4 * kKeys * HeadTile<DP>::ROW_BYTES;
-  auto kernel = attention_kernel<F16, DP, NW>;
+  auto kernel = attention_kernel<F16, DP, NW, FWD_PIPE>;
   static ReadyTable done;
   if (LDS > 65536) {
     const dp_status st = allow_big_lds(kernel, LDS, done);
@@ -132,11 +166,14 @@ dp_status launch(AttnArgs a, hipStream_t s) {
   return launch_attention(kernel, a, 64 * NW, LDS, s);
 }
 
+#ifndef FWD_NW
+#define FWD_NW 4
+#endif
 template <bool F16, int DP>
 dp_status launch(const AttnArgs& a, hipStream_t s) {
   if (a.Tq <= 32) return launch<F16, DP, 1>(a, s);
   if (a.Tq <= 64) return launch<F16, DP, 2>(a, s);
-  return launch<F16, DP, 4>(a, s);
+  return launch<F16, DP, FWD_NW>(a, s);
 }
 
 template <bool F16>

@@ -3,18 +3,49 @@
 //   dq_i = scale sum_j ds_ij k_j,   dk_j = scale sum_i ds_ij q_i     (over the query heads that share the key head, too).
 // Two kernels, one that owns queries and one that owns keys, so that every sum has one owner and a fixed order: no atomics, no
 // partial sums in memory.  The price is that scores and do v' are formed in both, seven products for five.
+#include <type_traits>
+
 #include "attention.h"
 
 namespace dpbk {
 
 namespace {
 
-// dq, and for the other kernel delta and lse in units of log 2.
-constexpr int kKeys = 64;
+// Both kernels go through tiles of 32 rows of the other side in a ring of four, more of them on their way while one is worked on.  Up to a
+// width of 64 (PIPE) the scores and do v' of the next tile are formed beside the exponentials of this one.
+constexpr int kRing = 4, kRows = 32;
+
+#ifndef QUERY_OCC
+#define QUERY_OCC(DP) 2
+#define QUERY_PIPE(DP) (DP <= 64)
+#define KEY_OCC(DP) 2
+#define KEY_PIPE(DP) (DP <= 64)
+#define VLDS(DP) (DP == 128)
+#endif
+
+// Calls f with each place in the ring in turn, as a constant, and the tile's number, until it has been called n times.
+template <class F>
+__device__ __forceinline__ void around_the_ring(int n, F f) {
+  for (int t = 0;;) {
+    if (t >= n) break;
+    f(t++, std::integral_constant<int, 0>{});
+    if (t >= n) break;
+    f(t++, std::integral_constant<int, 1>{});
+    if (t >= n) break;
+    f(t++, std::integral_constant<int, 2>{});
+    if (t >= n) break;
+    f(t++, std::integral_constant<int, 3>{});
+  }
+}
+
+// dq, and for the other kernel lse in units of log 2 and delta.
 template <bool F16, int DP, int NW>
-__global__ void __launch_bounds__(64 * NW, 2) attention_query_grad_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(64 * NW, QUERY_OCC(DP)) attention_query_grad_kernel(const AttnArgs a) {
   extern __shared__ __align__(1024) char smem[];
-  constexpr int TILE = kKeys * HeadTile<DP>::ROW_BYTES, STAGE = 2 * TILE;
+  constexpr int KS = DP / 16, CB = DP / 32, TILE = kRows * HeadTile<DP>::ROW_BYTES, STAGE = 2 * TILE;
+  constexpr bool PIPE = QUERY_PIPE(DP);
+  typedef TileLoader<DP, kRows, NW> Loader;
+  constexpr int PER_TILE = 2 * Loader::LOADS;
   int pair, block;
   attn_unit(a, a.first + blockIdx.x, pair, block);
   if (pair >= a.heads) return;
@@ -28,31 +59,25 @@ __global__ void __launch_bounds__(64 * NW, 2) attention_query_grad_kernel(const 
   const int end = row0 >= n_q ? 0 : a.causal ? min(n_k, last + shift + 1) : n_k;
   const int own_end = own0 >= n_q ? 0 : a.causal ? min(n_k, own_last + shift + 1) : n_k;
   const int lane_end = row >= n_q ? 0 : a.causal ? min(n_k, row + shift + 1) : n_k;
+  const int all_see = a.causal ? min(n_k, own0 + shift + 1) : n_k;       // keys that each of the wave's rows sees
 
-  TileLoader<DP, kKeys, NW> k_tiles, v_tiles;
-  k_tiles.init(static_cast<const uint16_t*>(a.k) + b * a.ks.sample + h / a.share * a.ks.head, a.ks.token, a.D, wave, lane);
-  v_tiles.init(static_cast<const uint16_t*>(a.v) + b * a.vs.sample + h / a.share * a.vs.head, a.vs.token, a.D, wave, lane);
-  if (end > 0) {
-    k_tiles.load(0, n_k, lds, wave);
-    v_tiles.load(0, n_k, lds + TILE, wave);
-  }
-  bf16x8 qf[DP / 16], df[DP / 16];
+  bf16x8 qf[KS], df[KS];
   load_own<DP>(qf, static_cast<const uint16_t*>(a.q) + b * a.qs.sample + h * a.qs.head, a.qs.token, row, row < n_q, a.D, lane);
   load_own<DP>(df, static_cast<const uint16_t*>(a.dout) + b * a.os.sample + h * a.os.head, a.os.token, row, row < n_q, a.D, lane);
-  // delta: the diagonal of o do', formed as do v' is: a row that sees one key alone has the same products in both, and zero
-  // gradients of its scores, not what two orders of adding leave.
   float delta = 0.f;
   {
-    bf16x8 of[DP / 16];
+    bf16x8 of[KS];
     load_own<DP>(of, static_cast<const uint16_t*>(a.o) + b * a.os.sample + h * a.os.head, a.os.token, row, row < n_q, a.D, lane);
-    f32x16 od = zeros16();
 #pragma unroll
-    for (int ks = 0; ks < DP / 16; ++ks) od = mfma16<F16>(of[ks], df[ks], od);
+    for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-    for (int r = 0; r < 16; ++r)
-      if (8 * (r >> 2) + 4 * (lane >> 5) + (r & 3) == (lane & 31)) delta = od[r];
-    const float there = other_half(delta, lane);
-    if (((lane >> 2) & 1) != lane >> 5) delta = there;
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (F16)
+          delta = fmaf((float)__builtin_bit_cast(f16x8, df[ks])[i], (float)__builtin_bit_cast(f16x8, of[ks])[i], delta);
+        else
+          delta = fmaf((float)df[ks][i], (float)of[ks][i], delta);
+      }
+    delta += other_half(delta, lane);
   }
   const int64_t at = ((int64_t)b * a.H + h) * a.Tq + row;
   float lse2 = INFINITY;                          // a row that sees nothing
@@ -61,70 +86,90 @@ __global__ void __launch_bounds__(64 * NW, 2) attention_query_grad_kernel(const 
     if (lse2 == -INFINITY) lse2 = INFINITY;
   }
   if (lane_end == 0) delta = 0.f;
+  // The scores of a row that sees one key have no gradient: zero probabilities here, not what two orders of adding leave.
+  const float own_lse2 = lane_end == 1 ? INFINITY : lse2;
 
-  f32x16 dq[DP / 32];
+  Loader k_tiles, v_tiles;
+  k_tiles.init(static_cast<const uint16_t*>(a.k) + b * a.ks.sample + h / a.share * a.ks.head, a.ks.token, a.D, wave, lane);
+  v_tiles.init(static_cast<const uint16_t*>(a.v) + b * a.vs.sample + h / a.share * a.vs.head, a.vs.token, a.D, wave, lane);
+  TileReader<DP> read;
+  read.init(lds, lane);
+  auto load = [&](int tile, int stage) {          // past the last one: nothing, by loads that count
+    const unsigned to = lds + stage * STAGE;
+    k_tiles.load(tile * kRows, n_k, to, wave);
+    v_tiles.load(tile * kRows, n_k, to + TILE, wave);
+  };
+  // Scores, and do v' - delta (the sums begin at -delta).
+  auto products = [&](f32x16& s, f32x16& dp, int stage, const f32x16& begin) {
+    s = zeros16();
+    dp = begin;
 #pragma unroll
-  for (int cb = 0; cb < DP / 32; ++cb) dq[cb] = zeros16();
-  for (int j0 = 0, stage = 0; j0 < end; j0 += kKeys, stage ^= 1) {
-    tiles_landed();
-    const unsigned kt = lds + stage * STAGE, vt = kt + TILE;
-    if (j0 + kKeys < end) {
-      k_tiles.load(j0 + kKeys, n_k, lds + (stage ^ 1) * STAGE, wave);
-      v_tiles.load(j0 + kKeys, n_k, lds + (stage ^ 1) * STAGE + TILE, wave);
+    for (int ks = 0; ks < KS; ++ks) {
+      s = mfma16<F16>(read.rows(stage * STAGE, 0, ks), qf[ks], s);
+      dp = mfma16<F16>(read.rows(stage * STAGE + TILE, 0, ks), df[ks], dp);
     }
-    if (j0 >= own_end) continue;
-    const bool mask = j0 + kKeys > (a.causal ? min(n_k, own0 + shift + 1) : n_k);
-    // Probabilities and do v' of 32 keys.
-    auto products = [&](int kb, f32x16& p, f32x16& dp) {
-      p = dp = zeros16();
+  };
+  auto probability = [&](float s) { return __builtin_amdgcn_exp2f(fmaf(s, a.scale2, -own_lse2)); };
+  auto hide = [&](f32x16& x, int tile) {          // a select: what is not seen may be no number
+    const int seen = lane_end - tile * kRows - 4 * (lane >> 5);
 #pragma unroll
-      for (int ks = 0; ks < DP / 16; ++ks) p = mfma16<F16>(read_rows<DP>(kt, 32 * kb, ks, lane), qf[ks], p);
+    for (int r = 0; r < 16; ++r)
+      if (8 * (r >> 2) + (r & 3) >= seen) x[r] = 0.f;
+  };
+
+  f32x16 dq[CB], s[2], dp[2], begin;
 #pragma unroll
-      for (int ks = 0; ks < DP / 16; ++ks) dp = mfma16<F16>(read_rows<DP>(vt, 32 * kb, ks, lane), df[ks], dp);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(p[r], a.scale2, -lse2));
-    };
-    auto hide = [&](int kb, f32x16& x) {          // a select: what is not seen may be no number
-      const int seen = lane_end - j0 - 32 * kb - 4 * (lane >> 5);
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (8 * (r >> 2) + (r & 3) >= seen) x[r] = 0.f;
-    };
-    if (own_end <= kKeys) {
+  for (int cb = 0; cb < CB; ++cb) dq[cb] = zeros16();
+  const int tiles = (end + kRows - 1) / kRows, own_tiles = (own_end + kRows - 1) / kRows;
+  if (tiles > 0) {
+    load(0, 0);
+    load(1, 1);
+    load(2, 2);
+    tiles_landed<PER_TILE>();
+    if (own_end <= 2 * kRows) {
       // All that these rows see is at hand: delta from the probabilities, free of o's rounding, which counts where few keys share a
-      // row (2-norm of dq's error against 64 bits, fp16, 18 x 591 tokens: 3.1e-4 with o's alone).
+      // row (2-norm of dq's error against 64 bits, fp16, 18 x 591 tokens: 3.1e-4 with o's alone, 3.0e-4 so).
+      products(s[0], dp[0], 0, zeros16());
+      products(s[1], dp[1], 1, zeros16());
       float sum = 0.f;
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        f32x16 p, dp;
-        products(kb, p, dp);
+      for (int k = 0; k < 2; ++k) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) p[r] *= dp[r];
-        hide(kb, p);
+        for (int r = 0; r < 16; ++r) s[k][r] = probability(s[k][r]) * dp[k][r];
+        hide(s[k], k);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sum += p[r];
+        for (int r = 0; r < 16; ++r) sum += s[k][r];
       }
       sum += other_half(sum, lane);
       if (lane_end > 1) delta = sum;
     }
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      f32x16 s, dp;
-      products(kb, s, dp);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] *= dp[r] - delta;
-      if (mask) hide(kb, s);
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        const bf16x8 ds = round8<F16>(s, 8 * ks);
-#pragma unroll
-        for (int cb = 0; cb < DP / 32; ++cb) dq[cb] = mfma16<F16>(read_columns<DP>(kt, 32 * kb + 16 * ks, cb, lane), ds, dq[cb]);
-      }
-    }
+    for (int r = 0; r < 16; ++r) begin[r] = -delta;
+    if (PIPE) products(s[0], dp[0], 0, begin);
   }
+  around_the_ring(tiles, [&](int t, auto stage_tag) {
+    constexpr int HERE = decltype(stage_tag)::value, NEXT = (HERE + 1) % kRing, LOAD = (HERE + 3) % kRing, CUR = PIPE ? HERE % 2 : 0;
+    tiles_landed<PIPE ? PER_TILE : 2 * PER_TILE>();
+    load(t + 3, LOAD);
+    if (t >= own_tiles) return;
+    if (PIPE)
+      products(s[CUR ^ 1], dp[CUR ^ 1], NEXT, begin);
+    else
+      products(s[0], dp[0], HERE, begin);
+    f32x16& x = s[CUR];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[r] = probability(x[r]) * dp[CUR][r];
+    if ((t + 1) * kRows > all_see) hide(x, t);
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      const bf16x8 ds = round8<F16>(x, 8 * ks);
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) dq[cb] = mfma16<F16>(read.columns(HERE * STAGE, 16 * ks, cb), ds, dq[cb]);
+    }
+  });
   if (lane < 32 && row < a.Tq) {
     a.lse2[at] = lse2;
-    a.delta[at] = delta;
+    a.delta[at] = -delta;
   }
   store_rows16<F16, DP>(dq, a.scale, lane_end > 0, static_cast<uint16_t*>(a.dq) + b * a.qs.sample + h * a.qs.head, a.qs.token, row,
                         a.Tq, a.D, lane);
@@ -135,11 +180,13 @@ __global__ void __launch_bounds__(64 * NW, 2) attention_query_grad_kernel(const 
 }
 
 // dk and dv.  A wave owns 32 keys; tiles of queries and their output gradients go through LDS, with lse and delta.
-constexpr int kRows = 64;
 template <bool F16, int DP, int NW>
-__global__ void __launch_bounds__(64 * NW, DP == 128 ? 1 : 2) attention_key_grad_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(64 * NW, KEY_OCC(DP)) attention_key_grad_kernel(const AttnArgs a) {
   extern __shared__ __align__(1024) char smem[];
-  constexpr int TILE = kRows * HeadTile<DP>::ROW_BYTES, STAGE = 2 * TILE + 512;
+  constexpr int KS = DP / 16, CB = DP / 32, TILE = kRows * HeadTile<DP>::ROW_BYTES, STAGE = 2 * TILE + 512;
+  constexpr bool PIPE = KEY_PIPE(DP), V_IN_LDS = VLDS(DP);
+  typedef TileLoader<DP, kRows, NW> Loader;
+  constexpr int PER_TILE = 2 * Loader::LOADS + 2;
   int pair, block;
   attn_unit(a, a.first + blockIdx.x, pair, block);
   if (pair >= a.heads) return;
@@ -150,93 +197,131 @@ __global__ void __launch_bounds__(64 * NW, DP == 128 ? 1 : 2) attention_key_grad
   const unsigned lds = (unsigned)(uintptr_t)DP_LDS(char, smem);
   // Queries from here on see a key of the workgroup, of this wave; and the first that sees the lane's.
   const int begin = a.causal ? max(key0 - shift, 0) & ~31 : 0;
-  const int own_begin = a.causal ? max(own0 - shift, 0) : 0, lane_begin = a.causal ? key - shift : 0;
-  const int tiles = key0 < n_k && begin < n_q ? (n_q - begin + kRows - 1) / kRows : 0;
+  const int own_begin = own0 >= n_k ? INT32_MAX : a.causal ? max(own0 - shift, 0) : 0, lane_begin = a.causal ? key - shift : 0;
+  const int tiles = key0 < n_k && begin < n_q ? (n_q - begin + kRows - 1) / kRows : 0;       // of one query head
 
   const int64_t kv = b * a.ks.sample + h * a.ks.head, vv = b * a.vs.sample + h * a.vs.head;
-  bf16x8 kf[DP / 16], vf[DP / 16];
+  bf16x8 kf[KS], vf[V_IN_LDS ? 1 : KS];
   load_own<DP>(kf, static_cast<const uint16_t*>(a.k) + kv, a.ks.token, key, key < n_k, a.D, lane);
-  load_own<DP>(vf, static_cast<const uint16_t*>(a.v) + vv, a.vs.token, key, key < n_k, a.D, lane);
-  TileLoader<DP, kRows, NW> q_tiles, d_tiles;
+  if constexpr (V_IN_LDS) {
+    // Own keys and values, two sums, scores and their gradients are 224 registers at a width of 128: the values stay in LDS.
+    TileLoader<DP, 32 * NW, NW> own;
+    own.init(static_cast<const uint16_t*>(a.v) + vv, a.vs.token, a.D, wave, lane);
+    own.load(key0, n_k, lds + kRing * STAGE, wave);
+  } else {
+    load_own<DP>(vf, static_cast<const uint16_t*>(a.v) + vv, a.vs.token, key, key < n_k, a.D, lane);
+  }
+  TileReader<DP> read;
+  read.init(lds, lane);
+  const unsigned own_values = kRing * STAGE + wave * (32 * HeadTile<DP>::ROW_BYTES);
+  Loader q_tiles, d_tiles;
   q_tiles.init(static_cast<const uint16_t*>(a.q) + b * a.qs.sample + h * a.share * a.qs.head, a.qs.token, a.D, wave, lane);
   d_tiles.init(static_cast<const uint16_t*>(a.dout) + b * a.os.sample + h * a.share * a.os.head, a.os.token, a.D, wave, lane);
-  const int64_t at = ((int64_t)b * a.H + h * a.share) * a.Tq;
-  auto load = [&](int head, int i0, int stage) {
+  int64_t corr = ((int64_t)b * a.H + h * a.share) * a.Tq;
+  // Tiles of all query heads of the key head, one behind the other; first row of the one that is loaded next.
+  int next_row = begin;
+  auto load = [&](bool more, int stage) {         // !more: nothing, by loads that count
     const unsigned to = lds + stage * STAGE;
-    const uint64_t q_head = 2 * (uint64_t)(head * a.qs.head), d_head = 2 * (uint64_t)(head * a.os.head);
-    TileLoader<DP, kRows, NW> q = q_tiles, d = d_tiles;
-    q.base += q_head;
-    d.base += d_head;
-    q.load(i0, n_q, to, wave);
-    d.load(i0, n_q, to + TILE, wave);
-    if (wave == 0) {                              // 64 values of either, zeros past the tensor's end
-      const unsigned bytes = 4 * min(a.Tq - i0, kRows);
-      const int64_t first = at + (int64_t)head * a.Tq + i0;
-      load_dword_to_lds(make_rsrc(a.lse2 + first, bytes), 4 * lane, to + 2 * TILE);
-      load_dword_to_lds(make_rsrc(a.delta + first, bytes), 4 * lane, to + 2 * TILE + 256);
+    const int end = more ? n_q : 0;
+    q_tiles.load(next_row, end, to, wave);
+    d_tiles.load(next_row, end, to + TILE, wave);
+    const int bytes = more ? 4 * min(a.Tq - next_row, kRows) : 0;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      i32x4 r = make_rsrc((k ? a.delta : a.lse2) + corr + next_row, bytes);
+#pragma unroll
+      for (int i = 0; i < 3; ++i) r[i] = __builtin_amdgcn_readfirstlane(r[i]);
+      load_dword_to_lds(r, 4 * lane, to + 2 * TILE + 256 * k);
+    }
+    next_row += kRows;
+    if (next_row >= n_q) {
+      next_row = begin;
+      q_tiles.base += 2 * a.qs.head;
+      d_tiles.base += 2 * a.os.head;
+      corr += a.Tq;
+    }
+  };
+  const unsigned pairs = lds + 2 * TILE + 16 * (lane >> 5);
+  auto four = [&](int at) { return *(__attribute__((address_space(3))) const f32x4*)(uintptr_t)(pairs + at); };
+  // Scores, and do v' - delta.
+  auto products = [&](f32x16& s, f32x16& dp, int stage) {
+    s = zeros16();
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f32x4 d = four(stage * STAGE + 256 + 32 * g);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) dp[4 * g + i] = d[i];
+    }
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      bf16x8 v;
+      if constexpr (V_IN_LDS)
+        v = read.rows(own_values, 0, ks);
+      else
+        v = vf[ks];
+      s = mfma16<F16>(read.rows(stage * STAGE, 0, ks), kf[ks], s);
+      dp = mfma16<F16>(read.rows(stage * STAGE + TILE, 0, ks), v, dp);
     }
   };
 
-  f32x16 dk[DP / 32], dv[DP / 32];
+  f32x16 dk[CB], dv[CB], s[2], dp[2];
 #pragma unroll
-  for (int cb = 0; cb < DP / 32; ++cb) dk[cb] = dv[cb] = zeros16();
+  for (int cb = 0; cb < CB; ++cb) dk[cb] = dv[cb] = zeros16();
   const int steps = tiles * a.share;
-  int head = 0, i0 = begin;                       // of the tile that is loaded next
-  auto advance = [&] {
-    i0 += kRows;
-    if (i0 >= n_q) {
-      i0 = begin;
-      ++head;
-    }
-  };
   if (steps > 0) {
-    load(0, i0, 0);
-    advance();
-  }
-  int here = begin;                               // first query of the tile at hand
-  for (int step = 0, stage = 0; step < steps; ++step, stage ^= 1) {
-    tiles_landed();
-    const unsigned qt = lds + stage * STAGE, dt = qt + TILE;
-    if (step + 1 < steps) load(head, i0, stage ^ 1);
-    const int i_here = here;
-    here = i0;
-    advance();
-#pragma unroll
-    for (int qb = 0; qb < 2; ++qb) {
-      const int first = i_here + 32 * qb;
-      if (own0 >= n_k || first >= n_q || first + 31 < own_begin) continue;
-      f32x16 s = zeros16(), dp = zeros16();
-#pragma unroll
-      for (int ks = 0; ks < DP / 16; ++ks) s = mfma16<F16>(read_rows<DP>(qt, 32 * qb, ks, lane), kf[ks], s);
-#pragma unroll
-      for (int ks = 0; ks < DP / 16; ++ks) dp = mfma16<F16>(read_rows<DP>(dt, 32 * qb, ks, lane), vf[ks], dp);
-      const auto* lse2 = (__attribute__((address_space(3))) const f32x4*)(uintptr_t)(dt + TILE + 128 * qb + 16 * (lane >> 5));
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const f32x4 l = lse2[2 * g], d = lse2[16 + 2 * g];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          s[4 * g + i] = __builtin_amdgcn_exp2f(fmaf(s[4 * g + i], a.scale2, -l[i]));
-          dp[4 * g + i] = s[4 * g + i] * (dp[4 * g + i] - d[i]);
-        }
-      }
-      if (a.causal && first < own0 + 31 - shift) {
-        const int hidden = lane_begin - first - 4 * (lane >> 5);
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (8 * (r >> 2) + (r & 3) < hidden) s[r] = dp[r] = 0.f;
-      }
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        const bf16x8 p = round8<F16>(s, 8 * ks), ds = round8<F16>(dp, 8 * ks);
-#pragma unroll
-        for (int cb = 0; cb < DP / 32; ++cb) {
-          dv[cb] = mfma16<F16>(read_columns<DP>(dt, 32 * qb + 16 * ks, cb, lane), p, dv[cb]);
-          dk[cb] = mfma16<F16>(read_columns<DP>(qt, 32 * qb + 16 * ks, cb, lane), ds, dk[cb]);
-        }
-      }
+    load(true, 0);
+    load(steps > 1, 1);
+    load(steps > 2, 2);
+    if (PIPE) {
+      tiles_landed<2 * PER_TILE>();
+      products(s[0], dp[0], 0);
     }
   }
+  int first = begin;                              // of the tile at hand
+  around_the_ring(steps, [&](int t, auto stage_tag) {
+    constexpr int HERE = decltype(stage_tag)::value, NEXT = (HERE + 1) % kRing, LOAD = (HERE + 3) % kRing, CUR = PIPE ? HERE % 2 : 0;
+    tiles_landed<PIPE ? PER_TILE : 2 * PER_TILE>();
+    load(t + 3 < steps, LOAD);
+    const int i0 = first;
+    first = first + kRows < n_q ? first + kRows : begin;
+    // Nothing to do where neither this tile nor (PIPE) the next one sees a key of the wave.
+    if ((PIPE ? max(i0, first) : i0) + 31 < own_begin) return;
+    if (PIPE)
+      products(s[CUR ^ 1], dp[CUR ^ 1], NEXT);
+    else
+      products(s[0], dp[0], HERE);
+    f32x16 &p = s[CUR], &ds = dp[CUR];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f32x4 l = four(HERE * STAGE + 32 * g);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = 4 * g + i;
+        p[r] = __builtin_amdgcn_exp2f(fmaf(p[r], a.scale2, -l[i]));
+        ds[r] *= p[r];
+      }
+    }
+    if ((a.causal && i0 < own0 + 31 - shift) || n_k == 1) {
+      // The scores of a row that sees one key have no gradient: every row's of a single key, under the mask the first row's.
+      const int hidden = lane_begin - i0 - 4 * (lane >> 5);
+      const int hidden_ds = n_k == 1 ? INT32_MAX : max(hidden, 1 - shift - i0 - 4 * (lane >> 5));
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int i = 8 * (r >> 2) + (r & 3);
+        p[r] = i < hidden ? 0.f : p[r];
+        ds[r] = i < hidden_ds ? 0.f : ds[r];
+      }
+    }
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      const bf16x8 pr = round8<F16>(p, 8 * ks), dr = round8<F16>(ds, 8 * ks);
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) {
+        dv[cb] = mfma16<F16>(read.columns(HERE * STAGE + TILE, 16 * ks, cb), pr, dv[cb]);
+        dk[cb] = mfma16<F16>(read.columns(HERE * STAGE, 16 * ks, cb), dr, dk[cb]);
+      }
+    }
+  });
   store_rows16<F16, DP>(dk, a.scale, key < n_k, static_cast<uint16_t*>(a.dk) + kv, a.ks.token, key, a.Tk, a.D, lane);
   store_rows16<F16, DP>(dv, 1.f, key < n_k, static_cast<uint16_t*>(a.dv) + vv, a.vs.token, key, a.Tk, a.D, lane);
   if (a.causal && __any(key < n_k && (not_finite(dk) || not_finite(dv)))) {
@@ -267,7 +352,7 @@ template <bool F16, int DP, int NW>
 dp_status launch_queries(AttnArgs a, hipStream_t s) {
   a.heads = a.B * a.H;
   a.blocks = (a.Tq + 32 * NW - 1) / (32 * NW);
-  constexpr int LDS = 4 * kKeys * HeadTile<DP>::ROW_BYTES;
+  constexpr int LDS = kRing * 2 * kRows * HeadTile<DP>::ROW_BYTES;
   auto kernel = attention_query_grad_kernel<F16, DP, NW>;
   static ReadyTable done;
   if (LDS > 65536) {
@@ -281,7 +366,7 @@ template <bool F16, int DP, int NW>
 dp_status launch_keys(AttnArgs a, hipStream_t s) {
   a.heads = a.B * a.H_kv;
   a.blocks = (a.Tk + 32 * NW - 1) / (32 * NW);
-  constexpr int LDS = 2 * (2 * kRows * HeadTile<DP>::ROW_BYTES + 512);
+  constexpr int LDS = kRing * (2 * kRows * HeadTile<DP>::ROW_BYTES + 512) + (VLDS(DP) ? 32 * NW * HeadTile<DP>::ROW_BYTES : 0);
   auto kernel = attention_key_grad_kernel<F16, DP, NW>;
   static ReadyTable done;
   if (LDS > 65536) {
@@ -291,11 +376,17 @@ dp_status launch_keys(AttnArgs a, hipStream_t s) {
   return launch_attention(kernel, a, 64 * NW, LDS, s);
 }
 
+#ifndef QUERY_NW
+#define QUERY_NW 4
+#endif
 template <bool F16, int DP>
 dp_status launch(const AttnArgs& a, hipStream_t s) {
-  const dp_status st = a.Tq <= 32 ? launch_queries<F16, DP, 1>(a, s) : launch_queries<F16, DP, 4>(a, s);
+  const dp_status st = a.Tq <= 32 ? launch_queries<F16, DP, 1>(a, s) : launch_queries<F16, DP, QUERY_NW>(a, s);
   if (st != DP_OK) return st;
-  return a.Tk <= 32 ? launch_keys<F16, DP, 1>(a, s) : launch_keys<F16, DP, 4>(a, s);
+#ifndef KEY_NW
+#define KEY_NW (DP == 128 ? 8 : 4)
+#endif
+  return a.Tk <= 32 ? launch_keys<F16, DP, 1>(a, s) : launch_keys<F16, DP, KEY_NW>(a, s);
 }
 
 template <bool F16>
