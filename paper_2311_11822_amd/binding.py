@@ -22,6 +22,11 @@ try:                               # the same library's calls with native argume
     _pycall.set_array_type(C.Array)
 except ImportError:                # not built, or for another interpreter: every call goes through ctypes
     _pycall = None
+try:                               # likewise what stands around the linear layers
+    from . import _pycall_block
+    _pycall_block.set_array_type(C.Array)
+except ImportError:
+    _pycall_block = None
 
 DP_OK, DP_ERR_INVALID_ARG, DP_ERR_UNSUPPORTED, DP_ERR_WORKSPACE, DP_ERR_HIP = range(5)
 DP_F32, DP_BF16, DP_F16 = 0, 1, 2
@@ -95,8 +100,9 @@ EXPORTS = tuple(_PROTOS)
 for _name, (_res, _args) in _PROTOS.items():
     _fn = getattr(lib, _name)          # AttributeError here = header/library mismatch
     _fn.restype, _fn.argtypes = _res, _args
-    if hasattr(_pycall, _name):        # host arrays by their element type, everything else None
-        _pycall.set_host_arrays(_name, tuple(getattr(t, "_type_", None) if issubclass(t, C._Pointer) else None for t in _args))
+    for _module in (_pycall, _pycall_block):
+        if hasattr(_module, _name):    # host arrays by their element type, everything else None
+            _module.set_host_arrays(_name, tuple(getattr(t, "_type_", None) if issubclass(t, C._Pointer) else None for t in _args))
 
 
 class DpError(RuntimeError):
@@ -122,8 +128,9 @@ def _stream(stream) -> Optional[int]:
         # of one small layer makes three calls in 30 us); private to torch, so not taken for granted
         try:
             handle = torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
-            if _pycall:
-                _pycall.set_torch(torch._C)    # its calls look there themselves from now on
+            for module in (_pycall, _pycall_block):
+                if module:
+                    module.set_torch(torch._C)     # its calls look there themselves from now on
             return handle
         except AttributeError:
             pass
@@ -141,7 +148,7 @@ def _check(status: int, where: str) -> None:
 
 def _call(name: str, *args) -> None:
     """Library call `name`; device pointers as tensors, addresses or None, host arrays as ctypes arrays, the stream last."""
-    native = getattr(_pycall, name, None)
+    native = getattr(_pycall, name, None) or getattr(_pycall_block, name, None)
     status = native(*args) if native else None
     if status is None:                     # something that the native conversion leaves to ctypes
         fn = getattr(lib, name)
@@ -338,22 +345,24 @@ def dp_layer_norm_backward(x, dy, add, dt, B, T, d, gain, mean, rstd, dx, kept, 
 
 
 def attention_shape(B, H, H_kv, Tq, Tk, D, causal, scale, q_stride, k_stride, v_stride, o_stride, q_len=None, k_len=None):
-    """Strides: (sample, token, head), in elements.  The lengths are held by address: they live as long as the shape is used."""
+    """Strides: (sample, token, head), in elements.  The lengths are held by address: they live as long as the shape is used.
+    An array of one shape, as the calls take it."""
     three = C.c_int64 * 3
-    return dp_attention_shape(B, H, H_kv, Tq, Tk, D, int(causal), scale, three(*q_stride), three(*k_stride), three(*v_stride),
-                              three(*o_stride), _ptr(q_len), _ptr(k_len))
+    return (dp_attention_shape * 1)(dp_attention_shape(
+        B, H, H_kv, Tq, Tk, D, int(causal), scale, three(*q_stride), three(*k_stride), three(*v_stride), three(*o_stride),
+        _ptr(q_len), _ptr(k_len)))
 
 
 def dp_attention(shape, dt, q, k, v, o, lse, stream=None) -> None:
-    _call("dp_attention", C.byref(shape), dt, q, k, v, o, lse, stream)
+    _call("dp_attention", shape, dt, q, k, v, o, lse, stream)
 
 
 def dp_attention_backward_workspace_bytes(shape, dt) -> int:
-    return lib.dp_attention_backward_workspace_bytes(C.byref(shape), dt)
+    return lib.dp_attention_backward_workspace_bytes(shape, dt)
 
 
 def dp_attention_backward(shape, dt, q, k, v, o, lse, dout, dq, dk, dv, ws, stream=None) -> None:
-    _call("dp_attention_backward", C.byref(shape), dt, q, k, v, o, lse, dout, dq, dk, dv, ws, _nbytes(ws), stream)
+    _call("dp_attention_backward", shape, dt, q, k, v, o, lse, dout, dq, dk, dv, ws, _nbytes(ws), stream)
 
 
 def adamw_tensors(tensors: Sequence) -> "C.Array[dp_adamw_tensor]":

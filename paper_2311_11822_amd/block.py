@@ -30,35 +30,39 @@ class LayerNorm:
         self.gain, self.bias, self.eps = gain, bias, eps
         self._ws = {}                  # by shape and stream: calls on different streams do not share a workspace
 
-    def _check(self, x, others, floats):
-        if x.dim() != 3 or not x.is_contiguous():
+    def _check(self, x, like, rows, floats):
+        """Tensors of x's shape and type, [B, T] float32 ones, and others by (tensor, number of values); written out, for a call of a
+        few microseconds."""
+        shape, dtype, device = x.shape, x.dtype, x.get_device()
+        if len(shape) != 3 or not x.is_contiguous():
             raise ValueError("x: contiguous [B, T, d]")
-        B, T, d = x.shape
-        for name, p in (("gain", self.gain), ("bias", self.bias)):
-            _same(name, p, (d,), torch.float32, x.device)
-        for name, t in others:
-            _same(name, t, x.shape, x.dtype, x.device)
-        for name, t, shape in floats:
-            if t is not None and (t.numel() != shape or t.dtype != torch.float32 or t.device != x.device or not t.is_contiguous()):
-                raise ValueError(f"{name}: {shape} contiguous float32 values on {x.device}")
+        B, T, d = shape
+        for t in like:
+            if t is not None and (t.shape != shape or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous()):
+                raise ValueError(f"contiguous {tuple(shape)} of {dtype} on {x.device}, as x, not {tuple(t.shape)} of {t.dtype} on {t.device}")
+        for t in rows:
+            if t is not None and (t.numel() != B * T or t.dtype is not torch.float32 or t.get_device() != device or not t.is_contiguous()):
+                raise ValueError(f"mean, rstd: {B} x {T} contiguous float32 values on {x.device}")
+        for t, n in floats:
+            if t is not None and (t.numel() != n or t.dtype is not torch.float32 or t.get_device() != device or not t.is_contiguous()):
+                raise ValueError(f"{n} contiguous float32 values on {x.device}, not {tuple(t.shape)} of {t.dtype} on {t.device}")
         return _dtype(x), B, T, d
 
     def forward(self, x, y, mean=None, rstd=None, add=None, sum=None, stream=None) -> None:
         """x, y: [B, T, d]; mean, rstd: [B, T], kept for backward; add: joins x before the norm, the sum goes to `sum`."""
-        dt, B, T, d = self._check(x, (("y", y), ("add", add), ("sum", sum)), (("mean", mean, x.shape[0] * x.shape[1]),
-                                                                            ("rstd", rstd, x.shape[0] * x.shape[1])))
+        d = x.shape[-1]
+        dt, B, T, d = self._check(x, (y, add, sum), (mean, rstd), ((self.gain, d), (self.bias, d)))
         dp.dp_layer_norm(x, add, dt, B, T, d, self.gain, self.bias, self.eps, sum, y, mean, rstd, stream)
 
     def backward(self, x, dy, mean, rstd, dx, kept=None, sqnorm=None, add=None, stream=None) -> None:
         """dx: [B, T, d] or None; kept: [B, 2, d], per-sample gradients of gain and bias, and sqnorm: [B], their squared norms;
         add: the gradient that reaches x beside the norm."""
-        rows = x.shape[0] * x.shape[1]
-        dt, B, T, d = self._check(x, (("dy", dy), ("dx", dx), ("add", add)),
-                                  (("mean", mean, rows), ("rstd", rstd, rows), ("kept", kept, 2 * x.shape[0] * x.shape[2]),
-                                   ("sqnorm", sqnorm, x.shape[0])))
-        ws, stream = None, dp._stream(stream)
+        B, T, d = x.shape
+        dt, B, T, d = self._check(x, (dy, dx, add), (mean, rstd), ((self.gain, d), (kept, 2 * B * d), (sqnorm, B)))
+        ws = None
         if kept is not None:
-            key = (dt, B, T, d, x.device, stream)
+            stream = dp._stream(stream)
+            key = (dt, B, T, d, x.get_device(), stream)
             ws = self._ws.get(key)
             if ws is None:
                 n = dp.dp_layer_norm_workspace_bytes(dt, B, T, d)
@@ -79,47 +83,48 @@ class Attention:
     views of packed projections among them.  q_len, k_len: [B] int32 on the device, or None."""
 
     def __init__(self, q, k, v, o, causal: bool, scale: float, q_len=None, k_len=None):
-        self.device, self.dtype, self.dt = q.device, q.dtype, _dtype(q)
-        if q.dim() != 4 or k.dim() != 4:
-            raise ValueError("q, k: four axes")
+        self.device, self.index, self.dtype, self.dt = q.device, q.get_device(), q.dtype, _dtype(q)
+        if any(t.dim() != 4 for t in (q, k, v, o)) or q.shape != o.shape or k.shape != v.shape or q.shape[::3] != k.shape[::3]:
+            raise ValueError("q and o: [B, Tq, H, D], k and v: [B, Tk, H_kv, D]")
         B, Tq, H, D = q.shape
         Tk, H_kv = k.shape[1:3]
         for name, n in (("q_len", q_len), ("k_len", k_len)):
             _same(name, n, (B,), torch.int32, q.device)
         self.q_len, self.k_len = q_len, k_len             # held: the shape has their addresses
-        self.layout = {"q": (tuple(q.shape), q.stride()), "k": ((B, Tk, H_kv, D), k.stride()), "v": ((B, Tk, H_kv, D), v.stride()),
-                       "o": (tuple(q.shape), o.stride())}
-        self.rows = (B, H, Tq)
-        for name, t in (("q", q), ("k", k), ("v", v), ("o", o)):
-            self._check(name, t, name)
-            if t.shape[3] > 1 and t.stride(3) != 1:
-                raise ValueError(f"{name}: columns of a head are adjacent")
+        self.q_shape, self.k_shape, self.rows = q.shape, k.shape, torch.Size((B, H, Tq))
+        self.strides = tuple(t.stride() for t in (q, k, v, o))
+        for t in (q, k, v, o):
+            if D > 1 and t.stride(3) != 1:
+                raise ValueError("columns of a head are adjacent")
         # an axis of one entry has whatever stride; none is needed of it
         strides = [[st if n > 1 else 0 for n, st in zip(t.shape[:3], t.stride()[:3])] for t in (q, k, v, o)]
         self.shape = dp.attention_shape(B, H, H_kv, Tq, Tk, D, causal, scale, *strides, q_len, k_len)
+        self._check((q, o), (k, v), (q, k, v, o), None)
         self._ws = {}
 
-    def _check(self, name, t, like):
-        shape, strides = self.layout[like]
-        if t.dtype != self.dtype or t.device != self.device or tuple(t.shape) != shape or t.stride() != strides:
-            raise ValueError(f"{name}: {shape} in strides {strides}, {self.dtype} on {self.device}")
-
-    def _check_lse(self, lse):
-        _same("lse", lse, self.rows, torch.float32, self.device)
+    def _check(self, of_queries, of_keys, four, lse):
+        """of_queries, of_keys: by shape and type; four: in the strides of q, k, v and o."""
+        dtype, index = self.dtype, self.index
+        for shape, tensors in ((self.q_shape, of_queries), (self.k_shape, of_keys)):
+            for t in tensors:
+                if t.shape != shape or t.dtype is not dtype or t.get_device() != index:
+                    raise ValueError(f"{tuple(shape)} of {dtype} on {self.device}, not {tuple(t.shape)} of {t.dtype} on {t.device}")
+        for t, strides in zip(four, self.strides):
+            if t.stride() != strides:
+                raise ValueError(f"strides {strides}, not {t.stride()}")
+        if lse is not None and (lse.shape != self.rows or lse.dtype is not torch.float32 or lse.get_device() != index or
+                                not lse.is_contiguous()):
+            raise ValueError(f"lse: contiguous {tuple(self.rows)} of float32 on {self.device}")
 
     def forward(self, q, k, v, o, lse, stream=None) -> None:
         """o in its strides; lse: [B, H, Tq] float32, kept for backward."""
-        for name, t in (("q", q), ("k", k), ("v", v), ("o", o)):
-            self._check(name, t, name)
-        self._check_lse(lse)
+        self._check((q, o), (k, v), (q, k, v, o), lse)
         dp.dp_attention(self.shape, self.dt, q, k, v, o, lse, stream)
 
     def backward(self, q, k, v, o, lse, do, dq, dk, dv, stream=None) -> None:
         """do in o's strides; dq, dk, dv in those of q, k and v."""
-        for name, t, like in (("q", q, "q"), ("k", k, "k"), ("v", v, "v"), ("o", o, "o"), ("do", do, "o"), ("dq", dq, "q"),
-                              ("dk", dk, "k"), ("dv", dv, "v")):
-            self._check(name, t, like)
-        self._check_lse(lse)
+        self._check((q, o, do, dq), (k, v, dk, dv), (q, k, v, o), lse)
+        self._check((), (), (dq, dk, dv, do), None)
         stream = dp._stream(stream)
         ws = self._ws.get(stream)
         if ws is None:                                    # calls on different streams do not share a workspace

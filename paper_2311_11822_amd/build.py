@@ -12,6 +12,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdp_bk.so")
 PYCALL = os.path.join(HERE, "_pycall" + sysconfig.get_config_var("EXT_SUFFIX"))     # the library's calls for this Python
+PYCALL_BLOCK = os.path.join(HERE, "_pycall_block" + sysconfig.get_config_var("EXT_SUFFIX"))     # those around the linear layers
 SOURCES = ["dp_api.hip", "noise.hip", "clip.hip", "fp32_kernels.hip", "ghost.hip", "tn_gemm.hip", "grad_gemm.hip", "grad_packed.hip", "ghost_big.hip", "ghost_brief.hip", "bias.hip", "layerwise.hip", "kept.hip", "ghost_sample.hip", "perex_dma.hip", "perex_narrow.hip",
            "train_api.hip", "norm.hip", "attention.hip", "attention_grad.hip", "adamw.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
@@ -54,15 +55,17 @@ def build_pycall() -> None:
     """The calls with native argument conversion.  Without Python's headers or a host compiler there are none, and the
     binding goes through ctypes."""
     cxx, headers = shutil.which(os.environ.get("CXX", "g++")), sysconfig.get_paths()["include"]
-    if os.path.exists(PYCALL):
-        os.remove(PYCALL)                                # never one of another build beside the library
+    for module in (PYCALL, PYCALL_BLOCK):
+        if os.path.exists(module):
+            os.remove(module)                            # never one of another build beside the library
     if not cxx or not os.path.exists(os.path.join(headers, "Python.h")):
         print(f"{os.path.basename(PYCALL)} not built: no host C++ compiler or no Python.h; the binding uses ctypes", file=sys.stderr)
         return
-    subprocess.run([cxx, "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", "-Wall",
-                    "-I", os.path.join(ROOT, "include"), "-I", headers,
-                    os.path.join(CSRC, "pycall.cpp"), "-o", PYCALL, "-L", HERE, "-l:libdp_bk.so", "-Wl,-rpath,$ORIGIN"],
-                   check=True)
+    for module, flags in ((PYCALL, []), (PYCALL_BLOCK, ["-DDP_BLOCK_CALLS"])):
+        subprocess.run([cxx, "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", "-Wall", *flags,
+                        "-I", os.path.join(ROOT, "include"), "-I", headers,
+                        os.path.join(CSRC, "pycall.cpp"), "-o", module, "-L", HERE, "-l:libdp_bk.so", "-Wl,-rpath,$ORIGIN"],
+                       check=True)
 
 
 if __name__ == "__main__":

@@ -14,6 +14,8 @@
 // rows' reads of one column and the transposing reads of four rows fall on different banks.
 #pragma once
 
+#include <type_traits>
+
 #include "dp_internal.h"
 #include "lds_dma.h"
 
@@ -35,7 +37,7 @@ struct AttnArgs {
   float scale, scale2;            // scale2: scale * log2(e)
   AttnSide qs, ks, vs, os;
   int heads, blocks;              // of the launch: (sample, head) pairs and their blocks of rows
-  int spread;                     // 1: a pair's blocks on one XCD
+  int spread, group;              // attn_unit
   unsigned first;                 // number of the launch's first workgroup
 };
 
@@ -54,15 +56,16 @@ struct HeadTile {
 // Valid rows of sample b: a length beyond the tensor's, or below zero, counts as the nearest that is none.
 __device__ __forceinline__ int valid_rows(const int32_t* len, int b, int T) { return len ? min(max(len[b], 0), T) : T; }
 
-// (sample and head, block) of workgroup id.  With `spread` the blocks of a pair go to one XCD (id % 8), whose L2 then holds its
-// keys and values; ids past the last pair come out at or past a.heads.  Every other pair has its blocks in the opposite order:
-// workgroups go to compute units in turn, and under a causal mask a unit would otherwise get the longest block of every pair.
+// (sample and head, block) of workgroup id; a unit past the last pair comes out at or past a.heads.  With `spread` a pair's blocks go to
+// one XCD (id % 8), whose L2 then holds its keys and values.  Pairs come in groups of a.group (to an XCD): the group's block 0, its block 1 ...,
+// so that under a causal mask, with the longest as block 0, the units that get a short one last are those that had much before.
 __device__ __forceinline__ void attn_unit(const AttnArgs& a, unsigned id, int& pair, int& block) {
-  const unsigned i = a.spread ? id >> 3 : id;
-  const int turn = (int)(i / (unsigned)a.blocks);
-  pair = a.spread ? turn * 8 + (int)(id & 7) : turn;
-  block = (int)(i % (unsigned)a.blocks);
-  if (turn & 1) block = a.blocks - 1 - block;
+  const unsigned i = a.spread ? id >> 3 : id, per_group = (unsigned)(a.group * a.blocks), g = i / per_group, rest = i - g * per_group;
+  const unsigned left = (unsigned)(a.spread ? a.heads / 8 + (a.heads % 8 != 0) : a.heads) - g * a.group;
+  const unsigned size = left < (unsigned)a.group ? left : (unsigned)a.group;       // of this group
+  block = (int)(rest / size);
+  pair = (int)(g * a.group + rest - block * size);
+  if (a.spread) pair = 8 * pair + (int)(id & 7);
   pair = __builtin_amdgcn_readfirstlane(pair);    // (the divisions run on the vector side)
   block = __builtin_amdgcn_readfirstlane(block);
 }
@@ -97,11 +100,10 @@ struct TileLoader {
   }
 };
 
-// All loads into LDS but the LATER last ones have landed, here and (after the barrier) in the other waves; and every wave is
-// through with its reads so far.
-template <int LATER = 0>
+// All loads into LDS issued so far have landed, here and (after the barrier) in the other waves; and every wave is through with its
+// reads so far.
 __device__ __forceinline__ void tiles_landed() {
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LATER) : "memory");
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
 // Where in LDS a lane finds its operands of a tile that begins at `lds`, worked out once: a tile elsewhere is a constant in the instruction.
@@ -199,6 +201,17 @@ __device__ __forceinline__ void store_rows16(const f32x16 (&acc)[DP / 32], float
       }
       if (col < D) *reinterpret_cast<uint2*>(p + col) = make_uint2(w[0] | (uint32_t)w[1] << 16, w[2] | (uint32_t)w[3] << 16);
     }
+}
+
+// Calls f with a tile's number and the stage that it lies in, as a constant, for n tiles.
+template <class F>
+__device__ __forceinline__ void two_stages(int n, F f) {
+  for (int t = 0;;) {
+    if (t >= n) break;
+    f(t++, std::integral_constant<int, 0>{});
+    if (t >= n) break;
+    f(t++, std::integral_constant<int, 1>{});
+  }
 }
 
 // Whether some value is an infinity or no number.
@@ -349,10 +362,14 @@ struct Half<true> {
 };
 
 // Launches `blocks` of a.heads pairs, in runs below the grid's limit.
+constexpr int64_t kGroupBytes = 3 << 20;
 template <class K>
-dp_status launch_attention(K kernel, AttnArgs a, int threads, int lds, hipStream_t s) {
-  // A pair's blocks stay on one XCD where the pairs fill the eight of them (padded up to a multiple of eight).
+dp_status launch_attention(K kernel, AttnArgs a, int64_t shared_bytes, int threads, int lds, hipStream_t s) {
+  // A pair's blocks stay on one XCD where the pairs fill the eight of them (padded up to a multiple of eight); a group of pairs is what half
+  // an L2 cache holds of what their blocks share.
   a.spread = a.blocks > 1 && (a.heads % 8 == 0 || a.heads >= 64);
+  const int64_t group = kGroupBytes / (shared_bytes > 0 ? shared_bytes : 1);
+  a.group = (int)(group < 1 ? 1 : group > a.heads ? a.heads : group);
   const int64_t n = (int64_t)(a.spread ? (a.heads + 7) / 8 * 8 : a.heads) * a.blocks;
   return launch_in_runs(n, [&](dim3 grid, int first) {
     AttnArgs run = a;

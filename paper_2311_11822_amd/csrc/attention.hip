@@ -1,26 +1,19 @@
 // Attention, forward: o_i = sum_j p_ij v_j with p_ij = exp(scale q_i k_j - lse_i) over the keys j that row i sees, in one pass over keys and
 // values with a running maximum and sum.
-#include <type_traits>
-
 #include "attention.h"
 
 namespace dpbk {
 
 namespace {
 
-#ifndef FWD_OCC
-#define FWD_OCC(DP) (DP <= 64 ? 3 : 2)
-#endif
-#ifndef FWD_PIPE
-#define FWD_PIPE (DP > 64)
-#endif
-constexpr int kKeys = 64;                         // of a tile
 constexpr float kLazy = 8.f;                      // a maximum may be passed by 2^8 before sums are expressed in a new one
 
-template <bool F16, int DP, int NW, bool PIPE>
-__global__ void __launch_bounds__(64 * NW, FWD_OCC(DP)) attention_kernel(const AttnArgs a) {
+// NW waves of 32 queries each, tiles of KEYS keys in two stages.
+template <bool F16, int DP, int NW, int KEYS>
+__global__ void __launch_bounds__(64 * NW, 2) attention_kernel(const AttnArgs a) {
   extern __shared__ __align__(1024) char smem[];
-  constexpr int TILE = kKeys * HeadTile<DP>::ROW_BYTES;
+  constexpr int KS = DP / 16, CB = DP / 32, KB = KEYS / 32, TILE = KEYS * HeadTile<DP>::ROW_BYTES;
+  constexpr int V = 2 * TILE;                     // two stages of keys, then two of values
   int pair, block;
   attn_unit(a, a.first + blockIdx.x, pair, block);
   if (pair >= a.heads) return;
@@ -38,15 +31,17 @@ __global__ void __launch_bounds__(64 * NW, FWD_OCC(DP)) attention_kernel(const A
   const int lane_end = row >= n_q ? 0 : a.causal ? min(n_k, row + shift + 1) : n_k;
 
   const uint16_t* q = static_cast<const uint16_t*>(a.q) + b * a.qs.sample + h * a.qs.head;
-  TileLoader<DP, kKeys, NW> k_tiles, v_tiles;
+  TileLoader<DP, KEYS, NW> k_tiles, v_tiles;
   k_tiles.init(static_cast<const uint16_t*>(a.k) + b * a.ks.sample + h / a.share * a.ks.head, a.ks.token, a.D, wave, lane);
   v_tiles.init(static_cast<const uint16_t*>(a.v) + b * a.vs.sample + h / a.share * a.vs.head, a.vs.token, a.D, wave, lane);
-  constexpr int KS = DP / 16, CB = DP / 32;
-  constexpr int V = 2 * TILE;                     // two stages of keys, then two of values
-  if (end > 0) {
-    k_tiles.load(0, n_k, lds, wave);
-    if (PIPE) k_tiles.load(kKeys, n_k, lds + TILE, wave);
-    v_tiles.load(0, n_k, lds + V, wave);
+  // A tile's scores are formed beside the exponentials of the tile before it, so its keys are loaded a step before its values.
+  auto load_keys = [&](int tile, int stage) { k_tiles.load(tile * KEYS, n_k, lds + stage * TILE, wave); };
+  auto load_values = [&](int tile, int stage) { v_tiles.load(tile * KEYS, n_k, lds + V + stage * TILE, wave); };
+  const int tiles = (end + KEYS - 1) / KEYS;
+  if (tiles > 0) {
+    load_keys(0, 0);
+    if (tiles > 1) load_keys(1, 1);
+    load_values(0, 0);
   }
   bf16x8 qf[KS];
   load_own<DP>(qf, q, a.qs.token, row, row < n_q, a.D, lane);
@@ -57,39 +52,39 @@ __global__ void __launch_bounds__(64 * NW, FWD_OCC(DP)) attention_kernel(const A
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb) o[cb] = zeros16();
   float most = -3.4028235e38f, total = 0.f;       // of scale2 * score; total: of this half's keys
-  auto scores = [&](f32x16 (&to)[2], int tile) {
+  auto scores = [&](f32x16 (&to)[KB], int tile) {
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
+    for (int kb = 0; kb < KB; ++kb) {
       to[kb] = zeros16();
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) to[kb] = mfma16<F16>(read.rows(tile, 32 * kb, ks), qf[ks], to[kb]);
     }
   };
   const int all_see = a.causal ? min(n_k, own0 + shift + 1) : n_k;       // keys that each of the wave's rows sees
-  // One tile, in stage STAGE.  PIPE: s has its scores, and next gets those of the tile behind it (behind the last one: of what LDS holds,
-  // and not used).
-  auto step = [&](f32x16 (&s)[2], f32x16 (&next)[2], int j0, auto stage_tag) {
-    constexpr int STAGE = decltype(stage_tag)::value, HERE = STAGE * TILE, THERE = TILE - HERE;
+  f32x16 both[2][KB];
+  if (tiles > 0) {
     tiles_landed();
-    if (PIPE) {
-      if (j0 + 2 * kKeys < end) k_tiles.load(j0 + 2 * kKeys, n_k, lds + HERE, wave);
-    } else {
-      if (j0 + kKeys < end) k_tiles.load(j0 + kKeys, n_k, lds + THERE, wave);
-    }
-    if (j0 + kKeys < end) v_tiles.load(j0 + kKeys, n_k, lds + V + THERE, wave);
+    scores(both[0], 0);                           // (the next barrier says that all waves are through with these keys)
+  }
+  two_stages(tiles, [&](int t, auto stage) {
+    constexpr int HERE = decltype(stage)::value, NEXT = HERE ^ 1;
+    f32x16(&s)[KB] = both[HERE], (&next)[KB] = both[NEXT];
+    const int j0 = t * KEYS;
+    tiles_landed();
+    if (t + 2 < tiles) load_keys(t + 2, HERE);
+    if (t + 1 < tiles) load_values(t + 1, NEXT);
     if (j0 >= own_end) return;
-    if (!PIPE) scores(s, HERE);
-    if (j0 + kKeys > all_see) {
+    if (j0 + KEYS > all_see) {
       const int seen = lane_end - j0 - 4 * (lane >> 5);
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
+      for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           if (32 * kb + 8 * (r >> 2) + (r & 3) >= seen) s[kb][r] = -INFINITY;
     }
     float top = s[0][0];
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+    for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int r = 0; r < 16; ++r) top = fmaxf(top, s[kb][r]);
     top = fmaxf(top, other_half(top, lane)) * a.scale2;
@@ -102,34 +97,21 @@ __global__ void __launch_bounds__(64 * NW, FWD_OCC(DP)) attention_kernel(const A
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[cb][r] *= fix;
     }
-    if (PIPE) scores(next, THERE);
+    scores(next, NEXT * TILE);                    // (behind the last tile: of what LDS holds, and not used)
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
+    for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         s[kb][r] = __builtin_amdgcn_exp2f(fmaf(s[kb][r], a.scale2, -most));
         total += s[kb][r];
       }
 #pragma unroll
-    for (int ks = 0; ks < kKeys / 16; ++ks) {
+    for (int ks = 0; ks < KEYS / 16; ++ks) {
       const bf16x8 p = round8<F16>(s[ks >> 1], 8 * (ks & 1));
 #pragma unroll
-      for (int cb = 0; cb < CB; ++cb) o[cb] = mfma16<F16>(read.columns(V + HERE, 16 * ks, cb), p, o[cb]);
+      for (int cb = 0; cb < CB; ++cb) o[cb] = mfma16<F16>(read.columns(V + HERE * TILE, 16 * ks, cb), p, o[cb]);
     }
-  };
-  if (end > 0) {
-    f32x16 s[2], t[2];
-    if (PIPE) {
-      tiles_landed();
-      scores(s, 0);                               // (the next barrier says that all waves are through with these keys)
-    }
-    for (int j0 = 0;;) {
-      step(s, t, j0, std::integral_constant<int, 0>{});
-      if ((j0 += kKeys) >= end) break;
-      step(t, s, j0, std::integral_constant<int, 1>{});
-      if ((j0 += kKeys) >= end) break;
-    }
-  }
+  });
   total += other_half(total, lane);
   const bool there = lane_end > 0 && total != 0.f;
   store_rows16<F16, DP>(o, 1.f / total, there, static_cast<uint16_t*>(a.out) + b * a.os.sample + h * a.os.head, a.os.token, row,
@@ -152,28 +134,25 @@ __global__ void __launch_bounds__(256) attention_f32_kernel(const AttnArgs a) {
   if (i < a.Tq) rows.forward(i);
 }
 
-template <bool F16, int DP, int NW>
+template <bool F16, int DP, int NW, int KEYS>
 dp_status launch(AttnArgs a, hipStream_t s) {
   a.heads = a.B * a.H;
   a.blocks = (a.Tq + 32 * NW - 1) / (32 * NW);
-  constexpr int LDS = 4 * kKeys * HeadTile<DP>::ROW_BYTES;
-  auto kernel = attention_kernel<F16, DP, NW, FWD_PIPE>;
+  constexpr int LDS = 4 * KEYS * HeadTile<DP>::ROW_BYTES;
+  auto kernel = attention_kernel<F16, DP, NW, KEYS>;
   static ReadyTable done;
   if (LDS > 65536) {
     const dp_status st = allow_big_lds(kernel, LDS, done);
     if (st != DP_OK) return st;
   }
-  return launch_attention(kernel, a, 64 * NW, LDS, s);
+  return launch_attention(kernel, a, (int64_t)4 * a.Tk * a.D, 64 * NW, LDS, s);
 }
 
-#ifndef FWD_NW
-#define FWD_NW 4
-#endif
 template <bool F16, int DP>
 dp_status launch(const AttnArgs& a, hipStream_t s) {
-  if (a.Tq <= 32) return launch<F16, DP, 1>(a, s);
-  if (a.Tq <= 64) return launch<F16, DP, 2>(a, s);
-  return launch<F16, DP, FWD_NW>(a, s);
+  if (a.Tq <= 32) return launch<F16, DP, 1, 32>(a, s);
+  if (a.Tq <= 64) return launch<F16, DP, 2, 64>(a, s);
+  return launch<F16, DP, 4, 64>(a, s);
 }
 
 template <bool F16>
@@ -191,7 +170,7 @@ dp_status launch_attention_forward(const AttnArgs& args, dp_dtype dt, hipStream_
   AttnArgs a = args;
   a.heads = a.B * a.H;
   a.blocks = (a.Tq + 3) / 4;
-  return launch_attention(attention_f32_kernel, a, 256, 0, s);
+  return launch_attention(attention_f32_kernel, a, (int64_t)8 * a.Tk * a.D, 256, 0, s);
 }
 
 }  // namespace dpbk

@@ -3,49 +3,26 @@
 //   dq_i = scale sum_j ds_ij k_j,   dk_j = scale sum_i ds_ij q_i     (over the query heads that share the key head, too).
 // Two kernels, one that owns queries and one that owns keys, so that every sum has one owner and a fixed order: no atomics, no
 // partial sums in memory.  The price is that scores and do v' are formed in both, seven products for five.
-#include <type_traits>
-
 #include "attention.h"
 
 namespace dpbk {
 
 namespace {
 
-// Both kernels go through tiles of 32 rows of the other side in a ring of four, more of them on their way while one is worked on.  Up to a
-// width of 64 (PIPE) the scores and do v' of the next tile are formed beside the exponentials of this one.
-constexpr int kRing = 4, kRows = 32;
-
-#ifndef QUERY_OCC
-#define QUERY_OCC(DP) 2
-#define QUERY_PIPE(DP) (DP <= 64)
-#define KEY_OCC(DP) 2
-#define KEY_PIPE(DP) (DP <= 64)
-#define VLDS(DP) (DP == 128)
-#endif
-
-// Calls f with each place in the ring in turn, as a constant, and the tile's number, until it has been called n times.
-template <class F>
-__device__ __forceinline__ void around_the_ring(int n, F f) {
-  for (int t = 0;;) {
-    if (t >= n) break;
-    f(t++, std::integral_constant<int, 0>{});
-    if (t >= n) break;
-    f(t++, std::integral_constant<int, 1>{});
-    if (t >= n) break;
-    f(t++, std::integral_constant<int, 2>{});
-    if (t >= n) break;
-    f(t++, std::integral_constant<int, 3>{});
-  }
-}
+// Both kernels go through tiles of 32 rows of the other side, in two stages.  (A ring of four changes nothing.)
+// (With the next tile's scores and do v' beside the exponentials, as in the forward pass, there are registers for two workgroups of
+// width 64 instead of three: 2 x 4096 tokens, 12 heads, 214 us where this takes 233; 8 x 512, 20 heads, 56 and 48; 32 x 197 50 and 41.)
+constexpr int kRows = 32;
+constexpr int grad_workgroups(int DP) { return DP <= 64 ? 3 : 2; }
+// Own keys and values, two sums, scores and their gradients are 224 registers at a width of 128: there the values stay in LDS.
+constexpr bool values_in_lds(int DP) { return DP == 128; }
 
 // dq, and for the other kernel lse in units of log 2 and delta.
 template <bool F16, int DP, int NW>
-__global__ void __launch_bounds__(64 * NW, QUERY_OCC(DP)) attention_query_grad_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(64 * NW, grad_workgroups(DP)) attention_query_grad_kernel(const AttnArgs a) {
   extern __shared__ __align__(1024) char smem[];
   constexpr int KS = DP / 16, CB = DP / 32, TILE = kRows * HeadTile<DP>::ROW_BYTES, STAGE = 2 * TILE;
-  constexpr bool PIPE = QUERY_PIPE(DP);
   typedef TileLoader<DP, kRows, NW> Loader;
-  constexpr int PER_TILE = 2 * Loader::LOADS;
   int pair, block;
   attn_unit(a, a.first + blockIdx.x, pair, block);
   if (pair >= a.heads) return;
@@ -85,7 +62,7 @@ __global__ void __launch_bounds__(64 * NW, QUERY_OCC(DP)) attention_query_grad_k
     lse2 = a.lse[at] * kLog2e;
     if (lse2 == -INFINITY) lse2 = INFINITY;
   }
-  if (lane_end == 0) delta = 0.f;
+  if (lane_end <= 0) delta = 0.f;
   // The scores of a row that sees one key have no gradient: zero probabilities here, not what two orders of adding leave.
   const float own_lse2 = lane_end == 1 ? INFINITY : lse2;
 
@@ -94,7 +71,7 @@ __global__ void __launch_bounds__(64 * NW, QUERY_OCC(DP)) attention_query_grad_k
   v_tiles.init(static_cast<const uint16_t*>(a.v) + b * a.vs.sample + h / a.share * a.vs.head, a.vs.token, a.D, wave, lane);
   TileReader<DP> read;
   read.init(lds, lane);
-  auto load = [&](int tile, int stage) {          // past the last one: nothing, by loads that count
+  auto load = [&](int tile, int stage) {
     const unsigned to = lds + stage * STAGE;
     k_tiles.load(tile * kRows, n_k, to, wave);
     v_tiles.load(tile * kRows, n_k, to + TILE, wave);
@@ -117,52 +94,47 @@ __global__ void __launch_bounds__(64 * NW, QUERY_OCC(DP)) attention_query_grad_k
       if (8 * (r >> 2) + (r & 3) >= seen) x[r] = 0.f;
   };
 
-  f32x16 dq[CB], s[2], dp[2], begin;
+  f32x16 dq[CB], begin;
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb) dq[cb] = zeros16();
   const int tiles = (end + kRows - 1) / kRows, own_tiles = (own_end + kRows - 1) / kRows;
   if (tiles > 0) {
     load(0, 0);
     load(1, 1);
-    load(2, 2);
-    tiles_landed<PER_TILE>();
+    if (end <= 2 * kRows + 32 * NW) tiles_landed();       // some wave's rows may end within two tiles
     if (own_end <= 2 * kRows) {
       // All that these rows see is at hand: delta from the probabilities, free of o's rounding, which counts where few keys share a
       // row (2-norm of dq's error against 64 bits, fp16, 18 x 591 tokens: 3.1e-4 with o's alone, 3.0e-4 so).
-      products(s[0], dp[0], 0, zeros16());
-      products(s[1], dp[1], 1, zeros16());
       float sum = 0.f;
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
+      for (int t = 0; t < 2; ++t) {
+        f32x16 s, dp;
+        products(s, dp, t, zeros16());
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[k][r] = probability(s[k][r]) * dp[k][r];
-        hide(s[k], k);
+        for (int r = 0; r < 16; ++r) s[r] = probability(s[r]) * dp[r];
+        hide(s, t);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sum += s[k][r];
+        for (int r = 0; r < 16; ++r) sum += s[r];
       }
       sum += other_half(sum, lane);
       if (lane_end > 1) delta = sum;
     }
 #pragma unroll
     for (int r = 0; r < 16; ++r) begin[r] = -delta;
-    if (PIPE) products(s[0], dp[0], 0, begin);
   }
-  around_the_ring(tiles, [&](int t, auto stage_tag) {
-    constexpr int HERE = decltype(stage_tag)::value, NEXT = (HERE + 1) % kRing, LOAD = (HERE + 3) % kRing, CUR = PIPE ? HERE % 2 : 0;
-    tiles_landed<PIPE ? PER_TILE : 2 * PER_TILE>();
-    load(t + 3, LOAD);
+  two_stages(tiles, [&](int t, auto stage) {
+    constexpr int HERE = decltype(stage)::value;
+    tiles_landed();
+    if (t > 0 && t + 1 < tiles) load(t + 1, HERE ^ 1);
     if (t >= own_tiles) return;
-    if (PIPE)
-      products(s[CUR ^ 1], dp[CUR ^ 1], NEXT, begin);
-    else
-      products(s[0], dp[0], HERE, begin);
-    f32x16& x = s[CUR];
+    f32x16 s, dp;
+    products(s, dp, HERE, begin);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) x[r] = probability(x[r]) * dp[CUR][r];
-    if ((t + 1) * kRows > all_see) hide(x, t);
+    for (int r = 0; r < 16; ++r) s[r] = probability(s[r]) * dp[r];
+    if ((t + 1) * kRows > all_see) hide(s, t);
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
-      const bf16x8 ds = round8<F16>(x, 8 * ks);
+      const bf16x8 ds = round8<F16>(s, 8 * ks);
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) dq[cb] = mfma16<F16>(read.columns(HERE * STAGE, 16 * ks, cb), ds, dq[cb]);
     }
@@ -181,12 +153,11 @@ __global__ void __launch_bounds__(64 * NW, QUERY_OCC(DP)) attention_query_grad_k
 
 // dk and dv.  A wave owns 32 keys; tiles of queries and their output gradients go through LDS, with lse and delta.
 template <bool F16, int DP, int NW>
-__global__ void __launch_bounds__(64 * NW, KEY_OCC(DP)) attention_key_grad_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(64 * NW, grad_workgroups(DP)) attention_key_grad_kernel(const AttnArgs a) {
   extern __shared__ __align__(1024) char smem[];
   constexpr int KS = DP / 16, CB = DP / 32, TILE = kRows * HeadTile<DP>::ROW_BYTES, STAGE = 2 * TILE + 512;
-  constexpr bool PIPE = KEY_PIPE(DP), V_IN_LDS = VLDS(DP);
+  constexpr bool V_IN_LDS = values_in_lds(DP);
   typedef TileLoader<DP, kRows, NW> Loader;
-  constexpr int PER_TILE = 2 * Loader::LOADS + 2;
   int pair, block;
   attn_unit(a, a.first + blockIdx.x, pair, block);
   if (pair >= a.heads) return;
@@ -207,25 +178,25 @@ __global__ void __launch_bounds__(64 * NW, KEY_OCC(DP)) attention_key_grad_kerne
     // Own keys and values, two sums, scores and their gradients are 224 registers at a width of 128: the values stay in LDS.
     TileLoader<DP, 32 * NW, NW> own;
     own.init(static_cast<const uint16_t*>(a.v) + vv, a.vs.token, a.D, wave, lane);
-    own.load(key0, n_k, lds + kRing * STAGE, wave);
+    own.load(key0, n_k, lds + 2 * STAGE, wave);
   } else {
     load_own<DP>(vf, static_cast<const uint16_t*>(a.v) + vv, a.vs.token, key, key < n_k, a.D, lane);
   }
   TileReader<DP> read;
   read.init(lds, lane);
-  const unsigned own_values = kRing * STAGE + wave * (32 * HeadTile<DP>::ROW_BYTES);
+  const unsigned own_values = 2 * STAGE + wave * (32 * HeadTile<DP>::ROW_BYTES);
   Loader q_tiles, d_tiles;
   q_tiles.init(static_cast<const uint16_t*>(a.q) + b * a.qs.sample + h * a.share * a.qs.head, a.qs.token, a.D, wave, lane);
   d_tiles.init(static_cast<const uint16_t*>(a.dout) + b * a.os.sample + h * a.share * a.os.head, a.os.token, a.D, wave, lane);
   int64_t corr = ((int64_t)b * a.H + h * a.share) * a.Tq;
   // Tiles of all query heads of the key head, one behind the other; first row of the one that is loaded next.
   int next_row = begin;
-  auto load = [&](bool more, int stage) {         // !more: nothing, by loads that count
+  auto load = [&](int stage) {
     const unsigned to = lds + stage * STAGE;
-    const int end = more ? n_q : 0;
-    q_tiles.load(next_row, end, to, wave);
-    d_tiles.load(next_row, end, to + TILE, wave);
-    const int bytes = more ? 4 * min(a.Tq - next_row, kRows) : 0;
+    q_tiles.load(next_row, n_q, to, wave);
+    d_tiles.load(next_row, n_q, to + TILE, wave);
+    const int bytes = 4 * min(a.Tq - next_row, kRows);
+    if (wave == 0)
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       i32x4 r = make_rsrc((k ? a.delta : a.lse2) + corr + next_row, bytes);
@@ -264,33 +235,21 @@ __global__ void __launch_bounds__(64 * NW, KEY_OCC(DP)) attention_key_grad_kerne
     }
   };
 
-  f32x16 dk[CB], dv[CB], s[2], dp[2];
+  f32x16 dk[CB], dv[CB];
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb) dk[cb] = dv[cb] = zeros16();
   const int steps = tiles * a.share;
-  if (steps > 0) {
-    load(true, 0);
-    load(steps > 1, 1);
-    load(steps > 2, 2);
-    if (PIPE) {
-      tiles_landed<2 * PER_TILE>();
-      products(s[0], dp[0], 0);
-    }
-  }
+  if (steps > 0) load(0);
   int first = begin;                              // of the tile at hand
-  around_the_ring(steps, [&](int t, auto stage_tag) {
-    constexpr int HERE = decltype(stage_tag)::value, NEXT = (HERE + 1) % kRing, LOAD = (HERE + 3) % kRing, CUR = PIPE ? HERE % 2 : 0;
-    tiles_landed<PIPE ? PER_TILE : 2 * PER_TILE>();
-    load(t + 3 < steps, LOAD);
+  two_stages(steps, [&](int t, auto stage) {
+    constexpr int HERE = decltype(stage)::value;
+    tiles_landed();
+    if (t + 1 < steps) load(HERE ^ 1);
     const int i0 = first;
     first = first + kRows < n_q ? first + kRows : begin;
-    // Nothing to do where neither this tile nor (PIPE) the next one sees a key of the wave.
-    if ((PIPE ? max(i0, first) : i0) + 31 < own_begin) return;
-    if (PIPE)
-      products(s[CUR ^ 1], dp[CUR ^ 1], NEXT);
-    else
-      products(s[0], dp[0], HERE);
-    f32x16 &p = s[CUR], &ds = dp[CUR];
+    if (i0 + 31 < own_begin) return;              // no query of the tile sees a key of the wave
+    f32x16 p, ds;
+    products(p, ds, HERE);
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       const f32x4 l = four(HERE * STAGE + 32 * g);
@@ -352,41 +311,35 @@ template <bool F16, int DP, int NW>
 dp_status launch_queries(AttnArgs a, hipStream_t s) {
   a.heads = a.B * a.H;
   a.blocks = (a.Tq + 32 * NW - 1) / (32 * NW);
-  constexpr int LDS = kRing * 2 * kRows * HeadTile<DP>::ROW_BYTES;
+  constexpr int LDS = 4 * kRows * HeadTile<DP>::ROW_BYTES;
   auto kernel = attention_query_grad_kernel<F16, DP, NW>;
   static ReadyTable done;
   if (LDS > 65536) {
     const dp_status st = allow_big_lds(kernel, LDS, done);
     if (st != DP_OK) return st;
   }
-  return launch_attention(kernel, a, 64 * NW, LDS, s);
+  return launch_attention(kernel, a, (int64_t)4 * a.Tk * a.D, 64 * NW, LDS, s);
 }
 
 template <bool F16, int DP, int NW>
 dp_status launch_keys(AttnArgs a, hipStream_t s) {
   a.heads = a.B * a.H_kv;
   a.blocks = (a.Tk + 32 * NW - 1) / (32 * NW);
-  constexpr int LDS = kRing * (2 * kRows * HeadTile<DP>::ROW_BYTES + 512) + (VLDS(DP) ? 32 * NW * HeadTile<DP>::ROW_BYTES : 0);
+  constexpr int LDS = 2 * (2 * kRows * HeadTile<DP>::ROW_BYTES + 512) + (values_in_lds(DP) ? 32 * NW * HeadTile<DP>::ROW_BYTES : 0);
   auto kernel = attention_key_grad_kernel<F16, DP, NW>;
   static ReadyTable done;
   if (LDS > 65536) {
     const dp_status st = allow_big_lds(kernel, LDS, done);
     if (st != DP_OK) return st;
   }
-  return launch_attention(kernel, a, 64 * NW, LDS, s);
+  return launch_attention(kernel, a, (int64_t)4 * a.Tq * a.D * a.share, 64 * NW, LDS, s);
 }
 
-#ifndef QUERY_NW
-#define QUERY_NW 4
-#endif
 template <bool F16, int DP>
 dp_status launch(const AttnArgs& a, hipStream_t s) {
-  const dp_status st = a.Tq <= 32 ? launch_queries<F16, DP, 1>(a, s) : launch_queries<F16, DP, QUERY_NW>(a, s);
+  const dp_status st = a.Tq <= 32 ? launch_queries<F16, DP, 1>(a, s) : launch_queries<F16, DP, 4>(a, s);
   if (st != DP_OK) return st;
-#ifndef KEY_NW
-#define KEY_NW (DP == 128 ? 8 : 4)
-#endif
-  return a.Tk <= 32 ? launch_keys<F16, DP, 1>(a, s) : launch_keys<F16, DP, KEY_NW>(a, s);
+  return a.Tk <= 32 ? launch_keys<F16, DP, 1>(a, s) : launch_keys<F16, DP, 4>(a, s);
 }
 
 template <bool F16>
@@ -404,11 +357,11 @@ dp_status launch_attention_backward(const AttnArgs& args, dp_dtype dt, hipStream
   AttnArgs a = args;
   a.heads = a.B * a.H;
   a.blocks = (a.Tq + 3) / 4;
-  const dp_status st = launch_attention(attention_query_grad_f32_kernel, a, 256, 0, s);
+  const dp_status st = launch_attention(attention_query_grad_f32_kernel, a, (int64_t)8 * a.Tk * a.D, 256, 0, s);
   if (st != DP_OK) return st;
   a.heads = a.B * a.H_kv;
   a.blocks = (a.Tk + 3) / 4;
-  return launch_attention(attention_key_grad_f32_kernel, a, 256, 0, s);
+  return launch_attention(attention_key_grad_f32_kernel, a, (int64_t)8 * a.Tq * a.D * a.share, 256, 0, s);
 }
 
 }  // namespace dpbk

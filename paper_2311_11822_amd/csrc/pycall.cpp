@@ -156,6 +156,16 @@ PyObject* set_torch(PyObject*, PyObject* module) {
   Py_RETURN_NONE;
 }
 
+#ifdef DP_BLOCK_CALLS                          // a module of its own: what stands around the linear layers
+#define DP_MODULE _pycall_block
+#define DP_CALLS(X) \
+  X(dp_layer_norm) \
+  X(dp_layer_norm_backward) \
+  X(dp_attention) \
+  X(dp_attention_backward) \
+  X(dp_adamw_multi)
+#else
+#define DP_MODULE _pycall
 #define DP_CALLS(X) \
   X(dp_ghost_norm) \
   X(dp_perex_norm) \
@@ -172,6 +182,11 @@ PyObject* set_torch(PyObject*, PyObject* module) {
   X(dp_clipped_grad_kept_multi) \
   X(dp_private_step_multi) \
   X(dp_layerwise_clipped_grad)
+#endif
+#define DP_JOIN(a, b) a##b
+#define DP_INIT(name) DP_JOIN(PyInit_, name)
+#define DP_TEXT(x) #x
+#define DP_NAME(name) DP_TEXT(name)
 
 // set_host_arrays(name, types): for each argument of call `name` the ctypes type of the host array's elements, or None.
 PyObject* set_host_arrays(PyObject*, PyObject* args) {
@@ -192,11 +207,11 @@ PyMethodDef methods[] = {DP_CALLS(DP_METHOD)
                          {"set_host_arrays", set_host_arrays, METH_VARARGS, nullptr},
                          {"set_torch", set_torch, METH_O, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
-PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, DP_NAME(DP_MODULE), nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__pycall(void) {
+PyMODINIT_FUNC DP_INIT(DP_MODULE)(void) {
   data_ptr_name = PyUnicode_InternFromString("data_ptr");
   type_name = PyUnicode_InternFromString("_type_");
   device_name = PyUnicode_InternFromString("_cuda_getDevice");
