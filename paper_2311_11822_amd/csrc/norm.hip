@@ -3,6 +3,7 @@
 //   kept_i = (sum_t dy h, sum_t dy) of sample i,  sqnorm_i = |kept_i|^2.
 // Streams over memory: a row is read once and held in registers (as stored) between its statistics and its result; the gradients of
 // gain and bias grow in the registers of the lanes that hold their columns while a workgroup goes through its rows.
+#include <algorithm>
 #include <type_traits>
 
 #include "train.h"
@@ -165,78 +166,91 @@ __global__ void __launch_bounds__(kThreads) layer_norm_kernel(const NormArgs a, 
   }
 }
 
-// Workgroup (chunk, sample): its row groups take rows in turn.  The gradients of gain and bias are then added over the groups
-// through LDS, in their order.
+// Workgroup (chunk, sample): its row groups take rows in turn, the next one's values on their way while one is worked on; gain is in LDS
+// (read again for every row, it would be as many bytes out of L2 as the rows themselves).  The gradients of gain and bias are then
+// added over the groups through LDS, in their order.  4 x 2048 rows of 12288 bf16 values: 214 us with loads where they are used and
+// gain out of L2.
 template <int DT, int VEC, int TPR, int P>
-__global__ void __launch_bounds__(kThreads) layer_norm_backward_kernel(const NormArgs a, int first_block) {
+__global__ void __launch_bounds__(kThreads, P <= (DT == DP_F32 ? 8 : VEC > 1 ? 24 : 0) ? 4 : 2) layer_norm_backward_kernel(const NormArgs a, int first_block) {
   constexpr int N = P / VEC, GROUPS = kThreads / TPR;
+  constexpr bool AHEAD = P <= 32;                  // (no registers for it beyond)
+  extern __shared__ __align__(16) float gains[];   // then, in the same place, the groups' sums
   __shared__ float red[kThreads / 64][2];
-  __shared__ float joined[GROUPS > 1 ? GROUPS : 1][GROUPS > 1 ? 2 * VEC * TPR : 1];
   const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
   const unsigned id = first_block + blockIdx.x;
   const int chunk = id % (unsigned)a.chunks, b = id / (unsigned)a.chunks;
   const int first = chunk * a.chunk_rows, end = min(first + a.chunk_rows, a.T);
+  struct Row {
+    Piece<DT, VEC> x[N], dy[N];
+    float mean, rstd;
+  };
+  auto load = [&](Row& r, int in_sample) {
+    const int64_t row = (int64_t)b * a.T + in_sample, at = row * a.d;
+    r.mean = a.mean[row];
+    r.rstd = a.rstd[row];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int col = VEC * (n * TPR + t);
+      if (col < a.d) {
+        r.x[n].load(a.x, at + col);
+        r.dy[n].load(a.dy, at + col);
+      }
+    }
+  };
+  Row row;
+  if (first + group < end) load(row, first + group);
+  for (int k = threadIdx.x; k < a.d; k += kThreads) gains[k] = a.gain ? a.gain[k] : 1.f;
+  __syncthreads();
   float dgain[N][VEC] = {}, dbias[N][VEC] = {};
   const float width = 1.f / a.d;
   for (int r = first; r < end; r += GROUPS) {
     const bool there = GROUPS == 1 || r + group < end;
-    const int64_t row = (int64_t)b * a.T + r + group, at = row * a.d;
-    Piece<DT, VEC> x[N], dy[N], add[N];
-    float mean = 0.f, rstd = 0.f;
-    if (there) {
-      mean = a.mean[row];
-      rstd = a.rstd[row];
-#pragma unroll
-      for (int n = 0; n < N; ++n) {
-        const int col = VEC * (n * TPR + t);
-        if (col < a.d) {
-          x[n].load(a.x, at + col);
-          dy[n].load(a.dy, at + col);
-          if (a.add) add[n].load(a.add, at + col);
-        }
-      }
-    }
+    Row next;
+    if (AHEAD && r + group + GROUPS < end) load(next, r + group + GROUPS);
     float sums[2] = {0.f, 0.f};
     if (there) {
 #pragma unroll
       for (int n = 0; n < N; ++n) {
         const int col = VEC * (n * TPR + t);
-        if (col < a.d) {
-          float gain[VEC];
-          load_params<VEC>(gain, a.gain, col, 1.f);
+        if (col < a.d)
 #pragma unroll
           for (int k = 0; k < VEC; ++k) {
-            const float h = (x[n].get(k) - mean) * rstd, g = dy[n].get(k), u = g * gain[k];
+            const float h = (row.x[n].get(k) - row.mean) * row.rstd, g = row.dy[n].get(k), u = g * gains[col + k];
             dgain[n][k] = fmaf(g, h, dgain[n][k]);
             dbias[n][k] += g;
             sums[0] += u;
             sums[1] = fmaf(u, h, sums[1]);
           }
-        }
       }
     }
-    if (!a.out) continue;
-    row_sums<TPR>(sums, red);
-    const float mean_u = sums[0] * width, mean_uh = sums[1] * width;
-    if (there) {
+    if (a.out) {
+      row_sums<TPR>(sums, red);
+      const float mean_u = sums[0] * width, mean_uh = sums[1] * width;
+      if (there) {
+        const int64_t at = ((int64_t)b * a.T + r + group) * a.d;
 #pragma unroll
-      for (int n = 0; n < N; ++n) {
-        const int col = VEC * (n * TPR + t);
-        if (col < a.d) {
-          float gain[VEC], dx[VEC];
-          load_params<VEC>(gain, a.gain, col, 1.f);
+        for (int n = 0; n < N; ++n) {
+          const int col = VEC * (n * TPR + t);
+          if (col < a.d) {
+            Piece<DT, VEC> add, out;
+            if (a.add) add.load(a.add, at + col);
+            float dx[VEC];
 #pragma unroll
-          for (int k = 0; k < VEC; ++k) {
-            const float h = (x[n].get(k) - mean) * rstd, u = dy[n].get(k) * gain[k];
-            dx[k] = (u - mean_u - h * mean_uh) * rstd;
-            if (a.add) dx[k] += add[n].get(k);
+            for (int k = 0; k < VEC; ++k) {
+              const float h = (row.x[n].get(k) - row.mean) * row.rstd, u = row.dy[n].get(k) * gains[col + k];
+              dx[k] = (u - mean_u - h * mean_uh) * row.rstd;
+              if (a.add) dx[k] += add.get(k);
+            }
+            out.set(dx);
+            out.store(a.out, at + col);
           }
-          Piece<DT, VEC> out;
-          out.set(dx);
-          out.store(a.out, at + col);
         }
       }
     }
+    if (AHEAD)
+      row = next;
+    else if (r + group + GROUPS < end)
+      load(row, r + group + GROUPS);
   }
   if (!a.kept) return;
   float* to = a.chunks > 1 ? a.partial + (int64_t)id * 2 * a.d : a.kept + (int64_t)b * 2 * a.d;
@@ -244,19 +258,20 @@ __global__ void __launch_bounds__(kThreads) layer_norm_backward_kernel(const Nor
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     if constexpr (GROUPS > 1) {
+      constexpr int SUMS = 2 * VEC * TPR;          // of a group
       __syncthreads();
 #pragma unroll
       for (int k = 0; k < VEC; ++k) {
-        joined[group][VEC * t + k] = dgain[n][k];
-        joined[group][VEC * (TPR + t) + k] = dbias[n][k];
+        gains[group * SUMS + VEC * t + k] = dgain[n][k];
+        gains[group * SUMS + VEC * (TPR + t) + k] = dbias[n][k];
       }
       __syncthreads();
-      for (int c = threadIdx.x; c < 2 * VEC * TPR; c += kThreads) {
+      for (int c = threadIdx.x; c < SUMS; c += kThreads) {
         const int half = c / (VEC * TPR), col = n * VEC * TPR + c % (VEC * TPR);
         if (col < a.d) {
           float v = 0.f;
 #pragma unroll
-          for (int g = 0; g < GROUPS; ++g) v += joined[g][c];
+          for (int g = 0; g < GROUPS; ++g) v += gains[g * SUMS + c];
           to[(int64_t)half * a.d + col] = v;
           square[0] = fmaf(v, v, square[0]);
         }
@@ -279,23 +294,62 @@ __global__ void __launch_bounds__(kThreads) layer_norm_backward_kernel(const Nor
   }
 }
 
-// kept[i, k] = the sample's chunks added in order; strips of 256 columns, `strips` to a sample.
-__global__ void __launch_bounds__(256) layer_norm_join_kernel(const float* __restrict__ partial, int chunks, int width, int strips,
-                                                              int first_block, float* __restrict__ kept) {
-  const unsigned id = first_block + blockIdx.x, b = id / (unsigned)strips, k = id % (unsigned)strips * 256 + threadIdx.x;
-  if (k >= (unsigned)width) return;
-  const float* p = partial + (int64_t)b * chunks * width + k;
+// The sum of a column over chunks c, c + step ..., in their order, eight loads in flight.
+__device__ __forceinline__ float add_chunks(const float* p, int c, int step, int chunks, int width) {
   float v = 0.f;
-  int c = 0;
-  for (; c + 8 <= chunks; c += 8) {
+  for (; c + 7 * step < chunks; c += 8 * step) {
     float x[8];
 #pragma unroll
-    for (int q = 0; q < 8; ++q) x[q] = p[(int64_t)(c + q) * width];
+    for (int q = 0; q < 8; ++q) x[q] = p[(int64_t)(c + q * step) * width];
 #pragma unroll
     for (int q = 0; q < 8; ++q) v += x[q];
   }
-  for (; c < chunks; ++c) v += p[(int64_t)c * width];
-  kept[(int64_t)b * width + k] = v;
+  for (; c < chunks; c += step) v += p[(int64_t)c * width];
+  return v;
+}
+
+// kept[i, k] = the sample's chunks added up; strips of 64 columns, `strips` to a sample, the chunks dealt to 16 waves.  (One sample of 512
+// chunks of 8192 values, a thread to a column: 30 us, all latency.)
+constexpr int kJoinThreads = 1024;
+__global__ void __launch_bounds__(kJoinThreads) layer_norm_join_kernel(const float* __restrict__ partial, int chunks, int width, int strips,
+                                                                       int first_block, float* __restrict__ kept) {
+  __shared__ float part[kJoinThreads / 64][64];
+  const unsigned id = first_block + blockIdx.x, b = id / (unsigned)strips, k = id % (unsigned)strips * 64 + (threadIdx.x & 63);
+  const int wave = threadIdx.x >> 6;
+  if (k < (unsigned)width)
+    part[wave][threadIdx.x & 63] = add_chunks(partial + (int64_t)b * chunks * width + k, wave, kJoinThreads / 64, chunks, width);
+  __syncthreads();
+  if (wave == 0 && k < (unsigned)width) {
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < kJoinThreads / 64; ++w) v += part[w][threadIdx.x];
+    kept[(int64_t)b * width + k] = v;
+  }
+}
+
+// The same and the squared norm in one launch, a workgroup to a sample, where a sample's chunks are few values.
+constexpr int kJoinValues = 1 << 16;
+__global__ void __launch_bounds__(kJoinThreads) layer_norm_join_norm_kernel(const float* __restrict__ partial, int chunks, int width,
+                                                                            int first_block, float* __restrict__ kept,
+                                                                            float* __restrict__ sqnorm) {
+  __shared__ float red[kJoinThreads / 64];
+  const unsigned b = first_block + blockIdx.x;
+  float square = 0.f;
+  for (int k = threadIdx.x; k < width; k += kJoinThreads) {
+    const float v = add_chunks(partial + (int64_t)b * chunks * width + k, 0, 1, chunks, width);
+    kept[(int64_t)b * width + k] = v;
+    square = fmaf(v, v, square);
+  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) square += __shfl_xor(square, off);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = square;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    float total = 0.f;
+#pragma unroll
+    for (int w = 0; w < kJoinThreads / 64; ++w) total += red[w];
+    sqnorm[b] = total;
+  }
 }
 
 // Calls f with the form for rows of width d: threads to a row and values to a thread.
@@ -359,16 +413,27 @@ dp_status launch_layer_norm_backward(NormArgs a, dp_dtype dt, hipStream_t s) {
   a.chunk_rows = (a.T + a.chunks - 1) / a.chunks;
   dp_status st = by_type(dt, a.d, [&](auto type, auto vec) {
     return by_width(a.d, [&](auto tpr, auto per) {
+      constexpr int VEC = decltype(vec)::value, TPR = decltype(tpr)::value, GROUPS = kThreads / TPR;
+      auto kernel = layer_norm_backward_kernel<decltype(type)::value, VEC, TPR, decltype(per)::value>;
+      const int lds = 4 * std::max(a.d, GROUPS > 1 ? GROUPS * 2 * VEC * TPR : 0);
+      static ReadyTable done;
+      if (lds > 65536) {
+        const dp_status ready = allow_big_lds(kernel, 4 * kNormMaxWidth, done);
+        if (ready != DP_OK) return ready;
+      }
       return launch_in_runs((int64_t)a.B * a.chunks, [&](dim3 grid, int first) {
-        hipLaunchKernelGGL((layer_norm_backward_kernel<decltype(type)::value, decltype(vec)::value, decltype(tpr)::value, decltype(per)::value>),
-                           grid, dim3(kThreads), 0, s, a, first);
+        hipLaunchKernelGGL(kernel, grid, dim3(kThreads), lds, s, a, first);
       });
     });
   });
   if (st != DP_OK || !a.kept || a.chunks == 1) return st;
-  const int strips = (2 * a.d + 255) / 256;
+  if ((int64_t)a.chunks * 2 * a.d <= kJoinValues)
+    return launch_in_runs(a.B, [&](dim3 grid, int first) {
+      hipLaunchKernelGGL(layer_norm_join_norm_kernel, grid, dim3(kJoinThreads), 0, s, a.partial, a.chunks, 2 * a.d, first, a.kept, a.sqnorm);
+    });
+  const int strips = (2 * a.d + 63) / 64;
   st = launch_in_runs((int64_t)a.B * strips, [&](dim3 grid, int first) {
-    hipLaunchKernelGGL(layer_norm_join_kernel, grid, dim3(256), 0, s, a.partial, a.chunks, 2 * a.d, strips, first, a.kept);
+    hipLaunchKernelGGL(layer_norm_join_kernel, grid, dim3(kJoinThreads), 0, s, a.partial, a.chunks, 2 * a.d, strips, first, a.kept);
   });
   return st != DP_OK ? st : launch_row_sqnorm(a.kept, a.B, 2 * a.d, a.sqnorm, s);
 }
