@@ -139,6 +139,39 @@ struct TileReader {
   }
 };
 
+// N matrix instructions whose operands are asked for AHEAD instructions before.  The order is fixed here: left to itself the compiler
+// reads an operand right before its use and waits for LDS each time.  begin() may come early, with other work behind it.
+template <int N, int AHEAD_>
+struct Stretch {
+  static constexpr int AHEAD = AHEAD_ < N ? AHEAD_ : N;
+  bf16x8 f[N];
+  template <class Read>
+  __device__ __forceinline__ void begin(Read read) {
+#pragma unroll
+    for (int m = 0; m < AHEAD; ++m) f[m] = read(m);
+    DP_PIN();
+  }
+  template <class Read, class Multiply, class Beside>
+  __device__ __forceinline__ void run(Read read, Multiply multiply, Beside beside) {
+    DP_PIN();
+#pragma unroll
+    for (int m = 0; m < N; ++m) {
+      if (m + AHEAD < N) f[m + AHEAD] = read(m + AHEAD);
+      multiply(m, f[m]);
+      beside(m);
+      DP_PIN();
+    }
+  }
+};
+
+// What these loads bring is there from here on.  (Otherwise the wait for them may come where they are first used, in a loop, and would be one
+// for the tiles on their way as well.)
+template <int N>
+__device__ __forceinline__ void have(bf16x8 (&f)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(f[i]));
+}
+
 // The wave's own operand from memory: row `row` (zeros where !there), columns 16 ks + 8 (lane / 32) .. + 7.
 template <int DP>
 __device__ __forceinline__ void load_own(bf16x8 (&f)[DP / 16], const uint16_t* head, int64_t token_stride, int row, bool there,
@@ -181,26 +214,37 @@ __device__ __forceinline__ f32x16 zeros16() {
   return z;
 }
 
-// A 32-row result (columns by register, the wave's rows by lane) times f, rounded, to memory: four columns of a row are eight bytes.
-// Rows with there == false get zeros; rows from `rows` on are not in the tensor.
+// A 32-row result (columns by register, the wave's rows by lane) times f, rounded, to memory: turned in LDS (`lds`: 32 rows of the wave's
+// own), so that whole rows leave, 16 bytes a lane.  Rows with there == false get zeros; rows from `rows` on are not in the tensor.
 template <bool F16, int DP>
 __device__ __forceinline__ void store_rows16(const f32x16 (&acc)[DP / 32], float f, bool there, uint16_t* head, int64_t token_stride,
-                                             int row, int rows, int D, int lane) {
-  if (row >= rows) return;
-  uint16_t* p = head + row * token_stride;
+                                             int row0, int rows, int D, unsigned lds, int lane) {
+  typedef HeadTile<DP> H;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-  for (int cb = 0; cb < DP / 32; ++cb)
+  for (int cb = 0; cb < DP / 32; ++cb) {
+    f32x16 x;
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const int col = 32 * cb + 8 * g + 4 * (lane >> 5);
-      uint16_t w[4];
+    for (int r = 0; r < 16; ++r) x[r] = there ? acc[cb][r] * f : 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float x = there ? acc[cb][4 * g + i] * f : 0.f;
-        w[i] = F16 ? __builtin_bit_cast(uint16_t, (_Float16)x) : __builtin_bit_cast(uint16_t, (__bf16)x);
-      }
-      if (col < D) *reinterpret_cast<uint2*>(p + col) = make_uint2(w[0] | (uint32_t)w[1] << 16, w[2] | (uint32_t)w[3] << 16);
+    for (int g = 0; g < 4; g += 2) {
+      const uint4 w = __builtin_bit_cast(uint4, round8<F16>(x, 4 * g));
+      const unsigned at = lds + (lane & 31) * H::ROW_BYTES + 8 * (lane >> 5);
+      auto put = [&](int chunk, uint32_t lo, uint32_t hi) {
+        *(__attribute__((address_space(3))) uint64_t*)(uintptr_t)(at + (chunk ^ H::swizzle(lane & 31)) * 16) = lo | (uint64_t)hi << 32;
+      };
+      put(4 * cb + g, w.x, w.y);
+      put(4 * cb + g + 1, w.z, w.w);
     }
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+  for (int i = 0; i < 32 * H::CHUNKS / 64; ++i) {
+    const int id = i * 64 + lane, row = id / H::CHUNKS, chunk = id % H::CHUNKS;
+    typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+    const u32x4 w = *(__attribute__((address_space(3))) const u32x4*)(uintptr_t)(lds + row * H::ROW_BYTES + (chunk ^ H::swizzle(row)) * 16);
+    if (row0 + row < rows && chunk * 8 < D) *reinterpret_cast<u32x4*>(head + (row0 + row) * token_stride + chunk * 8) = w;
+  }
 }
 
 // Calls f with a tile's number and the stage that it lies in, as a constant, for n tiles.

@@ -45,6 +45,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attention_kernel(const AttnArgs a)
   }
   bf16x8 qf[KS];
   load_own<DP>(qf, q, a.qs.token, row, row < n_q, a.D, lane);
+  have(qf);
   TileReader<DP> read;
   read.init(lds, lane);
 
@@ -114,8 +115,9 @@ __global__ void __launch_bounds__(64 * NW, 2) attention_kernel(const AttnArgs a)
   });
   total += other_half(total, lane);
   const bool there = lane_end > 0 && total != 0.f;
-  store_rows16<F16, DP>(o, 1.f / total, there, static_cast<uint16_t*>(a.out) + b * a.os.sample + h * a.os.head, a.os.token, row,
-                        a.Tq, a.D, lane);
+  tiles_landed();                                 // LDS is free
+  store_rows16<F16, DP>(o, 1.f / total, there, static_cast<uint16_t*>(a.out) + b * a.os.sample + h * a.os.head, a.os.token, own0,
+                        a.Tq, a.D, lds + wave * 32 * HeadTile<DP>::ROW_BYTES, lane);
   if (lane < 32 && row < a.Tq)
     a.lse[((int64_t)b * a.H + h) * a.Tq + row] = there ? most * kLn2 + logf(total) : -INFINITY;
   // A zero probability times an infinity is no number: rows beside a token that they do not see.

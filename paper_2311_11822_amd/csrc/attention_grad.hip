@@ -14,6 +14,7 @@ namespace {
 // width 64 instead of three: 2 x 4096 tokens, 12 heads, 214 us where this takes 233; 8 x 512, 20 heads, 56 and 48; 32 x 197 50 and 41.)
 constexpr int kRows = 32;
 constexpr int grad_workgroups(int DP) { return DP <= 64 ? 3 : 2; }
+constexpr int grad_ahead(int DP) { return DP <= 64 ? 2 : 4; }      // operands: registers for three workgroups, or for longer ways
 // Own keys and values, two sums, scores and their gradients are 224 registers at a width of 128: there the values stay in LDS.
 constexpr bool values_in_lds(int DP) { return DP == 128; }
 
@@ -78,13 +79,18 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DP)) attention_query_
   };
   // Scores, and do v' - delta (the sums begin at -delta).
   auto products = [&](f32x16& s, f32x16& dp, int stage, const f32x16& begin) {
-    s = zeros16();
-    dp = begin;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      s = mfma16<F16>(read.rows(stage * STAGE, 0, ks), qf[ks], s);
-      dp = mfma16<F16>(read.rows(stage * STAGE + TILE, 0, ks), df[ks], dp);
-    }
+    auto operand = [&](int m) { return read.rows(stage * STAGE + m / KS * TILE, 0, m % KS); };
+    Stretch<2 * KS, grad_ahead(DP)> run;
+    run.begin(operand);
+    run.run(operand,
+            [&](int m, bf16x8 f) {
+              const int ks = m % KS;
+              if (m < KS)
+                s = mfma16<F16>(f, qf[ks], ks == 0 ? zeros16() : s);
+              else
+                dp = mfma16<F16>(f, df[ks], ks == 0 ? begin : dp);
+            },
+            [](int) {});
   };
   auto probability = [&](float s) { return __builtin_amdgcn_exp2f(fmaf(s, a.scale2, -own_lse2)); };
   auto hide = [&](f32x16& x, int tile) {          // a select: what is not seen may be no number
@@ -129,22 +135,22 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DP)) attention_query_
     if (t >= own_tiles) return;
     f32x16 s, dp;
     products(s, dp, HERE, begin);
+    auto operand = [&](int m) { return read.columns(HERE * STAGE, 16 * (m / CB), m % CB); };
+    Stretch<2 * CB, grad_ahead(DP)> run;
+    run.begin(operand);
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[r] = probability(s[r]) * dp[r];
     if ((t + 1) * kRows > all_see) hide(s, t);
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      const bf16x8 ds = round8<F16>(s, 8 * ks);
-#pragma unroll
-      for (int cb = 0; cb < CB; ++cb) dq[cb] = mfma16<F16>(read.columns(HERE * STAGE, 16 * ks, cb), ds, dq[cb]);
-    }
+    const bf16x8 ds[2] = {round8<F16>(s, 0), round8<F16>(s, 8)};
+    run.run(operand, [&](int m, bf16x8 f) { dq[m % CB] = mfma16<F16>(f, ds[m / CB], dq[m % CB]); }, [](int) {});
   });
   if (lane < 32 && row < a.Tq) {
     a.lse2[at] = lse2;
     a.delta[at] = -delta;
   }
-  store_rows16<F16, DP>(dq, a.scale, lane_end > 0, static_cast<uint16_t*>(a.dq) + b * a.qs.sample + h * a.qs.head, a.qs.token, row,
-                        a.Tq, a.D, lane);
+  tiles_landed();                                 // LDS is free
+  store_rows16<F16, DP>(dq, a.scale, lane_end > 0, static_cast<uint16_t*>(a.dq) + b * a.qs.sample + h * a.qs.head, a.qs.token, own0,
+                        a.Tq, a.D, lds + wave * 32 * HeadTile<DP>::ROW_BYTES, lane);
   if (a.causal && __any(lane_end > 0 && not_finite(dq))) {
     const AttnRows<typename Half<F16>::T> rows(a, b, h, lane);
     for (int i = own0; i < min(own0 + 32, n_q); ++i) rows.query_gradient(i);
@@ -216,23 +222,32 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DP)) attention_key_gr
   auto four = [&](int at) { return *(__attribute__((address_space(3))) const f32x4*)(uintptr_t)(pairs + at); };
   // Scores, and do v' - delta.
   auto products = [&](f32x16& s, f32x16& dp, int stage) {
-    s = zeros16();
+    // The operands of LDS in the order of their instructions: Q's rows, then do's (and the values).
+    constexpr int PER = V_IN_LDS ? 2 : 1;
+    auto operand = [&](int m) {
+      const int n = m - KS;
+      if (m < KS) return read.rows(stage * STAGE, 0, m);
+      return V_IN_LDS && n % PER ? read.rows(own_values, 0, n / PER) : read.rows(stage * STAGE + TILE, 0, n / PER);
+    };
+    Stretch<KS + PER * KS, grad_ahead(DP)> run;
+    run.begin(operand);
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       const f32x4 d = four(stage * STAGE + 256 + 32 * g);
 #pragma unroll
       for (int i = 0; i < 4; ++i) dp[4 * g + i] = d[i];
     }
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      bf16x8 v;
-      if constexpr (V_IN_LDS)
-        v = read.rows(own_values, 0, ks);
-      else
-        v = vf[ks];
-      s = mfma16<F16>(read.rows(stage * STAGE, 0, ks), kf[ks], s);
-      dp = mfma16<F16>(read.rows(stage * STAGE + TILE, 0, ks), v, dp);
-    }
+    run.run(operand,
+            [&](int m, bf16x8 f) {
+              const int n = m - KS, ks = m < KS ? m : n / PER;
+              if (m < KS)
+                s = mfma16<F16>(f, kf[ks], ks == 0 ? zeros16() : s);
+              else if (!V_IN_LDS)
+                dp = mfma16<F16>(f, vf[V_IN_LDS ? 0 : ks], dp);
+              else if (n % PER)
+                dp = mfma16<F16>(run.f[m - 1], f, dp);
+            },
+            [](int) {});
   };
 
   f32x16 dk[CB], dv[CB];
@@ -250,6 +265,10 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DP)) attention_key_gr
     if (i0 + 31 < own_begin) return;              // no query of the tile sees a key of the wave
     f32x16 p, ds;
     products(p, ds, HERE);
+    // Instruction m: columns m / 2 % CB of rows 16 (m / 2 / CB) on, of dv or of dk.
+    auto operand = [&](int m) { return read.columns(HERE * STAGE + (m & 1 ? 0 : TILE), 16 * (m / 2 / CB), m / 2 % CB); };
+    Stretch<4 * CB, grad_ahead(DP)> run;
+    run.begin(operand);
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       const f32x4 l = four(HERE * STAGE + 32 * g);
@@ -271,18 +290,21 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DP)) attention_key_gr
         ds[r] = i < hidden_ds ? 0.f : ds[r];
       }
     }
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      const bf16x8 pr = round8<F16>(p, 8 * ks), dr = round8<F16>(ds, 8 * ks);
-#pragma unroll
-      for (int cb = 0; cb < CB; ++cb) {
-        dv[cb] = mfma16<F16>(read.columns(HERE * STAGE + TILE, 16 * ks, cb), pr, dv[cb]);
-        dk[cb] = mfma16<F16>(read.columns(HERE * STAGE, 16 * ks, cb), dr, dk[cb]);
-      }
-    }
+    const bf16x8 pr[2] = {round8<F16>(p, 0), round8<F16>(p, 8)}, dr[2] = {round8<F16>(ds, 0), round8<F16>(ds, 8)};
+    run.run(operand,
+            [&](int m, bf16x8 f) {
+              const int cb = m / 2 % CB, ks = m / 2 / CB;
+              if (m & 1)
+                dk[cb] = mfma16<F16>(f, dr[ks], dk[cb]);
+              else
+                dv[cb] = mfma16<F16>(f, pr[ks], dv[cb]);
+            },
+            [](int) {});
   });
-  store_rows16<F16, DP>(dk, a.scale, key < n_k, static_cast<uint16_t*>(a.dk) + kv, a.ks.token, key, a.Tk, a.D, lane);
-  store_rows16<F16, DP>(dv, 1.f, key < n_k, static_cast<uint16_t*>(a.dv) + vv, a.vs.token, key, a.Tk, a.D, lane);
+  tiles_landed();                                 // LDS is free
+  const unsigned own_rows = lds + wave * 32 * HeadTile<DP>::ROW_BYTES;
+  store_rows16<F16, DP>(dk, a.scale, key < n_k, static_cast<uint16_t*>(a.dk) + kv, a.ks.token, own0, a.Tk, a.D, own_rows, lane);
+  store_rows16<F16, DP>(dv, 1.f, key < n_k, static_cast<uint16_t*>(a.dv) + vv, a.vs.token, own0, a.Tk, a.D, own_rows, lane);
   if (a.causal && __any(key < n_k && (not_finite(dk) || not_finite(dv)))) {
     const AttnRows<typename Half<F16>::T> rows(a, b, h, lane);
     for (int j = own0; j < min(own0 + 32, n_k); ++j) rows.key_gradient(j);
