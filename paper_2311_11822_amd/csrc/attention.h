@@ -271,22 +271,32 @@ __device__ __forceinline__ bool not_finite(const f32x16 (&acc)[N]) {
 
 // ---- One row by one wave, in fp32 throughout: what the 32-bit type runs on, and what a 16-bit row is formed by again where a value that
 // it does not see (a later token's, under a causal mask) is an infinity or no number and has spoilt its tile's products.
-// A lane takes one of 64 keys for the scores, and columns lane and lane + 64 for the sums.
+// A lane takes one of 64 keys for the scores, its row against the wave's own, which lies in LDS; and columns lane and lane + 64 for the
+// sums.  8 x 61 tokens, 6 heads of 128, backward: @F32@.
 
-template <class E>
-__device__ __forceinline__ float widen(E x) {
-  return (float)x;
-}
-template <class E>
-__device__ __forceinline__ E narrow(float x) {
-  return (E)x;
-}
+constexpr int kRowFloats = 256;                   // of LDS to a wave: two own rows
 
-template <class E>
-__device__ __forceinline__ float dot_rows(const E* x, const E* y, int D) {
-  float s = 0.f;
-  for (int d = 0; d < D; ++d) s = fmaf(widen(x[d]), widen(y[d]), s);
-  return s;
+// Products of N rows (a lane's, in memory) with own rows at `own` + 128 n in LDS.  whole: four elements at a time.
+template <int N, class E>
+__device__ __forceinline__ void dot_rows(float (&s)[N], const E* const (&row)[N], const float* own, int D, bool whole) {
+  typedef __attribute__((ext_vector_type(4))) E E4;
+#pragma unroll
+  for (int n = 0; n < N; ++n) s[n] = 0.f;
+  if (whole) {
+#pragma unroll 4
+    for (int d = 0; d < D; d += 4)
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        const E4 y = *reinterpret_cast<const E4*>(row[n] + d);
+        const f32x4 x = *reinterpret_cast<const f32x4*>(own + 128 * n + d);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[n] = fmaf(x[i], (float)y[i], s[n]);
+      }
+  } else {
+    for (int d = 0; d < D; ++d)
+#pragma unroll
+      for (int n = 0; n < N; ++n) s[n] = fmaf(own[128 * n + d], (float)row[n][d], s[n]);
+  }
 }
 
 __device__ __forceinline__ float wave_max(float x) {
@@ -300,14 +310,24 @@ __device__ __forceinline__ float wave_sum(float x) {
   return x;
 }
 
-// acc += sum_j w_j rows[j], j < n <= 64 (w_j in lane j).
+// acc += sum_j w_j rows[j], j < n <= 64 (w_j in lane j), in order, eight rows in flight.
 template <class E>
 __device__ __forceinline__ void add_rows(float (&acc)[2], float w, const E* rows, int64_t stride, int n, int D, int lane) {
-  for (int j = 0; j < n; ++j) {
-    const float wj = __shfl(w, j);
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
-      if (lane + 64 * c < D) acc[c] = fmaf(wj, widen(rows[j * stride + lane + 64 * c]), acc[c]);
+  for (int c = 0; c < 2; ++c) {
+    const int col = lane + 64 * c;
+    if (c > 0 && D <= 64) break;
+    const E* p = rows + min(col, D - 1);
+    int j = 0;
+    for (; j + 8 <= n; j += 8) {
+      E x[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) x[q] = p[(j + q) * stride];
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        acc[c] = fmaf(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), j + q)), (float)x[q], acc[c]);
+    }
+    for (; j < n; ++j) acc[c] = fmaf(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), j)), (float)p[j * stride], acc[c]);
   }
 }
 
@@ -315,30 +335,44 @@ template <class E>
 __device__ __forceinline__ void store_row(const float (&acc)[2], float f, E* row, int D, int lane) {
 #pragma unroll
   for (int c = 0; c < 2; ++c)
-    if (lane + 64 * c < D) row[lane + 64 * c] = narrow<E>(acc[c] * f);
+    if (lane + 64 * c < D) row[lane + 64 * c] = (E)(acc[c] * f);
 }
 
 template <class E>
 struct AttnRows {
   const AttnArgs& a;
+  float* own;                                     // the wave's, in LDS
   int b, h, lane, n_q, n_k;
-  __device__ AttnRows(const AttnArgs& args, int b_, int h_, int lane_) : a(args), b(b_), h(h_), lane(lane_) {
+  bool whole;
+  __device__ AttnRows(const AttnArgs& args, float* own_, int b_, int h_, int lane_) : a(args), own(own_), b(b_), h(h_), lane(lane_) {
     n_q = valid_rows(a.q_len, b, a.Tq);
     n_k = valid_rows(a.k_len, b, a.Tk);
+    const int64_t all = a.D | a.qs.sample | a.qs.token | a.qs.head | a.ks.sample | a.ks.token | a.ks.head | a.vs.sample | a.vs.token |
+                        a.vs.head | a.os.sample | a.os.token | a.os.head;
+    whole = (all & 3) == 0;
   }
   __device__ const E* query(const void* t, const AttnSide& s, int head) const { return (const E*)t + b * s.sample + head * s.head; }
   __device__ int keys_of(int i) const {         // row i sees keys below this
     return i >= n_q ? 0 : a.causal ? min(max(i + n_k - n_q + 1, 0), n_k) : n_k;
+  }
+  __device__ void keep_own(const E* row, int n) const {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    for (int d = lane; d < a.D; d += 64) own[128 * n + d] = (float)row[d];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
 
   __device__ void forward(int i) const {
     const E *q = query(a.q, a.qs, h) + i * a.qs.token, *k = query(a.k, a.ks, h / a.share), *v = query(a.v, a.vs, h / a.share);
     const int n = keys_of(i);
     float most = -INFINITY, total = 0.f, acc[2] = {0.f, 0.f};
+    keep_own(q, 0);
     for (int j0 = 0; j0 < n; j0 += 64) {
-      const float s = j0 + lane < n ? a.scale2 * dot_rows(q, k + (j0 + lane) * a.ks.token, a.D) : -INFINITY;
-      const float top = fmaxf(most, wave_max(s)), ref = top == -INFINITY ? 0.f : top;
-      const float p = exp2f(s - ref), fix = exp2f(most - ref);
+      const E* const rows[1] = {k + min(j0 + lane, n - 1) * a.ks.token};
+      float s[1];
+      dot_rows<1, E>(s, rows, own, a.D, whole);
+      s[0] = j0 + lane < n ? a.scale2 * s[0] : -INFINITY;
+      const float top = fmaxf(most, wave_max(s[0])), ref = top == -INFINITY ? 0.f : top;
+      const float p = exp2f(s[0] - ref), fix = exp2f(most - ref);
       most = top;
       total = total * fix + wave_sum(p);
 #pragma unroll
@@ -349,10 +383,13 @@ struct AttnRows {
     if (lane == 0) a.lse[((int64_t)b * a.H + h) * a.Tq + i] = total != 0.f ? most * kLn2 + logf(total) : -INFINITY;
   }
 
-  // Probability and its gradient of one (query, key) pair.
-  __device__ void pair(const E* q, const E* dout, const E* k, const E* v, float lse2, float delta, float& p, float& ds) const {
-    p = exp2f(fmaf(a.scale2, dot_rows(q, k, a.D), -lse2));
-    ds = p * (dot_rows(dout, v, a.D) - delta);
+  // Probability, and its score's gradient, of a lane's row against the own rows.
+  __device__ void pair(const E* x, const E* y, float lse2, float delta, float& p, float& ds) const {
+    const E* const rows[2] = {x, y};
+    float s[2];
+    dot_rows<2, E>(s, rows, own, a.D, whole);
+    p = exp2f(fmaf(a.scale2, s[0], -lse2));
+    ds = p * (s[1] - delta);
   }
 
   __device__ void query_gradient(int i) const {
@@ -361,17 +398,24 @@ struct AttnRows {
     const int n = keys_of(i);
     const int64_t at = ((int64_t)b * a.H + h) * a.Tq + i;
     const float lse = a.lse[at], lse2 = n == 0 || lse == -INFINITY ? INFINITY : lse * kLog2e;
-    const float delta = n == 0 ? 0.f : dot_rows(dout, o, a.D);
+    keep_own(q, 0);
+    keep_own(dout, 1);
+    float delta[1] = {0.f};                       // formed as do v' is: a row of one key has the same products in both
+    if (n > 0) {
+      const E* const rows[1] = {o};
+      dot_rows<1, E>(delta, rows, own + 128, a.D, whole);
+    }
     float acc[2] = {0.f, 0.f};
     for (int j0 = 0; j0 < n; j0 += 64) {
-      float p = 0.f, ds = 0.f;
-      if (j0 + lane < n) pair(q, dout, k + (j0 + lane) * a.ks.token, v + (j0 + lane) * a.vs.token, lse2, delta, p, ds);
+      const int j = min(j0 + lane, n - 1);
+      float p, ds;
+      pair(k + j * a.ks.token, v + j * a.vs.token, lse2, delta[0], p, ds);
       add_rows(acc, ds, k + j0 * a.ks.token, a.ks.token, min(64, n - j0), a.D, lane);
     }
     store_row(acc, a.scale, (E*)a.dq + b * a.qs.sample + h * a.qs.head + i * a.qs.token, a.D, lane);
     if (lane == 0) {
       a.lse2[at] = lse2;
-      a.delta[at] = -delta;
+      a.delta[at] = -delta[0];
     }
   }
 
@@ -380,13 +424,17 @@ struct AttnRows {
     const E *k = query(a.k, a.ks, h) + j * a.ks.token, *v = query(a.v, a.vs, h) + j * a.vs.token;
     float dk[2] = {0.f, 0.f}, dv[2] = {0.f, 0.f};
     const int from = a.causal ? max(j - (n_k - n_q), 0) : 0;
+    keep_own(k, 0);
+    keep_own(v, 1);
     for (int hq = h * a.share; j < n_k && hq < (h + 1) * a.share; ++hq) {
       const E *q = query(a.q, a.qs, hq), *dout = query(a.dout, a.os, hq);
       const int64_t at = ((int64_t)b * a.H + hq) * a.Tq;
       for (int i0 = from; i0 < n_q; i0 += 64) {
-        float p = 0.f, ds = 0.f;
-        const int i = i0 + lane;
-        if (i < n_q) pair(q + i * a.qs.token, dout + i * a.os.token, k, v, a.lse2[at + i], -a.delta[at + i], p, ds);
+        const int i = min(i0 + lane, n_q - 1);
+        float p, ds;
+        pair(q + i * a.qs.token, dout + i * a.os.token, a.lse2[at + i], -a.delta[at + i], p, ds);
+        // no gradient of the scores of a row that sees one key (a 16-bit row's delta is not formed as do v' is)
+        if (keys_of(i) == 1) ds = 0.f;
         add_rows(dv, p, dout + i0 * a.os.token, a.os.token, min(64, n_q - i0), a.D, lane);
         add_rows(dk, ds, q + i0 * a.qs.token, a.qs.token, min(64, n_q - i0), a.D, lane);
       }

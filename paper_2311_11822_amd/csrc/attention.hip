@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attention_kernel(const AttnArgs a)
     a.lse[((int64_t)b * a.H + h) * a.Tq + row] = there ? most * kLn2 + logf(total) : -INFINITY;
   // A zero probability times an infinity is no number: rows beside a token that they do not see.
   if (a.causal && __any(there && (not_finite(o) || !(fabsf(total) < INFINITY)))) {
-    const AttnRows<typename Half<F16>::T> rows(a, b, h, lane);
+    const AttnRows<typename Half<F16>::T> rows(a, reinterpret_cast<float*>(smem + wave * 32 * HeadTile<DP>::ROW_BYTES), b, h, lane);
     for (int i = own0; i < min(own0 + 32, n_q); ++i) rows.forward(i);
   }
 }
@@ -131,8 +131,9 @@ __global__ void __launch_bounds__(256) attention_f32_kernel(const AttnArgs a) {
   int pair, block;
   attn_unit(a, a.first + blockIdx.x, pair, block);
   if (pair >= a.heads) return;
-  const AttnRows<float> rows(a, pair / a.H, pair % a.H, threadIdx.x & 63);
-  const int i = block * 4 + (threadIdx.x >> 6);
+  __shared__ __align__(16) float own[4 * kRowFloats];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = block * 4 + wave;
+  const AttnRows<float> rows(a, own + wave * kRowFloats, pair / a.H, pair % a.H, threadIdx.x & 63);
   if (i < a.Tq) rows.forward(i);
 }
 

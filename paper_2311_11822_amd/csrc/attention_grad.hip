@@ -152,7 +152,7 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DP)) attention_query_
   store_rows16<F16, DP>(dq, a.scale, lane_end > 0, static_cast<uint16_t*>(a.dq) + b * a.qs.sample + h * a.qs.head, a.qs.token, own0,
                         a.Tq, a.D, lds + wave * 32 * HeadTile<DP>::ROW_BYTES, lane);
   if (a.causal && __any(lane_end > 0 && not_finite(dq))) {
-    const AttnRows<typename Half<F16>::T> rows(a, b, h, lane);
+    const AttnRows<typename Half<F16>::T> rows(a, reinterpret_cast<float*>(smem + wave * 32 * HeadTile<DP>::ROW_BYTES), b, h, lane);
     for (int i = own0; i < min(own0 + 32, n_q); ++i) rows.query_gradient(i);
   }
 }
@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DP)) attention_key_gr
   store_rows16<F16, DP>(dk, a.scale, key < n_k, static_cast<uint16_t*>(a.dk) + kv, a.ks.token, own0, a.Tk, a.D, own_rows, lane);
   store_rows16<F16, DP>(dv, 1.f, key < n_k, static_cast<uint16_t*>(a.dv) + vv, a.vs.token, own0, a.Tk, a.D, own_rows, lane);
   if (a.causal && __any(key < n_k && (not_finite(dk) || not_finite(dv)))) {
-    const AttnRows<typename Half<F16>::T> rows(a, b, h, lane);
+    const AttnRows<typename Half<F16>::T> rows(a, reinterpret_cast<float*>(smem + wave * 32 * HeadTile<DP>::ROW_BYTES), b, h, lane);
     for (int j = own0; j < min(own0 + 32, n_k); ++j) rows.key_gradient(j);
   }
 }
@@ -315,8 +315,9 @@ __global__ void __launch_bounds__(256) attention_query_grad_f32_kernel(const Att
   int pair, block;
   attn_unit(a, a.first + blockIdx.x, pair, block);
   if (pair >= a.heads) return;
-  const AttnRows<float> rows(a, pair / a.H, pair % a.H, threadIdx.x & 63);
-  const int i = block * 4 + (threadIdx.x >> 6);
+  __shared__ __align__(16) float own[4 * kRowFloats];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = block * 4 + wave;
+  const AttnRows<float> rows(a, own + wave * kRowFloats, pair / a.H, pair % a.H, threadIdx.x & 63);
   if (i < a.Tq) rows.query_gradient(i);
 }
 
@@ -324,8 +325,9 @@ __global__ void __launch_bounds__(256) attention_key_grad_f32_kernel(const AttnA
   int pair, block;
   attn_unit(a, a.first + blockIdx.x, pair, block);
   if (pair >= a.heads) return;
-  const AttnRows<float> rows(a, pair / a.H_kv, pair % a.H_kv, threadIdx.x & 63);
-  const int j = block * 4 + (threadIdx.x >> 6);
+  __shared__ __align__(16) float own[4 * kRowFloats];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = block * 4 + wave;
+  const AttnRows<float> rows(a, own + wave * kRowFloats, pair / a.H_kv, pair % a.H_kv, threadIdx.x & 63);
   if (j < a.Tk) rows.key_gradient(j);
 }
 
