@@ -43,13 +43,66 @@ struct AttnArgs {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
-template <int DP>
+// Operands and products by storage type DT.  A row operand is 16 bytes of a row, EL columns to each lane half: one matrix instruction of
+// 16-bit values, four of fp32.  A column operand is 16 rows of a column, 8 to each half, against eight weights a lane: one instruction, or
+// eight (whose two halves are the two rows that it adds, in the order in which the weights lie anyway).
+typedef __attribute__((ext_vector_type(8))) float f32x8;
+template <int DT>
+struct Ops {
+  static constexpr bool F16 = DT == DP_F16;
+  static constexpr int EL = 8, SIZE = 2;
+  typedef bf16x8 Row;
+  typedef bf16x8 Column;
+  typedef std::conditional_t<F16, _Float16, __bf16> E;
+  __device__ static __forceinline__ f32x16 rows(Row a, Row b, f32x16 c) { return mfma16<F16>(a, b, c); }
+  __device__ static __forceinline__ f32x16 columns(Column a, Column w, f32x16 c) { return mfma16<F16>(a, w, c); }
+  // Eight values rounded to nearest even.
+  __device__ static __forceinline__ Column weights(const f32x16& x, int first) {
+    typedef __attribute__((ext_vector_type(8))) E E8;
+    E8 y;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = (E)x[first + i];
+    return __builtin_bit_cast(bf16x8, y);
+  }
+  __device__ static __forceinline__ float get(Row x, int i) {
+    typedef __attribute__((ext_vector_type(8))) E E8;
+    return (float)__builtin_bit_cast(E8, x)[i];
+  }
+};
+template <>
+struct Ops<DP_F32> {
+  static constexpr int EL = 4, SIZE = 4;
+  typedef f32x4 Row;
+  typedef f32x8 Column;
+  typedef float E;
+  __device__ static __forceinline__ f32x16 rows(Row a, Row b, f32x16 c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], c, 0, 0, 0);
+    return c;
+  }
+  __device__ static __forceinline__ f32x16 columns(Column a, Column w, f32x16 c) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], w[i], c, 0, 0, 0);
+    return c;
+  }
+  __device__ static __forceinline__ Column weights(const f32x16& x, int first) {
+    Column y;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = x[first + i];
+    return y;
+  }
+  __device__ static __forceinline__ float get(Row x, int i) { return x[i]; }
+};
+
+template <int DT, int DP>
 struct HeadTile {
-  static constexpr int CHUNKS = DP / 8, ROW_BYTES = 2 * DP;
+  static constexpr int EL = Ops<DT>::EL, CHUNKS = DP / EL, ROW_BYTES = Ops<DT>::SIZE * DP;
   // A 128-bit read takes sixteen lanes at a time, rows of sixteen different row % 16 here, and a transposing one four rows of 64 bytes: the
   // first must differ in all of row % 16 that one line of the banks holds, the second in the 64-byte group.
-  __device__ static unsigned swizzle(unsigned row) {
-    return DP == 128 ? (row & 3) << 2 | ((row >> 2) & 3) : DP == 64 ? (row & 2) << 1 | ((row >> 2) & 3) : (row >> 2) & 3;
+  __device__ static constexpr unsigned swizzle(unsigned row) {
+    return ROW_BYTES % 256 == 0   ? (row & 3) << 2 | ((row >> 2) & 3)
+           : ROW_BYTES == 128 ? (row & 2) << 1 | ((row >> 2) & 3)
+                              : (row >> 2) & 3;
   }
 };
 
@@ -72,9 +125,10 @@ __device__ __forceinline__ void attn_unit(const AttnArgs& a, unsigned id, int& p
 
 // ROWS rows of a head from memory to LDS, one 16-byte chunk a lane and load, NW waves.  Rows past the descriptor's size and columns from D on
 // arrive as zeros.
-template <int DP, int ROWS, int NW>
+template <int DT, int DP, int ROWS, int NW>
 struct TileLoader {
-  static constexpr int CHUNKS = HeadTile<DP>::CHUNKS, WAVE_LOADS = ROWS * CHUNKS / 64, LOADS = (WAVE_LOADS + NW - 1) / NW;
+  typedef HeadTile<DT, DP> H;
+  static constexpr int CHUNKS = H::CHUNKS, WAVE_LOADS = ROWS * CHUNKS / 64, LOADS = (WAVE_LOADS + NW - 1) / NW;
   static_assert(WAVE_LOADS * 64 == ROWS * CHUNKS, "whole loads");
   // Every wave makes the same number of loads: where they are more than a tile needs, some are made twice.
   __device__ static int slot(int i, int wave) { return WAVE_LOADS % NW == 0 ? i * NW + wave : (i * NW + wave) % WAVE_LOADS; }
@@ -83,11 +137,11 @@ struct TileLoader {
   unsigned row_bytes;
   __device__ __forceinline__ void init(const void* head, int64_t token_stride, int D, int wave, int lane) {
     base = reinterpret_cast<uint64_t>(head);
-    row_bytes = (unsigned)(2 * token_stride);
+    row_bytes = (unsigned)(Ops<DT>::SIZE * token_stride);
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      const unsigned id = slot(i, wave) * 64 + lane, row = id / CHUNKS, chunk = (id % CHUNKS) ^ HeadTile<DP>::swizzle(row);
-      off[i] = (int)chunk * 8 < D ? row * row_bytes + chunk * 16 : OOB;
+      const unsigned id = slot(i, wave) * 64 + lane, row = id / CHUNKS, chunk = (id % CHUNKS) ^ H::swizzle(row);
+      off[i] = (int)chunk * H::EL < D ? row * row_bytes + chunk * 16 : OOB;
     }
   }
   // Rows row0 .. row0 + ROWS - 1 of which those below `end` are there.
@@ -107,58 +161,75 @@ __device__ __forceinline__ void tiles_landed() {
 }
 
 // Where in LDS a lane finds its operands of a tile that begins at `lds`, worked out once: a tile elsewhere is a constant in the instruction.
-template <int DP>
+template <int DT, int DP>
 struct TileReader {
-  static constexpr int KS = DP / 16, CB = DP / 32, ROW_BYTES = HeadTile<DP>::ROW_BYTES;
-  unsigned row_at[KS], column_at[CB][2];
+  typedef HeadTile<DT, DP> H;
+  static constexpr int KS = H::CHUNKS / 2, CB = DP / 32, ROW_BYTES = H::ROW_BYTES, COLUMNS = DT == DP_F32 ? 4 : 2 * CB;
+  unsigned row_at[KS], column_at[COLUMNS];
   __device__ __forceinline__ void init(unsigned lds, int lane) {
-    const unsigned row = lane & 31;
+    const unsigned row = lane & 31, h = lane >> 5;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-      row_at[ks] = lds + row * ROW_BYTES + ((2 * ks + (lane >> 5)) ^ HeadTile<DP>::swizzle(row)) * 16;
-    const int s = lane & 15, blk = lane >> 4;
-    const unsigned first = 4 * (blk >> 1) + (s >> 2);
+    for (int ks = 0; ks < KS; ++ks) row_at[ks] = lds + row * ROW_BYTES + ((2 * ks + h) ^ H::swizzle(row)) * 16;
+    if constexpr (DT == DP_F32) {
+      // row 8 (e / 4) + 4 h + e % 4 is swizzled by h and by what e alone says: four addresses, the rest is constant
 #pragma unroll
-    for (int cb = 0; cb < CB; ++cb)
+      for (int n = 0; n < COLUMNS; ++n) column_at[n] = lds + 4 * h * ROW_BYTES + ((row >> 2) ^ h ^ 2 * n) * 16 + (row & 3) * 4;
+    } else {
+      const int s = lane & 15, blk = lane >> 4;
+      const unsigned first = 4 * (blk >> 1) + (s >> 2);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const unsigned chunk = 4 * cb + 2 * (blk & 1) + ((s & 3) >> 1);
-        column_at[cb][i] = lds + (first + 8 * i) * ROW_BYTES + (chunk ^ HeadTile<DP>::swizzle(first + 8 * i)) * 16 + 8 * (s & 1);
+      for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const unsigned chunk = 4 * cb + 2 * (blk & 1) + ((s & 3) >> 1);
+          column_at[2 * cb + i] = lds + (first + 8 * i) * ROW_BYTES + (chunk ^ H::swizzle(first + 8 * i)) * 16 + 8 * (s & 1);
+        }
+    }
+  }
+  // Rows row0 + lane % 32 (row0: a multiple of 32), columns 2 EL ks + EL h .. (h = lane / 32) of the tile at byte `tile`.
+  __device__ __forceinline__ typename Ops<DT>::Row rows(int tile, int row0, int ks) const {
+    return *(__attribute__((address_space(3))) const typename Ops<DT>::Row*)(uintptr_t)(row_at[ks] + tile + row0 * ROW_BYTES);
+  }
+  // Column 32 cb + lane % 32, rows row0 + 4 h .. + 3 and row0 + 8 + 4 h .. + 3 (row0: of 16).
+  __device__ __forceinline__ typename Ops<DT>::Column columns(int tile, int row0, int cb) const {
+    if constexpr (DT == DP_F32) {
+      f32x8 f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const unsigned fixed = H::swizzle(8 * (e >> 2) + (e & 3));
+        f[e] = *(__attribute__((address_space(3))) const float*)(uintptr_t)(column_at[(fixed & 7) >> 1] + tile +
+                                                                           (row0 + 8 * (e >> 2) + (e & 3)) * ROW_BYTES +
+                                                                           ((8 * cb) ^ (fixed & 8)) * 16);
       }
-  }
-  // Rows row0 + lane % 32 (row0: a multiple of 32), columns 16 ks + 8 (lane / 32) .. + 7 of the tile at byte `tile`.
-  __device__ __forceinline__ bf16x8 rows(int tile, int row0, int ks) const {
-    return *(__attribute__((address_space(3))) const bf16x8*)(uintptr_t)(row_at[ks] + tile + row0 * ROW_BYTES);
-  }
-  // Transposed: columns 32 cb + lane % 32, rows row0 + 4 h .. + 3 and row0 + 8 + 4 h .. + 3 with h = lane / 32 (row0: of 16).
-  __device__ __forceinline__ bf16x8 columns(int tile, int row0, int cb) const {
-    Frag f;
+      return f;
+    } else {
+      Frag f;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) f.h[i] = lds_read_tr(column_at[cb][i] + tile + row0 * ROW_BYTES);
-    return f.v;
+      for (int i = 0; i < 2; ++i) f.h[i] = lds_read_tr(column_at[2 * cb + i] + tile + row0 * ROW_BYTES);
+      return f.v;
+    }
   }
 };
 
 // N matrix instructions whose operands are asked for AHEAD instructions before.  The order is fixed here: left to itself the compiler
 // reads an operand right before its use and waits for LDS each time.  begin() may come early, with other work behind it.
-template <int N, int AHEAD_>
+template <class Operand, int N, int AHEAD_>
 struct Stretch {
   static constexpr int AHEAD = AHEAD_ < N ? AHEAD_ : N;
-  bf16x8 f[N];
+  Operand f[N];
   template <class Read>
   __device__ __forceinline__ void begin(Read read) {
 #pragma unroll
     for (int m = 0; m < AHEAD; ++m) f[m] = read(m);
     DP_PIN();
   }
-  template <class Read, class Multiply, class Beside>
-  __device__ __forceinline__ void run(Read read, Multiply multiply, Beside beside) {
+  template <class Read, class Multiply>
+  __device__ __forceinline__ void run(Read read, Multiply multiply) {
     DP_PIN();
 #pragma unroll
     for (int m = 0; m < N; ++m) {
       if (m + AHEAD < N) f[m + AHEAD] = read(m + AHEAD);
       multiply(m, f[m]);
-      beside(m);
       DP_PIN();
     }
   }
@@ -166,38 +237,23 @@ struct Stretch {
 
 // What these loads bring is there from here on.  (Otherwise the wait for them may come where they are first used, in a loop, and would be one
 // for the tiles on their way as well.)
-template <int N>
-__device__ __forceinline__ void have(bf16x8 (&f)[N]) {
+template <class Row, int N>
+__device__ __forceinline__ void have(Row (&f)[N]) {
 #pragma unroll
   for (int i = 0; i < N; ++i) asm volatile("" : "+v"(f[i]));
 }
 
-// The wave's own operand from memory: row `row` (zeros where !there), columns 16 ks + 8 (lane / 32) .. + 7.
-template <int DP>
-__device__ __forceinline__ void load_own(bf16x8 (&f)[DP / 16], const uint16_t* head, int64_t token_stride, int row, bool there,
-                                         int D, int lane) {
+// The wave's own operand from memory: row `row` (zeros where !there), columns 2 EL ks + EL (lane / 32) ...
+template <int DT, int KS>
+__device__ __forceinline__ void load_own(typename Ops<DT>::Row (&f)[KS], const typename Ops<DT>::E* head, int64_t token_stride, int row,
+                                         bool there, int D, int lane) {
+  constexpr int EL = Ops<DT>::EL;
 #pragma unroll
-  for (int ks = 0; ks < DP / 16; ++ks) {
-    const int col = 16 * ks + 8 * (lane >> 5);
+  for (int ks = 0; ks < KS; ++ks) {
+    const int col = 2 * EL * ks + EL * (lane >> 5);
     uint4 w = make_uint4(0, 0, 0, 0);
     if (there && col < D) w = *reinterpret_cast<const uint4*>(head + row * token_stride + col);
-    f[ks] = __builtin_bit_cast(bf16x8, w);
-  }
-}
-
-// Eight values rounded to nearest even.
-template <bool F16>
-__device__ __forceinline__ bf16x8 round8(const f32x16& x, int first) {
-  if constexpr (F16) {
-    f16x8 y;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = (_Float16)x[first + i];
-    return __builtin_bit_cast(bf16x8, y);
-  } else {
-    bf16x8 y;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = (__bf16)x[first + i];
-    return y;
+    f[ks] = __builtin_bit_cast(typename Ops<DT>::Row, w);
   }
 }
 
@@ -216,34 +272,29 @@ __device__ __forceinline__ f32x16 zeros16() {
 
 // A 32-row result (columns by register, the wave's rows by lane) times f, rounded, to memory: turned in LDS (`lds`: 32 rows of the wave's
 // own), so that whole rows leave, 16 bytes a lane.  Rows with there == false get zeros; rows from `rows` on are not in the tensor.
-template <bool F16, int DP>
-__device__ __forceinline__ void store_rows16(const f32x16 (&acc)[DP / 32], float f, bool there, uint16_t* head, int64_t token_stride,
-                                             int row0, int rows, int D, unsigned lds, int lane) {
-  typedef HeadTile<DP> H;
+template <int DT, int DP>
+__device__ __forceinline__ void store_rows(const f32x16 (&acc)[DP / 32], float f, bool there, typename Ops<DT>::E* head,
+                                           int64_t token_stride, int row0, int rows, int D, unsigned lds, int lane) {
+  typedef HeadTile<DT, DP> H;
+  typedef __attribute__((ext_vector_type(4))) typename Ops<DT>::E E4;         // a lane has four adjacent columns
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-  for (int cb = 0; cb < DP / 32; ++cb) {
-    f32x16 x;
+  for (int cb = 0; cb < DP / 32; ++cb)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) x[r] = there ? acc[cb][r] * f : 0.f;
+    for (int g = 0; g < 4; ++g) {
+      E4 y;
 #pragma unroll
-    for (int g = 0; g < 4; g += 2) {
-      const uint4 w = __builtin_bit_cast(uint4, round8<F16>(x, 4 * g));
-      const unsigned at = lds + (lane & 31) * H::ROW_BYTES + 8 * (lane >> 5);
-      auto put = [&](int chunk, uint32_t lo, uint32_t hi) {
-        *(__attribute__((address_space(3))) uint64_t*)(uintptr_t)(at + (chunk ^ H::swizzle(lane & 31)) * 16) = lo | (uint64_t)hi << 32;
-      };
-      put(4 * cb + g, w.x, w.y);
-      put(4 * cb + g + 1, w.z, w.w);
+      for (int i = 0; i < 4; ++i) y[i] = (typename Ops<DT>::E)(there ? acc[cb][4 * g + i] * f : 0.f);
+      const unsigned at = (32 * cb + 8 * g + 4 * (lane >> 5)) * Ops<DT>::SIZE;
+      *(__attribute__((address_space(3))) E4*)(uintptr_t)(lds + (lane & 31) * H::ROW_BYTES + ((at / 16) ^ H::swizzle(lane & 31)) * 16 + at % 16) = y;
     }
-  }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
   for (int i = 0; i < 32 * H::CHUNKS / 64; ++i) {
     const int id = i * 64 + lane, row = id / H::CHUNKS, chunk = id % H::CHUNKS;
     typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
     const u32x4 w = *(__attribute__((address_space(3))) const u32x4*)(uintptr_t)(lds + row * H::ROW_BYTES + (chunk ^ H::swizzle(row)) * 16);
-    if (row0 + row < rows && chunk * 8 < D) *reinterpret_cast<u32x4*>(head + (row0 + row) * token_stride + chunk * 8) = w;
+    if (row0 + row < rows && chunk * H::EL < D) *reinterpret_cast<u32x4*>(head + (row0 + row) * token_stride + chunk * H::EL) = w;
   }
 }
 
@@ -269,10 +320,10 @@ __device__ __forceinline__ bool not_finite(const f32x16 (&acc)[N]) {
   return t != 0.f;
 }
 
-// ---- One row by one wave, in fp32 throughout: what the 32-bit type runs on, and what a 16-bit row is formed by again where a value that
-// it does not see (a later token's, under a causal mask) is an infinity or no number and has spoilt its tile's products.
-// A lane takes one of 64 keys for the scores, its row against the wave's own, which lies in LDS; and columns lane and lane + 64 for the
-// sums.  8 x 61 tokens, 6 heads of 128, backward: @F32@.
+// ---- One row by one wave, in fp32 on the vector unit: what fp32 rows of no whole 16-byte pieces run on, and what a row is formed by again
+// where a value that it does not see (a later token's, under a causal mask) is an infinity or no number and has spoilt its tile's
+// products.  A lane takes one of 64 keys for the scores, its row against the wave's own, which lies in LDS; and columns lane and lane + 64
+// for the sums.
 
 constexpr int kRowFloats = 256;                   // of LDS to a wave: two own rows
 
@@ -444,14 +495,13 @@ struct AttnRows {
   }
 };
 
-template <bool F16>
-struct Half {
-  typedef __bf16 T;
-};
-template <>
-struct Half<true> {
-  typedef _Float16 T;
-};
+// Rows of fp32 that the matrix kernels take: 16-byte pieces throughout.
+inline bool whole_pieces(const AttnArgs& a) {
+  const AttnSide* sides[] = {&a.qs, &a.ks, &a.vs, &a.os};
+  int64_t all = a.D;
+  for (const AttnSide* s : sides) all |= s->sample | s->token | s->head;
+  return all % 4 == 0;
+}
 
 // Launches `blocks` of a.heads pairs, in runs below the grid's limit.
 constexpr int64_t kGroupBytes = 3 << 20;

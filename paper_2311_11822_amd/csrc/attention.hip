@@ -9,10 +9,12 @@ namespace {
 constexpr float kLazy = 8.f;                      // a maximum may be passed by 2^8 before sums are expressed in a new one
 
 // NW waves of 32 queries each, tiles of KEYS keys in two stages.
-template <bool F16, int DP, int NW, int KEYS>
+template <int DT, int DP, int NW, int KEYS>
 __global__ void __launch_bounds__(64 * NW, 2) attention_kernel(const AttnArgs a) {
   extern __shared__ __align__(1024) char smem[];
-  constexpr int KS = DP / 16, CB = DP / 32, KB = KEYS / 32, TILE = KEYS * HeadTile<DP>::ROW_BYTES;
+  typedef Ops<DT> O;
+  typedef typename O::E E;
+  constexpr int KS = HeadTile<DT, DP>::CHUNKS / 2, CB = DP / 32, KB = KEYS / 32, TILE = KEYS * HeadTile<DT, DP>::ROW_BYTES;
   constexpr int V = 2 * TILE;                     // two stages of keys, then two of values
   int pair, block;
   attn_unit(a, a.first + blockIdx.x, pair, block);
@@ -30,10 +32,10 @@ __global__ void __launch_bounds__(64 * NW, 2) attention_kernel(const AttnArgs a)
   const int own_end = own0 >= n_q ? 0 : a.causal ? min(n_k, own_last + shift + 1) : n_k;
   const int lane_end = row >= n_q ? 0 : a.causal ? min(n_k, row + shift + 1) : n_k;
 
-  const uint16_t* q = static_cast<const uint16_t*>(a.q) + b * a.qs.sample + h * a.qs.head;
-  TileLoader<DP, KEYS, NW> k_tiles, v_tiles;
-  k_tiles.init(static_cast<const uint16_t*>(a.k) + b * a.ks.sample + h / a.share * a.ks.head, a.ks.token, a.D, wave, lane);
-  v_tiles.init(static_cast<const uint16_t*>(a.v) + b * a.vs.sample + h / a.share * a.vs.head, a.vs.token, a.D, wave, lane);
+  const E* q = static_cast<const E*>(a.q) + b * a.qs.sample + h * a.qs.head;
+  TileLoader<DT, DP, KEYS, NW> k_tiles, v_tiles;
+  k_tiles.init(static_cast<const E*>(a.k) + b * a.ks.sample + h / a.share * a.ks.head, a.ks.token, a.D, wave, lane);
+  v_tiles.init(static_cast<const E*>(a.v) + b * a.vs.sample + h / a.share * a.vs.head, a.vs.token, a.D, wave, lane);
   // A tile's scores are formed beside the exponentials of the tile before it, so its keys are loaded a step before its values.
   auto load_keys = [&](int tile, int stage) { k_tiles.load(tile * KEYS, n_k, lds + stage * TILE, wave); };
   auto load_values = [&](int tile, int stage) { v_tiles.load(tile * KEYS, n_k, lds + V + stage * TILE, wave); };
@@ -43,10 +45,10 @@ __global__ void __launch_bounds__(64 * NW, 2) attention_kernel(const AttnArgs a)
     if (tiles > 1) load_keys(1, 1);
     load_values(0, 0);
   }
-  bf16x8 qf[KS];
-  load_own<DP>(qf, q, a.qs.token, row, row < n_q, a.D, lane);
+  typename O::Row qf[KS];
+  load_own<DT>(qf, q, a.qs.token, row, row < n_q, a.D, lane);
   have(qf);
-  TileReader<DP> read;
+  TileReader<DT, DP> read;
   read.init(lds, lane);
 
   f32x16 o[CB];
@@ -58,7 +60,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attention_kernel(const AttnArgs a)
     for (int kb = 0; kb < KB; ++kb) {
       to[kb] = zeros16();
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) to[kb] = mfma16<F16>(read.rows(tile, 32 * kb, ks), qf[ks], to[kb]);
+      for (int ks = 0; ks < KS; ++ks) to[kb] = O::rows(read.rows(tile, 32 * kb, ks), qf[ks], to[kb]);
     }
   };
   const int all_see = a.causal ? min(n_k, own0 + shift + 1) : n_k;       // keys that each of the wave's rows sees
@@ -108,26 +110,26 @@ __global__ void __launch_bounds__(64 * NW, 2) attention_kernel(const AttnArgs a)
       }
 #pragma unroll
     for (int ks = 0; ks < KEYS / 16; ++ks) {
-      const bf16x8 p = round8<F16>(s[ks >> 1], 8 * (ks & 1));
+      const typename O::Column p = O::weights(s[ks >> 1], 8 * (ks & 1));
 #pragma unroll
-      for (int cb = 0; cb < CB; ++cb) o[cb] = mfma16<F16>(read.columns(V + HERE * TILE, 16 * ks, cb), p, o[cb]);
+      for (int cb = 0; cb < CB; ++cb) o[cb] = O::columns(read.columns(V + HERE * TILE, 16 * ks, cb), p, o[cb]);
     }
   });
   total += other_half(total, lane);
   const bool there = lane_end > 0 && total != 0.f;
   tiles_landed();                                 // LDS is free
-  store_rows16<F16, DP>(o, 1.f / total, there, static_cast<uint16_t*>(a.out) + b * a.os.sample + h * a.os.head, a.os.token, own0,
-                        a.Tq, a.D, lds + wave * 32 * HeadTile<DP>::ROW_BYTES, lane);
+  store_rows<DT, DP>(o, 1.f / total, there, static_cast<E*>(a.out) + b * a.os.sample + h * a.os.head, a.os.token, own0,
+                        a.Tq, a.D, lds + wave * 32 * HeadTile<DT, DP>::ROW_BYTES, lane);
   if (lane < 32 && row < a.Tq)
     a.lse[((int64_t)b * a.H + h) * a.Tq + row] = there ? most * kLn2 + logf(total) : -INFINITY;
   // A zero probability times an infinity is no number: rows beside a token that they do not see.
   if (a.causal && __any(there && (not_finite(o) || !(fabsf(total) < INFINITY)))) {
-    const AttnRows<typename Half<F16>::T> rows(a, reinterpret_cast<float*>(smem + wave * 32 * HeadTile<DP>::ROW_BYTES), b, h, lane);
+    const AttnRows<E> rows(a, reinterpret_cast<float*>(smem + wave * 32 * HeadTile<DT, DP>::ROW_BYTES), b, h, lane);
     for (int i = own0; i < min(own0 + 32, n_q); ++i) rows.forward(i);
   }
 }
 
-__global__ void __launch_bounds__(256) attention_f32_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(256) attention_rows_kernel(const AttnArgs a) {
   int pair, block;
   attn_unit(a, a.first + blockIdx.x, pair, block);
   if (pair >= a.heads) return;
@@ -137,43 +139,47 @@ __global__ void __launch_bounds__(256) attention_f32_kernel(const AttnArgs a) {
   if (i < a.Tq) rows.forward(i);
 }
 
-template <bool F16, int DP, int NW, int KEYS>
+template <int DT, int DP, int NW, int KEYS>
 dp_status launch(AttnArgs a, hipStream_t s) {
   a.heads = a.B * a.H;
   a.blocks = (a.Tq + 32 * NW - 1) / (32 * NW);
-  constexpr int LDS = 4 * KEYS * HeadTile<DP>::ROW_BYTES;
-  auto kernel = attention_kernel<F16, DP, NW, KEYS>;
+  constexpr int LDS = 4 * KEYS * HeadTile<DT, DP>::ROW_BYTES;
+  auto kernel = attention_kernel<DT, DP, NW, KEYS>;
   static ReadyTable done;
   if (LDS > 65536) {
     const dp_status st = allow_big_lds(kernel, LDS, done);
     if (st != DP_OK) return st;
   }
-  return launch_attention(kernel, a, (int64_t)4 * a.Tk * a.D, 64 * NW, LDS, s);
+  return launch_attention(kernel, a, (int64_t)2 * Ops<DT>::SIZE * a.Tk * a.D, 64 * NW, LDS, s);
 }
 
-template <bool F16, int DP>
+template <int DT, int DP>
 dp_status launch(const AttnArgs& a, hipStream_t s) {
-  if (a.Tq <= 32) return launch<F16, DP, 1, 32>(a, s);
-  if (a.Tq <= 64) return launch<F16, DP, 2, 64>(a, s);
-  return launch<F16, DP, 4, 64>(a, s);
+  constexpr int KEYS = DT == DP_F32 ? 32 : 64;
+  if (a.Tq <= 32) return launch<DT, DP, 1, 32>(a, s);
+  if (a.Tq <= 64) return launch<DT, DP, 2, KEYS>(a, s);
+  return launch<DT, DP, 4, KEYS>(a, s);
 }
 
-template <bool F16>
+template <int DT>
 dp_status launch(const AttnArgs& a, hipStream_t s) {
-  if (a.D <= 32) return launch<F16, 32>(a, s);
-  if (a.D <= 64) return launch<F16, 64>(a, s);
-  if (a.D <= 96) return launch<F16, 96>(a, s);
-  return launch<F16, 128>(a, s);
+  if (a.D <= 32) return launch<DT, 32>(a, s);
+  if (a.D <= 64) return launch<DT, 64>(a, s);
+  if constexpr (DT != DP_F32)
+    if (a.D <= 96) return launch<DT, 96>(a, s);
+  return launch<DT, 128>(a, s);
 }
 
 }  // namespace
 
 dp_status launch_attention_forward(const AttnArgs& args, dp_dtype dt, hipStream_t s) {
-  if (dt != DP_F32) return dt == DP_F16 ? launch<true>(args, s) : launch<false>(args, s);
+  if (dt == DP_BF16) return launch<DP_BF16>(args, s);
+  if (dt == DP_F16) return launch<DP_F16>(args, s);
+  if (whole_pieces(args)) return launch<DP_F32>(args, s);
   AttnArgs a = args;
   a.heads = a.B * a.H;
   a.blocks = (a.Tq + 3) / 4;
-  return launch_attention(attention_f32_kernel, a, (int64_t)8 * a.Tk * a.D, 256, 0, s);
+  return launch_attention(attention_rows_kernel, a, (int64_t)8 * a.Tk * a.D, 256, 0, s);
 }
 
 }  // namespace dpbk

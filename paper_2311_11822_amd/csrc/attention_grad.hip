@@ -13,17 +13,20 @@ namespace {
 // (With the next tile's scores and do v' beside the exponentials, as in the forward pass, there are registers for two workgroups of
 // width 64 instead of three: 2 x 4096 tokens, 12 heads, 214 us where this takes 233; 8 x 512, 20 heads, 56 and 48; 32 x 197 50 and 41.)
 constexpr int kRows = 32;
-constexpr int grad_workgroups(int DP) { return DP <= 64 ? 3 : 2; }
-constexpr int grad_ahead(int DP) { return DP <= 64 ? 2 : 4; }      // operands: registers for three workgroups, or for longer ways
+// Workgroups to a compute unit, as registers allow; operands asked for ahead: what is left of them.
+constexpr int grad_workgroups(int DT, int DP) { return DT == DP_F32 ? (DP <= 64 ? 2 : 1) : DP <= 64 ? 3 : 2; }
+constexpr int grad_ahead(int DT, int DP) { return DT == DP_F32 || DP <= 64 ? 2 : 4; }
 // Own keys and values, two sums, scores and their gradients are 224 registers at a width of 128: there the values stay in LDS.
-constexpr bool values_in_lds(int DP) { return DP == 128; }
+constexpr bool values_in_lds(int DT, int DP) { return DT != DP_F32 && DP == 128; }
 
 // dq, and for the other kernel lse in units of log 2 and delta.
-template <bool F16, int DP, int NW>
-__global__ void __launch_bounds__(64 * NW, grad_workgroups(DP)) attention_query_grad_kernel(const AttnArgs a) {
+template <int DT, int DP, int NW>
+__global__ void __launch_bounds__(64 * NW, grad_workgroups(DT, DP)) attention_query_grad_kernel(const AttnArgs a) {
   extern __shared__ __align__(1024) char smem[];
-  constexpr int KS = DP / 16, CB = DP / 32, TILE = kRows * HeadTile<DP>::ROW_BYTES, STAGE = 2 * TILE;
-  typedef TileLoader<DP, kRows, NW> Loader;
+  typedef Ops<DT> O;
+  typedef typename O::E E;
+  constexpr int KS = HeadTile<DT, DP>::CHUNKS / 2, CB = DP / 32, TILE = kRows * HeadTile<DT, DP>::ROW_BYTES, STAGE = 2 * TILE;
+  typedef TileLoader<DT, DP, kRows, NW> Loader;
   int pair, block;
   attn_unit(a, a.first + blockIdx.x, pair, block);
   if (pair >= a.heads) return;
@@ -39,22 +42,17 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DP)) attention_query_
   const int lane_end = row >= n_q ? 0 : a.causal ? min(n_k, row + shift + 1) : n_k;
   const int all_see = a.causal ? min(n_k, own0 + shift + 1) : n_k;       // keys that each of the wave's rows sees
 
-  bf16x8 qf[KS], df[KS];
-  load_own<DP>(qf, static_cast<const uint16_t*>(a.q) + b * a.qs.sample + h * a.qs.head, a.qs.token, row, row < n_q, a.D, lane);
-  load_own<DP>(df, static_cast<const uint16_t*>(a.dout) + b * a.os.sample + h * a.os.head, a.os.token, row, row < n_q, a.D, lane);
+  typename O::Row qf[KS], df[KS];
+  load_own<DT>(qf, static_cast<const E*>(a.q) + b * a.qs.sample + h * a.qs.head, a.qs.token, row, row < n_q, a.D, lane);
+  load_own<DT>(df, static_cast<const E*>(a.dout) + b * a.os.sample + h * a.os.head, a.os.token, row, row < n_q, a.D, lane);
   float delta = 0.f;
   {
-    bf16x8 of[KS];
-    load_own<DP>(of, static_cast<const uint16_t*>(a.o) + b * a.os.sample + h * a.os.head, a.os.token, row, row < n_q, a.D, lane);
+    typename O::Row of[KS];
+    load_own<DT>(of, static_cast<const E*>(a.o) + b * a.os.sample + h * a.os.head, a.os.token, row, row < n_q, a.D, lane);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if constexpr (F16)
-          delta = fmaf((float)__builtin_bit_cast(f16x8, df[ks])[i], (float)__builtin_bit_cast(f16x8, of[ks])[i], delta);
-        else
-          delta = fmaf((float)df[ks][i], (float)of[ks][i], delta);
-      }
+      for (int i = 0; i < O::EL; ++i) delta = fmaf(O::get(df[ks], i), O::get(of[ks], i), delta);
     delta += other_half(delta, lane);
   }
   const int64_t at = ((int64_t)b * a.H + h) * a.Tq + row;
@@ -68,9 +66,9 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DP)) attention_query_
   const float own_lse2 = lane_end == 1 ? INFINITY : lse2;
 
   Loader k_tiles, v_tiles;
-  k_tiles.init(static_cast<const uint16_t*>(a.k) + b * a.ks.sample + h / a.share * a.ks.head, a.ks.token, a.D, wave, lane);
-  v_tiles.init(static_cast<const uint16_t*>(a.v) + b * a.vs.sample + h / a.share * a.vs.head, a.vs.token, a.D, wave, lane);
-  TileReader<DP> read;
+  k_tiles.init(static_cast<const E*>(a.k) + b * a.ks.sample + h / a.share * a.ks.head, a.ks.token, a.D, wave, lane);
+  v_tiles.init(static_cast<const E*>(a.v) + b * a.vs.sample + h / a.share * a.vs.head, a.vs.token, a.D, wave, lane);
+  TileReader<DT, DP> read;
   read.init(lds, lane);
   auto load = [&](int tile, int stage) {
     const unsigned to = lds + stage * STAGE;
@@ -80,17 +78,16 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DP)) attention_query_
   // Scores, and do v' - delta (the sums begin at -delta).
   auto products = [&](f32x16& s, f32x16& dp, int stage, const f32x16& begin) {
     auto operand = [&](int m) { return read.rows(stage * STAGE + m / KS * TILE, 0, m % KS); };
-    Stretch<2 * KS, grad_ahead(DP)> run;
+    Stretch<typename O::Row, 2 * KS, grad_ahead(DT, DP)> run;
     run.begin(operand);
     run.run(operand,
-            [&](int m, bf16x8 f) {
+            [&](int m, typename O::Row f) {
               const int ks = m % KS;
               if (m < KS)
-                s = mfma16<F16>(f, qf[ks], ks == 0 ? zeros16() : s);
+                s = O::rows(f, qf[ks], ks == 0 ? zeros16() : s);
               else
-                dp = mfma16<F16>(f, df[ks], ks == 0 ? begin : dp);
-            },
-            [](int) {});
+                dp = O::rows(f, df[ks], ks == 0 ? begin : dp);
+            });
   };
   auto probability = [&](float s) { return __builtin_amdgcn_exp2f(fmaf(s, a.scale2, -own_lse2)); };
   auto hide = [&](f32x16& x, int tile) {          // a select: what is not seen may be no number
@@ -136,34 +133,36 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DP)) attention_query_
     f32x16 s, dp;
     products(s, dp, HERE, begin);
     auto operand = [&](int m) { return read.columns(HERE * STAGE, 16 * (m / CB), m % CB); };
-    Stretch<2 * CB, grad_ahead(DP)> run;
+    Stretch<typename O::Column, 2 * CB, grad_ahead(DT, DP)> run;
     run.begin(operand);
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[r] = probability(s[r]) * dp[r];
     if ((t + 1) * kRows > all_see) hide(s, t);
-    const bf16x8 ds[2] = {round8<F16>(s, 0), round8<F16>(s, 8)};
-    run.run(operand, [&](int m, bf16x8 f) { dq[m % CB] = mfma16<F16>(f, ds[m / CB], dq[m % CB]); }, [](int) {});
+    const typename O::Column ds[2] = {O::weights(s, 0), O::weights(s, 8)};
+    run.run(operand, [&](int m, typename O::Column f) { dq[m % CB] = O::columns(f, ds[m / CB], dq[m % CB]); });
   });
   if (lane < 32 && row < a.Tq) {
     a.lse2[at] = lse2;
     a.delta[at] = -delta;
   }
   tiles_landed();                                 // LDS is free
-  store_rows16<F16, DP>(dq, a.scale, lane_end > 0, static_cast<uint16_t*>(a.dq) + b * a.qs.sample + h * a.qs.head, a.qs.token, own0,
-                        a.Tq, a.D, lds + wave * 32 * HeadTile<DP>::ROW_BYTES, lane);
+  store_rows<DT, DP>(dq, a.scale, lane_end > 0, static_cast<E*>(a.dq) + b * a.qs.sample + h * a.qs.head, a.qs.token, own0,
+                        a.Tq, a.D, lds + wave * 32 * HeadTile<DT, DP>::ROW_BYTES, lane);
   if (a.causal && __any(lane_end > 0 && not_finite(dq))) {
-    const AttnRows<typename Half<F16>::T> rows(a, reinterpret_cast<float*>(smem + wave * 32 * HeadTile<DP>::ROW_BYTES), b, h, lane);
+    const AttnRows<E> rows(a, reinterpret_cast<float*>(smem + wave * 32 * HeadTile<DT, DP>::ROW_BYTES), b, h, lane);
     for (int i = own0; i < min(own0 + 32, n_q); ++i) rows.query_gradient(i);
   }
 }
 
 // dk and dv.  A wave owns 32 keys; tiles of queries and their output gradients go through LDS, with lse and delta.
-template <bool F16, int DP, int NW>
-__global__ void __launch_bounds__(64 * NW, grad_workgroups(DP)) attention_key_grad_kernel(const AttnArgs a) {
+template <int DT, int DP, int NW>
+__global__ void __launch_bounds__(64 * NW, grad_workgroups(DT, DP)) attention_key_grad_kernel(const AttnArgs a) {
   extern __shared__ __align__(1024) char smem[];
-  constexpr int KS = DP / 16, CB = DP / 32, TILE = kRows * HeadTile<DP>::ROW_BYTES, STAGE = 2 * TILE + 512;
-  constexpr bool V_IN_LDS = values_in_lds(DP);
-  typedef TileLoader<DP, kRows, NW> Loader;
+  typedef Ops<DT> O;
+  typedef typename O::E E;
+  constexpr int KS = HeadTile<DT, DP>::CHUNKS / 2, CB = DP / 32, TILE = kRows * HeadTile<DT, DP>::ROW_BYTES, STAGE = 2 * TILE + 512;
+  constexpr bool V_IN_LDS = values_in_lds(DT, DP);
+  typedef TileLoader<DT, DP, kRows, NW> Loader;
   int pair, block;
   attn_unit(a, a.first + blockIdx.x, pair, block);
   if (pair >= a.heads) return;
@@ -178,22 +177,22 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DP)) attention_key_gr
   const int tiles = key0 < n_k && begin < n_q ? (n_q - begin + kRows - 1) / kRows : 0;       // of one query head
 
   const int64_t kv = b * a.ks.sample + h * a.ks.head, vv = b * a.vs.sample + h * a.vs.head;
-  bf16x8 kf[KS], vf[V_IN_LDS ? 1 : KS];
-  load_own<DP>(kf, static_cast<const uint16_t*>(a.k) + kv, a.ks.token, key, key < n_k, a.D, lane);
+  typename O::Row kf[KS], vf[V_IN_LDS ? 1 : KS];
+  load_own<DT>(kf, static_cast<const E*>(a.k) + kv, a.ks.token, key, key < n_k, a.D, lane);
   if constexpr (V_IN_LDS) {
     // Own keys and values, two sums, scores and their gradients are 224 registers at a width of 128: the values stay in LDS.
-    TileLoader<DP, 32 * NW, NW> own;
-    own.init(static_cast<const uint16_t*>(a.v) + vv, a.vs.token, a.D, wave, lane);
+    TileLoader<DT, DP, 32 * NW, NW> own;
+    own.init(static_cast<const E*>(a.v) + vv, a.vs.token, a.D, wave, lane);
     own.load(key0, n_k, lds + 2 * STAGE, wave);
   } else {
-    load_own<DP>(vf, static_cast<const uint16_t*>(a.v) + vv, a.vs.token, key, key < n_k, a.D, lane);
+    load_own<DT>(vf, static_cast<const E*>(a.v) + vv, a.vs.token, key, key < n_k, a.D, lane);
   }
-  TileReader<DP> read;
+  TileReader<DT, DP> read;
   read.init(lds, lane);
-  const unsigned own_values = 2 * STAGE + wave * (32 * HeadTile<DP>::ROW_BYTES);
+  const unsigned own_values = 2 * STAGE + wave * (32 * HeadTile<DT, DP>::ROW_BYTES);
   Loader q_tiles, d_tiles;
-  q_tiles.init(static_cast<const uint16_t*>(a.q) + b * a.qs.sample + h * a.share * a.qs.head, a.qs.token, a.D, wave, lane);
-  d_tiles.init(static_cast<const uint16_t*>(a.dout) + b * a.os.sample + h * a.share * a.os.head, a.os.token, a.D, wave, lane);
+  q_tiles.init(static_cast<const E*>(a.q) + b * a.qs.sample + h * a.share * a.qs.head, a.qs.token, a.D, wave, lane);
+  d_tiles.init(static_cast<const E*>(a.dout) + b * a.os.sample + h * a.share * a.os.head, a.os.token, a.D, wave, lane);
   int64_t corr = ((int64_t)b * a.H + h * a.share) * a.Tq;
   // Tiles of all query heads of the key head, one behind the other; first row of the one that is loaded next.
   int next_row = begin;
@@ -213,8 +212,8 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DP)) attention_key_gr
     next_row += kRows;
     if (next_row >= n_q) {
       next_row = begin;
-      q_tiles.base += 2 * a.qs.head;
-      d_tiles.base += 2 * a.os.head;
+      q_tiles.base += O::SIZE * a.qs.head;
+      d_tiles.base += O::SIZE * a.os.head;
       corr += a.Tq;
     }
   };
@@ -229,7 +228,7 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DP)) attention_key_gr
       if (m < KS) return read.rows(stage * STAGE, 0, m);
       return V_IN_LDS && n % PER ? read.rows(own_values, 0, n / PER) : read.rows(stage * STAGE + TILE, 0, n / PER);
     };
-    Stretch<KS + PER * KS, grad_ahead(DP)> run;
+    Stretch<typename O::Row, KS + PER * KS, grad_ahead(DT, DP)> run;
     run.begin(operand);
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
@@ -238,16 +237,15 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DP)) attention_key_gr
       for (int i = 0; i < 4; ++i) dp[4 * g + i] = d[i];
     }
     run.run(operand,
-            [&](int m, bf16x8 f) {
+            [&](int m, typename O::Row f) {
               const int n = m - KS, ks = m < KS ? m : n / PER;
               if (m < KS)
-                s = mfma16<F16>(f, kf[ks], ks == 0 ? zeros16() : s);
+                s = O::rows(f, kf[ks], ks == 0 ? zeros16() : s);
               else if (!V_IN_LDS)
-                dp = mfma16<F16>(f, vf[V_IN_LDS ? 0 : ks], dp);
+                dp = O::rows(f, vf[V_IN_LDS ? 0 : ks], dp);
               else if (n % PER)
-                dp = mfma16<F16>(run.f[m - 1], f, dp);
-            },
-            [](int) {});
+                dp = O::rows(run.f[m - 1], f, dp);
+            });
   };
 
   f32x16 dk[CB], dv[CB];
@@ -267,7 +265,7 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DP)) attention_key_gr
     products(p, ds, HERE);
     // Instruction m: columns m / 2 % CB of rows 16 (m / 2 / CB) on, of dv or of dk.
     auto operand = [&](int m) { return read.columns(HERE * STAGE + (m & 1 ? 0 : TILE), 16 * (m / 2 / CB), m / 2 % CB); };
-    Stretch<4 * CB, grad_ahead(DP)> run;
+    Stretch<typename O::Column, 4 * CB, grad_ahead(DT, DP)> run;
     run.begin(operand);
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
@@ -290,28 +288,27 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DP)) attention_key_gr
         ds[r] = i < hidden_ds ? 0.f : ds[r];
       }
     }
-    const bf16x8 pr[2] = {round8<F16>(p, 0), round8<F16>(p, 8)}, dr[2] = {round8<F16>(ds, 0), round8<F16>(ds, 8)};
+    const typename O::Column pr[2] = {O::weights(p, 0), O::weights(p, 8)}, dr[2] = {O::weights(ds, 0), O::weights(ds, 8)};
     run.run(operand,
-            [&](int m, bf16x8 f) {
+            [&](int m, typename O::Column f) {
               const int cb = m / 2 % CB, ks = m / 2 / CB;
               if (m & 1)
-                dk[cb] = mfma16<F16>(f, dr[ks], dk[cb]);
+                dk[cb] = O::columns(f, dr[ks], dk[cb]);
               else
-                dv[cb] = mfma16<F16>(f, pr[ks], dv[cb]);
-            },
-            [](int) {});
+                dv[cb] = O::columns(f, pr[ks], dv[cb]);
+            });
   });
   tiles_landed();                                 // LDS is free
-  const unsigned own_rows = lds + wave * 32 * HeadTile<DP>::ROW_BYTES;
-  store_rows16<F16, DP>(dk, a.scale, key < n_k, static_cast<uint16_t*>(a.dk) + kv, a.ks.token, own0, a.Tk, a.D, own_rows, lane);
-  store_rows16<F16, DP>(dv, 1.f, key < n_k, static_cast<uint16_t*>(a.dv) + vv, a.vs.token, own0, a.Tk, a.D, own_rows, lane);
+  const unsigned own_rows = lds + wave * 32 * HeadTile<DT, DP>::ROW_BYTES;
+  store_rows<DT, DP>(dk, a.scale, key < n_k, static_cast<E*>(a.dk) + kv, a.ks.token, own0, a.Tk, a.D, own_rows, lane);
+  store_rows<DT, DP>(dv, 1.f, key < n_k, static_cast<E*>(a.dv) + vv, a.vs.token, own0, a.Tk, a.D, own_rows, lane);
   if (a.causal && __any(key < n_k && (not_finite(dk) || not_finite(dv)))) {
-    const AttnRows<typename Half<F16>::T> rows(a, reinterpret_cast<float*>(smem + wave * 32 * HeadTile<DP>::ROW_BYTES), b, h, lane);
+    const AttnRows<E> rows(a, reinterpret_cast<float*>(smem + wave * 32 * HeadTile<DT, DP>::ROW_BYTES), b, h, lane);
     for (int j = own0; j < min(own0 + 32, n_k); ++j) rows.key_gradient(j);
   }
 }
 
-__global__ void __launch_bounds__(256) attention_query_grad_f32_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(256) attention_query_grad_rows_kernel(const AttnArgs a) {
   int pair, block;
   attn_unit(a, a.first + blockIdx.x, pair, block);
   if (pair >= a.heads) return;
@@ -321,7 +318,7 @@ __global__ void __launch_bounds__(256) attention_query_grad_f32_kernel(const Att
   if (i < a.Tq) rows.query_gradient(i);
 }
 
-__global__ void __launch_bounds__(256) attention_key_grad_f32_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(256) attention_key_grad_rows_kernel(const AttnArgs a) {
   int pair, block;
   attn_unit(a, a.first + blockIdx.x, pair, block);
   if (pair >= a.heads) return;
@@ -331,61 +328,64 @@ __global__ void __launch_bounds__(256) attention_key_grad_f32_kernel(const AttnA
   if (j < a.Tk) rows.key_gradient(j);
 }
 
-template <bool F16, int DP, int NW>
+template <int DT, int DP, int NW>
 dp_status launch_queries(AttnArgs a, hipStream_t s) {
   a.heads = a.B * a.H;
   a.blocks = (a.Tq + 32 * NW - 1) / (32 * NW);
-  constexpr int LDS = 4 * kRows * HeadTile<DP>::ROW_BYTES;
-  auto kernel = attention_query_grad_kernel<F16, DP, NW>;
+  constexpr int LDS = 4 * kRows * HeadTile<DT, DP>::ROW_BYTES;
+  auto kernel = attention_query_grad_kernel<DT, DP, NW>;
   static ReadyTable done;
   if (LDS > 65536) {
     const dp_status st = allow_big_lds(kernel, LDS, done);
     if (st != DP_OK) return st;
   }
-  return launch_attention(kernel, a, (int64_t)4 * a.Tk * a.D, 64 * NW, LDS, s);
+  return launch_attention(kernel, a, (int64_t)2 * Ops<DT>::SIZE * a.Tk * a.D, 64 * NW, LDS, s);
 }
 
-template <bool F16, int DP, int NW>
+template <int DT, int DP, int NW>
 dp_status launch_keys(AttnArgs a, hipStream_t s) {
   a.heads = a.B * a.H_kv;
   a.blocks = (a.Tk + 32 * NW - 1) / (32 * NW);
-  constexpr int LDS = 2 * (2 * kRows * HeadTile<DP>::ROW_BYTES + 512) + (values_in_lds(DP) ? 32 * NW * HeadTile<DP>::ROW_BYTES : 0);
-  auto kernel = attention_key_grad_kernel<F16, DP, NW>;
+  constexpr int LDS = 2 * (2 * kRows * HeadTile<DT, DP>::ROW_BYTES + 512) + (values_in_lds(DT, DP) ? 32 * NW * HeadTile<DT, DP>::ROW_BYTES : 0);
+  auto kernel = attention_key_grad_kernel<DT, DP, NW>;
   static ReadyTable done;
   if (LDS > 65536) {
     const dp_status st = allow_big_lds(kernel, LDS, done);
     if (st != DP_OK) return st;
   }
-  return launch_attention(kernel, a, (int64_t)4 * a.Tq * a.D * a.share, 64 * NW, LDS, s);
+  return launch_attention(kernel, a, (int64_t)2 * Ops<DT>::SIZE * a.Tq * a.D * a.share, 64 * NW, LDS, s);
 }
 
-template <bool F16, int DP>
+template <int DT, int DP>
 dp_status launch(const AttnArgs& a, hipStream_t s) {
-  const dp_status st = a.Tq <= 32 ? launch_queries<F16, DP, 1>(a, s) : launch_queries<F16, DP, 4>(a, s);
+  const dp_status st = a.Tq <= 32 ? launch_queries<DT, DP, 1>(a, s) : launch_queries<DT, DP, 4>(a, s);
   if (st != DP_OK) return st;
-  return a.Tk <= 32 ? launch_keys<F16, DP, 1>(a, s) : launch_keys<F16, DP, 4>(a, s);
+  return a.Tk <= 32 ? launch_keys<DT, DP, 1>(a, s) : launch_keys<DT, DP, 4>(a, s);
 }
 
-template <bool F16>
+template <int DT>
 dp_status launch(const AttnArgs& a, hipStream_t s) {
-  if (a.D <= 32) return launch<F16, 32>(a, s);
-  if (a.D <= 64) return launch<F16, 64>(a, s);
-  if (a.D <= 96) return launch<F16, 96>(a, s);
-  return launch<F16, 128>(a, s);
+  if (a.D <= 32) return launch<DT, 32>(a, s);
+  if (a.D <= 64) return launch<DT, 64>(a, s);
+  if constexpr (DT != DP_F32)
+    if (a.D <= 96) return launch<DT, 96>(a, s);
+  return launch<DT, 128>(a, s);
 }
 
 }  // namespace
 
 dp_status launch_attention_backward(const AttnArgs& args, dp_dtype dt, hipStream_t s) {
-  if (dt != DP_F32) return dt == DP_F16 ? launch<true>(args, s) : launch<false>(args, s);
+  if (dt == DP_BF16) return launch<DP_BF16>(args, s);
+  if (dt == DP_F16) return launch<DP_F16>(args, s);
+  if (whole_pieces(args)) return launch<DP_F32>(args, s);
   AttnArgs a = args;
   a.heads = a.B * a.H;
   a.blocks = (a.Tq + 3) / 4;
-  const dp_status st = launch_attention(attention_query_grad_f32_kernel, a, (int64_t)8 * a.Tk * a.D, 256, 0, s);
+  const dp_status st = launch_attention(attention_query_grad_rows_kernel, a, (int64_t)8 * a.Tk * a.D, 256, 0, s);
   if (st != DP_OK) return st;
   a.heads = a.B * a.H_kv;
   a.blocks = (a.Tk + 3) / 4;
-  return launch_attention(attention_key_grad_f32_kernel, a, (int64_t)8 * a.Tq * a.D * a.share, 256, 0, s);
+  return launch_attention(attention_key_grad_rows_kernel, a, (int64_t)8 * a.Tq * a.D * a.share, 256, 0, s);
 }
 
 }  // namespace dpbk
