@@ -34,6 +34,8 @@ struct AttnArgs {
   int B, H, H_kv, share;          // share: query heads to a key head
   int Tq, Tk, D;
   int causal;
+  int parts;                      // key gradients: the query heads of a key head are dealt to this many workgroups
+  float* partial;                 // parts > 1: [2 (dk, dv)][parts][B][H_kv][Tk][D]
   float scale, scale2;            // scale2: scale * log2(e)
   AttnSide qs, ks, vs, os;
   int heads, blocks;              // of the launch: (sample, head) pairs and their blocks of rows
@@ -298,6 +300,22 @@ __device__ __forceinline__ void store_rows(const f32x16 (&acc)[DP / 32], float f
   }
 }
 
+// The same result as it is, fp32, to rows of D columns.
+template <int DP>
+__device__ __forceinline__ void store_partial(const f32x16 (&acc)[DP / 32], bool there, float* head, int row, int rows, int D, int lane) {
+  if (row >= rows) return;
+#pragma unroll
+  for (int cb = 0; cb < DP / 32; ++cb)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int col = 32 * cb + 8 * g + 4 * (lane >> 5);
+      f32x4 y;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = there ? acc[cb][4 * g + i] : 0.f;
+      if (col < D) *reinterpret_cast<f32x4*>(head + (int64_t)row * D + col) = y;
+    }
+}
+
 // Calls f with a tile's number and the stage that it lies in, as a constant, for n tiles.
 template <class F>
 __device__ __forceinline__ void two_stages(int n, F f) {
@@ -382,11 +400,11 @@ __device__ __forceinline__ void add_rows(float (&acc)[2], float w, const E* rows
   }
 }
 
-template <class E>
-__device__ __forceinline__ void store_row(const float (&acc)[2], float f, E* row, int D, int lane) {
+template <class T>
+__device__ __forceinline__ void store_row(const float (&acc)[2], float f, T* row, int D, int lane) {
 #pragma unroll
   for (int c = 0; c < 2; ++c)
-    if (lane + 64 * c < D) row[lane + 64 * c] = (E)(acc[c] * f);
+    if (lane + 64 * c < D) row[lane + 64 * c] = (T)(acc[c] * f);
 }
 
 template <class E>
@@ -470,14 +488,14 @@ struct AttnRows {
     }
   }
 
-  // h: a key head.
-  __device__ void key_gradient(int j) const {
+  // h: a key head, of whose query heads first .. last - 1 count; to partial sums (rows of D values) or, null, to the gradients.
+  __device__ void key_gradient(int j, int first, int last, float* dk_part, float* dv_part) const {
     const E *k = query(a.k, a.ks, h) + j * a.ks.token, *v = query(a.v, a.vs, h) + j * a.vs.token;
     float dk[2] = {0.f, 0.f}, dv[2] = {0.f, 0.f};
     const int from = a.causal ? max(j - (n_k - n_q), 0) : 0;
     keep_own(k, 0);
     keep_own(v, 1);
-    for (int hq = h * a.share; j < n_k && hq < (h + 1) * a.share; ++hq) {
+    for (int hq = first; j < n_k && hq < last; ++hq) {
       const E *q = query(a.q, a.qs, hq), *dout = query(a.dout, a.os, hq);
       const int64_t at = ((int64_t)b * a.H + hq) * a.Tq;
       for (int i0 = from; i0 < n_q; i0 += 64) {
@@ -489,6 +507,11 @@ struct AttnRows {
         add_rows(dv, p, dout + i0 * a.os.token, a.os.token, min(64, n_q - i0), a.D, lane);
         add_rows(dk, ds, q + i0 * a.qs.token, a.qs.token, min(64, n_q - i0), a.D, lane);
       }
+    }
+    if (dk_part) {
+      store_row(dk, 1.f, dk_part + (int64_t)j * a.D, a.D, lane);
+      store_row(dv, 1.f, dv_part + (int64_t)j * a.D, a.D, lane);
+      return;
     }
     store_row(dk, a.scale, (E*)a.dk + b * a.ks.sample + h * a.ks.head + j * a.ks.token, a.D, lane);
     store_row(dv, 1.f, (E*)a.dv + b * a.vs.sample + h * a.vs.head + j * a.vs.token, a.D, lane);
@@ -521,6 +544,9 @@ dp_status launch_attention(K kernel, AttnArgs a, int64_t shared_bytes, int threa
 }
 
 dp_status launch_attention_forward(const AttnArgs& a, dp_dtype dt, hipStream_t s);
+// Workgroups that the query heads of a key head are dealt to in the backward pass, and floats that they need where it is more than one.
+int attention_parts(const AttnArgs& a);
+int64_t attention_partial_floats(const AttnArgs& a);
 dp_status launch_attention_backward(const AttnArgs& a, dp_dtype dt, hipStream_t s);
 
 }  // namespace dpbk

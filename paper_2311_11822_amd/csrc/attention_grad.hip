@@ -13,6 +13,7 @@ namespace {
 // (With the next tile's scores and do v' beside the exponentials, as in the forward pass, there are registers for two workgroups of
 // width 64 instead of three: 2 x 4096 tokens, 12 heads, 214 us where this takes 233; 8 x 512, 20 heads, 56 and 48; 32 x 197 50 and 41.)
 constexpr int kRows = 32;
+constexpr int kPartUnits = 256;                   // compute units
 // Workgroups to a compute unit, as registers allow; operands asked for ahead: what is left of them.
 constexpr int grad_workgroups(int DT, int DP) { return DT == DP_F32 ? (DP <= 64 ? 2 : 1) : DP <= 64 ? 3 : 2; }
 constexpr int grad_ahead(int DT, int DP) { return DT == DP_F32 || DP <= 64 ? 2 : 4; }
@@ -104,8 +105,9 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DT, DP)) attention_qu
   if (tiles > 0) {
     load(0, 0);
     load(1, 1);
-    if (end <= 2 * kRows + 32 * NW) tiles_landed();       // some wave's rows may end within two tiles
-    if (own_end <= 2 * kRows) {
+    constexpr bool ROUNDED = DT != DP_F32;        // o is
+    if (ROUNDED && end <= 2 * kRows + 32 * NW) tiles_landed();       // some wave's rows may end within two tiles
+    if (ROUNDED && own_end <= 2 * kRows) {
       // All that these rows see is at hand: delta from the probabilities, free of o's rounding, which counts where few keys share a
       // row (2-norm of dq's error against 64 bits, fp16, 18 x 591 tokens: 3.1e-4 with o's alone, 3.0e-4 so).
       float sum = 0.f;
@@ -166,7 +168,9 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DT, DP)) attention_ke
   int pair, block;
   attn_unit(a, a.first + blockIdx.x, pair, block);
   if (pair >= a.heads) return;
-  const int b = pair / a.H_kv, h = pair % a.H_kv;
+  // (A unit is a sample, a key head and a part of the query heads that share it.)
+  const int part = pair % a.parts, b = pair / a.parts / a.H_kv, h = pair / a.parts % a.H_kv;
+  const int heads = a.share / a.parts, q_head = h * a.share + part * heads;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n_q = valid_rows(a.q_len, b, a.Tq), n_k = valid_rows(a.k_len, b, a.Tk), shift = n_k - n_q;
   const int key0 = block * 32 * NW, own0 = key0 + 32 * wave, key = own0 + (lane & 31);
@@ -191,10 +195,10 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DT, DP)) attention_ke
   read.init(lds, lane);
   const unsigned own_values = 2 * STAGE + wave * (32 * HeadTile<DT, DP>::ROW_BYTES);
   Loader q_tiles, d_tiles;
-  q_tiles.init(static_cast<const E*>(a.q) + b * a.qs.sample + h * a.share * a.qs.head, a.qs.token, a.D, wave, lane);
-  d_tiles.init(static_cast<const E*>(a.dout) + b * a.os.sample + h * a.share * a.os.head, a.os.token, a.D, wave, lane);
-  int64_t corr = ((int64_t)b * a.H + h * a.share) * a.Tq;
-  // Tiles of all query heads of the key head, one behind the other; first row of the one that is loaded next.
+  q_tiles.init(static_cast<const E*>(a.q) + b * a.qs.sample + q_head * a.qs.head, a.qs.token, a.D, wave, lane);
+  d_tiles.init(static_cast<const E*>(a.dout) + b * a.os.sample + q_head * a.os.head, a.os.token, a.D, wave, lane);
+  int64_t corr = ((int64_t)b * a.H + q_head) * a.Tq;
+  // Tiles of the part's query heads, one behind the other; first row of the one that is loaded next.
   int next_row = begin;
   auto load = [&](int stage) {
     const unsigned to = lds + stage * STAGE;
@@ -251,7 +255,7 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DT, DP)) attention_ke
   f32x16 dk[CB], dv[CB];
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb) dk[cb] = dv[cb] = zeros16();
-  const int steps = tiles * a.share;
+  const int steps = tiles * heads;
   if (steps > 0) load(0);
   int first = begin;                              // of the tile at hand
   two_stages(steps, [&](int t, auto stage) {
@@ -299,13 +303,42 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DT, DP)) attention_ke
             });
   });
   tiles_landed();                                 // LDS is free
-  const unsigned own_rows = lds + wave * 32 * HeadTile<DT, DP>::ROW_BYTES;
-  store_rows<DT, DP>(dk, a.scale, key < n_k, static_cast<E*>(a.dk) + kv, a.ks.token, own0, a.Tk, a.D, own_rows, lane);
-  store_rows<DT, DP>(dv, 1.f, key < n_k, static_cast<E*>(a.dv) + vv, a.vs.token, own0, a.Tk, a.D, own_rows, lane);
+  float *dk_part = nullptr, *dv_part = nullptr;
+  if (a.parts > 1) {
+    dk_part = a.partial + (((int64_t)part * a.B + b) * a.H_kv + h) * a.Tk * a.D;
+    dv_part = dk_part + (int64_t)a.parts * a.B * a.H_kv * a.Tk * a.D;
+    store_partial<DP>(dk, key < n_k, dk_part, key, a.Tk, a.D, lane);
+    store_partial<DP>(dv, key < n_k, dv_part, key, a.Tk, a.D, lane);
+  } else {
+    const unsigned own_rows = lds + wave * 32 * HeadTile<DT, DP>::ROW_BYTES;
+    store_rows<DT, DP>(dk, a.scale, key < n_k, static_cast<E*>(a.dk) + kv, a.ks.token, own0, a.Tk, a.D, own_rows, lane);
+    store_rows<DT, DP>(dv, 1.f, key < n_k, static_cast<E*>(a.dv) + vv, a.vs.token, own0, a.Tk, a.D, own_rows, lane);
+  }
   if (a.causal && __any(key < n_k && (not_finite(dk) || not_finite(dv)))) {
     const AttnRows<E> rows(a, reinterpret_cast<float*>(smem + wave * 32 * HeadTile<DT, DP>::ROW_BYTES), b, h, lane);
-    for (int j = own0; j < min(own0 + 32, n_k); ++j) rows.key_gradient(j);
+    for (int j = own0; j < min(own0 + 32, n_k); ++j) rows.key_gradient(j, q_head, q_head + heads, dk_part, dv_part);
   }
+}
+
+// dk and dv from the parts' sums, in their order; four columns a thread.
+template <class E>
+__global__ void __launch_bounds__(256) attention_join_kernel(const AttnArgs a, int64_t pieces) {
+  typedef __attribute__((ext_vector_type(4))) E E4;
+  const int64_t id = ((int64_t)a.first + blockIdx.x) * 256 + threadIdx.x;
+  if (id >= 2 * pieces) return;
+  const bool values = id >= pieces;
+  const int64_t at = values ? id - pieces : id, size = 4 * pieces;              // elements of a part
+  const float* p = a.partial + (values ? size * a.parts : 0) + 4 * at;
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int part = 0; part < a.parts; ++part) sum += *reinterpret_cast<const f32x4*>(p + part * size);
+  const int64_t row = 4 * at / a.D;                                             // of [B][H_kv][Tk]
+  const int col = (int)(4 * at - row * a.D), j = (int)(row % a.Tk), h = (int)(row / a.Tk % a.H_kv), b = (int)(row / a.Tk / a.H_kv);
+  const AttnSide& s = values ? a.vs : a.ks;
+  const float f = values ? 1.f : a.scale;
+  E4 y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = (E)(sum[i] * f);
+  *reinterpret_cast<E4*>(static_cast<E*>(values ? a.dv : a.dk) + b * s.sample + h * s.head + j * s.token + col) = y;
 }
 
 __global__ void __launch_bounds__(256) attention_query_grad_rows_kernel(const AttnArgs a) {
@@ -325,7 +358,7 @@ __global__ void __launch_bounds__(256) attention_key_grad_rows_kernel(const Attn
   __shared__ __align__(16) float own[4 * kRowFloats];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), j = block * 4 + wave;
   const AttnRows<float> rows(a, own + wave * kRowFloats, pair / a.H_kv, pair % a.H_kv, threadIdx.x & 63);
-  if (j < a.Tk) rows.key_gradient(j);
+  if (j < a.Tk) rows.key_gradient(j, rows.h * a.share, (rows.h + 1) * a.share, nullptr, nullptr);
 }
 
 template <int DT, int DP, int NW>
@@ -344,16 +377,21 @@ dp_status launch_queries(AttnArgs a, hipStream_t s) {
 
 template <int DT, int DP, int NW>
 dp_status launch_keys(AttnArgs a, hipStream_t s) {
-  a.heads = a.B * a.H_kv;
+  a.heads = a.B * a.H_kv * a.parts;
   a.blocks = (a.Tk + 32 * NW - 1) / (32 * NW);
   constexpr int LDS = 2 * (2 * kRows * HeadTile<DT, DP>::ROW_BYTES + 512) + (values_in_lds(DT, DP) ? 32 * NW * HeadTile<DT, DP>::ROW_BYTES : 0);
   auto kernel = attention_key_grad_kernel<DT, DP, NW>;
   static ReadyTable done;
-  if (LDS > 65536) {
-    const dp_status st = allow_big_lds(kernel, LDS, done);
-    if (st != DP_OK) return st;
-  }
-  return launch_attention(kernel, a, (int64_t)2 * Ops<DT>::SIZE * a.Tq * a.D * a.share, 64 * NW, LDS, s);
+  dp_status st = DP_OK;
+  if (LDS > 65536) st = allow_big_lds(kernel, LDS, done);
+  if (st == DP_OK) st = launch_attention(kernel, a, (int64_t)2 * Ops<DT>::SIZE * a.Tq * a.D * (a.share / a.parts), 64 * NW, LDS, s);
+  if (st != DP_OK || a.parts == 1) return st;
+  const int64_t pieces = (int64_t)a.B * a.H_kv * a.Tk * a.D / 4;
+  return launch_in_runs((2 * pieces + 255) / 256, [&](dim3 grid, int first) {
+    AttnArgs run = a;
+    run.first = (unsigned)first;
+    hipLaunchKernelGGL(attention_join_kernel<typename Ops<DT>::E>, grid, dim3(256), 0, s, run, pieces);
+  });
 }
 
 template <int DT, int DP>
@@ -373,6 +411,22 @@ dp_status launch(const AttnArgs& a, hipStream_t s) {
 }
 
 }  // namespace
+
+// Where key heads are few, a workgroup to each of their blocks leaves compute units idle while it goes through its query heads one after the
+// other: these are dealt to several, in as many parts as fill the units, whose sums are then joined.  2 x 128 tokens, fp32, 48 heads of
+// 128 that share 6: 312 us in one part.
+int attention_parts(const AttnArgs& a) {
+  const int64_t units = (int64_t)a.B * a.H_kv * ((a.Tk + 127) / 128);
+  int parts = 1;
+  for (int p = 2; p <= a.share && units * parts < kPartUnits; ++p)
+    if (a.share % p == 0) parts = p;
+  return parts;
+}
+
+int64_t attention_partial_floats(const AttnArgs& a) {
+  const int parts = attention_parts(a);
+  return parts > 1 ? (int64_t)2 * parts * a.B * a.H_kv * a.Tk * a.D : 0;
+}
 
 dp_status launch_attention_backward(const AttnArgs& args, dp_dtype dt, hipStream_t s) {
   if (dt == DP_BF16) return launch<DP_BF16>(args, s);

@@ -63,6 +63,13 @@ dp_status attention_args(const dp_attention_shape* p, dp_dtype dt, AttnArgs& a) 
   return DP_OK;
 }
 
+// The backward pass's workspace: rows' corrections, in whole 16 bytes, then partial sums.
+int64_t padded_rows(const AttnArgs& a) { return ((int64_t)2 * a.B * a.H * a.Tq + 3) / 4 * 4; }
+int parts_of(const AttnArgs& a, dp_dtype dt) { return dt != DP_F32 || whole_pieces(a) ? attention_parts(a) : 1; }
+size_t backward_workspace(const AttnArgs& a, dp_dtype dt) {
+  return (size_t)(padded_rows(a) + (parts_of(a, dt) > 1 ? attention_partial_floats(a) : 0)) * sizeof(float);
+}
+
 template <class... P>
 bool all_there(P... p) {
   return ((p && aligned(p, 16)) && ...);
@@ -144,7 +151,7 @@ dp_status dp_attention(const dp_attention_shape* shape, dp_dtype dt, const void*
 
 size_t dp_attention_backward_workspace_bytes(const dp_attention_shape* shape, dp_dtype dt) {
   AttnArgs a;
-  return attention_args(shape, dt, a) == DP_OK ? (size_t)2 * a.B * a.H * a.Tq * sizeof(float) : 0;
+  return attention_args(shape, dt, a) == DP_OK ? backward_workspace(a, dt) : 0;
 }
 
 dp_status dp_attention_backward(const dp_attention_shape* shape, dp_dtype dt, const void* q, const void* k, const void* v,
@@ -155,7 +162,7 @@ dp_status dp_attention_backward(const dp_attention_shape* shape, dp_dtype dt, co
   if (st != DP_OK) return st;
   if (!all_there(q, k, v, o, dout, dq, dk, dv) || !lse || !aligned(lse, 4)) return DP_ERR_INVALID_ARG;
   const int64_t rows = (int64_t)a.B * a.H * a.Tq;
-  if (!ws || ws_bytes < (size_t)2 * rows * sizeof(float)) return DP_ERR_WORKSPACE;
+  if (!ws || ws_bytes < backward_workspace(a, dt)) return DP_ERR_WORKSPACE;
   if (!aligned(ws, 16)) return DP_ERR_INVALID_ARG;
   a.q = q;
   a.k = k;
@@ -168,6 +175,8 @@ dp_status dp_attention_backward(const dp_attention_shape* shape, dp_dtype dt, co
   a.dv = dv;
   a.lse2 = static_cast<float*>(ws);
   a.delta = a.lse2 + rows;
+  a.parts = parts_of(a, dt);
+  a.partial = a.lse2 + padded_rows(a);
   return launch_attention_backward(a, dt, static_cast<hipStream_t>(stream));
 }
 
