@@ -444,14 +444,16 @@ dp_status dp_layer_norm_backward(const void* x, const void* dy, const void* add,
  *   Heads: H_kv divides H; query heads h share key head h / (H / H_kv).
  *   Layout: element strides of sample, token and head, for q, k, v and o; columns are adjacent.  Packed projections ([B, T, 3 * H * D] and
  *     the like) need no copies.  Strides are >= 0 and, for 16-bit types, multiples of 8; a token stride is from D to 2^23 (of one
- *     token: whatever).
+ *     token: whatever).  What is read may be broadcast (stride 0); what is written may not overlap itself: by growing stride, each
+ *     axis steps over all that the ones before span (DP_ERR_INVALID_ARG else; the gradients have the strides of q, k and v).
  *   Lengths: q_len[b] queries and k_len[b] keys of sample b are there (device, [B] int32; NULL: all; values are held to 0 .. T).
  *     What lies behind them is not read.
  *   causal = 1: the ends are aligned; row i sees keys up to i + (keys there) - (queries there).
  * Rows that see no key, and rows that are not there, are zeros, with lse = -infinity.  What a row does not see does not reach
  * it, infinities and NaN included.
- * D is at most 128 and, for 16-bit types, a multiple of 8.  16-bit types run on the matrix cores, with probabilities rounded to the
- * type before their product with v; DP_F32 runs on the vector units, for small networks.  scale is positive and finite.
+ * D is at most 128 and, for 16-bit types, a multiple of 8.  All types run on the matrix cores, 16-bit ones with
+ * probabilities rounded to the type before their product with v; DP_F32 whose D or strides are not multiples of 4, or whose arrays are not 16-byte aligned, runs on the vector
+ * units, for small networks.  scale is positive and finite.
  */
 typedef struct {
   int32_t B, H, H_kv, Tq, Tk, D;
@@ -464,7 +466,7 @@ typedef struct {
 
 /*
  *   shape     HOST
- *   q, k, v, o   device, of type dt, 16-byte aligned
+ *   q, k, v, o   device, of type dt, 16-byte aligned (DP_F32: 4-byte; the matrix cores want 16)
  *   lse       device, [B, H, Tq] fp32, kept for the backward pass
  */
 dp_status dp_attention(const dp_attention_shape* shape, dp_dtype dt, const void* q, const void* k, const void* v, void* o, float* lse,

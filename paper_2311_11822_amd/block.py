@@ -23,12 +23,29 @@ def _same(name: str, x: Optional[torch.Tensor], shape, dtype, device) -> None:
         raise ValueError(f"{name}: contiguous {tuple(shape)} of {dtype} on {device}, not {tuple(x.shape)} of {x.dtype} on {x.device}")
 
 
+class _Workspaces:
+    """Scratch memory, one for each device and stream (calls on different streams do not share one) that grows as calls need."""
+
+    def __init__(self):
+        self.held = {}
+
+    def __call__(self, nbytes: int, device: torch.device, index: int, stream: int) -> torch.Tensor:
+        ws = self.held.get((index, stream))
+        if ws is None or ws.numel() < nbytes:
+            # of that stream's own memory: what is given back is not handed to another stream while calls still use it
+            current = torch.cuda.current_stream(device)
+            own = current if current.cuda_stream == stream else torch.cuda.ExternalStream(stream, device)
+            with torch.cuda.stream(own):
+                ws = self.held[index, stream] = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        return ws
+
+
 class LayerNorm:
     """gain, bias: [d] float32, or None (ones, zeros)."""
 
     def __init__(self, gain: Optional[torch.Tensor], bias: Optional[torch.Tensor], eps: float = 1e-5):
         self.gain, self.bias, self.eps = gain, bias, eps
-        self._ws = {}                  # by shape and stream: calls on different streams do not share a workspace
+        self._ws, self._need = _Workspaces(), {}
 
     def _check(self, x, like, rows, floats):
         """Tensors of x's shape and type, [B, T] float32 ones, and others by (tensor, number of values); written out, for a call of a
@@ -46,6 +63,8 @@ class LayerNorm:
         for t, n in floats:
             if t is not None and (t.numel() != n or t.dtype is not torch.float32 or t.get_device() != device or not t.is_contiguous()):
                 raise ValueError(f"{n} contiguous float32 values on {x.device}, not {tuple(t.shape)} of {t.dtype} on {t.device}")
+        if device < 0:
+            raise ValueError(f"tensors on a GPU, not {x.device}")
         return _dtype(x), B, T, d
 
     def forward(self, x, y, mean=None, rstd=None, add=None, sum=None, stream=None) -> None:
@@ -62,13 +81,12 @@ class LayerNorm:
         ws = None
         if kept is not None:
             stream = dp._stream(stream)
-            key = (dt, B, T, d, x.get_device(), stream)
-            ws = self._ws.get(key)
-            if ws is None:
-                n = dp.dp_layer_norm_workspace_bytes(dt, B, T, d)
-                if n == 0:
+            need = self._need.get((dt, B, T, d))
+            if need is None:
+                need = self._need[dt, B, T, d] = dp.dp_layer_norm_workspace_bytes(dt, B, T, d)
+                if need == 0:
                     raise dp.DpError(dp.DP_ERR_UNSUPPORTED, "dp_layer_norm_workspace_bytes")
-                ws = self._ws[key] = torch.empty(n, dtype=torch.uint8, device=x.device)
+            ws = self._ws(need, x.device, x.get_device(), stream)
         dp.dp_layer_norm_backward(x, dy, add, dt, B, T, d, self.gain, mean, rstd, dx, kept, sqnorm, ws, stream)
 
     @staticmethod
@@ -100,7 +118,11 @@ class Attention:
         strides = [[st if n > 1 else 0 for n, st in zip(t.shape[:3], t.stride()[:3])] for t in (q, k, v, o)]
         self.shape = dp.attention_shape(B, H, H_kv, Tq, Tk, D, causal, scale, *strides, q_len, k_len)
         self._check((q, o), (k, v), (q, k, v, o), None)
-        self._ws = {}
+        self._ws, self._need = _Workspaces(), dp.dp_attention_backward_workspace_bytes(self.shape, self.dt)
+        if self._need == 0:
+            raise ValueError("sizes, strides or scale that attention does not take")
+        if self.index < 0:
+            raise ValueError(f"tensors on a GPU, not {q.device}")
 
     def _check(self, of_queries, of_keys, four, lse):
         """of_queries, of_keys: by shape and type; four: in the strides of q, k, v and o."""
@@ -126,12 +148,7 @@ class Attention:
         self._check((q, o, do, dq), (k, v, dk, dv), (q, k, v, o), lse)
         self._check((), (), (dq, dk, dv, do), None)
         stream = dp._stream(stream)
-        ws = self._ws.get(stream)
-        if ws is None:                                    # calls on different streams do not share a workspace
-            n = dp.dp_attention_backward_workspace_bytes(self.shape, self.dt)
-            if n == 0:
-                raise dp.DpError(dp.DP_ERR_UNSUPPORTED, "dp_attention_backward_workspace_bytes")
-            ws = self._ws[stream] = torch.empty(n, dtype=torch.uint8, device=self.device)
+        ws = self._ws(self._need, self.device, self.index, stream)
         dp.dp_attention_backward(self.shape, self.dt, q, k, v, o, lse, do, dq, dk, dv, ws, stream)
 
 
@@ -165,6 +182,8 @@ class AdamW:
                 want = -(-size // 256) if k in (4, 5) else size
                 if t is not None and (t.dtype != kind or t.device != device or t.numel() != want or not t.is_contiguous()):
                     raise ValueError(f"{name}: contiguous, {want} values of {kind} on {device}")
+        if device.type != "cuda":
+            raise ValueError(f"tensors on a GPU, not {device}")
         self.tensors = dp.adamw_tensors([(*tensors, tensors[0].numel(), d) for tensors, d in zip(self.held, decay)])
 
     def step(self, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, grad_scale: float = 1.0,

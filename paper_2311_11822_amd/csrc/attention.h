@@ -43,6 +43,13 @@ struct AttnArgs {
   unsigned first;                 // number of the launch's first workgroup
 };
 
+// Arrays that begin at 16 bytes (16-bit ones always do).
+__host__ __device__ inline bool aligned_arrays(const AttnArgs& a) {
+  return ((uintptr_t)a.q & 15) == 0 && ((uintptr_t)a.k & 15) == 0 && ((uintptr_t)a.v & 15) == 0 && ((uintptr_t)a.o & 15) == 0 &&
+         ((uintptr_t)a.out & 15) == 0 && ((uintptr_t)a.dout & 15) == 0 && ((uintptr_t)a.dq & 15) == 0 &&
+         ((uintptr_t)a.dk & 15) == 0 && ((uintptr_t)a.dv & 15) == 0;
+}
+
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // Operands and products by storage type DT.  A row operand is 16 bytes of a row, EL columns to each lane half: one matrix instruction of
@@ -418,7 +425,7 @@ struct AttnRows {
     n_k = valid_rows(a.k_len, b, a.Tk);
     const int64_t all = a.D | a.qs.sample | a.qs.token | a.qs.head | a.ks.sample | a.ks.token | a.ks.head | a.vs.sample | a.vs.token |
                         a.vs.head | a.os.sample | a.os.token | a.os.head;
-    whole = (all & 3) == 0;
+    whole = (all & 3) == 0 && aligned_arrays(a);
   }
   __device__ const E* query(const void* t, const AttnSide& s, int head) const { return (const E*)t + b * s.sample + head * s.head; }
   __device__ int keys_of(int i) const {         // row i sees keys below this
@@ -523,7 +530,7 @@ inline bool whole_pieces(const AttnArgs& a) {
   const AttnSide* sides[] = {&a.qs, &a.ks, &a.vs, &a.os};
   int64_t all = a.D;
   for (const AttnSide* s : sides) all |= s->sample | s->token | s->head;
-  return all % 4 == 0;
+  return all % 4 == 0 && aligned_arrays(a);
 }
 
 // Launches `blocks` of a.heads pairs, in runs below the grid's limit.

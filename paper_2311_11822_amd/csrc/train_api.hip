@@ -2,6 +2,8 @@
 // host, before anything is launched.
 #include <math.h>
 
+#include <algorithm>
+
 #include "attention.h"
 #include "train.h"
 
@@ -70,10 +72,24 @@ size_t backward_workspace(const AttnArgs& a, dp_dtype dt) {
   return (size_t)(padded_rows(a) + (parts_of(a, dt) > 1 ? attention_partial_floats(a) : 0)) * sizeof(float);
 }
 
-template <class... P>
-bool all_there(P... p) {
-  return ((p && aligned(p, 16)) && ...);
+// No two elements of an array that is written share a place: by growing stride, each axis steps over all that the ones before span.
+bool apart(const AttnSide& s, int B, int T, int H, int D) {
+  struct { int64_t stride, n; } axes[] = {{s.sample, B}, {s.token, T}, {s.head, H}};
+  std::sort(axes, axes + 3, [](const auto& a, const auto& b) { return a.stride < b.stride; });
+  int64_t span = D;
+  for (const auto& axis : axes) {
+    if (axis.n == 1) continue;
+    if (axis.stride < span) return false;
+    span += axis.stride * (axis.n - 1);
+  }
+  return true;
 }
+
+template <class... P>
+bool all_there(uintptr_t to, P... p) {
+  return ((p && aligned(p, to)) && ...);
+}
+uintptr_t attention_alignment(dp_dtype dt) { return dt == DP_F32 ? 4 : 16; }
 
 }  // namespace
 
@@ -81,7 +97,7 @@ extern "C" {
 
 dp_status dp_layer_norm(const void* x, const void* add, dp_dtype dt, int B, int T, int d, const float* gain, const float* bias,
                         float eps, void* sum, void* y, float* mean, float* rstd, void* stream) {
-  if (!all_there(x, y) || !aligned(add, 16) || !aligned(sum, 16) || !add != !sum) return DP_ERR_INVALID_ARG;
+  if (!all_there(16, x, y) || !aligned(add, 16) || !aligned(sum, 16) || !add != !sum) return DP_ERR_INVALID_ARG;
   if (!aligned(gain, 4) || !aligned(bias, 4) || !aligned(mean, 4) || !aligned(rstd, 4)) return DP_ERR_INVALID_ARG;
   if (!(eps >= 0.f) || isinf(eps)) return DP_ERR_INVALID_ARG;
   const dp_status st = norm_shape(dt, B, T, d);
@@ -109,7 +125,7 @@ size_t dp_layer_norm_workspace_bytes(dp_dtype dt, int B, int T, int d) {
 dp_status dp_layer_norm_backward(const void* x, const void* dy, const void* add, dp_dtype dt, int B, int T, int d, const float* gain,
                                  const float* mean, const float* rstd, void* dx, float* kept, float* sqnorm_out, void* ws,
                                  size_t ws_bytes, void* stream) {
-  if (!all_there(x, dy) || !mean || !rstd || (!dx && !kept) || !kept != !sqnorm_out || (add && !dx)) return DP_ERR_INVALID_ARG;
+  if (!all_there(16, x, dy) || !mean || !rstd || (!dx && !kept) || !kept != !sqnorm_out || (add && !dx)) return DP_ERR_INVALID_ARG;
   if (!aligned(add, 16) || !aligned(dx, 16) || !aligned(kept, 16)) return DP_ERR_INVALID_ARG;
   if (!aligned(gain, 4) || !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(sqnorm_out, 4)) return DP_ERR_INVALID_ARG;
   const dp_status st = norm_shape(dt, B, T, d);
@@ -140,7 +156,7 @@ dp_status dp_attention(const dp_attention_shape* shape, dp_dtype dt, const void*
   AttnArgs a;
   const dp_status st = attention_args(shape, dt, a);
   if (st != DP_OK) return st;
-  if (!all_there(q, k, v, o) || !lse || !aligned(lse, 4)) return DP_ERR_INVALID_ARG;
+  if (!all_there(attention_alignment(dt), q, k, v, o) || !lse || !aligned(lse, 4) || !apart(a.os, a.B, a.Tq, a.H, a.D)) return DP_ERR_INVALID_ARG;
   a.q = q;
   a.k = k;
   a.v = v;
@@ -160,7 +176,10 @@ dp_status dp_attention_backward(const dp_attention_shape* shape, dp_dtype dt, co
   AttnArgs a;
   const dp_status st = attention_args(shape, dt, a);
   if (st != DP_OK) return st;
-  if (!all_there(q, k, v, o, dout, dq, dk, dv) || !lse || !aligned(lse, 4)) return DP_ERR_INVALID_ARG;
+  if (!all_there(attention_alignment(dt), q, k, v, o, dout, dq, dk, dv) || !lse || !aligned(lse, 4))
+    return DP_ERR_INVALID_ARG;
+  if (!apart(a.qs, a.B, a.Tq, a.H, a.D) || !apart(a.ks, a.B, a.Tk, a.H_kv, a.D) || !apart(a.vs, a.B, a.Tk, a.H_kv, a.D))
+    return DP_ERR_INVALID_ARG;
   const int64_t rows = (int64_t)a.B * a.H * a.Tq;
   if (!ws || ws_bytes < backward_workspace(a, dt)) return DP_ERR_WORKSPACE;
   if (!aligned(ws, 16)) return DP_ERR_INVALID_ARG;

@@ -320,6 +320,66 @@ def test_attention_layouts(block, dtype):
         assert all(torch.equal(x, y) for x, y in zip(grads, want[2]))
 
 
+# Widths and strides that are no multiples of 4, in fp32: rows are read an element at a time.  (The odd stride lies in the samples.)
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("shape", [(1, 1, 1, 1, 1, 1), (2, 7, 7, 2, 1, 3), (2, 33, 33, 3, 3, 18), (1, 70, 45, 2, 2, 30), (1, 5, 130, 4, 1, 127),
+                                   (2, 40, 40, 2, 2, 66), (1, 64, 64, 6, 2, 9)], ids=str)
+def test_attention_odd_widths(block, shape, causal):
+    Case(block, "f32", *shape, causal).check()
+
+
+def test_attention_odd_strides(block):
+    base = Case(block, "f32", 2, 70, 70, 2, 2, 32, True)
+    want = base.run()
+    place = lambda: torch.zeros(2 * (70 * 64 + 3), device="cuda").as_strided((2, 70, 2, 32), (70 * 64 + 3, 64, 32, 1))  # noqa: E731
+    views, o, do, lse = [place() for _ in range(3)], place(), place(), torch.empty((2, 2, 70), device="cuda")
+    for to, t in zip((*views, do), (base.q, base.k, base.v, base.do)):
+        to.copy_(t)
+    at = block.Attention(*views, o, True, base.scale)
+    at.forward(*views, o, lse)
+    grads = [place() for _ in range(3)]
+    at.backward(*views, o, lse, do, *grads)
+    for got, ref in zip((o, lse, *grads), (want[0], want[1], *want[2])):
+        assert rel(got, ref) <= 2 * FP32                                    # both sides within FP32 of the same
+
+
+# Few key heads that many query heads share: the heads' sums are formed in parts and joined.
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("shape", [(1, 33, 33, 6, 1, 64), (1, 128, 128, 7, 1, 128), (1, 100, 260, 12, 2, 32), (2, 20, 20, 48, 6, 96),
+                                   (1, 1, 1, 8, 2, 64), (3, 65, 65, 10, 1, 40), (1, 257, 257, 9, 3, 64)], ids=str)
+@pytest.mark.parametrize("causal", [False, True])
+def test_attention_shared_heads_in_parts(block, dtype, shape, causal):
+    Case(block, dtype, *shape, causal).check()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_attention_shared_heads_in_parts_ignore_what_is_not_seen(block, dtype):
+    c = Case(block, dtype, 2, 90, 90, 8, 1, 64, True, q_len=[0, 61], k_len=[90, 77])
+    for t in (c.q, c.do):
+        t[0], t[1, 61:] = math.nan, math.inf
+    for t in (c.k, c.v):
+        t[1, 77:] = math.nan
+    c.check()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_attention_of_broadcast_inputs(block, dtype):
+    """One sample's keys and one head's queries for all: read where they are; gradients in such layouts are refused."""
+    gen = torch.Generator().manual_seed(5)
+    q = rand(gen, (2, 40, 1, 32), dtype).cuda().expand(2, 40, 4, 32)
+    k, v = (rand(gen, (1, 50, 2, 32), dtype).cuda().expand(2, 50, 2, 32) for _ in range(2))
+    out = []
+    for views in ((q, k, v), (q.contiguous(), k.contiguous(), v.contiguous())):
+        o, lse = torch.empty((2, 40, 4, 32), dtype=q.dtype, device="cuda"), torch.empty((2, 4, 40), device="cuda")
+        at = block.Attention(*views, o, True, 0.2)
+        at.forward(*views, o, lse)
+        out.append((o, lse))
+        if views[0] is q:
+            with pytest.raises(block.dp.DpError):
+                at.backward(*views, o, lse, torch.empty_like(o), *views)
+    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
+
+
 def test_attention_gradient_against_differences(block):
     """A directional derivative of the fp32 forward pass against the gradients."""
     gen = torch.Generator().manual_seed(11)
@@ -514,3 +574,69 @@ def test_on_another_stream(block):
         got = c.run()
     stream.synchronize()
     assert torch.equal(got[0], want[0]) and all(torch.equal(x, y) for x, y in zip(got[2], want[2]))
+
+
+def test_replayed_in_a_graph(block):
+    """Norm and attention, forward and backward, captured once and replayed on new inputs, with eager calls in between."""
+    B, T, H, D = 2, 150, 6, 32
+    d = H * D
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    new = lambda *s, dt=torch.bfloat16: torch.empty(s, dtype=dt, device="cuda")  # noqa: E731
+    f = torch.float32
+    x, add, total, y, dx = (new(B, T, d) for _ in range(5))
+    mean, rstd, kept, sq = new(B, T, dt=f), new(B, T, dt=f), new(B, 2, d, dt=f), new(B, dt=f)
+    kv, dkv, o, do, dq, lse = new(B, T, 2, 1, D), new(B, T, 2, 1, D), new(B, T, H, D), new(B, T, H, D), new(B, T, H, D), new(B, H, T, dt=f)
+    norm = block.LayerNorm(torch.ones(d, device="cuda"), torch.zeros(d, device="cuda"))
+    q, (k, v), (dk, dv) = y.view(B, T, H, D), kv.unbind(2), dkv.unbind(2)
+    at = block.Attention(q, k, v, o, True, D ** -0.5)
+
+    def run():
+        norm.forward(x, y, mean, rstd, add, total)
+        at.forward(q, k, v, o, lse)
+        at.backward(q, k, v, o, lse, do, dq, dk, dv)
+        norm.backward(total, dq.view(B, T, d), mean, rstd, dx, kept, sq, add)
+
+    def fill():
+        for t in (x, add, kv, do):
+            t.copy_(torch.randn(t.shape, generator=gen, device="cuda"))
+
+    outputs = (total, y, mean, rstd, o, lse, dq, dkv, dx, kept, sq)
+    fill()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()                                             # workspaces are there before the capture
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        run()
+    for _ in range(4):
+        fill()
+        for t in outputs:
+            t.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in outputs]
+        run()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, outputs))
+
+
+def test_workspaces_grow_and_follow_streams(block):
+    """One object on calls of growing and shrinking sizes, on its own stream, another one, and one given by its handle."""
+    gen = torch.Generator().manual_seed(4)
+    norm = block.LayerNorm(None, None)
+    streams = [None, torch.cuda.Stream(), torch.cuda.Stream().cuda_stream]
+    for T in (40, 400, 7, 1000):
+        x, dy = (rand(gen, (3, T, 96), "f32").cuda() for _ in range(2))
+        mean, rstd = torch.empty((3, T), device="cuda"), torch.empty((3, T), device="cuda")
+        norm.forward(x, torch.empty_like(x), mean, rstd)
+        torch.cuda.synchronize()
+        out = []
+        for stream in streams:
+            dx, kept, sq = torch.empty_like(x), torch.empty((3, 2, 96), device="cuda"), torch.empty(3, device="cuda")
+            torch.cuda.synchronize()
+            norm.backward(x, dy, mean, rstd, dx, kept, sq, stream=stream)
+            torch.cuda.synchronize()
+            out.append((dx, kept, sq))
+        assert all(torch.equal(a, b) for other in out[1:] for a, b in zip(other, out[0]))
