@@ -121,6 +121,23 @@ __device__ __forceinline__ void decode(float (&x)[4], uint32_t w, float scale) {
   x[3] = hi[1] * scale;
 }
 
+// A wave's 8-bit step is bound by its instructions, divisions and square roots for the most part, which as the compiler has them
+// serve all of fp32's range.  These round as they do, to nearest even, where nothing is lost below fp32's smallest numbers: the remainder
+// of a quotient (or of a root's square) is exact there.
+__device__ __forceinline__ float reciprocal(float d) {
+  const float r = __builtin_amdgcn_rcpf(d);
+  return fmaf(fmaf(-d, r, 1.f), r, r);
+}
+__device__ __forceinline__ float divide(float n, float d, float r) {          // r: reciprocal(d)
+  const float q = n * r;
+  return fmaf(fmaf(-d, q, n), r, q);
+}
+__device__ __forceinline__ float root_of(float x) {                            // 0, or from 2^-96 on; the instruction is off by a unit at most
+  const float s = __builtin_amdgcn_sqrtf(x), down = __uint_as_float(__float_as_uint(s) - 1), up = __uint_as_float(__float_as_uint(s) + 1);
+  const float to_down = fmaf(-down, s, x), to_up = fmaf(-up, s, x);
+  return to_up > 0.f ? up : to_down <= 0.f ? down : s;
+}
+
 // Codes of a block of 256 values (four to a lane) and its scale.  dither: in [0, 1), a value for each element.
 template <bool ROOT>
 __device__ __forceinline__ uint32_t encode(const float (&x)[4], const float (&dither)[4], float& scale) {
@@ -131,12 +148,21 @@ __device__ __forceinline__ uint32_t encode(const float (&x)[4], const float (&di
   for (int off = 32; off > 0; off >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off));
   scale = __uint_as_float(top) * (1.f / 448.f);
   const float unit = scale > 0.f ? scale : 1.f;
-  float c[4];
+  float c[4], quotient[4];
+  if (__builtin_amdgcn_readfirstlane(unit > 0x1p-60f && unit < 0x1p60f)) {
+    const float r = reciprocal(unit);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) quotient[i] = divide(fabsf(x[i]), unit, r);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) quotient[i] = fabsf(x[i]) / unit;
+  }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const float a = fabsf(x[i]) / unit;
+    const float a = quotient[i];
     const int e = max(__builtin_amdgcn_frexp_expf(a) - 1, -6) - 3;
-    const float y = ldexpf(a, -e), low = floorf(y), rest = ROOT ? (y - low) * (y + low) / (2.f * low + 1.f) : y - low;
+    const float y = ldexpf(a, -e), low = floorf(y), between = 2.f * low + 1.f;
+    const float rest = ROOT ? divide((y - low) * (y + low), between, reciprocal(between)) : y - low;
     const float q = ldexpf(low + floorf(rest + dither[i]), e);
     c[i] = a > 0.f ? copysignf(fminf(fmaxf(q, 0x1p-9f), 448.f), x[i]) : 0.f;
   }
@@ -170,15 +196,30 @@ struct Block {
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[i] *= v[i];
     }
-    float root[4];
+    float root[4], fixed[4];                       // roots of v and of v / (1 - beta2^t)
+    uint32_t least = ~0u;                          // of v but zeros
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float gi = g[i] * a.grad_scale;
-      m[i] = a.beta1 * m[i] + a.rest1 * gi;
-      v[i] = a.beta2 * v[i] + a.rest2 * gi * gi;
-      root[i] = sqrtf(v[i]);
-      w[i] = w[i] * t.keep - a.lr * (m[i] * a.fix1 / (sqrtf(v[i] * a.fix2) + a.eps));
+      g[i] *= a.grad_scale;
+      m[i] = a.beta1 * m[i] + a.rest1 * g[i];
+      v[i] = a.beta2 * v[i] + a.rest2 * g[i] * g[i];
+      least = min(least, __float_as_uint(v[i]) - 1);
     }
+    if (BITS == 8 && !__any(least < __float_as_uint(0x1p-96f) - 1)) {          // (fix2 is at least 1)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        root[i] = root_of(v[i]);
+        fixed[i] = root_of(v[i] * a.fix2);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        root[i] = sqrtf(v[i]);
+        fixed[i] = sqrtf(v[i] * a.fix2);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = w[i] * t.keep - a.lr * (m[i] * a.fix1 / (fixed[i] + a.eps));
     store4<VEC>(w, t.param, at, lane, left);
     if constexpr (COPY != DP_F32) {
       uint16_t* c = static_cast<uint16_t*>(t.copy) + at;
