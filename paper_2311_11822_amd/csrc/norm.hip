@@ -14,29 +14,43 @@ namespace {
 
 constexpr int kThreads = 512;
 
-// P values a thread as VEC-wide pieces: piece n of thread t holds columns VEC (n TPR + t) ...
+// P values a thread as pieces of VEC: piece n of thread t holds columns VEC (n TPR + t) ...
 template <int DT, int VEC>
-struct Piece {                                     // VEC values as stored
-  static constexpr int WORDS = DT == DP_F32 ? VEC : (VEC + 1) / 2;
+struct Piece {                                     // VEC values as stored, 16 bytes
+  static constexpr int WORDS = 4, SIZE = DT == DP_F32 ? 4 : 2;
   uint32_t w[WORDS];
   __device__ __forceinline__ void load(const void* base, int64_t at) {
-    if constexpr (DT != DP_F32 && VEC == 1) {
-      w[0] = static_cast<const uint16_t*>(base)[at];
-    } else if constexpr (WORDS == 1) {
-      w[0] = static_cast<const uint32_t*>(base)[at];
-    } else {
-      const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const char*>(base) + at * (DT == DP_F32 ? 4 : 2));
-      w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-    }
+    const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const char*>(base) + at * SIZE);
+    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+  }
+  // The same where the array may end within the piece, `left` values on.
+  __device__ __forceinline__ void load(const void* base, int64_t at, int64_t left) {
+    if (left >= VEC) return load(base, at);
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) w[i] = 0;
+#pragma unroll
+    for (int k = 0; k < VEC; ++k)
+      if (k < left) {
+        if constexpr (DT == DP_F32)
+          w[k] = static_cast<const uint32_t*>(base)[at + k];
+        else
+          w[k / 2] |= (uint32_t) static_cast<const uint16_t*>(base)[at + k] << (16 * (k & 1));
+      }
   }
   __device__ __forceinline__ void store(void* base, int64_t at) const {
-    if constexpr (DT != DP_F32 && VEC == 1) {
-      static_cast<uint16_t*>(base)[at] = (uint16_t)w[0];
-    } else if constexpr (WORDS == 1) {
-      static_cast<uint32_t*>(base)[at] = w[0];
-    } else {
-      *reinterpret_cast<uint4*>(static_cast<char*>(base) + at * (DT == DP_F32 ? 4 : 2)) = make_uint4(w[0], w[1], w[2], w[3]);
-    }
+    *reinterpret_cast<uint4*>(static_cast<char*>(base) + at * SIZE) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  // Values from..to - 1 of it.
+  __device__ __forceinline__ void store(void* base, int64_t at, int from, int to) const {
+    if (from <= 0 && to >= VEC) return store(base, at);
+#pragma unroll
+    for (int k = 0; k < VEC; ++k)
+      if (k >= from && k < to) {
+        if constexpr (DT == DP_F32)
+          static_cast<uint32_t*>(base)[at + k] = w[k];
+        else
+          static_cast<uint16_t*>(base)[at + k] = (uint16_t)(w[k / 2] >> (16 * (k & 1)));
+      }
   }
   __device__ __forceinline__ float get(int k) const {
     if constexpr (DT == DP_F32) return __uint_as_float(w[k]);
@@ -52,7 +66,7 @@ struct Piece {                                     // VEC values as stored
     } else {
 #pragma unroll
       for (int k = 0; k < WORDS; ++k) {
-        const float lo = x[2 * k], hi = VEC == 1 ? 0.f : x[(2 * k + 1) % VEC];
+        const float lo = x[2 * k], hi = x[2 * k + 1];
         typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
         typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
         if constexpr (DT == DP_BF16)
@@ -88,62 +102,100 @@ __device__ __forceinline__ void row_sums(float (&x)[N], float (*red)[N]) {
   }
 }
 
-template <int VEC>
-__device__ __forceinline__ void load_params(float (&v)[VEC], const float* p, int col, float none) {
+// A parameter's values of columns col ..; those outside of a row of d are whatever.
+template <int VEC, bool SHIFT>
+__device__ __forceinline__ void load_params(float (&v)[VEC], const float* p, int col, int d, float none) {
+  typedef f32x4 Four __attribute__((aligned(4)));
+  if (!p) {
 #pragma unroll
-  for (int k = 0; k < VEC; ++k) v[k] = p ? p[col + k] : none;
+    for (int k = 0; k < VEC; ++k) v[k] = none;
+  } else if (!SHIFT || (col >= 0 && col + VEC <= d)) {
+#pragma unroll
+    for (int k = 0; k < VEC; k += 4) {
+      const f32x4 four = *reinterpret_cast<const Four*>(p + col + k);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[k + i] = four[i];
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) v[k] = p[min(max(col + k, 0), d - 1)];
+  }
 }
 
-template <int DT, int VEC, int TPR, int P>
+// A wave to a row of up to 2048 values, else a workgroup; registers hold the row between the two sums and the result (variance around
+// the mean, not from a sum of squares: no cancellation).  Bound by memory: 8 x 512 rows of 1280 bf16 values with the residual sum, 42 MB in
+// 8.9 us; 4 x 2048 x 12288 80 us, 5.0 TB/s, with the sum 147 us, 5.5 TB/s.
+// SHIFT: rows of no whole number of pieces.  Pieces lie at 16 bytes all the same, the first `ahead` values of a row's first one belong to the
+// row before; what a row does not own is loaded (where the array has it) but takes no part, and its own are stored one by one there.
+// (2048 x 12289 fp16: 26 us, and 58 an element at a time.)
+template <int DT, int VEC, int TPR, int P, bool SHIFT>
 __global__ void __launch_bounds__(kThreads) layer_norm_kernel(const NormArgs a, int64_t rows, int first_block) {
   constexpr int N = P / VEC, GROUPS = kThreads / TPR;
   __shared__ float red[kThreads / 64][1];
   const int t = threadIdx.x % TPR;
   const int64_t row = ((int64_t)first_block + blockIdx.x) * GROUPS + threadIdx.x / TPR;
   if (TPR == 64 && row >= rows) return;            // (a whole workgroup's row otherwise: always there)
-  const int64_t at = row * a.d;
+  const int64_t at = row * a.d, total = rows * a.d;
+  const int ahead = SHIFT ? (int)(at & (VEC - 1)) : 0;
+  auto own = [&](int col, int k) { return !SHIFT || (unsigned)(col + k) < (unsigned)a.d; };
+  auto load = [&](Piece<DT, VEC>& p, const void* from, int col) {
+    if constexpr (SHIFT)
+      p.load(from, at + col, total - (at + col));
+    else
+      p.load(from, at + col);
+  };
+  auto store = [&](const Piece<DT, VEC>& p, void* to, int col) {
+    if constexpr (SHIFT)
+      p.store(to, at + col, -col, a.d - col);
+    else
+      p.store(to, at + col);
+  };
   Piece<DT, VEC> x[N];
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    const int col = VEC * (n * TPR + t);
-    if (col < a.d) x[n].load(a.x, at + col);
+    const int col = VEC * (n * TPR + t) - ahead;
+    if (col < a.d) load(x[n], a.x, col);
   }
   if (a.add) {
     Piece<DT, VEC> y[N];
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      const int col = VEC * (n * TPR + t);
-      if (col < a.d) y[n].load(a.add, at + col);
+      const int col = VEC * (n * TPR + t) - ahead;
+      if (col < a.d) load(y[n], a.add, col);
     }
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      const int col = VEC * (n * TPR + t);
+      const int col = VEC * (n * TPR + t) - ahead;
       if (col < a.d) {
         float s[VEC];
 #pragma unroll
         for (int k = 0; k < VEC; ++k) s[k] = x[n].get(k) + y[n].get(k);
         x[n].set(s);                               // the stream as it is kept is what is normalised
-        x[n].store(a.sum, at + col);
+        store(x[n], a.sum, col);
       }
     }
   }
   float sum[1] = {0.f};
 #pragma unroll
-  for (int n = 0; n < N; ++n)
-    if (VEC * (n * TPR + t) < a.d)
+  for (int n = 0; n < N; ++n) {
+    const int col = VEC * (n * TPR + t) - ahead;
+    if (col < a.d)
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) sum[0] += x[n].get(k);
+      for (int k = 0; k < VEC; ++k) sum[0] += own(col, k) ? x[n].get(k) : 0.f;
+  }
   row_sums<TPR>(sum, red);
   const float mean = sum[0] / a.d;
   float square[1] = {0.f};
 #pragma unroll
-  for (int n = 0; n < N; ++n)
-    if (VEC * (n * TPR + t) < a.d)
+  for (int n = 0; n < N; ++n) {
+    const int col = VEC * (n * TPR + t) - ahead;
+    if (col < a.d)
 #pragma unroll
       for (int k = 0; k < VEC; ++k) {
-        const float c = x[n].get(k) - mean;
+        const float c = own(col, k) ? x[n].get(k) - mean : 0.f;
         square[0] = fmaf(c, c, square[0]);
       }
+  }
   row_sums<TPR>(square, red);
   const float rstd = 1.f / sqrtf(square[0] / a.d + a.eps);
   if (t == 0) {
@@ -152,34 +204,48 @@ __global__ void __launch_bounds__(kThreads) layer_norm_kernel(const NormArgs a, 
   }
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    const int col = VEC * (n * TPR + t);
+    const int col = VEC * (n * TPR + t) - ahead;
     if (col < a.d) {
       float gain[VEC], bias[VEC], y[VEC];
-      load_params<VEC>(gain, a.gain, col, 1.f);
-      load_params<VEC>(bias, a.bias, col, 0.f);
+      load_params<VEC, SHIFT>(gain, a.gain, col, a.d, 1.f);
+      load_params<VEC, SHIFT>(bias, a.bias, col, a.d, 0.f);
 #pragma unroll
       for (int k = 0; k < VEC; ++k) y[k] = fmaf((x[n].get(k) - mean) * rstd, gain[k], bias[k]);
       Piece<DT, VEC> out;
       out.set(y);
-      out.store(a.out, at + col);
+      store(out, a.out, col);
     }
   }
 }
 
 // Workgroup (chunk, sample): its row groups take rows in turn, the next one's values on their way while one is worked on; gain is in LDS
-// (read again for every row, it would be as many bytes out of L2 as the rows themselves).  The gradients of gain and bias are then
-// added over the groups through LDS, in their order.  4 x 2048 rows of 12288 bf16 values: 214 us with loads where they are used and
-// gain out of L2.
-template <int DT, int VEC, int TPR, int P>
-__global__ void __launch_bounds__(kThreads, P <= (DT == DP_F32 ? 8 : VEC > 1 ? 24 : 0) ? 4 : 2) layer_norm_backward_kernel(const NormArgs a, int first_block) {
-  constexpr int N = P / VEC, GROUPS = kThreads / TPR;
+// (read again for every row, it would be as many bytes out of L2 as the rows themselves).  The gradients of gain and bias stay in the
+// registers of the lanes that hold their columns and are then added over the groups through LDS, in their order.  Bound by memory: the
+// rows, and the chunks' sums, written and read once more.  4 x 2048 rows of 12288 bf16 values: 166 us with the join, 3.6 TB/s of the rows
+// alone (140 us where only dx is asked for); 214 us with loads where they are used and gain out of L2.  16 x 256 rows of 768: 12 us,
+// most of it two launches and a wave's two or three turns to memory.  Shifted rows: 2048 x 12289 fp16 81 us, an element at a time 319.
+template <int DT, int VEC, int TPR, int P, int THREADS, bool SHIFT>
+__global__ void __launch_bounds__(THREADS, THREADS == 1024 || P <= (DT == DP_F32 ? 8 : SHIFT ? 16 : 24) ? 4 : 2) layer_norm_backward_kernel(const NormArgs a, int first_block) {
+  constexpr int N = P / VEC, GROUPS = THREADS / TPR;
   constexpr bool AHEAD = P <= 32;                  // (no registers for it beyond)
-  extern __shared__ __align__(16) float gains[];   // then, in the same place, the groups' sums
-  __shared__ float red[kThreads / 64][2];
+  extern __shared__ __align__(16) float lds[];     // gain; then, in the same place, sums over groups
+  __shared__ float red[THREADS / 64][2];
+  float* const gains = lds + (SHIFT ? VEC : 0);    // (read up to a piece before its first and behind its last)
   const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
   const unsigned id = first_block + blockIdx.x;
   const int chunk = id % (unsigned)a.chunks, b = id / (unsigned)a.chunks;
-  const int first = chunk * a.chunk_rows, end = min(first + a.chunk_rows, a.T);
+  // Rows first + group, + step, ... below end.  With SHIFT a group's rows are all ahead by the same: a multiple of VEC apart.
+  const int phases = SHIFT && GROUPS == 1 ? min(VEC, a.T) : 1, step = GROUPS * phases;
+  const int first = chunk / phases * a.chunk_rows + chunk % phases, end = min(chunk / phases * a.chunk_rows + a.chunk_rows, a.T);
+  const int ahead = SHIFT ? (int)((((int64_t)b * a.T + first + group) * a.d) & (VEC - 1)) : 0;
+  const int64_t total = (int64_t)a.B * a.T * a.d;
+  auto own = [&](int col, int k) { return !SHIFT || (unsigned)(col + k) < (unsigned)a.d; };
+  auto load_piece = [&](Piece<DT, VEC>& p, const void* from, int64_t at) {
+    if constexpr (SHIFT)
+      p.load(from, at, total - at);
+    else
+      p.load(from, at);
+  };
   struct Row {
     Piece<DT, VEC> x[N], dy[N];
     float mean, rstd;
@@ -190,32 +256,34 @@ __global__ void __launch_bounds__(kThreads, P <= (DT == DP_F32 ? 8 : VEC > 1 ? 2
     r.rstd = a.rstd[row];
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      const int col = VEC * (n * TPR + t);
+      const int col = VEC * (n * TPR + t) - ahead;
       if (col < a.d) {
-        r.x[n].load(a.x, at + col);
-        r.dy[n].load(a.dy, at + col);
+        load_piece(r.x[n], a.x, at + col);
+        load_piece(r.dy[n], a.dy, at + col);
       }
     }
   };
   Row row;
   if (first + group < end) load(row, first + group);
-  for (int k = threadIdx.x; k < a.d; k += kThreads) gains[k] = a.gain ? a.gain[k] : 1.f;
+  for (int k = threadIdx.x; k < a.d; k += THREADS) gains[k] = a.gain ? a.gain[k] : 1.f;
+  if (SHIFT && threadIdx.x < VEC) lds[threadIdx.x] = gains[a.d + threadIdx.x] = 0.f;
   __syncthreads();
   float dgain[N][VEC] = {}, dbias[N][VEC] = {};
   const float width = 1.f / a.d;
-  for (int r = first; r < end; r += GROUPS) {
+  for (int r = first; r < end; r += step) {
     const bool there = GROUPS == 1 || r + group < end;
     Row next;
-    if (AHEAD && r + group + GROUPS < end) load(next, r + group + GROUPS);
+    if (AHEAD && r + group + step < end) load(next, r + group + step);
     float sums[2] = {0.f, 0.f};
     if (there) {
 #pragma unroll
       for (int n = 0; n < N; ++n) {
-        const int col = VEC * (n * TPR + t);
+        const int col = VEC * (n * TPR + t) - ahead;
         if (col < a.d)
 #pragma unroll
           for (int k = 0; k < VEC; ++k) {
-            const float h = (row.x[n].get(k) - row.mean) * row.rstd, g = row.dy[n].get(k), u = g * gains[col + k];
+            const float h = own(col, k) ? (row.x[n].get(k) - row.mean) * row.rstd : 0.f, g = own(col, k) ? row.dy[n].get(k) : 0.f;
+            const float u = g * gains[col + k];
             dgain[n][k] = fmaf(g, h, dgain[n][k]);
             dbias[n][k] += g;
             sums[0] += u;
@@ -230,10 +298,10 @@ __global__ void __launch_bounds__(kThreads, P <= (DT == DP_F32 ? 8 : VEC > 1 ? 2
         const int64_t at = ((int64_t)b * a.T + r + group) * a.d;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-          const int col = VEC * (n * TPR + t);
+          const int col = VEC * (n * TPR + t) - ahead;
           if (col < a.d) {
             Piece<DT, VEC> add, out;
-            if (a.add) add.load(a.add, at + col);
+            if (a.add) load_piece(add, a.add, at + col);
             float dx[VEC];
 #pragma unroll
             for (int k = 0; k < VEC; ++k) {
@@ -242,54 +310,81 @@ __global__ void __launch_bounds__(kThreads, P <= (DT == DP_F32 ? 8 : VEC > 1 ? 2
               if (a.add) dx[k] += add.get(k);
             }
             out.set(dx);
-            out.store(a.out, at + col);
+            if constexpr (SHIFT)
+              out.store(a.out, at + col, -col, a.d - col);
+            else
+              out.store(a.out, at + col);
           }
         }
       }
     }
     if (AHEAD)
       row = next;
-    else if (r + group + GROUPS < end)
-      load(row, r + group + GROUPS);
+    else if (r + group + step < end)
+      load(row, r + group + step);
   }
   if (!a.kept) return;
   float* to = a.chunks > 1 ? a.partial + (int64_t)id * 2 * a.d : a.kept + (int64_t)b * 2 * a.d;
   float square[1] = {0.f};
+  if constexpr (GROUPS == 1) {
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    if constexpr (GROUPS > 1) {
-      constexpr int SUMS = 2 * VEC * TPR;          // of a group
-      __syncthreads();
+    for (int n = 0; n < N; ++n)
 #pragma unroll
       for (int k = 0; k < VEC; ++k) {
-        gains[group * SUMS + VEC * t + k] = dgain[n][k];
-        gains[group * SUMS + VEC * (TPR + t) + k] = dbias[n][k];
-      }
-      __syncthreads();
-      for (int c = threadIdx.x; c < SUMS; c += kThreads) {
-        const int half = c / (VEC * TPR), col = n * VEC * TPR + c % (VEC * TPR);
-        if (col < a.d) {
-          float v = 0.f;
-#pragma unroll
-          for (int g = 0; g < GROUPS; ++g) v += gains[g * SUMS + c];
-          to[(int64_t)half * a.d + col] = v;
-          square[0] = fmaf(v, v, square[0]);
-        }
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) {
-        const int col = VEC * (n * TPR + t) + k;
-        if (col < a.d) {
+        const int col = VEC * (n * TPR + t) - ahead + k;
+        if (own(col, 0) && col < a.d) {
           to[col] = dgain[n][k];
           to[(int64_t)a.d + col] = dbias[n][k];
           square[0] = fmaf(dgain[n][k], dgain[n][k], fmaf(dbias[n][k], dbias[n][k], square[0]));
         }
       }
+  } else if constexpr (SHIFT) {
+    // A group's pieces lie `ahead` columns before where its columns are: each group's sums as they lie, and the shift where they are read.
+    const int region = (a.d + 2 * VEC - 1) / VEC * VEC;
+    for (int half = 0; half < 2; ++half) {
+      __syncthreads();
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        const int col = VEC * (n * TPR + t);
+        if (col < region)
+#pragma unroll
+          for (int k = 0; k < VEC; ++k) lds[group * region + col + k] = half ? dbias[n][k] : dgain[n][k];
+      }
+      __syncthreads();
+      for (int c = threadIdx.x; c < a.d; c += THREADS) {
+        float v = 0.f;
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g)
+          v += lds[g * region + c + (int)((((int64_t)b * a.T + first + g) * a.d) & (VEC - 1))];
+        to[half * a.d + c] = v;
+        square[0] = fmaf(v, v, square[0]);
+      }
+    }
+  } else {
+    constexpr int SUMS = 2 * VEC * TPR;            // of a group
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) {
+        lds[group * SUMS + VEC * t + k] = dgain[n][k];
+        lds[group * SUMS + VEC * (TPR + t) + k] = dbias[n][k];
+      }
+      __syncthreads();
+      for (int c = threadIdx.x; c < SUMS; c += THREADS) {
+        const int half = c / (VEC * TPR), col = n * VEC * TPR + c % (VEC * TPR);
+        if (col < a.d) {
+          float v = 0.f;
+#pragma unroll
+          for (int g = 0; g < GROUPS; ++g) v += lds[g * SUMS + c];
+          to[(int64_t)half * a.d + col] = v;
+          square[0] = fmaf(v, v, square[0]);
+        }
+      }
     }
   }
   if (a.chunks == 1) {
-    row_sums<kThreads>(square, reinterpret_cast<float(*)[1]>(red));
+    row_sums<THREADS>(square, reinterpret_cast<float(*)[1]>(red));
     if (threadIdx.x == 0) a.sqnorm[b] = square[0];
   }
 }
@@ -352,79 +447,115 @@ __global__ void __launch_bounds__(kJoinThreads) layer_norm_join_norm_kernel(cons
   }
 }
 
-// Calls f with the form for rows of width d: threads to a row and values to a thread.
-template <class F>
-dp_status by_width(int d, F f) {
+// Values to a piece, and the values that a row's pieces cover at most.
+constexpr int piece_values(int dt) { return dt == DP_F32 ? 4 : 8; }
+int covered(dp_dtype dt, int d) { return d % piece_values(dt) == 0 ? d : d + piece_values(dt) - 1; }
+constexpr int kWaveWidth = 2048;                   // of rows that a wave takes alone
+
+// Calls f with the form for rows that cover `width` values: threads to a row and values to a thread.
+template <int THREADS, bool SHIFT, class F>
+dp_status by_width(int width, F f) {
   using std::integral_constant;
-  const int per = d <= 2048 ? (d + 63) / 64 : (d + kThreads - 1) / kThreads;
-  auto go = [&](auto tpr) {
+  const int per = width <= kWaveWidth ? (width + 63) / 64 : (width + THREADS - 1) / THREADS;
+  if (width <= kWaveWidth) {
+    const integral_constant<int, 64> tpr{};
     if (per <= 8) return f(tpr, integral_constant<int, 8>{});
-    if (per <= 16) return f(tpr, integral_constant<int, 16>{});
+    if (THREADS == 1024 || per <= 16) return f(tpr, integral_constant<int, 16>{});
+    if constexpr (THREADS == 512) return per <= 24 ? f(tpr, integral_constant<int, 24>{}) : f(tpr, integral_constant<int, 32>{});
+  }
+  const integral_constant<int, THREADS> tpr{};
+  if (per <= 8) return f(tpr, integral_constant<int, 8>{});
+  if (THREADS == 1024 || per <= 16) return f(tpr, integral_constant<int, 16>{});
+  if constexpr (THREADS == 512) {
     if (per <= 24) return f(tpr, integral_constant<int, 24>{});
-    return f(tpr, integral_constant<int, 32>{});
-  };
-  if (d <= 2048) return go(integral_constant<int, 64>{});
-  if (per <= 32) return go(integral_constant<int, kThreads>{});
-  return f(integral_constant<int, kThreads>{}, integral_constant<int, 64>{});
+    if (per <= 32) return f(tpr, integral_constant<int, 32>{});
+    return f(tpr, integral_constant<int, SHIFT ? 72 : 64>{});
+  }
+  return DP_ERR_UNSUPPORTED;
 }
 
+// Calls f with the type and whether rows are shifted.
 template <class F>
 dp_status by_type(dp_dtype dt, int d, F f) {
   using std::integral_constant;
-  if (dt == DP_F32) {
-    if (d % 4 == 0) return f(integral_constant<int, DP_F32>{}, integral_constant<int, 4>{});
-    return f(integral_constant<int, DP_F32>{}, integral_constant<int, 1>{});
-  }
-  const bool whole = d % 8 == 0;
-  if (dt == DP_F16) {
-    if (whole) return f(integral_constant<int, DP_F16>{}, integral_constant<int, 8>{});
-    return f(integral_constant<int, DP_F16>{}, integral_constant<int, 1>{});
-  }
-  if (whole) return f(integral_constant<int, DP_BF16>{}, integral_constant<int, 8>{});
-  return f(integral_constant<int, DP_BF16>{}, integral_constant<int, 1>{});
+  auto go = [&](auto type) {
+    return d % piece_values(decltype(type)::value) ? f(type, std::true_type{}) : f(type, std::false_type{});
+  };
+  if (dt == DP_F32) return go(integral_constant<int, DP_F32>{});
+  return dt == DP_F16 ? go(integral_constant<int, DP_F16>{}) : go(integral_constant<int, DP_BF16>{});
+}
+
+// Threads to a workgroup of the backward pass: 512, of which a compute unit has two, or 1024, one, where a thread's part of a row is at most 32
+// bytes (twice the waves leave it 128 registers) and that brings something: wide rows leave half as many sums to be joined (4 x
+// 2048 x 12288 bf16: 166 us, with 512 threads 184), waves that take rows alone have one each where two were (32 x 197 x 768: 12.8 and 16.1; a
+// sample of up to 8 rows has none for the other waves: 512 x 1 x 1024, 10.6 and 9.8).  Beyond, 2 x 1000 x 32768: 206 us with 1024, 183.
+int backward_threads(dp_dtype dt, int T, int d) {
+  const int width = covered(dt, d), bytes = width * (dt == DP_F32 ? 4 : 2);
+  if (width <= 1024) return T > 8 ? 1024 : 512;
+  return bytes > 16384 && bytes <= 32768 ? 1024 : 512;
 }
 
 }  // namespace
 
 dp_status launch_layer_norm(const NormArgs& a, dp_dtype dt, hipStream_t s) {
   const int64_t rows = (int64_t)a.B * a.T;
-  return by_type(dt, a.d, [&](auto type, auto vec) {
-    return by_width(a.d, [&](auto tpr, auto per) {
-      constexpr int GROUPS = kThreads / decltype(tpr)::value;
+  return by_type(dt, a.d, [&](auto type, auto shift) {
+    return by_width<kThreads, decltype(shift)::value>(covered(dt, a.d), [&](auto tpr, auto per) {
+      constexpr int DT = decltype(type)::value, GROUPS = kThreads / decltype(tpr)::value;
       return launch_in_runs((rows + GROUPS - 1) / GROUPS, [&](dim3 grid, int first) {
-        hipLaunchKernelGGL((layer_norm_kernel<decltype(type)::value, decltype(vec)::value, decltype(tpr)::value, decltype(per)::value>),
+        hipLaunchKernelGGL((layer_norm_kernel<DT, piece_values(DT), decltype(tpr)::value, decltype(per)::value, decltype(shift)::value>),
                            grid, dim3(kThreads), 0, s, a, rows, first);
       });
     });
   });
 }
 
-int layer_norm_chunks(dp_dtype, int B, int T, int d) {
-  const int64_t rows = (int64_t)B * T;
-  const int groups = d <= 2048 ? kThreads / 64 : 1;
-  int64_t per = (rows + 511) / 512;                // two workgroups to a compute unit
-  per = per < 2 * groups ? 2 * groups : per;
-  per = per < 16 ? 16 : per;
-  return (int)((T + per - 1) / per);
+namespace {
+
+// How a sample's T rows are dealt to workgroups: chunks of `rows` rows, a whole number of phases (the rows of a chunk that are shifted
+// alike make a workgroup where one works on one row at a time).
+struct Dealt {
+  int chunks, rows;
+};
+Dealt deal(dp_dtype dt, int B, int T, int d) {
+  const int64_t all = (int64_t)B * T;
+  const int threads = backward_threads(dt, T, d), units = 262144 / threads;      // 512 threads: two workgroups to a compute unit, 1024: one
+  const bool alone = covered(dt, d) <= kWaveWidth;
+  const int phases = !alone && d % piece_values(dt) ? std::min(piece_values(dt), T) : 1;
+  int64_t per = std::max<int64_t>((all + units - 1) / units, alone ? 16 : 8);         // to a workgroup
+  const int64_t strips = std::max<int64_t>(1, (T + per * phases - 1) / (per * phases));
+  const int64_t rows = ((T + strips - 1) / strips + phases - 1) / phases * phases;
+  return {(int)((T + rows - 1) / rows * phases), (int)rows};
 }
 
+}  // namespace
+
+int layer_norm_chunks(dp_dtype dt, int B, int T, int d) { return deal(dt, B, T, d).chunks; }
+
 dp_status launch_layer_norm_backward(NormArgs a, dp_dtype dt, hipStream_t s) {
-  a.chunks = layer_norm_chunks(dt, a.B, a.T, a.d);
-  a.chunk_rows = (a.T + a.chunks - 1) / a.chunks;
-  dp_status st = by_type(dt, a.d, [&](auto type, auto vec) {
-    return by_width(a.d, [&](auto tpr, auto per) {
-      constexpr int VEC = decltype(vec)::value, TPR = decltype(tpr)::value, GROUPS = kThreads / TPR;
-      auto kernel = layer_norm_backward_kernel<decltype(type)::value, VEC, TPR, decltype(per)::value>;
-      const int lds = 4 * std::max(a.d, GROUPS > 1 ? GROUPS * 2 * VEC * TPR : 0);
-      static ReadyTable done;
-      if (lds > 65536) {
-        const dp_status ready = allow_big_lds(kernel, 4 * kNormMaxWidth, done);
-        if (ready != DP_OK) return ready;
-      }
-      return launch_in_runs((int64_t)a.B * a.chunks, [&](dim3 grid, int first) {
-        hipLaunchKernelGGL(kernel, grid, dim3(kThreads), lds, s, a, first);
+  const Dealt dealt = deal(dt, a.B, a.T, a.d);
+  a.chunks = dealt.chunks;
+  a.chunk_rows = dealt.rows;
+  dp_status st = by_type(dt, a.d, [&](auto type, auto shift) {
+    auto by_threads = [&](auto threads) {
+      constexpr int THREADS = decltype(threads)::value;
+      return by_width<THREADS, decltype(shift)::value>(covered(dt, a.d), [&](auto tpr, auto per) {
+        constexpr int DT = decltype(type)::value, VEC = piece_values(DT), TPR = decltype(tpr)::value, GROUPS = THREADS / TPR;
+        constexpr bool SHIFT = decltype(shift)::value;
+        auto kernel = layer_norm_backward_kernel<DT, VEC, TPR, decltype(per)::value, THREADS, SHIFT>;
+        const int lds = 4 * std::max(a.d + (SHIFT ? 2 * VEC : 0), GROUPS == 1 ? 0 : SHIFT ? GROUPS * ((a.d + 2 * VEC - 1) / VEC * VEC) : GROUPS * 2 * VEC * TPR);
+        static ReadyTable done;
+        if (lds > 65536) {
+          const dp_status ready = allow_big_lds(kernel, 4 * (kNormMaxWidth + 16), done);
+          if (ready != DP_OK) return ready;
+        }
+        return launch_in_runs((int64_t)a.B * a.chunks, [&](dim3 grid, int first) {
+          hipLaunchKernelGGL(kernel, grid, dim3(THREADS), lds, s, a, first);
+        });
       });
-    });
+    };
+    return backward_threads(dt, a.T, a.d) == 1024 ? by_threads(std::integral_constant<int, 1024>{})
+                                                  : by_threads(std::integral_constant<int, 512>{});
   });
   if (st != DP_OK || !a.kept || a.chunks == 1) return st;
   if ((int64_t)a.chunks * 2 * a.d <= kJoinValues)

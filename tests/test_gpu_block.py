@@ -47,6 +47,10 @@ def rand(gen, shape, dtype, scale=1.0):
 NORM_SIZES = [(1, 1, 1), (4, 8, 16), (3, 5, 7), (2, 33, 64), (2, 9, 768), (1, 70, 1280), (5, 1, 2048), (2, 3, 2050), (1, 19, 2056),
               (2, 4, 12288), (1, 2, 4097), (1, 3, 16392), (1, 2, 32768), (300, 1, 40), (2, 200, 24), (1, 5, 8191)]
 
+# Rows that begin at every place of a 16-byte piece: by waves and by workgroups, few and many rows to a sample, the last widths of a form.
+NORM_SIZES += [(2, 37, 4099), (3, 50, 1021), (1, 20, 9001), (2, 70, 2041), (1, 33, 2045), (1, 3, 32767), (1, 9, 16383), (3, 9, 1017), (1, 300, 2049),
+               (2, 11, 8185), (1, 130, 3), (40, 3, 2058)]
+
 
 def norm_reference(x, gain, bias, eps):
     x = x.double()
@@ -126,6 +130,28 @@ def test_layer_norm_backward(block, dtype, B, T, d):
     norm.clipped_gradient(kept, C.cuda(), grad)
     want_sum = (C.double()[:, None, None] * want_kept).sum(0)
     assert (grad.cpu().double() - want_sum).norm() <= 4 * FP32 * (C.double()[:, None, None] * want_kept).norm() * math.sqrt(B)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [1021, 4100, 4099])
+def test_layer_norm_in_place(block, dtype, d):
+    """The sum over x or over what is added, dx over dy or over what is added: the same bits, rows beside them whole."""
+    gen = torch.Generator().manual_seed(d)
+    x, add, dy = (rand(gen, (2, 30, d), dtype).cuda() for _ in range(3))
+    norm = block.LayerNorm(torch.randn(d, generator=gen).cuda(), None)
+    new = lambda: (torch.empty((2, 30), device="cuda"), torch.empty((2, 30), device="cuda"))  # noqa: E731
+    y, total, stats = torch.empty_like(x), torch.empty_like(x), new()
+    norm.forward(x, y, *stats, add, total)
+    for over in (0, 1):
+        args, other = [x.clone(), add.clone()], torch.empty_like(x)
+        norm.forward(args[0], other, *new(), args[1], args[over])
+        assert torch.equal(args[over], total) and torch.equal(other, y)
+    dx, kept, sq = torch.empty_like(x), torch.empty((2, 2, d), device="cuda"), torch.empty(2, device="cuda")
+    norm.backward(total, dy, *stats, dx, kept, sq, add)
+    for over in (0, 1):
+        args, k2, s2 = [dy.clone(), add.clone()], torch.empty_like(kept), torch.empty_like(sq)
+        norm.backward(total, args[0], *stats, args[over], k2, s2, args[1])
+        assert torch.equal(args[over], dx) and torch.equal(k2, kept) and torch.equal(s2, sq)
 
 
 def test_layer_norm_gradient_against_differences(block):
