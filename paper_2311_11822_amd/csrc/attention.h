@@ -323,6 +323,36 @@ __device__ __forceinline__ void store_partial(const f32x16 (&acc)[DP / 32], bool
     }
 }
 
+// Several waves may own the same 32 rows and take the other side's tiles in turn.  In how many floats they hand N values a lane to the first.
+constexpr int handed_floats(int n) { return 64 * n; }
+template <int N>
+__device__ __forceinline__ void hand_over(const f32x16 (&acc)[N], float* to, int lane) {
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) to[(16 * n + r) * 64 + lane] = acc[n][r];
+}
+template <int N>
+__device__ __forceinline__ void take_over(f32x16 (&acc)[N], const float* from, int lane) {
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[n][r] += from[(16 * n + r) * 64 + lane];
+}
+
+// How many they are: as LDS has room for tiles of 32 rows to each, in two stages.
+constexpr int split_waves(int row_bytes) { return row_bytes <= 128 ? 8 : row_bytes <= 256 ? 4 : 2; }
+// Whether there are so few rows (of `heads` pairs) that their workgroups leave compute units idle, and so many of the other side that turns are
+// worth the joining.  In us, forward and both passes' gradients, one wave's and split: bf16, 8 heads of 64, 1 x 1 query, 4096 keys 59 + 71,
+// 20 + 27; 1 head, 4096 tokens 49 + 145, 21 + 50; 8 heads, 2048 tokens 28 + 79, 21 + 54; but 24 heads, 512 tokens 11 + 29, 15 + 41.  fp32, whose tiles take
+// eight times as long: 2 x 512 tokens, 8 heads of 128 73 + 239, 58 + 142; 4 x 128, 6 heads of 64 15 + 43, 11 + 25; but 8 x 128, 12 heads 16
+// + 49, 20 + 50.
+template <int DT>
+bool split_rows(int64_t heads, int rows, int others) {
+  const int64_t workgroups = heads * ((rows + 127) / 128);
+  return DT == DP_F32 ? workgroups <= 64 && others > 64 : workgroups <= 128 && others >= 1024;
+}
+
 // Calls f with a tile's number and the stage that it lies in, as a constant, for n tiles.
 template <class F>
 __device__ __forceinline__ void two_stages(int n, F f) {

@@ -9,19 +9,19 @@ namespace {
 constexpr float kLazy = 8.f;                      // a maximum may be passed by 2^8 before sums are expressed in a new one
 
 // NW waves of 32 queries each, tiles of KEYS keys in two stages.
-template <int DT, int DP, int NW, int KEYS>
-__global__ void __launch_bounds__(64 * NW, 2) attention_kernel(const AttnArgs a) {
+template <int DT, int DP, int NW, int SPLIT, int KEYS>
+__global__ void __launch_bounds__(64 * NW * SPLIT, 2) attention_kernel(const AttnArgs a) {
   extern __shared__ __align__(1024) char smem[];
   typedef Ops<DT> O;
   typedef typename O::E E;
-  constexpr int KS = HeadTile<DT, DP>::CHUNKS / 2, CB = DP / 32, KB = KEYS / 32, TILE = KEYS * HeadTile<DT, DP>::ROW_BYTES;
+  constexpr int KS = HeadTile<DT, DP>::CHUNKS / 2, CB = DP / 32, KB = KEYS / 32, TILE = SPLIT * KEYS * HeadTile<DT, DP>::ROW_BYTES;
   constexpr int V = 2 * TILE;                     // two stages of keys, then two of values
   int pair, block;
   attn_unit(a, a.first + blockIdx.x, pair, block);
   if (pair >= a.heads) return;
   const int b = pair / a.H, h = pair % a.H;
   if (a.causal) block = a.blocks - 1 - block;     // the longest first
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = id % NW, turn = id / NW;
   const int n_q = valid_rows(a.q_len, b, a.Tq), n_k = valid_rows(a.k_len, b, a.Tk), shift = n_k - n_q;
   const int row0 = block * 32 * NW, own0 = row0 + 32 * wave, row = own0 + (lane & 31);
   const unsigned lds = (unsigned)(uintptr_t)DP_LDS(char, smem);
@@ -33,13 +33,13 @@ __global__ void __launch_bounds__(64 * NW, 2) attention_kernel(const AttnArgs a)
   const int lane_end = row >= n_q ? 0 : a.causal ? min(n_k, row + shift + 1) : n_k;
 
   const E* q = static_cast<const E*>(a.q) + b * a.qs.sample + h * a.qs.head;
-  TileLoader<DT, DP, KEYS, NW> k_tiles, v_tiles;
-  k_tiles.init(static_cast<const E*>(a.k) + b * a.ks.sample + h / a.share * a.ks.head, a.ks.token, a.D, wave, lane);
-  v_tiles.init(static_cast<const E*>(a.v) + b * a.vs.sample + h / a.share * a.vs.head, a.vs.token, a.D, wave, lane);
+  TileLoader<DT, DP, SPLIT * KEYS, NW * SPLIT> k_tiles, v_tiles;
+  k_tiles.init(static_cast<const E*>(a.k) + b * a.ks.sample + h / a.share * a.ks.head, a.ks.token, a.D, id, lane);
+  v_tiles.init(static_cast<const E*>(a.v) + b * a.vs.sample + h / a.share * a.vs.head, a.vs.token, a.D, id, lane);
   // A tile's scores are formed beside the exponentials of the tile before it, so its keys are loaded a step before its values.
-  auto load_keys = [&](int tile, int stage) { k_tiles.load(tile * KEYS, n_k, lds + stage * TILE, wave); };
-  auto load_values = [&](int tile, int stage) { v_tiles.load(tile * KEYS, n_k, lds + V + stage * TILE, wave); };
-  const int tiles = (end + KEYS - 1) / KEYS;
+  auto load_keys = [&](int tile, int stage) { k_tiles.load(tile * SPLIT * KEYS, n_k, lds + stage * TILE, id); };
+  auto load_values = [&](int tile, int stage) { v_tiles.load(tile * SPLIT * KEYS, n_k, lds + V + stage * TILE, id); };
+  const int tiles = (end + SPLIT * KEYS - 1) / (SPLIT * KEYS);
   if (tiles > 0) {
     load_keys(0, 0);
     if (tiles > 1) load_keys(1, 1);
@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attention_kernel(const AttnArgs a)
   load_own<DT>(qf, q, a.qs.token, row, row < n_q, a.D, lane);
   have(qf);
   TileReader<DT, DP> read;
-  read.init(lds, lane);
+  read.init(lds + turn * KEYS * HeadTile<DT, DP>::ROW_BYTES, lane);
 
   f32x16 o[CB];
 #pragma unroll
@@ -72,7 +72,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attention_kernel(const AttnArgs a)
   two_stages(tiles, [&](int t, auto stage) {
     constexpr int HERE = decltype(stage)::value, NEXT = HERE ^ 1;
     f32x16(&s)[KB] = both[HERE], (&next)[KB] = both[NEXT];
-    const int j0 = t * KEYS;
+    const int j0 = (t * SPLIT + turn) * KEYS;
     tiles_landed();
     if (t + 2 < tiles) load_keys(t + 2, HERE);
     if (t + 1 < tiles) load_values(t + 1, NEXT);
@@ -116,8 +116,32 @@ __global__ void __launch_bounds__(64 * NW, 2) attention_kernel(const AttnArgs a)
     }
   });
   total += other_half(total, lane);
+  if constexpr (SPLIT > 1) {
+    constexpr int EACH = handed_floats(16 * CB + 2);
+    float* const mine = reinterpret_cast<float*>(smem) + id * EACH;
+    tiles_landed();
+    if (turn > 0) {
+      hand_over(o, mine, lane);
+      mine[16 * CB * 64 + lane] = most;
+      mine[(16 * CB + 1) * 64 + lane] = total;
+    }
+    tiles_landed();
+    if (turn > 0) return;
+#pragma unroll
+    for (int w = 1; w < SPLIT; ++w) {
+      const float* theirs = mine + w * NW * EACH;
+      const float higher = fmaxf(most, theirs[16 * CB * 64 + lane]);
+      const float fix = __builtin_amdgcn_exp2f(most - higher), their_fix = __builtin_amdgcn_exp2f(theirs[16 * CB * 64 + lane] - higher);
+      most = higher;
+      total = total * fix + theirs[(16 * CB + 1) * 64 + lane] * their_fix;
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[cb][r] = o[cb][r] * fix + theirs[(16 * cb + r) * 64 + lane] * their_fix;
+    }
+  }
   const bool there = lane_end > 0 && total != 0.f;
-  tiles_landed();                                 // LDS is free
+  if (SPLIT == 1) tiles_landed();                 // LDS is free
   store_rows<DT, DP>(o, 1.f / total, there, static_cast<E*>(a.out) + b * a.os.sample + h * a.os.head, a.os.token, own0,
                         a.Tq, a.D, lds + wave * 32 * HeadTile<DT, DP>::ROW_BYTES, lane);
   if (lane < 32 && row < a.Tq)
@@ -139,26 +163,27 @@ __global__ void __launch_bounds__(256) attention_rows_kernel(const AttnArgs a) {
   if (i < a.Tq) rows.forward(i);
 }
 
-template <int DT, int DP, int NW, int KEYS>
+template <int DT, int DP, int NW, int SPLIT, int KEYS>
 dp_status launch(AttnArgs a, hipStream_t s) {
   a.heads = a.B * a.H;
   a.blocks = (a.Tq + 32 * NW - 1) / (32 * NW);
-  constexpr int LDS = 4 * KEYS * HeadTile<DT, DP>::ROW_BYTES;
-  auto kernel = attention_kernel<DT, DP, NW, KEYS>;
+  constexpr int LDS = 4 * SPLIT * KEYS * HeadTile<DT, DP>::ROW_BYTES;
+  auto kernel = attention_kernel<DT, DP, NW, SPLIT, KEYS>;
   static ReadyTable done;
   if (LDS > 65536) {
     const dp_status st = allow_big_lds(kernel, LDS, done);
     if (st != DP_OK) return st;
   }
-  return launch_attention(kernel, a, (int64_t)2 * Ops<DT>::SIZE * a.Tk * a.D, 64 * NW, LDS, s);
+  return launch_attention(kernel, a, (int64_t)2 * Ops<DT>::SIZE * a.Tk * a.D, 64 * NW * SPLIT, LDS, s);
 }
 
 template <int DT, int DP>
 dp_status launch(const AttnArgs& a, hipStream_t s) {
-  constexpr int KEYS = DT == DP_F32 ? 32 : 64;
-  if (a.Tq <= 32) return launch<DT, DP, 1, 32>(a, s);
-  if (a.Tq <= 64) return launch<DT, DP, 2, KEYS>(a, s);
-  return launch<DT, DP, 4, KEYS>(a, s);
+  constexpr int KEYS = DT == DP_F32 ? 32 : 64, SPLIT = split_waves(HeadTile<DT, DP>::ROW_BYTES);
+  if (split_rows<DT>((int64_t)a.B * a.H, a.Tq, a.Tk)) return launch<DT, DP, 1, SPLIT, 32>(a, s);
+  if (a.Tq <= 32) return launch<DT, DP, 1, 1, 32>(a, s);
+  if (a.Tq <= 64) return launch<DT, DP, 2, 1, 32>(a, s);
+  return launch<DT, DP, 4, 1, KEYS>(a, s);
 }
 
 template <int DT>

@@ -21,19 +21,20 @@ constexpr int grad_ahead(int DT, int DP) { return DT == DP_F32 || DP <= 64 ? 2 :
 constexpr bool values_in_lds(int DT, int DP) { return DT != DP_F32 && DP == 128; }
 
 // dq, and for the other kernel lse in units of log 2 and delta.
-template <int DT, int DP, int NW>
-__global__ void __launch_bounds__(64 * NW, grad_workgroups(DT, DP)) attention_query_grad_kernel(const AttnArgs a) {
+template <int DT, int DP, int NW, int SPLIT>
+__global__ void __launch_bounds__(64 * NW * SPLIT, SPLIT == 8 ? 2 : SPLIT > 1 ? 1 : grad_workgroups(DT, DP)) attention_query_grad_kernel(const AttnArgs a) {
   extern __shared__ __align__(1024) char smem[];
   typedef Ops<DT> O;
   typedef typename O::E E;
-  constexpr int KS = HeadTile<DT, DP>::CHUNKS / 2, CB = DP / 32, TILE = kRows * HeadTile<DT, DP>::ROW_BYTES, STAGE = 2 * TILE;
-  typedef TileLoader<DT, DP, kRows, NW> Loader;
+  constexpr int KS = HeadTile<DT, DP>::CHUNKS / 2, CB = DP / 32, TILE = SPLIT * kRows * HeadTile<DT, DP>::ROW_BYTES, STAGE = 2 * TILE;
+  constexpr int SUB = kRows * HeadTile<DT, DP>::ROW_BYTES;           // one wave's tile of a stage's
+  typedef TileLoader<DT, DP, SPLIT * kRows, NW * SPLIT> Loader;
   int pair, block;
   attn_unit(a, a.first + blockIdx.x, pair, block);
   if (pair >= a.heads) return;
   const int b = pair / a.H, h = pair % a.H;
   if (a.causal) block = a.blocks - 1 - block;     // the longest first
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = id % NW, turn = id / NW;
   const int n_q = valid_rows(a.q_len, b, a.Tq), n_k = valid_rows(a.k_len, b, a.Tk), shift = n_k - n_q;
   const int row0 = block * 32 * NW, own0 = row0 + 32 * wave, row = own0 + (lane & 31);
   const unsigned lds = (unsigned)(uintptr_t)DP_LDS(char, smem);
@@ -67,18 +68,18 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DT, DP)) attention_qu
   const float own_lse2 = lane_end == 1 ? INFINITY : lse2;
 
   Loader k_tiles, v_tiles;
-  k_tiles.init(static_cast<const E*>(a.k) + b * a.ks.sample + h / a.share * a.ks.head, a.ks.token, a.D, wave, lane);
-  v_tiles.init(static_cast<const E*>(a.v) + b * a.vs.sample + h / a.share * a.vs.head, a.vs.token, a.D, wave, lane);
+  k_tiles.init(static_cast<const E*>(a.k) + b * a.ks.sample + h / a.share * a.ks.head, a.ks.token, a.D, id, lane);
+  v_tiles.init(static_cast<const E*>(a.v) + b * a.vs.sample + h / a.share * a.vs.head, a.vs.token, a.D, id, lane);
   TileReader<DT, DP> read;
-  read.init(lds, lane);
+  read.init(lds + turn * SUB, lane);
   auto load = [&](int tile, int stage) {
     const unsigned to = lds + stage * STAGE;
-    k_tiles.load(tile * kRows, n_k, to, wave);
-    v_tiles.load(tile * kRows, n_k, to + TILE, wave);
+    k_tiles.load(tile * SPLIT * kRows, n_k, to, id);
+    v_tiles.load(tile * SPLIT * kRows, n_k, to + TILE, id);
   };
   // Scores, and do v' - delta (the sums begin at -delta).
-  auto products = [&](f32x16& s, f32x16& dp, int stage, const f32x16& begin) {
-    auto operand = [&](int m) { return read.rows(stage * STAGE + m / KS * TILE, 0, m % KS); };
+  auto products = [&](f32x16& s, f32x16& dp, int at, const f32x16& begin) {
+    auto operand = [&](int m) { return read.rows(at + m / KS * TILE, 0, m % KS); };
     Stretch<typename O::Row, 2 * KS, grad_ahead(DT, DP)> run;
     run.begin(operand);
     run.run(operand,
@@ -101,7 +102,7 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DT, DP)) attention_qu
   f32x16 dq[CB], begin;
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb) dq[cb] = zeros16();
-  const int tiles = (end + kRows - 1) / kRows, own_tiles = (own_end + kRows - 1) / kRows;
+  const int tiles = (end + SPLIT * kRows - 1) / (SPLIT * kRows), own_tiles = (own_end + kRows - 1) / kRows;
   if (tiles > 0) {
     load(0, 0);
     load(1, 1);
@@ -114,7 +115,7 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DT, DP)) attention_qu
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         f32x16 s, dp;
-        products(s, dp, t, zeros16());
+        products(s, dp, SPLIT > 1 ? (t - turn) * SUB : t * STAGE, zeros16());
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = probability(s[r]) * dp[r];
         hide(s, t);
@@ -131,23 +132,33 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DT, DP)) attention_qu
     constexpr int HERE = decltype(stage)::value;
     tiles_landed();
     if (t > 0 && t + 1 < tiles) load(t + 1, HERE ^ 1);
-    if (t >= own_tiles) return;
+    const int tile = t * SPLIT + turn;
+    if (tile >= own_tiles) return;
     f32x16 s, dp;
-    products(s, dp, HERE, begin);
+    products(s, dp, HERE * STAGE, begin);
     auto operand = [&](int m) { return read.columns(HERE * STAGE, 16 * (m / CB), m % CB); };
     Stretch<typename O::Column, 2 * CB, grad_ahead(DT, DP)> run;
     run.begin(operand);
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[r] = probability(s[r]) * dp[r];
-    if ((t + 1) * kRows > all_see) hide(s, t);
+    if ((tile + 1) * kRows > all_see) hide(s, tile);
     const typename O::Column ds[2] = {O::weights(s, 0), O::weights(s, 8)};
     run.run(operand, [&](int m, typename O::Column f) { dq[m % CB] = O::columns(f, ds[m / CB], dq[m % CB]); });
   });
+  tiles_landed();                                 // LDS is free
+  if constexpr (SPLIT > 1) {
+    constexpr int EACH = handed_floats(16 * CB);
+    float* const mine = reinterpret_cast<float*>(smem) + id * EACH;
+    if (turn > 0) hand_over(dq, mine, lane);
+    tiles_landed();
+    if (turn > 0) return;
+#pragma unroll
+    for (int w = 1; w < SPLIT; ++w) take_over(dq, mine + w * NW * EACH, lane);
+  }
   if (lane < 32 && row < a.Tq) {
     a.lse2[at] = lse2;
     a.delta[at] = -delta;
   }
-  tiles_landed();                                 // LDS is free
   store_rows<DT, DP>(dq, a.scale, lane_end > 0, static_cast<E*>(a.dq) + b * a.qs.sample + h * a.qs.head, a.qs.token, own0,
                         a.Tq, a.D, lds + wave * 32 * HeadTile<DT, DP>::ROW_BYTES, lane);
   if (a.causal && __any(lane_end > 0 && not_finite(dq))) {
@@ -156,64 +167,65 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DT, DP)) attention_qu
   }
 }
 
-// dk and dv.  A wave owns 32 keys; tiles of queries and their output gradients go through LDS, with lse and delta.
-template <int DT, int DP, int NW>
-__global__ void __launch_bounds__(64 * NW, grad_workgroups(DT, DP)) attention_key_grad_kernel(const AttnArgs a) {
+// dk and dv.  A wave owns 32 keys (SPLIT waves the same ones); tiles of queries and their output gradients go through LDS, with lse and delta.
+template <int DT, int DP, int NW, int SPLIT>
+__global__ void __launch_bounds__(64 * NW * SPLIT, SPLIT == 8 ? 2 : SPLIT > 1 ? 1 : grad_workgroups(DT, DP)) attention_key_grad_kernel(const AttnArgs a) {
   extern __shared__ __align__(1024) char smem[];
   typedef Ops<DT> O;
   typedef typename O::E E;
-  constexpr int KS = HeadTile<DT, DP>::CHUNKS / 2, CB = DP / 32, TILE = kRows * HeadTile<DT, DP>::ROW_BYTES, STAGE = 2 * TILE + 512;
+  constexpr int KS = HeadTile<DT, DP>::CHUNKS / 2, CB = DP / 32, TILE = SPLIT * kRows * HeadTile<DT, DP>::ROW_BYTES, STAGE = 2 * TILE + 512 * SPLIT;
+  constexpr int SUB = kRows * HeadTile<DT, DP>::ROW_BYTES;
   constexpr bool V_IN_LDS = values_in_lds(DT, DP);
-  typedef TileLoader<DT, DP, kRows, NW> Loader;
+  typedef TileLoader<DT, DP, SPLIT * kRows, NW * SPLIT> Loader;
   int pair, block;
   attn_unit(a, a.first + blockIdx.x, pair, block);
   if (pair >= a.heads) return;
   // (A unit is a sample, a key head and a part of the query heads that share it.)
   const int part = pair % a.parts, b = pair / a.parts / a.H_kv, h = pair / a.parts % a.H_kv;
   const int heads = a.share / a.parts, q_head = h * a.share + part * heads;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = id % NW, turn = id / NW;
   const int n_q = valid_rows(a.q_len, b, a.Tq), n_k = valid_rows(a.k_len, b, a.Tk), shift = n_k - n_q;
   const int key0 = block * 32 * NW, own0 = key0 + 32 * wave, key = own0 + (lane & 31);
   const unsigned lds = (unsigned)(uintptr_t)DP_LDS(char, smem);
   // Queries from here on see a key of the workgroup, of this wave; and the first that sees the lane's.
   const int begin = a.causal ? max(key0 - shift, 0) & ~31 : 0;
   const int own_begin = own0 >= n_k ? INT32_MAX : a.causal ? max(own0 - shift, 0) : 0, lane_begin = a.causal ? key - shift : 0;
-  const int tiles = key0 < n_k && begin < n_q ? (n_q - begin + kRows - 1) / kRows : 0;       // of one query head
+  const int tiles = key0 < n_k && begin < n_q ? (n_q - begin + SPLIT * kRows - 1) / (SPLIT * kRows) : 0;       // of one query head
 
   const int64_t kv = b * a.ks.sample + h * a.ks.head, vv = b * a.vs.sample + h * a.vs.head;
   typename O::Row kf[KS], vf[V_IN_LDS ? 1 : KS];
   load_own<DT>(kf, static_cast<const E*>(a.k) + kv, a.ks.token, key, key < n_k, a.D, lane);
   if constexpr (V_IN_LDS) {
     // Own keys and values, two sums, scores and their gradients are 224 registers at a width of 128: the values stay in LDS.
-    TileLoader<DT, DP, 32 * NW, NW> own;
-    own.init(static_cast<const E*>(a.v) + vv, a.vs.token, a.D, wave, lane);
-    own.load(key0, n_k, lds + 2 * STAGE, wave);
+    TileLoader<DT, DP, 32 * NW, NW * SPLIT> own;
+    own.init(static_cast<const E*>(a.v) + vv, a.vs.token, a.D, id, lane);
+    own.load(key0, n_k, lds + 2 * STAGE, id);
   } else {
     load_own<DT>(vf, static_cast<const E*>(a.v) + vv, a.vs.token, key, key < n_k, a.D, lane);
   }
   TileReader<DT, DP> read;
-  read.init(lds, lane);
-  const unsigned own_values = 2 * STAGE + wave * (32 * HeadTile<DT, DP>::ROW_BYTES);
+  read.init(lds + turn * SUB, lane);
+  const unsigned own_values = 2 * STAGE + wave * SUB - turn * SUB;
   Loader q_tiles, d_tiles;
-  q_tiles.init(static_cast<const E*>(a.q) + b * a.qs.sample + q_head * a.qs.head, a.qs.token, a.D, wave, lane);
-  d_tiles.init(static_cast<const E*>(a.dout) + b * a.os.sample + q_head * a.os.head, a.os.token, a.D, wave, lane);
+  q_tiles.init(static_cast<const E*>(a.q) + b * a.qs.sample + q_head * a.qs.head, a.qs.token, a.D, id, lane);
+  d_tiles.init(static_cast<const E*>(a.dout) + b * a.os.sample + q_head * a.os.head, a.os.token, a.D, id, lane);
   int64_t corr = ((int64_t)b * a.H + q_head) * a.Tq;
   // Tiles of the part's query heads, one behind the other; first row of the one that is loaded next.
   int next_row = begin;
   auto load = [&](int stage) {
     const unsigned to = lds + stage * STAGE;
-    q_tiles.load(next_row, n_q, to, wave);
-    d_tiles.load(next_row, n_q, to + TILE, wave);
-    const int bytes = 4 * min(a.Tq - next_row, kRows);
+    q_tiles.load(next_row, n_q, to, id);
+    d_tiles.load(next_row, n_q, to + TILE, id);
+    const int corr_row = min(next_row + turn * kRows, a.Tq), bytes = 4 * min(a.Tq - corr_row, kRows);
     if (wave == 0)
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      i32x4 r = make_rsrc((k ? a.delta : a.lse2) + corr + next_row, bytes);
+      i32x4 r = make_rsrc((k ? a.delta : a.lse2) + corr + corr_row, bytes);
 #pragma unroll
       for (int i = 0; i < 3; ++i) r[i] = __builtin_amdgcn_readfirstlane(r[i]);
-      load_dword_to_lds(r, 4 * lane, to + 2 * TILE + 256 * k);
+      load_dword_to_lds(r, 4 * lane, to + 2 * TILE + 512 * turn + 256 * k);
     }
-    next_row += kRows;
+    next_row += SPLIT * kRows;
     if (next_row >= n_q) {
       next_row = begin;
       q_tiles.base += O::SIZE * a.qs.head;
@@ -221,7 +233,7 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DT, DP)) attention_ke
       corr += a.Tq;
     }
   };
-  const unsigned pairs = lds + 2 * TILE + 16 * (lane >> 5);
+  const unsigned pairs = lds + 2 * TILE + 512 * turn + 16 * (lane >> 5);
   auto four = [&](int at) { return *(__attribute__((address_space(3))) const f32x4*)(uintptr_t)(pairs + at); };
   // Scores, and do v' - delta.
   auto products = [&](f32x16& s, f32x16& dp, int stage) {
@@ -262,9 +274,9 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DT, DP)) attention_ke
     constexpr int HERE = decltype(stage)::value;
     tiles_landed();
     if (t + 1 < steps) load(HERE ^ 1);
-    const int i0 = first;
-    first = first + kRows < n_q ? first + kRows : begin;
-    if (i0 + 31 < own_begin) return;              // no query of the tile sees a key of the wave
+    const int i0 = first + turn * kRows;
+    first = first + SPLIT * kRows < n_q ? first + SPLIT * kRows : begin;
+    if (i0 + 31 < own_begin || i0 >= n_q) return;         // no query of the tile sees a key of the wave
     f32x16 p, ds;
     products(p, ds, HERE);
     // Instruction m: columns m / 2 % CB of rows 16 (m / 2 / CB) on, of dv or of dk.
@@ -303,6 +315,21 @@ __global__ void __launch_bounds__(64 * NW, grad_workgroups(DT, DP)) attention_ke
             });
   });
   tiles_landed();                                 // LDS is free
+  if constexpr (SPLIT > 1) {
+    constexpr int EACH = handed_floats(32 * CB);
+    float* const mine = reinterpret_cast<float*>(smem) + (id - NW) * EACH;
+    if (turn > 0) {
+      hand_over(dk, mine, lane);
+      hand_over(dv, mine + EACH / 2, lane);
+    }
+    tiles_landed();
+    if (turn > 0) return;
+#pragma unroll
+    for (int w = 1; w < SPLIT; ++w) {
+      take_over(dk, mine + w * NW * EACH, lane);
+      take_over(dv, mine + w * NW * EACH + EACH / 2, lane);
+    }
+  }
   float *dk_part = nullptr, *dv_part = nullptr;
   if (a.parts > 1) {
     dk_part = a.partial + (((int64_t)part * a.B + b) * a.H_kv + h) * a.Tk * a.D;
@@ -361,30 +388,30 @@ __global__ void __launch_bounds__(256) attention_key_grad_rows_kernel(const Attn
   if (j < a.Tk) rows.key_gradient(j, rows.h * a.share, (rows.h + 1) * a.share, nullptr, nullptr);
 }
 
-template <int DT, int DP, int NW>
+template <int DT, int DP, int NW, int SPLIT>
 dp_status launch_queries(AttnArgs a, hipStream_t s) {
   a.heads = a.B * a.H;
   a.blocks = (a.Tq + 32 * NW - 1) / (32 * NW);
-  constexpr int LDS = 4 * kRows * HeadTile<DT, DP>::ROW_BYTES;
-  auto kernel = attention_query_grad_kernel<DT, DP, NW>;
+  constexpr int LDS = 4 * SPLIT * kRows * HeadTile<DT, DP>::ROW_BYTES;
+  auto kernel = attention_query_grad_kernel<DT, DP, NW, SPLIT>;
   static ReadyTable done;
   if (LDS > 65536) {
     const dp_status st = allow_big_lds(kernel, LDS, done);
     if (st != DP_OK) return st;
   }
-  return launch_attention(kernel, a, (int64_t)2 * Ops<DT>::SIZE * a.Tk * a.D, 64 * NW, LDS, s);
+  return launch_attention(kernel, a, (int64_t)2 * Ops<DT>::SIZE * a.Tk * a.D, 64 * NW * SPLIT, LDS, s);
 }
 
-template <int DT, int DP, int NW>
+template <int DT, int DP, int NW, int SPLIT>
 dp_status launch_keys(AttnArgs a, hipStream_t s) {
   a.heads = a.B * a.H_kv * a.parts;
   a.blocks = (a.Tk + 32 * NW - 1) / (32 * NW);
-  constexpr int LDS = 2 * (2 * kRows * HeadTile<DT, DP>::ROW_BYTES + 512) + (values_in_lds(DT, DP) ? 32 * NW * HeadTile<DT, DP>::ROW_BYTES : 0);
-  auto kernel = attention_key_grad_kernel<DT, DP, NW>;
+  constexpr int LDS = 2 * SPLIT * (2 * kRows * HeadTile<DT, DP>::ROW_BYTES + 512) + (values_in_lds(DT, DP) ? 32 * NW * HeadTile<DT, DP>::ROW_BYTES : 0);
+  auto kernel = attention_key_grad_kernel<DT, DP, NW, SPLIT>;
   static ReadyTable done;
   dp_status st = DP_OK;
   if (LDS > 65536) st = allow_big_lds(kernel, LDS, done);
-  if (st == DP_OK) st = launch_attention(kernel, a, (int64_t)2 * Ops<DT>::SIZE * a.Tq * a.D * (a.share / a.parts), 64 * NW, LDS, s);
+  if (st == DP_OK) st = launch_attention(kernel, a, (int64_t)2 * Ops<DT>::SIZE * a.Tq * a.D * (a.share / a.parts), 64 * NW * SPLIT, LDS, s);
   if (st != DP_OK || a.parts == 1) return st;
   const int64_t pieces = (int64_t)a.B * a.H_kv * a.Tk * a.D / 4;
   return launch_in_runs((2 * pieces + 255) / 256, [&](dim3 grid, int first) {
@@ -396,9 +423,13 @@ dp_status launch_keys(AttnArgs a, hipStream_t s) {
 
 template <int DT, int DP>
 dp_status launch(const AttnArgs& a, hipStream_t s) {
-  const dp_status st = a.Tq <= 32 ? launch_queries<DT, DP, 1>(a, s) : launch_queries<DT, DP, 4>(a, s);
+  constexpr int SPLIT = split_waves(HeadTile<DT, DP>::ROW_BYTES);
+  const dp_status st = split_rows<DT>((int64_t)a.B * a.H, a.Tq, a.Tk) ? launch_queries<DT, DP, 1, SPLIT>(a, s)
+                       : a.Tq <= 32                               ? launch_queries<DT, DP, 1, 1>(a, s)
+                                                                  : launch_queries<DT, DP, 4, 1>(a, s);
   if (st != DP_OK) return st;
-  return a.Tk <= 32 ? launch_keys<DT, DP, 1>(a, s) : launch_keys<DT, DP, 4>(a, s);
+  if (split_rows<DT>((int64_t)a.B * a.H_kv * a.parts, a.Tk, a.Tq)) return launch_keys<DT, DP, 1, SPLIT>(a, s);
+  return a.Tk <= 32 ? launch_keys<DT, DP, 1, 1>(a, s) : launch_keys<DT, DP, 4, 1>(a, s);
 }
 
 template <int DT>

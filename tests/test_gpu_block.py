@@ -369,6 +369,29 @@ def test_attention_odd_strides(block):
         assert rel(got, ref) <= 2 * FP32                                    # both sides within FP32 of the same
 
 
+# Few rows on one side and many on the other: waves take these in turn and are joined.  (The shapes of many tokens are for what is beside
+# the rows: lengths that leave some waves nothing, a mask that ends within a turn.)
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("Tq,Tk,H,Hkv,D,q_len,k_len", [
+    (1, 1500, 2, 1, 64, None, None), (5, 1100, 2, 2, 128, None, [1100, 37]), (40, 1999, 4, 2, 96, [40, 17], [65, 1999]),
+    (1300, 6, 2, 1, 64, [1300, 1], None), (1057, 1057, 1, 1, 32, [1057, 33], [1057, 33]), (1, 1024, 1, 1, 128, None, [0, 1024]),
+    (1025, 1, 2, 2, 64, None, None), (70, 1200, 2, 1, 8, [0, 70], [1200, 1000])], ids=str)
+def test_attention_of_few_rows(block, dtype, Tq, Tk, H, Hkv, D, q_len, k_len, causal):
+    Case(block, dtype, 2, Tq, Tk, H, Hkv, D, causal, q_len=q_len, k_len=k_len).check()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_attention_of_few_rows_ignores_what_is_not_seen(block, dtype):
+    c = Case(block, dtype, 2, 9, 1300, 2, 1, 64, True, q_len=[9, 4], k_len=[1300, 800])
+    c.k[1, 800:], c.v[1, 800:], c.q[1, 4:], c.do[1, 4:] = math.nan, math.inf, math.nan, math.inf
+    c.v[0, 1299] = math.inf                               # the last row alone sees it
+    o, lse, grads = c.run()
+    want, want_lse = c.reference()
+    assert rel(lse, want_lse) <= FP32 and rel(o[0, :8], want[0, :8]) <= max(2.5 * U[dtype], FP32) and rel(o[1], want[1]) <= max(2.5 * U[dtype], FP32)
+    assert not torch.isfinite(o[0, 8]).any() and all(torch.isfinite(g[1]).all() for g in grads) and torch.isfinite(grads[0][0, :8]).all()
+
+
 # Few key heads that many query heads share: the heads' sums are formed in parts and joined.
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("shape", [(1, 33, 33, 6, 1, 64), (1, 128, 128, 7, 1, 128), (1, 100, 260, 12, 2, 32), (2, 20, 20, 48, 6, 96),
