@@ -6,11 +6,13 @@
 // the register (8 (r / 4) + 4 (lane / 32) + r % 4) and the wave's own row in the lane (lane % 32), so that
 //  * a softmax over keys is a reduction within a lane and one exchange between its halves, and maxima, sums and their
 //    corrections are one value a lane;
-//  * sixteen such values, rounded to 16 bits, are the second operand of the next product as they lie: lane half h holds
+//  * sixteen such values, rounded to 16 bits (fp32: as they are), are the second operand of the next product as they lie: lane half h holds
 //    rows 4 h .. 4 h + 3 and 8 + 4 h .. 8 + 4 h + 3 of every 16.  A sum does not care for its order, so the first operand is
 //    read in the same one (two transposing LDS reads, of rows 4 h and 8 + 4 h on), and no probability passes through LDS.
+// Rounding a probability or a score's gradient to the type costs half a unit of it, independently of the others: as much as the result's own
+// rounding; sums, maxima, lse and delta are fp32.
 //
-// LDS holds rows of a head (DP columns of 16 bits) as they come from memory, 16-byte chunks XOR-swizzled by row such that eight
+// LDS holds rows of a head (DP columns) as they come from memory, 16-byte chunks XOR-swizzled by row such that eight
 // rows' reads of one column and the transposing reads of four rows fall on different banks.
 #pragma once
 

@@ -8,7 +8,12 @@ namespace {
 
 constexpr float kLazy = 8.f;                      // a maximum may be passed by 2^8 before sums are expressed in a new one
 
-// NW waves of 32 queries each, tiles of KEYS keys in two stages.
+// NW waves of 32 queries each (SPLIT waves the same ones, whose turns at the tiles are joined at the end), tiles of KEYS keys in two stages.
+// A pair's keys and values come out of L2 for all blocks but the first; what is left is work on scores: four matrix instructions a tile for
+// D = 64 and as many issue cycles of exponentials, maxima and roundings beside them, with a barrier a tile, three workgroups to a
+// unit.  2 x 4096 causal tokens, 12 heads of 64, bf16: 69 us, 750 TFLOP/s of the 1400 of a large product.  16 x 256: 10 us and 32 x 197
+// (fp16, all seen) 14 us for the 5 and 8 that q, k, v and o take from memory: a launch, and a workgroup's loads, few tiles and stores one after
+// the other.  Tried without gain: four stages, two and eight waves, operands asked for ahead in a fixed order.
 template <int DT, int DP, int NW, int SPLIT, int KEYS>
 __global__ void __launch_bounds__(64 * NW * SPLIT, 2) attention_kernel(const AttnArgs a) {
   extern __shared__ __align__(1024) char smem[];
@@ -153,6 +158,7 @@ __global__ void __launch_bounds__(64 * NW * SPLIT, 2) attention_kernel(const Att
   }
 }
 
+// fp32 rows of no whole 16-byte pieces, four to a workgroup.
 __global__ void __launch_bounds__(256) attention_rows_kernel(const AttnArgs a) {
   int pair, block;
   attn_unit(a, a.first + blockIdx.x, pair, block);
@@ -179,11 +185,15 @@ dp_status launch(AttnArgs a, hipStream_t s) {
 
 template <int DT, int DP>
 dp_status launch(const AttnArgs& a, hipStream_t s) {
-  constexpr int KEYS = DT == DP_F32 ? 32 : 64, SPLIT = split_waves(HeadTile<DT, DP>::ROW_BYTES);
+  constexpr int LONG = DT == DP_F32 ? 32 : 64, SPLIT = split_waves(HeadTile<DT, DP>::ROW_BYTES);
   if (split_rows<DT>((int64_t)a.B * a.H, a.Tq, a.Tk)) return launch<DT, DP, 1, SPLIT, 32>(a, s);
+  // One wave for few queries (512 x 32 tokens, 12 heads of 64: 20 us, with four 40), two up to 64 (256 x 48: 17 and 24).  Tiles of 64 keys hide
+  // more of a turn's latency (1 x 3000 tokens, 9 heads: 39 us, of 32 keys 48), but leave more of a short row's last tile empty (64 x 128: 13.7 and
+  // 12.4; 32 x 197 14.7 and 13.8; 18 x 591 34 and 36).
   if (a.Tq <= 32) return launch<DT, DP, 1, 1, 32>(a, s);
   if (a.Tq <= 64) return launch<DT, DP, 2, 1, 32>(a, s);
-  return launch<DT, DP, 4, 1, KEYS>(a, s);
+  if (a.Tk <= 256) return launch<DT, DP, 4, 1, 32>(a, s);
+  return launch<DT, DP, 4, 1, LONG>(a, s);
 }
 
 template <int DT>

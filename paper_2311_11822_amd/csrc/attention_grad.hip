@@ -9,20 +9,26 @@ namespace dpbk {
 
 namespace {
 
-// Both kernels go through tiles of 32 rows of the other side, in two stages.  (A ring of four changes nothing.)
-// (With the next tile's scores and do v' beside the exponentials, as in the forward pass, there are registers for two workgroups of
-// width 64 instead of three: 2 x 4096 tokens, 12 heads, 214 us where this takes 233; 8 x 512, 20 heads, 56 and 48; 32 x 197 50 and 41.)
+// Both kernels go through tiles of 32 rows of the other side, in two stages, a barrier a tile.  Bound by the turn of a tile, not by the
+// matrix cores' rate: its products depend on each other through the exponentials, and registers allow two or three workgroups to a unit to fill the
+// gaps.  4 x 2048 causal tokens, 96 heads of 128, bf16: 1520 us (dq 44 % of it), 1.0e12 operations that count (1.4e12 done): 680 TFLOP/s, half
+// of a large product's rate.  8 x 512, 20 heads of 64: 21 and 24 us for the 17 that the tensors take from memory.
+// Tried without gain: a ring of four stages; the next tile's scores beside the exponentials, as in the forward pass (there are registers for two
+// workgroups of width 64 instead of three: 2 x 4096 tokens, 12 heads, 7 % faster at the time, 8 x 512 17 % slower); two and eight waves; one
+// wave to a SIMD with 512 registers.
 constexpr int kRows = 32;
 constexpr int kPartUnits = 256;                   // compute units
 // Workgroups to a compute unit, as registers allow; operands asked for ahead: what is left of them.
 constexpr int grad_workgroups(int DT, int DP) { return DT == DP_F32 ? (DP <= 64 ? 2 : 1) : DP <= 64 ? 3 : 2; }
+constexpr int grad_waves(int DT, int DP, int SPLIT) { return SPLIT == 8 ? 2 : SPLIT > 1 ? 1 : grad_workgroups(DT, DP); }     // to a SIMD
 constexpr int grad_ahead(int DT, int DP) { return DT == DP_F32 || DP <= 64 ? 2 : 4; }
 // Own keys and values, two sums, scores and their gradients are 224 registers at a width of 128: there the values stay in LDS.
 constexpr bool values_in_lds(int DT, int DP) { return DT != DP_F32 && DP == 128; }
 
-// dq, and for the other kernel lse in units of log 2 and delta.
+// dq, and for the other kernel lse in units of log 2 and delta.  A wave owns 32 queries (SPLIT waves the same ones).
 template <int DT, int DP, int NW, int SPLIT>
-__global__ void __launch_bounds__(64 * NW * SPLIT, SPLIT == 8 ? 2 : SPLIT > 1 ? 1 : grad_workgroups(DT, DP)) attention_query_grad_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(64 * NW * SPLIT, grad_waves(DT, DP, SPLIT))
+attention_query_grad_kernel(const AttnArgs a) {
   extern __shared__ __align__(1024) char smem[];
   typedef Ops<DT> O;
   typedef typename O::E E;
@@ -169,7 +175,8 @@ __global__ void __launch_bounds__(64 * NW * SPLIT, SPLIT == 8 ? 2 : SPLIT > 1 ? 
 
 // dk and dv.  A wave owns 32 keys (SPLIT waves the same ones); tiles of queries and their output gradients go through LDS, with lse and delta.
 template <int DT, int DP, int NW, int SPLIT>
-__global__ void __launch_bounds__(64 * NW * SPLIT, SPLIT == 8 ? 2 : SPLIT > 1 ? 1 : grad_workgroups(DT, DP)) attention_key_grad_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(64 * NW * SPLIT, grad_waves(DT, DP, SPLIT))
+attention_key_grad_kernel(const AttnArgs a) {
   extern __shared__ __align__(1024) char smem[];
   typedef Ops<DT> O;
   typedef typename O::E E;
@@ -406,7 +413,8 @@ template <int DT, int DP, int NW, int SPLIT>
 dp_status launch_keys(AttnArgs a, hipStream_t s) {
   a.heads = a.B * a.H_kv * a.parts;
   a.blocks = (a.Tk + 32 * NW - 1) / (32 * NW);
-  constexpr int LDS = 2 * SPLIT * (2 * kRows * HeadTile<DT, DP>::ROW_BYTES + 512) + (values_in_lds(DT, DP) ? 32 * NW * HeadTile<DT, DP>::ROW_BYTES : 0);
+  constexpr int ROW = HeadTile<DT, DP>::ROW_BYTES;
+  constexpr int LDS = 2 * SPLIT * (2 * kRows * ROW + 512) + (values_in_lds(DT, DP) ? 32 * NW * ROW : 0);
   auto kernel = attention_key_grad_kernel<DT, DP, NW, SPLIT>;
   static ReadyTable done;
   dp_status st = DP_OK;
@@ -424,6 +432,7 @@ dp_status launch_keys(AttnArgs a, hipStream_t s) {
 template <int DT, int DP>
 dp_status launch(const AttnArgs& a, hipStream_t s) {
   constexpr int SPLIT = split_waves(HeadTile<DT, DP>::ROW_BYTES);
+  // (One wave for few rows: 512 x 32 tokens, 12 heads of 64: 64 us, with four 95.)
   const dp_status st = split_rows<DT>((int64_t)a.B * a.H, a.Tq, a.Tk) ? launch_queries<DT, DP, 1, SPLIT>(a, s)
                        : a.Tq <= 32                               ? launch_queries<DT, DP, 1, 1>(a, s)
                                                                   : launch_queries<DT, DP, 4, 1>(a, s);

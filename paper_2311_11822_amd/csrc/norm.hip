@@ -225,7 +225,8 @@ __global__ void __launch_bounds__(kThreads) layer_norm_kernel(const NormArgs a, 
 // alone (140 us where only dx is asked for); 214 us with loads where they are used and gain out of L2.  16 x 256 rows of 768: 12 us,
 // most of it two launches and a wave's two or three turns to memory.  Shifted rows: 2048 x 12289 fp16 81 us, an element at a time 319.
 template <int DT, int VEC, int TPR, int P, int THREADS, bool SHIFT>
-__global__ void __launch_bounds__(THREADS, THREADS == 1024 || P <= (DT == DP_F32 ? 8 : SHIFT ? 16 : 24) ? 4 : 2) layer_norm_backward_kernel(const NormArgs a, int first_block) {
+__global__ void __launch_bounds__(THREADS, THREADS == 1024 || P <= (DT == DP_F32 ? 8 : SHIFT ? 16 : 24) ? 4 : 2)
+layer_norm_backward_kernel(const NormArgs a, int first_block) {
   constexpr int N = P / VEC, GROUPS = THREADS / TPR;
   constexpr bool AHEAD = P <= 32;                  // (no registers for it beyond)
   extern __shared__ __align__(16) float lds[];     // gain; then, in the same place, sums over groups
@@ -543,7 +544,8 @@ dp_status launch_layer_norm_backward(NormArgs a, dp_dtype dt, hipStream_t s) {
         constexpr int DT = decltype(type)::value, VEC = piece_values(DT), TPR = decltype(tpr)::value, GROUPS = THREADS / TPR;
         constexpr bool SHIFT = decltype(shift)::value;
         auto kernel = layer_norm_backward_kernel<DT, VEC, TPR, decltype(per)::value, THREADS, SHIFT>;
-        const int lds = 4 * std::max(a.d + (SHIFT ? 2 * VEC : 0), GROUPS == 1 ? 0 : SHIFT ? GROUPS * ((a.d + 2 * VEC - 1) / VEC * VEC) : GROUPS * 2 * VEC * TPR);
+        const int sums = GROUPS == 1 ? 0 : SHIFT ? GROUPS * ((a.d + 2 * VEC - 1) / VEC * VEC) : GROUPS * 2 * VEC * TPR;
+        const int lds = 4 * std::max(a.d + (SHIFT ? 2 * VEC : 0), sums);
         static ReadyTable done;
         if (lds > 65536) {
           const dp_status ready = allow_big_lds(kernel, 4 * (kNormMaxWidth + 16), done);
