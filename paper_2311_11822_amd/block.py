@@ -24,15 +24,19 @@ def _same(name: str, x: Optional[torch.Tensor], shape, dtype, device) -> None:
 
 
 class _Workspaces:
-    """Scratch memory, one for each device and stream (calls on different streams do not share one) that grows as calls need."""
+    """Scratch memory, one for each device and stream (calls on different streams do not share one) that grows as calls need.  What it has
+    outgrown stays as long as the object (a captured graph may have its address); by halves at least, so all of it is bounded."""
 
     def __init__(self):
-        self.held = {}
+        self.held, self.outgrown = {}, []
 
     def __call__(self, nbytes: int, device: torch.device, index: int, stream: int) -> torch.Tensor:
         ws = self.held.get((index, stream))
         if ws is None or ws.numel() < nbytes:
-            # of that stream's own memory: what is given back is not handed to another stream while calls still use it
+            if ws is not None:
+                self.outgrown.append(ws)
+                nbytes = max(nbytes, ws.numel() * 3 // 2)
+            # of that stream's own memory: what comes from another's may still be in use there
             current = torch.cuda.current_stream(device)
             own = current if current.cuda_stream == stream else torch.cuda.ExternalStream(stream, device)
             with torch.cuda.stream(own):

@@ -689,3 +689,39 @@ def test_workspaces_grow_and_follow_streams(block):
             torch.cuda.synchronize()
             out.append((dx, kept, sq))
         assert all(torch.equal(a, b) for other in out[1:] for a, b in zip(other, out[0]))
+
+
+def test_a_captured_workspace_stays(block):
+    """A graph that holds a workspace's address is replayed after the object has needed a larger one."""
+    gen = torch.Generator().manual_seed(9)
+    norm = block.LayerNorm(None, None)
+
+    def case(T):
+        x, dy = (rand(gen, (2, T, 512), "f32").cuda() for _ in range(2))
+        stats = torch.empty((2, T), device="cuda"), torch.empty((2, T), device="cuda")
+        norm.forward(x, torch.empty_like(x), *stats)
+        dx, kept, sq = torch.empty_like(x), torch.empty((2, 2, 512), device="cuda"), torch.empty(2, device="cuda")
+        return (lambda: norm.backward(x, dy, *stats, dx, kept, sq)), (dx, kept, sq)
+
+    side = torch.cuda.Stream()
+    small, outputs = case(200)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        small()
+    side.synchronize()
+    want = [t.clone() for t in outputs]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        small()
+    large, _ = case(4000)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        with torch.cuda.stream(side):
+            large()
+            guard = [torch.full((1 << 14,), 5.0, device="cuda") for _ in range(64)]       # would take freed memory
+        side.synchronize()
+        for t in outputs:
+            t.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outputs, want)) and all((g == 5.0).all() for g in guard)
