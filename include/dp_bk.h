@@ -442,18 +442,19 @@ dp_status dp_layer_norm_backward(const void* x, const void* dy, const void* add,
  * Attention of Tq queries over Tk keys, H heads of width D:  o_i = sum_j p_ij v_j,  p_ij = exp(scale q_i . k_j - lse_i)
  * over the keys j that row i sees, lse_i = log sum_j exp(scale q_i . k_j).
  *   Heads: H_kv divides H; query heads h share key head h / (H / H_kv).
- *   Layout: element strides of sample, token and head, for q, k, v and o; columns are adjacent.  Packed projections ([B, T, 3 * H * D] and
- *     the like) need no copies.  Strides are >= 0 and, for 16-bit types, multiples of 8; a token stride is from D to 2^23 (of one
- *     token: whatever).  What is read may be broadcast (stride 0); what is written may not overlap itself: by growing stride, each
- *     axis steps over all that the ones before span (DP_ERR_INVALID_ARG else; the gradients have the strides of q, k and v).
+ *   Layout: element strides of sample, token and head, for q, k, v and o; columns are adjacent.  Packed projections
+ *     ([B, T, 3 * H * D] and the like) need no copies.  Strides are >= 0 and, for 16-bit types, multiples of 8; a token stride is
+ *     from D to 2^23 (of one token: whatever).  What is read may be broadcast (stride 0); what is written may not overlap
+ *     itself: by growing stride, each axis steps over all that the ones before span (DP_ERR_INVALID_ARG else; the gradients have
+ *     the strides of q, k and v).
  *   Lengths: q_len[b] queries and k_len[b] keys of sample b are there (device, [B] int32; NULL: all; values are held to 0 .. T).
  *     What lies behind them is not read.
  *   causal = 1: the ends are aligned; row i sees keys up to i + (keys there) - (queries there).
  * Rows that see no key, and rows that are not there, are zeros, with lse = -infinity.  What a row does not see does not reach
  * it, infinities and NaN included.
  * D is at most 128 and, for 16-bit types, a multiple of 8.  All types run on the matrix cores, 16-bit ones with
- * probabilities rounded to the type before their product with v; DP_F32 whose D or strides are not multiples of 4, or whose arrays are not 16-byte aligned, runs on the vector
- * units, for small networks.  scale is positive and finite.
+ * probabilities rounded to the type before their product with v; DP_F32 whose D or strides are not multiples of 4, or whose
+ * arrays are not 16-byte aligned, runs on the vector units, for small networks.  scale is positive and finite.
  */
 typedef struct {
   int32_t B, H, H_kv, Tq, Tk, D;
@@ -468,9 +469,12 @@ typedef struct {
  *   shape     HOST
  *   q, k, v, o   device, of type dt, 16-byte aligned (DP_F32: 4-byte; the matrix cores want 16)
  *   lse       device, [B, H, Tq] fp32, kept for the backward pass
+ *   ws        device scratch, >= dp_attention_workspace_bytes(...), 16-byte aligned, with which few queries (single tokens) on many keys are
+ *             spread over the device; or NULL: slower there, otherwise the same to rounding.  The size is 0 where it is not used.
  */
+size_t dp_attention_workspace_bytes(const dp_attention_shape* shape, dp_dtype dt);
 dp_status dp_attention(const dp_attention_shape* shape, dp_dtype dt, const void* q, const void* k, const void* v, void* o, float* lse,
-                       void* stream);
+                       void* ws, size_t ws_bytes, void* stream);
 
 /*
  * Backward pass, which forms the probabilities again from lse:
@@ -494,11 +498,12 @@ dp_status dp_attention_backward(const dp_attention_shape* shape, dp_dtype dt, co
  *   tensors     HOST array; param fp32 [n]; grad [n] of type grad_dt; n = 0: nothing to do.  Elements need no more than their own
  *               alignment; where all of a tensor's arrays are aligned to four elements they are moved four at a time.
  *   state_bits  32: m and v are fp32 [n].
- *               8: m and the root of v are e4m3 numbers (sign, 4 bits of exponent, 3 of fraction; largest 448), one byte each [n], in units of
- *               m_scale and v_scale, fp32 [ceil(n / 256)]: the largest magnitude of each 256 values, over 448.  A value is
- *               rounded up where its place between its neighbours (v's: between their squares) is at least 1 - f, f the fractional part of e (sqrt(2) - 1) + step (golden ratio - 1) for
- *               element e (in 32-bit integers: (e * 0x6A09E667 + step * 0x9E3779B1) >> 8, over 2^24), so that slow averages do
- *               move; one above zero is not rounded to zero.  All-zero bytes and scales are zero states.
+ *               8: m and the root of v are e4m3 numbers (sign, 4 bits of exponent, 3 of fraction; largest 448), one byte each [n], in
+ *               units of m_scale and v_scale, fp32 [ceil(n / 256)]: the largest magnitude of each 256 values, over 448.  A value is
+ *               rounded up where its place between its neighbours (v's: between their squares) is at least 1 - f, f the fractional
+ *               part of e (sqrt(2) - 1) + step (golden ratio - 1) for element e (in 32-bit integers: (e * 0x6A09E667 + step *
+ *               0x9E3779B1) >> 8, over 2^24), so that slow averages do move; one above zero is not rounded to zero.  All-zero bytes
+ *               and scales are zero states.
  *               An infinite or undefined state makes those of its 256 undefined.
  *   copy_dt     DP_BF16 or DP_F16: the new param is also written to copy [n], rounded to nearest even; DP_F32: copy is not used
  *   step        counts from 1

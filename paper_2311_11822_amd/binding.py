@@ -89,7 +89,8 @@ _PROTOS = {
     "dp_layer_norm": (_i, [_vp, _vp, _i, _i, _i, _i, _vp, _vp, _f, _vp, _vp, _vp, _vp, _vp]),
     "dp_layer_norm_workspace_bytes": (_sz, [_i, _i, _i, _i]),
     "dp_layer_norm_backward": (_i, [_vp, _vp, _vp, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
-    "dp_attention": (_i, [C.POINTER(dp_attention_shape), _i, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "dp_attention_workspace_bytes": (_sz, [C.POINTER(dp_attention_shape), _i]),
+    "dp_attention": (_i, [C.POINTER(dp_attention_shape), _i, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "dp_attention_backward_workspace_bytes": (_sz, [C.POINTER(dp_attention_shape), _i]),
     "dp_attention_backward": (_i, [C.POINTER(dp_attention_shape), _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "dp_adamw_multi": (_i, [C.POINTER(dp_adamw_tensor), _i, _i, _i, _i, C.c_double, C.c_double, C.c_double, C.c_double, C.c_double,
@@ -353,8 +354,12 @@ def attention_shape(B, H, H_kv, Tq, Tk, D, causal, scale, q_stride, k_stride, v_
         _ptr(q_len), _ptr(k_len)))
 
 
-def dp_attention(shape, dt, q, k, v, o, lse, stream=None) -> None:
-    _call("dp_attention", shape, dt, q, k, v, o, lse, stream)
+def dp_attention_workspace_bytes(shape, dt) -> int:
+    return lib.dp_attention_workspace_bytes(shape, dt)
+
+
+def dp_attention(shape, dt, q, k, v, o, lse, ws=None, stream=None) -> None:
+    _call("dp_attention", shape, dt, q, k, v, o, lse, ws, _nbytes(ws), stream)
 
 
 def dp_attention_backward_workspace_bytes(shape, dt) -> int:

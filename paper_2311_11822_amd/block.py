@@ -123,6 +123,7 @@ class Attention:
         self.shape = dp.attention_shape(B, H, H_kv, Tq, Tk, D, causal, scale, *strides, q_len, k_len)
         self._check((q, o), (k, v), (q, k, v, o), None)
         self._ws, self._need = _Workspaces(), dp.dp_attention_backward_workspace_bytes(self.shape, self.dt)
+        self._forward_need = dp.dp_attention_workspace_bytes(self.shape, self.dt)
         if self._need == 0:
             raise ValueError("sizes, strides or scale that attention does not take")
         if self.index < 0:
@@ -145,7 +146,11 @@ class Attention:
     def forward(self, q, k, v, o, lse, stream=None) -> None:
         """o in its strides; lse: [B, H, Tq] float32, kept for backward."""
         self._check((q, o), (k, v), (q, k, v, o), lse)
-        dp.dp_attention(self.shape, self.dt, q, k, v, o, lse, stream)
+        ws = None
+        if self._forward_need:
+            stream = dp._stream(stream)
+            ws = self._ws(self._forward_need, self.device, self.index, stream)
+        dp.dp_attention(self.shape, self.dt, q, k, v, o, lse, ws, stream)
 
     def backward(self, q, k, v, o, lse, do, dq, dk, dv, stream=None) -> None:
         """do in o's strides; dq, dk, dv in those of q, k and v."""

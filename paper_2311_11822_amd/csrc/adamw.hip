@@ -2,7 +2,7 @@
 //   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,  g = grad_scale * grad,
 //   w = w (1 - lr decay) - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps).
 // A stream over memory: 28 bytes an element with 32-bit states and gradients, 16 with 8-bit states.  A stack of 85 million parameters, 32 bits
-// and a bf16 copy, in two launches: 500 us, 5.1 TB/s, what a copy reaches.  226 million with 8-bit states: 784 to 804 us, 4.6 TB/s, some
+// and a bf16 copy, in two launches: 500 us, 5.1 TB/s, what a copy reaches.  226 million with 8-bit states: 784 to 808 us, 4.6 TB/s, some
 // 130 vector instructions an element beside it.
 //
 // 8-bit states are e4m3 numbers in units of their block's largest / 448, m itself and the root of v (whose range they cover where

@@ -37,7 +37,8 @@ struct AttnArgs {
   int Tq, Tk, D;
   int causal;
   int parts;                      // key gradients: the query heads of a key head are dealt to this many workgroups
-  float* partial;                 // parts > 1: [2 (dk, dv)][parts][B][H_kv][Tk][D]
+  float* partial;                 // parts > 1: [2 (dk, dv)][parts][B][H_kv][Tk][D]; key_parts > 1: [key_parts][B][H][Tq][D], then maximum and sum
+  int key_parts, part_keys;       // forward: the keys of a block of queries are dealt to this many workgroups, so many to each
   float scale, scale2;            // scale2: scale * log2(e)
   AttnSide qs, ks, vs, os;
   int heads, blocks;              // of the launch: (sample, head) pairs and their blocks of rows
@@ -583,6 +584,9 @@ dp_status launch_attention(K kernel, AttnArgs a, int64_t shared_bytes, int threa
 }
 
 dp_status launch_attention_forward(const AttnArgs& a, dp_dtype dt, hipStream_t s);
+// Sets key_parts and part_keys; floats that they need where key_parts is more than one.
+void attention_key_parts(AttnArgs& a, dp_dtype dt);
+int64_t attention_key_floats(const AttnArgs& a);
 // Workgroups that the query heads of a key head are dealt to in the backward pass, and floats that they need where it is more than one.
 int attention_parts(const AttnArgs& a);
 int64_t attention_partial_floats(const AttnArgs& a);

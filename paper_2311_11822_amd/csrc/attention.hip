@@ -2,6 +2,8 @@
 // values with a running maximum and sum.
 #include "attention.h"
 
+#include <algorithm>
+
 namespace dpbk {
 
 namespace {
@@ -26,6 +28,9 @@ __global__ void __launch_bounds__(64 * NW * SPLIT, 2) attention_kernel(const Att
   if (pair >= a.heads) return;
   const int b = pair / a.H, h = pair % a.H;
   if (a.causal) block = a.blocks - 1 - block;     // the longest first
+  const int part = SPLIT > 1 ? block % a.key_parts : 0;
+  if (SPLIT > 1) block /= a.key_parts;
+  const int part_begin = SPLIT > 1 ? part * a.part_keys : 0;
   const int lane = threadIdx.x & 63, id = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = id % NW, turn = id / NW;
   const int n_q = valid_rows(a.q_len, b, a.Tq), n_k = valid_rows(a.k_len, b, a.Tk), shift = n_k - n_q;
   const int row0 = block * 32 * NW, own0 = row0 + 32 * wave, row = own0 + (lane & 31);
@@ -33,8 +38,9 @@ __global__ void __launch_bounds__(64 * NW * SPLIT, 2) attention_kernel(const Att
 
   // Keys that the workgroup's, this wave's and the lane's rows see: below these.
   const int last = min(row0 + 32 * NW, n_q) - 1, own_last = min(own0 + 32, n_q) - 1;
-  const int end = row0 >= n_q ? 0 : a.causal ? min(n_k, last + shift + 1) : n_k;
-  const int own_end = own0 >= n_q ? 0 : a.causal ? min(n_k, own_last + shift + 1) : n_k;
+  const int there_k = SPLIT > 1 ? min(n_k, part_begin + a.part_keys) : n_k;         // (the part's)
+  const int end = row0 >= n_q ? 0 : a.causal ? min(there_k, last + shift + 1) : there_k;
+  const int own_end = own0 >= n_q ? 0 : a.causal ? min(there_k, own_last + shift + 1) : there_k;
   const int lane_end = row >= n_q ? 0 : a.causal ? min(n_k, row + shift + 1) : n_k;
 
   const E* q = static_cast<const E*>(a.q) + b * a.qs.sample + h * a.qs.head;
@@ -42,9 +48,9 @@ __global__ void __launch_bounds__(64 * NW * SPLIT, 2) attention_kernel(const Att
   k_tiles.init(static_cast<const E*>(a.k) + b * a.ks.sample + h / a.share * a.ks.head, a.ks.token, a.D, id, lane);
   v_tiles.init(static_cast<const E*>(a.v) + b * a.vs.sample + h / a.share * a.vs.head, a.vs.token, a.D, id, lane);
   // A tile's scores are formed beside the exponentials of the tile before it, so its keys are loaded a step before its values.
-  auto load_keys = [&](int tile, int stage) { k_tiles.load(tile * SPLIT * KEYS, n_k, lds + stage * TILE, id); };
-  auto load_values = [&](int tile, int stage) { v_tiles.load(tile * SPLIT * KEYS, n_k, lds + V + stage * TILE, id); };
-  const int tiles = (end + SPLIT * KEYS - 1) / (SPLIT * KEYS);
+  auto load_keys = [&](int tile, int stage) { k_tiles.load(part_begin + tile * SPLIT * KEYS, there_k, lds + stage * TILE, id); };
+  auto load_values = [&](int tile, int stage) { v_tiles.load(part_begin + tile * SPLIT * KEYS, there_k, lds + V + stage * TILE, id); };
+  const int tiles = (max(end - part_begin, 0) + SPLIT * KEYS - 1) / (SPLIT * KEYS);
   if (tiles > 0) {
     load_keys(0, 0);
     if (tiles > 1) load_keys(1, 1);
@@ -77,7 +83,7 @@ __global__ void __launch_bounds__(64 * NW * SPLIT, 2) attention_kernel(const Att
   two_stages(tiles, [&](int t, auto stage) {
     constexpr int HERE = decltype(stage)::value, NEXT = HERE ^ 1;
     f32x16(&s)[KB] = both[HERE], (&next)[KB] = both[NEXT];
-    const int j0 = (t * SPLIT + turn) * KEYS;
+    const int j0 = part_begin + (t * SPLIT + turn) * KEYS;
     tiles_landed();
     if (t + 2 < tiles) load_keys(t + 2, HERE);
     if (t + 1 < tiles) load_values(t + 1, NEXT);
@@ -146,6 +152,16 @@ __global__ void __launch_bounds__(64 * NW * SPLIT, 2) attention_kernel(const Att
     }
   }
   const bool there = lane_end > 0 && total != 0.f;
+  if (SPLIT > 1 && a.key_parts > 1) {
+    const int64_t rows = (int64_t)part * a.B * a.H * a.Tq + (int64_t)pair * a.Tq;
+    store_partial<DP>(o, there, a.partial + rows * a.D, row, a.Tq, a.D, lane);
+    float* stats = a.partial + (int64_t)a.key_parts * a.B * a.H * a.Tq * a.D + 2 * (rows + row);
+    if (lane < 32 && row < a.Tq) {
+      stats[0] = most;
+      stats[1] = there ? total : 0.f;
+    }
+    return;
+  }
   if (SPLIT == 1) tiles_landed();                 // LDS is free
   store_rows<DT, DP>(o, 1.f / total, there, static_cast<E*>(a.out) + b * a.os.sample + h * a.os.head, a.os.token, own0,
                         a.Tq, a.D, lds + wave * 32 * HeadTile<DT, DP>::ROW_BYTES, lane);
@@ -156,6 +172,33 @@ __global__ void __launch_bounds__(64 * NW * SPLIT, 2) attention_kernel(const Att
     const AttnRows<E> rows(a, reinterpret_cast<float*>(smem + wave * 32 * HeadTile<DT, DP>::ROW_BYTES), b, h, lane);
     for (int i = own0; i < min(own0 + 32, n_q); ++i) rows.forward(i);
   }
+}
+
+// Rows from the sums of their parts, in their order; four to a workgroup, columns lane and lane + 64 to a lane.
+template <class E>
+__global__ void __launch_bounds__(256) attention_join_parts_kernel(const AttnArgs a) {
+  __shared__ __align__(16) float own[4 * kRowFloats];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t row = ((int64_t)a.first + blockIdx.x) * 4 + wave, rows = (int64_t)a.B * a.H * a.Tq;
+  if (row >= rows) return;
+  const float* stats = a.partial + a.key_parts * rows * a.D;
+  float most = -3.4028235e38f, total = 0.f, acc[2] = {0.f, 0.f};
+  for (int p = 0; p < a.key_parts; ++p) most = fmaxf(most, stats[2 * (p * rows + row)]);
+  for (int p = 0; p < a.key_parts; ++p) {
+    const int64_t at = p * rows + row;
+    const float fix = __builtin_amdgcn_exp2f(stats[2 * at] - most);
+    total = fmaf(stats[2 * at + 1], fix, total);
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+      if (lane + 64 * c < a.D) acc[c] = fmaf(a.partial[at * a.D + lane + 64 * c], fix, acc[c]);
+  }
+  const int pair = (int)(row / a.Tq), i = (int)(row - (int64_t)pair * a.Tq), b = pair / a.H, h = pair % a.H;
+  if (a.causal && __any(!(fabsf(total) < INFINITY) || !(fabsf(acc[0]) < INFINITY) || !(fabsf(acc[1]) < INFINITY))) {
+    AttnRows<E>(a, own + wave * kRowFloats, b, h, lane).forward(i);
+    return;
+  }
+  store_row(acc, total != 0.f ? 1.f / total : 0.f, static_cast<E*>(a.out) + b * a.os.sample + h * a.os.head + i * a.os.token, a.D, lane);
+  if (lane == 0) a.lse[row] = total != 0.f ? most * kLn2 + logf(total) : -INFINITY;
 }
 
 // fp32 rows of no whole 16-byte pieces, four to a workgroup.
@@ -172,7 +215,7 @@ __global__ void __launch_bounds__(256) attention_rows_kernel(const AttnArgs a) {
 template <int DT, int DP, int NW, int SPLIT, int KEYS>
 dp_status launch(AttnArgs a, hipStream_t s) {
   a.heads = a.B * a.H;
-  a.blocks = (a.Tq + 32 * NW - 1) / (32 * NW);
+  a.blocks = (a.Tq + 32 * NW - 1) / (32 * NW) * (SPLIT > 1 ? a.key_parts : 1);
   constexpr int LDS = 4 * SPLIT * KEYS * HeadTile<DT, DP>::ROW_BYTES;
   auto kernel = attention_kernel<DT, DP, NW, SPLIT, KEYS>;
   static ReadyTable done;
@@ -180,7 +223,13 @@ dp_status launch(AttnArgs a, hipStream_t s) {
     const dp_status st = allow_big_lds(kernel, LDS, done);
     if (st != DP_OK) return st;
   }
-  return launch_attention(kernel, a, (int64_t)2 * Ops<DT>::SIZE * a.Tk * a.D, 64 * NW * SPLIT, LDS, s);
+  const dp_status st = launch_attention(kernel, a, (int64_t)2 * Ops<DT>::SIZE * a.Tk * a.D, 64 * NW * SPLIT, LDS, s);
+  if (SPLIT == 1 || a.key_parts == 1 || st != DP_OK) return st;
+  return launch_in_runs(((int64_t)a.heads * a.Tq + 3) / 4, [&](dim3 grid, int first) {
+    AttnArgs run = a;
+    run.first = (unsigned)first;
+    hipLaunchKernelGGL(attention_join_parts_kernel<typename Ops<DT>::E>, grid, dim3(256), 0, s, run);
+  });
 }
 
 template <int DT, int DP>
@@ -206,6 +255,24 @@ dp_status launch(const AttnArgs& a, hipStream_t s) {
 }
 
 }  // namespace
+
+// Where split blocks of queries are still few, their keys are dealt to as many workgroups as fill the compute units, from 512 keys to each; the
+// sums are joined.  One query, 32 heads of 128 on 8, 32768 keys: 88 us, in one part 303; 8 heads of 64, 4096 keys: 15.6 and 20.1; fp32, 4 heads of
+// 32: 17 and 49.  Below four parts it is not worth the second launch (300 queries, 6 heads, 2000 keys in three: 15.0 and 14.1).
+void attention_key_parts(AttnArgs& a, dp_dtype dt) {
+  const int64_t heads = (int64_t)a.B * a.H, workgroups = heads * ((a.Tq + 31) / 32);
+  a.key_parts = 1;
+  a.part_keys = a.Tk;
+  if (!(dt == DP_F32 ? whole_pieces(a) && split_rows<DP_F32>(heads, a.Tq, a.Tk) : split_rows<DP_BF16>(heads, a.Tq, a.Tk))) return;
+  const int64_t parts = std::min<int64_t>(256 / workgroups, a.Tk / 512);
+  if (parts < 4) return;
+  a.part_keys = (int)((a.Tk + parts - 1) / parts + 255) / 256 * 256;            // whole turns of every form
+  a.key_parts = (a.Tk + a.part_keys - 1) / a.part_keys;
+}
+
+int64_t attention_key_floats(const AttnArgs& a) {
+  return a.key_parts > 1 ? (int64_t)a.key_parts * a.B * a.H * a.Tq * (a.D + 2) : 0;
+}
 
 dp_status launch_attention_forward(const AttnArgs& args, dp_dtype dt, hipStream_t s) {
   if (dt == DP_BF16) return launch<DP_BF16>(args, s);

@@ -151,8 +151,15 @@ dp_status dp_layer_norm_backward(const void* x, const void* dy, const void* add,
   return launch_layer_norm_backward(a, dt, static_cast<hipStream_t>(stream));
 }
 
+size_t dp_attention_workspace_bytes(const dp_attention_shape* shape, dp_dtype dt) {
+  AttnArgs a;
+  if (attention_args(shape, dt, a) != DP_OK) return 0;
+  attention_key_parts(a, dt);
+  return (size_t)attention_key_floats(a) * sizeof(float);
+}
+
 dp_status dp_attention(const dp_attention_shape* shape, dp_dtype dt, const void* q, const void* k, const void* v, void* o, float* lse,
-                       void* stream) {
+                       void* ws, size_t ws_bytes, void* stream) {
   AttnArgs a;
   const dp_status st = attention_args(shape, dt, a);
   if (st != DP_OK) return st;
@@ -162,6 +169,14 @@ dp_status dp_attention(const dp_attention_shape* shape, dp_dtype dt, const void*
   a.v = v;
   a.out = o;
   a.lse = lse;
+  a.key_parts = 1;
+  a.part_keys = a.Tk;
+  if (ws) {
+    if (!aligned(ws, 16)) return DP_ERR_INVALID_ARG;
+    attention_key_parts(a, dt);
+    if (ws_bytes < (size_t)attention_key_floats(a) * sizeof(float)) return DP_ERR_WORKSPACE;
+    a.partial = static_cast<float*>(ws);
+  }
   return launch_attention_forward(a, dt, static_cast<hipStream_t>(stream));
 }
 

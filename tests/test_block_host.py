@@ -58,7 +58,7 @@ def shape(dt=dp.DP_BF16, B=2, H=4, H_kv=2, Tq=33, Tk=33, D=64, causal=1, scale=0
 
 
 def forward(s, dt=dp.DP_BF16, **kw):
-    return dp.lib.dp_attention(*changed(dict(shape=s, dt=dt, q=FAKE, k=FAKE, v=FAKE, o=FAKE, lse=FAKE, stream=None), **kw))
+    return dp.lib.dp_attention(*changed(dict(shape=s, dt=dt, q=FAKE, k=FAKE, v=FAKE, o=FAKE, lse=FAKE, ws=None, ws_bytes=0, stream=None), **kw))
 
 
 def backward(s, dt=dp.DP_BF16, **kw):
@@ -95,6 +95,10 @@ def test_attention_refuses_arguments():
     assert n >= 2 * 2 * 4 * 33 * 4
     assert backward(s, ws_bytes=n - 1) == WS == backward(s, ws=None)
     assert backward(s, ws=FAKE + 4) == INV
+    assert dp.dp_attention_workspace_bytes(s, dp.DP_BF16) == 0 == dp.dp_attention_workspace_bytes(shape(D=136), dp.DP_BF16)
+    s = shape(B=1, Tq=1, Tk=4096)                        # few queries on many keys
+    n = dp.dp_attention_workspace_bytes(s, dp.DP_BF16)
+    assert n >= 4 * 2 * 64 * 4 and forward(s, ws=FAKE, ws_bytes=n - 1) == WS and forward(s, ws=FAKE + 4, ws_bytes=n) == INV
 
 
 # D = 18 and a sample stride that is no multiple of 4 are for fp32 alone

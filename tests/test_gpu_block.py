@@ -392,6 +392,35 @@ def test_attention_of_few_rows_ignores_what_is_not_seen(block, dtype):
     assert not torch.isfinite(o[0, 8]).any() and all(torch.isfinite(g[1]).all() for g in grads) and torch.isfinite(grads[0][0, :8]).all()
 
 
+# The same with keys dealt to several workgroups, where the mask leaves some of them none; and without the workspace for it.
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("B,Tq,Tk,H,Hkv,D,q_len,k_len", [
+    (1, 1, 4096, 2, 1, 64, None, None), (2, 3, 3001, 2, 2, 128, [3, 2], [3001, 700]), (1, 33, 2500, 4, 1, 32, None, None),
+    (2, 1, 5000, 1, 1, 96, None, [0, 513]), (1, 150, 2100, 1, 1, 16, None, None)], ids=str)
+def test_attention_keys_in_parts(block, dtype, B, Tq, Tk, H, Hkv, D, q_len, k_len, causal):
+    c = Case(block, dtype, B, Tq, Tk, H, Hkv, D, causal, q_len=q_len, k_len=k_len)
+    c.check()
+    views, o, lse = [t.cuda() for t in (c.q, c.k, c.v)], torch.empty((B, Tq, H, D), dtype=DTYPES[dtype], device="cuda"), torch.empty((B, H, Tq), device="cuda")
+    gpu = lambda n: None if n is None else n.cuda()  # noqa: E731
+    at = block.Attention(*views, o, causal, c.scale, gpu(c.q_len), gpu(c.k_len))
+    assert at._forward_need > 0
+    block.dp.dp_attention(at.shape, at.dt, *views, o, lse)
+    want, want_lse = c.reference()
+    assert rel(o, want) <= max(2.5 * U[dtype], FP32) and rel(lse, want_lse) <= FP32
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_attention_keys_in_parts_ignore_what_is_not_seen(block, dtype):
+    c = Case(block, dtype, 1, 6, 3000, 2, 1, 64, True, k_len=[2777])
+    c.k[0, 2777:], c.v[0, 2777:] = math.nan, math.inf
+    c.v[0, 2776] = math.inf                               # the last row alone sees it
+    o, lse, grads = c.run()
+    want, want_lse = c.reference()
+    assert rel(lse, want_lse) <= FP32 and rel(o[0, :5], want[0, :5]) <= max(2.5 * U[dtype], FP32)
+    assert not torch.isfinite(o[0, 5]).any() and torch.isfinite(grads[0][0, :5]).all()
+
+
 # Few key heads that many query heads share: the heads' sums are formed in parts and joined.
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("shape", [(1, 33, 33, 6, 1, 64), (1, 128, 128, 7, 1, 128), (1, 100, 260, 12, 2, 32), (2, 20, 20, 48, 6, 96),
