@@ -491,6 +491,14 @@ dp_status dp_attention_backward(const dp_attention_shape* shape, dp_dtype dt, co
                                 size_t ws_bytes, void* stream);
 
 /*
+ * Host query (no GPU): the rows of keys and values that a tile of the forward pass and of the query gradients' kernel holds, and those of queries and
+ * their output gradients in the key gradients' kernel; 1 where rows are taken one by one.  Arrays are taken to be 16-byte aligned.  Where few
+ * rows face many, tiles are larger, as far as rows that lie the token stride apart allow: rows * stride * size <= 2^31 bytes always.
+ *   rows      HOST, [3]
+ */
+dp_status dp_attention_tile_rows(const dp_attention_shape* shape, dp_dtype dt, int32_t* rows);
+
+/*
  * One AdamW step over many tensors (for a rank that holds one shard of the flattened gradient: one tensor), in place:
  *   g = grad_scale * grad;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2;
  *   param = param (1 - lr * weight_decay) - lr * m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps).

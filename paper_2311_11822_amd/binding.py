@@ -93,6 +93,7 @@ _PROTOS = {
     "dp_attention": (_i, [C.POINTER(dp_attention_shape), _i, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "dp_attention_backward_workspace_bytes": (_sz, [C.POINTER(dp_attention_shape), _i]),
     "dp_attention_backward": (_i, [C.POINTER(dp_attention_shape), _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "dp_attention_tile_rows": (_i, [C.POINTER(dp_attention_shape), _i, _vp]),
     "dp_adamw_multi": (_i, [C.POINTER(dp_adamw_tensor), _i, _i, _i, _i, C.c_double, C.c_double, C.c_double, C.c_double, C.c_double,
                            _u64, _vp]),
     "dp_ghost_tile_order": (C.c_int64, [_i, _i, _vp, _vp, _vp, _vp, C.c_int64]),
@@ -368,6 +369,13 @@ def dp_attention_backward_workspace_bytes(shape, dt) -> int:
 
 def dp_attention_backward(shape, dt, q, k, v, o, lse, dout, dq, dk, dv, ws, stream=None) -> None:
     _call("dp_attention_backward", shape, dt, q, k, v, o, lse, dout, dq, dk, dv, ws, _nbytes(ws), stream)
+
+
+def dp_attention_tile_rows(shape, dt) -> "tuple[int, int, int]":
+    """(keys to a tile forward, in the query gradients; queries to a tile in the key gradients) (host function)."""
+    rows = (C.c_int32 * 3)()
+    _check(lib.dp_attention_tile_rows(shape, dt, rows), "dp_attention_tile_rows")
+    return tuple(rows)
 
 
 def adamw_tensors(tensors: Sequence) -> "C.Array[dp_adamw_tensor]":

@@ -350,10 +350,34 @@ constexpr int split_waves(int row_bytes) { return row_bytes <= 128 ? 8 : row_byt
 // 20 + 27; 1 head, 4096 tokens 49 + 145, 21 + 50; 8 heads, 2048 tokens 28 + 79, 21 + 54; but 24 heads, 512 tokens 11 + 29, 15 + 41.  fp32, whose tiles take
 // eight times as long: 2 x 512 tokens, 8 heads of 128 73 + 239, 58 + 142; 4 x 128, 6 heads of 64 15 + 43, 11 + 25; but 8 x 128, 12 heads 16
 // + 49, 20 + 50.
-template <int DT>
-bool split_rows(int64_t heads, int rows, int others) {
+// Such a turn's tile is 32 rows for each wave: not where that many, as far apart as a side (x, y) has them, lie beyond the byte offsets of one
+// descriptor.
+template <int DT, int DP>
+bool split_rows(int64_t heads, int rows, int others, const AttnSide& x, const AttnSide& y) {
+  constexpr int64_t TILE_ROWS = 32 * split_waves(HeadTile<DT, DP>::ROW_BYTES);
+  if (TILE_ROWS * Ops<DT>::SIZE * (x.token > y.token ? x.token : y.token) > (int64_t)OOB) return false;
   const int64_t workgroups = heads * ((rows + 127) / 128);
   return DT == DP_F32 ? workgroups <= 64 && others > 64 : workgroups <= 128 && others >= 1024;
+}
+// Queries, which go through keys and values, and keys, which go through queries and their gradients.
+template <int DT, int DP>
+bool split_queries(const AttnArgs& a) {
+  return split_rows<DT, DP>((int64_t)a.B * a.H, a.Tq, a.Tk, a.ks, a.vs);
+}
+template <int DT, int DP>
+bool split_keys(const AttnArgs& a) {
+  return split_rows<DT, DP>((int64_t)a.B * a.H_kv * a.parts, a.Tk, a.Tq, a.qs, a.os);
+}
+
+// Calls f with the width that rows of D values are padded to.
+template <int DT, class F>
+auto by_head_width(int D, F f) {
+  using std::integral_constant;
+  if (D <= 32) return f(integral_constant<int, 32>{});
+  if (D <= 64) return f(integral_constant<int, 64>{});
+  if constexpr (DT != DP_F32)
+    if (D <= 96) return f(integral_constant<int, 96>{});
+  return f(integral_constant<int, 128>{});
 }
 
 // Calls f with a tile's number and the stage that it lies in, as a constant, for n tiles.
@@ -584,6 +608,9 @@ dp_status launch_attention(K kernel, AttnArgs a, int64_t shared_bytes, int threa
 }
 
 dp_status launch_attention_forward(const AttnArgs& a, dp_dtype dt, hipStream_t s);
+// Rows of the other side that a tile holds in the forward pass, and (a.parts set) in the two backward kernels; 1 where rows are taken one by one.
+int attention_forward_tile(const AttnArgs& a, dp_dtype dt);
+void attention_backward_tiles(const AttnArgs& a, dp_dtype dt, int& queries, int& keys);
 // Sets key_parts and part_keys; floats that they need where key_parts is more than one.
 void attention_key_parts(AttnArgs& a, dp_dtype dt);
 int64_t attention_key_floats(const AttnArgs& a);

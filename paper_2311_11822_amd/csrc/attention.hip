@@ -232,26 +232,45 @@ dp_status launch(AttnArgs a, hipStream_t s) {
   });
 }
 
-template <int DT, int DP>
-dp_status launch(const AttnArgs& a, hipStream_t s) {
-  constexpr int LONG = DT == DP_F32 ? 32 : 64, SPLIT = split_waves(HeadTile<DT, DP>::ROW_BYTES);
-  if (split_rows<DT>((int64_t)a.B * a.H, a.Tq, a.Tk)) return launch<DT, DP, 1, SPLIT, 32>(a, s);
+// Calls f with waves, waves on the same rows and keys to a tile.
+template <int DT, int DP, class F>
+auto by_form(const AttnArgs& a, F f) {
+  using std::integral_constant;
+  constexpr int LONG = DT == DP_F32 ? 32 : 64;
+  const integral_constant<int, 1> one{};
+  const integral_constant<int, 2> two{};
+  const integral_constant<int, 4> four{};
+  const integral_constant<int, 32> tile{};
+  if (split_queries<DT, DP>(a)) return f(one, integral_constant<int, split_waves(HeadTile<DT, DP>::ROW_BYTES)>{}, tile);
   // One wave for few queries (512 x 32 tokens, 12 heads of 64: 20 us, with four 40), two up to 64 (256 x 48: 17 and 24).  Tiles of 64 keys hide
   // more of a turn's latency (1 x 3000 tokens, 9 heads: 39 us, of 32 keys 48), but leave more of a short row's last tile empty (64 x 128: 13.7 and
   // 12.4; 32 x 197 14.7 and 13.8; 18 x 591 34 and 36).
-  if (a.Tq <= 32) return launch<DT, DP, 1, 1, 32>(a, s);
-  if (a.Tq <= 64) return launch<DT, DP, 2, 1, 32>(a, s);
-  if (a.Tk <= 256) return launch<DT, DP, 4, 1, 32>(a, s);
-  return launch<DT, DP, 4, 1, LONG>(a, s);
+  if (a.Tq <= 32) return f(one, one, tile);
+  if (a.Tq <= 64) return f(two, one, tile);
+  if (a.Tk <= 256) return f(four, one, tile);
+  return f(four, one, integral_constant<int, LONG>{});
 }
 
 template <int DT>
 dp_status launch(const AttnArgs& a, hipStream_t s) {
-  if (a.D <= 32) return launch<DT, 32>(a, s);
-  if (a.D <= 64) return launch<DT, 64>(a, s);
-  if constexpr (DT != DP_F32)
-    if (a.D <= 96) return launch<DT, 96>(a, s);
-  return launch<DT, 128>(a, s);
+  return by_head_width<DT>(a.D, [&](auto width) {
+    constexpr int DP = decltype(width)::value;
+    return by_form<DT, DP>(a, [&](auto waves, auto split, auto keys) {
+      return launch<DT, DP, decltype(waves)::value, decltype(split)::value, decltype(keys)::value>(a, s);
+    });
+  });
+}
+
+template <int DT>
+int tile_rows(const AttnArgs& a) {
+  return by_head_width<DT>(a.D, [&](auto width) {
+    return by_form<DT, decltype(width)::value>(a, [](auto, auto split, auto keys) { return split * keys; });
+  });
+}
+
+template <int DT>
+bool queries_are_split(const AttnArgs& a) {
+  return by_head_width<DT>(a.D, [&](auto width) { return split_queries<DT, decltype(width)::value>(a); });
 }
 
 }  // namespace
@@ -263,7 +282,7 @@ void attention_key_parts(AttnArgs& a, dp_dtype dt) {
   const int64_t heads = (int64_t)a.B * a.H, workgroups = heads * ((a.Tq + 31) / 32);
   a.key_parts = 1;
   a.part_keys = a.Tk;
-  if (!(dt == DP_F32 ? whole_pieces(a) && split_rows<DP_F32>(heads, a.Tq, a.Tk) : split_rows<DP_BF16>(heads, a.Tq, a.Tk))) return;
+  if (!(dt == DP_F32 ? whole_pieces(a) && queries_are_split<DP_F32>(a) : queries_are_split<DP_BF16>(a))) return;
   const int64_t parts = std::min<int64_t>(256 / workgroups, a.Tk / 512);
   if (parts < 4) return;
   a.part_keys = (int)((a.Tk + parts - 1) / parts + 255) / 256 * 256;            // whole turns of every form
@@ -272,6 +291,10 @@ void attention_key_parts(AttnArgs& a, dp_dtype dt) {
 
 int64_t attention_key_floats(const AttnArgs& a) {
   return a.key_parts > 1 ? (int64_t)a.key_parts * a.B * a.H * a.Tq * (a.D + 2) : 0;
+}
+
+int attention_forward_tile(const AttnArgs& a, dp_dtype dt) {
+  return dt != DP_F32 ? tile_rows<DP_BF16>(a) : whole_pieces(a) ? tile_rows<DP_F32>(a) : 1;
 }
 
 dp_status launch_attention_forward(const AttnArgs& args, dp_dtype dt, hipStream_t s) {

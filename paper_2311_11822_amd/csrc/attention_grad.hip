@@ -433,21 +433,26 @@ template <int DT, int DP>
 dp_status launch(const AttnArgs& a, hipStream_t s) {
   constexpr int SPLIT = split_waves(HeadTile<DT, DP>::ROW_BYTES);
   // (One wave for few rows: 512 x 32 tokens, 12 heads of 64: 64 us, with four 95.)
-  const dp_status st = split_rows<DT>((int64_t)a.B * a.H, a.Tq, a.Tk) ? launch_queries<DT, DP, 1, SPLIT>(a, s)
-                       : a.Tq <= 32                               ? launch_queries<DT, DP, 1, 1>(a, s)
-                                                                  : launch_queries<DT, DP, 4, 1>(a, s);
+  const dp_status st = split_queries<DT, DP>(a) ? launch_queries<DT, DP, 1, SPLIT>(a, s)
+                       : a.Tq <= 32             ? launch_queries<DT, DP, 1, 1>(a, s)
+                                                : launch_queries<DT, DP, 4, 1>(a, s);
   if (st != DP_OK) return st;
-  if (split_rows<DT>((int64_t)a.B * a.H_kv * a.parts, a.Tk, a.Tq)) return launch_keys<DT, DP, 1, SPLIT>(a, s);
+  if (split_keys<DT, DP>(a)) return launch_keys<DT, DP, 1, SPLIT>(a, s);
   return a.Tk <= 32 ? launch_keys<DT, DP, 1, 1>(a, s) : launch_keys<DT, DP, 4, 1>(a, s);
 }
 
 template <int DT>
 dp_status launch(const AttnArgs& a, hipStream_t s) {
-  if (a.D <= 32) return launch<DT, 32>(a, s);
-  if (a.D <= 64) return launch<DT, 64>(a, s);
-  if constexpr (DT != DP_F32)
-    if (a.D <= 96) return launch<DT, 96>(a, s);
-  return launch<DT, 128>(a, s);
+  return by_head_width<DT>(a.D, [&](auto width) { return launch<DT, decltype(width)::value>(a, s); });
+}
+
+template <int DT>
+void tile_rows(const AttnArgs& a, int& queries, int& keys) {
+  by_head_width<DT>(a.D, [&](auto width) {
+    constexpr int DP = decltype(width)::value, SPLIT = split_waves(HeadTile<DT, DP>::ROW_BYTES);
+    queries = kRows * (split_queries<DT, DP>(a) ? SPLIT : 1);
+    keys = kRows * (split_keys<DT, DP>(a) ? SPLIT : 1);
+  });
 }
 
 }  // namespace
@@ -466,6 +471,14 @@ int attention_parts(const AttnArgs& a) {
 int64_t attention_partial_floats(const AttnArgs& a) {
   const int parts = attention_parts(a);
   return parts > 1 ? (int64_t)2 * parts * a.B * a.H_kv * a.Tk * a.D : 0;
+}
+
+void attention_backward_tiles(const AttnArgs& a, dp_dtype dt, int& queries, int& keys) {
+  queries = keys = 1;
+  if (dt != DP_F32)
+    tile_rows<DP_BF16>(a, queries, keys);
+  else if (whole_pieces(a))
+    tile_rows<DP_F32>(a, queries, keys);
 }
 
 dp_status launch_attention_backward(const AttnArgs& args, dp_dtype dt, hipStream_t s) {

@@ -44,7 +44,8 @@ dp_status attention_args(const dp_attention_shape* p, dp_dtype dt, AttnArgs& a) 
   if (dt != DP_F32 && s.D % 8) return DP_ERR_INVALID_ARG;
   if (s.D > 128 || s.Tq > 1 << 30 || s.Tk > 1 << 30) return DP_ERR_UNSUPPORTED;
   for (int n = 0; n < 4; ++n)
-    if (tokens[n] > 1 && strides[n][1] > 1 << 23) return DP_ERR_UNSUPPORTED;      // a tile's rows lie within 32-bit offsets
+    // 128 rows of 16 bits, 64 of fp32, lie within 2^31 bytes: what a tile is at most, but for the split forms, whose rule looks at strides itself
+    if (tokens[n] > 1 && strides[n][1] > 1 << 23) return DP_ERR_UNSUPPORTED;
   const int64_t rows = s.Tq > s.Tk ? s.Tq : s.Tk;
   if ((int64_t)s.B * s.H > (1 << 30) || ((int64_t)s.B * s.H + 7) * ((rows + 3) / 4) > INT32_MAX) return DP_ERR_UNSUPPORTED;
   a = AttnArgs{};
@@ -178,6 +179,20 @@ dp_status dp_attention(const dp_attention_shape* shape, dp_dtype dt, const void*
     a.partial = static_cast<float*>(ws);
   }
   return launch_attention_forward(a, dt, static_cast<hipStream_t>(stream));
+}
+
+dp_status dp_attention_tile_rows(const dp_attention_shape* shape, dp_dtype dt, int32_t* rows) {
+  AttnArgs a;
+  if (!rows) return DP_ERR_INVALID_ARG;
+  const dp_status st = attention_args(shape, dt, a);
+  if (st != DP_OK) return st;
+  a.parts = parts_of(a, dt);
+  int queries, keys;
+  attention_backward_tiles(a, dt, queries, keys);
+  rows[0] = attention_forward_tile(a, dt);
+  rows[1] = queries;
+  rows[2] = keys;
+  return DP_OK;
 }
 
 size_t dp_attention_backward_workspace_bytes(const dp_attention_shape* shape, dp_dtype dt) {

@@ -101,6 +101,31 @@ def test_attention_refuses_arguments():
     assert n >= 4 * 2 * 64 * 4 and forward(s, ws=FAKE, ws_bytes=n - 1) == WS and forward(s, ws=FAKE + 4, ws_bytes=n) == INV
 
 
+# A tile's rows, a token stride apart, lie within the byte offsets of one descriptor (2^31), in all three kernels and up to the largest stride.
+@pytest.mark.parametrize("dt,size", [(dp.DP_BF16, 2), (dp.DP_F16, 2), (dp.DP_F32, 4)])
+@pytest.mark.parametrize("D", [8, 24, 32, 64, 72, 96, 104, 128])
+def test_attention_tiles_lie_within_offsets(dt, size, D):
+    strides = [1 << 12, 1 << 20, 1 << 21, (1 << 21) + 8, 1 << 22, (1 << 22) + 8, 1 << 23]
+    for Tq, Tk in ((1, 130), (1, 1100), (130, 1), (1100, 1), (1100, 1100), (33, 40000), (1 << 20, 3)):
+        for wide in strides:
+            # each side's stride, one at a time: keys and values bound two kernels' tiles, queries and results the third's
+            for name in "qkvo":
+                s = shape(H=1, H_kv=1, B=1, D=D, Tq=Tq, Tk=Tk, causal=0, **{name: (1 << 50, wide, D)})
+                rows = dp.dp_attention_tile_rows(s, dt)
+                assert all(r * size * (wide if name in side else D) <= 1 << 31 for r, side in zip(rows, ("kv", "kv", "qo")))
+                if dp.dp_attention_workspace_bytes(s, dt):              # keys in parts: whole tiles of the split form
+                    assert rows[0] > 64 or D > 64 and dt == dp.DP_F32
+    # the larger tiles of few rows are there where strides allow them
+    few = dp.dp_attention_tile_rows(shape(H=1, H_kv=1, B=1, D=D, Tq=1, Tk=1100), dt)
+    assert few[0] == few[1] == 32 * (8 if size * max(D, 32) <= 128 else 4 if size * D <= 256 else 2)
+
+
+def test_attention_tile_rows_refuses():
+    assert dp.lib.dp_attention_tile_rows(shape(), dp.DP_BF16, None) == INV == dp.lib.dp_attention_tile_rows(None, dp.DP_BF16, (ctypes.c_int32 * 3)())
+    assert dp.lib.dp_attention_tile_rows(shape(D=136), dp.DP_BF16, (ctypes.c_int32 * 3)()) == UNS
+    assert dp.dp_attention_tile_rows(shape(D=18), dp.DP_F32) == (1, 1, 1)
+
+
 # D = 18 and a sample stride that is no multiple of 4 are for fp32 alone
 def test_attention_widths_by_type():
     s = shape(D=18)

@@ -493,6 +493,29 @@ def test_attention_offsets_past_32_bits(block):
     assert torch.equal(o, want[0]) and torch.equal(lse, want[1])
 
 
+class WideCase(Case):
+    """The same on the GPU with tokens of q, k and v `stride` elements apart, in one buffer of NaN: only what the shape reaches may be read."""
+
+    def projections(self, make):
+        if not hasattr(self, "stride"):
+            return super().projections(make)
+        T, width = max(self.Tq, self.Tk), (self.H + 2 * self.Hkv) * self.D
+        wide = torch.full((self.B * T * self.stride + 2 * width,), math.nan, dtype=DTYPES[self.dtype], device="cuda")
+        view = lambda rows, heads, at: wide.as_strided((self.B, rows, heads, self.D), (T * self.stride, self.stride, self.D, 1), at * self.D)  # noqa: E731
+        return view(self.Tq, self.H, 0), view(self.Tk, self.Hkv, self.H), view(self.Tk, self.Hkv, self.H + self.Hkv)
+
+
+# Few rows against many that lie so far apart that one descriptor does not span the split forms' tiles; the strides beside that too.
+@pytest.mark.parametrize("dtype,stride,Tq,Tk,D", [
+    ("f32", 1 << 23, 1, 130, 24), ("f32", 1 << 23, 1, 130, 64), ("f32", 1 << 22, 3, 150, 32), ("f32", (1 << 21) + 4, 2, 300, 24), ("f32", 1 << 21, 2, 300, 24),
+    ("f32", 1 << 23, 2, 100, 128), ("f32", 1 << 23, 130, 1, 24), ("f32", 1 << 22, 150, 3, 64), ("bf16", (1 << 22) + 8, 1, 1100, 24), ("f16", 1 << 23, 1, 1030, 64),
+    ("bf16", (1 << 22) + 8, 1100, 2, 40), ("bf16", 1 << 23, 1, 1025, 104)])
+def test_attention_of_few_rows_far_apart(block, dtype, stride, Tq, Tk, D):
+    c = WideCase(block, dtype, 1, Tq, Tk, 2, 1, D, False)
+    c.stride = stride
+    c.check()
+
+
 # ------------------------------------------------------------------------------------------------ AdamW
 
 def fp8_reference(x, step, power):
