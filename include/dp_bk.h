@@ -480,7 +480,8 @@ dp_status dp_attention(const dp_attention_shape* shape, dp_dtype dt, const void*
  * Backward pass, which forms the probabilities again from lse:
  *   dv_j = sum_i p_ij do_i,  ds_ij = p_ij (do_i . v_j - do_i . o_i),  dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,
  * dk and dv summed over the query heads that share a key head.  Every element of dq, dk and dv that the shape reaches is written (zeros
- * where a row is not there); p and ds are rounded to the type before their products (16-bit types).
+ * where a row is not there); p and ds are rounded to the type before their products (16-bit types; in fp16 ds times a power of two that keeps it
+ * from over- and underflowing, taken out in fp32).
  *   o, lse    dp_attention's;  dout  the gradient of o, in o's strides
  *   dq, dk, dv   in the strides of q, k and v; they do not overlap each other nor an input
  *   ws        device scratch, >= dp_attention_backward_workspace_bytes(...), 16-byte aligned

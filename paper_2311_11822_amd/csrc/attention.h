@@ -10,7 +10,8 @@
 //    rows 4 h .. 4 h + 3 and 8 + 4 h .. 8 + 4 h + 3 of every 16.  A sum does not care for its order, so the first operand is
 //    read in the same one (two transposing LDS reads, of rows 4 h and 8 + 4 h on), and no probability passes through LDS.
 // Rounding a probability or a score's gradient to the type costs half a unit of it, independently of the others: as much as the result's own
-// rounding; sums, maxima, lse and delta are fp32.
+// rounding; sums, maxima, lse and delta are fp32.  fp16 has that unit from 2^-14 to 65504 only, which scores' gradients leave at both ends: they
+// are held times a power of two (Raised).
 //
 // LDS holds rows of a head (DP columns) as they come from memory, 16-byte chunks XOR-swizzled by row such that eight
 // rows' reads of one column and the transposing reads of four rows fall on different banks.
@@ -379,6 +380,46 @@ auto by_head_width(int D, F f) {
     if (D <= 96) return f(integral_constant<int, 96>{});
   return f(integral_constant<int, 128>{});
 }
+
+// The scores' gradients of a lane's own row in fp16, times 2^raise, which keeps them below 2 and the largest so far from about 2^-6 on (so that 2^-8 of it
+// has all bits and what a smaller one loses is 2^-19 of the largest at most).  It begins beyond need and is lowered where one outgrows it (the
+// sums so far with it, exactly); it is taken out of the sums in fp32.  (A gradient of 10^-3, the mean loss of 2048 tokens, would put scores'
+// gradients at 10^-7 else: the 2-norm of dq's error 9.4e-4 instead of 3.5e-4.)
+struct Raised {
+  int raise = 48;                                 // (a value is at most 2^41 as it is)
+  __device__ __forceinline__ float factor() const { return ldexpf(1.f, raise); }
+  // Rounded values of 2 and more, infinities and what is no number among them: their exponents' highest bit.
+  __device__ __forceinline__ static bool outgrown(const bf16x8 (&x)[2]) {
+    typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+    const u32x4 bits = __builtin_bit_cast(u32x4, x[0]) | __builtin_bit_cast(u32x4, x[1]);
+    return __any(((bits[0] | bits[1] | bits[2] | bits[3]) & 0x40004000u) != 0);
+  }
+  template <int N>
+  __device__ __forceinline__ void lower(f32x16& x, f32x16 (&sum)[N], int lane) {
+    float top = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) top = fmaxf(top, fabsf(x[r]));
+    top = fmaxf(top, other_half(top, lane));
+    if (top < 1.9f || !(top < INFINITY)) top = 0.015625f;            // (as it is)
+    const int by = -5 - __builtin_amdgcn_frexp_expf(top);
+    const float f = ldexpf(1.f, by);
+    raise += by;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[r] *= f;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sum[n][r] *= f;
+  }
+  template <int N>
+  __device__ __forceinline__ void take_out(f32x16 (&sum)[N]) const {
+    const float f = ldexpf(1.f, -raise);
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sum[n][r] *= f;
+  }
+};
 
 // Calls f with a tile's number and the stage that it lies in, as a constant, for n tiles.
 template <class F>

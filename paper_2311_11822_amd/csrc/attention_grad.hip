@@ -97,7 +97,9 @@ attention_query_grad_kernel(const AttnArgs a) {
                 dp = O::rows(f, df[ks], ks == 0 ? begin : dp);
             });
   };
-  auto probability = [&](float s) { return __builtin_amdgcn_exp2f(fmaf(s, a.scale2, -own_lse2)); };
+  constexpr bool F16 = DT == DP_F16;
+  Raised raised;
+  auto probability = [&](float s, float raise) { return __builtin_amdgcn_exp2f(fmaf(s, a.scale2, raise - own_lse2)); };      // times 2^raise
   auto hide = [&](f32x16& x, int tile) {          // a select: what is not seen may be no number
     const int seen = lane_end - tile * kRows - 4 * (lane >> 5);
 #pragma unroll
@@ -123,7 +125,7 @@ attention_query_grad_kernel(const AttnArgs a) {
         f32x16 s, dp;
         products(s, dp, SPLIT > 1 ? (t - turn) * SUB : t * STAGE, zeros16());
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = probability(s[r]) * dp[r];
+        for (int r = 0; r < 16; ++r) s[r] = probability(s[r], 0.f) * dp[r];
         hide(s, t);
 #pragma unroll
         for (int r = 0; r < 16; ++r) sum += s[r];
@@ -146,11 +148,17 @@ attention_query_grad_kernel(const AttnArgs a) {
     Stretch<typename O::Column, 2 * CB, grad_ahead(DT, DP)> run;
     run.begin(operand);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = probability(s[r]) * dp[r];
+    for (int r = 0; r < 16; ++r) s[r] = probability(s[r], F16 ? (float)raised.raise : 0.f) * dp[r];
     if ((tile + 1) * kRows > all_see) hide(s, tile);
-    const typename O::Column ds[2] = {O::weights(s, 0), O::weights(s, 8)};
+    typename O::Column ds[2] = {O::weights(s, 0), O::weights(s, 8)};
+    if constexpr (F16)
+      if (raised.outgrown(ds)) {
+        raised.lower(s, dq, lane);
+        ds[0] = O::weights(s, 0), ds[1] = O::weights(s, 8);
+      }
     run.run(operand, [&](int m, typename O::Column f) { dq[m % CB] = O::columns(f, ds[m / CB], dq[m % CB]); });
   });
+  if constexpr (F16) raised.take_out(dq);
   tiles_landed();                                 // LDS is free
   if constexpr (SPLIT > 1) {
     constexpr int EACH = handed_floats(16 * CB);
@@ -274,6 +282,8 @@ attention_key_grad_kernel(const AttnArgs a) {
   f32x16 dk[CB], dv[CB];
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb) dk[cb] = dv[cb] = zeros16();
+  constexpr bool F16 = DT == DP_F16;
+  Raised raised;
   const int steps = tiles * heads;
   if (steps > 0) load(0);
   int first = begin;                              // of the tile at hand
@@ -311,7 +321,18 @@ attention_key_grad_kernel(const AttnArgs a) {
         ds[r] = i < hidden_ds ? 0.f : ds[r];
       }
     }
-    const typename O::Column pr[2] = {O::weights(p, 0), O::weights(p, 8)}, dr[2] = {O::weights(ds, 0), O::weights(ds, 8)};
+    if constexpr (F16) {
+      const float f = raised.factor();
+#pragma unroll
+      for (int r = 0; r < 16; ++r) ds[r] *= f;
+    }
+    const typename O::Column pr[2] = {O::weights(p, 0), O::weights(p, 8)};
+    typename O::Column dr[2] = {O::weights(ds, 0), O::weights(ds, 8)};
+    if constexpr (F16)
+      if (raised.outgrown(dr)) {
+        raised.lower(ds, dk, lane);
+        dr[0] = O::weights(ds, 0), dr[1] = O::weights(ds, 8);
+      }
     run.run(operand,
             [&](int m, typename O::Column f) {
               const int cb = m / 2 % CB, ks = m / 2 / CB;
@@ -321,6 +342,7 @@ attention_key_grad_kernel(const AttnArgs a) {
                 dv[cb] = O::columns(f, pr[ks], dv[cb]);
             });
   });
+  if constexpr (F16) raised.take_out(dk);
   tiles_landed();                                 // LDS is free
   if constexpr (SPLIT > 1) {
     constexpr int EACH = handed_floats(32 * CB);

@@ -493,6 +493,58 @@ def test_attention_offsets_past_32_bits(block):
     assert torch.equal(o, want[0]) and torch.equal(lse, want[1])
 
 
+def check_fp16_gradients(block, Tq, Tk, H, Hkv, D, causal, change, seed=0):
+    """fp16 gradients against the definition in 64 bits.  The bound, in the 2-norm, is what rounding costs where the type has all its bits, half as
+    much again: the result's own rounding (as it is), and that of the scores' gradients or probabilities before their products, 2^-11 / sqrt(3)
+    of each at most in the mean, independent of each other.  1e-5 of the same parts is for fp32 sums, lse and exponentials."""
+    c = Case(block, "f16", 1, Tq, Tk, H, Hkv, D, causal, seed=seed)
+    change(c)
+    _, _, grads = c.run()
+    G = H // Hkv
+    q, do = c.q.double().transpose(1, 2), c.do.double().transpose(1, 2)
+    k, v = (t.double().transpose(1, 2).repeat_interleave(G, 1) for t in (c.k, c.v))
+    p = torch.softmax((q @ k.mT * c.scale).masked_fill(~c.seen(), -math.inf), -1).nan_to_num(0)
+    dp = do @ v.mT
+    ds = c.scale * p * (dp - (p * dp).sum(-1, keepdim=True))
+    shared = lambda t: t.reshape(1, Hkv, G, Tk, -1).sum(2).transpose(1, 2)  # noqa: E731
+    want = (ds @ k).transpose(1, 2), shared(ds.mT @ q), shared(p.mT @ do)
+    square = lambda w, t: (w.square() @ t.square().sum(-1, keepdim=True)).sum().item()  # noqa: E731
+    parts = math.sqrt(square(ds, k)), math.sqrt(square(ds.mT, q)), math.sqrt(square(p.mT, do))
+    for name, got, ref, part in zip(("dq", "dk", "dv"), grads, want, parts):
+        assert torch.isfinite(got).all()
+        own = (ref.half().double() - ref).norm().item()
+        off = (got.cpu().double() - ref).norm().item()
+        assert off <= 1.5 * math.hypot(own, part * 2 ** -11 / math.sqrt(3)) + 1e-5 * part, (name, off / ref.norm().item(), own / ref.norm().item())
+
+
+def times(name, factor):
+    """Multiplies a tensor of a Case by a number, or its tokens by powers of two that grow or shrink evenly between two exponents."""
+    def change(c):
+        t = getattr(c, name)
+        f = torch.tensor(float(factor)) if not isinstance(factor, tuple) else 2.0 ** torch.linspace(*factor, t.shape[1])[None, :, None, None]
+        t.copy_((t.double() * f).half())
+    return change
+
+
+def zeros(name, tokens):
+    return lambda c: getattr(c, name)[:, :tokens].zero_()
+
+
+# Small output gradients (Case's are of size 0.1), of long rows; gradients and values that grow or shrink from token to token; leading zeros; score
+# gradients beyond fp16's largest number; all with the forms of few rows, of shared heads and of each width.
+@pytest.mark.parametrize("shape,causal,changes", [
+    ((2048, 2048, 1, 1, 64), True, [times("do", 0.1)]), ((2048, 2048, 1, 1, 64), True, [times("do", 1e-2)]), ((2048, 2048, 1, 1, 64), True, [times("do", 1e-3)]),
+    ((2048, 2048, 1, 1, 64), True, [times("do", 3e-5)]), ((2048, 2048, 1, 1, 64), False, [times("do", 1e-2)]), ((1100, 1500, 2, 2, 128), True, [times("do", 1e-2)]),
+    ((900, 900, 2, 1, 96), False, [times("do", 1e-2)]), ((600, 600, 2, 2, 24), True, [times("do", 2e-3)]), ((3, 3000, 2, 2, 64), False, [times("do", 1e-2)]),
+    ((2500, 5, 2, 2, 128), False, [times("do", 1e-2)]), ((400, 400, 8, 1, 64), True, [times("do", 1e-2)]),
+    ((700, 700, 2, 2, 64), False, [times("do", (-12, 6)), times("v", (-8, 5))]), ((700, 700, 2, 2, 64), False, [times("do", (6, -12)), times("v", (5, -8))]),
+    ((500, 500, 2, 2, 128), True, [times("do", (-14, 4))]), ((1024, 1024, 1, 1, 64), True, [zeros("do", 300), times("do", 1e-2)]),
+    ((300, 300, 1, 1, 64), False, [zeros("v", 200), times("do", 1e-2)]), ((8, 8, 2, 2, 64), False, [times("do", 3e4), times("v", 30), times("k", 0.01), times("q", 0.01)]),
+    ((8, 200, 2, 2, 128), False, [times("do", 1e5), times("v", 30), times("k", 0.01), times("q", 0.01)])])
+def test_attention_fp16_gradients_of_any_size(block, shape, causal, changes):
+    check_fp16_gradients(block, *shape, causal, lambda c: [change(c) for change in changes])
+
+
 class WideCase(Case):
     """The same on the GPU with tokens of q, k and v `stride` elements apart, in one buffer of NaN: only what the shape reaches may be read."""
 
