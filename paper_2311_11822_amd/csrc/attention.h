@@ -11,7 +11,8 @@
 //    read in the same one (two transposing LDS reads, of rows 4 h and 8 + 4 h on), and no probability passes through LDS.
 // Rounding a probability or a score's gradient to the type costs half a unit of it, independently of the others: as much as the result's own
 // rounding; sums, maxima, lse and delta are fp32.  fp16 has that unit from 2^-14 to 65504 only, which scores' gradients leave at both ends: they
-// are held times a power of two (Raised).
+// are held times a power of two (Raised).  So are the key gradients' probabilities (kGain), which are 1 / n in a row of n equal scores; the forward
+// pass has them in units of the largest.
 //
 // LDS holds rows of a head (DP columns) as they come from memory, 16-byte chunks XOR-swizzled by row such that eight
 // rows' reads of one column and the transposing reads of four rows fall on different banks.
@@ -32,7 +33,7 @@ struct AttnArgs {
   const void *q, *k, *v, *o, *dout;
   void *out, *dq, *dk, *dv;
   float* lse;                     // [B, H, Tq]
-  float *lse2, *delta;            // backward, [B, H, Tq]: lse in units of log 2 (+inf: the row counts for nothing), and -delta
+  float *lse2, *delta;            // backward, [B, H, Tq]: lse in units of log 2, less kGain (+inf: the row counts for nothing), and -delta
   const int32_t *q_len, *k_len;   // [B] or null
   int B, H, H_kv, share;          // share: query heads to a key head
   int Tq, Tk, D;
@@ -55,6 +56,11 @@ __host__ __device__ inline bool aligned_arrays(const AttnArgs& a) {
 }
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+// What the key gradients' kernel has of probabilities: them times 2^kGain, at most 2^15 in fp16.  (4 queries on 60000 keys: the 2-norm of dv's error
+// 6.7e-4 without, 2.9e-4 with it.)
+template <class E>
+constexpr float kGain = std::is_same_v<E, _Float16> ? 15.f : 0.f;
 
 // Operands and products by storage type DT.  A row operand is 16 bytes of a row, EL columns to each lane half: one matrix instruction of
 // 16-bit values, four of fp32.  A column operand is 16 rows of a column, 8 to each half, against eight weights a lane: one instruction, or
@@ -387,7 +393,7 @@ auto by_head_width(int D, F f) {
 // gradients at 10^-7 else: the 2-norm of dq's error 9.4e-4 instead of 3.5e-4.)
 struct Raised {
   int raise = 48;                                 // (a value is at most 2^41 as it is)
-  __device__ __forceinline__ float factor() const { return ldexpf(1.f, raise); }
+  __device__ __forceinline__ float factor(int less) const { return ldexpf(1.f, raise - less); }
   // Rounded values of 2 and more, infinities and what is no number among them: their exponents' highest bit.
   __device__ __forceinline__ static bool outgrown(const bf16x8 (&x)[2]) {
     typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
@@ -412,8 +418,10 @@ struct Raised {
       for (int r = 0; r < 16; ++r) sum[n][r] *= f;
   }
   template <int N>
-  __device__ __forceinline__ void take_out(f32x16 (&sum)[N]) const {
-    const float f = ldexpf(1.f, -raise);
+  __device__ __forceinline__ void take_out(f32x16 (&sum)[N]) const { lower_by(sum, raise); }
+  template <int N>
+  __device__ __forceinline__ static void lower_by(f32x16 (&sum)[N], int by) {
+    const float f = ldexpf(1.f, -by);
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
@@ -588,7 +596,7 @@ struct AttnRows {
     }
     store_row(acc, a.scale, (E*)a.dq + b * a.qs.sample + h * a.qs.head + i * a.qs.token, a.D, lane);
     if (lane == 0) {
-      a.lse2[at] = lse2;
+      a.lse2[at] = lse2 - kGain<E>;
       a.delta[at] = -delta[0];
     }
   }
@@ -606,7 +614,7 @@ struct AttnRows {
       for (int i0 = from; i0 < n_q; i0 += 64) {
         const int i = min(i0 + lane, n_q - 1);
         float p, ds;
-        pair(q + i * a.qs.token, dout + i * a.os.token, a.lse2[at + i], -a.delta[at + i], p, ds);
+        pair(q + i * a.qs.token, dout + i * a.os.token, a.lse2[at + i] + kGain<E>, -a.delta[at + i], p, ds);
         // no gradient of the scores of a row that sees one key (a 16-bit row's delta is not formed as do v' is)
         if (keys_of(i) == 1) ds = 0.f;
         add_rows(dv, p, dout + i0 * a.os.token, a.os.token, min(64, n_q - i0), a.D, lane);

@@ -170,7 +170,7 @@ attention_query_grad_kernel(const AttnArgs a) {
     for (int w = 1; w < SPLIT; ++w) take_over(dq, mine + w * NW * EACH, lane);
   }
   if (lane < 32 && row < a.Tq) {
-    a.lse2[at] = lse2;
+    a.lse2[at] = lse2 - kGain<E>;
     a.delta[at] = -delta;
   }
   store_rows<DT, DP>(dq, a.scale, lane_end > 0, static_cast<E*>(a.dq) + b * a.qs.sample + h * a.qs.head, a.qs.token, own0,
@@ -322,7 +322,7 @@ attention_key_grad_kernel(const AttnArgs a) {
       }
     }
     if constexpr (F16) {
-      const float f = raised.factor();
+      const float f = raised.factor((int)kGain<E>);
 #pragma unroll
       for (int r = 0; r < 16; ++r) ds[r] *= f;
     }
@@ -342,7 +342,10 @@ attention_key_grad_kernel(const AttnArgs a) {
                 dv[cb] = O::columns(f, pr[ks], dv[cb]);
             });
   });
-  if constexpr (F16) raised.take_out(dk);
+  if constexpr (F16) {
+    raised.take_out(dk);
+    Raised::lower_by(dv, (int)kGain<E>);
+  }
   tiles_landed();                                 // LDS is free
   if constexpr (SPLIT > 1) {
     constexpr int EACH = handed_floats(32 * CB);

@@ -545,6 +545,12 @@ def test_attention_fp16_gradients_of_any_size(block, shape, causal, changes):
     check_fp16_gradients(block, *shape, causal, lambda c: [change(c) for change in changes])
 
 
+@pytest.mark.parametrize("Tq,Tk,D,causal", [(4, 60000, 64, False), (3, 60000, 128, True), (64, 60000, 64, False)])
+def test_attention_fp16_gradients_of_small_probabilities(block, Tq, Tk, D, causal):
+    """Rows so long that their probabilities are below fp16's smallest number with all its bits."""
+    check_fp16_gradients(block, Tq, Tk, 2, 1, D, causal, times("do", 1e3))
+
+
 class WideCase(Case):
     """The same on the GPU with tokens of q, k and v `stride` elements apart, in one buffer of NaN: only what the shape reaches may be read."""
 
