@@ -38,7 +38,8 @@ class _Workspaces:
                 nbytes = max(nbytes, ws.numel() * 3 // 2)
             # of that stream's own memory: what comes from another's may still be in use there
             current = torch.cuda.current_stream(device)
-            own = current if current.cuda_stream == stream else torch.cuda.ExternalStream(stream, device)
+            own = (current if current.cuda_stream == stream else torch.cuda.ExternalStream(stream, device) if stream
+                   else torch.cuda.default_stream(device))          # (an external stream of handle 0 would be a new one)
             with torch.cuda.stream(own):
                 ws = self.held[index, stream] = torch.empty(nbytes, dtype=torch.uint8, device=device)
         return ws

@@ -801,6 +801,20 @@ def test_workspaces_grow_and_follow_streams(block):
         assert all(torch.equal(a, b) for other in out[1:] for a, b in zip(other, out[0]))
 
 
+def segment_of(t):
+    """The allocator's segment that a tensor lies in."""
+    return next(s for s in torch.cuda.memory_snapshot() if s["address"] <= t.data_ptr() < s["address"] + s["total_size"])
+
+
+def test_workspaces_are_memory_of_the_stream_that_uses_them(block):
+    """The default stream by its handle, 0, and another one, while a third is current."""
+    device, side, other = torch.device("cuda", torch.cuda.current_device()), torch.cuda.Stream(), torch.cuda.Stream()
+    ws = block._Workspaces()
+    with torch.cuda.stream(side):
+        for stream in (0, other.cuda_stream, side.cuda_stream):
+            assert segment_of(ws(3 << 20, device, device.index, stream))["stream"] == stream
+
+
 def test_a_captured_workspace_stays(block):
     """A graph that holds a workspace's address is replayed after the object has needed a larger one."""
     gen = torch.Generator().manual_seed(9)
