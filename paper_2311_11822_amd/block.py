@@ -25,24 +25,40 @@ def _same(name: str, x: Optional[torch.Tensor], shape, dtype, device) -> None:
 
 class _Workspaces:
     """Scratch memory, one for each device and stream (calls on different streams do not share one) that grows as calls need.  What it has
-    outgrown stays as long as the object (a captured graph may have its address); by halves at least, so all of it is bounded."""
+    outgrown stays as long as the object (a captured graph may have its address); by halves at least, so all of it is bounded.
+
+    A graph that torch captures has its own, from the graph's pool: it may be replayed on any stream, beside other graphs of the same object
+    and calls that are not captured.  (A capture by other means has the stream's; its replays keep that stream's order.)"""
 
     def __init__(self):
         self.held, self.outgrown = {}, []
 
     def __call__(self, nbytes: int, device: torch.device, index: int, stream: int) -> torch.Tensor:
         ws = self.held.get((index, stream))
-        if ws is None or ws.numel() < nbytes:
-            if ws is not None:
-                self.outgrown.append(ws)
-                nbytes = max(nbytes, ws.numel() * 3 // 2)
+        capturing = torch.cuda.is_current_stream_capturing()
+        if ws is None or ws.numel() < nbytes or capturing:
             # of that stream's own memory: what comes from another's may still be in use there
             current = torch.cuda.current_stream(device)
             own = (current if current.cuda_stream == stream else torch.cuda.ExternalStream(stream, device) if stream
                    else torch.cuda.default_stream(device))          # (an external stream of handle 0 would be a new one)
             with torch.cuda.stream(own):
-                ws = self.held[index, stream] = torch.empty(nbytes, dtype=torch.uint8, device=device)
+                if capturing:
+                    fresh = torch.empty(nbytes, dtype=torch.uint8, device=device)
+                    if _of_a_graph(fresh):
+                        return fresh                      # the pool's as long as the graph
+                if ws is None or ws.numel() < nbytes:
+                    if ws is not None:
+                        self.outgrown.append(ws)
+                        nbytes = max(nbytes, ws.numel() * 3 // 2)
+                    ws = self.held[index, stream] = torch.empty(nbytes, dtype=torch.uint8, device=device)
         return ws
+
+
+def _of_a_graph(x: torch.Tensor) -> bool:
+    """Whether x lies in the memory pool of a graph that is captured (looked up in the allocator's whole list: for captures alone)."""
+    at = x.data_ptr()
+    return any(s["address"] <= at < s["address"] + s["total_size"] and tuple(s["segment_pool_id"]) != (0, 0)
+               for s in torch.cuda.memory_snapshot())
 
 
 class LayerNorm:

@@ -815,6 +815,52 @@ def test_workspaces_are_memory_of_the_stream_that_uses_them(block):
             assert segment_of(ws(3 << 20, device, device.index, stream))["stream"] == stream
 
 
+def test_graphs_do_not_share_workspaces(block):
+    """Two graphs of one object, captured on one stream, and calls on that stream that are not captured: each has scratch of its own, so
+    that all of them may run at once."""
+    gen = torch.Generator().manual_seed(10)
+    norm, used, capture = block.LayerNorm(None, None), [], torch.cuda.Stream()
+    inner = norm._ws
+    norm._ws = lambda *args: used.append(inner(*args)) or used[-1]
+
+    def case():
+        x, dy = (rand(gen, (4, 900, 768), "f32").cuda() for _ in range(2))
+        stats = torch.empty((4, 900), device="cuda"), torch.empty((4, 900), device="cuda")
+        norm.forward(x, torch.empty_like(x), *stats)
+        dx, kept, sq = torch.empty_like(x), torch.empty((4, 2, 768), device="cuda"), torch.empty(4, device="cuda")
+        return (lambda: norm.backward(x, dy, *stats, dx, kept, sq)), (dx, kept, sq)
+
+    cases, graphs, want = [case() for _ in range(3)], [], []
+    torch.cuda.synchronize()
+    with torch.cuda.stream(capture):
+        for call, outputs in cases:
+            call()
+            want.append([t.clone() for t in outputs])
+    torch.cuda.synchronize()
+    for call, _ in cases[:2]:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=capture):
+            call()
+    eager, first, second = used[0], used[-2], used[-1]
+    spans = sorted((t.data_ptr(), t.data_ptr() + t.numel()) for t in (eager, first, second))
+    assert all(a[1] <= b[0] for a, b in zip(spans, spans[1:]))
+    del used[:], eager, first, second
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        for _, outputs in cases:
+            for t in outputs:
+                t.fill_(7.0)
+        torch.cuda.synchronize()
+        for _ in range(4):
+            for graph, stream in zip(graphs, streams):
+                with torch.cuda.stream(stream):
+                    graph.replay()
+            with torch.cuda.stream(capture):
+                cases[2][0]()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for (_, outputs), w in zip(cases, want) for a, b in zip(outputs, w))
+
+
 def test_a_captured_workspace_stays(block):
     """A graph that holds a workspace's address is replayed after the object has needed a larger one."""
     gen = torch.Generator().manual_seed(9)
