@@ -154,7 +154,7 @@ class Attention:
                 if t.shape != shape or t.dtype is not dtype or t.get_device() != index:
                     raise ValueError(f"{tuple(shape)} of {dtype} on {self.device}, not {tuple(t.shape)} of {t.dtype} on {t.device}")
         for t, strides in zip(four, self.strides):
-            if t.stride() != strides:
+            if t.stride() != strides and any(n > 1 and st != want for n, st, want in zip(t.shape, t.stride(), strides)):
                 raise ValueError(f"strides {strides}, not {t.stride()}")
         if lse is not None and (lse.shape != self.rows or lse.dtype is not torch.float32 or lse.get_device() != index or
                                 not lse.is_contiguous()):

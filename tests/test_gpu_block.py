@@ -458,6 +458,29 @@ def test_attention_of_broadcast_inputs(block, dtype):
     assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
 
 
+@pytest.mark.parametrize("shape", [(1, 1, 2, 32), (1, 5, 1, 32), (2, 1, 1, 32)])
+def test_attention_of_axes_of_one_entry(block, shape):
+    """An axis of one entry has no stride: tensors that differ in it alone are taken, and give the same; where there are more entries, refused."""
+    gen = torch.Generator().manual_seed(6)
+    tensors = [rand(gen, shape, "bf16").cuda() for _ in range(5)]
+    out = []
+    at = block.Attention(*tensors[:4], False, 0.3)
+    for other in (False, True):
+        def view(t):
+            strides = [4096 if other and n == 1 else st for n, st in zip(shape, t.stride())]
+            return torch.empty(t.numel(), dtype=t.dtype, device="cuda").as_strided(shape, strides).copy_(t)
+        q, k, v, o, do = (view(t) for t in tensors)
+        assert other == (q.stride() != tensors[0].stride())
+        lse, grads = torch.empty((shape[0], shape[2], shape[1]), device="cuda"), [view(t) for t in tensors[:3]]
+        at.forward(q, k, v, o, lse)
+        at.backward(q, k, v, o, lse, do, *grads)
+        out.append([t.clone() for t in (o, lse, *grads)])
+    assert all(torch.equal(a, b) for a, b in zip(*out))
+    if shape[1] > 1:
+        with pytest.raises(ValueError):
+            at.forward(torch.zeros((1, 10, 1, 32), dtype=torch.bfloat16, device="cuda")[:, ::2], *tensors[1:4], lse)
+
+
 def test_attention_gradient_against_differences(block):
     """A directional derivative of the fp32 forward pass against the gradients."""
     gen = torch.Generator().manual_seed(11)
