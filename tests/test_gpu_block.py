@@ -10,6 +10,7 @@ of a number just above a power of two: 2^-8 for bf16 (8 bits of significand), 2^
 """
 import math
 
+import numpy as np
 import pytest
 import torch
 
@@ -86,6 +87,24 @@ def test_layer_norm(block, dtype, B, T, d):
     bare = torch.empty_like(dev[0])
     block.LayerNorm(None, None, 1e-5).forward(dev[0], bare)
     assert rel(bare, norm_reference(x, torch.ones(d), torch.zeros(d), 1e-5)[0]) <= U[dtype] + 4 * FP32 or d == 1
+
+
+# The mean of n values comes out of fp32 sums of up to 72 values a thread, 6 steps in a wave and 8 waves: within 100 * 2^-24 of its size.  y errs by
+# that times rstd, and by its own rounding; the variance, formed around that mean, by its square.
+@pytest.mark.parametrize("dtype,shift", [("f32", 1e3), ("f32", -3e4), ("f16", 300.0), ("bf16", 40.0)])
+@pytest.mark.parametrize("d", [64, 1000, 1021, 4096, 12289])
+def test_layer_norm_of_rows_far_from_zero(block, dtype, shift, d):
+    gen = torch.Generator().manual_seed(d)
+    x = (torch.randn((2, 5, d), generator=gen, dtype=torch.float64) + shift).to(DTYPES[dtype])
+    gain, bias = rand(gen, (d,), "f32"), rand(gen, (d,), "f32")
+    y, mean, rstd = torch.empty_like(x, device="cuda"), torch.empty((2, 5), device="cuda"), torch.empty((2, 5), device="cuda")
+    block.LayerNorm(gain.cuda(), bias.cuda(), 1e-5).forward(x.cuda(), y, mean, rstd)
+    want, m, r = norm_reference(x, gain, bias, 1e-5)
+    off = 100 * 2.0 ** -24 * abs(shift)
+    assert (mean.cpu().double() - m).abs().max() <= off
+    assert ((rstd.cpu().double() - r).abs() <= r * (FP32 + (off * r) ** 2)).all()
+    err = (y.cpu().double() - want).norm().item()
+    assert err <= U[dtype] * want.norm().item() + (off + 2.0 ** -24 * abs(shift)) * (r[..., None] * gain.double()).norm().item() + 4 * FP32 * want.norm().item()
 
 
 def norm_grad_reference(x, dy, gain, mean, rstd):
@@ -725,6 +744,95 @@ def test_adamw_8_bit_averages_move(block):
     assert abs(second - 1) < 0.03                 # the average's own noise is sqrt(2 / 2000 / 4096) = 0.05 %, the codes' a few parts in a thousand
 
 
+def adamw_8_bits_once(block, g, steps=2, **kw):
+    """Parameters, codes and scales of some steps from zero states."""
+    n = g.numel()
+    p, state = torch.ones(n, device="cuda"), [torch.zeros(n, device="cuda").to(torch.float8_e4m3fn) for _ in range(2)]
+    scales = [torch.zeros(-(-n // 256), device="cuda") for _ in range(2)]
+    opt = block.AdamW([p], [g], [state[0]], [state[1]], 0.0, None, [scales[0]], [scales[1]])
+    for step in range(1, steps + 1):
+        opt.step(step, **{**dict(lr=0.25, beta1=0.875, beta2=0.9375, eps=0.0), **kw})
+    return p, *[c.view(torch.uint8) for c in state], *scales
+
+
+# 8-bit states have quotients and roots of two forms: short ones where nothing underflows, the compiler's elsewhere.  Both round to nearest, so that a
+# change of all gradients by a power of two (betas whose products with it are exact, no eps) changes scales by it and nothing else.
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_adamw_8_bits_of_either_form(block, dtype):
+    gen = torch.Generator().manual_seed(21)
+    g = rand(gen, (256 * 300 + 77,), dtype).cuda()
+    g = torch.where(g.abs() < 2.0 ** -6, torch.full_like(g, 0.5), g)      # (nothing underflows: squares of 2^-58 / 16, rounded in 8 bits)
+    p, m, v, ms, vs = adamw_8_bits_once(block, g)
+    assert (ms.min() > 2.0 ** -50) and (ms.max() < 2.0 ** 50)
+    for by in (-30, -52, 20, 55):                         # -52: scales below 2^-60, averages of squares below 2^-96
+        p2, m2, v2, ms2, vs2 = adamw_8_bits_once(block, g * 2.0 ** by)
+        assert torch.equal(p2, p) and torch.equal(m2, m) and torch.equal(v2, v), by
+        assert torch.equal(ms2, ms * 2.0 ** by) and torch.equal(vs2, vs * 2.0 ** by), by
+    # scales beyond 2^60, where squares are infinite: the average alone
+    _, m2, _, ms2, _ = adamw_8_bits_once(block, g * 2.0 ** 76, steps=1)
+    _, m, _, ms, _ = adamw_8_bits_once(block, g, steps=1)
+    assert ms2.min() > 2.0 ** 60 and torch.equal(m2, m) and torch.equal(ms2, ms * 2.0 ** 76)
+
+
+def adamw_8_bits_definition(g, steps, lr, beta1, beta2, eps, grad_scale):
+    """The same in numpy's fp32, an operation at a time, from the header's text: parameters, code values and scales."""
+    f, n = np.float32, g.size
+    spread = lambda x: np.repeat(x, 256)[:n]  # noqa: E731
+    p, m8, v8 = np.ones(n, f), np.zeros(n, f), np.zeros(n, f)
+    ms, vs = np.zeros(-(-n // 256), f), np.zeros(-(-n // 256), f)
+    b1, b2, rest1, rest2 = f(beta1), f(beta2), f(1 - beta1), f(1 - beta2)
+
+    def coded(x, power, step):
+        e = np.arange(n, dtype=np.uint64)
+        dither = (((e * 0x6A09E667 + step * 0x9E3779B1) & 0xFFFFFFFF) >> 8).astype(f) * f(2.0 ** -24)
+        blocks = np.zeros(-(-n // 256) * 256, f)
+        blocks[:n] = np.abs(x)
+        scale = blocks.reshape(-1, 256).max(1) * f(1 / 448)
+        a = np.abs(x) / np.where(spread(scale) > 0, spread(scale), f(1))
+        unit = np.maximum(np.frexp(a)[1] - 1, -6) - 3
+        y = np.ldexp(a, -unit)
+        low = np.floor(y)
+        place = (y - low) * (y + low) / (f(2) * low + f(1)) if power == 2 else y - low
+        c = np.clip(np.ldexp(low + np.floor(place + dither), unit), f(2.0 ** -9), f(448))
+        return np.where(a > 0, np.copysign(c, x), f(0)).astype(f), scale
+
+    for step in range(1, steps + 1):
+        gs = g * f(grad_scale)
+        m, v = m8 * spread(ms), v8 * spread(vs)
+        m, v = b1 * m + rest1 * gs, b2 * (v * v) + rest2 * gs * gs
+        fix1, fix2 = f(1) / f(1 - beta1 ** step), f(1) / f(1 - beta2 ** step)
+        p = p - f(lr) * (m * fix1 / (np.sqrt(v * fix2) + f(eps)))
+        (m8, ms), (v8, vs) = coded(m, 1, step), coded(np.sqrt(v), 2, step)
+    return p, m8, v8, ms, vs
+
+
+@pytest.mark.parametrize("hyper", [dict(lr=0.25, beta1=0.875, beta2=0.9375, eps=0.0, grad_scale=1.0), dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=0.3)])
+def test_adamw_8_bits_to_the_bit(block, hyper):
+    """Every operation is rounded alone, to nearest: fp32 code elsewhere gives the same bits, rare sizes of gradients among them."""
+    gen = torch.Generator().manual_seed(23)
+    g = torch.randn(256 * 400 + 77, generator=gen) * 2.0 ** torch.randint(-12, 12, (256 * 400 + 77,), generator=gen)
+    got = adamw_8_bits_once(block, g.cuda(), steps=5, **hyper)
+    want = adamw_8_bits_definition(g.numpy(), 5, **hyper)
+    for name, x, y in zip(("param", "m", "v", "m_scale", "v_scale"), got, want):
+        x = x.view(torch.float8_e4m3fn).float() if x.dtype == torch.uint8 else x
+        assert np.array_equal(x.cpu().numpy(), y), (name, (x.cpu().numpy() != y).sum())
+
+
+def test_adamw_8_bits_beside_tiny_squares(block):
+    """One value whose square is below 2^-96 puts the roots of its 256 on the compiler's form: the others' bits stay."""
+    gen = torch.Generator().manual_seed(22)
+    g = rand(gen, (256 * 200,), "f32").cuda()
+    g[::256] = 0.0
+    tiny = g.clone()
+    tiny[::256] = 2.0 ** -60
+    want, got = adamw_8_bits_once(block, g, grad_scale=0.3), adamw_8_bits_once(block, tiny, grad_scale=0.3)
+    others = torch.arange(g.numel(), device="cuda") % 256 != 0
+    for a, b in zip(want[:3], got[:3]):
+        assert torch.equal(a[others], b[others])
+    assert torch.equal(want[3], got[3]) and torch.equal(want[4], got[4])
+    assert (want[2][::256] == 0).all() and (got[2][::256] == 1).all()     # the smallest code: not rounded to zero
+
+
 def test_adamw_many_tensors_and_undefined_values(block):
     """More tensors than a launch takes; NaN in a gradient stays in its own element (32 bits) or its 256 (8 bits)."""
     n = 300
@@ -756,6 +864,55 @@ def test_on_another_stream(block):
         got = c.run()
     stream.synchronize()
     assert torch.equal(got[0], want[0]) and all(torch.equal(x, y) for x, y in zip(got[2], want[2]))
+
+
+@pytest.mark.parametrize("by", ["current", "object", "handle"])
+def test_calls_wait_for_their_stream(block, by):
+    """Inputs that a stream fills behind a long piece of work: every call runs after them, on that stream, however it is named."""
+    gen = torch.Generator().manual_seed(13)
+    B, T, H, D = 2, 70, 4, 32
+    new = lambda *s, dt=torch.float32: torch.zeros(s, dtype=dt, device="cuda")  # noqa: E731
+    x, dy, y, dx = (new(B, T, H * D) for _ in range(4))
+    mean, rstd, kept, sq = new(B, T), new(B, T), new(B, 2, H * D), new(B)
+    q, k, v, o, do, dq, dk, dv = (new(B, T, H, D) for _ in range(8))
+    few, o1, lse, lse1 = new(B, 1, H, D), new(B, 1, H, D), new(B, H, T), new(B, H, 1)
+    far_k, far_v = new(B, 2100, H, D), new(B, 2100, H, D)
+    p, g, m, s = (new(5000) for _ in range(4))
+    inputs = [x, dy, q, k, v, do, few, far_k, far_v, p, g]
+    values = [torch.randn(t.shape, generator=gen).cuda() for t in inputs]
+    norm, at, at1 = block.LayerNorm(None, None), block.Attention(q, k, v, o, True, 0.2), block.Attention(few, far_k, far_v, o1, False, 0.2)
+    assert at1._forward_need > 0
+    opt = block.AdamW([p], [g], [m], [s], 0.0)
+
+    def run(stream):
+        norm.forward(x, y, mean, rstd, stream=stream)
+        norm.backward(x, dy, mean, rstd, dx, kept, sq, stream=stream)
+        at.forward(q, k, v, o, lse, stream)
+        at.backward(q, k, v, o, lse, do, dq, dk, dv, stream)
+        at1.forward(few, far_k, far_v, o1, lse1, stream)
+        opt.step(1, 0.1, stream=stream)
+
+    outputs = [y, mean, rstd, dx, kept, sq, o, lse, dq, dk, dv, o1, lse1, p, m, s]
+    for t, value in zip(inputs, values):
+        t.copy_(value)
+    run(None)
+    want = [t.clone() for t in outputs]
+    side, a = torch.cuda.Stream(), torch.randn(4096, 4096, device="cuda")
+    for t in (*inputs, *outputs):
+        t.zero_()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(20):                               # some tens of milliseconds
+            a = torch.mm(a, a).clamp_(-1, 1)
+        for t, value in zip(inputs, values):
+            t.copy_(value)
+        assert not side.query()                           # still at it
+        if by == "current":
+            run(None)
+    if by != "current":
+        run(side if by == "object" else side.cuda_stream)
+    side.synchronize()
+    assert all(torch.equal(t, w) for t, w in zip(outputs, want))
 
 
 def test_replayed_in_a_graph(block):
