@@ -1,9 +1,9 @@
 // One AdamW step over many tensors (decoupled weight decay):
 //   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,  g = grad_scale * grad,
-//   w = w (1 - lr decay) - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps).
+//   w = w (1 - lr decay) - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps).
 // A stream over memory: 28 bytes an element with 32-bit states and gradients, 16 with 8-bit states.  A stack of 85 million parameters, 32 bits
-// and a bf16 copy, in two launches: 500 us, 5.1 TB/s, what a copy reaches.  226 million with 8-bit states: 784 to 808 us, 4.6 TB/s, some
-// 130 vector instructions an element beside it.
+// and a bf16 copy, in two launches: 500 us, 5.1 TB/s, what a copy reaches.  226 million with 8-bit states: 784 to 840 us by card and run, 4.3 to 4.6 TB/s,
+// some 130 vector instructions an element beside it.
 //
 // 8-bit states are e4m3 numbers in units of their block's largest / 448, m itself and the root of v (whose range they cover where
 // they would not that of v).  Rounding to nearest would lose the small steps of a slow average, so values are rounded up where
@@ -125,7 +125,8 @@ __device__ __forceinline__ void decode(float (&x)[4], uint32_t w, float scale) {
 
 // A wave's 8-bit step is bound by its instructions, divisions and square roots for the most part, which as the compiler has them
 // serve all of fp32's range.  These round as they do, to nearest even, where nothing is lost below fp32's smallest numbers: the remainder
-// of a quotient (or of a root's square) is exact there.
+// of a quotient (or of a root's square) is exact there.  Quotients by their remainder over a corrected reciprocal is Markstein's method; a root
+// whose remainders against both neighbours decide is Tuckerman's test.
 __device__ __forceinline__ float reciprocal(float d) {
   const float r = __builtin_amdgcn_rcpf(d);
   return fmaf(fmaf(-d, r, 1.f), r, r);

@@ -13,8 +13,8 @@ constexpr float kLazy = 8.f;                      // a maximum may be passed by 
 // NW waves of 32 queries each (SPLIT waves the same ones, whose turns at the tiles are joined at the end), tiles of KEYS keys in two stages.
 // A pair's keys and values come out of L2 for all blocks but the first; what is left is work on scores: four matrix instructions a tile for
 // D = 64 and as many issue cycles of exponentials, maxima and roundings beside them, with a barrier a tile, three workgroups to a
-// unit.  2 x 4096 causal tokens, 12 heads of 64, bf16: 69 us, 750 TFLOP/s of the 1400 of a large product.  16 x 256: 10 us and 32 x 197
-// (fp16, all seen) 14 us for the 5 and 8 that q, k, v and o take from memory: a launch, and a workgroup's loads, few tiles and stores one after
+// unit.  2 x 4096 causal tokens, 12 heads of 64, bf16: 70 to 75 us by card and run, 690 to 740 TFLOP/s of the 1400 of a large product.  16 x 256: 10 us and 32 x 197
+// (fp16, all seen) 14 to 15 us for the 5 and 8 that q, k, v and o take from memory: a launch, and a workgroup's loads, few tiles and stores one after
 // the other.  Tried without gain: four stages, two and eight waves, operands asked for ahead in a fixed order.
 template <int DT, int DP, int NW, int SPLIT, int KEYS>
 __global__ void __launch_bounds__(64 * NW * SPLIT, 2) attention_kernel(const AttnArgs a) {

@@ -1,8 +1,10 @@
 // Attention, backward.  With p_ij = exp(scale q_i k_j - lse_i) formed again from the forward pass's lse:
 //   dv_j = sum_i p_ij do_i,   ds_ij = p_ij (do_i v_j - delta_i),   delta_i = do_i o_i,
 //   dq_i = scale sum_j ds_ij k_j,   dk_j = scale sum_i ds_ij q_i     (over the query heads that share the key head, too).
-// Two kernels, one that owns queries and one that owns keys, so that every sum has one owner and a fixed order: no atomics, no
-// partial sums in memory.  The price is that scores and do v' are formed in both, seven products for five.
+// Two kernels, one that owns queries and one that owns keys, so that every sum has one owner and a fixed order, without atomics.  The price is
+// that scores and do v' are formed in both, seven products for five.  Where key heads are too few to fill the device the query heads
+// that share one are dealt to several workgroups: their fp32 sums of dk and dv lie in the workspace and a third kernel joins them, in a fixed order
+// too.
 #include "attention.h"
 
 namespace dpbk {
@@ -11,8 +13,10 @@ namespace {
 
 // Both kernels go through tiles of 32 rows of the other side, in two stages, a barrier a tile.  Bound by the turn of a tile, not by the
 // matrix cores' rate: its products depend on each other through the exponentials, and registers allow two or three workgroups to a unit to fill the
-// gaps.  4 x 2048 causal tokens, 96 heads of 128, bf16: 1520 us (dq 44 % of it), 1.0e12 operations that count (1.4e12 done): 680 TFLOP/s, half
-// of a large product's rate.  8 x 512, 20 heads of 64: 21 and 24 us for the 17 that the tensors take from memory.
+// gaps.  4 x 2048 causal tokens, 96 heads of 128, bf16: 1520 to 1610 us by card and run (dq 44 % of it), 1.0e12 operations that count (1.4e12 done): 640 to
+// 680 TFLOP/s, half of a large product's rate.  8 x 512, 20 heads of 64: 21 and 24 us for the 17 that the tensors take from memory.  fp16's powers of two
+// (Raised) take 7 to 9 %: both passes of 4 x 1024 tokens, 12 heads of 64, 57 us, without them 52.
+// The key kernel at its full registers keeps 12 (width 64) and 16 bytes (128) of a lane in scratch, fp16 24 and 8.
 // Tried without gain: a ring of four stages; the next tile's scores beside the exponentials, as in the forward pass (there are registers for two
 // workgroups of width 64 instead of three: 2 x 4096 tokens, 12 heads, 7 % faster at the time, 8 x 512 17 % slower); two and eight waves; one
 // wave to a SIMD with 512 registers.

@@ -487,9 +487,15 @@ dp_status by_type(dp_dtype dt, int d, F f) {
 }
 
 // Threads to a workgroup of the backward pass: 512, of which a compute unit has two, or 1024, one, where a thread's part of a row is at most 32
-// bytes (twice the waves leave it 128 registers) and that brings something: wide rows leave half as many sums to be joined (4 x
+// bytes (64 of narrow fp32 rows; twice the waves leave it 128 registers) and that brings something: wide rows leave half as many sums to be joined (4 x
 // 2048 x 12288 bf16: 166 us, with 512 threads 184), waves that take rows alone have one each where two were (32 x 197 x 768: 12.8 and 16.1; a
 // sample of up to 8 rows has none for the other waves: 512 x 1 x 1024, 10.6 and 9.8).  Beyond, 2 x 1000 x 32768: 206 us with 1024, 183.
+// Both sides of the lines, us with 512 and 1024 threads.  Wide, 4 x 2048 (fp32: 4 x 1024) rows: bf16 of 4096 54 and 72, 8192 117 and 124, 8200 134 and 136,
+// 9216 144 and 139, 10240 153 and 148, 14336 221 and 189, 16384 254 and 207; fp32 of 4096 44 and 51, 4100 58 and 54, 5120 70 and 59, 8192 116 and 102; shifted
+// bf16 of 8195 196 and 221, 12289 253 and 251, 16377 306 and 283.  (2 x 300 and 16 x 128 rows: 1024 ahead from 8200 and 4100 on, by up to 15 %.)
+// Narrow: bf16 32 x 197 rows of 520 14.1 and 11.5, 1024 17.3 and 13.7, 16 x 256 and 1 x 4096 the same within 3 %; 512 x 4 rows of 768 8.1 and 10.2; fp32 32 x
+// 197 of 768 22.2 and 16.5, 1024 26.6 and 20.4, but 16 x 256 of 1024 14.9 and 16.5.  It loses where few rows are shifted in fp32 (16 x 256 of 513: 12.4 and
+// 19.1; 32 x 197: 21.1 and 21.2).
 int backward_threads(dp_dtype dt, int T, int d) {
   const int width = covered(dt, d), bytes = width * (dt == DP_F32 ? 4 : 2);
   if (width <= 1024) return T > 8 ? 1024 : 512;
