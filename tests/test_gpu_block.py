@@ -902,7 +902,7 @@ def test_calls_wait_for_their_stream(block, by):
         t.zero_()
     torch.cuda.synchronize()
     with torch.cuda.stream(side):
-        for _ in range(20):                               # some tens of milliseconds
+        for _ in range(60):                               # some tens of milliseconds
             a = torch.mm(a, a).clamp_(-1, 1)
         for t, value in zip(inputs, values):
             t.copy_(value)
