@@ -533,6 +533,112 @@ typedef struct {
 dp_status dp_adamw_multi(const dp_adamw_tensor* tensors, int n_tensors, dp_dtype grad_dt, int state_bits, dp_dtype copy_dt, double lr,
                          double beta1, double beta2, double eps, double grad_scale, uint64_t step, void* stream);
 
+/*
+ * What gated transformer blocks run besides: the position rotation of queries and keys, with or without a norm of each head before it,
+ * the gated feed-forward layer's products, and an optimizer that orthogonalises the update.  Sums and statistics are fp32 at least; what is
+ * stored in 16 bits is rounded once, to nearest even.
+ */
+
+/*
+ * Heads of queries and keys, between their projection and attention.
+ *   B, T      samples and tokens;  H, H_kv: heads of the queries and of the keys (H_kv = 0: queries alone, the keys' pointers and strides are
+ *             not looked at);  D: a head's width, at most 256 and, for 16-bit types, a multiple of 8
+ *   rotary    the first `rotary` columns of a head turn (even, from 0 to D); the others pass
+ *   interleaved   1: columns 2 i and 2 i + 1 are a pair; 0: columns i and i + rotary / 2
+ *   amplitude multiplies both of a pair (contexts longer than a model was made for: some ask for more than 1)
+ *   q_stride .. k_out_stride   element strides of sample, token and head, as of dp_attention_shape; columns are adjacent.  For 16-bit types
+ *             multiples of 8.  What is read may be broadcast (stride 0), what is written may not overlap itself.
+ *   turns     device fp64 [rotary / 2], 8-byte aligned: of pair i, whole turns from one position to the next (dp_rotary_turns makes them)
+ *   position  device int32 [B, T], or NULL: token t is at position t
+ *   len       device int32 [B], or NULL: all tokens are there.  Rows from len[b] on (held to 0 .. T) are neither read nor written.
+ * Angles are taken modulo whole turns in 64 bits: far positions lose nothing.  Results may lie where their own input does, in the same strides;
+ * otherwise what is written overlaps nothing else.
+ */
+typedef struct {
+  int32_t B, T, H, H_kv, D;
+  int32_t rotary, interleaved;
+  float amplitude;
+  int64_t q_stride[3], k_stride[3], q_out_stride[3], k_out_stride[3];   /* sample, token, head */
+  const double* turns;
+  const int32_t* position;
+  const int32_t* len;
+} dp_heads_shape;
+
+/*
+ * Turns for `rotary` columns (host function): pair i has base^(-2 i / rotary) / (2 pi), changed for longer contexts by
+ *   DP_ROTARY_LINEAR   all divided by `factor`
+ *   DP_ROTARY_BASE     base times factor^(rotary / (rotary - 2)) (one pair alone: as it is)
+ *   DP_ROTARY_PARTS    those that make `fast` turns or more within the `original` context stay, those of `slow` or fewer are divided by
+ *                      `factor`, in between both are mixed by the turns' place between slow and fast
+ *   turns     HOST fp64 [rotary / 2]
+ */
+typedef enum { DP_ROTARY_PLAIN = 0, DP_ROTARY_LINEAR = 1, DP_ROTARY_BASE = 2, DP_ROTARY_PARTS = 3 } dp_rotary_scaling;
+dp_status dp_rotary_turns(double* turns, int rotary, double base, dp_rotary_scaling scaling, double factor, double original, double slow,
+                          double fast);
+
+/*
+ * Rotation:  (x1, x2) -> amplitude (x1 cos - x2 sin, x2 cos + x1 sin)  of each pair, by position * turns[i] turns; and its gradient, the
+ * same with the angle's sign changed.
+ *   shape     HOST
+ *   q, k, q_out, k_out   device, of type dt, 16-byte aligned (DP_F32: 4-byte)
+ *   dq_out, dk_out   in the strides of q_out and k_out;  dq, dk  in those of q and k
+ */
+dp_status dp_rotary(const dp_heads_shape* shape, dp_dtype dt, const void* q, const void* k, void* q_out, void* k_out, void* stream);
+dp_status dp_rotary_backward(const dp_heads_shape* shape, dp_dtype dt, const void* dq_out, const void* dk_out, void* dq, void* dk,
+                             void* stream);
+
+/*
+ * Norm of each head, then the rotation:  y = R(h gain),  h = x r,  r = 1 / sqrt(mean_D(x^2) + eps).  rotary = 0: the norm alone.
+ *   q_gain, k_gain   device fp32 [D], shared by all heads of their side, or NULL: ones
+ */
+dp_status dp_head_norm(const dp_heads_shape* shape, dp_dtype dt, const void* q, const void* k, const float* q_gain, const float* k_gain,
+                       float eps, void* q_out, void* k_out, void* stream);
+
+/*
+ * Its backward pass, with g = R'(dy), u = g gain:  dx = r (u - h mean_D(u h)),
+ *   kept[i] = sum_{t, heads} g h: sample i's gradients of q_gain and, behind it, k_gain: [B, 2, D] fp32 (H_kv = 0: [B, 1, D]);
+ *   sqnorm_out[i] = ||kept[i]||^2, one more row of sqnorm.  dp_clipped_bias_grad(kept, B, 2 * D, C, grad, ...) then adds the clipped gradients up.
+ *   q, k      what dp_head_norm was given;  dq_out, dk_out  in the strides of q_out, k_out;  dq, dk  in those of q, k; each may be its dq_out
+ *             or its q where strides are the same
+ *   kept, sqnorm_out   both or neither NULL
+ *   ws        device scratch, >= dp_head_norm_workspace_bytes(...), 16-byte aligned; not used without kept
+ */
+size_t dp_head_norm_workspace_bytes(const dp_heads_shape* shape, dp_dtype dt);
+dp_status dp_head_norm_backward(const dp_heads_shape* shape, dp_dtype dt, const void* q, const void* k, const void* dq_out,
+                                const void* dk_out, const float* q_gain, const float* k_gain, float eps, void* dq, void* dk, float* kept,
+                                float* sqnorm_out, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Gated feed-forward layer, from its input to what its last projection reads, in one pass:
+ *   gate = x w_gate + b_gate,  up = x w_up + b_up,  h = act(gate) up.
+ * gate and up are formed in fp32 and rounded where they are stored; h comes from the unrounded ones.
+ *   x         device, [rows, d] of type dt (rows = B T)
+ *   w_gate, w_up   device, [d, f] of type dt;  b_gate, b_up  device, [f] of type dt, each or NULL
+ *   gate, up  device, [rows, f] of type dt, kept for the backward pass; both or neither NULL
+ *   h         device, [rows, f] of type dt
+ *   ws        device scratch, >= dp_gated_workspace_bytes(...), 16-byte aligned; the size is 0 where it is not used
+ * For 16-bit types d and f are multiples of 8 and arrays 16-byte aligned (DP_F32: 4-byte).  d and f are at most 2^20.  Results overlap nothing.
+ * act: silu x s(x), s the logistic function; gelu x Phi(x); gelu_tanh its form by tanh; relu; sigmoid s(x).
+ */
+typedef enum { DP_ACT_SILU = 0, DP_ACT_GELU = 1, DP_ACT_GELU_TANH = 2, DP_ACT_RELU = 3, DP_ACT_SIGMOID = 4 } dp_activation;
+size_t dp_gated_workspace_bytes(dp_dtype dt, int rows, int d, int f);
+dp_status dp_gated(const void* x, dp_dtype dt, int rows, int d, int f, const void* w_gate, const void* w_up, const void* b_gate,
+                   const void* b_up, dp_activation act, void* gate, void* up, void* h, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Its backward pass.  dgate and dup are the output gradients of the two projections, book-kept as the `g` of two linear layers whose input
+ * is x (dp_layer); the last projection's are (h, dy).
+ *   dh = dy w_down' (or given),  dgate = dh up act'(gate),  dup = dh act(gate),  dx = dgate w_gate' + dup w_up'  (of dgate and dup as stored)
+ *   dy        device, [rows, d_out] of type dt, with w_down device [f, d_out];  or, w_down NULL, dh itself, [rows, f] (d_out is not looked at)
+ *   gate, up  dp_gated's;  dgate, dup  device, [rows, f] of type dt; they may be gate and up, or one of them dh
+ *   dx        device, [rows, d] of type dt, or NULL: not wanted (then the weights may be NULL)
+ *   ws        device scratch, >= dp_gated_backward_workspace_bytes(...), 16-byte aligned; the size is 0 where it is not used
+ */
+size_t dp_gated_backward_workspace_bytes(dp_dtype dt, int rows, int d, int f, int d_out);
+dp_status dp_gated_backward(const void* dy, const void* w_down, int d_out, const void* gate, const void* up, dp_dtype dt, int rows, int d,
+                            int f, const void* w_gate, const void* w_up, dp_activation act, void* dgate, void* dup, void* dx, void* ws,
+                            size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

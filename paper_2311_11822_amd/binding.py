@@ -32,6 +32,8 @@ DP_OK, DP_ERR_INVALID_ARG, DP_ERR_UNSUPPORTED, DP_ERR_WORKSPACE, DP_ERR_HIP = ra
 DP_F32, DP_BF16, DP_F16 = 0, 1, 2
 DP_CLIP_STANDARD, DP_CLIP_AUTOMATIC = 0, 1
 DP_PATH_GHOST, DP_PATH_PEREX = 0, 1
+DP_ROTARY_PLAIN, DP_ROTARY_LINEAR, DP_ROTARY_BASE, DP_ROTARY_PARTS = range(4)
+DP_ACT_SILU, DP_ACT_GELU, DP_ACT_GELU_TANH, DP_ACT_RELU, DP_ACT_SIGMOID = range(5)
 
 
 class dp_layer(C.Structure):
@@ -43,6 +45,12 @@ class dp_attention_shape(C.Structure):
     _fields_ = [*((k, C.c_int32) for k in ("B", "H", "H_kv", "Tq", "Tk", "D", "causal")), ("scale", C.c_float),
                 *((k, C.c_int64 * 3) for k in ("q_stride", "k_stride", "v_stride", "o_stride")), ("q_len", C.c_void_p),
                 ("k_len", C.c_void_p)]
+
+
+class dp_heads_shape(C.Structure):
+    _fields_ = [*((k, C.c_int32) for k in ("B", "T", "H", "H_kv", "D", "rotary", "interleaved")), ("amplitude", C.c_float),
+                *((k, C.c_int64 * 3) for k in ("q_stride", "k_stride", "q_out_stride", "k_out_stride")), ("turns", C.c_void_p),
+                ("position", C.c_void_p), ("len", C.c_void_p)]
 
 
 class dp_adamw_tensor(C.Structure):
@@ -96,6 +104,16 @@ _PROTOS = {
     "dp_attention_tile_rows": (_i, [C.POINTER(dp_attention_shape), _i, _vp]),
     "dp_adamw_multi": (_i, [C.POINTER(dp_adamw_tensor), _i, _i, _i, _i, C.c_double, C.c_double, C.c_double, C.c_double, C.c_double,
                            _u64, _vp]),
+    "dp_rotary_turns": (_i, [C.POINTER(C.c_double), _i, C.c_double, _i, C.c_double, C.c_double, C.c_double, C.c_double]),
+    "dp_rotary": (_i, [C.POINTER(dp_heads_shape), _i, _vp, _vp, _vp, _vp, _vp]),
+    "dp_rotary_backward": (_i, [C.POINTER(dp_heads_shape), _i, _vp, _vp, _vp, _vp, _vp]),
+    "dp_head_norm": (_i, [C.POINTER(dp_heads_shape), _i, _vp, _vp, _vp, _vp, _f, _vp, _vp, _vp]),
+    "dp_head_norm_workspace_bytes": (_sz, [C.POINTER(dp_heads_shape), _i]),
+    "dp_head_norm_backward": (_i, [C.POINTER(dp_heads_shape), _i, _vp, _vp, _vp, _vp, _vp, _vp, _f, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "dp_gated_workspace_bytes": (_sz, [_i, _i, _i, _i]),
+    "dp_gated": (_i, [_vp, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "dp_gated_backward_workspace_bytes": (_sz, [_i, _i, _i, _i, _i]),
+    "dp_gated_backward": (_i, [_vp, _vp, _i, _vp, _vp, _i, _i, _i, _i, _vp, _vp, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
     "dp_ghost_tile_order": (C.c_int64, [_i, _i, _vp, _vp, _vp, _vp, C.c_int64]),
 }
 EXPORTS = tuple(_PROTOS)
@@ -389,6 +407,60 @@ def adamw_tensors(tensors: Sequence) -> "C.Array[dp_adamw_tensor]":
 def dp_adamw_multi(tensors, grad_dt, state_bits, copy_dt, lr, beta1, beta2, eps, grad_scale, step, stream=None) -> None:
     arr = tensors if isinstance(tensors, C.Array) else adamw_tensors(tensors)
     _call("dp_adamw_multi", arr, len(arr), grad_dt, state_bits, copy_dt, lr, beta1, beta2, eps, grad_scale, step, stream)
+
+
+def heads_shape(B, T, H, H_kv, D, rotary, interleaved, amplitude, q_stride, k_stride, q_out_stride, k_out_stride, turns=None, position=None,
+                len=None):
+    """Strides: (sample, token, head), in elements.  Turns, positions and lengths are held by address, as attention_shape's lengths are."""
+    three = C.c_int64 * 3
+    return (dp_heads_shape * 1)(dp_heads_shape(
+        B, T, H, H_kv, D, rotary, int(interleaved), amplitude, three(*q_stride), three(*k_stride), three(*q_out_stride),
+        three(*k_out_stride), _ptr(turns), _ptr(position), _ptr(len)))
+
+
+def dp_rotary_turns(rotary, base=10000.0, scaling=DP_ROTARY_PLAIN, factor=1.0, original=1.0, slow=1.0, fast=32.0):
+    """numpy float64 [rotary / 2] (host function)."""
+    import numpy as np
+    out = np.zeros(max(rotary // 2, 1))
+    _check(lib.dp_rotary_turns(out.ctypes.data_as(C.POINTER(C.c_double)), rotary, base, scaling, factor, original, slow, fast),
+           "dp_rotary_turns")
+    return out[:rotary // 2]
+
+
+def dp_rotary(shape, dt, q, k, q_out, k_out, stream=None) -> None:
+    _call("dp_rotary", shape, dt, q, k, q_out, k_out, stream)
+
+
+def dp_rotary_backward(shape, dt, dq_out, dk_out, dq, dk, stream=None) -> None:
+    _call("dp_rotary_backward", shape, dt, dq_out, dk_out, dq, dk, stream)
+
+
+def dp_head_norm(shape, dt, q, k, q_gain, k_gain, eps, q_out, k_out, stream=None) -> None:
+    _call("dp_head_norm", shape, dt, q, k, q_gain, k_gain, eps, q_out, k_out, stream)
+
+
+def dp_head_norm_workspace_bytes(shape, dt) -> int:
+    return lib.dp_head_norm_workspace_bytes(shape, dt)
+
+
+def dp_head_norm_backward(shape, dt, q, k, dq_out, dk_out, q_gain, k_gain, eps, dq, dk, kept, sqnorm_out, ws, stream=None) -> None:
+    _call("dp_head_norm_backward", shape, dt, q, k, dq_out, dk_out, q_gain, k_gain, eps, dq, dk, kept, sqnorm_out, ws, _nbytes(ws), stream)
+
+
+def dp_gated_workspace_bytes(dt, rows, d, f) -> int:
+    return lib.dp_gated_workspace_bytes(dt, rows, d, f)
+
+
+def dp_gated(x, dt, rows, d, f, w_gate, w_up, b_gate, b_up, act, gate, up, h, ws=None, stream=None) -> None:
+    _call("dp_gated", x, dt, rows, d, f, w_gate, w_up, b_gate, b_up, act, gate, up, h, ws, _nbytes(ws), stream)
+
+
+def dp_gated_backward_workspace_bytes(dt, rows, d, f, d_out) -> int:
+    return lib.dp_gated_backward_workspace_bytes(dt, rows, d, f, d_out)
+
+
+def dp_gated_backward(dy, w_down, d_out, gate, up, dt, rows, d, f, w_gate, w_up, act, dgate, dup, dx, ws=None, stream=None) -> None:
+    _call("dp_gated_backward", dy, w_down, d_out, gate, up, dt, rows, d, f, w_gate, w_up, act, dgate, dup, dx, ws, _nbytes(ws), stream)
 
 
 def dp_clipped_grad_tile_order(d_in: int, d_out: int):

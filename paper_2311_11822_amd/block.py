@@ -1,8 +1,9 @@
-"""What stands around the linear layers of a transformer block in a private training step: layer norm, attention and the
-optimizer.  Each object holds what a program keeps from step to step (parameters, layouts, workspaces) and checks the
-tensors that it is given; all arithmetic is the library's."""
+"""What stands around the linear layers of a transformer block in a private training step: layer norm, attention, the rotation and
+norms of heads, gated feed-forward layers' products and the optimizers.  Each object holds what a program keeps from step to step
+(parameters, layouts, workspaces) and checks the tensors that it is given; all arithmetic is the library's."""
 from __future__ import annotations
 
+import math
 from typing import Optional, Sequence
 
 import torch
@@ -216,3 +217,184 @@ class AdamW:
              stream=None) -> None:
         """step counts from 1; grad_scale: what makes the gradient's sum over samples a mean."""
         dp.dp_adamw_multi(self.tensors, self.grad_dt, self.bits, self.copy_dt, lr, beta1, beta2, eps, grad_scale, step, stream)
+
+
+SCALINGS = {"none": dp.DP_ROTARY_PLAIN, "linear": dp.DP_ROTARY_LINEAR, "base": dp.DP_ROTARY_BASE, "parts": dp.DP_ROTARY_PARTS}
+
+
+def rotary_turns(rotary: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original: float = 1.0, slow: float = 1.0,
+                 fast: float = 32.0) -> torch.Tensor:
+    """Whole turns of each pair of `rotary` columns from one position to the next, [rotary / 2] float64 on the CPU.  scaling, for contexts
+    longer than `original` by `factor`: "linear" (all turns slower), "base" (a larger base), "parts" (slower where a pair makes few
+    turns within the original context: as they are from `fast` turns on, 1 / factor up to `slow`)."""
+    if scaling not in SCALINGS:
+        raise ValueError(f"scaling: {', '.join(SCALINGS)}, not {scaling}")
+    return torch.from_numpy(dp.dp_rotary_turns(rotary, base, SCALINGS[scaling], factor, original, slow, fast))
+
+
+class _Heads:
+    """The layout of calls on heads, from tensors as they will be given: q and q_out [B, T, H, D], k and k_out [B, T, H_kv, D] or None,
+    views of packed projections among them."""
+
+    def __init__(self, q, k, q_out, k_out, turns, interleaved, amplitude, position, length):
+        if (k is None) != (k_out is None):
+            raise ValueError("k and k_out: both or neither")
+        self.tensors = 1 if k is None else 2
+        given = (q, q_out) if k is None else (q, k, q_out, k_out)
+        self.device, self.index, self.dtype, self.dt = q.device, q.get_device(), q.dtype, _dtype(q)
+        if any(t.dim() != 4 for t in given) or (k is not None and (q.shape[:2] != k.shape[:2] or q.shape[3] != k.shape[3])):
+            raise ValueError("q: [B, T, H, D], k: [B, T, H_kv, D]")
+        B, T, H, D = q.shape
+        rotary = 0
+        if turns is not None:
+            rotary = 2 * turns.numel()
+            _same("turns", turns, (turns.numel(),), torch.float64, q.device)
+        _same("position", position, (B, T), torch.int32, q.device)
+        _same("length", length, (B,), torch.int32, q.device)
+        if rotary > D:
+            raise ValueError(f"turns: of no more than {D // 2} pairs, not {turns.numel()}")
+        self.held = (turns, position, length)             # the shape has their addresses
+        self.shapes = (q.shape, None if k is None else k.shape)
+        self.in_strides = tuple(t.stride() for t in given[:self.tensors])
+        self.out_strides = tuple(t.stride() for t in given[self.tensors:])
+        for t in given:
+            if D > 1 and t.stride(3) != 1:
+                raise ValueError("columns of a head are adjacent")
+        three = lambda t: [st if n > 1 else 0 for n, st in zip(t.shape[:3], t.stride()[:3])] if t is not None else (0, 0, 0)  # noqa: E731
+        self.shape = dp.heads_shape(B, T, H, 0 if k is None else k.shape[2], D, rotary, interleaved, amplitude, three(q), three(k),
+                                    three(q_out), three(k_out), turns, position, length)
+        self._check((q, k), self.in_strides)
+        self._check((q_out, k_out), self.out_strides)
+        if dp.dp_head_norm_workspace_bytes(self.shape, self.dt) == 0:
+            raise ValueError("sizes or strides that heads do not have")
+        if self.index < 0:
+            raise ValueError(f"tensors on a GPU, not {q.device}")
+
+    def _check(self, pair, strides):
+        """Queries and keys of the layout's shapes, in these strides (an axis of one entry has whatever stride)."""
+        if (pair[1] is None) != (self.tensors == 1):
+            raise ValueError("queries and keys" if self.tensors == 2 else "queries alone")
+        for t, shape, want in zip(pair, self.shapes, strides):
+            if t.shape != shape or t.dtype is not self.dtype or t.get_device() != self.index:
+                raise ValueError(f"{tuple(shape)} of {self.dtype} on {self.device}, not {tuple(t.shape)} of {t.dtype} on {t.device}")
+            if t.stride() != want and any(n > 1 and st != w for n, st, w in zip(shape, t.stride(), want)):
+                raise ValueError(f"strides {want}, not {t.stride()}")
+
+
+class Rotary(_Heads):
+    """Position rotation of queries and keys.  turns: of each pair, float64 on the device (rotary_turns); the first 2 * len(turns)
+    columns of a head turn, interleaved pairs or halves.  position: [B, T] int32, None: 0, 1, 2 ...; length: [B] int32, rows behind it
+    are left as they are.  Turns, positions and lengths are read by every call: a program changes them in place."""
+
+    def __init__(self, q, k, q_out, k_out, turns, interleaved: bool = False, amplitude: float = 1.0, position=None, length=None):
+        if turns is None:
+            raise ValueError("turns of pairs")
+        super().__init__(q, k, q_out, k_out, turns, interleaved, amplitude, position, length)
+
+    def forward(self, q, k, q_out, k_out, stream=None) -> None:
+        """q_out may be q and k_out k, where their strides are the same."""
+        self._check((q, k), self.in_strides)
+        self._check((q_out, k_out), self.out_strides)
+        dp.dp_rotary(self.shape, self.dt, q, k, q_out, k_out, stream)
+
+    def backward(self, dq_out, dk_out, dq, dk, stream=None) -> None:
+        """dq_out, dk_out in the strides of q_out and k_out; dq, dk in those of q and k."""
+        self._check((dq_out, dk_out), self.out_strides)
+        self._check((dq, dk), self.in_strides)
+        dp.dp_rotary_backward(self.shape, self.dt, dq_out, dk_out, dq, dk, stream)
+
+
+class HeadNorm(_Heads):
+    """Norm of each head, x / sqrt(mean(x^2) + eps) * gain, and the rotation behind it (turns None: none).  Gains: [D] float32, of all
+    query heads and of all key heads, or None (ones)."""
+
+    def __init__(self, q, k, q_out, k_out, q_gain=None, k_gain=None, eps: float = 1e-6, turns=None, interleaved: bool = False,
+                 amplitude: float = 1.0, position=None, length=None):
+        super().__init__(q, k, q_out, k_out, turns, interleaved, amplitude, position, length)
+        for name, gain in (("q_gain", q_gain), ("k_gain", k_gain)):
+            _same(name, gain, (q.shape[3],), torch.float32, q.device)
+        self.gains, self.eps = (q_gain, k_gain), eps
+        self.kept_shape = torch.Size((q.shape[0], self.tensors, q.shape[3]))
+        self._ws, self._need = _Workspaces(), dp.dp_head_norm_workspace_bytes(self.shape, self.dt)
+
+    def forward(self, q, k, q_out, k_out, stream=None) -> None:
+        self._check((q, k), self.in_strides)
+        self._check((q_out, k_out), self.out_strides)
+        dp.dp_head_norm(self.shape, self.dt, q, k, *self.gains, self.eps, q_out, k_out, stream)
+
+    def backward(self, q, k, dq_out, dk_out, dq, dk, kept=None, sqnorm=None, stream=None) -> None:
+        """q, k: what forward was given; kept: [B, 2, D] ([B, 1, D] without keys), per-sample gradients of the gains, and sqnorm: [B], their
+        squared norms (LayerNorm.clipped_gradient adds the clipped ones up)."""
+        self._check((q, k), self.in_strides)
+        self._check((dq_out, dk_out), self.out_strides)
+        self._check((dq, dk), self.in_strides)
+        _same("kept", kept, self.kept_shape, torch.float32, self.device)
+        _same("sqnorm", sqnorm, self.kept_shape[:1], torch.float32, self.device)
+        ws = None
+        if kept is not None:
+            stream = dp._stream(stream)
+            ws = self._ws(self._need, self.device, self.index, stream)
+        dp.dp_head_norm_backward(self.shape, self.dt, q, k, dq_out, dk_out, *self.gains, self.eps, dq, dk, kept, sqnorm, ws, stream)
+
+
+ACTIVATIONS = {"silu": dp.DP_ACT_SILU, "gelu": dp.DP_ACT_GELU, "gelu_tanh": dp.DP_ACT_GELU_TANH, "relu": dp.DP_ACT_RELU,
+               "sigmoid": dp.DP_ACT_SIGMOID}
+
+
+class GatedFeedForward:
+    """h = act(x w_gate + b_gate) (x w_up + b_up).  w_gate, w_up: [d, f]; biases: [f] or None; w_down: [f, d_out], the projection that reads
+    h (its product is the program's own), or None: then the backward pass is given h's gradient.  All of the activations' type."""
+
+    def __init__(self, w_gate, w_up, w_down=None, b_gate=None, b_up=None, activation: str = "silu"):
+        if activation not in ACTIVATIONS:
+            raise ValueError(f"activation: {', '.join(ACTIVATIONS)}, not {activation}")
+        if w_gate.dim() != 2 or (w_down is not None and (w_down.dim() != 2 or w_down.shape[0] != w_gate.shape[1])):
+            raise ValueError("w_gate, w_up: [d, f]; w_down: [f, d_out]")
+        self.device, self.index, self.dtype, self.dt = w_gate.device, w_gate.get_device(), w_gate.dtype, _dtype(w_gate)
+        self.d, self.f = w_gate.shape
+        for name, t, shape in (("w_gate", w_gate, w_gate.shape), ("w_up", w_up, w_gate.shape), ("b_gate", b_gate, (self.f,)),
+                               ("b_up", b_up, (self.f,)), ("w_down", w_down, None if w_down is None else w_down.shape)):
+            _same(name, t, shape, self.dtype, self.device)
+        if self.index < 0:
+            raise ValueError(f"tensors on a GPU, not {self.device}")
+        self.act, self.weights, self.biases, self.w_down = ACTIVATIONS[activation], (w_gate, w_up), (b_gate, b_up), w_down
+        self.d_out = self.f if w_down is None else w_down.shape[1]
+        self._ws, self._need = _Workspaces(), {}
+
+    def _check(self, *sides) -> int:
+        """(width, tensors): [..., width] each, all of the same rows; their number."""
+        lead = None
+        for width, tensors in sides:
+            for t in tensors:
+                if t is None:
+                    continue
+                if lead is None:
+                    lead = t.shape[:-1]
+                if (t.dim() < 2 or t.shape[:-1] != lead or t.shape[-1] != width or t.dtype is not self.dtype or t.get_device() != self.index or
+                        not t.is_contiguous()):
+                    raise ValueError(f"contiguous [rows.., {width}] of {self.dtype} on {self.device}, not {tuple(t.shape)} of {t.dtype} on {t.device}")
+        return math.prod(lead)
+
+    def _scratch(self, key, stream, size, *args):
+        """The workspace of calls like this one, or None, and their stream."""
+        need = self._need.get(key)
+        if need is None:
+            need = self._need[key] = size(*args)
+        if need == 0:
+            return None, stream
+        stream = dp._stream(stream)
+        return self._ws(need, self.device, self.index, stream), stream
+
+    def forward(self, x, h, gate=None, up=None, stream=None) -> None:
+        """x: [B, T, d] or [rows, d]; h, and gate and up (kept for backward, or None): [.., f]."""
+        rows = self._check((self.d, (x,)), (self.f, (h, gate, up)))
+        ws, stream = self._scratch(rows, stream, dp.dp_gated_workspace_bytes, self.dt, rows, self.d, self.f)
+        dp.dp_gated(x, self.dt, rows, self.d, self.f, *self.weights, *self.biases, self.act, gate, up, h, ws, stream)
+
+    def backward(self, dy, gate, up, dgate, dup, dx=None, stream=None) -> None:
+        """dy: [.., d_out], or with no w_down h's own gradient [.., f]; dgate, dup: [.., f], output gradients of the two projections (may be gate
+        and up); dx: [.., d] or None."""
+        rows = self._check((self.d_out, (dy,)), (self.f, (gate, up, dgate, dup)), (self.d, (dx,)))
+        ws, stream = self._scratch((rows, dx is None), stream, dp.dp_gated_backward_workspace_bytes, self.dt, rows, self.d, self.f, self.d_out)
+        dp.dp_gated_backward(dy, self.w_down, self.d_out, gate, up, self.dt, rows, self.d, self.f, *self.weights, self.act, dgate, dup, dx, ws,
+                             stream)

@@ -163,7 +163,13 @@ PyObject* set_torch(PyObject*, PyObject* module) {
   X(dp_layer_norm_backward) \
   X(dp_attention) \
   X(dp_attention_backward) \
-  X(dp_adamw_multi)
+  X(dp_adamw_multi) \
+  X(dp_rotary) \
+  X(dp_rotary_backward) \
+  X(dp_head_norm) \
+  X(dp_head_norm_backward) \
+  X(dp_gated) \
+  X(dp_gated_backward)
 #else
 #define DP_MODULE _pycall
 #define DP_CALLS(X) \

@@ -1,0 +1,363 @@
+"""Rotation and norms of heads, gated feed-forward layers and the orthogonalising optimizer against plain 64-bit implementations on the
+CPU, at the sizes, layouts, positions and lengths where they can go wrong.
+
+Tolerances, relative in the 2-norm unless said otherwise.  U is half a unit in the last place of the storage type, relative to the
+value: what one rounding may err by.
+  stored results     one rounding: U, and what the fp32 arithmetic before it errs by
+  FP32               2e-6: some ten fp32 operations in a row (each 2^-24 = 6e-8 at most), or a sum of up to 1000 products in fp32 (sqrt(1000) 2^-24);
+                     an angle, a fraction of a turn rounded to fp32, is within 2 pi 2^-26 = 9.4e-8
+"""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+U = {"bf16": 2.0 ** -8, "f16": 2.0 ** -11, "f32": 2.0 ** -24}
+FP32 = 2e-6
+
+
+@pytest.fixture(scope="module")
+def block():
+    from paper_2311_11822_amd import block as b
+    assert torch.cuda.is_available()
+    return b
+
+
+def rel(got, want):
+    got, want = got.detach().cpu().double(), want.detach().cpu().double()
+    assert got.shape == want.shape
+    assert torch.equal(torch.isfinite(got), torch.isfinite(want))
+    fine = torch.isfinite(want)
+    norm = want[fine].norm().item()
+    off = (got[fine] - want[fine]).norm().item()
+    return off / norm if norm else (0.0 if off == 0 else math.inf)
+
+
+def rand(gen, shape, dtype, scale=1.0):
+    return (torch.randn(shape, generator=gen, dtype=torch.float64) * scale).to(DTYPES[dtype])
+
+
+# ------------------------------------------------------------------------------------------------ heads
+
+def turn(x, turns, interleaved, amplitude, position, back=False):
+    """x [B, T, h, D] in 64 bits; position [B, T]."""
+    n = 2 * len(turns)
+    angle = 2 * math.pi * (position.double()[..., None, None] * turns)
+    cos, sin = amplitude * angle.cos(), amplitude * angle.sin() * (-1 if back else 1)
+    y = x.clone()
+    a, b = (slice(0, n, 2), slice(1, n, 2)) if interleaved else (slice(0, n // 2), slice(n // 2, n))
+    y[..., a], y[..., b] = x[..., a] * cos - x[..., b] * sin, x[..., b] * cos + x[..., a] * sin
+    return y
+
+
+class Heads:
+    """Inputs of one layout on the CPU and on the device, as views of a packed projection."""
+
+    def __init__(self, dtype, B, T, H, Hkv, D, rotary, interleaved, start=None, ragged=False, amplitude=1.0, seed=0):
+        gen = torch.Generator().manual_seed(seed + B * 7919 + T * 31 + D)
+        self.B, self.T, self.H, self.Hkv, self.D, self.dtype, self.ragged = B, T, H, Hkv, D, dtype, ragged
+        self.x = rand(gen, (B, T, H + 2 * Hkv, D), dtype, 1.5)
+        self.dy = [rand(gen, (B, T, h, D), dtype) for h in (H, Hkv)]
+        self.gains = [1 + 0.3 * rand(gen, (D,), "f32") for _ in range(2)]
+        self.kw = dict(interleaved=interleaved, amplitude=amplitude)
+        self.position = torch.arange(T, dtype=torch.int32).repeat(B, 1)
+        if start is not None:
+            self.position += torch.randint(start, start + 1000, (B, 1), generator=gen, dtype=torch.int32)
+            self.kw["position"] = self.position.cuda()
+        self.len = torch.full((B,), T)
+        if ragged:
+            self.len = torch.randint(0, T + 1, (B,), generator=gen)
+            self.len[0] = T
+            self.kw["length"] = self.len.to(torch.int32).cuda()
+        self.there = (torch.arange(T) < self.len[:, None])[..., None, None]
+        self.rotary = rotary
+
+    def views(self, packed):
+        return packed[:, :, :self.H], (packed[:, :, self.H:self.H + self.Hkv] if self.Hkv else None)
+
+    def make(self, block, kind):
+        turns = block.rotary_turns(self.rotary) if self.rotary else None
+        self.turns = turns if turns is not None else torch.zeros(0, dtype=torch.float64)
+        if turns is not None:
+            self.kw["turns"] = turns.cuda()
+        self.q, self.k = self.views(self.x.cuda())
+        fresh = lambda h: torch.full((self.B, self.T, h, self.D), 7.0, dtype=DTYPES[self.dtype], device="cuda") if h else None  # noqa: E731
+        self.out = [fresh(self.H), fresh(self.Hkv)]
+        gains = [g.cuda() for g in self.gains] if kind == "HeadNorm" else []
+        if not self.Hkv and gains:
+            gains[1] = None
+        return getattr(block, kind)(self.q, self.k, *self.out, *gains, **self.kw)
+
+    def turned(self, x, back=False):
+        return turn(x, self.turns, self.kw["interleaved"], self.kw["amplitude"], self.position, back) if self.rotary else x
+
+    def check(self, got, want, tol):
+        """Rows that are there to `tol`, the others untouched."""
+        there = self.there.expand(want.shape)
+        assert rel(got.cpu()[there], want[there]) <= tol
+        assert (got.cpu()[~there] == 7).all()
+
+    @property
+    def sides(self):
+        return range(2 if self.Hkv else 1)
+
+
+HEADS = [  # B, T, H, Hkv, D, rotary, interleaved
+    (1, 1, 1, 1, 8, 8, False), (2, 5, 3, 0, 16, 16, True), (8, 1, 12, 12, 64, 64, False), (3, 33, 4, 2, 64, 64, False),
+    (2, 70, 6, 2, 128, 128, False), (2, 17, 5, 1, 128, 64, True), (3, 9, 7, 7, 56, 56, False), (2, 40, 2, 2, 24, 20, False),
+    (2, 21, 3, 1, 40, 6, False), (1, 300, 2, 1, 256, 256, False), (1, 19, 9, 3, 256, 130, True), (2, 11, 20, 20, 72, 2, False),
+    (5, 130, 1, 1, 8, 4, True), (1, 2, 70, 70, 64, 64, False), (1, 1100, 3, 3, 32, 32, False), (2, 3, 300, 1, 8, 6, False)]
+HEADS_F32 = HEADS + [(2, 13, 3, 2, 1, 0, False), (2, 9, 2, 1, 3, 2, True), (1, 37, 5, 5, 255, 254, False), (3, 8, 2, 2, 130, 66, True),
+                     (2, 6, 4, 4, 6, 6, False), (1, 5, 2, 2, 2, 2, False), (2, 12, 3, 3, 129, 126, False)]
+LAYOUTS = [(d, s) for d in DTYPES for s in (HEADS_F32 if d == "f32" else HEADS)]
+
+
+@pytest.mark.parametrize("dtype,size", LAYOUTS, ids=str)
+def test_rotary(block, dtype, size):
+    if size[5] == 0:
+        return
+    for start, ragged, amplitude in ((None, False, 1.0), (100000, True, 1.3)):
+        h = Heads(dtype, *size, start, ragged, amplitude)
+        plan = h.make(block, "Rotary")
+        plan.forward(h.q, h.k, *h.out)
+        for w in h.sides:
+            x = (h.q, h.k)[w].cpu().double()
+            h.check(h.out[w], h.turned(x), U[dtype] + FP32)
+        # the gradient, in the projection's layout; values behind queries and keys stay
+        packed = torch.full(h.x.shape, 7.0, dtype=DTYPES[dtype], device="cuda")
+        dq, dk = h.views(packed)
+        dy = [t.cuda() if w in h.sides else None for w, t in enumerate(h.dy)]
+        plan.backward(*dy, dq, dk)
+        for w in h.sides:
+            h.check((dq, dk)[w], h.turned(h.dy[w].double(), True), U[dtype] + FP32)
+        assert (packed[:, :, h.H + h.Hkv:] == 7).all()
+        # in place
+        q, k = (None if t is None else t.clone() for t in (h.q, h.k))
+        if h.H + 2 * h.Hkv == h.H:
+            continue
+        same = block.Rotary(q, k, q, k, **h.kw)
+        same.forward(q, k, q, k)
+        for w in h.sides:
+            there = h.there.expand(h.out[w].shape).cuda()
+            assert torch.equal((q, k)[w][there], h.out[w][there])
+
+
+@pytest.mark.parametrize("dtype,size", LAYOUTS, ids=str)
+def test_head_norm(block, dtype, size):
+    for start, ragged, rotary in ((None, False, size[5]), (5000, True, size[5]), (None, True, 0)):
+        h = Heads(dtype, *size[:5], rotary, size[6], start, ragged)
+        plan = h.make(block, "HeadNorm")
+        plan.forward(h.q, h.k, *h.out)
+        packed = torch.full(h.x.shape, 7.0, dtype=DTYPES[dtype], device="cuda")
+        grads = h.views(packed)
+        dy = [t.cuda() if w in h.sides else None for w, t in enumerate(h.dy)]
+        kept = torch.empty((h.B, len(h.sides), h.D), device="cuda")
+        sqnorm = torch.empty(h.B, device="cuda")
+        plan.backward(h.q, h.k, *dy, *grads, kept, sqnorm)
+        want = []
+        for w in h.sides:
+            x, gain = (h.q, h.k)[w].cpu().double(), h.gains[w].double()
+            r = (x.square().mean(-1, keepdim=True) + 1e-6) ** -0.5
+            h.check(h.out[w], h.turned(x * r * gain), U[dtype] + 4 * FP32)
+            g = h.turned(h.dy[w].double(), True)
+            u = g * gain
+            dx = r * (u - x * r * (u * x * r).mean(-1, keepdim=True))
+            if h.D > 1:                                  # (of one column all of dx cancels)
+                h.check(grads[w], dx, U[dtype] + 8 * FP32)
+            want.append((g * x * r * h.there).sum((1, 2)))
+        want = torch.stack(want, 1)
+        # sums of up to 1100 tokens' heads, each term's own error 4 FP32 of it at most, independent of the others'
+        scale = (h.dy[0].double().square().sum((1, 2)).sqrt().max() * 4).item()
+        assert (kept.cpu().double() - want).abs().max() <= 4 * FP32 * max(scale, want.abs().max().item())
+        assert rel(sqnorm, kept.double().square().sum((1, 2))) <= FP32
+        # without the gains' gradients, and in place of dy: the same bits
+        if h.Hkv:
+            again = [t.clone() for t in dy]
+            inplace = block.HeadNorm(*again, *h.out, *[g.cuda() for g in h.gains], **h.kw)
+            xs = [t.contiguous() for t in (h.q, h.k)]
+            inplace.backward(*xs, *again, *again)
+            for w in h.sides:
+                there = h.there.expand(again[w].shape).cuda()
+                assert torch.equal(again[w][there], grads[w][there])
+                assert torch.equal(again[w][~there], dy[w][~there])
+
+
+def test_rotary_far_positions(block):
+    """Negative and largest positions: the angle is the fraction of a turn in 64 bits."""
+    at = torch.tensor([[0, 1, -1, 2 ** 31 - 1, -2 ** 31, 123456789, -99999999]], dtype=torch.int32)
+    gen = torch.Generator().manual_seed(5)
+    x = rand(gen, (1, 7, 2, 32), "f32")
+    turns = block.rotary_turns(32, 500000.0)
+    q = x.cuda()
+    out = torch.empty_like(q)
+    block.Rotary(q, None, out, None, turns.cuda(), position=at.cuda()).forward(q, None, out, None)
+    # 2^31 positions in 64 bits: 2^-53 2^31 of a turn and its own angle's rounding in the reference as well
+    assert rel(out, turn(x.double(), turns, False, 1.0, at)) <= FP32
+
+
+def test_rotary_rows_behind_and_empty(block):
+    """Lengths of zero, below it and beyond T; what lies behind a length may be anything."""
+    x = torch.full((4, 6, 2, 16), math.nan)
+    lens = torch.tensor([0, -3, 99, 2], dtype=torch.int32)
+    x[2], x[3, :2] = 1.0, 1.0
+    q, out = x.cuda(), torch.full(x.shape, 7.0).cuda()
+    gain, kept, sqnorm = torch.ones(16, device="cuda"), torch.empty((4, 1, 16), device="cuda"), torch.empty(4, device="cuda")
+    norm = block.HeadNorm(q, None, out, None, gain, None, turns=block.rotary_turns(16).cuda(), length=lens.cuda())
+    norm.forward(q, None, out, None)
+    assert (out[:2] == 7).all() and (out[3, 2:] == 7).all() and torch.isfinite(out).all()
+    dq = torch.full(x.shape, 7.0).cuda()
+    norm.backward(q, None, q, None, dq, None, kept, sqnorm)
+    assert (dq[:2] == 7).all() and (dq[3, 2:] == 7).all() and torch.isfinite(dq).all()
+    assert (kept[:2] == 0).all() and (sqnorm[:2] == 0).all() and torch.isfinite(kept).all()
+
+
+def along(f, x, direction, step):
+    return (f(x + step * direction) - f(x - step * direction)) / (2 * step)
+
+
+def test_head_norm_gradient_by_differences(block):
+    """Central differences along the gradient itself, where they are its norm.  Step 2^-5 of values of size 1.5: third derivatives leave some
+    (2^-5 / 1.5)^2 / 6 = 7e-5 of it, fp32 values FP32 / 2^-5 = 6e-5 of |y| |dy| over |dx|, which is some 10 here."""
+    h = Heads("f32", 2, 5, 3, 2, 16, 12, False, 50)
+    plan = h.make(block, "HeadNorm")
+    x, dy = [t.contiguous() for t in (h.q, h.k)], [t.cuda() for t in h.dy]
+    plan = block.HeadNorm(*x, *h.out, *[g.cuda() for g in h.gains], **h.kw)
+    dx, kept, sqnorm = [torch.empty_like(t) for t in x], torch.empty((2, 2, 16), device="cuda"), torch.empty(2, device="cuda")
+    plan.backward(*x, *dy, *dx, kept, sqnorm)
+
+    def loss(w, value, gains=None):
+        now = plan if gains is None else block.HeadNorm(*x, *h.out, *gains, **h.kw)
+        at = list(x)
+        if w is not None:
+            at[w] = value.float()
+        now.forward(*at, *h.out)
+        return sum((a.double() * b.double()).sum() for a, b in zip(h.out, dy)).item()
+
+    for w in range(2):
+        n = dx[w].double().norm()
+        v = dx[w].double() / n
+        assert abs(along(lambda t: loss(w, t), x[w].double(), v, 2.0 ** -5) - n.item()) <= 2e-3 * n.item()
+        total = kept.double().sum(0)[w]
+        v = total / total.norm()
+        gains = [g.cuda() for g in h.gains]
+
+        def of_gain(t):
+            return loss(None, None, [t.float() if i == w else g for i, g in enumerate(gains)])
+        # y is linear in the gains
+        assert abs(along(of_gain, gains[w].double(), v, 2.0 ** -3) - total.norm().item()) <= 1e-3 * total.norm().item()
+
+
+# ------------------------------------------------------------------------------------------------ gated feed-forward layers
+
+def act_reference(x, act):
+    x = x.clone().requires_grad_()
+    y = {"silu": lambda: x * torch.sigmoid(x), "gelu": lambda: 0.5 * x * torch.special.erfc(-x * 0.5 ** 0.5),
+         "gelu_tanh": lambda: x * torch.sigmoid(2 * (2 / math.pi) ** 0.5 * (x + 0.044715 * x ** 3)),
+         "relu": lambda: torch.where(x > 0, x, 0.0), "sigmoid": lambda: torch.sigmoid(x)}[act]()
+    return y.detach(), torch.autograd.grad(y.sum(), x)[0]
+
+
+ACTS = ["silu", "gelu", "gelu_tanh", "relu", "sigmoid"]
+GATED = [  # rows, d, f, d_out
+    (1, 8, 8, 8), (1, 1280, 24, 8), (3, 64, 136, 64), (16, 40, 520, 40), (17, 264, 64, 128), (33, 48, 200, 48), (64, 128, 256, 128), (65, 72, 72, 72),
+    (111, 60, 168, 60), (128, 512, 128, 512), (200, 96, 1032, 96), (257, 88, 264, 40), (300, 776, 512, 776), (520, 256, 512, 264), (1030, 40, 40, 40),
+    (4, 2056, 1000, 24), (31, 16, 4104, 16), (700, 1032, 264, 512)]
+GATED_F32 = GATED + [(1, 1, 1, 1), (5, 3, 7, 2), (111, 60, 161, 61), (130, 257, 65, 33), (64, 17, 129, 130)]
+GATED_CASES = [(d, *s) for d in DTYPES for s in (GATED_F32 if d == "f32" else [(r, 8 * -(-a // 8), b, 8 * -(-c // 8)) for r, a, b, c in GATED])]
+
+
+def same(x, want, tol, dtype):
+    """To a stored result's rounding and `tol` of what came before it."""
+    assert rel(x, want) <= U[dtype] + tol, (rel(x, want), U[dtype] + tol)
+
+
+@pytest.mark.parametrize("dtype,rows,d,f,d_out", GATED_CASES)
+def test_gated_forward(block, dtype, rows, d, f, d_out):
+    gen = torch.Generator().manual_seed(rows * 1009 + d)
+    x, wg, wu = rand(gen, (rows, d), dtype), rand(gen, (d, f), dtype, d ** -0.5), rand(gen, (d, f), dtype, d ** -0.5)
+    bg, bu = rand(gen, (f,), dtype), rand(gen, (f,), dtype)
+    act = ACTS[(rows + d) % 5]
+    for biases in (False, True):
+        layer = block.GatedFeedForward(wg.cuda(), wu.cuda(), None, *((bg.cuda(), bu.cuda()) if biases else (None, None)), activation=act)
+        guard = torch.full((3, rows + 1, f), 7.0, dtype=DTYPES[dtype], device="cuda")           # a row behind each result stays
+        gate, up, h = (t[:rows] for t in guard)
+        layer.forward(x.cuda(), h, gate, up)
+        want_gate = x.double() @ wg.double() + (bg.double() if biases else 0)
+        want_up = x.double() @ wu.double() + (bu.double() if biases else 0)
+        same(gate, want_gate, FP32, dtype)
+        same(up, want_up, FP32, dtype)
+        same(h, act_reference(want_gate, act)[0] * want_up, 4 * FP32 + (2e-4 if dtype == "bf16" else 1e-4 if dtype == "f16" else 0), dtype)
+        assert (guard[:, rows] == 7).all()
+        alone = torch.empty_like(h)
+        layer.forward(x.cuda(), alone)
+        assert torch.equal(alone, h)
+
+
+@pytest.mark.parametrize("dtype,rows,d,f,d_out", GATED_CASES)
+def test_gated_backward(block, dtype, rows, d, f, d_out):
+    gen = torch.Generator().manual_seed(rows * 1013 + f)
+    wg, wu, wd = rand(gen, (d, f), dtype, f ** -0.5), rand(gen, (d, f), dtype, f ** -0.5), rand(gen, (f, d_out), dtype, d_out ** -0.5)
+    gate, up, dy, dh = rand(gen, (rows, f), dtype, 1.5), rand(gen, (rows, f), dtype), rand(gen, (rows, d_out), dtype), rand(gen, (rows, f), dtype)
+    act = ACTS[(rows + f) % 5]
+    value, slope = act_reference(gate.double(), act)
+    for down in (True, False):
+        layer = block.GatedFeedForward(wg.cuda(), wu.cuda(), wd.cuda() if down else None, activation=act)
+        guard = torch.full((2, rows + 1, f), 7.0, dtype=DTYPES[dtype], device="cuda")
+        dgate, dup = (t[:rows] for t in guard)
+        below = torch.full((rows + 1, d), 7.0, dtype=DTYPES[dtype], device="cuda")
+        given = (dy if down else dh).cuda()
+        layer.backward(given, gate.cuda(), up.cuda(), dgate, dup, below[:rows])
+        back = dy.double() @ wd.double().t() if down else dh.double()
+        same(dgate, back * up.double() * slope, 4 * FP32 + (0 if dtype == "f32" else 2e-4), dtype)
+        same(dup, back * value, 4 * FP32 + (0 if dtype == "f32" else 2e-4), dtype)
+        # of the two as they are stored
+        want = dgate.cpu().double() @ wg.double().t() + dup.cpu().double() @ wu.double().t()
+        same(below[:rows], want, 4 * FP32, dtype)
+        assert (guard[:, rows] == 7).all() and (below[rows] == 7).all()
+        # in the place of what it reads, and without dx: the same bits
+        g2, u2 = gate.cuda(), up.cuda()
+        layer.backward(given, g2, u2, g2, u2)
+        assert torch.equal(g2, dgate) and torch.equal(u2, dup)
+        if not down:
+            g2 = gate.cuda()
+            layer.backward(given, g2, up.cuda(), g2, given)
+            assert torch.equal(g2, dgate) and torch.equal(given, dup)
+
+
+@pytest.mark.parametrize("act", ACTS)
+def test_gated_extreme_gates(block, act):
+    """Gates far from zero: shares of exactly 0 and 1, no NaN where the value has none."""
+    gate = torch.tensor([[-300.0, -90.0, -40.0, -12.0, -1e-30, 0.0, 1e-30, 12.0, 40.0, 90.0, 300.0, -3.0, 3.0, -0.5, 0.5, 1.0]])
+    layer = block.GatedFeedForward(torch.eye(16).cuda(), torch.eye(16).cuda(), activation=act)
+    up, dh = torch.full((1, 16), 2.0), torch.full((1, 16), 3.0)
+    dgate, dup = torch.empty((1, 16), device="cuda"), torch.empty((1, 16), device="cuda")
+    layer.backward(dh.cuda(), gate.cuda(), up.cuda(), dgate, dup)
+    value, slope = act_reference(gate.double(), act)
+    # absolute, where a share is next to nothing; gelu's tail at -12 is some 1e-32
+    assert ((dup.cpu().double() - 3 * value).abs() <= 4 * FP32 * (3 * value).abs() + 1e-30).all()
+    assert ((dgate.cpu().double() - 6 * slope).abs() <= 8 * FP32 * (6 * slope).abs() + 1e-6 * (slope.abs() < 1e-3) + 1e-30).all()
+    h = torch.empty((1, 16), device="cuda")
+    layer.forward(gate.cuda(), h)
+    assert ((h.cpu().double() - value * gate.double()).abs() <= 4 * FP32 * (value * gate.double()).abs() + 1e-30).all()
+
+
+def test_gated_gradient_by_differences(block):
+    """Central differences of sum(dh h) along dx, as for the norms: step 2^-5, third derivatives of a gate of size 1 leave some 2e-4 of it."""
+    gen = torch.Generator().manual_seed(3)
+    for act in ("silu", "gelu", "gelu_tanh", "sigmoid"):
+        x, wg, wu = rand(gen, (9, 24), "f32").cuda(), rand(gen, (24, 40), "f32", 0.2).cuda(), rand(gen, (24, 40), "f32", 0.2).cuda()
+        dh, layer = rand(gen, (9, 40), "f32").cuda(), None
+        layer = block.GatedFeedForward(wg, wu, activation=act)
+        gate, up, h, dgate, dup = (torch.empty((9, 40), device="cuda") for _ in range(5))
+        dx = torch.empty_like(x)
+        layer.forward(x, h, gate, up)
+        layer.backward(dh, gate, up, dgate, dup, dx)
+
+        def loss(t):
+            layer.forward(t.float(), h)
+            return (h.double() * dh.double()).sum().item()
+        n = dx.double().norm().item()
+        assert abs(along(loss, x.double(), dx.double() / n, 2.0 ** -5) - n) <= 2e-3 * n
