@@ -19,6 +19,9 @@ struct GatedArgs {
   int parts;
 };
 
+// The products: x with both weights; dy with w_down; dgate and dup with theirs.
+enum GatedPass { kForward, kHidden, kInput };
+dp_status launch_gated_tiles(const GatedArgs& a, dp_dtype dt, GatedPass pass, hipStream_t s);      // 16-bit types (gated_tiles.hip)
 dp_status launch_gated_forward(const GatedArgs& a, dp_dtype dt, hipStream_t s);
 dp_status launch_gated_backward(const GatedArgs& a, dp_dtype dt, hipStream_t s);
 

@@ -8,11 +8,10 @@ namespace dpbk {
 namespace {
 
 constexpr int kThreads = 256, kRows = 64, kCols = 64, kDepth = 16;     // a tile: 64 rows, two sets of 64 columns; 16 terms at a time
-enum GatedPass { kForward, kHidden, kInput };
 
 // Two sets of columns side by side: forward the gate's and up's, else a product's at n0 and n0 + 64.  A wave has 32 rows and 32 columns of
 // each set.  As [row][k], columns' operands [k][column] as they lie (forward) or [column][k].
-template <int DT, int PASS>
+template <int PASS>
 __global__ void __launch_bounds__(kThreads) gated_f32_kernel(const GatedArgs a, int tiles_n) {
   constexpr int PITCH = kDepth + 1;
   __shared__ float la[kRows * PITCH], lb[2][PASS == kForward ? kDepth * kCols : kCols * PITCH];
@@ -20,11 +19,7 @@ __global__ void __launch_bounds__(kThreads) gated_f32_kernel(const GatedArgs a, 
   const int tm = blockIdx.x / (unsigned)tiles_n, tn = blockIdx.x - tm * tiles_n;
   const int m0 = tm * kRows, n0 = tn * (PASS == kForward ? kCols : 2 * kCols);
   const int N = PASS == kInput ? a.d : a.f, K = PASS == kForward ? a.d : PASS == kHidden ? a.d_out : a.f;
-  auto value = [](const void* base, int64_t at) {
-    Values<DT, 1> v;
-    v.load(base, at);
-    return v.get(0);
-  };
+  auto value = [](const void* base, int64_t at) { return static_cast<const float*>(base)[at]; };
   f32x16 acc[2];
 #pragma unroll
   for (int s = 0; s < 2; ++s)
@@ -75,11 +70,7 @@ __global__ void __launch_bounds__(kThreads) gated_f32_kernel(const GatedArgs a, 
     }
   }
   // lane: column 32 (wave & 1) + lane % 32; register r: row 8 (r / 4) + 4 (lane / 32) + r % 4 of the wave's 32
-  auto put = [](void* base, int64_t at, float x) {
-    Values<DT, 1> v;
-    v.set({x});
-    v.store(base, at);
-  };
+  auto put = [](void* base, int64_t at, float x) { static_cast<float*>(base)[at] = x; };
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
     const int m = m0 + 32 * (wave >> 1) + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
@@ -149,27 +140,28 @@ dp_status launch_slopes(const GatedArgs& a, hipStream_t s) {
   return hip_status(hipGetLastError());
 }
 
-template <int DT, int PASS>
+template <int PASS>
 dp_status launch_f32(const GatedArgs& a, hipStream_t s) {
   const int N = PASS == kInput ? a.d : a.f, width = PASS == kForward ? kCols : 2 * kCols;
   const int64_t tiles_n = (N + width - 1) / width, tiles_m = (a.rows + kRows - 1) / kRows;
-  gated_f32_kernel<DT, PASS><<<dim3((unsigned)(tiles_m * tiles_n)), kThreads, 0, s>>>(a, (int)tiles_n);
+  gated_f32_kernel<PASS><<<dim3((unsigned)(tiles_m * tiles_n)), kThreads, 0, s>>>(a, (int)tiles_n);
   return hip_status(hipGetLastError());
-}
-
-template <int DT>
-dp_status backward(const GatedArgs& a, hipStream_t s) {
-  dp_status st = a.w_down ? launch_f32<DT, kHidden>(a, s) : launch_slopes<DT>(a, s);
-  return st == DP_OK && a.dx ? launch_f32<DT, kInput>(a, s) : st;
 }
 
 }  // namespace
 
 dp_status launch_gated_forward(const GatedArgs& a, dp_dtype dt, hipStream_t s) {
-  return dt == DP_F32 ? launch_f32<DP_F32, kForward>(a, s) : dt == DP_BF16 ? launch_f32<DP_BF16, kForward>(a, s) : launch_f32<DP_F16, kForward>(a, s);
+  return dt == DP_F32 ? launch_f32<kForward>(a, s) : launch_gated_tiles(a, dt, kForward, s);
 }
+
 dp_status launch_gated_backward(const GatedArgs& a, dp_dtype dt, hipStream_t s) {
-  return dt == DP_F32 ? backward<DP_F32>(a, s) : dt == DP_BF16 ? backward<DP_BF16>(a, s) : backward<DP_F16>(a, s);
+  dp_status st;
+  if (!a.w_down)
+    st = dt == DP_F32 ? launch_slopes<DP_F32>(a, s) : dt == DP_BF16 ? launch_slopes<DP_BF16>(a, s) : launch_slopes<DP_F16>(a, s);
+  else
+    st = dt == DP_F32 ? launch_f32<kHidden>(a, s) : launch_gated_tiles(a, dt, kHidden, s);
+  if (st != DP_OK || !a.dx) return st;
+  return dt == DP_F32 ? launch_f32<kInput>(a, s) : launch_gated_tiles(a, dt, kInput, s);
 }
 
 }  // namespace dpbk
