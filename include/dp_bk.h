@@ -639,6 +639,32 @@ dp_status dp_gated_backward(const void* dy, const void* w_down, int d_out, const
                             int f, const void* w_gate, const void* w_up, dp_activation act, void* dgate, void* dup, void* dx, void* ws,
                             size_t ws_bytes, void* stream);
 
+/*
+ * One step of an optimizer that orthogonalises its update, over many matrices, in place:
+ *   g = grad_scale grad;  m = beta m + g;  u = g + beta m (nesterov = 1) or m;  X = u / (||u||_F + eps);
+ *   `iterations` times  X <- a X + b A X + c A^2 X,  A = X X'  (on the shorter side);
+ *   param = param (1 - lr weight_decay) - lr scale X.
+ * Products are as exact as fp32's (values in two fp16 halves, three products of them, sums in fp32).
+ *   tensors      HOST array; param, m fp32 [rows, cols]; grad of type grad_dt; copy of type copy_dt (DP_F32: not used), the new param rounded;
+ *                elements need no more than their own alignment.  rows and cols are at most 2^20, the shorter at most 2^16.
+ *   coefficients HOST fp64 [iterations, 3]: a, b, c of each iteration, 1 to 32 of them.  Singular values, which start in [0, 1], may not leave
+ *                |x| <= 15 on the way, nor A's polynomial (DP_ERR_UNSUPPORTED).
+ *   ws           device scratch, >= dp_muon_workspace_bytes(...), 16-byte aligned: some 8 bytes an element of up to 40 matrices at a time and 8 of
+ *                each shorter side squared
+ * Matrices go in runs of up to 40, each of them a few launches whatever the number of its matrices.
+ */
+typedef struct {
+  float* param;
+  const void* grad;
+  float* m;
+  void* copy;
+  int32_t rows, cols;
+  float weight_decay, scale;
+} dp_muon_tensor;
+size_t dp_muon_workspace_bytes(const dp_muon_tensor* tensors, int n_tensors);
+dp_status dp_muon_multi(const dp_muon_tensor* tensors, int n_tensors, dp_dtype grad_dt, dp_dtype copy_dt, double lr, double beta, int nesterov,
+                        double grad_scale, double eps, const double* coefficients, int iterations, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

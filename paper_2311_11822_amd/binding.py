@@ -58,6 +58,11 @@ class dp_adamw_tensor(C.Structure):
                 ("weight_decay", C.c_float), ("reserved", C.c_int32)]
 
 
+class dp_muon_tensor(C.Structure):
+    _fields_ = [*((k, C.c_void_p) for k in ("param", "grad", "m", "copy")), ("rows", C.c_int32), ("cols", C.c_int32),
+                ("weight_decay", C.c_float), ("scale", C.c_float)]
+
+
 _vp, _i, _f, _u64, _sz = C.c_void_p, C.c_int, C.c_float, C.c_uint64, C.c_size_t
 _PROTOS = {
     "dp_status_string": (C.c_char_p, [_i]),
@@ -114,6 +119,9 @@ _PROTOS = {
     "dp_gated": (_i, [_vp, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
     "dp_gated_backward_workspace_bytes": (_sz, [_i, _i, _i, _i, _i]),
     "dp_gated_backward": (_i, [_vp, _vp, _i, _vp, _vp, _i, _i, _i, _i, _vp, _vp, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "dp_muon_workspace_bytes": (_sz, [C.POINTER(dp_muon_tensor), _i]),
+    "dp_muon_multi": (_i, [C.POINTER(dp_muon_tensor), _i, _i, _i, C.c_double, C.c_double, _i, C.c_double, C.c_double, C.POINTER(C.c_double), _i,
+                          _vp, _sz, _vp]),
     "dp_ghost_tile_order": (C.c_int64, [_i, _i, _vp, _vp, _vp, _vp, C.c_int64]),
 }
 EXPORTS = tuple(_PROTOS)
@@ -461,6 +469,28 @@ def dp_gated_backward_workspace_bytes(dt, rows, d, f, d_out) -> int:
 
 def dp_gated_backward(dy, w_down, d_out, gate, up, dt, rows, d, f, w_gate, w_up, act, dgate, dup, dx, ws=None, stream=None) -> None:
     _call("dp_gated_backward", dy, w_down, d_out, gate, up, dt, rows, d, f, w_gate, w_up, act, dgate, dup, dx, ws, _nbytes(ws), stream)
+
+
+def muon_tensors(tensors: Sequence) -> "C.Array[dp_muon_tensor]":
+    """tensors: sequence of (param, grad, m, copy, rows, cols, weight_decay, scale)."""
+    arr = (dp_muon_tensor * len(tensors))()
+    for k, (param, grad, m, copy, *rest) in enumerate(tensors):
+        arr[k] = dp_muon_tensor(_ptr(param), _ptr(grad), _ptr(m), _ptr(copy), *rest)
+    return arr
+
+
+def dp_muon_workspace_bytes(tensors) -> int:
+    arr = tensors if isinstance(tensors, C.Array) else muon_tensors(tensors)
+    return lib.dp_muon_workspace_bytes(arr, len(arr))
+
+
+def dp_muon_multi(tensors, grad_dt, copy_dt, lr, beta, nesterov, grad_scale, eps, coefficients, ws, stream=None) -> None:
+    """coefficients: sequence of (a, b, c), or a ctypes array of them one behind the other."""
+    arr = tensors if isinstance(tensors, C.Array) else muon_tensors(tensors)
+    abc = coefficients
+    if not isinstance(abc, C.Array):
+        abc = (C.c_double * (3 * len(coefficients)))(*[x for row in coefficients for x in row])
+    _call("dp_muon_multi", arr, len(arr), grad_dt, copy_dt, lr, beta, int(nesterov), grad_scale, eps, abc, len(abc) // 3, ws, _nbytes(ws), stream)
 
 
 def dp_clipped_grad_tile_order(d_in: int, d_out: int):

@@ -398,3 +398,44 @@ class GatedFeedForward:
         ws, stream = self._scratch((rows, dx is None), stream, dp.dp_gated_backward_workspace_bytes, self.dt, rows, self.d, self.f, self.d_out)
         dp.dp_gated_backward(dy, self.w_down, self.d_out, gate, up, self.dt, rows, self.d, self.f, *self.weights, self.act, dgate, dup, dx, ws,
                              stream)
+
+
+class Muon:
+    """Matrices whose update is orthogonalised before it is taken.  param, momentum: [rows, cols] float32; grad: one type; copy: 16-bit tensors that
+    take the new parameters, or None; decay: a factor for each matrix, or one for all; scale: likewise, of the update (None: 0.2 times
+    the root of the longer side, an AdamW update's size).  The tensors are held: their addresses go to the library."""
+
+    COEFFICIENTS = ((3.4445, -4.7750, 2.0315),) * 5
+
+    def __init__(self, param: Sequence, grad: Sequence, momentum: Sequence, decay, copy: Optional[Sequence] = None, scale=None):
+        n = len(param)
+        if scale is None:
+            scale = [0.2 * math.sqrt(max(p.shape)) if p.dim() == 2 else 0.0 for p in param]
+        decay, scale = ([float(x)] * n if isinstance(x, (int, float)) else list(x) for x in (decay, scale))
+        if n == 0 or any(len(x) != n for x in (grad, momentum, decay, scale)) or (copy is not None and len(copy) != n):
+            raise ValueError("lists of one length, of a matrix at least")
+        self.grad_dt = _dtype(grad[0])
+        self.copy_dt = _dtype(copy[0]) if copy is not None else dp.DP_F32
+        if copy is not None and self.copy_dt == dp.DP_F32:
+            raise TypeError("copy: 16-bit tensors")
+        self.device, self.index = param[0].device, param[0].get_device()
+        self.held = list(zip(param, grad, momentum, copy if copy is not None else [None] * n))
+        kinds = (torch.float32, grad[0].dtype, torch.float32, copy[0].dtype if copy is not None else None)
+        for tensors in self.held:
+            if tensors[0].dim() != 2:
+                raise ValueError(f"param: matrices, not {tuple(tensors[0].shape)}")
+            for name, t, kind in zip(("param", "grad", "momentum", "copy"), tensors, kinds):
+                _same(name, t, tensors[0].shape, kind, self.device)
+        if self.index < 0:
+            raise ValueError(f"tensors on a GPU, not {self.device}")
+        self.tensors = dp.muon_tensors([(*t, *t[0].shape, d, x) for t, d, x in zip(self.held, decay, scale)])
+        self._ws, self._need = _Workspaces(), dp.dp_muon_workspace_bytes(self.tensors)
+        if self._need == 0:
+            raise ValueError("sizes that the library does not take")
+
+    def step(self, lr: float, beta: float = 0.95, nesterov: bool = True, grad_scale: float = 1.0, coefficients=COEFFICIENTS, eps: float = 1e-7,
+             stream=None) -> None:
+        """grad_scale: what makes the gradient's sum over samples a mean; coefficients: (a, b, c) of each iteration X <- a X + b A X + c A^2 X."""
+        stream = dp._stream(stream)
+        ws = self._ws(self._need, self.device, self.index, stream)
+        dp.dp_muon_multi(self.tensors, self.grad_dt, self.copy_dt, lr, beta, nesterov, grad_scale, eps, coefficients, ws, stream)

@@ -67,6 +67,7 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) gated_tile_kerne
   p.M = a.rows;
   p.N = PASS == kInput ? a.d : a.f;
   p.K = PASS == kForward ? a.d : PASS == kHidden ? a.d_out : a.f;
+  p.terms = p.K;
   p.lda = p.K;
   p.ldb = PASS == kForward ? p.N : p.K;
   p.segments = PASS == kInput ? 2 : 1;

@@ -1,0 +1,371 @@
+// An optimizer step on matrices whose update is orthogonalised:
+//   m = beta m + g,  u = g + beta m (or m),  X = u / (|u| + eps);  so many times  X <- (a + b A + c A^2) X,  A = X X';
+//   param = keep param - rate X.
+// X is taken with its shorter side as rows (turned on the way in and out), so A is the smaller square.
+//
+// Products as exact as fp32's at the rate of 16-bit ones: a value v is kept as two fp16 numbers, h = fp16(2^12 v) and l = fp16(2^12 v - h),
+// together within 2^-23 of v (2^-37 of 1 where v is next to nothing), and h h' + h l' + l h' are three segments of one contraction in fp32; l l',
+// 2^-24 of it, is left out.  2^12 keeps the halves of entries from 2^-15 up out of fp16's subnormal range; entries are bounded by singular
+// values, which the host has followed through the polynomials.  (fp32 matrix instructions have 1/16 of the 16-bit rate, a third of it 1/3.)
+// A, the square and the polynomial of A are symmetric: tiles on and above the diagonal are formed, and leave turned as well.
+// Matrices travel together: a launch does one step of up to 40 of them.
+#include <math.h>
+
+#include <algorithm>
+
+#include "muon.h"
+#include "piece.h"
+#include "product.h"
+
+namespace dpbk {
+
+namespace {
+
+constexpr int kThreads = 256, kSide = 64;            // elementwise passes: squares of 64 x 64
+constexpr float kScale = 4096.f;
+
+struct Matrix {
+  float* param;
+  const void* grad;
+  float* momentum;
+  void* copy;
+  _Float16 *x[2], *gram, *poly;                      // [2 (h, l)][m][n or m, to multiples of 8]
+  int rows, cols;
+  float keep, rate;
+  int parts;                                         // partial sums of |u|^2, at `partial`
+  unsigned begin;                                    // first workgroup
+  float* partial;
+};
+struct Group {
+  int n;
+  float beta, ahead, grad_scale, eps;
+  float a, b, c;
+  int from;                                          // x[from] is X, x[1 - from] what comes of it
+  Matrix t[kMuonGroup];
+};
+
+__host__ __device__ inline int eights(int n) { return (n + 7) & ~7; }
+__host__ __device__ inline int64_t part_values(int64_t size) {
+  const int64_t per = (size + kMuonParts - 1) / kMuonParts;
+  return per < 4096 ? 4096 : (per + 1023) / 1024 * 1024;
+}
+
+// The matrix that owns workgroup `id`; whole waves call.
+__device__ __forceinline__ int owner(const Group& g, unsigned id) {
+  static_assert(kMuonGroup <= 64, "a lane to a matrix");
+  const int lane = threadIdx.x & 63;
+  const unsigned begin = g.t[lane < g.n ? lane : 0].begin;
+  return __builtin_amdgcn_readfirstlane(__builtin_popcountll(__ballot(lane < g.n && begin <= id)) - 1);
+}
+
+__device__ __forceinline__ float block_sum(float x, float* red) {
+  for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
+  __syncthreads();
+  float s = 0.f;
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) s += red[w];
+  return s;
+}
+
+// m = beta m + g, and a part's sum of u^2.  Bound by memory.
+template <int DT>
+__global__ void __launch_bounds__(kThreads) muon_momentum_kernel(const Group g) {
+  __shared__ float red[kThreads / 64];
+  const Matrix& t = g.t[owner(g, blockIdx.x)];
+  const int part = blockIdx.x - t.begin;
+  const int64_t size = (int64_t)t.rows * t.cols, per = part_values(size), first = part * per, end = first + per < size ? first + per : size;
+  float sum = 0.f;
+  for (int64_t i = first + threadIdx.x; i < end; i += kThreads) {
+    Values<DT, 1> v;
+    v.load(t.grad, i);
+    const float grad = v.get(0) * g.grad_scale, m = fmaf(g.beta, t.momentum[i], grad);
+    t.momentum[i] = m;
+    const float u = g.ahead < 0.f ? m : fmaf(g.ahead, m, grad);
+    sum = fmaf(u, u, sum);
+  }
+  sum = block_sum(sum, red);
+  if (threadIdx.x == 0) t.partial[part] = sum;
+}
+
+struct Halves {
+  _Float16 h, l;
+  __device__ __forceinline__ explicit Halves(float v) : h((_Float16)v), l((_Float16)(v - (float)h)) {}
+};
+
+// A square of X = u / (|u| + eps), turned where the matrix is higher than wide; zeros behind its columns.
+template <int DT>
+__global__ void __launch_bounds__(kThreads) muon_start_kernel(const Group g) {
+  __shared__ float red[kThreads / 64], tile[kSide][kSide + 1];
+  const Matrix& t = g.t[owner(g, blockIdx.x)];
+  const bool turned = t.rows > t.cols;
+  const int m = turned ? t.cols : t.rows, n = turned ? t.rows : t.cols, pitch = eights(n), across = (pitch + kSide - 1) / kSide;
+  float sum = 0.f;
+  for (int i = threadIdx.x; i < t.parts; i += kThreads) sum += t.partial[i];
+  const float norm = sqrtf(block_sum(sum, red)) + g.eps;            // (0: all of u is, and X with it)
+  const int id = blockIdx.x - t.begin, r0 = id / across * kSide, c0 = (id - id / across * across) * kSide;       // of X
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  auto value = [&](int64_t i) {
+    Values<DT, 1> v;
+    v.load(t.grad, i);
+    const float m1 = t.momentum[i];
+    return g.ahead < 0.f ? m1 : fmaf(g.ahead, m1, v.get(0) * g.grad_scale);
+  };
+  for (int k = wave; k < kSide; k += kThreads / 64) {            // rows of the matrix as it lies
+    const int row = (turned ? c0 : r0) + k, col = (turned ? r0 : c0) + lane;
+    tile[k][lane] = row < t.rows && col < t.cols ? value((int64_t)row * t.cols + col) : 0.f;
+  }
+  __syncthreads();
+  _Float16* const x = t.x[g.from];
+  for (int k = wave; k < kSide; k += kThreads / 64) {
+    const int r = r0 + k, c = c0 + lane;
+    if (r < m && c < pitch) {
+      const float u = turned ? tile[lane][k] : tile[k][lane];
+      const Halves v(norm == 0.f ? 0.f : u / norm * kScale);
+      x[(int64_t)r * pitch + c] = v.h;
+      x[(int64_t)(m + r) * pitch + c] = v.l;
+    }
+  }
+}
+
+// param = keep param - rate X, and its 16-bit copy.
+template <int DT>                                    // of the copy; DP_F32: none
+__global__ void __launch_bounds__(kThreads) muon_apply_kernel(const Group g) {
+  __shared__ float tile[kSide][kSide + 1];
+  const Matrix& t = g.t[owner(g, blockIdx.x)];
+  const bool turned = t.rows > t.cols;
+  const int m = turned ? t.cols : t.rows, n = turned ? t.rows : t.cols, pitch = eights(n), across = (n + kSide - 1) / kSide;
+  const int id = blockIdx.x - t.begin, r0 = id / across * kSide, c0 = (id - id / across * across) * kSide;       // of X
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const _Float16* const x = t.x[g.from];
+  for (int k = wave; k < kSide; k += kThreads / 64) {
+    const int r = r0 + k, c = c0 + lane;
+    if (r < m && c < n) tile[k][lane] = ((float)x[(int64_t)r * pitch + c] + (float)x[(int64_t)(m + r) * pitch + c]) * (1.f / kScale);
+  }
+  __syncthreads();
+  for (int k = wave; k < kSide; k += kThreads / 64) {
+    const int row = (turned ? c0 : r0) + k, col = (turned ? r0 : c0) + lane;
+    if (row < t.rows && col < t.cols) {
+      const int64_t at = (int64_t)row * t.cols + col;
+      const float w = fmaf(t.keep, t.param[at], -t.rate * (turned ? tile[lane][k] : tile[k][lane]));
+      t.param[at] = w;
+      if constexpr (DT != DP_F32) {
+        Values<DT, 1> v;
+        v.set({w});
+        v.store(t.copy, at);
+      }
+    }
+  }
+}
+
+enum MuonStep { kGram, kPoly, kUpdate };
+
+// Tiles of one step.  Symmetric results: tile row by tile row from the diagonal on.
+template <int STEP, class S>
+__global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) muon_product_kernel(const Group g, int total) {
+  extern __shared__ __attribute__((aligned(1024))) unsigned char lds_raw[];
+  const unsigned lds0 = (unsigned)(uintptr_t)lds_raw;
+  const int logical = grad_logical_tile(blockIdx.x, total);
+  const Matrix& t = g.t[owner(g, logical)];
+  const int m = imin(t.rows, t.cols), n = imax(t.rows, t.cols), mp = eights(m), np = eights(n);
+  const int tiles_m = (m + S::BM - 1) / S::BM;
+  int tm, tn, rest = logical - (int)t.begin;
+  if constexpr (STEP == kUpdate) {
+    grad_tile_of(tiles_m, (np + S::BN - 1) / S::BN, rest, tm, tn);
+  } else {
+    for (tm = 0; rest >= tiles_m - tm; ++tm) rest -= tiles_m - tm;
+    tn = tm + rest;
+  }
+  const int m0 = tm * S::BM, n0[2] = {tn * S::BN, tn * S::BN + (STEP == kUpdate ? S::BN / 2 : 0)};
+  const _Float16 *a, *b;
+  ProductShape p;
+  p.M = m;
+  p.segments = 3;
+  if constexpr (STEP == kGram) {
+    a = b = t.x[g.from];
+    p.N = m;
+    p.K = p.lda = p.ldb = np;
+  } else if constexpr (STEP == kPoly) {
+    a = b = t.gram;
+    p.N = m;
+    p.K = p.lda = p.ldb = mp;
+  } else {
+    a = t.poly;
+    b = t.x[g.from];
+    p.N = p.ldb = np;
+    p.K = p.lda = mp;
+  }
+  p.terms = m;
+  const _Float16 *al = a + (int64_t)m * p.lda, *bl = b + (int64_t)m * p.ldb;
+  p.s[0] = {a, b, b};
+  p.s[1] = {a, bl, bl};
+  p.s[2] = {al, b, b};
+  f32x16 acc[S::TM][S::TN];
+  product_tile<S, true>(p, m0, n0, lds0, acc);
+  _Float16* const out = STEP == kGram ? t.gram : STEP == kPoly ? t.poly : t.x[1 - g.from];
+  const int pitch = STEP == kUpdate ? np : mp;
+  auto put = [&](int row, int col, const float (&v)[8]) {
+    f16x8 h, l;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const Halves w(v[k]);
+      h[k] = w.h;
+      l[k] = w.l;
+    }
+    *reinterpret_cast<f16x8*>(out + (int64_t)row * pitch + col) = h;
+    *reinterpret_cast<f16x8*>(out + (int64_t)(m + row) * pitch + col) = l;
+  };
+  // what is stored of eight values of the product
+  auto finish = [&](int row, int col, const float (&acc8)[8], float (&v)[8]) {
+    if constexpr (STEP == kPoly) {
+      const f16x8 h = *reinterpret_cast<const f16x8*>(t.gram + (int64_t)row * mp + col);
+      const f16x8 l = *reinterpret_cast<const f16x8*>(t.gram + (int64_t)(m + row) * mp + col);
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        v[k] = fmaf(g.c / kScale, acc8[k], g.b * ((float)h[k] + (float)l[k])) + (row == col + k ? g.a * kScale : 0.f);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = acc8[k] * (1.f / kScale);
+    }
+  };
+  auto store = [&](int row, int col, int set, const float (&acc8)[2][8]) {
+    const int r = m0 + row, c = n0[set] + col;
+    if (r >= m || c >= pitch) return;
+    float v[8];
+    finish(r, c, acc8[0], v);
+    put(r, c, v);
+  };
+  if constexpr (STEP == kUpdate) {
+    product_rows<S, false>(acc, lds0, store);
+  } else {
+    // below the diagonal: rows of the tile's columns
+    auto across = [&](int row, int col, const float (&acc8)[8]) {
+      const int r = n0[0] + col, c = m0 + row;
+      if (r >= m || c >= mp) return;
+      float v[8];
+      finish(r, c, acc8, v);
+      put(r, c, v);
+    };
+    product_rows<S, false>(acc, lds0, store, tm != tn, across);
+  }
+}
+
+template <class F>
+unsigned lay_out(Group& g, F workgroups) {
+  unsigned total = 0;
+  for (int i = 0; i < g.n; ++i) {
+    g.t[i].begin = total;
+    total += (unsigned)workgroups(g.t[i]);
+  }
+  return total;
+}
+
+template <int STEP, int SIDE>
+int64_t tiles_of(const Matrix& t) {
+  const int64_t m = std::min(t.rows, t.cols), n = eights(std::max(t.rows, t.cols)), tm = (m + SIDE - 1) / SIDE;
+  return STEP == kUpdate ? tm * ((n + SIDE - 1) / SIDE) : tm * (tm + 1) / 2;
+}
+
+template <int STEP, class S>
+dp_status launch_product(Group& g, hipStream_t s) {
+  static ReadyTable ready;
+  const dp_status st = allow_big_lds(muon_product_kernel<STEP, S>, S::LDS_BYTES, ready);
+  if (st != DP_OK) return st;
+  const unsigned total = lay_out(g, [](const Matrix& t) { return tiles_of<STEP, S::BM>(t); });
+  muon_product_kernel<STEP, S><<<dim3(total), S::NT, S::LDS_BYTES, s>>>(g, (int)total);
+  return hip_status(hipGetLastError());
+}
+
+// Large tiles where they come in whole rounds, as elsewhere.
+template <int STEP>
+dp_status launch_step(Group& g, hipStream_t s) {
+  constexpr bool COLUMNS = STEP == kUpdate;
+  int64_t big = 0, mid = 0;
+  for (int i = 0; i < g.n; ++i) {
+    big += tiles_of<STEP, 256>(g.t[i]);
+    mid += tiles_of<STEP, 128>(g.t[i]);
+  }
+  const bool large = (big + kBigRound - 1) / kBigRound * kBigRoundCost <= (mid + kMidRound - 1) / kMidRound * kMidRoundCost;
+  return large ? launch_product<STEP, BigProduct<COLUMNS>>(g, s) : launch_product<STEP, MidProduct<COLUMNS>>(g, s);
+}
+
+// Bytes of a matrix's two X, A, polynomial and partial sums.
+size_t matrix_bytes(int rows, int cols, size_t (&at)[5]) {
+  const int64_t m = std::min(rows, cols), n = std::max(rows, cols);
+  const size_t x = (size_t)4 * m * eights((int)n), square = (size_t)4 * m * eights((int)m), sizes[5] = {x, x, square, square, kMuonParts * 4};
+  size_t total = 0;
+  for (int i = 0; i < 5; ++i) {
+    at[i] = total;
+    total += (sizes[i] + 255) / 256 * 256;
+  }
+  return total;
+}
+
+}  // namespace
+
+size_t muon_workspace(const MuonTensor* tensors, int n) {
+  size_t total = 0, at[5];
+  for (int i = 0; i < n; ++i) total += matrix_bytes(tensors[i].rows, tensors[i].cols, at);
+  return total;
+}
+
+dp_status launch_muon(const MuonTensor* tensors, int n, const MuonArgs& a, dp_dtype grad_dt, dp_dtype copy_dt, void* ws, hipStream_t s) {
+  Group g = {};
+  g.n = n;
+  g.beta = a.beta;
+  g.ahead = a.ahead;
+  g.grad_scale = a.grad_scale;
+  g.eps = a.eps;
+  char* base = static_cast<char*>(ws);
+  for (int i = 0; i < g.n; ++i) {
+    const MuonTensor& from = tensors[i];
+    Matrix& t = g.t[i];
+    size_t at[5];
+    const size_t bytes = matrix_bytes(from.rows, from.cols, at);
+    t.param = from.param;
+    t.grad = from.grad;
+    t.momentum = from.momentum;
+    t.copy = from.copy;
+    t.rows = from.rows;
+    t.cols = from.cols;
+    t.keep = from.keep;
+    t.rate = from.rate;
+    t.x[0] = reinterpret_cast<_Float16*>(base + at[0]);
+    t.x[1] = reinterpret_cast<_Float16*>(base + at[1]);
+    t.gram = reinterpret_cast<_Float16*>(base + at[2]);
+    t.poly = reinterpret_cast<_Float16*>(base + at[3]);
+    t.partial = reinterpret_cast<float*>(base + at[4]);
+    const int64_t size = (int64_t)t.rows * t.cols;
+    t.parts = (int)((size + part_values(size) - 1) / part_values(size));
+    base += bytes;
+  }
+  auto launch = [&](auto kernel, unsigned total) {
+    kernel<<<dim3(total), kThreads, 0, s>>>(g);
+    return hip_status(hipGetLastError());
+  };
+  unsigned total = lay_out(g, [](const Matrix& t) { return t.parts; });
+  dp_status st = launch(grad_dt == DP_F32 ? muon_momentum_kernel<DP_F32> : grad_dt == DP_BF16 ? muon_momentum_kernel<DP_BF16> : muon_momentum_kernel<DP_F16>, total);
+  if (st != DP_OK) return st;
+  auto squares = [](const Matrix& t, bool padded) {
+    const int64_t m = std::min(t.rows, t.cols), c = std::max(t.rows, t.cols);
+    return ((m + kSide - 1) / kSide) * (((padded ? eights((int)c) : c) + kSide - 1) / kSide);
+  };
+  total = lay_out(g, [&](const Matrix& t) { return squares(t, true); });
+  st = launch(grad_dt == DP_F32 ? muon_start_kernel<DP_F32> : grad_dt == DP_BF16 ? muon_start_kernel<DP_BF16> : muon_start_kernel<DP_F16>, total);
+  for (int k = 0; k < a.iterations && st == DP_OK; ++k) {
+    g.a = (float)a.coefficients[3 * k];
+    g.b = (float)a.coefficients[3 * k + 1];
+    g.c = (float)a.coefficients[3 * k + 2];
+    st = launch_step<kGram>(g, s);
+    if (st == DP_OK) st = launch_step<kPoly>(g, s);
+    if (st == DP_OK) st = launch_step<kUpdate>(g, s);
+    g.from = 1 - g.from;
+  }
+  if (st != DP_OK) return st;
+  total = lay_out(g, [&](const Matrix& t) { return squares(t, false); });
+  st = launch(copy_dt == DP_F32 ? muon_apply_kernel<DP_F32> : copy_dt == DP_BF16 ? muon_apply_kernel<DP_BF16> : muon_apply_kernel<DP_F16>, total);
+  if (st != DP_OK) return st;
+  return DP_OK;
+}
+
+}  // namespace dpbk

@@ -13,6 +13,8 @@
 // The first operand of an instruction is B's: a lane has one row of the result and four adjacent columns to a register quad.
 #pragma once
 
+#include <type_traits>
+
 #include "dp_internal.h"
 #include "lds_dma.h"
 #include "tile_order.h"
@@ -24,6 +26,7 @@ struct ProductSegment {
 };
 struct ProductShape {
   int M, N, K;                      // K: of a segment; K and N (columns) are multiples of 8
+  int terms;                        // columns: rows of B that are there (K or fewer: A has zeros beyond)
   int lda, ldb;                     // elements from one row (of columns: term) to the next
   int segments;
   ProductSegment s[3];
@@ -104,7 +107,7 @@ __device__ __forceinline__ void product_tile(const ProductShape& p, int m0, cons
   };
   auto open_block = [&]() {                                        // columns: terms p_k .. of the segment that are there
     if constexpr (S::COLUMNS) {
-      const unsigned n = p_seg < p.segments ? (unsigned)imin(p.K - p_k, BK) * b_pitch : 0;
+      const unsigned n = p_seg < p.segments ? (unsigned)imax(imin(p.terms - p_k, BK), 0) * b_pitch : 0;
       rb[0][2] = rb[1][2] = (int)n;
     }
   };
@@ -215,9 +218,14 @@ __device__ __forceinline__ void product_tile(const ProductShape& p, int m0, cons
 }
 
 // acc's rows to store(row of the tile, first column, values): columns 8 at a time, of both sets where PAIRS (v[0] and v[1]), else of one
-// fragment (v[0]).  The wave's 32 rows at a time are turned in LDS, so that whole rows leave.
-template <class S, bool PAIRS, class Store>
-__device__ __forceinline__ void product_rows(const f32x16 (&acc)[S::TM][S::TN], unsigned lds0, Store store) {
+// fragment (v[0]).  The wave's 32 rows at a time are turned in LDS, so that whole rows leave.  across(first row, column, values): the same
+// by columns, rows 8 at a time, where `mirror`.
+struct NoMirror {
+  __device__ void operator()(int, int, const float (&)[8]) const {}
+};
+template <class S, bool PAIRS, class Store, class Across = NoMirror>
+__device__ __forceinline__ void product_rows(const f32x16 (&acc)[S::TM][S::TN], unsigned lds0, Store store, bool mirror = false,
+                                             Across across = {}) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / S::WN * S::WTM, wc = wave % S::WN;
   const unsigned slab = lds0 + wave * S::SLAB_BYTES;
@@ -249,6 +257,16 @@ __device__ __forceinline__ void product_rows(const f32x16 (&acc)[S::TM][S::TN], 
       // column within a set, or within the tile
       const int col = S::COLUMNS ? 32 * wc + c % 32 : 64 * wc + c;
       store(wm + 32 * x + r, col, S::COLUMNS && !PAIRS ? c / 32 : 0, v);
+    }
+    if (!std::is_same_v<Across, NoMirror> && mirror) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          v[e] = *(__attribute__((address_space(3))) const float*)(uintptr_t)(slab + 4 * ((8 * i + e) * S::SLAB_PITCH + lane));
+        across(wm + 32 * x + 8 * i, 64 * wc + lane, v);
+      }
     }
   }
 }

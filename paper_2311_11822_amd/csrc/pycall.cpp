@@ -169,7 +169,8 @@ PyObject* set_torch(PyObject*, PyObject* module) {
   X(dp_head_norm) \
   X(dp_head_norm_backward) \
   X(dp_gated) \
-  X(dp_gated_backward)
+  X(dp_gated_backward) \
+  X(dp_muon_multi)
 #else
 #define DP_MODULE _pycall
 #define DP_CALLS(X) \

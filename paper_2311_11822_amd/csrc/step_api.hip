@@ -6,6 +6,7 @@
 
 #include "gated.h"
 #include "heads.h"
+#include "muon.h"
 
 using namespace dpbk;
 
@@ -93,6 +94,52 @@ dp_status gated_shape(dp_dtype dt, int rows, int d, int f, int d_out) {
   return DP_OK;
 }
 bool act_ok(dp_activation act) { return act >= DP_ACT_SILU && act <= DP_ACT_SIGMOID; }
+
+// Matrices of a step, as far as their sizes go.
+dp_status muon_sizes(const dp_muon_tensor* tensors, int n) {
+  if (!tensors || n <= 0) return DP_ERR_INVALID_ARG;
+  for (int i = 0; i < n; ++i) {
+    const int rows = tensors[i].rows, cols = tensors[i].cols;
+    if (rows <= 0 || cols <= 0) return DP_ERR_INVALID_ARG;
+    if (rows > kMuonMostSide || cols > kMuonMostSide || std::min(rows, cols) > kMuonMostShort) return DP_ERR_UNSUPPORTED;
+  }
+  return n <= 1 << 20 ? DP_OK : DP_ERR_UNSUPPORTED;
+}
+
+// The matrices in even runs of as many as travel together; weight decay and scale where the launcher wants what comes of them.
+template <class F>
+dp_status muon_runs(const dp_muon_tensor* tensors, int n, F run) {
+  const int runs = (n + kMuonGroup - 1) / kMuonGroup, per = (n + runs - 1) / runs;
+  MuonTensor t[kMuonGroup];
+  for (int first = 0; first < n; first += per) {
+    const int count = std::min(n, first + per) - first;
+    for (int i = 0; i < count; ++i) {
+      const dp_muon_tensor& from = tensors[first + i];
+      t[i] = {from.param, from.grad, from.m, from.copy, from.rows, from.cols, from.weight_decay, from.scale};
+    }
+    const dp_status st = run(t, count);
+    if (st != DP_OK) return st;
+  }
+  return DP_OK;
+}
+
+// Where singular values from [0, 1] go under x <- a x + b x^3 + c x^5: x, x^2 and a + b x^2 + c x^4 stay within what two halves hold.
+bool muon_values_fit(const double* abc, int iterations) {
+  double most = 1.;
+  for (int k = 0; k < iterations; ++k) {
+    const double a = abc[3 * k], b = abc[3 * k + 1], c = abc[3 * k + 2];
+    if (!isfinite(a) || !isfinite(b) || !isfinite(c) || most * most > kMuonMost) return false;
+    double next = 0., poly = 0.;
+    for (int i = 0; i <= 4096; ++i) {
+      const double x = most * i / 4096., s = x * x, p = a + s * (b + c * s);
+      poly = std::max(poly, fabs(p));
+      next = std::max(next, fabs(x * p));
+    }
+    if (poly > kMuonMost || next > kMuonMost) return false;
+    most = next * 1.001;                               // between the points
+  }
+  return true;
+}
 
 }  // namespace
 
@@ -241,6 +288,46 @@ dp_status dp_gated_backward(const void* dy, const void* w_down, int d_out, const
   a.f = f;
   a.act = act;
   return launch_gated_backward(a, dt, static_cast<hipStream_t>(stream));
+}
+
+size_t dp_muon_workspace_bytes(const dp_muon_tensor* tensors, int n_tensors) {
+  if (muon_sizes(tensors, n_tensors) != DP_OK) return 0;
+  size_t most = 0;
+  muon_runs(tensors, n_tensors, [&](const MuonTensor* run, int n) {
+    most = std::max(most, muon_workspace(run, n));
+    return DP_OK;
+  });
+  return most;
+}
+
+dp_status dp_muon_multi(const dp_muon_tensor* tensors, int n_tensors, dp_dtype grad_dt, dp_dtype copy_dt, double lr, double beta, int nesterov,
+                        double grad_scale, double eps, const double* coefficients, int iterations, void* ws, size_t ws_bytes, void* stream) {
+  if (!dtype_ok(grad_dt) || !dtype_ok(copy_dt) || !coefficients || iterations < 1 || iterations > 32) return DP_ERR_INVALID_ARG;
+  if (nesterov != 0 && nesterov != 1) return DP_ERR_INVALID_ARG;
+  if (!(lr >= 0.) || isinf(lr) || !(beta >= 0. && beta < 1.) || !(eps >= 0.) || isinf(eps) || !isfinite(grad_scale)) return DP_ERR_INVALID_ARG;
+  dp_status st = muon_sizes(tensors, n_tensors);
+  if (st != DP_OK) return st;
+  const uintptr_t grad_size = grad_dt == DP_F32 ? 4 : 2;
+  for (int i = 0; i < n_tensors; ++i) {
+    const dp_muon_tensor& t = tensors[i];
+    if (!t.param || !t.grad || !t.m || !aligned(t.param, 4) || !aligned(t.grad, grad_size) || !aligned(t.m, 4)) return DP_ERR_INVALID_ARG;
+    if (copy_dt != DP_F32 && (!t.copy || !aligned(t.copy, 2))) return DP_ERR_INVALID_ARG;
+    if (!isfinite(t.weight_decay) || !isfinite(t.scale)) return DP_ERR_INVALID_ARG;
+  }
+  if (!muon_values_fit(coefficients, iterations)) return DP_ERR_UNSUPPORTED;
+  if (!ws || ws_bytes < dp_muon_workspace_bytes(tensors, n_tensors)) return DP_ERR_WORKSPACE;
+  if (!aligned(ws, 16)) return DP_ERR_INVALID_ARG;
+  MuonArgs a = {};
+  a.beta = (float)beta;
+  a.ahead = nesterov ? (float)beta : -1.f;
+  a.grad_scale = (float)grad_scale;
+  a.eps = (float)eps;
+  a.iterations = iterations;
+  a.coefficients = coefficients;
+  return muon_runs(tensors, n_tensors, [&](MuonTensor* run, int n) {
+    for (int i = 0; i < n; ++i) run[i].keep = (float)(1. - lr * (double)run[i].keep), run[i].rate = (float)(lr * (double)run[i].rate);
+    return launch_muon(run, n, a, grad_dt, copy_dt, ws, static_cast<hipStream_t>(stream));
+  });
 }
 
 }  // extern "C"

@@ -362,3 +362,84 @@ def test_gated_gradient_by_differences(block):
             return (h.double() * dh.double()).sum().item()
         n = dx.double().norm().item()
         assert abs(along(loss, x.double(), dx.double() / n, 2.0 ** -5) - n) <= 2e-3 * n
+
+
+# ------------------------------------------------------------------------------------------------ orthogonalised updates
+
+ABC = [(3.4445, -4.7750, 2.0315)] * 5
+
+
+def orthogonal(u, eps=1e-7, abc=ABC):
+    x = u / (u.norm() + eps)
+    turned = x.shape[0] > x.shape[1]
+    x = x.t() if turned else x
+    for a, b, c in abc:
+        gram = x @ x.t()
+        x = a * x + b * (gram @ x) + c * (gram @ (gram @ x))
+    return x.t() if turned else x
+
+
+def muon_tolerance(shape):
+    """Of X against its norm.  Entries are kept within 2^-23 of their size, products' sums within FP32.  Five iterations multiply what a
+    direction next to no singular value is off by 3.4445^5 = 485 at most (what later ones add, by less: 1.41 times as much in all), of a matrix
+    that starts with norm 1 and ends with about the root of its shorter side; then fifteen products' own."""
+    return 1.41 * 485 * 2.0 ** -23 / min(shape) ** 0.5 + 8 * FP32
+
+
+MUON_SHAPES = [[(1, 1)], [(1, 40), (40, 1), (2, 3)], [(16, 16), (24, 72), (72, 24), (65, 24), (24, 65)], [(128, 128), (129, 127), (127, 300), (260, 140)],
+               [(520, 300), (256, 1030)], [(33, 2000)] * 3 + [(2000, 33)] * 2, [(8, 9 + i) for i in range(83)], [(1300, 1100)], [(700, 2600)] * 14]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("shapes", MUON_SHAPES, ids=lambda s: f"{len(s)}x{s[0]}")
+def test_muon(block, dtype, shapes):
+    gen = torch.Generator().manual_seed(len(shapes) + shapes[0][0])
+    some = sorted({0, len(shapes) // 2, len(shapes) - 1})          # those that the reference forms
+    offset = 3                                                      # of no alignment but the elements' own
+    make = lambda kind, scale: [(torch.randn(math.prod(s) + offset, generator=gen) * scale).to(kind).cuda()[offset:].view(s) for s in shapes]  # noqa: E731
+    param, grad, momentum = make(torch.float32, 0.02), make(DTYPES[dtype], 1.0), make(torch.float32, 0.5)
+    copy = make(torch.bfloat16, 0.0)
+    w0, g0, m0 = ([x[i].cpu().double() for i in some] for x in (param, grad, momentum))
+    opt = block.Muon(param, grad, momentum, 0.1, copy, 0.5)
+    for nesterov in (True, False):
+        opt.step(0.1, 0.9, nesterov, 0.25, ABC)
+        for k, i in enumerate(some):
+            g = 0.25 * g0[k]
+            m0[k] = 0.9 * m0[k] + g
+            assert rel(momentum[i], m0[k]) <= FP32
+            x = orthogonal(g + 0.9 * m0[k] if nesterov else m0[k])
+            want = w0[k] * (1 - 0.1 * 0.1) - 0.1 * 0.5 * x
+            off = (param[i].cpu().double() - want).norm()
+            assert off <= 0.05 * muon_tolerance(shapes[i]) * x.norm() + FP32 * want.norm(), (shapes[i], off / x.norm() / 0.05, muon_tolerance(shapes[i]))
+            assert torch.equal(copy[i], param[i].bfloat16())
+            w0[k], m0[k] = param[i].cpu().double(), momentum[i].cpu().double()
+
+
+def test_muon_wide_range_and_special_values(block):
+    """Singular values over six decades; a zero update; what is not a number stays in its matrix."""
+    gen = torch.Generator().manual_seed(9)
+    q = torch.linalg.qr(torch.randn((96, 96), generator=gen, dtype=torch.float64))[0]
+    v = torch.linalg.qr(torch.randn((200, 96), generator=gen, dtype=torch.float64))[0]
+    wide = (q * 10.0 ** torch.linspace(0, -6, 96, dtype=torch.float64)) @ v.t()
+    grads = [wide.float(), torch.zeros(20, 30), torch.full((9, 9), math.nan), 1e15 * torch.eye(16)]
+    dev = [g.cuda() for g in grads]
+    param, momentum = ([torch.zeros_like(g) for g in dev] for _ in range(2))
+    block.Muon(param, dev, momentum, 0.0, scale=1.0).step(1.0, 0.5, eps=1e-35)
+    want = -orthogonal(grads[0].double() * 1.5, 1e-35)
+    assert (param[0].cpu().double() - want).norm() <= muon_tolerance((96, 200)) * 96 ** 0.5
+    assert (param[1] == 0).all()
+    assert torch.isnan(param[2]).all()
+    assert rel(param[3], -orthogonal(torch.eye(16, dtype=torch.float64))) <= muon_tolerance((16, 16))
+
+
+def test_muon_other_polynomials(block):
+    """One iteration, and different ones in turn; the cubic x (3 - x^2) / 2 alone."""
+    gen = torch.Generator().manual_seed(4)
+    g = torch.randn((40, 56), generator=gen)
+    for abc in ([(1.5, -0.5, 0.0)], [(1.5, -0.5, 0.0)] * 12, [(4.0, -6.0, 2.5), (2.0, -1.5, 0.5), (1.875, -1.25, 0.375)]):
+        param, momentum = torch.zeros_like(g, device="cuda"), torch.zeros_like(g, device="cuda")
+        block.Muon([param], [g.cuda()], [momentum], 0.0, scale=1.0).step(1.0, 0.0, False, coefficients=abc)
+        want = -orthogonal(g.double(), abc=abc)
+        # the smallest singular value's direction grows by the product of the a's at most
+        grown = math.prod(a for a, _, _ in abc)
+        assert (param.cpu().double() - want).norm() <= (1.5 * min(grown, 500) * 2.0 ** -23 + 3 * len(abc) * FP32) * max(1.0, want.norm().item())
