@@ -4,10 +4,12 @@
 // its own origin, which is how a gate and its factor meet in one lane).
 //  * 256 x 256 tiles by eight waves of 128 x 64, or 128 x 128 by four of 64 x 64 (two workgroups to a compute unit).  Accumulators and
 //    operands of one k-step and the next lie in registers.
-//  * memory -> LDS without registers (16 bytes a lane), five stages of 32 terms, one barrier to a stage: in iteration i a wave waits for its
-//    own loads of block i + 1, meets the others, asks for block i + 4 into the place of block i - 1, and multiplies block i.
-//  * LDS holds [m][32 k] in rows of 64 bytes: a 128-bit read takes sixteen lanes at a time, here sixteen rows at one place of four, so that
-//    place is XORed with row / 4 and all banks are met.  [k][n] halves have rows of 256 or 128 bytes; the transposing read takes four
+//  * memory -> LDS without registers (16 bytes a lane), two stages of 64 terms: whole 128-byte lines of [m][k] rows.  (Stages of 32, five of
+//    them, took each line in two halves a microsecond apart, and through the first-level cache twice: 4096 x 65536 x 12288 6050 us.)
+//    One barrier to a stage, before its last k-step: the next stage has landed, and the last operands of this one are in registers, so
+//    that its place is free; the loads of the stage after the next go out within that k-step and have three more to land.
+//  * LDS holds [m][64 k] in rows of 128 bytes: a 128-bit read takes sixteen lanes at a time, here sixteen rows at one place of eight, so that
+//    place is XORed with row / 2 and all banks are met.  [k][n] halves have rows of 256 or 128 bytes; the transposing read takes four
 //    rows of 64 bytes at a time, which the XOR by k spreads over the four groups of banks.
 //  * rows, columns and terms past the end arrive as zeros: by the descriptor's size, or by an offset past it.
 // The first operand of an instruction is B's: a lane has one row of the result and four adjacent columns to a register quad.
@@ -32,44 +34,44 @@ struct ProductShape {
   ProductSegment s[3];
 };
 
-template <int BM_, int WM_, int WN_, int NSTAGE_, bool COLUMNS_>
+template <int BM_, int WM_, int WN_, bool COLUMNS_>
 struct ProductTile {
-  static constexpr int BM = BM_, BN = BM_, BK = 32, NSTAGE = NSTAGE_, WM = WM_, WN = WN_, NW = WM * WN, NT = 64 * NW;
+  static constexpr int BM = BM_, BN = BM_, BK = 64, NSTAGE = 2, WM = WM_, WN = WN_, NW = WM * WN, NT = 64 * NW;
   static constexpr bool COLUMNS = COLUMNS_;
   static constexpr int WTM = BM / WM, TM = WTM / 32, TN = 2;
   static constexpr int ROW_BYTES = 2 * BK, A_BYTES = BM * ROW_BYTES, B_BYTES = BN * ROW_BYTES, STAGE_BYTES = A_BYTES + B_BYTES;
   static constexpr int HALF_BYTES = B_BYTES / 2, COL_BYTES = BN;               // a term's columns of one set
-  static constexpr int LDS_BYTES = NSTAGE * STAGE_BYTES, LOADS = 2;            // of an operand, wave and block
+  static constexpr int LDS_BYTES = NSTAGE * STAGE_BYTES, LOADS = 4;            // of an operand, wave and stage
   // epilogue: a wave's 32 rows of 64 columns, fp32
   static constexpr int SLAB_PITCH = 68, SLAB_BYTES = 32 * SLAB_PITCH * 4;
   static_assert(BN / WN == 64 && LOADS * NW * 1024 == A_BYTES && NW * SLAB_BYTES <= LDS_BYTES, "load split, fragments, epilogue");
 };
 template <bool COLUMNS>
-using BigProduct = ProductTile<256, 2, 4, 5, COLUMNS>;
+using BigProduct = ProductTile<256, 2, 4, COLUMNS>;
 template <bool COLUMNS>
-using MidProduct = ProductTile<128, 2, 2, 5, COLUMNS>;
+using MidProduct = ProductTile<128, 2, 2, COLUMNS>;
 
 // The tile at (m0, n0) (columns: of either set n0[0], n0[1]) into acc.  acc[x][y], lane, register r: row 32 x + lane % 32 of the wave's, column
 // 8 (r / 4) + 4 (lane / 32) + r % 4 of its fragment y: column 32 (wave % WN) of set y, or 64 (wave % WN) + 32 y of the tile.
 template <class S, bool F16>
 __device__ __forceinline__ void product_tile(const ProductShape& p, int m0, const int (&n0)[2], unsigned lds0, f32x16 (&acc)[S::TM][S::TN]) {
-  constexpr int NSTAGE = S::NSTAGE, BLOCK_LOADS = 2 * S::LOADS, BK = S::BK;
+  constexpr int BK = S::BK;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
   // ---- memory -> LDS
-  const int chunk = (lane & 3) ^ ((lane >> 4) & 3);                // 16-byte piece of a row's 32 terms
+  const int chunk = (lane & 7) ^ ((4 * (wave & 1) + (lane >> 4)) & 7);         // 16-byte piece of a row's 64 terms
   const unsigned a_pitch = 2u * p.lda, b_pitch = 2u * p.ldb;
   unsigned va[S::LOADS], vb[S::LOADS];
 #pragma unroll
   for (int l = 0; l < S::LOADS; ++l) {
-    const unsigned row = 16 * (l * S::NW + wave) + (lane >> 2);
+    const unsigned row = 8 * (l * S::NW + wave) + (lane >> 3);
     va[l] = row * a_pitch + chunk * 16;
     if constexpr (S::COLUMNS) {
       constexpr int PIECES = S::COL_BYTES / 16;
-      const unsigned k = wave * (1024 / S::COL_BYTES) + lane / PIECES, at = lane % PIECES;
+      const unsigned k = ((l & 1) * S::NW + wave) * (1024 / S::COL_BYTES) + lane / PIECES, at = lane % PIECES;
       const unsigned c = S::COL_BYTES == 256 ? at ^ ((k & 3) << 2) : at ^ ((k & 2) << 1);
-      const int col = n0[l] + 8 * (int)c;
+      const int col = n0[l >> 1] + 8 * (int)c;
       vb[l] = col < p.N ? k * b_pitch + 2u * col : OOB;
     } else {
       vb[l] = row * b_pitch + chunk * 16;
@@ -79,7 +81,7 @@ __device__ __forceinline__ void product_tile(const ProductShape& p, int m0, cons
   const unsigned b_bytes = S::COLUMNS ? 0 : (unsigned)imax(imin(p.N - n0[0], S::BN), 0) * b_pitch;
   const unsigned lds_ld = lds0 + wave * 1024;
   i32x4 ra, rb[2];
-  int p_seg = 0, p_k = 0, p_stage = 0;                             // of the block to ask for next
+  int p_seg = 0, p_k = 0, p_stage = 0;                             // of the stage to ask for next; its place
   auto scalar = [](i32x4 r) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_readfirstlane(r[i]);
@@ -111,18 +113,17 @@ __device__ __forceinline__ void product_tile(const ProductShape& p, int m0, cons
       rb[0][2] = rb[1][2] = (int)n;
     }
   };
-  auto prefetch = [&](int l) {
-    const unsigned k = (unsigned)p_k;
-    const bool in = p_k + 8 * chunk < p.K;
-    const unsigned to = lds_ld + p_stage * S::STAGE_BYTES;
-    load_to_lds(scalar(ra), in ? va[l] : OOB, 2 * k, to + l * S::NW * 1024);
+  auto prefetch_a = [&](int l) {
+    load_to_lds(scalar(ra), p_k + 8 * chunk < p.K ? va[l] : OOB, 2u * p_k, lds_ld + p_stage + l * S::NW * 1024);
+  };
+  auto prefetch_b = [&](int l) {
     if constexpr (S::COLUMNS)
-      load_to_lds(scalar(rb[l]), vb[l], 0, to + S::A_BYTES + l * S::HALF_BYTES);
+      load_to_lds(scalar(rb[l >> 1]), vb[l], 0, lds_ld + p_stage + S::A_BYTES + l * S::NW * 1024);
     else
-      load_to_lds(scalar(rb[0]), in ? vb[l] : OOB, 2 * k, to + S::A_BYTES + l * S::NW * 1024);
+      load_to_lds(scalar(rb[0]), p_k + 8 * chunk < p.K ? vb[l] : OOB, 2u * p_k, lds_ld + p_stage + S::A_BYTES + l * S::NW * 1024);
   };
   auto prefetch_advance = [&]() {
-    p_stage = p_stage + 1 == NSTAGE ? 0 : p_stage + 1;
+    p_stage = S::STAGE_BYTES - p_stage;
     p_k += BK;
     if constexpr (S::COLUMNS) {
 #pragma unroll
@@ -141,10 +142,10 @@ __device__ __forceinline__ void product_tile(const ProductShape& p, int m0, cons
   };
 
   // ---- LDS -> operands
-  const int row = lane & 31, sw = (row >> 2) & 3, wm = wave / S::WN * S::WTM, wc = wave % S::WN;
-  unsigned a_rd[2], b_rd[2];
+  const int row = lane & 31, sw = (row >> 1) & 7, wm = wave / S::WN * S::WTM, wc = wave % S::WN;
+  unsigned a_rd[4], b_rd[4];
 #pragma unroll
-  for (int ks = 0; ks < 2; ++ks) {
+  for (int ks = 0; ks < 4; ++ks) {
     const unsigned place = (unsigned)((2 * ks + (lane >> 5)) ^ sw) << 4;
     a_rd[ks] = lds0 + (wm + row) * S::ROW_BYTES + place;
     if constexpr (S::COLUMNS) {
@@ -180,38 +181,52 @@ __device__ __forceinline__ void product_tile(const ProductShape& p, int m0, cons
   };
   constexpr int ITEMS = S::TM + S::TN, STEPS = S::TM * S::TN;
 
-  const int blocks = p.segments * ((p.K + BK - 1) / BK);
+  const int stages = p.segments * ((p.K + BK - 1) / BK);
   open_segment();
   open_block();
-#pragma unroll 1
-  for (int q = 0; q < NSTAGE - 1; ++q) {
-    prefetch(0);
-    prefetch(1);
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+#pragma unroll
+    for (int l = 0; l < S::LOADS; ++l) {
+      prefetch_a(l);
+      prefetch_b(l);
+    }
     prefetch_advance();
+    if (q == 0) asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
   }
-  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((NSTAGE - 2) * BLOCK_LOADS) : "memory");
 #pragma unroll
   for (int q = 0; q < ITEMS; ++q) read_frag(0, q, 0, 0);
   unsigned c_base = 0;
-  for (int kb = 0; kb < blocks; ++kb) {
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((NSTAGE - 3) * BLOCK_LOADS) : "memory");
-    DP_PIN();
-    unsigned n_base = c_base + S::STAGE_BYTES == S::LDS_BYTES ? 0 : c_base + S::STAGE_BYTES;
-    asm("" : "+s"(c_base), "+s"(n_base));
+  for (int st = 0; st < stages; ++st) {
+    asm("" : "+s"(c_base));
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
+    for (int ks = 0; ks < 4; ++ks) {
+      if (ks == 3) {                                               // the next stage is there, this one's operands are in registers
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        c_base = S::STAGE_BYTES - c_base;
+        asm("" : "+s"(c_base));
+      }
+      DP_PIN();
 #pragma unroll
       for (int slot = 0; slot < STEPS; ++slot) {
         const int x = slot / S::TN, y = slot % S::TN;
-        acc[x][y] = mfma16<F16>(fb[ks][y].v, fa[ks][x].v, acc[x][y]);
+        acc[x][y] = mfma16<F16>(fb[ks & 1][y].v, fa[ks & 1][x].v, acc[x][y]);
         DP_PIN();
-        if (slot < ITEMS) read_frag(ks ^ 1, slot, ks ? n_base : c_base, ks ^ 1);
-        if (slot == STEPS - 2) prefetch(ks);
-        if (slot == STEPS - 1 && ks == 1) prefetch_advance();
+        if (slot < ITEMS) read_frag(~ks & 1, slot, c_base, (ks + 1) & 3);
+        if (ks == 3) {
+          constexpr int PER = 2 * S::LOADS / STEPS;
+#pragma unroll
+          for (int e = slot * PER; e < slot * PER + PER; ++e) {
+            if (e & 1)
+              prefetch_b(e >> 1);
+            else
+              prefetch_a(e >> 1);
+          }
+          if (slot == STEPS - 1) prefetch_advance();
+        }
         DP_PIN();
       }
     }
-    c_base = n_base;
   }
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");      // loads past the end
   __syncthreads();
