@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) gated_tile_kerne
   int tm, tn;
   grad_tile_of(tiles_m, tiles_n, grad_logical_tile(blockIdx.x, tiles_m * tiles_n), tm, tn);
   const int m0 = tm * S::BM, n = tn * (S::COLUMNS ? S::BN / 2 : S::BN), n0[2] = {n, n};
-  f32x16 acc[S::TM][S::TN];
+  f32x4 acc[S::TM][S::TN];
   product_tile<S, DT == DP_F16>(p, m0, n0, lds0, acc);
   product_rows<S, PASS == kForward>(acc, lds0, [&](int row, int col, int, const float (&v)[2][8]) {
     if (m0 + row >= p.M || n + col >= p.N) return;

@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) muon_product_ker
   p.s[0] = {a, b, b};
   p.s[1] = {a, bl, bl};
   p.s[2] = {al, b, b};
-  f32x16 acc[S::TM][S::TN];
+  f32x4 acc[S::TM][S::TN];
   product_tile<S, true>(p, m0, n0, lds0, acc);
   _Float16* const out = STEP == kGram ? t.gram : STEP == kPoly ? t.poly : t.x[1 - g.from];
   const int pitch = STEP == kUpdate ? np : mp;

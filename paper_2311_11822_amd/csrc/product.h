@@ -38,12 +38,16 @@ template <int BM_, int WM_, int WN_, bool COLUMNS_>
 struct ProductTile {
   static constexpr int BM = BM_, BN = BM_, BK = 64, NSTAGE = 2, WM = WM_, WN = WN_, NW = WM * WN, NT = 64 * NW;
   static constexpr bool COLUMNS = COLUMNS_;
-  static constexpr int WTM = BM / WM, TM = WTM / 32, TN = 2;
+  static constexpr int WTM = BM / WM, TM = WTM / 16, TN = 4;                   // 16 x 16 results of a wave
   static constexpr int ROW_BYTES = 2 * BK, A_BYTES = BM * ROW_BYTES, B_BYTES = BN * ROW_BYTES, STAGE_BYTES = A_BYTES + B_BYTES;
   static constexpr int HALF_BYTES = B_BYTES / 2, COL_BYTES = BN;               // a term's columns of one set
   static constexpr int LDS_BYTES = NSTAGE * STAGE_BYTES, LOADS = 4;            // of an operand, wave and stage
   // epilogue: a wave's 32 rows of 64 columns, fp32
   static constexpr int SLAB_PITCH = 68, SLAB_BYTES = 32 * SLAB_PITCH * 4;
+  // columns: the 16-byte place of a term's row is XORed with this
+  __device__ static constexpr unsigned spread(unsigned k) {
+    return COL_BYTES == 256 ? (k & 3) << 2 | (k >> 2 & 2) : (k & 2) << 1 | (k >> 2 & 2);
+  }
   static_assert(BN / WN == 64 && LOADS * NW * 1024 == A_BYTES && NW * SLAB_BYTES <= LDS_BYTES, "load split, fragments, epilogue");
 };
 template <bool COLUMNS>
@@ -51,10 +55,10 @@ using BigProduct = ProductTile<256, 2, 4, COLUMNS>;
 template <bool COLUMNS>
 using MidProduct = ProductTile<128, 2, 2, COLUMNS>;
 
-// The tile at (m0, n0) (columns: of either set n0[0], n0[1]) into acc.  acc[x][y], lane, register r: row 32 x + lane % 32 of the wave's, column
-// 8 (r / 4) + 4 (lane / 32) + r % 4 of its fragment y: column 32 (wave % WN) of set y, or 64 (wave % WN) + 32 y of the tile.
+// The tile at (m0, n0) (columns: of either set n0[0], n0[1]) into acc.  acc[x][y], lane, register r: row 16 x + lane % 16 of the wave's, column
+// 16 y + 4 (lane / 16) + r of its 64: those of the tile from 64 (wave % WN) on, or 32 of each set from 32 (wave % WN) on.
 template <class S, bool F16>
-__device__ __forceinline__ void product_tile(const ProductShape& p, int m0, const int (&n0)[2], unsigned lds0, f32x16 (&acc)[S::TM][S::TN]) {
+__device__ __forceinline__ void product_tile(const ProductShape& p, int m0, const int (&n0)[2], unsigned lds0, f32x4 (&acc)[S::TM][S::TN]) {
   constexpr int BK = S::BK;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -70,7 +74,7 @@ __device__ __forceinline__ void product_tile(const ProductShape& p, int m0, cons
     if constexpr (S::COLUMNS) {
       constexpr int PIECES = S::COL_BYTES / 16;
       const unsigned k = ((l & 1) * S::NW + wave) * (1024 / S::COL_BYTES) + lane / PIECES, at = lane % PIECES;
-      const unsigned c = S::COL_BYTES == 256 ? at ^ ((k & 3) << 2) : at ^ ((k & 2) << 1);
+      const unsigned c = at ^ S::spread(k);
       const int col = n0[l >> 1] + 8 * (int)c;
       vb[l] = col < p.N ? k * b_pitch + 2u * col : OOB;
     } else {
@@ -142,17 +146,16 @@ __device__ __forceinline__ void product_tile(const ProductShape& p, int m0, cons
   };
 
   // ---- LDS -> operands
-  const int row = lane & 31, sw = (row >> 1) & 7, wm = wave / S::WN * S::WTM, wc = wave % S::WN;
-  unsigned a_rd[4], b_rd[4];
+  const int row = lane & 15, wm = wave / S::WN * S::WTM, wc = wave % S::WN;
+  unsigned a_rd[2], b_rd[2];
 #pragma unroll
-  for (int ks = 0; ks < 4; ++ks) {
-    const unsigned place = (unsigned)((2 * ks + (lane >> 5)) ^ sw) << 4;
+  for (int ks = 0; ks < 2; ++ks) {
+    const unsigned place = (unsigned)((4 * ks + (lane >> 4)) ^ (row >> 1)) << 4;
     a_rd[ks] = lds0 + (wm + row) * S::ROW_BYTES + place;
     if constexpr (S::COLUMNS) {
-      const int blk = lane >> 4, s = lane & 15, k = 8 * (blk >> 1) + (s >> 2);
-      const unsigned c = (unsigned)(32 * wc + 16 * (blk & 1) + 4 * (s & 3)) >> 3;
-      const unsigned at = S::COL_BYTES == 256 ? c ^ ((k & 3) << 2) : c ^ ((k & 2) << 1);
-      b_rd[ks] = lds0 + S::A_BYTES + (16 * ks + k) * S::COL_BYTES + (at << 4) + 8 * (s & 1);
+      const int k = 8 * (lane >> 4) + (row >> 2);
+      const unsigned c = (unsigned)(32 * wc + 4 * (row & 3)) >> 3;
+      b_rd[ks] = lds0 + S::A_BYTES + (32 * ks + k) * S::COL_BYTES + ((c ^ S::spread(k)) << 4) + 8 * (row & 1);
     } else {
       b_rd[ks] = lds0 + S::A_BYTES + (64 * wc + row) * S::ROW_BYTES + place;
     }
@@ -160,26 +163,22 @@ __device__ __forceinline__ void product_tile(const ProductShape& p, int m0, cons
 #pragma unroll
   for (int x = 0; x < S::TM; ++x)
 #pragma unroll
-    for (int y = 0; y < S::TN; ++y)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[x][y][r] = 0.f;
-  Frag fa[2][S::TM], fb[2][S::TN];
+    for (int y = 0; y < S::TN; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+  // B's operands of a k-step of 32 and the next; A's, each used by four instructions in a row, AHEAD of their use.
+  constexpr int AHEAD = 3;
+  Frag fa[4], fb[2][S::TN];
   typedef __attribute__((address_space(3))) const bf16x8* Lds;
-  // Items of a k-step's operands in the order in which its matrix instructions need them: B 0, A 0, B 1, A 1 ...
-  auto read_frag = [&](int buf, int q, unsigned base, int ks) {
-    const bool is_b = q == 0 || q == 2;
-    const int i = is_b ? q >> 1 : q == 1 ? 0 : q - 2;
-    if (!is_b) {
-      fa[buf][i].v = *(Lds)(uintptr_t)(a_rd[ks] + base + i * 32 * S::ROW_BYTES);
-    } else if constexpr (S::COLUMNS) {
-      const unsigned at = b_rd[ks] + base + i * S::HALF_BYTES;
-      fb[buf][i].h[0] = lds_read_tr(at);
-      fb[buf][i].h[1] = lds_read_tr(at + 4 * S::COL_BYTES);
+  auto read_a = [&](int x, unsigned base, int ks) { fa[x & 3].v = *(Lds)(uintptr_t)(a_rd[ks] + base + x * 16 * S::ROW_BYTES); };
+  auto read_b = [&](int y, unsigned base, int ks) {
+    if constexpr (S::COLUMNS) {
+      // the second 16 columns of a set: two places on, which the XOR (of bit 1, by k, too) turns into two places back
+      const unsigned at = ((b_rd[ks] + base) ^ ((y & 1) << 5)) + (y >> 1) * S::HALF_BYTES;
+      fb[ks][y].h[0] = lds_read_tr(at);
+      fb[ks][y].h[1] = lds_read_tr(at + 4 * S::COL_BYTES);
     } else {
-      fb[buf][i].v = *(Lds)(uintptr_t)(b_rd[ks] + base + i * 32 * S::ROW_BYTES);
+      fb[ks][y].v = *(Lds)(uintptr_t)(b_rd[ks] + base + y * 16 * S::ROW_BYTES);
     }
   };
-  constexpr int ITEMS = S::TM + S::TN, STEPS = S::TM * S::TN;
 
   const int stages = p.segments * ((p.K + BK - 1) / BK);
   open_segment();
@@ -195,36 +194,45 @@ __device__ __forceinline__ void product_tile(const ProductShape& p, int m0, cons
     if (q == 0) asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
   }
 #pragma unroll
-  for (int q = 0; q < ITEMS; ++q) read_frag(0, q, 0, 0);
+  for (int y = 0; y < S::TN; ++y) read_b(y, 0, 0);
+#pragma unroll
+  for (int x = 0; x < AHEAD; ++x) read_a(x, 0, 0);
   unsigned c_base = 0;
   for (int st = 0; st < stages; ++st) {
     asm("" : "+s"(c_base));
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) {
-      if (ks == 3) {                                               // the next stage is there, this one's operands are in registers
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        c_base = S::STAGE_BYTES - c_base;
-        asm("" : "+s"(c_base));
-      }
-      DP_PIN();
+    for (int ks = 0; ks < 2; ++ks) {
 #pragma unroll
-      for (int slot = 0; slot < STEPS; ++slot) {
-        const int x = slot / S::TN, y = slot % S::TN;
-        acc[x][y] = mfma16<F16>(fb[ks & 1][y].v, fa[ks & 1][x].v, acc[x][y]);
-        DP_PIN();
-        if (slot < ITEMS) read_frag(~ks & 1, slot, c_base, (ks + 1) & 3);
-        if (ks == 3) {
-          constexpr int PER = 2 * S::LOADS / STEPS;
-#pragma unroll
-          for (int e = slot * PER; e < slot * PER + PER; ++e) {
-            if (e & 1)
-              prefetch_b(e >> 1);
-            else
-              prefetch_a(e >> 1);
-          }
-          if (slot == STEPS - 1) prefetch_advance();
+      for (int x = 0; x < S::TM; ++x) {
+        constexpr int TURN = S::TM - AHEAD;                        // from here on operands of the next k-step
+        if (ks == 1 && x == TURN) {                                // the next stage is there, this one's operands are in registers
+          asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+          c_base = S::STAGE_BYTES - c_base;
+          asm("" : "+s"(c_base));
         }
         DP_PIN();
+#pragma unroll
+        for (int y = 0; y < S::TN; ++y) {
+          acc[x][y] = mfma16<F16>(fb[ks][y].v, fa[x & 3].v, acc[x][y]);
+          DP_PIN();
+          const int k_next = x >= TURN ? ks ^ 1 : ks;
+          if (y == 0) read_a((x + AHEAD) % S::TM, c_base, k_next);
+          // B's of the next k-step, four of them over the last AHEAD rows
+          if (x >= TURN && (y == 1 || (y == 2 && x == TURN))) read_b(x - TURN + (y == 1 ? (x > TURN) : 1), c_base, ks ^ 1);
+          if (ks == 1 && x >= TURN) {
+            constexpr int SLOTS = AHEAD * S::TN, LOADS = 2 * S::LOADS;
+            const int slot = (x - TURN) * S::TN + y;
+#pragma unroll
+            for (int e = slot * LOADS / SLOTS; e < (slot + 1) * LOADS / SLOTS; ++e) {
+              if (e & 1)
+                prefetch_b(e >> 1);
+              else
+                prefetch_a(e >> 1);
+            }
+            if (slot == SLOTS - 1) prefetch_advance();
+          }
+          DP_PIN();
+        }
       }
     }
   }
@@ -239,22 +247,20 @@ struct NoMirror {
   __device__ void operator()(int, int, const float (&)[8]) const {}
 };
 template <class S, bool PAIRS, class Store, class Across = NoMirror>
-__device__ __forceinline__ void product_rows(const f32x16 (&acc)[S::TM][S::TN], unsigned lds0, Store store, bool mirror = false,
+__device__ __forceinline__ void product_rows(const f32x4 (&acc)[S::TM][S::TN], unsigned lds0, Store store, bool mirror = false,
                                              Across across = {}) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / S::WN * S::WTM, wc = wave % S::WN;
   const unsigned slab = lds0 + wave * S::SLAB_BYTES;
   typedef __attribute__((address_space(3))) f32x4* Lds;
 #pragma unroll
-  for (int x = 0; x < S::TM; ++x) {
+  for (int x = 0; x < S::TM / 2; ++x) {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-    for (int y = 0; y < S::TN; ++y)
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const f32x4 v = {acc[x][y][4 * g], acc[x][y][4 * g + 1], acc[x][y][4 * g + 2], acc[x][y][4 * g + 3]};
-        *(Lds)(uintptr_t)(slab + 4 * ((lane & 31) * S::SLAB_PITCH + 32 * y + 8 * g + 4 * (lane >> 5))) = v;
-      }
+      for (int y = 0; y < S::TN; ++y)
+        *(Lds)(uintptr_t)(slab + 4 * ((16 * h + (lane & 15)) * S::SLAB_PITCH + 16 * y + 4 * (lane >> 4))) = acc[2 * x + h][y];
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     constexpr int LANES = PAIRS ? 4 : 8, PASSES = 32 * LANES / 64;
 #pragma unroll
