@@ -24,7 +24,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
 # and the 256 accumulators move to scratch memory.
 # Where the packed rows' loop begins in memory moves the narrow tiles by 5 % (24 layers 768 x 16, 512 x 32 tokens: 257 us at a
 # multiple of 64 bytes, up to 272 elsewhere).
-PER_FILE_FLAGS = {"grad_gemm.hip": ["-mllvm", "-pragma-unroll-threshold=1000000"], "grad_packed.hip": ["-falign-loops=64"]}
+PER_FILE_FLAGS = {"grad_gemm.hip": ["-mllvm", "-pragma-unroll-threshold=1000000"], "gated_tiles.hip": ["-mllvm", "-pragma-unroll-threshold=1000000"], "grad_packed.hip": ["-falign-loops=64"]}
 
 
 def build(verbose: bool = False) -> str:

@@ -4,10 +4,11 @@
 // its own origin, which is how a gate and its factor meet in one lane).
 //  * 256 x 256 tiles by eight waves of 128 x 64, or 128 x 128 by four of 64 x 64 (two workgroups to a compute unit).  Accumulators and
 //    operands of one k-step and the next lie in registers.
-//  * memory -> LDS without registers (16 bytes a lane), two stages of 64 terms: whole 128-byte lines of [m][k] rows.  (Stages of 32, five of
-//    them, took each line in two halves a microsecond apart, and through the first-level cache twice: 4096 x 65536 x 12288 6050 us.)
-//    One barrier to a stage, before its last k-step: the next stage has landed, and the last operands of this one are in registers, so
-//    that its place is free; the loads of the stage after the next go out within that k-step and have three more to land.
+//  * memory -> LDS without registers (16 bytes a lane), stages of 64 terms: whole 128-byte lines of [m][k] rows.  (Stages of 32, five of
+//    them, took each line in two halves a microsecond apart, and through the first-level cache twice: 4096 x 65536 x 12288 6050 us, two stages of
+//    64 with these instructions 5020.)  A has three places in LDS and B two, all of it: B's of a stage is free once its operands are in
+//    registers, half a stage before A's, so B's loads have 1.4 stages to land and A's two.
+//    Two barriers to a stage of the large tiles: M, behind the last read of B; E, behind the last one of A, where the next stage has landed.
 //  * LDS holds [m][64 k] in rows of 128 bytes: a 128-bit read takes sixteen lanes at a time, here sixteen rows at one place of eight, so that
 //    place is XORed with row / 2 and all banks are met.  [k][n] halves have rows of 256 or 128 bytes; the transposing read takes four
 //    rows of 64 bytes at a time, which the XOR by k spreads over the four groups of banks.
@@ -36,19 +37,20 @@ struct ProductShape {
 
 template <int BM_, int WM_, int WN_, bool COLUMNS_>
 struct ProductTile {
-  static constexpr int BM = BM_, BN = BM_, BK = 64, NSTAGE = 2, WM = WM_, WN = WN_, NW = WM * WN, NT = 64 * NW;
+  static constexpr int BM = BM_, BN = BM_, BK = 64, A_PLACES = 3, B_PLACES = 2, WM = WM_, WN = WN_, NW = WM * WN, NT = 64 * NW;
   static constexpr bool COLUMNS = COLUMNS_;
-  static constexpr int WTM = BM / WM, TM = WTM / 16, TN = 4;                   // 16 x 16 results of a wave
-  static constexpr int ROW_BYTES = 2 * BK, A_BYTES = BM * ROW_BYTES, B_BYTES = BN * ROW_BYTES, STAGE_BYTES = A_BYTES + B_BYTES;
+  static constexpr int WTM = BM / WM, WTN = BN / WN, TM = WTM / 16, TN = WTN / 16;       // 16 x 16 results of a wave
+  static constexpr int ROW_BYTES = 2 * BK, A_BYTES = BM * ROW_BYTES, B_BYTES = BN * ROW_BYTES;
+  static constexpr int B_AT = A_PLACES * A_BYTES;                              // of B's first place
   static constexpr int HALF_BYTES = B_BYTES / 2, COL_BYTES = BN;               // a term's columns of one set
-  static constexpr int LDS_BYTES = NSTAGE * STAGE_BYTES, LOADS = 4;            // of an operand, wave and stage
-  // epilogue: a wave's 32 rows of 64 columns, fp32
-  static constexpr int SLAB_PITCH = 68, SLAB_BYTES = 32 * SLAB_PITCH * 4;
+  static constexpr int LDS_BYTES = B_AT + B_PLACES * B_BYTES, LOADS = A_BYTES / (NW * 1024);     // of an operand, wave and stage
+  // epilogue: 32 rows of a wave's columns, fp32
+  static constexpr int SLAB_PITCH = WTN + 4, SLAB_BYTES = 32 * SLAB_PITCH * 4;
   // columns: the 16-byte place of a term's row is XORed with this
   __device__ static constexpr unsigned spread(unsigned k) {
     return COL_BYTES == 256 ? (k & 3) << 2 | (k >> 2 & 2) : (k & 2) << 1 | (k >> 2 & 2);
   }
-  static_assert(BN / WN == 64 && LOADS * NW * 1024 == A_BYTES && NW * SLAB_BYTES <= LDS_BYTES, "load split, fragments, epilogue");
+  static_assert(LOADS * NW * 1024 == A_BYTES && LOADS % 2 == 0 && NW * SLAB_BYTES <= LDS_BYTES, "load split, fragments, epilogue");
 };
 template <bool COLUMNS>
 using BigProduct = ProductTile<256, 2, 4, COLUMNS>;
@@ -56,7 +58,7 @@ template <bool COLUMNS>
 using MidProduct = ProductTile<128, 2, 2, COLUMNS>;
 
 // The tile at (m0, n0) (columns: of either set n0[0], n0[1]) into acc.  acc[x][y], lane, register r: row 16 x + lane % 16 of the wave's, column
-// 16 y + 4 (lane / 16) + r of its 64: those of the tile from 64 (wave % WN) on, or 32 of each set from 32 (wave % WN) on.
+// 16 y + 4 (lane / 16) + r of its WTN: those of the tile from WTN (wave % WN) on, or half as many of each set.
 template <class S, bool F16>
 __device__ __forceinline__ void product_tile(const ProductShape& p, int m0, const int (&n0)[2], unsigned lds0, f32x4 (&acc)[S::TM][S::TN]) {
   constexpr int BK = S::BK;
@@ -73,9 +75,9 @@ __device__ __forceinline__ void product_tile(const ProductShape& p, int m0, cons
     va[l] = row * a_pitch + chunk * 16;
     if constexpr (S::COLUMNS) {
       constexpr int PIECES = S::COL_BYTES / 16;
-      const unsigned k = ((l & 1) * S::NW + wave) * (1024 / S::COL_BYTES) + lane / PIECES, at = lane % PIECES;
+      const unsigned k = (l % (S::LOADS / 2) * S::NW + wave) * (1024 / S::COL_BYTES) + lane / PIECES, at = lane % PIECES;
       const unsigned c = at ^ S::spread(k);
-      const int col = n0[l >> 1] + 8 * (int)c;
+      const int col = n0[l / (S::LOADS / 2)] + 8 * (int)c;
       vb[l] = col < p.N ? k * b_pitch + 2u * col : OOB;
     } else {
       vb[l] = row * b_pitch + chunk * 16;
@@ -85,50 +87,55 @@ __device__ __forceinline__ void product_tile(const ProductShape& p, int m0, cons
   const unsigned b_bytes = S::COLUMNS ? 0 : (unsigned)imax(imin(p.N - n0[0], S::BN), 0) * b_pitch;
   const unsigned lds_ld = lds0 + wave * 1024;
   i32x4 ra, rb[2];
-  int p_seg = 0, p_k = 0, p_stage = 0;                             // of the stage to ask for next; its place
+  struct Stream {                                                  // the stage to ask for next: segment, first term, place in LDS
+    int seg = 0, k = 0, place;
+  } pa, pb;
+  pa.place = 0;
+  pb.place = S::B_AT;
   auto scalar = [](i32x4 r) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_readfirstlane(r[i]);
     return r;
   };
-  auto open_segment = [&]() {
-    if (p_seg < p.segments) {
-      const auto pick = [&](const void* first, const void* second, const void* third) {        // (an index would put them in memory)
-        return p_seg == 0 ? first : p_seg == 1 ? second : third;
-      };
-      const ProductSegment s = {pick(p.s[0].a, p.s[1].a, p.s[2].a), pick(p.s[0].b0, p.s[1].b0, p.s[2].b0), pick(p.s[0].b1, p.s[1].b1, p.s[2].b1)};
-      ra = make_rsrc(static_cast<const char*>(s.a) + (uint64_t)m0 * a_pitch, a_bytes);
-      if constexpr (S::COLUMNS) {
-        rb[0] = make_rsrc(s.b0, 0);
-        rb[1] = make_rsrc(s.b1, 0);
-      } else {
-        rb[0] = make_rsrc(static_cast<const char*>(s.b0) + (uint64_t)n0[0] * b_pitch, b_bytes);
-      }
-    } else {
-      ra[2] = rb[0][2] = 0;
-    }
-    ra = scalar(ra);
-    rb[0] = scalar(rb[0]);
-    if constexpr (S::COLUMNS) rb[1] = scalar(rb[1]);
+  auto pick = [&](int seg, const void* first, const void* second, const void* third) {         // (an index would put them in memory)
+    return static_cast<const char*>(seg == 0 ? first : seg == 1 ? second : third);
   };
-  auto open_block = [&]() {                                        // columns: terms p_k .. of the segment that are there
+  auto open_a = [&]() {
+    ra = make_rsrc(pick(pa.seg, p.s[0].a, p.s[1].a, p.s[2].a) + (uint64_t)m0 * a_pitch, pa.seg < p.segments ? a_bytes : 0);
+  };
+  auto open_b = [&]() {
+    const char* const b0 = pick(pb.seg, p.s[0].b0, p.s[1].b0, p.s[2].b0);
     if constexpr (S::COLUMNS) {
-      const unsigned n = p_seg < p.segments ? (unsigned)imax(imin(p.terms - p_k, BK), 0) * b_pitch : 0;
-      rb[0][2] = rb[1][2] = (int)n;
+      rb[0] = make_rsrc(b0, 0);
+      rb[1] = make_rsrc(pick(pb.seg, p.s[0].b1, p.s[1].b1, p.s[2].b1), 0);
+    } else {
+      rb[0] = make_rsrc(b0 + (uint64_t)n0[0] * b_pitch, pb.seg < p.segments ? b_bytes : 0);
     }
+  };
+  auto open_terms = [&]() {                                        // columns: terms pb.k .. of the segment that are there
+    if constexpr (S::COLUMNS) rb[0][2] = rb[1][2] = (int)(pb.seg < p.segments ? (unsigned)imax(imin(p.terms - pb.k, BK), 0) * b_pitch : 0);
   };
   auto prefetch_a = [&](int l) {
-    load_to_lds(scalar(ra), p_k + 8 * chunk < p.K ? va[l] : OOB, 2u * p_k, lds_ld + p_stage + l * S::NW * 1024);
+    load_to_lds(scalar(ra), pa.k + 8 * chunk < p.K ? va[l] : OOB, 2u * pa.k, lds_ld + pa.place + l * S::NW * 1024);
   };
   auto prefetch_b = [&](int l) {
     if constexpr (S::COLUMNS)
-      load_to_lds(scalar(rb[l >> 1]), vb[l], 0, lds_ld + p_stage + S::A_BYTES + l * S::NW * 1024);
+      load_to_lds(scalar(rb[l / (S::LOADS / 2)]), vb[l], 0, lds_ld + pb.place + l * S::NW * 1024);
     else
-      load_to_lds(scalar(rb[0]), p_k + 8 * chunk < p.K ? vb[l] : OOB, 2u * p_k, lds_ld + p_stage + S::A_BYTES + l * S::NW * 1024);
+      load_to_lds(scalar(rb[0]), pb.k + 8 * chunk < p.K ? vb[l] : OOB, 2u * pb.k, lds_ld + pb.place + l * S::NW * 1024);
   };
-  auto prefetch_advance = [&]() {
-    p_stage = S::STAGE_BYTES - p_stage;
-    p_k += BK;
+  auto advance_a = [&]() {
+    pa.place = pa.place == 2 * S::A_BYTES ? 0 : pa.place + S::A_BYTES;
+    pa.k += BK;
+    if (pa.k >= p.K) {
+      ++pa.seg;
+      if (pa.seg < p.segments) pa.k = 0;
+      open_a();
+    }
+  };
+  auto advance_b = [&]() {
+    pb.place = 2 * S::B_AT + S::B_BYTES - pb.place;
+    pb.k += BK;
     if constexpr (S::COLUMNS) {
 #pragma unroll
       for (int l = 0; l < 2; ++l) {
@@ -137,12 +144,12 @@ __device__ __forceinline__ void product_tile(const ProductShape& p, int m0, cons
         rb[l][1] = (int)(uint32_t)(q >> 32);
       }
     }
-    if (p_k >= p.K) {
-      p_k = p_seg + 1 < p.segments ? 0 : p_k;
-      ++p_seg;
-      open_segment();
+    if (pb.k >= p.K) {
+      ++pb.seg;
+      if (pb.seg < p.segments) pb.k = 0;
+      open_b();
     }
-    open_block();
+    open_terms();
   };
 
   // ---- LDS -> operands
@@ -154,10 +161,10 @@ __device__ __forceinline__ void product_tile(const ProductShape& p, int m0, cons
     a_rd[ks] = lds0 + (wm + row) * S::ROW_BYTES + place;
     if constexpr (S::COLUMNS) {
       const int k = 8 * (lane >> 4) + (row >> 2);
-      const unsigned c = (unsigned)(32 * wc + 4 * (row & 3)) >> 3;
-      b_rd[ks] = lds0 + S::A_BYTES + (32 * ks + k) * S::COL_BYTES + ((c ^ S::spread(k)) << 4) + 8 * (row & 1);
+      const unsigned c = (unsigned)(S::WTN / 2 * wc + 4 * (row & 3)) >> 3;
+      b_rd[ks] = lds0 + S::B_AT + (32 * ks + k) * S::COL_BYTES + ((c ^ S::spread(k)) << 4) + 8 * (row & 1);
     } else {
-      b_rd[ks] = lds0 + S::A_BYTES + (64 * wc + row) * S::ROW_BYTES + place;
+      b_rd[ks] = lds0 + S::B_AT + (S::WTN * wc + row) * S::ROW_BYTES + place;
     }
   }
 #pragma unroll
@@ -171,8 +178,8 @@ __device__ __forceinline__ void product_tile(const ProductShape& p, int m0, cons
   auto read_a = [&](int x, unsigned base, int ks) { fa[x & 3].v = *(Lds)(uintptr_t)(a_rd[ks] + base + x * 16 * S::ROW_BYTES); };
   auto read_b = [&](int y, unsigned base, int ks) {
     if constexpr (S::COLUMNS) {
-      // the second 16 columns of a set: two places on, which the XOR (of bit 1, by k, too) turns into two places back
-      const unsigned at = ((b_rd[ks] + base) ^ ((y & 1) << 5)) + (y >> 1) * S::HALF_BYTES;
+      // 16 columns further within a set are two places, in bits that the lane's own place has as the XOR by k alone left them
+      const unsigned at = ((b_rd[ks] + base) ^ (y % (S::TN / 2) << 5)) + y / (S::TN / 2) * S::HALF_BYTES;
       fb[ks][y].h[0] = lds_read_tr(at);
       fb[ks][y].h[1] = lds_read_tr(at + 4 * S::COL_BYTES);
     } else {
@@ -181,55 +188,77 @@ __device__ __forceinline__ void product_tile(const ProductShape& p, int m0, cons
   };
 
   const int stages = p.segments * ((p.K + BK - 1) / BK);
-  open_segment();
-  open_block();
+  open_a();
+  open_b();
+  open_terms();
 #pragma unroll
-  for (int q = 0; q < 2; ++q) {
+  for (int q = 0; q < 5; ++q) {                                    // A 0, B 0, A 1, B 1, A 2
 #pragma unroll
     for (int l = 0; l < S::LOADS; ++l) {
-      prefetch_a(l);
-      prefetch_b(l);
+      if (q & 1)
+        prefetch_b(l);
+      else
+        prefetch_a(l);
     }
-    prefetch_advance();
-    if (q == 0) asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    if (q & 1)
+      advance_b();
+    else
+      advance_a();
   }
+  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(3 * S::LOADS) : "memory");
 #pragma unroll
   for (int y = 0; y < S::TN; ++y) read_b(y, 0, 0);
 #pragma unroll
   for (int x = 0; x < AHEAD; ++x) read_a(x, 0, 0);
-  unsigned c_base = 0;
+  // SPLIT: barriers M and E; else one, of both (small tiles: a few instructions lie between the two).
+  constexpr bool SPLIT = S::TM > 4;
+  constexpr int TURN = S::TM - AHEAD;                              // from this row on operands of the next k-step
+  unsigned a_base = 0, b_base = 0;
   for (int st = 0; st < stages; ++st) {
-    asm("" : "+s"(c_base));
+    asm("" : "+s"(a_base), "+s"(b_base));
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
 #pragma unroll
       for (int x = 0; x < S::TM; ++x) {
-        constexpr int TURN = S::TM - AHEAD;                        // from here on operands of the next k-step
-        if (ks == 1 && x == TURN) {                                // the next stage is there, this one's operands are in registers
-          asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-          c_base = S::STAGE_BYTES - c_base;
-          asm("" : "+s"(c_base));
+        if (SPLIT && ks == 1 && x == 1) asm volatile("s_waitcnt lgkmcnt(1)\n\ts_barrier" ::: "memory");      // one of A's is younger
+        if (ks == 1 && x == TURN) {
+          asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((SPLIT ? 2 : 1) * S::LOADS) : "memory");
+          a_base = a_base == 2 * S::A_BYTES ? 0 : a_base + S::A_BYTES;
+          b_base = S::B_BYTES - b_base;
+          asm("" : "+s"(a_base), "+s"(b_base));
         }
         DP_PIN();
 #pragma unroll
         for (int y = 0; y < S::TN; ++y) {
           acc[x][y] = mfma16<F16>(fb[ks][y].v, fa[x & 3].v, acc[x][y]);
           DP_PIN();
-          const int k_next = x >= TURN ? ks ^ 1 : ks;
-          if (y == 0) read_a((x + AHEAD) % S::TM, c_base, k_next);
-          // B's of the next k-step, four of them over the last AHEAD rows
-          if (x >= TURN && (y == 1 || (y == 2 && x == TURN))) read_b(x - TURN + (y == 1 ? (x > TURN) : 1), c_base, ks ^ 1);
+          if (y == 0) read_a((x + AHEAD) % S::TM, a_base, x >= TURN ? ks ^ 1 : ks);
+          constexpr int SLOTS = AHEAD * S::TN;
+          const int slot = (x - TURN) * S::TN + y;                 // of the last AHEAD rows
+          // B's of the next k-step, each behind an instruction that reads none of A's
+          if (x >= TURN && y != 0) {
+            const int from = (slot - (x - TURN) - 1) * S::TN / (SLOTS - AHEAD), to = (slot - (x - TURN)) * S::TN / (SLOTS - AHEAD);
+#pragma unroll
+            for (int b = from; b < to; ++b) read_b(b, b_base, ks ^ 1);
+          }
+          // loads: B's behind M (or E), A's behind E
+          if (SPLIT && ks == 1 && x >= 1 && x < 1 + S::LOADS && y == 2) {
+            prefetch_b(x - 1);
+            if (x == S::LOADS) advance_b();
+          }
           if (ks == 1 && x >= TURN) {
-            constexpr int SLOTS = AHEAD * S::TN, LOADS = 2 * S::LOADS;
-            const int slot = (x - TURN) * S::TN + y;
+            constexpr int LOADS = (SPLIT ? 1 : 2) * S::LOADS;
 #pragma unroll
             for (int e = slot * LOADS / SLOTS; e < (slot + 1) * LOADS / SLOTS; ++e) {
-              if (e & 1)
-                prefetch_b(e >> 1);
+              if (SPLIT || e >= S::LOADS)
+                prefetch_a(e % S::LOADS);
               else
-                prefetch_a(e >> 1);
+                prefetch_b(e);
             }
-            if (slot == SLOTS - 1) prefetch_advance();
+            if (slot == SLOTS - 1) {
+              if (!SPLIT) advance_b();
+              advance_a();
+            }
           }
           DP_PIN();
         }
@@ -262,7 +291,7 @@ __device__ __forceinline__ void product_rows(const f32x4 (&acc)[S::TM][S::TN], u
       for (int y = 0; y < S::TN; ++y)
         *(Lds)(uintptr_t)(slab + 4 * ((16 * h + (lane & 15)) * S::SLAB_PITCH + 16 * y + 4 * (lane >> 4))) = acc[2 * x + h][y];
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    constexpr int LANES = PAIRS ? 4 : 8, PASSES = 32 * LANES / 64;
+    constexpr int LANES = S::WTN / (PAIRS ? 16 : 8), PASSES = 32 * LANES / 64;
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) {
       const int r = i * (64 / LANES) + lane / LANES, c = 8 * (lane % LANES);
@@ -271,22 +300,24 @@ __device__ __forceinline__ void product_rows(const f32x4 (&acc)[S::TM][S::TN], u
       for (int s = 0; s < (PAIRS ? 2 : 1); ++s)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const f32x4 w = *(Lds)(uintptr_t)(slab + 4 * (r * S::SLAB_PITCH + 32 * s + c + 4 * h));
+          const f32x4 w = *(Lds)(uintptr_t)(slab + 4 * (r * S::SLAB_PITCH + S::WTN / 2 * s + c + 4 * h));
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[s][4 * h + e] = w[e];
         }
       // column within a set, or within the tile
-      const int col = S::COLUMNS ? 32 * wc + c % 32 : 64 * wc + c;
-      store(wm + 32 * x + r, col, S::COLUMNS && !PAIRS ? c / 32 : 0, v);
+      constexpr int HALF = S::WTN / 2;
+      const int col = S::COLUMNS ? HALF * wc + c % HALF : S::WTN * wc + c;
+      store(wm + 32 * x + r, col, S::COLUMNS && !PAIRS ? c / HALF : 0, v);
     }
     if (!std::is_same_v<Across, NoMirror> && mirror) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < 4 * (S::WTN / 64); ++i) {
+        const int r = 8 * (i % 4), c = 64 * (i / 4) + lane;
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          v[e] = *(__attribute__((address_space(3))) const float*)(uintptr_t)(slab + 4 * ((8 * i + e) * S::SLAB_PITCH + lane));
-        across(wm + 32 * x + 8 * i, 64 * wc + lane, v);
+          v[e] = *(__attribute__((address_space(3))) const float*)(uintptr_t)(slab + 4 * ((r + e) * S::SLAB_PITCH + c));
+        across(wm + 32 * x + r, S::WTN * wc + c, v);
       }
     }
   }
