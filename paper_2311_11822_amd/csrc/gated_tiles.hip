@@ -41,10 +41,12 @@ __device__ __forceinline__ void gated_forward_rows(const GatedArgs& a, int64_t a
 }
 
 template <int DT>
-__device__ __forceinline__ void gated_hidden_rows(const GatedArgs& a, int64_t at, const float (&dh)[8]) {
+struct GateAndUp {
   Values<DT, 8> gate, up;
-  gate.load(a.gate, at);
-  up.load(a.up, at);
+};
+template <int DT>
+__device__ __forceinline__ void gated_hidden_rows(const GatedArgs& a, int64_t at, const float (&dh)[8], GateAndUp<DT>& in) {
+  Values<DT, 8>&gate = in.gate, &up = in.up;
   float dg[8], du[8];
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
@@ -81,17 +83,31 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) gated_tile_kerne
   const int m0 = tm * S::BM, n = tn * (S::COLUMNS ? S::BN / 2 : S::BN), n0[2] = {n, n};
   f32x4 acc[S::TM][S::TN];
   product_tile<S, DT == DP_F16>(p, m0, n0, lds0, acc);
-  product_rows<S, PASS == kForward>(acc, lds0, [&](int row, int col, int, const float (&v)[2][8]) {
-    if (m0 + row >= p.M || n + col >= p.N) return;
-    const int64_t at = (int64_t)(m0 + row) * p.N + n + col;
-    if constexpr (PASS == kForward) gated_forward_rows<DT>(a, at, n + col, v);
-    if constexpr (PASS == kHidden) gated_hidden_rows<DT>(a, at, v[0]);
-    if constexpr (PASS == kInput) {
-      Values<DT, 8> out;
-      out.set(v[0]);
-      out.store(a.dx, at);
-    }
-  });
+  auto place = [&](int row, int col) { return (int64_t)(m0 + row) * p.N + n + col; };
+  auto inside = [&](int row, int col) { return m0 + row < p.M && n + col < p.N; };
+  if constexpr (PASS == kHidden) {
+    auto load = [&](int row, int col, int) {
+      GateAndUp<DT> in;
+      if (inside(row, col)) {
+        in.gate.load(a.gate, place(row, col));
+        in.up.load(a.up, place(row, col));
+      }
+      return in;
+    };
+    product_rows<S, false>(acc, lds0, load, [&](int row, int col, int, const float (&v)[2][8], GateAndUp<DT>& in) {
+      if (inside(row, col)) gated_hidden_rows<DT>(a, place(row, col), v[0], in);
+    });
+  } else {
+    product_rows<S, PASS == kForward>(acc, lds0, NoLoad{}, [&](int row, int col, int, const float (&v)[2][8], Nothing) {
+      if (!inside(row, col)) return;
+      if constexpr (PASS == kForward) gated_forward_rows<DT>(a, place(row, col), n + col, v);
+      if constexpr (PASS == kInput) {
+        Values<DT, 8> out;
+        out.set(v[0]);
+        out.store(a.dx, place(row, col));
+      }
+    });
+  }
 }
 
 template <int PASS, class S, int DT>
@@ -105,13 +121,20 @@ dp_status launch_tiles(const GatedArgs& a, hipStream_t s) {
   return hip_status(hipGetLastError());
 }
 
-// Large tiles where they come in whole rounds of the 256 that are resident, else small ones (512), a round of which takes three fifths of the time.
+// Large tiles or small ones.  256 large tiles are resident at a time and start and end together: 1.5 us to a stage of 64 terms, and what comes
+// before and after; 512 small ones, two to a compute unit, whose rounds run into each other: 0.9 us, and less beside it, since one's epilogue
+// runs beside the other's products.  Both as measured, us, large and small: forward 4096 x 768 x 2048 31.5, 36.3; 4728 x 784 x 2096 57.4,
+// 50.9; 4096 x 4096 x 11008 609, 728; hidden 16384 x 768 x 2048 112, 97; 4096 x 4096 x 11008 369, 371; input 4096 x 4096 x 11008 517, 752;
+// 2048 x 4096 x 4096 145, 118.
 template <int PASS, int DT>
 dp_status launch_pass(const GatedArgs& a, hipStream_t s) {
   constexpr bool COLUMNS = PASS == kForward;
-  const int64_t N = PASS == kInput ? a.d : a.f;
+  constexpr float kBigRest = PASS == kForward ? 10.f : PASS == kHidden ? 30.f : 8.f, kMidRest = PASS == kForward ? 9.f : PASS == kHidden ? 18.f : 8.f;
+  const int64_t N = PASS == kInput ? a.d : a.f, K = PASS == kForward ? a.d : PASS == kHidden ? a.d_out : a.f;
+  const float stages = (float)((K + 63) / 64 * (PASS == kInput ? 2 : 1));
   auto tiles = [&](int side) { return ((int64_t)a.rows + side - 1) / side * ((N * (COLUMNS ? 2 : 1) + side - 1) / side); };
-  const int64_t big = (tiles(256) + kBigRound - 1) / kBigRound * kBigRoundCost, mid = (tiles(128) + kMidRound - 1) / kMidRound * kMidRoundCost;
+  const float big = (float)((tiles(256) + 255) / 256) * (1.5f * stages + kBigRest);
+  const float mid = std::max(1.f, (float)tiles(128) / 512.f) * (0.9f * stages + kMidRest);
   return big <= mid ? launch_tiles<PASS, BigProduct<COLUMNS>, DT>(a, s) : launch_tiles<PASS, MidProduct<COLUMNS>, DT>(a, s);
 }
 

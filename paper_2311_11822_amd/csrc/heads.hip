@@ -73,18 +73,24 @@ struct Unit {
   }
 };
 
+// A workgroup has one side (queries or keys) of a run of tokens; its row groups take rows in turn, the next one's values on their way while
+// one is worked on.  Bound by memory.
 template <int DT, int VEC, int KIND>
 __global__ void __launch_bounds__(kThreads) heads_kernel(const HeadsArgs a) {
   constexpr int N = VEC == 1 ? 2 : 1;                  // units of a lane: rows are 64 lanes at most
+  constexpr bool GRAD = KIND == kNormGrad;
   extern __shared__ __align__(16) float2 angle[];      // then, in the same place, sums over row groups
   const int row_lanes = 1 << a.lanes, t = threadIdx.x & (row_lanes - 1), group = threadIdx.x >> a.lanes, groups = kThreads >> a.lanes;
-  const unsigned id = blockIdx.x;
-  const int b = id / (unsigned)a.chunks, chunk = id - b * a.chunks, half = a.turn / 2;
+  const int w = blockIdx.x >= a.begin;
+  const HeadsPlan plan = a.plan[w];
+  const unsigned id = blockIdx.x - (w ? a.begin : 0);
+  const int b = id / (unsigned)plan.chunks, chunk = id - b * plan.chunks, half = a.turn / 2, heads = a.heads[w];
   const int length = a.len ? min(max(a.len[b], 0), a.T) : a.T;
-  const int begin = min(chunk * a.chunk_tokens, length), end = min(begin + a.chunk_tokens, length);
+  const int begin = min(chunk * plan.chunk_tokens, length), end = min(begin + plan.chunk_tokens, length);
+  const HeadStrides in_stride = a.in_stride[w], out_stride = a.out_stride[w], dy_stride = a.dy_stride[w];
   Unit<VEC> unit[N];
   bool there[N][2];
-  float gain[2][N][2][VEC], sum[2][N][2][VEC];
+  float gain[N][2][VEC], sum[N][2][VEC];
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     unit[n].init(a, t + n * row_lanes);
@@ -92,192 +98,170 @@ __global__ void __launch_bounds__(kThreads) heads_kernel(const HeadsArgs a) {
     there[n][1] = there[n][0] && unit[n].second < a.D;
     if constexpr (KIND != kRotate) {
 #pragma unroll
-      for (int w = 0; w < 2; ++w)
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) {
+          gain[n][p][k] = there[n][p] && a.gain[w] ? a.gain[w][(p ? unit[n].second : unit[n].first) + k] : 1.f;
+          sum[n][p][k] = 0.f;
+        }
+    }
+  }
+  const float width = 1.f / a.D;
+  const int token_step = groups / heads, head_step = groups - token_step * heads;
+  struct Row {                                         // as stored
+    Values<DT, VEC> x[N][2], dy[GRAD ? N : 1][2];
+  };
+  const void *const in = a.in[w], *const dy_in = a.dy[w];
+  auto load = [&](Row& row, int token, int head) {
+    const int64_t at = b * in_stride.sample + token * in_stride.token + head * in_stride.head;
+    const int64_t dy_at = b * dy_stride.sample + token * dy_stride.token + head * dy_stride.head;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+        if (there[n][p]) {
+          row.x[n][p].load(in, at + (p ? unit[n].second : unit[n].first));
+          if constexpr (GRAD) row.dy[n][p].load(dy_in, dy_at + (p ? unit[n].second : unit[n].first));
+        }
+  };
+
+  for (int first = begin; first < end; first += plan.block_tokens) {
+    const int tokens = min(plan.block_tokens, end - first);
+    int token = group / heads, head = group - token * heads;
+    Row row;
+    if (token < tokens) load(row, first + token, head);
+    if (half) {
+      if (first > begin) __syncthreads();              // the last ones' angles have been read
+      work_out_angles(a, b, first, tokens, angle);
+      __syncthreads();
+    }
+    while (token < tokens) {
+      int next_token = token + token_step, next_head = head + head_step;
+      if (next_head >= heads) {
+        next_head -= heads;
+        ++next_token;
+      }
+      Row next;
+      if (next_token < tokens) load(next, first + next_token, next_head);
+      const float2* const at = angle + token * half;
+      float x[N][2][VEC], dy[N][2][VEC];
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
 #pragma unroll
         for (int p = 0; p < 2; ++p)
 #pragma unroll
           for (int k = 0; k < VEC; ++k) {
-            gain[w][n][p][k] = there[n][p] && a.gain[w] ? a.gain[w][(p ? unit[n].second : unit[n].first) + k] : 1.f;
-            sum[w][n][p][k] = 0.f;
+            x[n][p][k] = there[n][p] ? row.x[n][p].get(k) : 0.f;
+            if constexpr (GRAD) dy[n][p][k] = there[n][p] ? row.dy[n][p].get(k) : 0.f;
           }
-    }
-  }
-  const float width = 1.f / a.D;
-
-  for (int first = begin; first < end; first += a.block_tokens) {
-    const int tokens = min(a.block_tokens, end - first);
-    if (first > begin) __syncthreads();                // the last ones' angles have been read
-    if (half) {
-      work_out_angles(a, b, first, tokens, angle);
-      __syncthreads();
-    }
-    auto side = [&](auto w_tag) {
-      constexpr int w = decltype(w_tag)::value;
-      const int heads = a.heads[w], token_step = groups / max(heads, 1), head_step = groups - token_step * heads;
-      if (heads == 0) return;
-      int token = group / heads, head = group - token * heads;
-      for (; token < tokens; token += token_step, head += head_step) {
-        if (head >= heads) {
-          head -= heads;
-          if (++token >= tokens) break;
-        }
-        const int64_t in_row = b * a.in_stride[w].sample + (first + token) * a.in_stride[w].token + head * a.in_stride[w].head;
-        const int64_t out_row = b * a.out_stride[w].sample + (first + token) * a.out_stride[w].token + head * a.out_stride[w].head;
-        const float2* const at = angle + token * half;
-        float x[N][2][VEC];
+        if constexpr (GRAD) unit[n].turn(a, at, dy[n][0], dy[n][1]);
+      }
+      float r = 1.f, mean_uh = 0.f;
+      if constexpr (KIND != kRotate) {
+        float square = 0.f;
 #pragma unroll
         for (int n = 0; n < N; ++n)
 #pragma unroll
-          for (int p = 0; p < 2; ++p) {
-            Values<DT, VEC> v;
-            if (there[n][p]) v.load(a.in[w], in_row + (p ? unit[n].second : unit[n].first));
+          for (int p = 0; p < 2; ++p)
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) x[n][p][k] = there[n][p] ? v.get(k) : 0.f;
-          }
-        float dy[N][2][VEC];
-        if constexpr (KIND == kNormGrad) {
-          const int64_t row = b * a.dy_stride[w].sample + (first + token) * a.dy_stride[w].token + head * a.dy_stride[w].head;
+            for (int k = 0; k < VEC; ++k) square = fmaf(x[n][p][k], x[n][p][k], square);
+        r = 1.f / sqrtf(lanes_sum(square, a.lanes) * width + a.eps);
+      }
+      if constexpr (GRAD) {
+        float uh = 0.f;
 #pragma unroll
-          for (int n = 0; n < N; ++n) {
-#pragma unroll
-            for (int p = 0; p < 2; ++p) {
-              Values<DT, VEC> v;
-              if (there[n][p]) v.load(a.dy[w], row + (p ? unit[n].second : unit[n].first));
-#pragma unroll
-              for (int k = 0; k < VEC; ++k) dy[n][p][k] = there[n][p] ? v.get(k) : 0.f;
-            }
-            unit[n].turn(a, at, dy[n][0], dy[n][1]);
-          }
-        }
-        float r = 1.f, mean_uh = 0.f;
-        if constexpr (KIND != kRotate) {
-          float square = 0.f;
-#pragma unroll
-          for (int n = 0; n < N; ++n)
-#pragma unroll
-            for (int p = 0; p < 2; ++p)
-#pragma unroll
-              for (int k = 0; k < VEC; ++k) square = fmaf(x[n][p][k], x[n][p][k], square);
-          r = 1.f / sqrtf(lanes_sum(square, a.lanes) * width + a.eps);
-        }
-        if constexpr (KIND == kNormGrad) {
-          float uh = 0.f;
-#pragma unroll
-          for (int n = 0; n < N; ++n)
-#pragma unroll
-            for (int p = 0; p < 2; ++p)
-#pragma unroll
-              for (int k = 0; k < VEC; ++k) {
-                const float h = x[n][p][k] * r, u = dy[n][p][k] * gain[w][n][p][k];
-                sum[w][n][p][k] = fmaf(dy[n][p][k], h, sum[w][n][p][k]);
-                uh = fmaf(u, h, uh);
-              }
-          mean_uh = lanes_sum(uh, a.lanes) * width;
-        }
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-          if constexpr (KIND == kNorm) {
-#pragma unroll
-            for (int p = 0; p < 2; ++p)
-#pragma unroll
-              for (int k = 0; k < VEC; ++k) x[n][p][k] = x[n][p][k] * r * gain[w][n][p][k];
-          }
-          if constexpr (KIND == kNormGrad) {
-#pragma unroll
-            for (int p = 0; p < 2; ++p)
-#pragma unroll
-              for (int k = 0; k < VEC; ++k) x[n][p][k] = r * (dy[n][p][k] * gain[w][n][p][k] - x[n][p][k] * r * mean_uh);
-          } else {
-            unit[n].turn(a, at, x[n][0], x[n][1]);
-          }
+        for (int n = 0; n < N; ++n)
 #pragma unroll
           for (int p = 0; p < 2; ++p)
-            if (there[n][p]) {
-              Values<DT, VEC> v;
-              v.set(x[n][p]);
-              v.store(a.out[w], out_row + (p ? unit[n].second : unit[n].first));
-            }
-        }
-      }
-    };
-    side(std::integral_constant<int, 0>{});
-    side(std::integral_constant<int, 1>{});
-  }
-
-  if constexpr (KIND == kNormGrad) {
-    if (!a.kept) return;
-    // the row groups' sums, one after the other
-    float* const red = reinterpret_cast<float*>(angle);                // [groups][D]
-    const int sides = a.heads[1] ? 2 : 1;
-    float* const to = a.partial + ((int64_t)b * a.chunks + chunk) * sides * a.D;
-    auto join = [&](auto w_tag) {
-      constexpr int w = decltype(w_tag)::value;
-      __syncthreads();
 #pragma unroll
-      for (int n = 0; n < N; ++n)
+            for (int k = 0; k < VEC; ++k) {
+              x[n][p][k] *= r;
+              sum[n][p][k] = fmaf(dy[n][p][k], x[n][p][k], sum[n][p][k]);
+              dy[n][p][k] *= gain[n][p][k];
+              uh = fmaf(dy[n][p][k], x[n][p][k], uh);
+            }
+        mean_uh = lanes_sum(uh, a.lanes) * width;
+      }
+      const int64_t out_row = b * out_stride.sample + (first + token) * out_stride.token + head * out_stride.head;
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
 #pragma unroll
         for (int p = 0; p < 2; ++p)
 #pragma unroll
-          for (int k = 0; k < VEC; ++k)
-            if (there[n][p]) red[group * a.D + (p ? unit[n].second : unit[n].first) + k] = sum[w][n][p][k];
-      __syncthreads();
-      for (int c = threadIdx.x; c < a.D; c += kThreads) {
-        float s = 0.f;
-        for (int g = 0; g < groups; ++g) s += red[g * a.D + c];
-        to[w * a.D + c] = s;
-      }
-    };
-    join(std::integral_constant<int, 0>{});
-    if (a.heads[1]) join(std::integral_constant<int, 1>{});
-  }
-}
-
-// A workgroup to a sample: its chunks' sums, in their order by sixteenths, and the square of all of them.
-constexpr int kJoinThreads = 1024, kJoinParts = 16;
-__global__ void __launch_bounds__(kJoinThreads) heads_join_kernel(const float* partial, float* kept, float* sqnorm, int chunks, int columns) {
-  __shared__ float part[kJoinParts][64], square[kJoinParts];
-  const int b = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const float* from = partial + (int64_t)b * chunks * columns;
-  float total = 0.f;                                                   // of wave 0's lanes
-  for (int c0 = 0; c0 < columns; c0 += 64) {
-    const int c = c0 + lane;
-    float s = 0.f;
-    if (c < columns)
-      for (int k = wave; k < chunks; k += kJoinParts) s += from[(int64_t)k * columns + c];
-    part[wave][lane] = s;
-    __syncthreads();
-    if (wave == 0 && c < columns) {
-      float v = 0.f;
+          for (int k = 0; k < VEC; ++k) {
+            if constexpr (KIND == kNorm) x[n][p][k] = x[n][p][k] * r * gain[n][p][k];
+            if constexpr (GRAD) x[n][p][k] = r * (dy[n][p][k] - x[n][p][k] * mean_uh);
+          }
+        if constexpr (!GRAD) unit[n].turn(a, at, x[n][0], x[n][1]);
 #pragma unroll
-      for (int w = 0; w < kJoinParts; ++w) v += part[w][lane];
-      kept[(int64_t)b * columns + c] = v;
-      total = fmaf(v, v, total);
+        for (int p = 0; p < 2; ++p)
+          if (there[n][p]) {
+            Values<DT, VEC> v;
+            v.set(x[n][p]);
+            v.store(a.out[w], out_row + (p ? unit[n].second : unit[n].first));
+          }
+      }
+      row = next;
+      token = next_token;
+      head = next_head;
     }
+  }
+
+  if constexpr (GRAD) {
+    if (!a.kept) return;
+    // the row groups' sums, one after the other
+    float* const red = reinterpret_cast<float*>(angle);                // [groups][D]
     __syncthreads();
-  }
-  if (wave == 0) {
-    for (int off = 32; off > 0; off >>= 1) total += __shfl_xor(total, off);
-    if (lane == 0) sqnorm[b] = total;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int k = 0; k < VEC; ++k)
+          if (there[n][p]) red[group * a.D + (p ? unit[n].second : unit[n].first) + k] = sum[n][p][k];
+    __syncthreads();
+    float* const to = a.partial + (w ? (int64_t)a.B * a.plan[0].chunks * a.D : 0) + (int64_t)id * a.D;
+    for (int c = threadIdx.x; c < a.D; c += kThreads) {
+      float s = 0.f;
+      for (int g = 0; g < groups; ++g) s += red[g * a.D + c];
+      to[c] = s;
+    }
   }
 }
 
-template <int DT, int VEC>
-dp_status launch(const HeadsArgs& a, HeadsKind kind, size_t lds, hipStream_t s) {
-  const dim3 grid((unsigned)a.B * a.chunks);
-  if (kind == kRotate)
-    heads_kernel<DT, VEC, kRotate><<<grid, kThreads, lds, s>>>(a);
-  else if (kind == kNorm)
-    heads_kernel<DT, VEC, kNorm><<<grid, kThreads, lds, s>>>(a);
-  else
-    heads_kernel<DT, VEC, kNormGrad><<<grid, kThreads, lds, s>>>(a);
-  return hip_status(hipGetLastError());
+// A workgroup to a sample: its chunks' sums, by parts that are added in their order, and the square of all of them.
+constexpr int kJoinThreads = 1024;
+__global__ void __launch_bounds__(kJoinThreads) heads_join_kernel(const HeadsArgs a) {
+  __shared__ float part[kJoinThreads], square[kJoinThreads / 64];
+  const int b = blockIdx.x, sides = a.heads[1] ? 2 : 1, columns = sides * a.D;             // up to 512
+  const int parts = kJoinThreads / columns, p = threadIdx.x / columns, c = threadIdx.x - p * columns, w = c >= a.D;
+  const HeadsPlan plan = a.plan[w];
+  float s = 0.f;
+  if (p < parts) {
+    const float* from = a.partial + (w ? (int64_t)a.B * a.plan[0].chunks * a.D : 0) + (int64_t)b * plan.chunks * a.D + (c - w * a.D);
+#pragma unroll 8
+    for (int k = p; k < plan.chunks; k += parts) s += from[(int64_t)k * a.D];
+  }
+  part[threadIdx.x] = s;
+  __syncthreads();
+  float v = 0.f;
+  if (threadIdx.x < columns) {
+    for (int k = 0; k < parts; ++k) v += part[k * columns + threadIdx.x];
+    a.kept[(int64_t)b * columns + threadIdx.x] = v;
+  }
+  v *= v;
+  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
+  if ((threadIdx.x & 63) == 0) square[threadIdx.x >> 6] = v;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int k = 1; k < kJoinThreads / 64; ++k) v += square[k];
+    a.sqnorm[b] = v;
+  }
 }
-
-}  // namespace
 
 // Accesses of 16 bytes where rows begin at such and the pieces of two halves that turn together do, else the largest that fit: 8, 4 or 2.
-void heads_layout(HeadsArgs& a, dp_dtype dt, HeadsKind kind, int& vec) {
-  vec = dt == DP_F32 ? 4 : 8;
+int access_width(const HeadsArgs& a, dp_dtype dt) {
+  int vec = dt == DP_F32 ? 4 : 8;
   const int size = dt == DP_F32 ? 4 : 2;
   int64_t all = a.D | (a.interleaved ? 0 : a.turn / 2);
   for (int w = 0; w < 2; ++w)
@@ -288,26 +272,61 @@ void heads_layout(HeadsArgs& a, dp_dtype dt, HeadsKind kind, int& vec) {
       for (const void* p : arrays) all |= (int64_t)(reinterpret_cast<uintptr_t>(p) / size);
     }
   while (vec > 1 && all % vec) vec /= 2;
-  const int pieces = (a.D + vec - 1) / vec, units = (pieces + 1) / 2, per_lane = vec == 1 ? 2 : 1;
-  a.lanes = 0;
-  while ((1 << a.lanes) * per_lane < units) ++a.lanes;
-  const int groups = kThreads >> a.lanes, heads = a.heads[0] + a.heads[1];
-  // two turns of the workgroup's row groups at least, and no more angles than 16 KiB
-  a.block_tokens = std::max(1, std::min({(2 * groups + heads - 1) / heads, 2048 / std::max(1, a.turn / 2), a.T}));
-  const int64_t blocks = (int64_t)((a.T + a.block_tokens - 1) / a.block_tokens) * a.B;
-  const int64_t most = kind == kNormGrad ? 1024 : 4096;
-  a.chunk_tokens = a.block_tokens * (int)((blocks + most - 1) / most);
-  a.chunks = (a.T + a.chunk_tokens - 1) / a.chunk_tokens;
+  return vec;
 }
 
+// A side's tokens by workgroup: of a block's rows as few as can be leave row groups idle in their last turn (of two turns at least), no more angles
+// than 16 KiB, and no more workgroups than `most` and one to a sample.
+HeadsPlan plan_side(const HeadsArgs& a, int w, int most) {
+  const int groups = kThreads >> a.lanes, heads = a.heads[w];
+  const int least = std::max(1, std::min((2 * groups + heads - 1) / heads, a.T)), limit = std::max(1, std::min(2048 / std::max(1, a.turn / 2), a.T));
+  HeadsPlan plan = {};
+  double best = -1.;
+  for (int tokens = std::min(least, limit); tokens <= std::min(limit, 4 * least); ++tokens) {
+    const int64_t rows = (int64_t)tokens * heads, turns = (rows + groups - 1) / groups;
+    const double filled = (double)rows / (double)(turns * groups);
+    if (filled > best + 0.02) {
+      best = filled;
+      plan.block_tokens = tokens;
+    }
+  }
+  const int64_t blocks = (int64_t)((a.T + plan.block_tokens - 1) / plan.block_tokens) * a.B;
+  plan.chunk_tokens = plan.block_tokens * (int)((blocks + most - 1) / most);
+  plan.chunks = (a.T + plan.chunk_tokens - 1) / plan.chunk_tokens;
+  return plan;
+}
+
+template <int DT, int VEC>
+dp_status launch(const HeadsArgs& a, HeadsKind kind, unsigned blocks, size_t lds, hipStream_t s) {
+  if (kind == kRotate)
+    heads_kernel<DT, VEC, kRotate><<<dim3(blocks), kThreads, lds, s>>>(a);
+  else if (kind == kNorm)
+    heads_kernel<DT, VEC, kNorm><<<dim3(blocks), kThreads, lds, s>>>(a);
+  else
+    heads_kernel<DT, VEC, kNormGrad><<<dim3(blocks), kThreads, lds, s>>>(a);
+  return hip_status(hipGetLastError());
+}
+
+}  // namespace
+
 dp_status launch_heads(HeadsArgs a, dp_dtype dt, HeadsKind kind, hipStream_t s) {
-  int vec;
-  heads_layout(a, dt, kind, vec);
-  size_t lds = (size_t)a.block_tokens * (a.turn / 2) * sizeof(float2);
+  const int vec = access_width(a, dt);
+  const int pieces = (a.D + vec - 1) / vec, units = (pieces + 1) / 2, per_lane = vec == 1 ? 2 : 1;
+  while ((1 << a.lanes) * per_lane < units) ++a.lanes;
+  int tokens = 0;
+  unsigned blocks = 0;
+  for (int w = 0; w < 2; ++w) {
+    if (w == 1) a.begin = blocks;
+    if (!a.heads[w]) continue;
+    a.plan[w] = plan_side(a, w, kind == kNormGrad ? kHeadsGradChunks : kHeadsChunks);
+    blocks += (unsigned)(a.B * a.plan[w].chunks);
+    tokens = std::max(tokens, a.plan[w].block_tokens);
+  }
+  size_t lds = (size_t)tokens * (a.turn / 2) * sizeof(float2);
   if (kind == kNormGrad && a.kept) lds = std::max(lds, (size_t)(kThreads >> a.lanes) * a.D * sizeof(float));
   dp_status st;
 #define DP_LAUNCH(DT, VEC) \
-  if (dt == DT && vec == VEC) st = launch<DT, VEC>(a, kind, lds, s);
+  if (dt == DT && vec == VEC) st = launch<DT, VEC>(a, kind, blocks, lds, s);
   DP_LAUNCH(DP_F32, 4)
   else DP_LAUNCH(DP_F32, 2)
   else DP_LAUNCH(DP_F32, 1)
@@ -322,7 +341,7 @@ dp_status launch_heads(HeadsArgs a, dp_dtype dt, HeadsKind kind, hipStream_t s) 
   else return DP_ERR_UNSUPPORTED;
 #undef DP_LAUNCH
   if (st != DP_OK || kind != kNormGrad || !a.kept) return st;
-  heads_join_kernel<<<dim3(a.B), kJoinThreads, 0, s>>>(a.partial, a.kept, a.sqnorm, a.chunks, (a.heads[1] ? 2 : 1) * a.D);
+  heads_join_kernel<<<dim3(a.B), kJoinThreads, 0, s>>>(a);
   return hip_status(hipGetLastError());
 }
 

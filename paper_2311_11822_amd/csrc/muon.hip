@@ -228,7 +228,7 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) muon_product_ker
       for (int k = 0; k < 8; ++k) v[k] = acc8[k] * (1.f / kScale);
     }
   };
-  auto store = [&](int row, int col, int set, const float (&acc8)[2][8]) {
+  auto store = [&](int row, int col, int set, const float (&acc8)[2][8], Nothing) {
     const int r = m0 + row, c = n0[set] + col;
     if (r >= m || c >= pitch) return;
     float v[8];
@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) muon_product_ker
     put(r, c, v);
   };
   if constexpr (STEP == kUpdate) {
-    product_rows<S, false>(acc, lds0, store);
+    product_rows<S, false>(acc, lds0, NoLoad{}, store);
   } else {
     // below the diagonal: rows of the tile's columns
     auto across = [&](int row, int col, const float (&acc8)[8]) {
@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) muon_product_ker
       finish(r, c, acc8, v);
       put(r, c, v);
     };
-    product_rows<S, false>(acc, lds0, store, tm != tn, across);
+    product_rows<S, false>(acc, lds0, NoLoad{}, store, tm != tn, across);
   }
 }
 

@@ -269,19 +269,30 @@ __device__ __forceinline__ void product_tile(const ProductShape& p, int m0, cons
   __syncthreads();
 }
 
-// acc's rows to store(row of the tile, first column, values): columns 8 at a time, of both sets where PAIRS (v[0] and v[1]), else of one
-// fragment (v[0]).  The wave's 32 rows at a time are turned in LDS, so that whole rows leave.  across(first row, column, values): the same
-// by columns, rows 8 at a time, where `mirror`.
+// acc's rows to store(row of the tile, column, set, values, ahead): columns 8 at a time, of both sets where PAIRS (v[0] and v[1]), else of one
+// (v[0]).  The wave's 32 rows at a time are turned in LDS, so that whole rows leave.  ahead: what load(row, column, set) brought for this place,
+// asked for 32 rows before.  across(first row, column, values): the same by columns, rows 8 at a time, where `mirror`.
 struct NoMirror {
   __device__ void operator()(int, int, const float (&)[8]) const {}
 };
-template <class S, bool PAIRS, class Store, class Across = NoMirror>
-__device__ __forceinline__ void product_rows(const f32x4 (&acc)[S::TM][S::TN], unsigned lds0, Store store, bool mirror = false,
+struct Nothing {};
+struct NoLoad {
+  __device__ Nothing operator()(int, int, int) const { return {}; }
+};
+template <class S, bool PAIRS, class Load, class Store, class Across = NoMirror>
+__device__ __forceinline__ void product_rows(const f32x4 (&acc)[S::TM][S::TN], unsigned lds0, Load load, Store store, bool mirror = false,
                                              Across across = {}) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / S::WN * S::WTM, wc = wave % S::WN;
   const unsigned slab = lds0 + wave * S::SLAB_BYTES;
   typedef __attribute__((address_space(3))) f32x4* Lds;
+  constexpr int LANES = S::WTN / (PAIRS ? 16 : 8), PASSES = 32 * LANES / 64, HALF = S::WTN / 2;
+  const int c = 8 * (lane % LANES), set = S::COLUMNS && !PAIRS ? c / HALF : 0;
+  const int col = S::COLUMNS ? HALF * wc + c % HALF : S::WTN * wc + c;       // within a set, or within the tile
+  auto row_of = [&](int x, int i) { return 32 * x + i * (64 / LANES) + lane / LANES; };
+  decltype(load(0, 0, 0)) ahead[2][PASSES];
+#pragma unroll
+  for (int i = 0; i < PASSES; ++i) ahead[0][i] = load(wm + row_of(0, i), col, set);
 #pragma unroll
   for (int x = 0; x < S::TM / 2; ++x) {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -290,34 +301,32 @@ __device__ __forceinline__ void product_rows(const f32x4 (&acc)[S::TM][S::TN], u
 #pragma unroll
       for (int y = 0; y < S::TN; ++y)
         *(Lds)(uintptr_t)(slab + 4 * ((16 * h + (lane & 15)) * S::SLAB_PITCH + 16 * y + 4 * (lane >> 4))) = acc[2 * x + h][y];
+    if (x + 1 < S::TM / 2)
+#pragma unroll
+      for (int i = 0; i < PASSES; ++i) ahead[(x + 1) & 1][i] = load(wm + row_of(x + 1, i), col, set);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    constexpr int LANES = S::WTN / (PAIRS ? 16 : 8), PASSES = 32 * LANES / 64;
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) {
-      const int r = i * (64 / LANES) + lane / LANES, c = 8 * (lane % LANES);
       float v[2][8];
 #pragma unroll
       for (int s = 0; s < (PAIRS ? 2 : 1); ++s)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const f32x4 w = *(Lds)(uintptr_t)(slab + 4 * (r * S::SLAB_PITCH + S::WTN / 2 * s + c + 4 * h));
+          const f32x4 w = *(Lds)(uintptr_t)(slab + 4 * ((row_of(0, i)) * S::SLAB_PITCH + HALF * s + c + 4 * h));
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[s][4 * h + e] = w[e];
         }
-      // column within a set, or within the tile
-      constexpr int HALF = S::WTN / 2;
-      const int col = S::COLUMNS ? HALF * wc + c % HALF : S::WTN * wc + c;
-      store(wm + 32 * x + r, col, S::COLUMNS && !PAIRS ? c / HALF : 0, v);
+      store(wm + row_of(x, i), col, set, v, ahead[x & 1][i]);
     }
     if (!std::is_same_v<Across, NoMirror> && mirror) {
 #pragma unroll
       for (int i = 0; i < 4 * (S::WTN / 64); ++i) {
-        const int r = 8 * (i % 4), c = 64 * (i / 4) + lane;
+        const int r = 8 * (i % 4), at = 64 * (i / 4) + lane;
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          v[e] = *(__attribute__((address_space(3))) const float*)(uintptr_t)(slab + 4 * ((r + e) * S::SLAB_PITCH + c));
-        across(wm + 32 * x + r, S::WTN * wc + c, v);
+          v[e] = *(__attribute__((address_space(3))) const float*)(uintptr_t)(slab + 4 * ((r + e) * S::SLAB_PITCH + at));
+        across(wm + 32 * x + r, S::WTN * wc + at, v);
       }
     }
   }

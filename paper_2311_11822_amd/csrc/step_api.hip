@@ -64,9 +64,9 @@ dp_status heads_args(const dp_heads_shape* p, dp_dtype dt, bool backward, HeadsA
 
 bool sides_there(const HeadsArgs& a, dp_dtype dt, const void* q, const void* k) { return there(q, dt) && (a.heads[1] == 0 || there(k, dt)); }
 
-// Sums of a chunk's gains: chunks of all samples are no more than 1024 and one more for each, nor than tokens.
+// Sums of a chunk's gains: a side's chunks are no more than its bound and one more for each sample, nor than tokens.
 size_t head_norm_workspace(const HeadsArgs& a) {
-  const int64_t chunks = std::min((int64_t)a.B * a.T, (int64_t)1024 + a.B);
+  const int64_t chunks = std::min((int64_t)a.B * a.T, (int64_t)kHeadsGradChunks + a.B);
   return (size_t)chunks * (a.heads[1] ? 2 : 1) * a.D * sizeof(float);
 }
 
