@@ -16,9 +16,18 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// Sum over the 2^lanes lanes of a row, in each of them.
+// Sum over the 2^lanes lanes of a row, in each of them; up to sixteen without LDS: within four lanes, then eights and sixteens turned around.
+template <int CONTROL>
+__device__ __forceinline__ float lane_of(float x) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CONTROL, 0xF, 0xF, true));
+}
 __device__ __forceinline__ float lanes_sum(float x, int lanes) {
-  for (int n = 0; n < lanes; ++n) x += __shfl_xor(x, 1 << n);
+  if (lanes > 0) x += lane_of<0xB1>(x);                // quad_perm 1 0 3 2
+  if (lanes > 1) x += lane_of<0x4E>(x);                // quad_perm 2 3 0 1
+  if (lanes > 2) x += lane_of<0x141>(x);               // row_half_mirror
+  if (lanes > 3) x += lane_of<0x140>(x);               // row_mirror
+  if (lanes > 4) x += __shfl_xor(x, 16);
+  if (lanes > 5) x += __shfl_xor(x, 32);
   return x;
 }
 
@@ -112,9 +121,17 @@ __global__ void __launch_bounds__(kThreads) heads_kernel(const HeadsArgs a) {
     Values<DT, VEC> x[N][2], dy[GRAD ? N : 1][2];
   };
   const void *const in = a.in[w], *const dy_in = a.dy[w];
-  auto load = [&](Row& row, int token, int head) {
-    const int64_t at = b * in_stride.sample + token * in_stride.token + head * in_stride.head;
-    const int64_t dy_at = b * dy_stride.sample + token * dy_stride.token + head * dy_stride.head;
+  // Where a row lies, and from one of a group's rows to the next: a step, or one past the last head.
+  struct Place {
+    int64_t at, step, wrapped;
+    __device__ __forceinline__ void init(const HeadStrides& st, int b, int token, int head, int token_step, int head_step, int heads) {
+      at = b * st.sample + token * st.token + head * st.head;
+      step = token_step * st.token + head_step * st.head;
+      wrapped = step + st.token - heads * st.head;
+    }
+    __device__ __forceinline__ void next(bool wrap) { at += wrap ? wrapped : step; }
+  };
+  auto load = [&](Row& row, int64_t at, int64_t dy_at) {
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
@@ -128,21 +145,24 @@ __global__ void __launch_bounds__(kThreads) heads_kernel(const HeadsArgs a) {
   for (int first = begin; first < end; first += plan.block_tokens) {
     const int tokens = min(plan.block_tokens, end - first);
     int token = group / heads, head = group - token * heads;
+    Place x_at, dy_at, out_at;
+    x_at.init(in_stride, b, first + token, head, token_step, head_step, heads);
+    dy_at.init(dy_stride, b, first + token, head, token_step, head_step, heads);
+    out_at.init(out_stride, b, first + token, head, token_step, head_step, heads);
     Row row;
-    if (token < tokens) load(row, first + token, head);
+    if (token < tokens) load(row, x_at.at, dy_at.at);
     if (half) {
       if (first > begin) __syncthreads();              // the last ones' angles have been read
       work_out_angles(a, b, first, tokens, angle);
       __syncthreads();
     }
     while (token < tokens) {
-      int next_token = token + token_step, next_head = head + head_step;
-      if (next_head >= heads) {
-        next_head -= heads;
-        ++next_token;
-      }
+      const bool wrap = head + head_step >= heads;
+      const int next_token = token + token_step + wrap, next_head = head + head_step - (wrap ? heads : 0);
+      x_at.next(wrap);
+      dy_at.next(wrap);
       Row next;
-      if (next_token < tokens) load(next, first + next_token, next_head);
+      if (next_token < tokens) load(next, x_at.at, dy_at.at);
       const float2* const at = angle + token * half;
       float x[N][2][VEC], dy[N][2][VEC];
 #pragma unroll
@@ -165,7 +185,7 @@ __global__ void __launch_bounds__(kThreads) heads_kernel(const HeadsArgs a) {
           for (int p = 0; p < 2; ++p)
 #pragma unroll
             for (int k = 0; k < VEC; ++k) square = fmaf(x[n][p][k], x[n][p][k], square);
-        r = 1.f / sqrtf(lanes_sum(square, a.lanes) * width + a.eps);
+        r = __builtin_amdgcn_rsqf(lanes_sum(square, a.lanes) * width + a.eps);       // within one unit in the last place
       }
       if constexpr (GRAD) {
         float uh = 0.f;
@@ -182,7 +202,6 @@ __global__ void __launch_bounds__(kThreads) heads_kernel(const HeadsArgs a) {
             }
         mean_uh = lanes_sum(uh, a.lanes) * width;
       }
-      const int64_t out_row = b * out_stride.sample + (first + token) * out_stride.token + head * out_stride.head;
 #pragma unroll
       for (int n = 0; n < N; ++n) {
 #pragma unroll
@@ -198,9 +217,10 @@ __global__ void __launch_bounds__(kThreads) heads_kernel(const HeadsArgs a) {
           if (there[n][p]) {
             Values<DT, VEC> v;
             v.set(x[n][p]);
-            v.store(a.out[w], out_row + (p ? unit[n].second : unit[n].first));
+            v.store(a.out[w], out_at.at + (p ? unit[n].second : unit[n].first));
           }
       }
+      out_at.next(wrap);
       row = next;
       token = next_token;
       head = next_head;
@@ -275,17 +295,18 @@ int access_width(const HeadsArgs& a, dp_dtype dt) {
   return vec;
 }
 
-// A side's tokens by workgroup: of a block's rows as few as can be leave row groups idle in their last turn (of two turns at least), no more angles
+// A side's tokens by workgroup: of a block's rows as few as can be leave row groups idle in their last turn (of two at least), no more angles
 // than 16 KiB, and no more workgroups than `most` and one to a sample.
 HeadsPlan plan_side(const HeadsArgs& a, int w, int most) {
   const int groups = kThreads >> a.lanes, heads = a.heads[w];
-  const int least = std::max(1, std::min((2 * groups + heads - 1) / heads, a.T)), limit = std::max(1, std::min(2048 / std::max(1, a.turn / 2), a.T));
+  const int turns = (int64_t)a.B * a.T * heads >= (int64_t)2048 * groups ? 2 : 1;          // (few rows: all of them on their way at once)
+  const int least = std::max(1, std::min((turns * groups + heads - 1) / heads, a.T)), limit = std::max(1, std::min(2048 / std::max(1, a.turn / 2), a.T));
   HeadsPlan plan = {};
   double best = -1.;
   for (int tokens = std::min(least, limit); tokens <= std::min(limit, 4 * least); ++tokens) {
-    const int64_t rows = (int64_t)tokens * heads, turns = (rows + groups - 1) / groups;
-    const double filled = (double)rows / (double)(turns * groups);
-    if (filled > best + 0.02) {
+    const int64_t rows = (int64_t)tokens * heads, taken = (rows + groups - 1) / groups;
+    const double filled = (double)rows / (double)(taken * groups);
+    if (filled > best + (turns == 1 ? 0.2 : 0.02)) {
       best = filled;
       plan.block_tokens = tokens;
     }
