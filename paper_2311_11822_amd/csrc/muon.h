@@ -5,7 +5,7 @@
 
 namespace dpbk {
 
-constexpr int kMuonGroup = 40;             // tensors of a launch
+constexpr int kMuonGroup = 64;             // tensors of a launch: 6 KiB of kernel arguments
 constexpr int kMuonParts = 1024;           // partial sums of a tensor's square, at most
 constexpr int kMuonMostSide = 1 << 20, kMuonMostShort = 1 << 16;
 constexpr float kMuonMost = 15.f;          // values that 2^12 of still fit fp16

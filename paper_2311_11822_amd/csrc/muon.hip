@@ -8,7 +8,7 @@
 // 2^-24 of it, is left out.  2^12 keeps the halves of entries from 2^-15 up out of fp16's subnormal range; entries are bounded by singular
 // values, which the host has followed through the polynomials.  (fp32 matrix instructions have 1/16 of the 16-bit rate, a third of it 1/3.)
 // A, the square and the polynomial of A are symmetric: tiles on and above the diagonal are formed, and leave turned as well.
-// Matrices travel together: a launch does one step of up to 40 of them.
+// Matrices travel together: a launch does one step of up to 64 of them.
 #include <math.h>
 
 #include <algorithm>
@@ -276,17 +276,28 @@ dp_status launch_product(Group& g, hipStream_t s) {
   return hip_status(hipGetLastError());
 }
 
-// Large tiles where they come in whole rounds, as elsewhere.
+// Large tiles or small ones: 256 of the former are resident, 1.5 us to a stage of 64 terms, 512 of the latter, 0.85 us; what comes before and after a
+// contraction is the same again for some stages.  Workgroups are dealt out in order, the longest first: a launch takes their sum over those that
+// are resident, and some of the longest besides.
 template <int STEP>
 dp_status launch_step(Group& g, hipStream_t s) {
   constexpr bool COLUMNS = STEP == kUpdate;
-  int64_t big = 0, mid = 0;
-  for (int i = 0; i < g.n; ++i) {
-    big += tiles_of<STEP, 256>(g.t[i]);
-    mid += tiles_of<STEP, 128>(g.t[i]);
-  }
-  const bool large = (big + kBigRound - 1) / kBigRound * kBigRoundCost <= (mid + kMidRound - 1) / kMidRound * kMidRoundCost;
-  return large ? launch_product<STEP, BigProduct<COLUMNS>>(g, s) : launch_product<STEP, MidProduct<COLUMNS>>(g, s);
+  auto cost = [&](auto tiles, float stage, float rest, float resident) {
+    float sum = 0.f, longest = 0.f;
+    int64_t n = 0;
+    for (int i = 0; i < g.n; ++i) {
+      const Matrix& t = g.t[i];
+      const int k = STEP == kGram ? std::max(t.rows, t.cols) : std::min(t.rows, t.cols);
+      const float one = (float)(3 * ((k + 63) / 64)) * stage + rest;
+      sum += (float)tiles(t) * one;
+      longest = std::max(longest, one);
+      n += tiles(t);
+    }
+    return (float)n <= resident ? longest : sum / resident + longest / 2;
+  };
+  const float big = cost(tiles_of<STEP, 256>, 1.5f, STEP == kUpdate ? 12.f : 30.f, 256.f);
+  const float mid = cost(tiles_of<STEP, 128>, 0.85f, STEP == kUpdate ? 10.f : 18.f, 512.f);
+  return big <= mid ? launch_product<STEP, BigProduct<COLUMNS>>(g, s) : launch_product<STEP, MidProduct<COLUMNS>>(g, s);
 }
 
 // Bytes of a matrix's two X, A, polynomial and partial sums.
@@ -317,8 +328,13 @@ dp_status launch_muon(const MuonTensor* tensors, int n, const MuonArgs& a, dp_dt
   g.grad_scale = a.grad_scale;
   g.eps = a.eps;
   char* base = static_cast<char*>(ws);
+  int order[kMuonGroup];                             // the longest contractions first: others fill in behind them
+  for (int i = 0; i < n; ++i) order[i] = i;
+  std::stable_sort(order, order + n, [&](int i, int j) {
+    return std::max(tensors[i].rows, tensors[i].cols) > std::max(tensors[j].rows, tensors[j].cols);
+  });
   for (int i = 0; i < g.n; ++i) {
-    const MuonTensor& from = tensors[i];
+    const MuonTensor& from = tensors[order[i]];
     Matrix& t = g.t[i];
     size_t at[5];
     const size_t bytes = matrix_bytes(from.rows, from.cols, at);

@@ -320,8 +320,8 @@ __device__ __forceinline__ void product_rows(const f32x4 (&acc)[S::TM][S::TN], u
     }
     if (!std::is_same_v<Across, NoMirror> && mirror) {
 #pragma unroll
-      for (int i = 0; i < 4 * (S::WTN / 64); ++i) {
-        const int r = 8 * (i % 4), at = 64 * (i / 4) + lane;
+      for (int i = 0; i < S::WTN / 16; ++i) {                      // four lanes have the 32 rows of a column
+        const int r = 8 * (lane & 3), at = 16 * i + (lane >> 2);
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e)

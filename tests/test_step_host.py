@@ -230,10 +230,10 @@ def test_muon_refuses_polynomials(abc):
 
 
 def test_muon_workspace_is_of_one_run():
-    """Matrices go in runs of up to 40: the workspace is the largest run's."""
+    """Matrices go in runs of up to 64: the workspace is the largest run's."""
     one = [(None, None, None, None, 64, 128, 0.0, 1.0)]
-    assert dp.dp_muon_workspace_bytes(one * 40) == 40 * dp.dp_muon_workspace_bytes(one)
-    assert dp.dp_muon_workspace_bytes(one * 60) == 30 * dp.dp_muon_workspace_bytes(one)
+    assert dp.dp_muon_workspace_bytes(one * 64) == 64 * dp.dp_muon_workspace_bytes(one)
+    assert dp.dp_muon_workspace_bytes(one * 90) == 45 * dp.dp_muon_workspace_bytes(one)
 
 
 def test_muon_object_refuses():
