@@ -632,7 +632,8 @@ dp_status dp_gated(const void* x, dp_dtype dt, int rows, int d, int f, const voi
  *   dy        device, [rows, d_out] of type dt, with w_down device [f, d_out];  or, w_down NULL, dh itself, [rows, f] (d_out is not looked at)
  *   gate, up  dp_gated's;  dgate, dup  device, [rows, f] of type dt; they may be gate and up, or one of them dh
  *   dx        device, [rows, d] of type dt, or NULL: not wanted (then the weights may be NULL)
- *   ws        device scratch, >= dp_gated_backward_workspace_bytes(...), 16-byte aligned; the size is 0 where it is not used
+ *   ws        device scratch, >= dp_gated_backward_workspace_bytes(...), 16-byte aligned; not used without dx, nor where the size is 0.  (d_out is
+ *             not looked at for its size.)
  */
 size_t dp_gated_backward_workspace_bytes(dp_dtype dt, int rows, int d, int f, int d_out);
 dp_status dp_gated_backward(const void* dy, const void* w_down, int d_out, const void* gate, const void* up, dp_dtype dt, int rows, int d,

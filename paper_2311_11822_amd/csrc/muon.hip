@@ -196,6 +196,8 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) muon_product_ker
     p.K = p.lda = mp;
   }
   p.terms = m;
+  p.first = 0;
+  p.stages = 3 * ((p.K + kProductTerms - 1) / kProductTerms);
   const _Float16 *al = a + (int64_t)m * p.lda, *bl = b + (int64_t)m * p.ldb;
   p.s[0] = {a, b, b};
   p.s[1] = {a, bl, bl};

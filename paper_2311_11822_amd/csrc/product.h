@@ -27,17 +27,19 @@ namespace dpbk {
 struct ProductSegment {
   const void *a, *b0, *b1;          // b1: the second set's columns (columns only)
 };
+constexpr int kProductTerms = 64;   // of a stage
 struct ProductShape {
   int M, N, K;                      // K: of a segment; K and N (columns) are multiples of 8
   int terms;                        // columns: rows of B that are there (K or fewer: A has zeros beyond)
   int lda, ldb;                     // elements from one row (of columns: term) to the next
   int segments;
+  int first, stages;                // of all segments' stages one behind the other, those that this tile takes
   ProductSegment s[3];
 };
 
 template <int BM_, int WM_, int WN_, bool COLUMNS_>
 struct ProductTile {
-  static constexpr int BM = BM_, BN = BM_, BK = 64, A_PLACES = 3, B_PLACES = 2, WM = WM_, WN = WN_, NW = WM * WN, NT = 64 * NW;
+  static constexpr int BM = BM_, BN = BM_, BK = kProductTerms, A_PLACES = 3, B_PLACES = 2, WM = WM_, WN = WN_, NW = WM * WN, NT = 64 * NW;
   static constexpr bool COLUMNS = COLUMNS_;
   static constexpr int WTM = BM / WM, WTN = BN / WN, TM = WTM / 16, TN = WTN / 16;       // 16 x 16 results of a wave
   static constexpr int ROW_BYTES = 2 * BK, A_BYTES = BM * ROW_BYTES, B_BYTES = BN * ROW_BYTES;
@@ -87,10 +89,15 @@ __device__ __forceinline__ void product_tile(const ProductShape& p, int m0, cons
   const unsigned b_bytes = S::COLUMNS ? 0 : (unsigned)imax(imin(p.N - n0[0], S::BN), 0) * b_pitch;
   const unsigned lds_ld = lds0 + wave * 1024;
   i32x4 ra, rb[2];
-  struct Stream {                                                  // the stage to ask for next: segment, first term, place in LDS
-    int seg = 0, k = 0, place;
+  const int per = (p.K + BK - 1) / BK;                             // stages of a segment
+  struct Stream {                                                  // the stage to ask for next: segment, first term, place in LDS; how many there are
+    int seg, k, place, left;
   } pa, pb;
+  pa.seg = p.first >= per ? p.first >= 2 * per ? 2 : 1 : 0;
+  pa.k = (p.first - pa.seg * per) * BK;
   pa.place = 0;
+  pa.left = p.stages;
+  pb = pa;
   pb.place = S::B_AT;
   auto scalar = [](i32x4 r) {
 #pragma unroll
@@ -101,19 +108,19 @@ __device__ __forceinline__ void product_tile(const ProductShape& p, int m0, cons
     return static_cast<const char*>(seg == 0 ? first : seg == 1 ? second : third);
   };
   auto open_a = [&]() {
-    ra = make_rsrc(pick(pa.seg, p.s[0].a, p.s[1].a, p.s[2].a) + (uint64_t)m0 * a_pitch, pa.seg < p.segments ? a_bytes : 0);
+    ra = make_rsrc(pick(pa.seg, p.s[0].a, p.s[1].a, p.s[2].a) + (uint64_t)m0 * a_pitch, pa.left > 0 ? a_bytes : 0);
   };
   auto open_b = [&]() {
     const char* const b0 = pick(pb.seg, p.s[0].b0, p.s[1].b0, p.s[2].b0);
     if constexpr (S::COLUMNS) {
-      rb[0] = make_rsrc(b0, 0);
-      rb[1] = make_rsrc(pick(pb.seg, p.s[0].b1, p.s[1].b1, p.s[2].b1), 0);
+      rb[0] = make_rsrc(b0 + (uint64_t)pb.k * b_pitch, 0);
+      rb[1] = make_rsrc(pick(pb.seg, p.s[0].b1, p.s[1].b1, p.s[2].b1) + (uint64_t)pb.k * b_pitch, 0);
     } else {
-      rb[0] = make_rsrc(b0 + (uint64_t)n0[0] * b_pitch, pb.seg < p.segments ? b_bytes : 0);
+      rb[0] = make_rsrc(b0 + (uint64_t)n0[0] * b_pitch, pb.left > 0 ? b_bytes : 0);
     }
   };
   auto open_terms = [&]() {                                        // columns: terms pb.k .. of the segment that are there
-    if constexpr (S::COLUMNS) rb[0][2] = rb[1][2] = (int)(pb.seg < p.segments ? (unsigned)imax(imin(p.terms - pb.k, BK), 0) * b_pitch : 0);
+    if constexpr (S::COLUMNS) rb[0][2] = rb[1][2] = (int)(pb.left > 0 ? (unsigned)imax(imin(p.terms - pb.k, BK), 0) * b_pitch : 0);
   };
   auto prefetch_a = [&](int l) {
     load_to_lds(scalar(ra), pa.k + 8 * chunk < p.K ? va[l] : OOB, 2u * pa.k, lds_ld + pa.place + l * S::NW * 1024);
@@ -127,9 +134,10 @@ __device__ __forceinline__ void product_tile(const ProductShape& p, int m0, cons
   auto advance_a = [&]() {
     pa.place = pa.place == 2 * S::A_BYTES ? 0 : pa.place + S::A_BYTES;
     pa.k += BK;
-    if (pa.k >= p.K) {
+    --pa.left;
+    if (pa.k >= p.K || pa.left <= 0) {
+      pa.k = 0;
       ++pa.seg;
-      if (pa.seg < p.segments) pa.k = 0;
       open_a();
     }
   };
@@ -144,9 +152,10 @@ __device__ __forceinline__ void product_tile(const ProductShape& p, int m0, cons
         rb[l][1] = (int)(uint32_t)(q >> 32);
       }
     }
-    if (pb.k >= p.K) {
+    --pb.left;
+    if (pb.k >= p.K || pb.left <= 0) {
+      pb.k = 0;
       ++pb.seg;
-      if (pb.seg < p.segments) pb.k = 0;
       open_b();
     }
     open_terms();
@@ -187,7 +196,6 @@ __device__ __forceinline__ void product_tile(const ProductShape& p, int m0, cons
     }
   };
 
-  const int stages = p.segments * ((p.K + BK - 1) / BK);
   open_a();
   open_b();
   open_terms();
@@ -214,7 +222,7 @@ __device__ __forceinline__ void product_tile(const ProductShape& p, int m0, cons
   constexpr bool SPLIT = S::TM > 4;
   constexpr int TURN = S::TM - AHEAD;                              // from this row on operands of the next k-step
   unsigned a_base = 0, b_base = 0;
-  for (int st = 0; st < stages; ++st) {
+  for (int st = 0; st < p.stages; ++st) {
     asm("" : "+s"(a_base), "+s"(b_base));
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {

@@ -258,20 +258,24 @@ dp_status dp_gated(const void* x, dp_dtype dt, int rows, int d, int f, const voi
 }
 
 size_t dp_gated_backward_workspace_bytes(dp_dtype dt, int rows, int d, int f, int d_out) {
-  (void)dt, (void)rows, (void)d, (void)f, (void)d_out;
-  return 0;
+  if (dt == DP_F32 || gated_shape(dt, rows, d, f, d_out) != DP_OK) return 0;
+  return gated_input_workspace(rows, d, f, d_out);
 }
 
 dp_status dp_gated_backward(const void* dy, const void* w_down, int d_out, const void* gate, const void* up, dp_dtype dt, int rows, int d,
                             int f, const void* w_gate, const void* w_up, dp_activation act, void* dgate, void* dup, void* dx, void* ws,
                             size_t ws_bytes, void* stream) {
-  (void)ws, (void)ws_bytes;
   const dp_status st = gated_shape(dt, rows, d, f, w_down ? d_out : d);
   if (st != DP_OK) return st;
   if (!act_ok(act) || !aligned(w_down, alignment(dt)) || !aligned(dx, alignment(dt))) return DP_ERR_INVALID_ARG;
   for (const void* p : {dy, gate, up, (const void*)dgate, (const void*)dup})
     if (!there(p, dt)) return DP_ERR_INVALID_ARG;
   if (dx && (!there(w_gate, dt) || !there(w_up, dt))) return DP_ERR_INVALID_ARG;
+  const size_t need = dx && dt != DP_F32 ? gated_input_workspace(rows, d, f, w_down ? d_out : d) : 0;
+  if (need) {
+    if (!ws || ws_bytes < need) return DP_ERR_WORKSPACE;
+    if (!aligned(ws, 16)) return DP_ERR_INVALID_ARG;
+  }
   GatedArgs a = {};
   a.dy = dy;
   a.w_down = w_down;
@@ -283,6 +287,7 @@ dp_status dp_gated_backward(const void* dy, const void* w_down, int d_out, const
   a.dgate = dgate;
   a.dup = dup;
   a.dx = dx;
+  a.partial = static_cast<float*>(ws);
   a.rows = rows;
   a.d = d;
   a.f = f;
