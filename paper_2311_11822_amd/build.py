@@ -15,7 +15,7 @@ PYCALL = os.path.join(HERE, "_pycall" + sysconfig.get_config_var("EXT_SUFFIX")) 
 PYCALL_BLOCK = os.path.join(HERE, "_pycall_block" + sysconfig.get_config_var("EXT_SUFFIX"))     # those around the linear layers
 SOURCES = ["dp_api.hip", "noise.hip", "clip.hip", "fp32_kernels.hip", "ghost.hip", "tn_gemm.hip", "grad_gemm.hip", "grad_packed.hip", "ghost_big.hip", "ghost_brief.hip", "bias.hip", "layerwise.hip", "kept.hip", "ghost_sample.hip", "perex_dma.hip", "perex_narrow.hip",
            "train_api.hip", "norm.hip", "attention.hip", "attention_grad.hip", "adamw.hip",
-           "step_api.hip", "heads.hip", "gated.hip", "gated_tiles.hip", "gated_few.hip", "muon.hip"]
+           "step_api.hip", "heads.hip", "gated.hip", "gated_tiles.hip", "gated_few.hip", "muon.hip", "muon_small.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]

@@ -10,6 +10,9 @@ constexpr int kMuonParts = 1024;           // partial sums of a tensor's square,
 constexpr int kMuonMostSide = 1 << 20, kMuonMostShort = 1 << 16;
 constexpr float kMuonMost = 15.f;          // values that 2^12 of still fit fp16
 
+constexpr int kMuonMostIterations = 32;
+constexpr int kMuonSmallTiles = 6;         // sixteens of the shorter side of matrices that one workgroup holds
+
 struct MuonTensor {
   float* param;
   const void* grad;
@@ -24,6 +27,9 @@ struct MuonArgs {
   const double* coefficients;              // HOST, [iterations][3]
 };
 
+// Matrices that one workgroup holds (muon_small.hip), of one run; they use no workspace.
+bool muon_is_small(int rows, int cols);
+dp_status launch_muon_small(const MuonTensor* tensors, int n, const MuonArgs& a, dp_dtype grad_dt, dp_dtype copy_dt, hipStream_t s);
 // Of one run of up to kMuonGroup matrices.
 size_t muon_workspace(const MuonTensor* tensors, int n);
 dp_status launch_muon(const MuonTensor* tensors, int n, const MuonArgs& a, dp_dtype grad_dt, dp_dtype copy_dt, void* ws, hipStream_t s);

@@ -106,19 +106,24 @@ dp_status muon_sizes(const dp_muon_tensor* tensors, int n) {
   return n <= 1 << 20 ? DP_OK : DP_ERR_UNSUPPORTED;
 }
 
-// The matrices in even runs of as many as travel together; weight decay and scale where the launcher wants what comes of them.
+// The matrices in runs of as many as travel together, those that one workgroup holds by themselves; weight decay and scale where the launcher
+// wants what comes of them.
 template <class F>
 dp_status muon_runs(const dp_muon_tensor* tensors, int n, F run) {
-  const int runs = (n + kMuonGroup - 1) / kMuonGroup, per = (n + runs - 1) / runs;
   MuonTensor t[kMuonGroup];
-  for (int first = 0; first < n; first += per) {
-    const int count = std::min(n, first + per) - first;
-    for (int i = 0; i < count; ++i) {
-      const dp_muon_tensor& from = tensors[first + i];
-      t[i] = {from.param, from.grad, from.m, from.copy, from.rows, from.cols, from.weight_decay, from.scale};
+  for (const bool small : {false, true}) {
+    int total = 0, done = 0, count = 0;
+    for (int i = 0; i < n; ++i) total += muon_is_small(tensors[i].rows, tensors[i].cols) == small;
+    const int runs = (total + kMuonGroup - 1) / kMuonGroup, per = total ? (total + runs - 1) / runs : 0;
+    for (int i = 0; i < n; ++i) {
+      const dp_muon_tensor& from = tensors[i];
+      if (muon_is_small(from.rows, from.cols) != small) continue;
+      t[count++] = {from.param, from.grad, from.m, from.copy, from.rows, from.cols, from.weight_decay, from.scale};
+      if (++done < total && count < per) continue;
+      const dp_status st = run(t, count, small);
+      if (st != DP_OK) return st;
+      count = 0;
     }
-    const dp_status st = run(t, count);
-    if (st != DP_OK) return st;
   }
   return DP_OK;
 }
@@ -127,16 +132,27 @@ dp_status muon_runs(const dp_muon_tensor* tensors, int n, F run) {
 bool muon_values_fit(const double* abc, int iterations) {
   double most = 1.;
   for (int k = 0; k < iterations; ++k) {
-    const double a = abc[3 * k], b = abc[3 * k + 1], c = abc[3 * k + 2];
-    if (!isfinite(a) || !isfinite(b) || !isfinite(c) || most * most > kMuonMost) return false;
+    const double a = abc[3 * k], b = abc[3 * k + 1], c = abc[3 * k + 2], end = most * most;
+    if (!isfinite(a) || !isfinite(b) || !isfinite(c) || end > kMuonMost) return false;
     double next = 0., poly = 0.;
-    for (int i = 0; i <= 4096; ++i) {
-      const double x = most * i / 4096., s = x * x, p = a + s * (b + c * s);
+    auto at = [&](double s) {                          // s = x^2
+      if (!(s >= 0. && s <= end)) return;
+      const double p = a + s * (b + c * s);
       poly = std::max(poly, fabs(p));
-      next = std::max(next, fabs(x * p));
+      next = std::max(next, sqrt(s) * fabs(p));
+    };
+    at(0.);
+    at(end);
+    if (c != 0.) {
+      at(-b / (2. * c));                               // where the polynomial of A turns, and where x's does: a + 3 b s + 5 c s^2 = 0
+      const double root = sqrt(std::max(0., 9. * b * b - 20. * a * c));
+      at((-3. * b + root) / (10. * c));
+      at((-3. * b - root) / (10. * c));
+    } else if (b != 0.) {
+      at(-a / (3. * b));
     }
-    if (poly > kMuonMost || next > kMuonMost) return false;
-    most = next * 1.001;                               // between the points
+    if (!(poly <= kMuonMost && next <= kMuonMost)) return false;
+    most = next * 1.001;                               // what rounding adds
   }
   return true;
 }
@@ -298,8 +314,8 @@ dp_status dp_gated_backward(const void* dy, const void* w_down, int d_out, const
 size_t dp_muon_workspace_bytes(const dp_muon_tensor* tensors, int n_tensors) {
   if (muon_sizes(tensors, n_tensors) != DP_OK) return 0;
   size_t most = 0;
-  muon_runs(tensors, n_tensors, [&](const MuonTensor* run, int n) {
-    most = std::max(most, muon_workspace(run, n));
+  muon_runs(tensors, n_tensors, [&](const MuonTensor* run, int n, bool small) {
+    most = std::max(most, small ? (size_t)16 : muon_workspace(run, n));
     return DP_OK;
   });
   return most;
@@ -307,7 +323,7 @@ size_t dp_muon_workspace_bytes(const dp_muon_tensor* tensors, int n_tensors) {
 
 dp_status dp_muon_multi(const dp_muon_tensor* tensors, int n_tensors, dp_dtype grad_dt, dp_dtype copy_dt, double lr, double beta, int nesterov,
                         double grad_scale, double eps, const double* coefficients, int iterations, void* ws, size_t ws_bytes, void* stream) {
-  if (!dtype_ok(grad_dt) || !dtype_ok(copy_dt) || !coefficients || iterations < 1 || iterations > 32) return DP_ERR_INVALID_ARG;
+  if (!dtype_ok(grad_dt) || !dtype_ok(copy_dt) || !coefficients || iterations < 1 || iterations > kMuonMostIterations) return DP_ERR_INVALID_ARG;
   if (nesterov != 0 && nesterov != 1) return DP_ERR_INVALID_ARG;
   if (!(lr >= 0.) || isinf(lr) || !(beta >= 0. && beta < 1.) || !(eps >= 0.) || isinf(eps) || !isfinite(grad_scale)) return DP_ERR_INVALID_ARG;
   dp_status st = muon_sizes(tensors, n_tensors);
@@ -329,8 +345,9 @@ dp_status dp_muon_multi(const dp_muon_tensor* tensors, int n_tensors, dp_dtype g
   a.eps = (float)eps;
   a.iterations = iterations;
   a.coefficients = coefficients;
-  return muon_runs(tensors, n_tensors, [&](MuonTensor* run, int n) {
+  return muon_runs(tensors, n_tensors, [&](MuonTensor* run, int n, bool small) {
     for (int i = 0; i < n; ++i) run[i].keep = (float)(1. - lr * (double)run[i].keep), run[i].rate = (float)(lr * (double)run[i].rate);
+    if (small) return launch_muon_small(run, n, a, grad_dt, copy_dt, static_cast<hipStream_t>(stream));
     return launch_muon(run, n, a, grad_dt, copy_dt, ws, static_cast<hipStream_t>(stream));
   });
 }

@@ -231,9 +231,11 @@ def test_muon_refuses_polynomials(abc):
 
 def test_muon_workspace_is_of_one_run():
     """Matrices go in runs of up to 64: the workspace is the largest run's."""
-    one = [(None, None, None, None, 64, 128, 0.0, 1.0)]
+    one = [(None, None, None, None, 128, 160, 0.0, 1.0)]
     assert dp.dp_muon_workspace_bytes(one * 64) == 64 * dp.dp_muon_workspace_bytes(one)
     assert dp.dp_muon_workspace_bytes(one * 90) == 45 * dp.dp_muon_workspace_bytes(one)
+    small = [(None, None, None, None, 24, 72, 0.0, 1.0)]              # those that one workgroup holds need next to none
+    assert 0 < dp.dp_muon_workspace_bytes(small * 3) <= 256 and dp.dp_muon_workspace_bytes(small * 70 + one) == dp.dp_muon_workspace_bytes(one)
 
 
 def test_muon_object_refuses():
