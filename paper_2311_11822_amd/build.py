@@ -21,10 +21,11 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 # The gradient kernel's epilogue with noise is 16 copies of a large body; beyond the default size
 # limit the compiler stops honouring "#pragma unroll", the accumulator indices stay variable
-# and the 256 accumulators move to scratch memory.
+# and the 256 accumulators move to scratch memory.  Likewise product.h's tiles, whose stages are unrolled over all accumulators.
 # Where the packed rows' loop begins in memory moves the narrow tiles by 5 % (24 layers 768 x 16, 512 x 32 tokens: 257 us at a
 # multiple of 64 bytes, up to 272 elsewhere).
-PER_FILE_FLAGS = {"grad_gemm.hip": ["-mllvm", "-pragma-unroll-threshold=1000000"], "gated_tiles.hip": ["-mllvm", "-pragma-unroll-threshold=1000000"], "grad_packed.hip": ["-falign-loops=64"]}
+PER_FILE_FLAGS = {"grad_gemm.hip": ["-mllvm", "-pragma-unroll-threshold=1000000"], "gated_tiles.hip": ["-mllvm", "-pragma-unroll-threshold=1000000"],
+                  "muon.hip": ["-mllvm", "-pragma-unroll-threshold=1000000"], "grad_packed.hip": ["-falign-loops=64"]}
 
 
 def build(verbose: bool = False) -> str:

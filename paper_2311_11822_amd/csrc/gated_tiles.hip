@@ -77,7 +77,6 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) gated_tile_kerne
   if constexpr (PASS == kHidden) p.s[0] = {a.dy, a.w_down, nullptr};
   if constexpr (PASS == kInput) p.s[0] = {a.dgate, a.w_gate, nullptr};
   p.s[1] = PASS == kInput ? ProductSegment{a.dup, a.w_up, nullptr} : p.s[0];
-  p.s[2] = p.s[0];
   const int tiles = tiles_m * tiles_n, id = grad_logical_tile(blockIdx.x, tiles * parts);
   int tm, tn, part = 0;
   if constexpr (PASS == kInput) part = id / tiles;
@@ -85,7 +84,7 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) gated_tile_kerne
   const int64_t stages = p.segments * ((p.K + kProductTerms - 1) / kProductTerms);
   p.first = (int)(part * stages / parts);
   p.stages = (int)((part + 1) * stages / parts) - p.first;
-  const int m0 = tm * S::BM, n = tn * (S::COLUMNS ? S::BN / 2 : S::BN), n0[2] = {n, n};
+  const int m0 = tm * S::BM, n = tn * (S::SETS ? S::BN / 2 : S::BN), n0[2] = {n, n};
   f32x4 acc[S::TM][S::TN];
   product_tile<S, DT == DP_F16>(p, m0, n0, lds0, acc);
   auto place = [&](int row, int col) { return (int64_t)(m0 + row) * p.N + n + col; };
@@ -143,7 +142,7 @@ dp_status launch_tiles(const GatedArgs& a, int parts, hipStream_t s) {
   static ReadyTable ready;
   dp_status st = allow_big_lds(gated_tile_kernel<PASS, S, DT>, S::LDS_BYTES, ready);
   if (st != DP_OK) return st;
-  const int N = PASS == kInput ? a.d : a.f, width = S::COLUMNS ? S::BN / 2 : S::BN;
+  const int N = PASS == kInput ? a.d : a.f, width = S::SETS ? S::BN / 2 : S::BN;
   const int tiles_m = (a.rows + S::BM - 1) / S::BM, tiles_n = (N + width - 1) / width;
   gated_tile_kernel<PASS, S, DT><<<dim3((unsigned)tiles_m * tiles_n * parts), S::NT, S::LDS_BYTES, s>>>(a, tiles_m, tiles_n, parts);
   st = hip_status(hipGetLastError());
@@ -197,10 +196,10 @@ Choice choose(GatedPass pass, int rows, int d, int f, int d_out) {
 
 template <int PASS, int DT>
 dp_status launch_pass(const GatedArgs& a, hipStream_t s) {
-  constexpr bool COLUMNS = PASS == kForward;
+  constexpr ProductB B = PASS == kForward ? kColumnSets : kRowsOfTerms;
   const Choice c = choose((GatedPass)PASS, a.rows, a.d, a.f, a.d_out);
   if (c.few) return launch_gated_few(a, (dp_dtype)DT, (GatedPass)PASS, s);
-  return c.large ? launch_tiles<PASS, BigProduct<COLUMNS>, DT>(a, 1, s) : launch_tiles<PASS, MidProduct<COLUMNS>, DT>(a, c.parts, s);
+  return c.large ? launch_tiles<PASS, BigProduct<B>, DT>(a, 1, s) : launch_tiles<PASS, MidProduct<B>, DT>(a, c.parts, s);
 }
 
 }  // namespace

@@ -4,8 +4,8 @@
 // X is taken with its shorter side as rows (turned on the way in and out), so A is the smaller square.
 //
 // Products as exact as fp32's at the rate of 16-bit ones: a value v is kept as two fp16 numbers, h = fp16(2^12 v) and l = fp16(2^12 v - h),
-// together within 2^-23 of v (2^-37 of 1 where v is next to nothing), and h h' + h l' + l h' are three segments of one contraction in fp32; l l',
-// 2^-24 of it, is left out.  2^12 keeps the halves of entries from 2^-15 up out of fp16's subnormal range; entries are bounded by singular
+// together within 2^-23 of v (2^-37 of 1 where v is next to nothing), and h h' + h l' + l h' is added up in fp32; l l', 2^-24 of it, is left
+// out.  A row is blocks of 32 columns, 32 h and 32 l, a line each (product.h).  2^12 keeps the halves of entries from 2^-15 up out of fp16's subnormal range; entries are bounded by singular
 // values, which the host has followed through the polynomials.  (fp32 matrix instructions have 1/16 of the 16-bit rate, a third of it 1/3.)
 // A, the square and the polynomial of A are symmetric: tiles on and above the diagonal are formed, and leave turned as well.
 // Matrices travel together: a launch does one step of up to 64 of them.
@@ -29,7 +29,7 @@ struct Matrix {
   const void* grad;
   float* momentum;
   void* copy;
-  _Float16 *x[2], *gram, *poly;                      // [2 (h, l)][m][n or m, to multiples of 8]
+  _Float16 *x[2], *gram, *poly;                      // [m][n or m, to a multiple of 32][2]: 32 h, 32 l, 32 h ...
   int rows, cols;
   float keep, rate;
   int parts;                                         // partial sums of |u|^2, at `partial`
@@ -44,7 +44,9 @@ struct Group {
   Matrix t[kMuonGroup];
 };
 
-__host__ __device__ inline int eights(int n) { return (n + 7) & ~7; }
+__host__ __device__ inline int blocks_of(int n) { return (n + 31) & ~31; }
+// Where h of a row's column is; l is 32 on.
+__host__ __device__ inline int64_t half_at(int row, int col, int width) { return (int64_t)row * 2 * width + (col >> 5) * 64 + (col & 31); }
 __host__ __device__ inline int64_t part_values(int64_t size) {
   const int64_t per = (size + kMuonParts - 1) / kMuonParts;
   return per < 4096 ? 4096 : (per + 1023) / 1024 * 1024;
@@ -99,7 +101,7 @@ __global__ void __launch_bounds__(kThreads) muon_start_kernel(const Group g) {
   __shared__ float red[kThreads / 64], tile[kSide][kSide + 1];
   const Matrix& t = g.t[owner(g, blockIdx.x)];
   const bool turned = t.rows > t.cols;
-  const int m = turned ? t.cols : t.rows, n = turned ? t.rows : t.cols, pitch = eights(n), across = (pitch + kSide - 1) / kSide;
+  const int m = turned ? t.cols : t.rows, n = turned ? t.rows : t.cols, pitch = blocks_of(n), across = (pitch + kSide - 1) / kSide;
   float sum = 0.f;
   for (int i = threadIdx.x; i < t.parts; i += kThreads) sum += t.partial[i];
   const float norm = sqrtf(block_sum(sum, red)) + g.eps;            // (0: all of u is, and X with it)
@@ -122,8 +124,9 @@ __global__ void __launch_bounds__(kThreads) muon_start_kernel(const Group g) {
     if (r < m && c < pitch) {
       const float u = turned ? tile[lane][k] : tile[k][lane];
       const Halves v(norm == 0.f ? 0.f : u / norm * kScale);
-      x[(int64_t)r * pitch + c] = v.h;
-      x[(int64_t)(m + r) * pitch + c] = v.l;
+      const int64_t at = half_at(r, c, pitch);
+      x[at] = v.h;
+      x[at + 32] = v.l;
     }
   }
 }
@@ -134,13 +137,16 @@ __global__ void __launch_bounds__(kThreads) muon_apply_kernel(const Group g) {
   __shared__ float tile[kSide][kSide + 1];
   const Matrix& t = g.t[owner(g, blockIdx.x)];
   const bool turned = t.rows > t.cols;
-  const int m = turned ? t.cols : t.rows, n = turned ? t.rows : t.cols, pitch = eights(n), across = (n + kSide - 1) / kSide;
+  const int m = turned ? t.cols : t.rows, n = turned ? t.rows : t.cols, pitch = blocks_of(n), across = (n + kSide - 1) / kSide;
   const int id = blockIdx.x - t.begin, r0 = id / across * kSide, c0 = (id - id / across * across) * kSide;       // of X
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const _Float16* const x = t.x[g.from];
   for (int k = wave; k < kSide; k += kThreads / 64) {
     const int r = r0 + k, c = c0 + lane;
-    if (r < m && c < n) tile[k][lane] = ((float)x[(int64_t)r * pitch + c] + (float)x[(int64_t)(m + r) * pitch + c]) * (1.f / kScale);
+    if (r < m && c < n) {
+      const int64_t at = half_at(r, c, pitch);
+      tile[k][lane] = ((float)x[at] + (float)x[at + 32]) * (1.f / kScale);
+    }
   }
   __syncthreads();
   for (int k = wave; k < kSide; k += kThreads / 64) {
@@ -167,7 +173,7 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) muon_product_ker
   const unsigned lds0 = (unsigned)(uintptr_t)lds_raw;
   const int logical = grad_logical_tile(blockIdx.x, total);
   const Matrix& t = g.t[owner(g, logical)];
-  const int m = imin(t.rows, t.cols), n = imax(t.rows, t.cols), mp = eights(m), np = eights(n);
+  const int m = imin(t.rows, t.cols), mp = blocks_of(m), np = blocks_of(imax(t.rows, t.cols));
   const int tiles_m = (m + S::BM - 1) / S::BM;
   int tm, tn, rest = logical - (int)t.begin;
   if constexpr (STEP == kUpdate) {
@@ -176,32 +182,28 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) muon_product_ker
     for (tm = 0; rest >= tiles_m - tm; ++tm) rest -= tiles_m - tm;
     tn = tm + rest;
   }
-  const int m0 = tm * S::BM, n0[2] = {tn * S::BN, tn * S::BN + (STEP == kUpdate ? S::BN / 2 : 0)};
+  const int m0 = tm * S::BM, n = tn * S::BN, n0[2] = {n, n};
   const _Float16 *a, *b;
   ProductShape p;
   p.M = m;
-  p.segments = 3;
+  p.N = STEP == kUpdate ? np : m;
+  p.segments = 1;
+  p.terms = m;
+  p.first = 0;
   if constexpr (STEP == kGram) {
     a = b = t.x[g.from];
-    p.N = m;
-    p.K = p.lda = p.ldb = np;
+    p.K = p.lda = p.ldb = 2 * np;
   } else if constexpr (STEP == kPoly) {
     a = b = t.gram;
-    p.N = m;
-    p.K = p.lda = p.ldb = mp;
+    p.K = p.lda = p.ldb = 2 * mp;
   } else {
     a = t.poly;
     b = t.x[g.from];
-    p.N = p.ldb = np;
-    p.K = p.lda = mp;
+    p.ldb = 2 * np;
+    p.K = p.lda = 2 * mp;
   }
-  p.terms = m;
-  p.first = 0;
-  p.stages = 3 * ((p.K + kProductTerms - 1) / kProductTerms);
-  const _Float16 *al = a + (int64_t)m * p.lda, *bl = b + (int64_t)m * p.ldb;
-  p.s[0] = {a, b, b};
-  p.s[1] = {a, bl, bl};
-  p.s[2] = {al, b, b};
+  p.stages = p.K / kProductTerms;
+  p.s[0] = p.s[1] = {a, b, b};
   f32x4 acc[S::TM][S::TN];
   product_tile<S, true>(p, m0, n0, lds0, acc);
   _Float16* const out = STEP == kGram ? t.gram : STEP == kPoly ? t.poly : t.x[1 - g.from];
@@ -214,14 +216,15 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) muon_product_ker
       h[k] = w.h;
       l[k] = w.l;
     }
-    *reinterpret_cast<f16x8*>(out + (int64_t)row * pitch + col) = h;
-    *reinterpret_cast<f16x8*>(out + (int64_t)(m + row) * pitch + col) = l;
+    f16x8* const to = reinterpret_cast<f16x8*>(out + half_at(row, col, pitch));
+    to[0] = h;
+    to[4] = l;
   };
   // what is stored of eight values of the product
   auto finish = [&](int row, int col, const float (&acc8)[8], float (&v)[8]) {
     if constexpr (STEP == kPoly) {
-      const f16x8 h = *reinterpret_cast<const f16x8*>(t.gram + (int64_t)row * mp + col);
-      const f16x8 l = *reinterpret_cast<const f16x8*>(t.gram + (int64_t)(m + row) * mp + col);
+      const f16x8* const from = reinterpret_cast<const f16x8*>(t.gram + half_at(row, col, mp));
+      const f16x8 h = from[0], l = from[4];
 #pragma unroll
       for (int k = 0; k < 8; ++k)
         v[k] = fmaf(g.c / kScale, acc8[k], g.b * ((float)h[k] + (float)l[k])) + (row == col + k ? g.a * kScale : 0.f);
@@ -230,8 +233,8 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) muon_product_ker
       for (int k = 0; k < 8; ++k) v[k] = acc8[k] * (1.f / kScale);
     }
   };
-  auto store = [&](int row, int col, int set, const float (&acc8)[2][8], Nothing) {
-    const int r = m0 + row, c = n0[set] + col;
+  auto store = [&](int row, int col, int, const float (&acc8)[2][8], Nothing) {
+    const int r = m0 + row, c = n + col;
     if (r >= m || c >= pitch) return;
     float v[8];
     finish(r, c, acc8[0], v);
@@ -242,7 +245,7 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) muon_product_ker
   } else {
     // below the diagonal: rows of the tile's columns
     auto across = [&](int row, int col, const float (&acc8)[8]) {
-      const int r = n0[0] + col, c = m0 + row;
+      const int r = n + col, c = m0 + row;
       if (r >= m || c >= mp) return;
       float v[8];
       finish(r, c, acc8, v);
@@ -264,7 +267,7 @@ unsigned lay_out(Group& g, F workgroups) {
 
 template <int STEP, int SIDE>
 int64_t tiles_of(const Matrix& t) {
-  const int64_t m = std::min(t.rows, t.cols), n = eights(std::max(t.rows, t.cols)), tm = (m + SIDE - 1) / SIDE;
+  const int64_t m = std::min(t.rows, t.cols), n = blocks_of(std::max(t.rows, t.cols)), tm = (m + SIDE - 1) / SIDE;
   return STEP == kUpdate ? tm * ((n + SIDE - 1) / SIDE) : tm * (tm + 1) / 2;
 }
 
@@ -283,29 +286,29 @@ dp_status launch_product(Group& g, hipStream_t s) {
 // are resident, and some of the longest besides.
 template <int STEP>
 dp_status launch_step(Group& g, hipStream_t s) {
-  constexpr bool COLUMNS = STEP == kUpdate;
+  constexpr ProductB B = STEP == kUpdate ? kSplitColumns : kRowsOfTerms;
   auto cost = [&](auto tiles, float stage, float rest, float resident) {
     float sum = 0.f, longest = 0.f;
     int64_t n = 0;
     for (int i = 0; i < g.n; ++i) {
       const Matrix& t = g.t[i];
       const int k = STEP == kGram ? std::max(t.rows, t.cols) : std::min(t.rows, t.cols);
-      const float one = (float)(3 * ((k + 63) / 64)) * stage + rest;
+      const float one = (float)((k + 31) / 32) * stage + rest;
       sum += (float)tiles(t) * one;
       longest = std::max(longest, one);
       n += tiles(t);
     }
     return (float)n <= resident ? longest : sum / resident + longest / 2;
   };
-  const float big = cost(tiles_of<STEP, 256>, 1.5f, STEP == kUpdate ? 12.f : 30.f, 256.f);
-  const float mid = cost(tiles_of<STEP, 128>, 0.85f, STEP == kUpdate ? 10.f : 18.f, 512.f);
-  return big <= mid ? launch_product<STEP, BigProduct<COLUMNS>>(g, s) : launch_product<STEP, MidProduct<COLUMNS>>(g, s);
+  const float big = cost(tiles_of<STEP, 256>, 2.2f, STEP == kUpdate ? 12.f : 30.f, 256.f);
+  const float mid = cost(tiles_of<STEP, 128>, 1.2f, STEP == kUpdate ? 10.f : 18.f, 512.f);
+  return big <= mid ? launch_product<STEP, BigProduct<B, true>>(g, s) : launch_product<STEP, MidProduct<B, true>>(g, s);
 }
 
 // Bytes of a matrix's two X, A, polynomial and partial sums.
 size_t matrix_bytes(int rows, int cols, size_t (&at)[5]) {
   const int64_t m = std::min(rows, cols), n = std::max(rows, cols);
-  const size_t x = (size_t)4 * m * eights((int)n), square = (size_t)4 * m * eights((int)m), sizes[5] = {x, x, square, square, kMuonParts * 4};
+  const size_t x = (size_t)4 * m * blocks_of((int)n), square = (size_t)4 * m * blocks_of((int)m), sizes[5] = {x, x, square, square, kMuonParts * 4};
   size_t total = 0;
   for (int i = 0; i < 5; ++i) {
     at[i] = total;
@@ -366,7 +369,7 @@ dp_status launch_muon(const MuonTensor* tensors, int n, const MuonArgs& a, dp_dt
   if (st != DP_OK) return st;
   auto squares = [](const Matrix& t, bool padded) {
     const int64_t m = std::min(t.rows, t.cols), c = std::max(t.rows, t.cols);
-    return ((m + kSide - 1) / kSide) * (((padded ? eights((int)c) : c) + kSide - 1) / kSide);
+    return ((m + kSide - 1) / kSide) * (((padded ? blocks_of((int)c) : c) + kSide - 1) / kSide);
   };
   total = lay_out(g, [&](const Matrix& t) { return squares(t, true); });
   st = launch(grad_dt == DP_F32 ? muon_start_kernel<DP_F32> : grad_dt == DP_BF16 ? muon_start_kernel<DP_BF16> : muon_start_kernel<DP_F16>, total);

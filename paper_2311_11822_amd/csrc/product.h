@@ -1,7 +1,8 @@
-// Tiles of products on the 16-bit matrix instructions:  acc[m, n] = sum_s sum_k A_s[m, k] B_s[k, n]  over up to three segments s.
+// Tiles of products on the 16-bit matrix instructions:  acc[m, n] = sum_s sum_k A_s[m, k] B_s[k, n]  over up to two segments s; and, of values that
+// are two fp16 halves h + l each, with all of it but l l'.
 //
-// A has its terms adjacent ([m][k]); B as well ([n][k], "rows"), or its columns ([k][n], "columns": two sets of them side by side, each with
-// its own origin, which is how a gate and its factor meet in one lane).
+// A has its terms adjacent ([m][k]); B as well ([n][k], "rows"), or its columns ([k][n]): two sets of them side by side, each with its own
+// origin, which is how a gate and its factor meet in one lane ("sets"), or one of values in halves ("split").
 //  * 256 x 256 tiles by eight waves of 128 x 64, or 128 x 128 by four of 64 x 64 (two workgroups to a compute unit).  Accumulators and
 //    operands of one k-step and the next lie in registers.
 //  * memory -> LDS without registers (16 bytes a lane), stages of 64 terms: whole 128-byte lines of [m][k] rows.  (Stages of 32, five of
@@ -10,9 +11,12 @@
 //    registers, half a stage before A's, so B's loads have 1.4 stages to land and A's two.
 //    Two barriers to a stage of the large tiles: M, behind the last read of B; E, behind the last one of A, where the next stage has landed.
 //  * LDS holds [m][64 k] in rows of 128 bytes: a 128-bit read takes sixteen lanes at a time, here sixteen rows at one place of eight, so that
-//    place is XORed with row / 2 and all banks are met.  [k][n] halves have rows of 256 or 128 bytes; the transposing read takes four
-//    rows of 64 bytes at a time, which the XOR by k spreads over the four groups of banks.
+//    place is XORed with row / 2 and all banks are met.  [k][n] rows are of 128 to 1024 bytes; the transposing read takes eight rows of 32
+//    bytes at a time, which the XOR by k spreads over all banks.
 //  * rows, columns and terms past the end arrive as zeros: by the descriptor's size, or by an offset past it.
+//  * Halves: 32 terms are a line of 32 h and 32 l, so a stage is 32 terms of both, and its operands are read once for the three products of
+//    a term.  (As three segments of a product, h h', h l' and l h', everything was read one and a half times: A of 60 matrices of 768 rows,
+//    340 MB, 267 us.)
 // The first operand of an instruction is B's: a lane has one row of the result and four adjacent columns to a register quad.
 #pragma once
 
@@ -25,250 +29,337 @@
 namespace dpbk {
 
 struct ProductSegment {
-  const void *a, *b0, *b1;          // b1: the second set's columns (columns only)
+  const void *a, *b0, *b1;          // b1: the second set's columns (sets only)
 };
 constexpr int kProductTerms = 64;   // of a stage
+constexpr int kHalfTerms = 32;      // of one of values in halves
 struct ProductShape {
-  int M, N, K;                      // K: of a segment; K and N (columns) are multiples of 8
-  int terms;                        // columns: rows of B that are there (K or fewer: A has zeros beyond)
-  int lda, ldb;                     // elements from one row (of columns: term) to the next
+  int M, N, K;                      // K: of a segment, in 16-bit values (halves: both); K and N (columns) are multiples of 8
+  int terms;                        // columns: rows of B that are there (fewer than A has terms: A has zeros beyond)
+  int lda, ldb;                     // 16-bit values from one row (of columns: term) to the next
   int segments;
   int first, stages;                // of all segments' stages one behind the other, those that this tile takes
-  ProductSegment s[3];
+  ProductSegment s[2];
 };
 
-template <int BM_, int WM_, int WN_, bool COLUMNS_>
+enum ProductB { kRowsOfTerms, kColumnSets, kSplitColumns };
+template <int BM_, int WM_, int WN_, ProductB B_, bool HALVES_ = false>
 struct ProductTile {
   static constexpr int BM = BM_, BN = BM_, BK = kProductTerms, A_PLACES = 3, B_PLACES = 2, WM = WM_, WN = WN_, NW = WM * WN, NT = 64 * NW;
-  static constexpr bool COLUMNS = COLUMNS_;
+  static constexpr bool HALVES = HALVES_, SETS = B_ == kColumnSets, SPLIT = B_ == kSplitColumns, ROWS = B_ == kRowsOfTerms;
   static constexpr int WTM = BM / WM, WTN = BN / WN, TM = WTM / 16, TN = WTN / 16;       // 16 x 16 results of a wave
   static constexpr int ROW_BYTES = 2 * BK, A_BYTES = BM * ROW_BYTES, B_BYTES = BN * ROW_BYTES;
   static constexpr int B_AT = A_PLACES * A_BYTES;                              // of B's first place
-  static constexpr int HALF_BYTES = B_BYTES / 2, COL_BYTES = BN;               // a term's columns of one set
+  static constexpr int TERMS = HALVES ? kHalfTerms : BK;                       // of a stage
+  static constexpr int HALF_BYTES = B_BYTES / 2;                               // sets: of one of them
+  static constexpr int COL_BYTES = SPLIT ? 4 * BN : BN;                        // columns: a term's, of one set or of both halves
   static constexpr int LDS_BYTES = B_AT + B_PLACES * B_BYTES, LOADS = A_BYTES / (NW * 1024);     // of an operand, wave and stage
   // epilogue: 32 rows of a wave's columns, fp32
   static constexpr int SLAB_PITCH = WTN + 4, SLAB_BYTES = 32 * SLAB_PITCH * 4;
   // columns: the 16-byte place of a term's row is XORed with this
   __device__ static constexpr unsigned spread(unsigned k) {
-    return COL_BYTES == 256 ? (k & 3) << 2 | (k >> 2 & 2) : (k & 2) << 1 | (k >> 2 & 2);
+    return COL_BYTES >= 256 ? (k & 3) << 2 | (k >> 2 & 2) : (k & 2) << 1 | (k >> 2 & 2);
   }
   static_assert(LOADS * NW * 1024 == A_BYTES && LOADS % 2 == 0 && NW * SLAB_BYTES <= LDS_BYTES, "load split, fragments, epilogue");
+  static_assert(HALVES != SETS && HALVES >= SPLIT || !HALVES, "what there is");
 };
-template <bool COLUMNS>
-using BigProduct = ProductTile<256, 2, 4, COLUMNS>;
-template <bool COLUMNS>
-using MidProduct = ProductTile<128, 2, 2, COLUMNS>;
+template <ProductB B, bool HALVES = false>
+using BigProduct = ProductTile<256, 2, 4, B, HALVES>;
+template <ProductB B, bool HALVES = false>
+using MidProduct = ProductTile<128, 2, 2, B, HALVES>;
 
-// The tile at (m0, n0) (columns: of either set n0[0], n0[1]) into acc.  acc[x][y], lane, register r: row 16 x + lane % 16 of the wave's, column
-// 16 y + 4 (lane / 16) + r of its WTN: those of the tile from WTN (wave % WN) on, or half as many of each set.
-template <class S, bool F16>
-__device__ __forceinline__ void product_tile(const ProductShape& p, int m0, const int (&n0)[2], unsigned lds0, f32x4 (&acc)[S::TM][S::TN]) {
-  constexpr int BK = S::BK;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-
-  // ---- memory -> LDS
-  const int chunk = (lane & 7) ^ ((4 * (wave & 1) + (lane >> 4)) & 7);         // 16-byte piece of a row's 64 terms
-  const unsigned a_pitch = 2u * p.lda, b_pitch = 2u * p.ldb;
-  unsigned va[S::LOADS], vb[S::LOADS];
-#pragma unroll
-  for (int l = 0; l < S::LOADS; ++l) {
-    const unsigned row = 8 * (l * S::NW + wave) + (lane >> 3);
-    va[l] = row * a_pitch + chunk * 16;
-    if constexpr (S::COLUMNS) {
-      constexpr int PIECES = S::COL_BYTES / 16;
-      const unsigned k = (l % (S::LOADS / 2) * S::NW + wave) * (1024 / S::COL_BYTES) + lane / PIECES, at = lane % PIECES;
-      const unsigned c = at ^ S::spread(k);
-      const int col = n0[l / (S::LOADS / 2)] + 8 * (int)c;
-      vb[l] = col < p.N ? k * b_pitch + 2u * col : OOB;
-    } else {
-      vb[l] = row * b_pitch + chunk * 16;
-    }
-  }
-  const unsigned a_bytes = (unsigned)imin(p.M - m0, S::BM) * a_pitch;
-  const unsigned b_bytes = S::COLUMNS ? 0 : (unsigned)imax(imin(p.N - n0[0], S::BN), 0) * b_pitch;
-  const unsigned lds_ld = lds0 + wave * 1024;
-  i32x4 ra, rb[2];
-  const int per = (p.K + BK - 1) / BK;                             // stages of a segment
-  struct Stream {                                                  // the stage to ask for next: segment, first term, place in LDS; how many there are
+// Memory -> LDS: the stages of A and of B, each a stream of its own.
+template <class S>
+struct ProductLoads {
+  struct Stream {                   // the stage to ask for next: segment, first value or term of it, place in LDS; how many there are
     int seg, k, place, left;
-  } pa, pb;
-  pa.seg = p.first >= per ? p.first >= 2 * per ? 2 : 1 : 0;
-  pa.k = (p.first - pa.seg * per) * BK;
-  pa.place = 0;
-  pa.left = p.stages;
-  pb = pa;
-  pb.place = S::B_AT;
-  auto scalar = [](i32x4 r) {
+  };
+  const ProductShape& p;
+  int m0, chunk;
+  unsigned n_off, a_pitch, b_pitch, a_bytes, b_bytes, lds_ld;
+  unsigned va[S::LOADS], vb[S::LOADS];
+  i32x4 ra, rb[2];
+  Stream a, b;
+
+  __device__ static __forceinline__ i32x4 scalar(i32x4 r) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_readfirstlane(r[i]);
     return r;
-  };
-  auto pick = [&](int seg, const void* first, const void* second, const void* third) {         // (an index would put them in memory)
-    return static_cast<const char*>(seg == 0 ? first : seg == 1 ? second : third);
-  };
-  auto open_a = [&]() {
-    ra = make_rsrc(pick(pa.seg, p.s[0].a, p.s[1].a, p.s[2].a) + (uint64_t)m0 * a_pitch, pa.left > 0 ? a_bytes : 0);
-  };
-  auto open_b = [&]() {
-    const char* const b0 = pick(pb.seg, p.s[0].b0, p.s[1].b0, p.s[2].b0);
-    if constexpr (S::COLUMNS) {
-      rb[0] = make_rsrc(b0 + (uint64_t)pb.k * b_pitch, 0);
-      rb[1] = make_rsrc(pick(pb.seg, p.s[0].b1, p.s[1].b1, p.s[2].b1) + (uint64_t)pb.k * b_pitch, 0);
-    } else {
-      rb[0] = make_rsrc(b0 + (uint64_t)n0[0] * b_pitch, pb.left > 0 ? b_bytes : 0);
+  }
+  __device__ static __forceinline__ unsigned scalar(unsigned x) { return __builtin_amdgcn_readfirstlane(x); }
+  __device__ static __forceinline__ const char* pick(int seg, const void* first, const void* second) {
+    return static_cast<const char*>(seg == 0 ? first : second);                // (an index would put them in memory)
+  }
+  __device__ __forceinline__ ProductLoads(const ProductShape& shape, int m, const int (&n0)[2], unsigned lds0, int wave, int lane) : p(shape), m0(m) {
+    chunk = (lane & 7) ^ ((4 * (wave & 1) + (lane >> 4)) & 7);                 // 16-byte piece of a row's stage
+    a_pitch = 2u * p.lda;
+    b_pitch = 2u * p.ldb;
+    n_off = n0[0];
+#pragma unroll
+    for (int l = 0; l < S::LOADS; ++l) {
+      const unsigned row = 8 * (l * S::NW + wave) + (lane >> 3);
+      va[l] = row * a_pitch + chunk * 16;
+      if constexpr (S::ROWS) {
+        vb[l] = row * b_pitch + chunk * 16;
+      } else {
+        // 1 KiB of LDS: some terms' rows (of one set), or one
+        constexpr int PIECES = S::COL_BYTES / 16, SET_LOADS = S::SETS ? S::LOADS / 2 : S::LOADS;
+        const unsigned k = PIECES <= 64 ? (l % SET_LOADS * S::NW + wave) * (64 / PIECES) + lane / PIECES : 0, at = lane % PIECES;
+        const unsigned piece = at ^ S::spread(k), value = S::SETS ? n0[l / SET_LOADS] + 8 * piece : 2 * n0[0] + 8 * piece;
+        vb[l] = (int)value < (S::SPLIT ? p.ldb : p.N) ? k * b_pitch + 2 * value : OOB;
+      }
     }
-  };
-  auto open_terms = [&]() {                                        // columns: terms pb.k .. of the segment that are there
-    if constexpr (S::COLUMNS) rb[0][2] = rb[1][2] = (int)(pb.left > 0 ? (unsigned)imax(imin(p.terms - pb.k, BK), 0) * b_pitch : 0);
-  };
-  auto prefetch_a = [&](int l) {
-    load_to_lds(scalar(ra), pa.k + 8 * chunk < p.K ? va[l] : OOB, 2u * pa.k, lds_ld + pa.place + l * S::NW * 1024);
-  };
-  auto prefetch_b = [&](int l) {
-    if constexpr (S::COLUMNS)
-      load_to_lds(scalar(rb[l / (S::LOADS / 2)]), vb[l], 0, lds_ld + pb.place + l * S::NW * 1024);
+    a_bytes = (unsigned)imin(p.M - m0, S::BM) * a_pitch;
+    b_bytes = S::ROWS ? (unsigned)imax(imin(p.N - n0[0], S::BN), 0) * b_pitch : 0;
+    lds_ld = lds0 + wave * 1024;
+    const int per = (p.K + S::BK - 1) / S::BK;                                 // stages of a segment
+    a.seg = p.first >= per ? 1 : 0;
+    a.k = p.first - a.seg * per;
+    a.place = 0;
+    a.left = p.stages;
+    b = a;
+    a.k *= S::BK;
+    b.k *= S::ROWS ? S::BK : S::TERMS;
+    b.place = S::B_AT;
+    open_a();
+    open_b();
+  }
+  __device__ __forceinline__ void open_a() {
+    ra = make_rsrc(pick(a.seg, p.s[0].a, p.s[1].a) + (uint64_t)m0 * a_pitch, a.left > 0 ? a_bytes : 0);
+  }
+  __device__ __forceinline__ void open_b() {
+    const char* const b0 = pick(b.seg, p.s[0].b0, p.s[1].b0);
+    if constexpr (S::ROWS) {
+      rb[0] = make_rsrc(b0 + (uint64_t)n_off * b_pitch, b.left > 0 ? b_bytes : 0);
+    } else {
+      rb[0] = make_rsrc(b0 + (uint64_t)b.k * b_pitch, 0);
+      if constexpr (S::SETS) rb[1] = make_rsrc(pick(b.seg, p.s[0].b1, p.s[1].b1) + (uint64_t)b.k * b_pitch, 0);
+      open_terms();
+    }
+  }
+  __device__ __forceinline__ void open_terms() {                               // columns: terms b.k .. of the segment that are there
+    rb[0][2] = (int)(b.left > 0 ? (unsigned)imax(imin(p.terms - b.k, S::TERMS), 0) * b_pitch : 0);
+    if constexpr (S::SETS) rb[1][2] = rb[0][2];
+  }
+  __device__ __forceinline__ void load_a(int l) {
+    load_to_lds(scalar(ra), a.k + 8 * chunk < p.K ? va[l] : OOB, scalar(2u * a.k), scalar(lds_ld + a.place + l * S::NW * 1024));
+  }
+  __device__ __forceinline__ void load_b(int l) {
+    const unsigned to = scalar(lds_ld + b.place + l * S::NW * 1024);
+    if constexpr (S::ROWS)
+      load_to_lds(scalar(rb[0]), b.k + 8 * chunk < p.K ? vb[l] : OOB, scalar(2u * b.k), to);
     else
-      load_to_lds(scalar(rb[0]), pb.k + 8 * chunk < p.K ? vb[l] : OOB, 2u * pb.k, lds_ld + pb.place + l * S::NW * 1024);
-  };
-  auto advance_a = [&]() {
-    pa.place = pa.place == 2 * S::A_BYTES ? 0 : pa.place + S::A_BYTES;
-    pa.k += BK;
-    --pa.left;
-    if (pa.k >= p.K || pa.left <= 0) {
-      pa.k = 0;
-      ++pa.seg;
+      load_to_lds(scalar(rb[S::SETS ? l / (S::LOADS / 2) : 0]), vb[l], 0, to);
+  }
+  __device__ __forceinline__ void advance_a() {
+    a.place = a.place == 2 * S::A_BYTES ? 0 : a.place + S::A_BYTES;
+    a.k += S::BK;
+    --a.left;
+    if (a.k >= p.K || a.left <= 0) {
+      a.k = 0;
+      ++a.seg;
       open_a();
     }
-  };
-  auto advance_b = [&]() {
-    pb.place = 2 * S::B_AT + S::B_BYTES - pb.place;
-    pb.k += BK;
-    if constexpr (S::COLUMNS) {
+  }
+  __device__ __forceinline__ void advance_b() {
+    b.place = 2 * S::B_AT + S::B_BYTES - b.place;
+    b.k += S::ROWS ? S::BK : S::TERMS;
+    --b.left;
+    if (b.left <= 0 || (S::ROWS || !S::HALVES ? b.k >= p.K : 2 * b.k >= p.K)) {
+      b.k = 0;
+      ++b.seg;
+      open_b();
+    } else if constexpr (!S::ROWS) {
 #pragma unroll
-      for (int l = 0; l < 2; ++l) {
-        const uint64_t q = ((uint64_t)(uint32_t)rb[l][1] << 32 | (uint32_t)rb[l][0]) + (uint64_t)BK * b_pitch;
+      for (int l = 0; l < (S::SETS ? 2 : 1); ++l) {
+        const uint64_t q = ((uint64_t)(uint32_t)rb[l][1] << 32 | (uint32_t)rb[l][0]) + (uint64_t)S::TERMS * b_pitch;
         rb[l][0] = (int)(uint32_t)q;
         rb[l][1] = (int)(uint32_t)(q >> 32);
       }
-    }
-    --pb.left;
-    if (pb.k >= p.K || pb.left <= 0) {
-      pb.k = 0;
-      ++pb.seg;
-      open_b();
-    }
-    open_terms();
-  };
-
-  // ---- LDS -> operands
-  const int row = lane & 15, wm = wave / S::WN * S::WTM, wc = wave % S::WN;
-  unsigned a_rd[2], b_rd[2];
-#pragma unroll
-  for (int ks = 0; ks < 2; ++ks) {
-    const unsigned place = (unsigned)((4 * ks + (lane >> 4)) ^ (row >> 1)) << 4;
-    a_rd[ks] = lds0 + (wm + row) * S::ROW_BYTES + place;
-    if constexpr (S::COLUMNS) {
-      const int k = 8 * (lane >> 4) + (row >> 2);
-      const unsigned c = (unsigned)(S::WTN / 2 * wc + 4 * (row & 3)) >> 3;
-      b_rd[ks] = lds0 + S::B_AT + (32 * ks + k) * S::COL_BYTES + ((c ^ S::spread(k)) << 4) + 8 * (row & 1);
-    } else {
-      b_rd[ks] = lds0 + S::B_AT + (S::WTN * wc + row) * S::ROW_BYTES + place;
+      open_terms();
     }
   }
+  // A 0, B 0, A 1, B 1, A 2; the first two have landed.
+  __device__ __forceinline__ void begin() {
+#pragma unroll
+    for (int q = 0; q < 5; ++q) {
+#pragma unroll
+      for (int l = 0; l < S::LOADS; ++l) {
+        if (q & 1)
+          load_b(l);
+        else
+          load_a(l);
+      }
+      if (q & 1)
+        advance_b();
+      else
+        advance_a();
+    }
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(3 * S::LOADS) : "memory");
+  }
+};
+
+// LDS -> operands: where a lane finds them.  Part: the k-step of 32 terms, or h and l.
+template <class S>
+struct ProductReads {
+  unsigned a_rd[2], b_rd[2];
+  typedef __attribute__((address_space(3))) const bf16x8* Lds;
+  __device__ __forceinline__ ProductReads(unsigned lds0, int wave, int lane) {
+    const int row = lane & 15, wm = wave / S::WN * S::WTM, wc = wave % S::WN;
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {
+      const unsigned place = (unsigned)((4 * part + (lane >> 4)) ^ (row >> 1)) << 4;
+      a_rd[part] = lds0 + (wm + row) * S::ROW_BYTES + place;
+      if constexpr (S::ROWS) {
+        b_rd[part] = lds0 + S::B_AT + (S::WTN * wc + row) * S::ROW_BYTES + place;
+      } else {
+        const int k = 8 * (lane >> 4) + (row >> 2);
+        // split: blocks of 32 columns, 64 bytes of h and as many of l
+        const unsigned piece = (S::SETS ? (unsigned)(S::WTN / 2 * wc) >> 3 : (unsigned)(S::WTN * wc) >> 2) + ((row & 3) >> 1);
+        b_rd[part] = lds0 + S::B_AT + (S::SETS ? 32 * part + k : k) * S::COL_BYTES + ((piece ^ S::spread(k)) << 4) + 8 * (row & 1);
+      }
+    }
+  }
+  __device__ __forceinline__ bf16x8 a(int x, unsigned base, int part) const { return *(Lds)(uintptr_t)(a_rd[part] + base + x * 16 * S::ROW_BYTES); }
+  __device__ __forceinline__ void b(Frag& f, int y, unsigned base, int part) const {
+    if constexpr (S::ROWS) {
+      f.v = *(Lds)(uintptr_t)(b_rd[part] + base + y * 16 * S::ROW_BYTES);
+    } else {
+      // 16 columns further are two pieces; h and l, four; in bits that the lane's own piece has as the XOR by k alone left them
+      const unsigned at = S::SETS ? ((b_rd[part] + base) ^ (y % (S::TN / 2) << 5)) + y / (S::TN / 2) * S::HALF_BYTES
+                                  : (b_rd[part] + base) ^ ((y & 1) << 5 | part << 6 | (y >> 1) << 7);
+      f.h[0] = lds_read_tr(at);
+      f.h[1] = lds_read_tr(at + 4 * S::COL_BYTES);
+    }
+  }
+};
+
+// The tile at (m0, n0) (sets: of either set n0[0], n0[1]) into acc.  acc[x][y], lane, register r: row 16 x + lane % 16 of the wave's, column
+// 16 y + 4 (lane / 16) + r of its WTN: those of the tile from WTN (wave % WN) on, or half as many of each set.
+template <class S, bool F16>
+__device__ __forceinline__ void product_tile(const ProductShape& p, int m0, const int (&n0)[2], unsigned lds0, f32x4 (&acc)[S::TM][S::TN]) {
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  ProductLoads<S> load(p, m0, n0, lds0, wave, lane);
+  const ProductReads<S> read(lds0, wave, lane);
 #pragma unroll
   for (int x = 0; x < S::TM; ++x)
 #pragma unroll
     for (int y = 0; y < S::TN; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
-  // B's operands of a k-step of 32 and the next; A's, each used by four instructions in a row, AHEAD of their use.
-  constexpr int AHEAD = 3;
-  Frag fa[4], fb[2][S::TN];
-  typedef __attribute__((address_space(3))) const bf16x8* Lds;
-  auto read_a = [&](int x, unsigned base, int ks) { fa[x & 3].v = *(Lds)(uintptr_t)(a_rd[ks] + base + x * 16 * S::ROW_BYTES); };
-  auto read_b = [&](int y, unsigned base, int ks) {
-    if constexpr (S::COLUMNS) {
-      // 16 columns further within a set are two places, in bits that the lane's own place has as the XOR by k alone left them
-      const unsigned at = ((b_rd[ks] + base) ^ (y % (S::TN / 2) << 5)) + y / (S::TN / 2) * S::HALF_BYTES;
-      fb[ks][y].h[0] = lds_read_tr(at);
-      fb[ks][y].h[1] = lds_read_tr(at + 4 * S::COL_BYTES);
-    } else {
-      fb[ks][y].v = *(Lds)(uintptr_t)(b_rd[ks] + base + y * 16 * S::ROW_BYTES);
-    }
-  };
-
-  open_a();
-  open_b();
-  open_terms();
-#pragma unroll
-  for (int q = 0; q < 5; ++q) {                                    // A 0, B 0, A 1, B 1, A 2
-#pragma unroll
-    for (int l = 0; l < S::LOADS; ++l) {
-      if (q & 1)
-        prefetch_b(l);
-      else
-        prefetch_a(l);
-    }
-    if (q & 1)
-      advance_b();
-    else
-      advance_a();
-  }
-  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(3 * S::LOADS) : "memory");
-#pragma unroll
-  for (int y = 0; y < S::TN; ++y) read_b(y, 0, 0);
-#pragma unroll
-  for (int x = 0; x < AHEAD; ++x) read_a(x, 0, 0);
-  // SPLIT: barriers M and E; else one, of both (small tiles: a few instructions lie between the two).
-  constexpr bool SPLIT = S::TM > 4;
-  constexpr int TURN = S::TM - AHEAD;                              // from this row on operands of the next k-step
+  load.begin();
   unsigned a_base = 0, b_base = 0;
-  for (int st = 0; st < p.stages; ++st) {
+  auto next_bases = [&]() {
+    a_base = a_base == 2 * S::A_BYTES ? 0 : a_base + S::A_BYTES;
+    b_base = S::B_BYTES - b_base;
     asm("" : "+s"(a_base), "+s"(b_base));
+  };
+  if constexpr (S::HALVES) {
+    // A row of A's operands, h and l, is asked for a row ahead; B's of the next stage, of h and l, within the last row.
+    Frag fa[2][2], fb[2][2][S::TN];                                // [row % 2][h, l]; [stage % 2][h, l]
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
+    for (int part = 0; part < 2; ++part) {
+#pragma unroll
+      for (int y = 0; y < S::TN; ++y) read.b(fb[0][part][y], y, 0, part);
+      fa[0][part].v = read.a(0, 0, part);
+    }
+    auto stage = [&](auto turn_tag) {
+      constexpr int turn = decltype(turn_tag)::value, LAST = S::TM - 1;
 #pragma unroll
       for (int x = 0; x < S::TM; ++x) {
-        if (SPLIT && ks == 1 && x == 1) asm volatile("s_waitcnt lgkmcnt(1)\n\ts_barrier" ::: "memory");      // one of A's is younger
-        if (ks == 1 && x == TURN) {
-          asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((SPLIT ? 2 : 1) * S::LOADS) : "memory");
-          a_base = a_base == 2 * S::A_BYTES ? 0 : a_base + S::A_BYTES;
-          b_base = S::B_BYTES - b_base;
-          asm("" : "+s"(a_base), "+s"(b_base));
+        // M: B's operands are in registers (the last row's reads; two of A's are younger)
+        if (x == 1) asm volatile("s_waitcnt lgkmcnt(2)\n\ts_barrier" ::: "memory");
+        if (x == LAST) {                                           // E
+          asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * S::LOADS) : "memory");
+          next_bases();
         }
         DP_PIN();
 #pragma unroll
-        for (int y = 0; y < S::TN; ++y) {
-          acc[x][y] = mfma16<F16>(fb[ks][y].v, fa[x & 3].v, acc[x][y]);
+        for (int slot = 0; slot < 3 * S::TN; ++slot) {
+          const int product = slot / S::TN, y = slot % S::TN;      // h h, l of B, l of A
+          acc[x][y] = mfma16<F16>(fb[turn][product == 1][y].v, fa[x & 1][product == 2].v, acc[x][y]);
           DP_PIN();
-          if (y == 0) read_a((x + AHEAD) % S::TM, a_base, x >= TURN ? ks ^ 1 : ks);
-          constexpr int SLOTS = AHEAD * S::TN;
-          const int slot = (x - TURN) * S::TN + y;                 // of the last AHEAD rows
-          // B's of the next k-step, each behind an instruction that reads none of A's
-          if (x >= TURN && y != 0) {
-            const int from = (slot - (x - TURN) - 1) * S::TN / (SLOTS - AHEAD), to = (slot - (x - TURN)) * S::TN / (SLOTS - AHEAD);
+          if (slot < 2) fa[~x & 1][slot].v = read.a((x + 1) % S::TM, a_base, slot);
+          if (x == LAST && slot >= 2 && slot < 2 + 2 * S::TN) read.b(fb[turn ^ 1][(slot - 2) / S::TN][(slot - 2) % S::TN], (slot - 2) % S::TN, b_base, (slot - 2) / S::TN);
+          // loads: B's behind M, A's behind E
+          if (x >= 1 && x < LAST) {
+            constexpr int SLOTS = (LAST - 1) * 3 * S::TN;
+            const int at = (x - 1) * 3 * S::TN + slot;
 #pragma unroll
-            for (int b = from; b < to; ++b) read_b(b, b_base, ks ^ 1);
-          }
-          // loads: B's behind M (or E), A's behind E
-          if (SPLIT && ks == 1 && x >= 1 && x < 1 + S::LOADS && y == 2) {
-            prefetch_b(x - 1);
-            if (x == S::LOADS) advance_b();
-          }
-          if (ks == 1 && x >= TURN) {
-            constexpr int LOADS = (SPLIT ? 1 : 2) * S::LOADS;
-#pragma unroll
-            for (int e = slot * LOADS / SLOTS; e < (slot + 1) * LOADS / SLOTS; ++e) {
-              if (SPLIT || e >= S::LOADS)
-                prefetch_a(e % S::LOADS);
-              else
-                prefetch_b(e);
-            }
-            if (slot == SLOTS - 1) {
-              if (!SPLIT) advance_b();
-              advance_a();
+            for (int e = at * S::LOADS / SLOTS; e < (at + 1) * S::LOADS / SLOTS; ++e) {
+              load.load_b(e);
+              if (e == S::LOADS - 1) load.advance_b();
             }
           }
+          if (x == LAST && slot % 3 == 2 && slot / 3 < S::LOADS) {
+            load.load_a(slot / 3);
+            if (slot / 3 == S::LOADS - 1) load.advance_a();
+          }
           DP_PIN();
+        }
+      }
+    };
+    for (int st = 0; st < p.stages; st += 2) {                     // (a stage past the last one: zeros)
+      asm("" : "+s"(a_base), "+s"(b_base));
+      stage(std::integral_constant<int, 0>{});
+      stage(std::integral_constant<int, 1>{});
+    }
+  } else {
+    // B's operands of a k-step of 32 and the next; A's, each used by four instructions in a row, AHEAD of their use.
+    constexpr int AHEAD = 3;
+    Frag fa[4], fb[2][S::TN];
+#pragma unroll
+    for (int y = 0; y < S::TN; ++y) read.b(fb[0][y], y, 0, 0);
+#pragma unroll
+    for (int x = 0; x < AHEAD; ++x) fa[x].v = read.a(x, 0, 0);
+    // TWO: barriers M and E; else one, of both (small tiles: a few instructions lie between the two).
+    constexpr bool TWO = S::TM > 4;
+    constexpr int TURN = S::TM - AHEAD;                            // from this row on operands of the next k-step
+    for (int st = 0; st < p.stages; ++st) {
+      asm("" : "+s"(a_base), "+s"(b_base));
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+        for (int x = 0; x < S::TM; ++x) {
+          if (TWO && ks == 1 && x == 1) asm volatile("s_waitcnt lgkmcnt(1)\n\ts_barrier" ::: "memory");      // one of A's is younger
+          if (ks == 1 && x == TURN) {
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((TWO ? 2 : 1) * S::LOADS) : "memory");
+            next_bases();
+          }
+          DP_PIN();
+#pragma unroll
+          for (int y = 0; y < S::TN; ++y) {
+            acc[x][y] = mfma16<F16>(fb[ks][y].v, fa[x & 3].v, acc[x][y]);
+            DP_PIN();
+            if (y == 0) fa[(x + AHEAD) & 3].v = read.a((x + AHEAD) % S::TM, a_base, x >= TURN ? ks ^ 1 : ks);
+            constexpr int SLOTS = AHEAD * S::TN;
+            const int slot = (x - TURN) * S::TN + y;               // of the last AHEAD rows
+            // B's of the next k-step, each behind an instruction that reads none of A's
+            if (x >= TURN && y != 0) {
+              const int from = (slot - (x - TURN) - 1) * S::TN / (SLOTS - AHEAD), to = (slot - (x - TURN)) * S::TN / (SLOTS - AHEAD);
+#pragma unroll
+              for (int b = from; b < to; ++b) read.b(fb[ks ^ 1][b], b, b_base, ks ^ 1);
+            }
+            // loads: B's behind M (or E), A's behind E
+            if (TWO && ks == 1 && x >= 1 && x < 1 + S::LOADS && y == 2) {
+              load.load_b(x - 1);
+              if (x == S::LOADS) load.advance_b();
+            }
+            if (ks == 1 && x >= TURN) {
+              constexpr int LOADS = (TWO ? 1 : 2) * S::LOADS;
+#pragma unroll
+              for (int e = slot * LOADS / SLOTS; e < (slot + 1) * LOADS / SLOTS; ++e) {
+                if (TWO || e >= S::LOADS)
+                  load.load_a(e % S::LOADS);
+                else
+                  load.load_b(e);
+              }
+              if (slot == SLOTS - 1) {
+                if (!TWO) load.advance_b();
+                load.advance_a();
+              }
+            }
+            DP_PIN();
+          }
         }
       }
     }
@@ -295,8 +386,8 @@ __device__ __forceinline__ void product_rows(const f32x4 (&acc)[S::TM][S::TN], u
   const unsigned slab = lds0 + wave * S::SLAB_BYTES;
   typedef __attribute__((address_space(3))) f32x4* Lds;
   constexpr int LANES = S::WTN / (PAIRS ? 16 : 8), PASSES = 32 * LANES / 64, HALF = S::WTN / 2;
-  const int c = 8 * (lane % LANES), set = S::COLUMNS && !PAIRS ? c / HALF : 0;
-  const int col = S::COLUMNS ? HALF * wc + c % HALF : S::WTN * wc + c;       // within a set, or within the tile
+  const int c = 8 * (lane % LANES), set = S::SETS && !PAIRS ? c / HALF : 0;
+  const int col = S::SETS ? HALF * wc + c % HALF : S::WTN * wc + c;       // within a set, or within the tile
   auto row_of = [&](int x, int i) { return 32 * x + i * (64 / LANES) + lane / LANES; };
   decltype(load(0, 0, 0)) ahead[2][PASSES];
 #pragma unroll
