@@ -1,105 +1,160 @@
-// Gated feed-forward layers, fp32 forms: products on the fp32 matrix instructions, tiles through registers into LDS, any sizes.
+// Gated feed-forward layers, fp32 forms: products on the fp32 matrix instructions, any sizes and alignments.
 //   gate = x Wg + bg,  up = x Wu + bu,  h = act(gate) up;
 //   dh = dy Wd',  dgate = dh up act'(gate),  dup = dh act(gate),  dx = dgate Wg' + dup Wu'.
+#include <algorithm>
+
 #include "gated.h"
+#include "lds_dma.h"
+#include "tile_order.h"
 
 namespace dpbk {
 
 namespace {
 
-constexpr int kThreads = 256, kRows = 64, kCols = 64, kDepth = 16;     // a tile: 64 rows, two sets of 64 columns; 16 terms at a time
+constexpr int kThreads = 256, kWaves = 4, kTerms = 32;         // terms of a stage: 128 bytes of a row
 
-// Two sets of columns side by side: forward the gate's and up's, else a product's at n0 and n0 + 64.  A wave has 32 rows and 32 columns of
-// each set.  As [row][k], columns' operands [k][column] as they lie (forward) or [column][k].
-template <int PASS>
-__global__ void __launch_bounds__(kThreads) gated_f32_kernel(const GatedArgs a, int tiles_n) {
-  constexpr int PITCH = kDepth + 1;
-  __shared__ float la[kRows * PITCH], lb[2][PASS == kForward ? kDepth * kCols : kCols * PITCH];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int tm = blockIdx.x / (unsigned)tiles_n, tn = blockIdx.x - tm * tiles_n;
-  const int m0 = tm * kRows, n0 = tn * (PASS == kForward ? kCols : 2 * kCols);
+// A tile of 32 W x 32 W by four waves of 16 W x 16 W.  Its columns: forward two sets of half as many, the gate's and up's, else those of one product.
+// Memory -> LDS without registers, 4 bytes a lane, so that no row need begin anywhere in particular: 256 loads of 256 bytes to 64 KiB of a
+// stage cost a hundredth of the matrix instructions' time, which is 16 times that of 16-bit ones.  Two stages: one is multiplied, one on its way.
+// LDS holds [row][32 terms], 16-byte pieces XORed with row / 2, read 16 bytes a lane: four instructions take one of the four terms each, for both
+// operands the same.  Columns' operands [term][columns], pieces XORed with term / 4, are read term by term.
+template <int W, bool SETS>
+struct F32Tile {
+  static constexpr int SIDE = 32 * W, OPERAND_BYTES = SIDE * 128, STAGE_BYTES = 2 * OPERAND_BYTES, LOADS = OPERAND_BYTES / 256 / kWaves;
+  static constexpr int SET = SIDE / 2;                         // columns of a set
+};
+
+// All loads into LDS have landed, in the other waves' too, and every wave is through with its reads.
+__device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+template <int PASS, int W>
+__global__ void __launch_bounds__(kThreads, 2) gated_f32_kernel(const GatedArgs a, int tiles_m, int tiles_n) {
+  constexpr bool SETS = PASS == kForward;
+  typedef F32Tile<W, SETS> S;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char lds_raw[];
+  const unsigned lds0 = (unsigned)(uintptr_t)lds_raw;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int tm, tn;
+  grad_tile_of(tiles_m, tiles_n, grad_logical_tile(blockIdx.x, tiles_m * tiles_n), tm, tn);
+  const int m0 = tm * S::SIDE, n0 = tn * (SETS ? S::SET : S::SIDE);
   const int N = PASS == kInput ? a.d : a.f, K = PASS == kForward ? a.d : PASS == kHidden ? a.d_out : a.f;
-  auto value = [](const void* base, int64_t at) { return static_cast<const float*>(base)[at]; };
-  f32x16 acc[2];
+  const int per = (K + kTerms - 1) / kTerms, stages = per * (PASS == kInput ? 2 : 1);
+  const unsigned a_pitch = 4u * K, b_pitch = 4u * (SETS ? N : K);
+
+  // A load brings two rows' terms; a lane's place in them, and the term that lies there, by the load's parity
+  const int half = lane >> 5, at = lane & 31;
+  int term[2];
 #pragma unroll
-  for (int s = 0; s < 2; ++s)
+  for (int odd = 0; odd < 2; ++odd) term[odd] = ((at >> 2) ^ ((4 * odd + wave) & 7)) * 4 + (at & 3);
+  auto scalar = [](i32x4 r) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) acc[s][r] = 0.f;
-  const int segments = PASS == kInput ? 2 : 1;
-  for (int seg = 0; seg < segments; ++seg) {
-    const void* const A = PASS == kForward ? a.x : PASS == kHidden ? a.dy : seg ? a.dup : a.dgate;
-    const void* const W = PASS == kHidden ? a.w_down : seg ? a.w_up : a.w_gate;
-    for (int k0 = 0; k0 < K; k0 += kDepth) {
-      float ra[4], rb[2][4];
-      {
-        const int m = m0 + tid / 4, k = k0 + 4 * (tid % 4);
+    for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_readfirstlane(r[i]);
+    return r;
+  };
+  auto ask = [&](int st, unsigned to) {
+    const int seg = PASS == kInput && st >= per ? 1 : 0, k = (st - seg * per) * kTerms;
+    const char* const pa = static_cast<const char*>(PASS == kForward ? a.x : PASS == kHidden ? a.dy : seg ? a.dup : a.dgate);
+    const char* const pb = static_cast<const char*>(PASS == kHidden ? a.w_down : seg ? a.w_up : a.w_gate);
+    auto rows = [&](const char* base, int row0, int end, unsigned pitch, unsigned lds) {
+      const i32x4 r = scalar(make_rsrc(base + (uint64_t)row0 * pitch + 4ull * k, st < stages ? (unsigned)imax(imin(end - row0, S::SIDE), 0) * pitch : 0));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) ra[i] = m < a.rows && k + i < K ? value(A, (int64_t)m * K + k + i) : 0.f;
+      for (int l = 0; l < S::LOADS; ++l) {
+        const unsigned row = 2 * (l * kWaves + wave) + half;
+        load_dword_to_lds(r, k + term[l & 1] < K ? row * pitch + 4 * term[l & 1] : OOB, lds + (l * kWaves + wave) * 256);
       }
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (PASS == kForward) {
-            const int k = k0 + tid / 16, n = n0 + 4 * (tid % 16) + i;
-            rb[s][i] = k < K && n < N ? value(s ? a.w_up : a.w_gate, (int64_t)k * N + n) : 0.f;
-          } else {
-            const int n = n0 + kCols * s + tid / 4, k = k0 + 4 * (tid % 4) + i;
-            rb[s][i] = k < K && n < N ? value(W, (int64_t)n * K + k) : 0.f;
-          }
-        }
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < 4; ++i) la[tid / 4 * PITCH + 4 * (tid % 4) + i] = ra[i];
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          lb[s][PASS == kForward ? tid / 16 * kCols + 4 * (tid % 16) + i : tid / 4 * PITCH + 4 * (tid % 4) + i] = rb[s][i];
-      __syncthreads();
-#pragma unroll
-      for (int k = 0; k < kDepth; k += 2) {
-        const int kk = k + (lane >> 5), c = 32 * (wave & 1) + (lane & 31);
-        const float fa = la[(32 * (wave >> 1) + (lane & 31)) * PITCH + kk];
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const float fb = lb[s][PASS == kForward ? kk * kCols + c : c * PITCH + kk];
-          acc[s] = __builtin_amdgcn_mfma_f32_32x32x2f32(fa, fb, acc[s], 0, 0, 0);
-        }
-      }
-    }
-  }
-  // lane: column 32 (wave & 1) + lane % 32; register r: row 8 (r / 4) + 4 (lane / 32) + r % 4 of the wave's 32
-  auto put = [](void* base, int64_t at, float x) { static_cast<float*>(base)[at] = x; };
-#pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    const int m = m0 + 32 * (wave >> 1) + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
-    if (m >= a.rows) continue;
-    const int n = n0 + 32 * (wave & 1) + (lane & 31);
-    float slope;
-    if (PASS == kForward) {
-      if (n >= N) continue;
-      const int64_t at = (int64_t)m * N + n;
-      const float gate = acc[0][r] + (a.b_gate ? value(a.b_gate, n) : 0.f), up = acc[1][r] + (a.b_up ? value(a.b_up, n) : 0.f);
-      if (a.gate) {
-        put(a.gate, at, gate);
-        put(a.up, at, up);
-      }
-      put(a.h, at, activation<true, false>(a.act, gate, slope) * up);
+    };
+    rows(pa, m0, a.rows, a_pitch, to);
+    if constexpr (!SETS) {
+      rows(pb, n0, N, b_pitch, to + S::OPERAND_BYTES);
     } else {
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
-        if (n + kCols * s < N) {
-          const int64_t at = (int64_t)m * N + n + kCols * s;
-          if (PASS == kInput) {
-            put(a.dx, at, acc[s][r]);
-          } else {
-            const float dh = acc[s][r], v = activation<true, true>(a.act, value(a.gate, at), slope);
-            put(a.dgate, at, dh * value(a.up, at) * slope);
-            put(a.dup, at, dh * v);
-          }
+      for (int s = 0; s < 2; ++s) {
+        const char* const w = static_cast<const char*>(s ? a.w_up : a.w_gate);
+        const i32x4 r = scalar(make_rsrc(w + (uint64_t)k * b_pitch, st < stages ? (unsigned)imin(K - k, kTerms) * b_pitch : 0));
+        constexpr int PER = 64 / S::SET;                       // terms of a load
+#pragma unroll
+        for (int l = 0; l < S::LOADS / 2; ++l) {
+          const int kk = (l * kWaves + wave) * PER + lane / S::SET, c = lane % S::SET;
+          const int col = n0 + (((c >> 2) ^ (((kk >> 2) & 3) << (S::SET == 64 ? 2 : 1))) << 2) + (c & 3);
+          load_dword_to_lds(r, col < N ? kk * b_pitch + 4u * col : OOB, to + S::OPERAND_BYTES + s * S::OPERAND_BYTES / 2 + (l * kWaves + wave) * 256);
         }
+      }
     }
+  };
+  f32x4 acc[W][W];
+#pragma unroll
+  for (int x = 0; x < W; ++x)
+#pragma unroll
+    for (int y = 0; y < W; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int r16 = lane & 15, h = lane >> 4, wm = (wave >> 1) * 16 * W, wc = wave & 1;
+  typedef __attribute__((address_space(3))) const f32x4* Four;
+  typedef __attribute__((address_space(3))) const float* One;
+  ask(0, lds0);
+  landed();
+  for (int st = 0; st < stages; ++st) {
+    const unsigned from = lds0 + (st & 1) * S::STAGE_BYTES;
+    ask(st + 1, lds0 + (~st & 1) * S::STAGE_BYTES);
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      f32x4 fa[W], fb[W];
+      const unsigned place = ((4 * ks + h) ^ (r16 >> 1)) << 4;
+#pragma unroll
+      for (int x = 0; x < W; ++x) fa[x] = *(Four)(uintptr_t)(from + (wm + 16 * x + r16) * 128 + place);
+#pragma unroll
+      for (int y = 0; y < W; ++y) {
+        if constexpr (!SETS) {
+          fb[y] = *(Four)(uintptr_t)(from + S::OPERAND_BYTES + (16 * W * wc + 16 * y + r16) * 128 + place);
+        } else {
+          // frags 0 .. W / 2 - 1 of the gate's set, the others of up's
+          const int set = y / (W / 2), c = 8 * W * wc + 16 * (y % (W / 2)) + r16;
+          const unsigned piece = (unsigned)((c >> 2) ^ (h << (S::SET == 64 ? 2 : 1)));
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            fb[y][e] = *(One)(uintptr_t)(from + S::OPERAND_BYTES + set * S::OPERAND_BYTES / 2 + (16 * ks + 4 * h + e) * 4 * S::SET + piece * 16 + 4 * (c & 3));
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int x = 0; x < W; ++x)
+#pragma unroll
+          for (int y = 0; y < W; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[x][e], fb[y][e], acc[x][y], 0, 0, 0);
+    }
+    landed();
+  }
+
+  // lane: column lane % 16 of a fragment; register r: row 4 (lane / 16) + r
+  auto value = [](const void* base, int64_t place) { return static_cast<const float*>(base)[place]; };
+  auto put = [](void* base, int64_t place, float x) { static_cast<float*>(base)[place] = x; };
+  constexpr int COLS = SETS ? W / 2 : W;
+#pragma unroll
+  for (int y = 0; y < COLS; ++y) {
+    const int n = n0 + 16 * COLS * wc + 16 * y + r16;
+    if (n >= N) continue;
+    const float bg = PASS == kForward && a.b_gate ? value(a.b_gate, n) : 0.f, bu = PASS == kForward && a.b_up ? value(a.b_up, n) : 0.f;
+#pragma unroll
+    for (int x = 0; x < W; ++x)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int m = m0 + wm + 16 * x + 4 * h + r;
+        if (m >= a.rows) continue;
+        const int64_t place = (int64_t)m * N + n;
+        float slope;
+        if constexpr (PASS == kForward) {
+          const float gate = acc[x][y][r] + bg, up = acc[x][y + W / 2][r] + bu;
+          if (a.gate) {
+            put(a.gate, place, gate);
+            put(a.up, place, up);
+          }
+          put(a.h, place, activation<true, false>(a.act, gate, slope) * up);
+        } else if constexpr (PASS == kHidden) {
+          const float dh = acc[x][y][r], v = activation<true, true>(a.act, value(a.gate, place), slope);
+          put(a.dgate, place, dh * value(a.up, place) * slope);
+          put(a.dup, place, dh * v);
+        } else {
+          put(a.dx, place, acc[x][y][r]);
+        }
+      }
   }
 }
 
@@ -140,12 +195,24 @@ dp_status launch_slopes(const GatedArgs& a, hipStream_t s) {
   return hip_status(hipGetLastError());
 }
 
+template <int PASS, int W>
+dp_status launch_f32_tiles(const GatedArgs& a, hipStream_t s) {
+  typedef F32Tile<W, PASS == kForward> S;
+  static ReadyTable ready;
+  const dp_status st = allow_big_lds(gated_f32_kernel<PASS, W>, 2 * S::STAGE_BYTES, ready);
+  if (st != DP_OK) return st;
+  const int N = PASS == kInput ? a.d : a.f, width = PASS == kForward ? S::SET : S::SIDE;
+  const int tiles_n = (N + width - 1) / width, tiles_m = (a.rows + S::SIDE - 1) / S::SIDE;
+  gated_f32_kernel<PASS, W><<<dim3((unsigned)tiles_m * tiles_n), kThreads, 2 * S::STAGE_BYTES, s>>>(a, tiles_m, tiles_n);
+  return hip_status(hipGetLastError());
+}
+
+// Tiles of 128 x 128 where they are one to a compute unit at least, else of 64 x 64.
 template <int PASS>
 dp_status launch_f32(const GatedArgs& a, hipStream_t s) {
-  const int N = PASS == kInput ? a.d : a.f, width = PASS == kForward ? kCols : 2 * kCols;
-  const int64_t tiles_n = (N + width - 1) / width, tiles_m = (a.rows + kRows - 1) / kRows;
-  gated_f32_kernel<PASS><<<dim3((unsigned)(tiles_m * tiles_n)), kThreads, 0, s>>>(a, (int)tiles_n);
-  return hip_status(hipGetLastError());
+  const int64_t N = (int64_t)(PASS == kInput ? a.d : a.f) * (PASS == kForward ? 2 : 1);
+  const bool large = (int64_t)((a.rows + 127) / 128) * ((N + 127) / 128) >= 256;
+  return large ? launch_f32_tiles<PASS, 4>(a, s) : launch_f32_tiles<PASS, 2>(a, s);
 }
 
 }  // namespace
