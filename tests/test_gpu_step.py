@@ -443,3 +443,186 @@ def test_muon_other_polynomials(block):
         # the smallest singular value's direction grows by the product of the a's at most
         grown = math.prod(a for a, _, _ in abc)
         assert (param.cpu().double() - want).norm() <= (1.5 * min(grown, 500) * 2.0 ** -23 + 3 * len(abc) * FP32) * max(1.0, want.norm().item())
+
+
+# ------------------------------------------------------------------------------------------------ as programs call them
+
+class Step:
+    """Every call of this file once, with the tensors that a program keeps: rotation, head norms, gated layers of many and of few rows, whose input
+    gradients' contraction is dealt to several workgroups or not, and updates of matrices of both kinds."""
+
+    def __init__(self, block, seed, T=150):
+        self.gen = torch.Generator(device="cuda").manual_seed(seed)
+        new = lambda *s, dt=torch.bfloat16: torch.empty(s, dtype=dt, device="cuda")  # noqa: E731
+        B, H, D, d, f = 2, 6, 32, 96, 520
+        self.x, self.q, self.k = new(B, T, H + 2, D), new(B, T, H, D), new(B, T, 1, D)
+        self.dq, self.dk, self.dx = new(B, T, H, D), new(B, T, 1, D), new(B, T, H + 2, D)
+        self.kept, self.sq = new(B, 2, D, dt=torch.float32), new(B, dt=torch.float32)
+        views = lambda t: (t[:, :, :H], t[:, :, H:H + 1])  # noqa: E731
+        kw = dict(turns=block.rotary_turns(D).cuda(), position=torch.arange(2 * T, dtype=torch.int32, device="cuda").view(B, T))
+        norm = block.HeadNorm(*views(self.x), self.q, self.k, torch.ones(D, device="cuda"), None, **kw)
+        turn = block.Rotary(self.q, self.k, self.q, self.k, **kw)
+        self.w = [new(d, f), new(d, f), new(f, d)]
+        gated = block.GatedFeedForward(*self.w, activation="gelu")
+        rows = [(new(n, d), [new(n, f) for _ in range(5)], new(n, d)) for n in (7, 90, 600)]
+        self.p, self.g, self.m = ([torch.empty(s, device="cuda") for s in ((40, 24), (200, 136), (96, 300), (8, 8))] for _ in range(3))
+        muon = block.Muon(self.p, self.g, self.m, 0.1)
+        self.objects, self.inputs = (norm, gated, muon), [self.x, self.dq, self.dk, *self.w, *[r[0] for r in rows], *self.g]
+        self.outputs = [self.q, self.k, self.kept, self.sq, *[t for r in rows for t in (*r[1], r[2])], *self.p, *self.m]
+
+        def run():
+            norm.forward(*views(self.x), self.q, self.k)
+            turn.forward(self.q, self.k, self.q, self.k)
+            norm.backward(*views(self.x), self.dq, self.dk, *views(self.dx), self.kept, self.sq)
+            for x, (gate, up, h, dgate, dup), dx in rows:
+                gated.forward(x, h, gate, up)
+                gated.backward(x, gate, up, dgate, dup, dx)
+            muon.step(0.01)
+        self.run = run
+
+    def fill(self):
+        for t in (*self.inputs, *self.p, *self.m):
+            t.copy_(torch.randn(t.shape, generator=self.gen, device="cuda"))
+        for t in self.outputs[:-2 * len(self.p)]:
+            t.fill_(7.0)
+
+
+def test_step_replayed_in_a_graph(block):
+    """All of it captured once and replayed on new inputs, with eager calls in between."""
+    s = Step(block, 3)
+    s.fill()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        s.run()                                           # workspaces are there before the capture
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        s.run()
+    for _ in range(4):
+        s.fill()
+        state = [t.clone() for t in (*s.p, *s.m)]
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in s.outputs]
+        for t, before in zip((*s.p, *s.m), state):
+            t.copy_(before)
+        s.run()
+        torch.cuda.synchronize()
+        assert all(torch.isfinite(t).all() and torch.equal(a, t) for a, t in zip(got, s.outputs))
+
+
+def test_steps_on_streams_at_once(block):
+    """Two sets of objects and two streams, and graphs of one set beside its eager calls: none shares scratch with another."""
+    steps, want = [Step(block, 5), Step(block, 6, 90)], []
+    for s in steps:
+        s.fill()
+        s.state = [t.clone() for t in (*s.p, *s.m)]
+        s.run()
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in s.outputs])
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    used = []
+    for o in steps[0].objects:
+        inner = o._ws
+        o._ws = lambda *args, inner=inner: used.append(inner(*args)) or used[-1]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=streams[0]):
+        steps[0].run()
+    captured = [(t.data_ptr(), t.data_ptr() + t.numel()) for t in used]
+    del used[:]
+    with torch.cuda.stream(streams[0]):
+        steps[0].run()
+    spans = sorted(captured + [(t.data_ptr(), t.data_ptr() + t.numel()) for t in used])
+    torch.cuda.synchronize()
+    assert len(captured) >= 3 and all(a[1] <= b[0] for a, b in zip(spans, spans[1:]) if a != b)
+    for _ in range(6):
+        for s in steps:
+            for t, before in zip((*s.p, *s.m), s.state):
+                t.copy_(before)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(streams[0]):
+            graph.replay()
+        with torch.cuda.stream(streams[1]):
+            steps[1].run()
+        torch.cuda.synchronize()
+        for s, outputs in zip(steps, want):
+            assert all(torch.equal(a, b) for a, b in zip(s.outputs, outputs))
+
+
+def test_gated_rows_and_columns_do_not_meet(block):
+    """What is not a number stays in its row, or its weight's column, on every kernel: few rows, small and large tiles, fp32."""
+    for dtype, rows in (("bf16", 5), ("f16", 40), ("bf16", 300), ("f16", 2600), ("f32", 70), ("f32", 2600)):
+        d, f = 72, 1032 if rows < 2000 else 2120
+        gen = torch.Generator(device="cuda").manual_seed(rows)
+        r = lambda *s: torch.randn(s, generator=gen, device="cuda").to(DTYPES[dtype])  # noqa: E731
+        x, wg, wu, wd = r(rows, d), r(d, f), r(d, f), r(f, d)
+        x[rows - 2] = math.nan
+        x[1, 3] = math.inf
+        wg[:, f - 3] = math.nan
+        wd[5] = math.nan                                  # column 5 of dh
+        layer = block.GatedFeedForward(wg, wu, wd)
+        gate, up, h, dgate, dup = (torch.empty((rows, f), dtype=x.dtype, device="cuda") for _ in range(5))
+        dx = torch.empty_like(x)
+        layer.forward(x, h, gate, up)
+        bad_rows, fine = [1, rows - 2], torch.ones(rows, dtype=torch.bool)
+        fine[bad_rows] = False
+        columns = torch.ones(f, dtype=torch.bool)
+        columns[f - 3] = False
+        assert torch.isfinite(gate.cpu()[fine][:, columns]).all() and torch.isfinite(up.cpu()[fine]).all()
+        assert torch.isnan(gate.cpu()[:, f - 3]).all() and torch.isnan(up.cpu()[rows - 2]).all() and not torch.isfinite(up.cpu()[1]).any()
+        layer.backward(r(rows, d), up.nan_to_num(0, 0, 0), up.nan_to_num(0, 0, 0), dgate, dup)
+        columns[:] = True
+        columns[5] = False
+        assert torch.isfinite(dgate.cpu()[:, columns]).all() and torch.isnan(dgate.cpu()[:, 5]).any()
+        dgate, dup = r(rows, f), r(rows, f)
+        bad = block.GatedFeedForward(r(d, f), r(d, f))
+        dh = r(rows, f)
+        dh[rows - 1] = math.nan
+        bad.backward(dh, r(rows, f), r(rows, f), dgate, dup, dx)
+        assert torch.isfinite(dx[:rows - 1]).all() and torch.isnan(dx[rows - 1]).all()
+
+
+def test_far_offsets(block):
+    """Samples, rows and results more than 2^31 elements into their arrays."""
+    far = 2 ** 31 + 64
+    base = torch.zeros(far + 4096, dtype=torch.bfloat16, device="cuda")
+    gen = torch.Generator().manual_seed(1)
+    x = rand(gen, (2, 3, 4, 16), "bf16")
+    q = base.as_strided((2, 3, 4, 16), (far, 128, 16, 1))
+    q.copy_(x)
+    out = torch.zeros(far + 4096, dtype=torch.bfloat16, device="cuda").as_strided((2, 3, 4, 16), (far, 64, 16, 1))
+    turns = block.rotary_turns(16)
+    kept, sq = torch.empty((2, 1, 16), device="cuda"), torch.empty(2, device="cuda")
+    norm = block.HeadNorm(q, None, out, None, turns=turns.cuda())
+    norm.forward(q, None, out, None)
+    unit = x.double() * (x.double().square().mean(-1, keepdim=True) + 1e-6) ** -0.5
+    assert rel(out, turn(unit, turns, False, 1.0, torch.arange(3).repeat(2, 1))) <= U["bf16"] + 4 * FP32
+    norm.backward(q, None, out, None, q, None, kept, sq)              # in the place of the inputs
+    assert torch.isfinite(q).all() and torch.isfinite(kept).all()
+    del base, q, out
+    rows, d, f = 66000, 16, 32768
+    x, wg, wu = rand(gen, (rows, d), "bf16"), rand(gen, (d, f), "bf16", 0.25), rand(gen, (d, f), "bf16", 0.25)
+    gate, up, h = (torch.empty((rows, f), dtype=torch.bfloat16, device="cuda") for _ in range(3))
+    layer = block.GatedFeedForward(wg.cuda(), wu.cuda())
+    layer.forward(x.cuda(), h, gate, up)
+    some = [0, 1, 65535, 65536, rows - 1]
+    want = x[some].double() @ wg.double(), x[some].double() @ wu.double()
+    same(gate[some], want[0], FP32, "bf16")
+    same(up[some], want[1], FP32, "bf16")
+    dx = torch.empty((rows, d), dtype=torch.bfloat16, device="cuda")
+    layer.backward(h, gate, up, gate, up, dx)                         # in place of gate and up
+    same(dx[some], gate[some].cpu().double() @ wg.double().t() + up[some].cpu().double() @ wu.double().t(), 4 * FP32, "bf16")
+
+
+def test_repeated_calls_give_the_same_bits(block):
+    s = Step(block, 11)
+    s.fill()
+    state = [t.clone() for t in (*s.p, *s.m)]
+    s.run()
+    first = [t.clone() for t in s.outputs]
+    for _ in range(3):
+        for t, before in zip((*s.p, *s.m), state):
+            t.copy_(before)
+        s.run()
+        assert all(torch.equal(a, b) for a, b in zip(first, s.outputs))
