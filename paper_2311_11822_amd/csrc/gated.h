@@ -27,38 +27,72 @@ dp_status launch_gated_few(const GatedArgs& a, dp_dtype dt, GatedPass pass, hipS
 dp_status launch_gated_forward(const GatedArgs& a, dp_dtype dt, hipStream_t s);
 dp_status launch_gated_backward(const GatedArgs& a, dp_dtype dt, hipStream_t s);
 
-// The gate's activation: its value and, where asked for, its slope.  All but relu are shares of their argument (sigmoid: the share
-// itself), written with exp(-|v|) so that neither a share nor its complement is a difference.
-template <bool EXACT>                                  // fp32 results; 16-bit ones round more than the shorter exponential errs
-__device__ __forceinline__ float act_exp(float x) {
-  return EXACT ? expf(x) : __expf(x);
-}
-template <bool EXACT, bool SLOPE>
-__device__ __forceinline__ float activation(int act, float x, float& slope) {
-  if (act == DP_ACT_RELU) {
+// The gate's activation: its value and, where asked for, its slope.  All but relu are shares of their argument (sigmoid: the share itself).
+//
+// EXACT, for fp32 results: written with exp(-|v|), so that neither a share nor its complement is a difference.  For 16-bit ones some 2^-23 of 1 is
+// enough of a share, which takes half the instructions; gelu's is then Hastings' approximation of the normal distribution's tail (Abramowitz and
+// Stegun, 7.1.26: within 1.5e-7), whose exponential is its slope's as well.
+template <int ACT, bool EXACT, bool SLOPE>
+__device__ __forceinline__ float activation(float x, float& slope) {
+  constexpr float kLog2e = 1.44269504088896340736f;
+  if constexpr (ACT == DP_ACT_RELU) {
     slope = x > 0.f ? 1.f : 0.f;
     return x < 0.f ? 0.f : x;
+  } else if constexpr (ACT == DP_ACT_GELU) {
+    constexpr float kDensity = 0.39894228040143267794f, kRoot = 0.70710678118654752440f;
+    if constexpr (EXACT) {
+      const float share = 0.5f * erfcf(-kRoot * x);
+      if (SLOPE) slope = fmaf(x * kDensity, expf(-0.5f * x * x), share);
+      return x * share;
+    } else {
+      const float e = __builtin_amdgcn_exp2f(-0.5f * kLog2e * x * x), t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * kRoot, fabsf(x), 1.f));
+      float tail = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
+      tail = fmaf(t, tail, 0.5f * 1.421413741f);
+      tail = fmaf(t, tail, 0.5f * -0.284496736f);
+      tail = fmaf(t, tail, 0.5f * 0.254829592f) * t * e;
+      const float share = x < 0.f ? tail : 1.f - tail;
+      if (SLOPE) slope = fmaf(x * kDensity, e, share);
+      return x * share;
+    }
+  } else {
+    float v = x, dv = 1.f;
+    if constexpr (ACT == DP_ACT_GELU_TANH) {           // 1 + tanh(u) = 2 share(2 u)
+      constexpr float c = 1.59576912160573071176f, c3 = c * 0.044715f;
+      v = x * fmaf(c3, x * x, c);
+      dv = fmaf(3.f * c3, x * x, c);
+    }
+    float share, rise;
+    if constexpr (EXACT) {
+      const float e = expf(-fabsf(v)), r = 1.f / (1.f + e);
+      share = v < 0.f ? e * r : r;
+      rise = e * r * r * dv;                           // share (1 - share) dv
+    } else {
+      share = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * v));
+      rise = fmaf(-share, share, share) * dv;
+    }
+    if constexpr (ACT == DP_ACT_SIGMOID) {
+      slope = rise;
+      return share;
+    } else {
+      slope = fmaf(x, rise, share);
+      return x * share;
+    }
   }
-  if (act == DP_ACT_GELU) {
-    const float share = 0.5f * erfcf(-0.70710678118654752440f * x);
-    if (SLOPE) slope = fmaf(x * 0.39894228040143267794f, act_exp<EXACT>(-0.5f * x * x), share);
-    return x * share;
-  }
-  float v = x, dv = 1.f;
-  if (act == DP_ACT_GELU_TANH) {                       // 1 + tanh(u) = 2 share(2 u)
-    constexpr float c = 1.59576912160573071176f, c3 = c * 0.044715f;
-    v = x * fmaf(c3, x * x, c);
-    dv = fmaf(3.f * c3, x * x, c);
-  }
-  const float e = act_exp<EXACT>(-fabsf(v)), r = EXACT ? 1.f / (1.f + e) : __builtin_amdgcn_rcpf(1.f + e);
-  const float share = v < 0.f ? e * r : r;
-  const float rise = e * r * r * dv;                   // share (1 - share) dv
-  if (act == DP_ACT_SIGMOID) {
-    slope = rise;
-    return share;
-  }
-  slope = fmaf(x, rise, share);
-  return x * share;
+}
+
+// f(std::integral_constant<int, act>): the branch is taken once for all of a kernel's values.
+template <class F>
+__device__ __forceinline__ void with_activation(int act, F f) {
+  if (act == DP_ACT_SILU)
+    f(std::integral_constant<int, DP_ACT_SILU>{});
+  else if (act == DP_ACT_GELU)
+    f(std::integral_constant<int, DP_ACT_GELU>{});
+  else if (act == DP_ACT_GELU_TANH)
+    f(std::integral_constant<int, DP_ACT_GELU_TANH>{});
+  else if (act == DP_ACT_RELU)
+    f(std::integral_constant<int, DP_ACT_RELU>{});
+  else
+    f(std::integral_constant<int, DP_ACT_SIGMOID>{});
 }
 
 }  // namespace dpbk

@@ -127,6 +127,7 @@ __global__ void __launch_bounds__(kThreads, 2) gated_f32_kernel(const GatedArgs 
   auto value = [](const void* base, int64_t place) { return static_cast<const float*>(base)[place]; };
   auto put = [](void* base, int64_t place, float x) { static_cast<float*>(base)[place] = x; };
   constexpr int COLS = SETS ? W / 2 : W;
+  auto finish = [&](auto act) {
 #pragma unroll
   for (int y = 0; y < COLS; ++y) {
     const int n = n0 + 16 * COLS * wc + 16 * y + r16;
@@ -146,16 +147,20 @@ __global__ void __launch_bounds__(kThreads, 2) gated_f32_kernel(const GatedArgs 
             put(a.gate, place, gate);
             put(a.up, place, up);
           }
-          put(a.h, place, activation<true, false>(a.act, gate, slope) * up);
+          put(a.h, place, activation<decltype(act)::value, true, false>(gate, slope) * up);
         } else if constexpr (PASS == kHidden) {
-          const float dh = acc[x][y][r], v = activation<true, true>(a.act, value(a.gate, place), slope);
+          const float dh = acc[x][y][r], v = activation<decltype(act)::value, true, true>(value(a.gate, place), slope);
           put(a.dgate, place, dh * value(a.up, place) * slope);
           put(a.dup, place, dh * v);
         } else {
           put(a.dx, place, acc[x][y][r]);
         }
       }
-  }
+  }  };
+  if constexpr (PASS == kInput)
+    finish(std::integral_constant<int, DP_ACT_RELU>{});
+  else
+    with_activation(a.act, finish);
 }
 
 // dgate and dup where dh is given, VEC values a thread.
@@ -168,13 +173,15 @@ __global__ void __launch_bounds__(kThreads) gated_slopes_kernel(const GatedArgs 
   gate.load(a.gate, at);
   up.load(a.up, at);
   float dg[VEC], du[VEC];
+  with_activation(a.act, [&](auto act) {
 #pragma unroll
-  for (int k = 0; k < VEC; ++k) {
-    float slope;
-    const float v = activation<DT == DP_F32, true>(a.act, gate.get(k), slope);
-    dg[k] = dh.get(k) * up.get(k) * slope;
-    du[k] = dh.get(k) * v;
-  }
+    for (int k = 0; k < VEC; ++k) {
+      float slope;
+      const float v = activation<decltype(act)::value, DT == DP_F32, true>(gate.get(k), slope);
+      dg[k] = dh.get(k) * up.get(k) * slope;
+      du[k] = dh.get(k) * v;
+    }
+  });
   gate.set(dg);
   up.set(du);
   gate.store(a.dgate, at);

@@ -130,6 +130,7 @@ __global__ void __launch_bounds__(kThreads) gated_few_kernel(const GatedArgs a, 
 #pragma unroll
     for (int s = 0; s < SETS; ++s) *reinterpret_cast<f32x4*>(sums + ((m * SETS + s) * kWaves + wave) * 256 + r16 * 16 + 4 * h) = acc[m][s];
   __syncthreads();
+  auto finish = [&](auto act) {
   for (int e = tid; e < TM * 256; e += kThreads) {
     const int m = e >> 8, at = e & 255, r = 16 * m + (at >> 4), n = n0 + (at & 15);
     if (r >= a.rows || n >= N) continue;
@@ -158,15 +159,20 @@ __global__ void __launch_bounds__(kThreads) gated_few_kernel(const GatedArgs a, 
         put(a.gate, gate);
         put(a.up, up);
       }
-      put(a.h, activation<false, false>(a.act, gate, slope) * up);
+      put(a.h, activation<decltype(act)::value, false, false>(gate, slope) * up);
     } else if constexpr (PASS == kHidden) {
-      const float up = value(a.up, to), x = activation<false, true>(a.act, value(a.gate, to), slope);
+      const float up = value(a.up, to), x = activation<decltype(act)::value, false, true>(value(a.gate, to), slope);
       put(a.dgate, v[0] * up * slope);
       put(a.dup, v[0] * x);
     } else {
       put(a.dx, v[0]);
     }
   }
+  };
+  if constexpr (PASS == kInput)
+    finish(std::integral_constant<int, DP_ACT_RELU>{});
+  else
+    with_activation(a.act, finish);
 }
 
 template <int PASS, int TM, int DT>

@@ -11,7 +11,7 @@ namespace dpbk {
 
 namespace {
 
-template <int DT>
+template <int ACT, int DT>
 __device__ __forceinline__ void gated_forward_rows(const GatedArgs& a, int64_t at, int n, const float (&v)[2][8]) {
   Values<DT, 8> out, bias;
   float gate[8], up[8], h[8];
@@ -29,7 +29,7 @@ __device__ __forceinline__ void gated_forward_rows(const GatedArgs& a, int64_t a
   }
   float slope;
 #pragma unroll
-  for (int k = 0; k < 8; ++k) h[k] = activation<false, false>(a.act, gate[k], slope) * up[k];
+  for (int k = 0; k < 8; ++k) h[k] = activation<ACT, false, false>(gate[k], slope) * up[k];
   if (a.gate) {
     out.set(gate);
     out.store(a.gate, at);
@@ -44,14 +44,14 @@ template <int DT>
 struct GateAndUp {
   Values<DT, 8> gate, up;
 };
-template <int DT>
+template <int ACT, int DT>
 __device__ __forceinline__ void gated_hidden_rows(const GatedArgs& a, int64_t at, const float (&dh)[8], GateAndUp<DT>& in) {
   Values<DT, 8>&gate = in.gate, &up = in.up;
   float dg[8], du[8];
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     float slope;
-    const float v = activation<false, true>(a.act, gate.get(k), slope);
+    const float v = activation<ACT, false, true>(gate.get(k), slope);
     dg[k] = dh[k] * up.get(k) * slope;
     du[k] = dh[k] * v;
   }
@@ -62,7 +62,7 @@ __device__ __forceinline__ void gated_hidden_rows(const GatedArgs& a, int64_t at
 }
 
 template <int PASS, class S, int DT>
-__global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) gated_tile_kernel(const GatedArgs a, int tiles_m, int tiles_n, int parts) {
+__global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) gated_tile_kernel(const GatedArgs a, int tiles_m, int tiles_n, int whole, int parts) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds_raw[];
   const unsigned lds0 = (unsigned)(uintptr_t)lds_raw;
   ProductShape p;
@@ -77,16 +77,17 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) gated_tile_kerne
   if constexpr (PASS == kHidden) p.s[0] = {a.dy, a.w_down, nullptr};
   if constexpr (PASS == kInput) p.s[0] = {a.dgate, a.w_gate, nullptr};
   p.s[1] = PASS == kInput ? ProductSegment{a.dup, a.w_up, nullptr} : p.s[0];
-  const int tiles = tiles_m * tiles_n, id = grad_logical_tile(blockIdx.x, tiles * parts);
-  int tm, tn, part = 0;
-  if constexpr (PASS == kInput) part = id / tiles;
-  grad_tile_of(tiles_m, tiles_n, id - part * tiles, tm, tn);
+  // tiles from `whole` on are dealt to several workgroups, part by part
+  const int rest = tiles_m * tiles_n - whole, id = grad_logical_tile(blockIdx.x, whole + rest * parts);
+  const bool dealt = PASS == kInput && id >= whole;
+  const int part = dealt ? (id - whole) / rest : 0, tile = id - part * rest, shares = dealt ? parts : 1;
+  int tm, tn;
+  grad_tile_of(tiles_m, tiles_n, tile, tm, tn);
   const int64_t stages = p.segments * ((p.K + kProductTerms - 1) / kProductTerms);
-  p.first = (int)(part * stages / parts);
-  p.stages = (int)((part + 1) * stages / parts) - p.first;
+  p.first = (int)(part * stages / shares);
+  p.stages = (int)((part + 1) * stages / shares) - p.first;
   const int m0 = tm * S::BM, n = tn * (S::SETS ? S::BN / 2 : S::BN), n0[2] = {n, n};
   f32x4 acc[S::TM][S::TN];
-  product_tile<S, DT == DP_F16>(p, m0, n0, lds0, acc);
   auto place = [&](int row, int col) { return (int64_t)(m0 + row) * p.N + n + col; };
   auto inside = [&](int row, int col) { return m0 + row < p.M && n + col < p.N; };
   if constexpr (PASS == kHidden) {
@@ -98,57 +99,73 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) gated_tile_kerne
       }
       return in;
     };
-    product_rows<S, false>(acc, lds0, load, [&](int row, int col, int, const float (&v)[2][8], GateAndUp<DT>& in) {
-      if (inside(row, col)) gated_hidden_rows<DT>(a, place(row, col), v[0], in);
+    ProductAhead<S, false, decltype(load)> ahead(load);
+    product_tile<S, DT == DP_F16>(p, m0, n0, lds0, acc);
+    with_activation(a.act, [&](auto act) {
+      product_rows<S, false>(acc, lds0, ahead, [&](int row, int col, int, const float (&v)[2][8], GateAndUp<DT>& in) {
+        if (inside(row, col)) gated_hidden_rows<decltype(act)::value, DT>(a, place(row, col), v[0], in);
+      });
+    });
+  } else if constexpr (PASS == kForward) {
+    product_tile<S, DT == DP_F16>(p, m0, n0, lds0, acc);
+    NothingAhead<S, true> ahead(NoLoad{});
+    with_activation(a.act, [&](auto act) {
+      product_rows<S, true>(acc, lds0, ahead, [&](int row, int col, int, const float (&v)[2][8], Nothing) {
+        if (inside(row, col)) gated_forward_rows<decltype(act)::value, DT>(a, place(row, col), n + col, v);
+      });
     });
   } else {
-    product_rows<S, PASS == kForward>(acc, lds0, NoLoad{}, [&](int row, int col, int, const float (&v)[2][8], Nothing) {
+    product_tile<S, DT == DP_F16>(p, m0, n0, lds0, acc);
+    NothingAhead<S, false> ahead(NoLoad{});
+    product_rows<S, false>(acc, lds0, ahead, [&](int row, int col, int, const float (&v)[2][8], Nothing) {
       if (!inside(row, col)) return;
-      if constexpr (PASS == kForward) gated_forward_rows<DT>(a, place(row, col), n + col, v);
-      if constexpr (PASS == kInput) {
-        if (parts > 1) {
-          f32x4* const to = reinterpret_cast<f32x4*>(a.partial + (int64_t)part * p.M * p.N + place(row, col));
-          to[0] = f32x4{v[0][0], v[0][1], v[0][2], v[0][3]};
-          to[1] = f32x4{v[0][4], v[0][5], v[0][6], v[0][7]};
-          return;
-        }
-        Values<DT, 8> out;
-        out.set(v[0]);
-        out.store(a.dx, place(row, col));
+      if (dealt) {
+        f32x4* const to = reinterpret_cast<f32x4*>(a.partial + ((int64_t)part * rest + tile - whole) * (S::BM * S::BN) + row * S::BN + col);
+        to[0] = f32x4{v[0][0], v[0][1], v[0][2], v[0][3]};
+        to[1] = f32x4{v[0][4], v[0][5], v[0][6], v[0][7]};
+        return;
       }
+      Values<DT, 8> out;
+      out.set(v[0]);
+      out.store(a.dx, place(row, col));
     });
   }
 }
 
-// The parts' sums, in their order.
+// The parts' sums of the tiles from `whole` on, in their order: eight workgroups to a tile of 128 x 128, eight columns to a thread.
+constexpr int kJoinSide = 128;
 template <int DT>
-__global__ void __launch_bounds__(256) gated_join_kernel(const float* partial, void* dx, int64_t n, int parts) {
-  const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
-  if (at >= n) return;
+__global__ void __launch_bounds__(256) gated_join_kernel(const float* partial, void* dx, int rows, int d, int tiles_m, int tiles_n, int whole, int parts) {
+  const int rest = tiles_m * tiles_n - whole, t = blockIdx.x / 8, at = (blockIdx.x % 8 * 256 + threadIdx.x) * 8;
+  int tm, tn;
+  grad_tile_of(tiles_m, tiles_n, whole + t, tm, tn);
+  const int row = tm * kJoinSide + at / kJoinSide, col = tn * kJoinSide + at % kJoinSide;
+  if (row >= rows || col >= d) return;
   float v[8] = {};
   for (int p = 0; p < parts; ++p) {
-    const f32x4* from = reinterpret_cast<const f32x4*>(partial + p * n + at);
+    const f32x4* from = reinterpret_cast<const f32x4*>(partial + ((int64_t)p * rest + t) * (kJoinSide * kJoinSide) + at);
     const f32x4 x = from[0], y = from[1];
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] += x[k], v[4 + k] += y[k];
   }
   Values<DT, 8> out;
   out.set(v);
-  out.store(dx, at);
+  out.store(dx, (int64_t)row * d + col);
 }
 
+// whole: tiles that one workgroup has each; the others, parts.
 template <int PASS, class S, int DT>
-dp_status launch_tiles(const GatedArgs& a, int parts, hipStream_t s) {
+dp_status launch_tiles(const GatedArgs& a, int64_t whole, int parts, hipStream_t s) {
   static ReadyTable ready;
   dp_status st = allow_big_lds(gated_tile_kernel<PASS, S, DT>, S::LDS_BYTES, ready);
   if (st != DP_OK) return st;
   const int N = PASS == kInput ? a.d : a.f, width = S::SETS ? S::BN / 2 : S::BN;
-  const int tiles_m = (a.rows + S::BM - 1) / S::BM, tiles_n = (N + width - 1) / width;
-  gated_tile_kernel<PASS, S, DT><<<dim3((unsigned)tiles_m * tiles_n * parts), S::NT, S::LDS_BYTES, s>>>(a, tiles_m, tiles_n, parts);
+  const int tiles_m = (a.rows + S::BM - 1) / S::BM, tiles_n = (N + width - 1) / width, tiles = tiles_m * tiles_n;
+  const int first = (int)std::min<int64_t>(whole, tiles), rest = tiles - first;
+  gated_tile_kernel<PASS, S, DT><<<dim3((unsigned)(first + rest * parts)), S::NT, S::LDS_BYTES, s>>>(a, tiles_m, tiles_n, first, parts);
   st = hip_status(hipGetLastError());
-  if (st != DP_OK || parts == 1) return st;
-  const int64_t n = (int64_t)a.rows * a.d;
-  gated_join_kernel<DT><<<dim3((unsigned)((n / 8 + 255) / 256)), 256, 0, s>>>(a.partial, a.dx, n, parts);
+  if (st != DP_OK || rest == 0) return st;
+  gated_join_kernel<DT><<<dim3((unsigned)rest * 8), 256, 0, s>>>(a.partial, a.dx, a.rows, a.d, tiles_m, tiles_n, first, parts);
   return hip_status(hipGetLastError());
 }
 
@@ -166,31 +183,50 @@ dp_status launch_tiles(const GatedArgs& a, int parts, hipStream_t s) {
 // 64 x 12288 x 32768 407, 198; input 32 x 768 x 2048 3.3, 6.6; 16 x 4096 x 11008 27.9, 32.4; 64 x 4096 x 11008 62.1, 34.8.
 struct Choice {
   bool few, large;
-  int parts;
+  int64_t whole;                    // small tiles that one workgroup has each
+  int parts;                        // of the others
+  int64_t dealt;                    // how many those are
 };
 Choice choose(GatedPass pass, int rows, int d, int f, int d_out) {
   const int64_t N = pass == kInput ? d : f, K = pass == kForward ? d : pass == kHidden ? d_out : f;
   const int stages = (int)((K + kProductTerms - 1) / kProductTerms) * (pass == kInput ? 2 : 1);
   auto tiles = [&](int side) { return ((int64_t)rows + side - 1) / side * ((N * (pass == kForward ? 2 : 1) + side - 1) / side); };
-  Choice c = {false, true, 1};
+  Choice c = {false, true, INT64_MAX, 1, 0};
   if (rows <= kGatedFewRows) {
     const double products = (double)rows * (double)K * (double)N;
     c.few = pass == kForward ? tiles(128) < 160 : rows <= 16 || products <= (pass == kHidden ? 3e9 : 1.5e8);
     if (c.few) return c;
   }
-  const float big_rest = pass == kForward ? 10.f : pass == kHidden ? 30.f : 8.f, mid_rest = pass == kForward ? 9.f : pass == kHidden ? 18.f : 8.f;
+  const float big_rest = pass == kForward ? 9.f : pass == kHidden ? 26.f : 8.f, mid_rest = pass == kForward ? 8.f : pass == kHidden ? 14.f : 8.f;
   float best = (float)((tiles(256) + 255) / 256) * (1.5f * stages + big_rest);
-  for (int parts = 1; parts <= (pass == kInput ? 64 : 1) && (parts == 1 || 4 * parts <= stages); ++parts) {
-    const float n = (float)tiles(128) * parts;
-    const float stage = n <= 256.f ? 0.45f : n <= 512.f ? 0.8f : n <= 768.f ? 1.2f : 0.9f / 512.f * n;
-    float cost = stage * stages / parts + std::max(1.f, n / 512.f) * mid_rest;
-    if (parts > 1) cost += 4.f + (2 * parts + 0.5f) * ((float)rows * d * 4e-6f / 6.f);
+  const int64_t total = tiles(128);
+  auto consider = [&](int64_t whole, int parts) {
+    // a compute unit's workgroups: tile-stages at 0.4 us each, 0.05 more where one runs alone
+    const int64_t dealt = total - whole, pieces = dealt * parts, n = whole + pieces;
+    float cost;
+    if (n > 768) {
+      cost = 0.9f / 512.f * stages * (float)total;
+    } else {
+      const float longest = whole ? (float)stages : (float)stages / parts;
+      const float all = (float)((whole + 255) / 256) * stages + (float)((pieces + 255) / 256) * stages / parts;
+      cost = 0.4f * all + 0.05f * std::max(0.f, 2.f * longest - all);
+    }
+    cost += std::max(1.f, (float)n / 512.f) * mid_rest;
+    if (dealt) cost += 4.f + (2 * parts + 0.5f) * ((float)dealt * 65536e-6f / 6.f);
     if (cost < best) {
       best = cost;
       c.large = false;
+      c.whole = whole;
       c.parts = parts;
+      c.dealt = dealt;
     }
-  }
+  };
+  consider(total, 1);
+  if (pass == kInput)
+    for (int parts = 2; parts <= 64 && 4 * parts <= stages; ++parts) {
+      consider(0, parts);
+      if (total > 256 && total % 256) consider(total / 256 * 256, parts);
+    }
   return c;
 }
 
@@ -199,14 +235,14 @@ dp_status launch_pass(const GatedArgs& a, hipStream_t s) {
   constexpr ProductB B = PASS == kForward ? kColumnSets : kRowsOfTerms;
   const Choice c = choose((GatedPass)PASS, a.rows, a.d, a.f, a.d_out);
   if (c.few) return launch_gated_few(a, (dp_dtype)DT, (GatedPass)PASS, s);
-  return c.large ? launch_tiles<PASS, BigProduct<B>, DT>(a, 1, s) : launch_tiles<PASS, MidProduct<B>, DT>(a, c.parts, s);
+  return c.large ? launch_tiles<PASS, BigProduct<B>, DT>(a, c.whole, 1, s) : launch_tiles<PASS, MidProduct<B>, DT>(a, c.whole, c.parts, s);
 }
 
 }  // namespace
 
 size_t gated_input_workspace(int rows, int d, int f, int d_out) {
   const Choice c = choose(kInput, rows, d, f, d_out);
-  return c.parts > 1 ? (size_t)c.parts * rows * d * sizeof(float) : 0;
+  return (size_t)c.parts * c.dealt * (kJoinSide * kJoinSide) * sizeof(float);
 }
 
 dp_status launch_gated_tiles(const GatedArgs& a, dp_dtype dt, GatedPass pass, hipStream_t s) {

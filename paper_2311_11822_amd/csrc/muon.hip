@@ -241,7 +241,8 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) muon_product_ker
     put(r, c, v);
   };
   if constexpr (STEP == kUpdate) {
-    product_rows<S, false>(acc, lds0, NoLoad{}, store);
+    NothingAhead<S, false> ahead(NoLoad{});
+    product_rows<S, false>(acc, lds0, ahead, store);
   } else {
     // below the diagonal: rows of the tile's columns
     auto across = [&](int row, int col, const float (&acc8)[8]) {
@@ -251,7 +252,8 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) muon_product_ker
       finish(r, c, acc8, v);
       put(r, c, v);
     };
-    product_rows<S, false>(acc, lds0, NoLoad{}, store, tm != tn, across);
+    NothingAhead<S, false> ahead(NoLoad{});
+    product_rows<S, false>(acc, lds0, ahead, store, tm != tn, across);
   }
 }
 

@@ -21,6 +21,7 @@
 #pragma once
 
 #include <type_traits>
+#include <utility>
 
 #include "dp_internal.h"
 #include "lds_dma.h"
@@ -368,30 +369,58 @@ __device__ __forceinline__ void product_tile(const ProductShape& p, int m0, cons
   __syncthreads();
 }
 
-// acc's rows to store(row of the tile, column, set, values, ahead): columns 8 at a time, of both sets where PAIRS (v[0] and v[1]), else of one
-// (v[0]).  The wave's 32 rows at a time are turned in LDS, so that whole rows leave.  ahead: what load(row, column, set) brought for this place,
-// asked for 32 rows before.  across(first row, column, values): the same by columns, rows 8 at a time, where `mirror`.
-struct NoMirror {
-  __device__ void operator()(int, int, const float (&)[8]) const {}
+// Where a lane's eight columns of a result's rows are in the epilogue: PAIRS, of both sets, else of one.
+template <class S, bool PAIRS>
+struct ProductPlaces {
+  static constexpr int LANES = S::WTN / (PAIRS ? 16 : 8), PASSES = 32 * LANES / 64, HALF = S::WTN / 2, BLOCKS = S::TM / 2;
+  int c, set, col, first;           // column of the wave's, set, column within it or within the tile; row
+  __device__ __forceinline__ ProductPlaces() {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wc = wave % S::WN;
+    c = 8 * (lane % LANES);
+    set = S::SETS && !PAIRS ? c / HALF : 0;
+    col = S::SETS ? HALF * wc + c % HALF : S::WTN * wc + c;
+    first = wave / S::WN * S::WTM + lane / LANES;
+  }
+  __device__ __forceinline__ int row(int x, int i) const { return first + 32 * x + i * (64 / LANES); }       // of block x, pass i
+};
+
+// What load(row, column, set) brings for each place, asked for a block of 32 rows ahead.  (Asked for before the products, where a small tile's fit the
+// registers, it came no sooner: 4096 x 1280 x 3456 57.0 us, so 59.2.)
+template <class S, bool PAIRS, class Load>
+struct ProductAhead {
+  typedef ProductPlaces<S, PAIRS> Places;
+  Load load;
+  decltype(std::declval<Load>()(0, 0, 0)) values[2][Places::PASSES];
+  __device__ __forceinline__ explicit ProductAhead(Load l) : load(l) {}
+  __device__ __forceinline__ void ask(const Places& at, int x) {
+    if (x >= Places::BLOCKS) return;
+#pragma unroll
+    for (int i = 0; i < Places::PASSES; ++i) values[x & 1][i] = load(at.row(x, i), at.col, at.set);
+  }
 };
 struct Nothing {};
 struct NoLoad {
   __device__ Nothing operator()(int, int, int) const { return {}; }
 };
-template <class S, bool PAIRS, class Load, class Store, class Across = NoMirror>
-__device__ __forceinline__ void product_rows(const f32x4 (&acc)[S::TM][S::TN], unsigned lds0, Load load, Store store, bool mirror = false,
+template <class S, bool PAIRS>
+using NothingAhead = ProductAhead<S, PAIRS, NoLoad>;
+
+// acc's rows to store(row of the tile, column, set, values, ahead's): columns 8 at a time, of both sets where PAIRS (v[0] and v[1]), else of one
+// (v[0]).  The wave's 32 rows at a time are turned in LDS, so that whole rows leave.  across(first row, column, values): the same by columns, rows 8
+// at a time, where `mirror`.
+struct NoMirror {
+  __device__ void operator()(int, int, const float (&)[8]) const {}
+};
+template <class S, bool PAIRS, class Ahead, class Store, class Across = NoMirror>
+__device__ __forceinline__ void product_rows(const f32x4 (&acc)[S::TM][S::TN], unsigned lds0, Ahead& ahead, Store store, bool mirror = false,
                                              Across across = {}) {
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / S::WN * S::WTM, wc = wave % S::WN;
+  typedef ProductPlaces<S, PAIRS> Places;
+  const Places at;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / S::WN * S::WTM, wc = wave % S::WN;
   const unsigned slab = lds0 + wave * S::SLAB_BYTES;
   typedef __attribute__((address_space(3))) f32x4* Lds;
-  constexpr int LANES = S::WTN / (PAIRS ? 16 : 8), PASSES = 32 * LANES / 64, HALF = S::WTN / 2;
-  const int c = 8 * (lane % LANES), set = S::SETS && !PAIRS ? c / HALF : 0;
-  const int col = S::SETS ? HALF * wc + c % HALF : S::WTN * wc + c;       // within a set, or within the tile
-  auto row_of = [&](int x, int i) { return 32 * x + i * (64 / LANES) + lane / LANES; };
-  decltype(load(0, 0, 0)) ahead[2][PASSES];
-#pragma unroll
-  for (int i = 0; i < PASSES; ++i) ahead[0][i] = load(wm + row_of(0, i), col, set);
+  constexpr int PASSES = Places::PASSES, HALF = Places::HALF;
+  ahead.ask(at, 0);
 #pragma unroll
   for (int x = 0; x < S::TM / 2; ++x) {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -400,9 +429,7 @@ __device__ __forceinline__ void product_rows(const f32x4 (&acc)[S::TM][S::TN], u
 #pragma unroll
       for (int y = 0; y < S::TN; ++y)
         *(Lds)(uintptr_t)(slab + 4 * ((16 * h + (lane & 15)) * S::SLAB_PITCH + 16 * y + 4 * (lane >> 4))) = acc[2 * x + h][y];
-    if (x + 1 < S::TM / 2)
-#pragma unroll
-      for (int i = 0; i < PASSES; ++i) ahead[(x + 1) & 1][i] = load(wm + row_of(x + 1, i), col, set);
+    ahead.ask(at, x + 1);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) {
@@ -411,21 +438,21 @@ __device__ __forceinline__ void product_rows(const f32x4 (&acc)[S::TM][S::TN], u
       for (int s = 0; s < (PAIRS ? 2 : 1); ++s)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const f32x4 w = *(Lds)(uintptr_t)(slab + 4 * ((row_of(0, i)) * S::SLAB_PITCH + HALF * s + c + 4 * h));
+          const f32x4 w = *(Lds)(uintptr_t)(slab + 4 * ((at.row(0, i) - wm) * S::SLAB_PITCH + HALF * s + at.c + 4 * h));
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[s][4 * h + e] = w[e];
         }
-      store(wm + row_of(x, i), col, set, v, ahead[x & 1][i]);
+      store(at.row(x, i), at.col, at.set, v, ahead.values[x & 1][i]);
     }
     if (!std::is_same_v<Across, NoMirror> && mirror) {
 #pragma unroll
       for (int i = 0; i < S::WTN / 16; ++i) {                      // four lanes have the 32 rows of a column
-        const int r = 8 * (lane & 3), at = 16 * i + (lane >> 2);
+        const int r = 8 * (lane & 3), column = 16 * i + (lane >> 2);
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          v[e] = *(__attribute__((address_space(3))) const float*)(uintptr_t)(slab + 4 * ((r + e) * S::SLAB_PITCH + at));
-        across(wm + 32 * x + r, S::WTN * wc + at, v);
+          v[e] = *(__attribute__((address_space(3))) const float*)(uintptr_t)(slab + 4 * ((r + e) * S::SLAB_PITCH + column));
+        across(wm + 32 * x + r, S::WTN * wc + column, v);
       }
     }
   }
