@@ -173,12 +173,13 @@ dp_status launch_tiles(const GatedArgs& a, int64_t whole, int parts, hipStream_t
 //
 // 256 large tiles are resident at a time and start and end together: 1.5 us to a stage of 64 terms, and what comes before and after.  Small ones,
 // two to a compute unit, run into each other, one's epilogue beside the other's products: 0.45 us a stage alone on a unit, 0.8 two at a time (0.9
-// with all units full).  Both as measured, us, large and small: forward 4096 x 768 x 2048 31.5, 36.3; 4728 x 784 x 2096 57.4, 50.9;
-// 4096 x 4096 x 11008 609, 728; hidden 16384 x 768 x 2048 112, 97; 4096 x 4096 x 11008 369, 371; input 4096 x 4096 x 11008 517, 752; 2048 x 4096 x
-// 4096 145, 118.
+// with all units full).  Both as measured, us, large and small: forward 4096 x 768 x 2048 30.0, 35.0; 1000 x 1024 x 2816 28.6, 20.5;
+// 4096 x 4096 x 11008 616, 743; hidden 4096 x 1280 x 3456 47.0, 54.1; 16384 x 768 x 2048 92, 90; 2048 x 1280 x 3456 39.4, 28.4; input 4096 x 4096 x
+// 11008 517, 752; 2048 x 4096 x 4096 145, 118.
 // Input gradients contract over 2 f and have few tiles: where small ones leave compute units idle their contraction is dealt to `parts`
 // workgroups, whose sums go through memory (4 bytes an element and part, there and back, at some 6 TB/s) and one more launch.  1, 2, 4, 8 and 16
-// parts, us: 128 x 768 x 2048 27.5, 15.9, 9.9, 7.9, 9.4; 256 x 4096 x 11008 162, 89, 55, 54, 81; 4096 x 1280 x 3456 87.5, 90.6, 95.4, 137, 233.
+// parts, us: 128 x 768 x 2048 27.5, 15.9, 9.9, 7.9, 9.4; 256 x 4096 x 11008 162, 89, 55, 54, 81; 4096 x 1280 x 3456 95.0, 90.2, 94.4, 136, 229,
+// and 76.2 with 256 of its 320 tiles whole and the others, which would be a second one on some units, in four parts.
 // Few rows, there and on tiles (in parts), us: forward 64 x 1280 x 3456 9.7, 16.3; 32 x 4096 x 11008 54.6, 44.1; hidden 32 x 4096 x 11008 26.6, 37.6;
 // 64 x 12288 x 32768 407, 198; input 32 x 768 x 2048 3.3, 6.6; 16 x 4096 x 11008 27.9, 32.4; 64 x 4096 x 11008 62.1, 34.8.
 struct Choice {
@@ -197,7 +198,7 @@ Choice choose(GatedPass pass, int rows, int d, int f, int d_out) {
     c.few = pass == kForward ? tiles(128) < 160 : rows <= 16 || products <= (pass == kHidden ? 3e9 : 1.5e8);
     if (c.few) return c;
   }
-  const float big_rest = pass == kForward ? 9.f : pass == kHidden ? 26.f : 8.f, mid_rest = pass == kForward ? 8.f : pass == kHidden ? 14.f : 8.f;
+  const float big_rest = pass == kForward ? 9.f : pass == kHidden ? 19.f : 8.f, mid_rest = pass == kHidden ? 13.f : 8.f;
   float best = (float)((tiles(256) + 255) / 256) * (1.5f * stages + big_rest);
   const int64_t total = tiles(128);
   auto consider = [&](int64_t whole, int parts) {
