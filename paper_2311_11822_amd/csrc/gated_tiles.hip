@@ -61,8 +61,21 @@ __device__ __forceinline__ void gated_hidden_rows(const GatedArgs& a, int64_t at
   up.store(a.dup, at);
 }
 
+// The tiles of a launch: a grid of m x n, or, small ones, what the large tiles from `cut` on of a grid of large ones are cut into, four each.  The first
+// `whole` have a workgroup each, the others `parts`.
+struct Tiles {
+  int m, n, cut, whole, parts;
+  __host__ __device__ int count() const { return cut < 0 ? m * n : 4 * (m * n - cut); }
+  __device__ __forceinline__ void place(int tile, int& tm, int& tn) const {
+    if (cut < 0) return grad_tile_of(m, n, tile, tm, tn);
+    grad_tile_of(m, n, cut + tile / 4, tm, tn);
+    tm = 2 * tm + (tile >> 1 & 1);
+    tn = 2 * tn + (tile & 1);
+  }
+};
+
 template <int PASS, class S, int DT>
-__global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) gated_tile_kernel(const GatedArgs a, int tiles_m, int tiles_n, int whole, int parts) {
+__global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) gated_tile_kernel(const GatedArgs a, const Tiles tiles) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds_raw[];
   const unsigned lds0 = (unsigned)(uintptr_t)lds_raw;
   ProductShape p;
@@ -77,16 +90,16 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) gated_tile_kerne
   if constexpr (PASS == kHidden) p.s[0] = {a.dy, a.w_down, nullptr};
   if constexpr (PASS == kInput) p.s[0] = {a.dgate, a.w_gate, nullptr};
   p.s[1] = PASS == kInput ? ProductSegment{a.dup, a.w_up, nullptr} : p.s[0];
-  // tiles from `whole` on are dealt to several workgroups, part by part
-  const int rest = tiles_m * tiles_n - whole, id = grad_logical_tile(blockIdx.x, whole + rest * parts);
-  const bool dealt = PASS == kInput && id >= whole;
-  const int part = dealt ? (id - whole) / rest : 0, tile = id - part * rest, shares = dealt ? parts : 1;
+  const int rest = tiles.count() - tiles.whole, id = grad_logical_tile(blockIdx.x, tiles.whole + rest * tiles.parts);
+  const bool dealt = PASS == kInput && id >= tiles.whole;
+  const int part = dealt ? (id - tiles.whole) / rest : 0, tile = id - part * rest, shares = dealt ? tiles.parts : 1;
   int tm, tn;
-  grad_tile_of(tiles_m, tiles_n, tile, tm, tn);
+  tiles.place(tile, tm, tn);
   const int64_t stages = p.segments * ((p.K + kProductTerms - 1) / kProductTerms);
   p.first = (int)(part * stages / shares);
   p.stages = (int)((part + 1) * stages / shares) - p.first;
   const int m0 = tm * S::BM, n = tn * (S::SETS ? S::BN / 2 : S::BN), n0[2] = {n, n};
+  if (m0 >= p.M || n >= p.N) return;                   // of a large tile at the edge
   f32x4 acc[S::TM][S::TN];
   auto place = [&](int row, int col) { return (int64_t)(m0 + row) * p.N + n + col; };
   auto inside = [&](int row, int col) { return m0 + row < p.M && n + col < p.N; };
@@ -120,7 +133,7 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) gated_tile_kerne
     product_rows<S, false>(acc, lds0, ahead, [&](int row, int col, int, const float (&v)[2][8], Nothing) {
       if (!inside(row, col)) return;
       if (dealt) {
-        f32x4* const to = reinterpret_cast<f32x4*>(a.partial + ((int64_t)part * rest + tile - whole) * (S::BM * S::BN) + row * S::BN + col);
+        f32x4* const to = reinterpret_cast<f32x4*>(a.partial + ((int64_t)part * rest + tile - tiles.whole) * (S::BM * S::BN) + row * S::BN + col);
         to[0] = f32x4{v[0][0], v[0][1], v[0][2], v[0][3]};
         to[1] = f32x4{v[0][4], v[0][5], v[0][6], v[0][7]};
         return;
@@ -135,14 +148,14 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) gated_tile_kerne
 // The parts' sums of the tiles from `whole` on, in their order: eight workgroups to a tile of 128 x 128, eight columns to a thread.
 constexpr int kJoinSide = 128;
 template <int DT>
-__global__ void __launch_bounds__(256) gated_join_kernel(const float* partial, void* dx, int rows, int d, int tiles_m, int tiles_n, int whole, int parts) {
-  const int rest = tiles_m * tiles_n - whole, t = blockIdx.x / 8, at = (blockIdx.x % 8 * 256 + threadIdx.x) * 8;
+__global__ void __launch_bounds__(256) gated_join_kernel(const float* partial, void* dx, int rows, int d, const Tiles tiles) {
+  const int rest = tiles.count() - tiles.whole, t = blockIdx.x / 8, at = (blockIdx.x % 8 * 256 + threadIdx.x) * 8;
   int tm, tn;
-  grad_tile_of(tiles_m, tiles_n, whole + t, tm, tn);
+  tiles.place(tiles.whole + t, tm, tn);
   const int row = tm * kJoinSide + at / kJoinSide, col = tn * kJoinSide + at % kJoinSide;
   if (row >= rows || col >= d) return;
   float v[8] = {};
-  for (int p = 0; p < parts; ++p) {
+  for (int p = 0; p < tiles.parts; ++p) {
     const f32x4* from = reinterpret_cast<const f32x4*>(partial + ((int64_t)p * rest + t) * (kJoinSide * kJoinSide) + at);
     const f32x4 x = from[0], y = from[1];
 #pragma unroll
@@ -153,23 +166,23 @@ __global__ void __launch_bounds__(256) gated_join_kernel(const float* partial, v
   out.store(dx, (int64_t)row * d + col);
 }
 
-// whole: tiles that one workgroup has each; the others, parts.
-template <int PASS, class S, int DT>
-dp_status launch_tiles(const GatedArgs& a, int64_t whole, int parts, hipStream_t s) {
-  static ReadyTable ready;
-  dp_status st = allow_big_lds(gated_tile_kernel<PASS, S, DT>, S::LDS_BYTES, ready);
-  if (st != DP_OK) return st;
+template <int PASS, class S>
+Tiles grid_of(const GatedArgs& a, int cut) {
   const int N = PASS == kInput ? a.d : a.f, width = S::SETS ? S::BN / 2 : S::BN;
-  const int tiles_m = (a.rows + S::BM - 1) / S::BM, tiles_n = (N + width - 1) / width, tiles = tiles_m * tiles_n;
-  const int first = (int)std::min<int64_t>(whole, tiles), rest = tiles - first;
-  gated_tile_kernel<PASS, S, DT><<<dim3((unsigned)(first + rest * parts)), S::NT, S::LDS_BYTES, s>>>(a, tiles_m, tiles_n, first, parts);
-  st = hip_status(hipGetLastError());
-  if (st != DP_OK || rest == 0) return st;
-  gated_join_kernel<DT><<<dim3((unsigned)rest * 8), 256, 0, s>>>(a.partial, a.dx, a.rows, a.d, tiles_m, tiles_n, first, parts);
+  return {(a.rows + S::BM - 1) / S::BM, (N + width - 1) / width, cut, 0, 1};
+}
+
+// The first `blocks` workgroups of these tiles.
+template <int PASS, class S, int DT>
+dp_status launch_tiles(const GatedArgs& a, const Tiles& tiles, int64_t blocks, hipStream_t s) {
+  static ReadyTable ready;
+  const dp_status st = allow_big_lds(gated_tile_kernel<PASS, S, DT>, S::LDS_BYTES, ready);
+  if (st != DP_OK) return st;
+  gated_tile_kernel<PASS, S, DT><<<dim3((unsigned)blocks), S::NT, S::LDS_BYTES, s>>>(a, tiles);
   return hip_status(hipGetLastError());
 }
 
-// A pass's kernel: few rows, or large or small tiles, the latter in parts.
+// A pass's kernel: few rows; or large tiles, and small ones for what is left of whole rounds of them, or for all, some of them in parts.
 //
 // 256 large tiles are resident at a time and start and end together: 1.5 us to a stage of 64 terms, and what comes before and after.  Small ones,
 // two to a compute unit, run into each other, one's epilogue beside the other's products: 0.45 us a stage alone on a unit, 0.8 two at a time (0.9
@@ -183,8 +196,8 @@ dp_status launch_tiles(const GatedArgs& a, int64_t whole, int parts, hipStream_t
 // Few rows, there and on tiles (in parts), us: forward 64 x 1280 x 3456 9.7, 16.3; 32 x 4096 x 11008 54.6, 44.1; hidden 32 x 4096 x 11008 26.6, 37.6;
 // 64 x 12288 x 32768 407, 198; input 32 x 768 x 2048 3.3, 6.6; 16 x 4096 x 11008 27.9, 32.4; 64 x 4096 x 11008 62.1, 34.8.
 struct Choice {
-  bool few, large;
-  int64_t whole;                    // small tiles that one workgroup has each
+  bool few;
+  int64_t large, whole;             // large tiles; small ones, of what is left, that one workgroup has each
   int parts;                        // of the others
   int64_t dealt;                    // how many those are
 };
@@ -192,51 +205,72 @@ Choice choose(GatedPass pass, int rows, int d, int f, int d_out) {
   const int64_t N = pass == kInput ? d : f, K = pass == kForward ? d : pass == kHidden ? d_out : f;
   const int stages = (int)((K + kProductTerms - 1) / kProductTerms) * (pass == kInput ? 2 : 1);
   auto tiles = [&](int side) { return ((int64_t)rows + side - 1) / side * ((N * (pass == kForward ? 2 : 1) + side - 1) / side); };
-  Choice c = {false, true, INT64_MAX, 1, 0};
+  const int64_t all_large = tiles(256), all_small = tiles(128);
+  Choice c = {false, all_large, 0, 1, 0};
   if (rows <= kGatedFewRows) {
     const double products = (double)rows * (double)K * (double)N;
-    c.few = pass == kForward ? tiles(128) < 160 : rows <= 16 || products <= (pass == kHidden ? 3e9 : 1.5e8);
+    c.few = pass == kForward ? all_small < 160 : rows <= 16 || products <= (pass == kHidden ? 3e9 : 1.5e8);
     if (c.few) return c;
   }
   const float big_rest = pass == kForward ? 9.f : pass == kHidden ? 19.f : 8.f, mid_rest = pass == kHidden ? 13.f : 8.f;
-  float best = (float)((tiles(256) + 255) / 256) * (1.5f * stages + big_rest);
-  const int64_t total = tiles(128);
-  auto consider = [&](int64_t whole, int parts) {
-    // a compute unit's workgroups: tile-stages at 0.4 us each, 0.05 more where one runs alone
-    const int64_t dealt = total - whole, pieces = dealt * parts, n = whole + pieces;
-    float cost;
+  auto rounds = [&](int64_t large) { return (float)((large + 255) / 256) * (1.5f * stages + big_rest); };
+  float best = rounds(all_large);
+  auto consider = [&](int64_t large, int64_t whole, int parts) {
+    const int64_t total = large ? 4 * (all_large - large) : all_small, dealt = total - whole, pieces = dealt * parts, n = whole + pieces;
+    float cost = large ? rounds(large) + 2.f : 0.f;
     if (n > 768) {
-      cost = 0.9f / 512.f * stages * (float)total;
+      cost += (0.9f + 0.0004f * stages) / 512.f * stages * (float)total;
     } else {
+      // a compute unit's workgroups: tile-stages at 0.4 us each, 0.05 more where one runs alone
       const float longest = whole ? (float)stages : (float)stages / parts;
       const float all = (float)((whole + 255) / 256) * stages + (float)((pieces + 255) / 256) * stages / parts;
-      cost = 0.4f * all + 0.05f * std::max(0.f, 2.f * longest - all);
+      cost += 0.4f * all + 0.05f * std::max(0.f, 2.f * longest - all);
     }
     cost += std::max(1.f, (float)n / 512.f) * mid_rest;
     if (dealt) cost += 4.f + (2 * parts + 0.5f) * ((float)dealt * 65536e-6f / 6.f);
     if (cost < best) {
       best = cost;
-      c.large = false;
+      c.large = large;
       c.whole = whole;
       c.parts = parts;
       c.dealt = dealt;
     }
   };
-  consider(total, 1);
-  if (pass == kInput)
-    for (int parts = 2; parts <= 64 && 4 * parts <= stages; ++parts) {
-      consider(0, parts);
-      if (total > 256 && total % 256) consider(total / 256 * 256, parts);
-    }
+  for (const int64_t large : {(int64_t)0, all_large / 256 * 256}) {
+    if (large == all_large) continue;
+    const int64_t total = large ? 4 * (all_large - large) : all_small;
+    consider(large, total, 1);
+    if (pass == kInput)
+      for (int parts = 2; parts <= 64 && 4 * parts <= stages; ++parts) {
+        consider(large, 0, parts);
+        if (total > 256 && total % 256) consider(large, total / 256 * 256, parts);
+      }
+  }
   return c;
 }
 
 template <int PASS, int DT>
 dp_status launch_pass(const GatedArgs& a, hipStream_t s) {
   constexpr ProductB B = PASS == kForward ? kColumnSets : kRowsOfTerms;
+  typedef BigProduct<B> Big;
+  typedef MidProduct<B> Mid;
   const Choice c = choose((GatedPass)PASS, a.rows, a.d, a.f, a.d_out);
   if (c.few) return launch_gated_few(a, (dp_dtype)DT, (GatedPass)PASS, s);
-  return c.large ? launch_tiles<PASS, BigProduct<B>, DT>(a, c.whole, 1, s) : launch_tiles<PASS, MidProduct<B>, DT>(a, c.whole, c.parts, s);
+  Tiles tiles = grid_of<PASS, Big>(a, -1);
+  const int large = tiles.count();
+  dp_status st = DP_OK;
+  if (c.large > 0) {
+    tiles.whole = large;
+    st = launch_tiles<PASS, Big, DT>(a, tiles, c.large, s);
+  }
+  if (st != DP_OK || c.large == large) return st;
+  tiles = c.large > 0 ? grid_of<PASS, Big>(a, (int)c.large) : grid_of<PASS, Mid>(a, -1);
+  tiles.whole = (int)c.whole;
+  tiles.parts = c.parts;
+  st = launch_tiles<PASS, Mid, DT>(a, tiles, c.whole + c.dealt * c.parts, s);
+  if (st != DP_OK || c.dealt == 0) return st;
+  gated_join_kernel<DT><<<dim3((unsigned)c.dealt * 8), 256, 0, s>>>(a.partial, a.dx, a.rows, a.d, tiles);
+  return hip_status(hipGetLastError());
 }
 
 }  // namespace

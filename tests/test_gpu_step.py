@@ -265,7 +265,9 @@ GATED = [  # rows, d, f, d_out
     (1, 8, 8, 8), (1, 1280, 24, 8), (3, 64, 136, 64), (16, 40, 520, 40), (17, 264, 64, 128), (33, 48, 200, 48), (64, 128, 256, 128), (65, 72, 72, 72),
     (111, 60, 168, 60), (128, 512, 128, 512), (200, 96, 1032, 96), (257, 88, 264, 40), (300, 776, 512, 776), (520, 256, 512, 264), (1030, 40, 40, 40),
     (4, 2056, 1000, 24), (31, 16, 4104, 16), (700, 1032, 264, 512),
-    (2100, 72, 4104, 40), (2100, 4104, 136, 48), (1800, 520, 2600, 136)]
+    (2100, 72, 4104, 40), (2100, 4104, 136, 48), (1800, 520, 2600, 136),
+    # whole rounds of large tiles and some more: forward, hidden and input
+    (4400, 328, 2184, 16), (4400, 40, 4360, 776), (4400, 4360, 520, 24)]
 GATED_F32 = GATED + [(1, 1, 1, 1), (5, 3, 7, 2), (111, 60, 161, 61), (130, 257, 65, 33), (64, 17, 129, 130)]
 GATED_CASES = [(d, *s) for d in DTYPES for s in (GATED_F32 if d == "f32" else [(r, 8 * -(-a // 8), b, 8 * -(-c // 8)) for r, a, b, c in GATED])]
 
