@@ -113,6 +113,7 @@ __global__ void __launch_bounds__(kThreads) muon_start_kernel(const Group g) {
     const float m1 = t.momentum[i];
     return g.ahead < 0.f ? m1 : fmaf(g.ahead, m1, v.get(0) * g.grad_scale);
   };
+#pragma unroll
   for (int k = wave; k < kSide; k += kThreads / 64) {            // rows of the matrix as it lies
     const int row = (turned ? c0 : r0) + k, col = (turned ? r0 : c0) + lane;
     tile[k][lane] = row < t.rows && col < t.cols ? value((int64_t)row * t.cols + col) : 0.f;
@@ -141,19 +142,29 @@ __global__ void __launch_bounds__(kThreads) muon_apply_kernel(const Group g) {
   const int id = blockIdx.x - t.begin, r0 = id / across * kSide, c0 = (id - id / across * across) * kSide;       // of X
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const _Float16* const x = t.x[g.from];
-  for (int k = wave; k < kSide; k += kThreads / 64) {
-    const int r = r0 + k, c = c0 + lane;
+  constexpr int WAVES = kThreads / 64, PER = kSide / WAVES;
+  float param[PER];                                  // on its way while X is turned
+  const int col = (turned ? r0 : c0) + lane;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int row = (turned ? c0 : r0) + wave + i * WAVES;
+    param[i] = row < t.rows && col < t.cols ? t.param[(int64_t)row * t.cols + col] : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int k = wave + i * WAVES, r = r0 + k, c = c0 + lane;
     if (r < m && c < n) {
       const int64_t at = half_at(r, c, pitch);
       tile[k][lane] = ((float)x[at] + (float)x[at + 32]) * (1.f / kScale);
     }
   }
   __syncthreads();
-  for (int k = wave; k < kSide; k += kThreads / 64) {
-    const int row = (turned ? c0 : r0) + k, col = (turned ? r0 : c0) + lane;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int k = wave + i * WAVES, row = (turned ? c0 : r0) + k;
     if (row < t.rows && col < t.cols) {
       const int64_t at = (int64_t)row * t.cols + col;
-      const float w = fmaf(t.keep, t.param[at], -t.rate * (turned ? tile[lane][k] : tile[k][lane]));
+      const float w = fmaf(t.keep, param[i], -t.rate * (turned ? tile[lane][k] : tile[k][lane]));
       t.param[at] = w;
       if constexpr (DT != DP_F32) {
         Values<DT, 1> v;
@@ -387,8 +398,7 @@ dp_status launch_muon(const MuonTensor* tensors, int n, const MuonArgs& a, dp_dt
   if (st != DP_OK) return st;
   total = lay_out(g, [&](const Matrix& t) { return squares(t, false); });
   st = launch(copy_dt == DP_F32 ? muon_apply_kernel<DP_F32> : copy_dt == DP_BF16 ? muon_apply_kernel<DP_BF16> : muon_apply_kernel<DP_F16>, total);
-  if (st != DP_OK) return st;
-  return DP_OK;
+  return st;
 }
 
 }  // namespace dpbk
