@@ -541,7 +541,7 @@ dp_status dp_adamw_multi(const dp_adamw_tensor* tensors, int n_tensors, dp_dtype
 
 /*
  * Heads of queries and keys, between their projection and attention.
- *   B, T      samples and tokens;  H, H_kv: heads of the queries and of the keys (H_kv = 0: queries alone, the keys' pointers and strides are
+ *   B, T      samples (at most 2^21) and tokens;  H, H_kv: heads of the queries and of the keys (H_kv = 0: queries alone, the keys' pointers and strides are
  *             not looked at);  D: a head's width, at most 256 and, for 16-bit types, a multiple of 8
  *   rotary    the first `rotary` columns of a head turn (even, from 0 to D); the others pass
  *   interleaved   1: columns 2 i and 2 i + 1 are a pair; 0: columns i and i + rotary / 2
@@ -616,14 +616,12 @@ dp_status dp_head_norm_backward(const dp_heads_shape* shape, dp_dtype dt, const 
  *   w_gate, w_up   device, [d, f] of type dt;  b_gate, b_up  device, [f] of type dt, each or NULL
  *   gate, up  device, [rows, f] of type dt, kept for the backward pass; both or neither NULL
  *   h         device, [rows, f] of type dt
- *   ws        device scratch, >= dp_gated_workspace_bytes(...), 16-byte aligned; the size is 0 where it is not used
  * For 16-bit types d and f are multiples of 8 and arrays 16-byte aligned (DP_F32: 4-byte).  d and f are at most 2^20.  Results overlap nothing.
  * act: silu x s(x), s the logistic function; gelu x Phi(x); gelu_tanh its form by tanh; relu; sigmoid s(x).
  */
 typedef enum { DP_ACT_SILU = 0, DP_ACT_GELU = 1, DP_ACT_GELU_TANH = 2, DP_ACT_RELU = 3, DP_ACT_SIGMOID = 4 } dp_activation;
-size_t dp_gated_workspace_bytes(dp_dtype dt, int rows, int d, int f);
 dp_status dp_gated(const void* x, dp_dtype dt, int rows, int d, int f, const void* w_gate, const void* w_up, const void* b_gate,
-                   const void* b_up, dp_activation act, void* gate, void* up, void* h, void* ws, size_t ws_bytes, void* stream);
+                   const void* b_up, dp_activation act, void* gate, void* up, void* h, void* stream);
 
 /*
  * Its backward pass.  dgate and dup are the output gradients of the two projections, book-kept as the `g` of two linear layers whose input
@@ -652,6 +650,7 @@ dp_status dp_gated_backward(const void* dy, const void* w_down, int d_out, const
  *                |x| <= 15 on the way, nor A's polynomial (DP_ERR_UNSUPPORTED).
  *   ws           device scratch, >= dp_muon_workspace_bytes(...), 16-byte aligned: some 8 bytes an element of up to 64 matrices at a time and 8 of
  *                each shorter side squared
+ * What is written, workspace included, overlaps nothing else: no matrix is named twice.
  * Matrices go in runs of up to 64, each of them a few launches whatever the number of its matrices.
  */
 typedef struct {

@@ -375,27 +375,23 @@ class GatedFeedForward:
                     raise ValueError(f"contiguous [rows.., {width}] of {self.dtype} on {self.device}, not {tuple(t.shape)} of {t.dtype} on {t.device}")
         return math.prod(lead)
 
-    def _scratch(self, key, stream, size, *args):
-        """The workspace of calls like this one, or None, and their stream."""
-        need = self._need.get(key)
-        if need is None:
-            need = self._need[key] = size(*args)
-        if need == 0:
-            return None, stream
-        stream = dp._stream(stream)
-        return self._ws(need, self.device, self.index, stream), stream
-
     def forward(self, x, h, gate=None, up=None, stream=None) -> None:
         """x: [B, T, d] or [rows, d]; h, and gate and up (kept for backward, or None): [.., f]."""
         rows = self._check((self.d, (x,)), (self.f, (h, gate, up)))
-        ws, stream = self._scratch(rows, stream, dp.dp_gated_workspace_bytes, self.dt, rows, self.d, self.f)
-        dp.dp_gated(x, self.dt, rows, self.d, self.f, *self.weights, *self.biases, self.act, gate, up, h, ws, stream)
+        dp.dp_gated(x, self.dt, rows, self.d, self.f, *self.weights, *self.biases, self.act, gate, up, h, stream)
 
     def backward(self, dy, gate, up, dgate, dup, dx=None, stream=None) -> None:
         """dy: [.., d_out], or with no w_down h's own gradient [.., f]; dgate, dup: [.., f], output gradients of the two projections (may be gate
         and up); dx: [.., d] or None."""
         rows = self._check((self.d_out, (dy,)), (self.f, (gate, up, dgate, dup)), (self.d, (dx,)))
-        ws, stream = self._scratch((rows, dx is None), stream, dp.dp_gated_backward_workspace_bytes, self.dt, rows, self.d, self.f, self.d_out)
+        ws = None
+        if dx is not None:
+            need = self._need.get(rows)
+            if need is None:
+                need = self._need[rows] = dp.dp_gated_backward_workspace_bytes(self.dt, rows, self.d, self.f, self.d_out)
+            if need:
+                stream = dp._stream(stream)
+                ws = self._ws(need, self.device, self.index, stream)
         dp.dp_gated_backward(dy, self.w_down, self.d_out, gate, up, self.dt, rows, self.d, self.f, *self.weights, self.act, dgate, dup, dx, ws,
                              stream)
 
@@ -426,6 +422,9 @@ class Muon:
                 raise ValueError(f"param: matrices, not {tuple(tensors[0].shape)}")
             for name, t, kind in zip(("param", "grad", "momentum", "copy"), tensors, kinds):
                 _same(name, t, tensors[0].shape, kind, self.device)
+        written = [t.data_ptr() for tensors in self.held for t in (tensors[0], *tensors[2:]) if t is not None]
+        if len(set(written)) < len(written):
+            raise ValueError("param, momentum, copy: a tensor twice")
         if self.index < 0:
             raise ValueError(f"tensors on a GPU, not {self.device}")
         self.tensors = dp.muon_tensors([(*t, *t[0].shape, d, x) for t, d, x in zip(self.held, decay, scale)])

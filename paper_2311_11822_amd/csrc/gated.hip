@@ -129,63 +129,64 @@ __global__ void __launch_bounds__(kThreads, 2) gated_f32_kernel(const GatedArgs 
   constexpr int COLS = SETS ? W / 2 : W;
   auto finish = [&](auto act) {
 #pragma unroll
-  for (int y = 0; y < COLS; ++y) {
-    const int n = n0 + 16 * COLS * wc + 16 * y + r16;
-    if (n >= N) continue;
-    const float bg = PASS == kForward && a.b_gate ? value(a.b_gate, n) : 0.f, bu = PASS == kForward && a.b_up ? value(a.b_up, n) : 0.f;
+    for (int y = 0; y < COLS; ++y) {
+      const int n = n0 + 16 * COLS * wc + 16 * y + r16;
+      if (n >= N) continue;
+      const float bg = PASS == kForward && a.b_gate ? value(a.b_gate, n) : 0.f, bu = PASS == kForward && a.b_up ? value(a.b_up, n) : 0.f;
 #pragma unroll
-    for (int x = 0; x < W; ++x)
+      for (int x = 0; x < W; ++x)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int m = m0 + wm + 16 * x + 4 * h + r;
-        if (m >= a.rows) continue;
-        const int64_t place = (int64_t)m * N + n;
-        float slope;
-        if constexpr (PASS == kForward) {
-          const float gate = acc[x][y][r] + bg, up = acc[x][y + W / 2][r] + bu;
-          if (a.gate) {
-            put(a.gate, place, gate);
-            put(a.up, place, up);
+        for (int r = 0; r < 4; ++r) {
+          const int m = m0 + wm + 16 * x + 4 * h + r;
+          if (m >= a.rows) continue;
+          const int64_t place = (int64_t)m * N + n;
+          float slope;
+          if constexpr (PASS == kForward) {
+            const float gate = acc[x][y][r] + bg, up = acc[x][y + W / 2][r] + bu;
+            if (a.gate) {
+              put(a.gate, place, gate);
+              put(a.up, place, up);
+            }
+            put(a.h, place, activation<decltype(act)::value, true, false>(gate, slope) * up);
+          } else if constexpr (PASS == kHidden) {
+            const float dh = acc[x][y][r], v = activation<decltype(act)::value, true, true>(value(a.gate, place), slope);
+            put(a.dgate, place, dh * value(a.up, place) * slope);
+            put(a.dup, place, dh * v);
+          } else {
+            put(a.dx, place, acc[x][y][r]);
           }
-          put(a.h, place, activation<decltype(act)::value, true, false>(gate, slope) * up);
-        } else if constexpr (PASS == kHidden) {
-          const float dh = acc[x][y][r], v = activation<decltype(act)::value, true, true>(value(a.gate, place), slope);
-          put(a.dgate, place, dh * value(a.up, place) * slope);
-          put(a.dup, place, dh * v);
-        } else {
-          put(a.dx, place, acc[x][y][r]);
         }
-      }
-  }  };
+    }
+  };
   if constexpr (PASS == kInput)
     finish(std::integral_constant<int, DP_ACT_RELU>{});
   else
     with_activation(a.act, finish);
 }
 
-// dgate and dup where dh is given, VEC values a thread.
+// dgate and dup where dh is given, VEC values a thread at a time.  Bound by memory.
 template <int DT, int VEC>
 __global__ void __launch_bounds__(kThreads) gated_slopes_kernel(const GatedArgs a, int64_t n) {
-  const int64_t at = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * VEC;
-  if (at >= n) return;
-  Values<DT, VEC> dh, gate, up;
-  dh.load(a.dy, at);
-  gate.load(a.gate, at);
-  up.load(a.up, at);
-  float dg[VEC], du[VEC];
-  with_activation(a.act, [&](auto act) {
+  for (int64_t at = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * VEC; at < n; at += (int64_t)gridDim.x * kThreads * VEC) {
+    Values<DT, VEC> dh, gate, up;
+    dh.load(a.dy, at);
+    gate.load(a.gate, at);
+    up.load(a.up, at);
+    float dg[VEC], du[VEC];
+    with_activation(a.act, [&](auto act) {
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) {
-      float slope;
-      const float v = activation<decltype(act)::value, DT == DP_F32, true>(gate.get(k), slope);
-      dg[k] = dh.get(k) * up.get(k) * slope;
-      du[k] = dh.get(k) * v;
-    }
-  });
-  gate.set(dg);
-  up.set(du);
-  gate.store(a.dgate, at);
-  up.store(a.dup, at);
+      for (int k = 0; k < VEC; ++k) {
+        float slope;
+        const float v = activation<decltype(act)::value, DT == DP_F32, true>(gate.get(k), slope);
+        dg[k] = dh.get(k) * up.get(k) * slope;
+        du[k] = dh.get(k) * v;
+      }
+    });
+    gate.set(dg);
+    up.set(du);
+    gate.store(a.dgate, at);
+    up.store(a.dup, at);
+  }
 }
 
 template <int DT>
@@ -194,7 +195,7 @@ dp_status launch_slopes(const GatedArgs& a, hipStream_t s) {
   constexpr int WIDE = DT == DP_F32 ? 4 : 8;
   const uintptr_t all = (uintptr_t)a.dy | (uintptr_t)a.gate | (uintptr_t)a.up | (uintptr_t)a.dgate | (uintptr_t)a.dup;
   const bool wide = all % 16 == 0 && n % WIDE == 0;
-  const int64_t threads = wide ? n / WIDE : n, blocks = (threads + kThreads - 1) / kThreads;
+  const int64_t threads = wide ? n / WIDE : n, blocks = std::min<int64_t>((threads + kThreads - 1) / kThreads, 1 << 20);
   if (wide)
     gated_slopes_kernel<DT, WIDE><<<dim3((unsigned)blocks), kThreads, 0, s>>>(a, n);
   else

@@ -131,43 +131,43 @@ __global__ void __launch_bounds__(kThreads) gated_few_kernel(const GatedArgs a, 
     for (int s = 0; s < SETS; ++s) *reinterpret_cast<f32x4*>(sums + ((m * SETS + s) * kWaves + wave) * 256 + r16 * 16 + 4 * h) = acc[m][s];
   __syncthreads();
   auto finish = [&](auto act) {
-  for (int e = tid; e < TM * 256; e += kThreads) {
-    const int m = e >> 8, at = e & 255, r = 16 * m + (at >> 4), n = n0 + (at & 15);
-    if (r >= a.rows || n >= N) continue;
-    float v[SETS];
+    for (int e = tid; e < TM * 256; e += kThreads) {
+      const int m = e >> 8, at = e & 255, r = 16 * m + (at >> 4), n = n0 + (at & 15);
+      if (r >= a.rows || n >= N) continue;
+      float v[SETS];
 #pragma unroll
-    for (int s = 0; s < SETS; ++s) {
-      v[s] = 0.f;
+      for (int s = 0; s < SETS; ++s) {
+        v[s] = 0.f;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) v[s] += sums[((m * SETS + s) * kWaves + w) * 256 + at];
-    }
-    const int64_t to = (int64_t)r * N + n;
-    float slope;
-    Values<DT, 1> one;
-    auto value = [&](const void* from, int64_t place) {
-      Values<DT, 1> x;
-      x.load(from, place);
-      return x.get(0);
-    };
-    auto put = [&](void* out, float x) {
-      one.set({x});
-      one.store(out, to);
-    };
-    if constexpr (PASS == kForward) {
-      const float gate = v[0] + (a.b_gate ? value(a.b_gate, n) : 0.f), up = v[SETS - 1] + (a.b_up ? value(a.b_up, n) : 0.f);
-      if (a.gate) {
-        put(a.gate, gate);
-        put(a.up, up);
+        for (int w = 0; w < kWaves; ++w) v[s] += sums[((m * SETS + s) * kWaves + w) * 256 + at];
       }
-      put(a.h, activation<decltype(act)::value, false, false>(gate, slope) * up);
-    } else if constexpr (PASS == kHidden) {
-      const float up = value(a.up, to), x = activation<decltype(act)::value, false, true>(value(a.gate, to), slope);
-      put(a.dgate, v[0] * up * slope);
-      put(a.dup, v[0] * x);
-    } else {
-      put(a.dx, v[0]);
+      const int64_t to = (int64_t)r * N + n;
+      float slope;
+      Values<DT, 1> one;
+      auto value = [&](const void* from, int64_t place) {
+        Values<DT, 1> x;
+        x.load(from, place);
+        return x.get(0);
+      };
+      auto put = [&](void* out, float x) {
+        one.set({x});
+        one.store(out, to);
+      };
+      if constexpr (PASS == kForward) {
+        const float gate = v[0] + (a.b_gate ? value(a.b_gate, n) : 0.f), up = v[SETS - 1] + (a.b_up ? value(a.b_up, n) : 0.f);
+        if (a.gate) {
+          put(a.gate, gate);
+          put(a.up, up);
+        }
+        put(a.h, activation<decltype(act)::value, false, false>(gate, slope) * up);
+      } else if constexpr (PASS == kHidden) {
+        const float up = value(a.up, to), x = activation<decltype(act)::value, false, true>(value(a.gate, to), slope);
+        put(a.dgate, v[0] * up * slope);
+        put(a.dup, v[0] * x);
+      } else {
+        put(a.dx, v[0]);
+      }
     }
-  }
   };
   if constexpr (PASS == kInput)
     finish(std::integral_constant<int, DP_ACT_RELU>{});

@@ -5,7 +5,7 @@
 
 namespace dpbk {
 
-constexpr int kHeadsMaxWidth = 256;
+constexpr int kHeadsMaxWidth = 256, kHeadsMostSamples = 1 << 21;      // (a workgroup to a sample at least, and fewer than 2^32 threads)
 
 struct HeadStrides {                 // elements from one sample, token, head to the next
   int64_t sample, token, head;

@@ -1,5 +1,5 @@
-// Entry points of what gated transformer blocks run besides: heads' rotation and norms, gated feed-forward layers.  Arguments
-// are checked here, on the host, before anything is launched.
+// Entry points of what gated transformer blocks run besides: heads' rotation and norms, gated feed-forward layers, orthogonalised updates.
+// Arguments are checked here, on the host, before anything is launched.
 #include <math.h>
 
 #include <algorithm>
@@ -31,7 +31,7 @@ dp_status heads_args(const dp_heads_shape* p, dp_dtype dt, bool backward, HeadsA
     for (int i = 0; i < 3; ++i)
       if (strides[n][i] < 0 || strides[n][i] > (int64_t)1 << 40 || (dt != DP_F32 && strides[n][i] % 8)) return DP_ERR_INVALID_ARG;
   }
-  if (s.D > kHeadsMaxWidth || (int64_t)s.B * s.T > INT32_MAX || (int64_t)s.H + s.H_kv > 1 << 20) return DP_ERR_UNSUPPORTED;
+  if (s.D > kHeadsMaxWidth || s.B > kHeadsMostSamples || (int64_t)s.B * s.T > INT32_MAX || (int64_t)s.H + s.H_kv > 1 << 20) return DP_ERR_UNSUPPORTED;
   a = HeadsArgs{};
   a.heads[0] = s.H;
   a.heads[1] = s.H_kv;
@@ -52,11 +52,11 @@ dp_status heads_args(const dp_heads_shape* p, dp_dtype dt, bool backward, HeadsA
     // what is written does not overlap itself: by growing stride, each axis steps over all that the ones before span
     struct { int64_t stride, n; } axes[] = {{a.out_stride[w].sample, s.B}, {a.out_stride[w].token, s.T}, {a.out_stride[w].head, a.heads[w]}};
     std::sort(axes, axes + 3, [](const auto& x, const auto& y) { return x.stride < y.stride; });
-    int64_t span = s.D;
+    __int128 span = s.D;
     for (const auto& axis : axes) {
       if (axis.n == 1) continue;
       if (axis.stride < span) return DP_ERR_INVALID_ARG;
-      span += axis.stride * (axis.n - 1);
+      span += (__int128)axis.stride * (axis.n - 1);
     }
   }
   return DP_OK;
@@ -244,14 +244,8 @@ dp_status dp_head_norm_backward(const dp_heads_shape* shape, dp_dtype dt, const 
   return launch_heads(a, dt, kNormGrad, static_cast<hipStream_t>(stream));
 }
 
-size_t dp_gated_workspace_bytes(dp_dtype dt, int rows, int d, int f) {
-  (void)dt, (void)rows, (void)d, (void)f;
-  return 0;
-}
-
 dp_status dp_gated(const void* x, dp_dtype dt, int rows, int d, int f, const void* w_gate, const void* w_up, const void* b_gate,
-                   const void* b_up, dp_activation act, void* gate, void* up, void* h, void* ws, size_t ws_bytes, void* stream) {
-  (void)ws, (void)ws_bytes;
+                   const void* b_up, dp_activation act, void* gate, void* up, void* h, void* stream) {
   const dp_status st = gated_shape(dt, rows, d, f, d);
   if (st != DP_OK) return st;
   if (!act_ok(act) || !there(x, dt) || !there(w_gate, dt) || !there(w_up, dt) || !there(h, dt) || !gate != !up) return DP_ERR_INVALID_ARG;

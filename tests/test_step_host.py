@@ -42,12 +42,17 @@ def calls(s, dt=dp.DP_BF16, q=FAKE, k=FAKE, q_out=FAKE, k_out=FAKE):
     (dict(rotary=-2), INV), (dict(rotary=7), INV), (dict(interleaved=2), INV), (dict(amplitude=math.nan), INV), (dict(amplitude=math.inf), INV),
     (dict(turns=None), INV), (dict(turns=FAKE + 4), INV), (dict(position=FAKE + 2), INV), (dict(len=FAKE + 1), INV), (dict(q=(8448, 256, -64)), INV),
     (dict(k=(8448, 132, 64)), INV), (dict(qo=(8448, 256, 60)), INV), (dict(D=264, rotary=64), UNS), (dict(B=1 << 16, T=1 << 16), UNS),
-    (dict(H=1 << 21), UNS)], ids=str)
+    (dict(H=1 << 21), UNS), (dict(B=(1 << 21) + 1, T=1), UNS)], ids=str)
 def test_heads_refuse_shapes(change, status):
     s = shape(**change)
     forward, back = calls(s)
     assert forward == (status,) * 2 and back == (status,) * 2
     assert dp.dp_head_norm_workspace_bytes(s, dp.DP_BF16) == 0
+
+
+def test_heads_refuse_strides_whose_span_passes_64_bits():
+    far = (1 << 40, 1 << 39, 64)                          # 2^24 tokens span 2^63
+    assert calls(shape(B=2, T=1 << 24, qo=far, ko=far, q=far, k=far)) == ((INV,) * 2,) * 2
 
 
 def test_heads_refuse_arguments():
@@ -137,8 +142,7 @@ def test_heads_objects_refuse():
 
 # ------------------------------------------------------------------------------------------------ gated feed-forward layers
 
-GATED = dict(x=FAKE, dt=dp.DP_BF16, rows=4, d=16, f=24, w_gate=FAKE, w_up=FAKE, b_gate=None, b_up=None, act=0, gate=None, up=None, h=FAKE, ws=None,
-             ws_bytes=0, stream=None)
+GATED = dict(x=FAKE, dt=dp.DP_BF16, rows=4, d=16, f=24, w_gate=FAKE, w_up=FAKE, b_gate=None, b_up=None, act=0, gate=None, up=None, h=FAKE, stream=None)
 
 
 @pytest.mark.parametrize("change,status", [
@@ -163,15 +167,10 @@ def test_gated_backward_refuses(change, status):
 
 
 def test_gated_workspaces():
-    for size, args in ((dp.dp_gated_workspace_bytes, (4, 16, 24)), (dp.dp_gated_backward_workspace_bytes, (4, 16, 24, 16))):
-        assert size(7, *args) == 0 == size(dp.DP_BF16, 0, *args[1:])
+    size = dp.dp_gated_backward_workspace_bytes
+    assert size(7, 4, 16, 24, 16) == 0 == size(dp.DP_BF16, 0, 16, 24, 16)
     # where a workspace is used it is asked for
     for rows, d, f in ((1, 1280, 3456), (1, 16, 1 << 20), (1, 1 << 20, 16), (64, 768, 2048), (4096, 1280, 3456)):
-        n = dp.dp_gated_workspace_bytes(dp.DP_BF16, rows, d, f)
-        if n:
-            args = dict(GATED, rows=rows, d=d, f=f)
-            assert dp.lib.dp_gated(*changed(args, ws=FAKE, ws_bytes=n - 1)) == WS == dp.lib.dp_gated(*changed(args))
-            assert dp.lib.dp_gated(*changed(args, ws=FAKE + 4, ws_bytes=n)) == INV
         n = dp.dp_gated_backward_workspace_bytes(dp.DP_F16, rows, d, f, d)
         if n:
             args = dict(GATED_BACK, rows=rows, d=d, f=f, d_out=d)
@@ -246,6 +245,10 @@ def test_muon_object_refuses():
                      (right, dict(copy=[])), (right, dict(copy=[f(3, 5).half()])), (right, dict(scale=[1.0, 2.0])), (right, {})]:
         with pytest.raises(ValueError):
             block.Muon(*args, **kw)
+    twice = f(3, 4)
+    for args in (([twice] * 2, [f(3, 4)] * 2, [f(3, 4), f(3, 4)]), ([f(3, 4), f(3, 4)], [f(3, 4)] * 2, [twice] * 2), ([twice], [f(3, 4)], [twice])):
+        with pytest.raises(ValueError, match="twice"):
+            block.Muon(*args, 0.0)
     with pytest.raises(TypeError):
         block.Muon(*right, copy=[f(3, 4)])
     with pytest.raises(TypeError):
