@@ -616,12 +616,14 @@ dp_status dp_head_norm_backward(const dp_heads_shape* shape, dp_dtype dt, const 
  *   w_gate, w_up   device, [d, f] of type dt;  b_gate, b_up  device, [f] of type dt, each or NULL
  *   gate, up  device, [rows, f] of type dt, kept for the backward pass; both or neither NULL
  *   h         device, [rows, f] of type dt
+ *   ws        device scratch, >= dp_gated_workspace_bytes(...), 16-byte aligned; not used where the size is 0
  * For 16-bit types d and f are multiples of 8 and arrays 16-byte aligned (DP_F32: 4-byte).  d and f are at most 2^20.  Results overlap nothing.
  * act: silu x s(x), s the logistic function; gelu x Phi(x); gelu_tanh its form by tanh; relu; sigmoid s(x).
  */
 typedef enum { DP_ACT_SILU = 0, DP_ACT_GELU = 1, DP_ACT_GELU_TANH = 2, DP_ACT_RELU = 3, DP_ACT_SIGMOID = 4 } dp_activation;
+size_t dp_gated_workspace_bytes(dp_dtype dt, int rows, int d, int f);
 dp_status dp_gated(const void* x, dp_dtype dt, int rows, int d, int f, const void* w_gate, const void* w_up, const void* b_gate,
-                   const void* b_up, dp_activation act, void* gate, void* up, void* h, void* stream);
+                   const void* b_up, dp_activation act, void* gate, void* up, void* h, void* ws, size_t ws_bytes, void* stream);
 
 /*
  * Its backward pass.  dgate and dup are the output gradients of the two projections, book-kept as the `g` of two linear layers whose input
@@ -630,8 +632,8 @@ dp_status dp_gated(const void* x, dp_dtype dt, int rows, int d, int f, const voi
  *   dy        device, [rows, d_out] of type dt, with w_down device [f, d_out];  or, w_down NULL, dh itself, [rows, f] (d_out is not looked at)
  *   gate, up  dp_gated's;  dgate, dup  device, [rows, f] of type dt; they may be gate and up, or one of them dh
  *   dx        device, [rows, d] of type dt, or NULL: not wanted (then the weights may be NULL)
- *   ws        device scratch, >= dp_gated_backward_workspace_bytes(...), 16-byte aligned; not used without dx, nor where the size is 0.  (d_out is
- *             not looked at for its size.)
+ *   ws        device scratch, >= dp_gated_backward_workspace_bytes(...), 16-byte aligned; not used where the size is 0.  The size is for calls with
+ *             dx or without; d_out = 0: with no w_down
  */
 size_t dp_gated_backward_workspace_bytes(dp_dtype dt, int rows, int d, int f, int d_out);
 dp_status dp_gated_backward(const void* dy, const void* w_down, int d_out, const void* gate, const void* up, dp_dtype dt, int rows, int d,

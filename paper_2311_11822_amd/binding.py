@@ -115,7 +115,8 @@ _PROTOS = {
     "dp_head_norm": (_i, [C.POINTER(dp_heads_shape), _i, _vp, _vp, _vp, _vp, _f, _vp, _vp, _vp]),
     "dp_head_norm_workspace_bytes": (_sz, [C.POINTER(dp_heads_shape), _i]),
     "dp_head_norm_backward": (_i, [C.POINTER(dp_heads_shape), _i, _vp, _vp, _vp, _vp, _vp, _vp, _f, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
-    "dp_gated": (_i, [_vp, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp, _vp, _vp, _vp]),
+    "dp_gated_workspace_bytes": (_sz, [_i, _i, _i, _i]),
+    "dp_gated": (_i, [_vp, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
     "dp_gated_backward_workspace_bytes": (_sz, [_i, _i, _i, _i, _i]),
     "dp_gated_backward": (_i, [_vp, _vp, _i, _vp, _vp, _i, _i, _i, _i, _vp, _vp, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
     "dp_muon_workspace_bytes": (_sz, [C.POINTER(dp_muon_tensor), _i]),
@@ -454,8 +455,12 @@ def dp_head_norm_backward(shape, dt, q, k, dq_out, dk_out, q_gain, k_gain, eps, 
     _call("dp_head_norm_backward", shape, dt, q, k, dq_out, dk_out, q_gain, k_gain, eps, dq, dk, kept, sqnorm_out, ws, _nbytes(ws), stream)
 
 
-def dp_gated(x, dt, rows, d, f, w_gate, w_up, b_gate, b_up, act, gate, up, h, stream=None) -> None:
-    _call("dp_gated", x, dt, rows, d, f, w_gate, w_up, b_gate, b_up, act, gate, up, h, stream)
+def dp_gated_workspace_bytes(dt, rows, d, f) -> int:
+    return lib.dp_gated_workspace_bytes(dt, rows, d, f)
+
+
+def dp_gated(x, dt, rows, d, f, w_gate, w_up, b_gate, b_up, act, gate, up, h, ws=None, stream=None) -> None:
+    _call("dp_gated", x, dt, rows, d, f, w_gate, w_up, b_gate, b_up, act, gate, up, h, ws, _nbytes(ws), stream)
 
 
 def dp_gated_backward_workspace_bytes(dt, rows, d, f, d_out) -> int:

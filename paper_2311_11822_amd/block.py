@@ -375,23 +375,28 @@ class GatedFeedForward:
                     raise ValueError(f"contiguous [rows.., {width}] of {self.dtype} on {self.device}, not {tuple(t.shape)} of {t.dtype} on {t.device}")
         return math.prod(lead)
 
+    def _scratch(self, key, stream, size, *args):
+        """The workspace of calls like this one, or None, and their stream."""
+        need = self._need.get(key)
+        if need is None:
+            need = self._need[key] = size(*args)
+        if need == 0:
+            return None, stream
+        stream = dp._stream(stream)
+        return self._ws(need, self.device, self.index, stream), stream
+
     def forward(self, x, h, gate=None, up=None, stream=None) -> None:
         """x: [B, T, d] or [rows, d]; h, and gate and up (kept for backward, or None): [.., f]."""
         rows = self._check((self.d, (x,)), (self.f, (h, gate, up)))
-        dp.dp_gated(x, self.dt, rows, self.d, self.f, *self.weights, *self.biases, self.act, gate, up, h, stream)
+        ws, stream = self._scratch((rows,), stream, dp.dp_gated_workspace_bytes, self.dt, rows, self.d, self.f)
+        dp.dp_gated(x, self.dt, rows, self.d, self.f, *self.weights, *self.biases, self.act, gate, up, h, ws, stream)
 
     def backward(self, dy, gate, up, dgate, dup, dx=None, stream=None) -> None:
         """dy: [.., d_out], or with no w_down h's own gradient [.., f]; dgate, dup: [.., f], output gradients of the two projections (may be gate
         and up); dx: [.., d] or None."""
         rows = self._check((self.d_out, (dy,)), (self.f, (gate, up, dgate, dup)), (self.d, (dx,)))
-        ws = None
-        if dx is not None:
-            need = self._need.get(rows)
-            if need is None:
-                need = self._need[rows] = dp.dp_gated_backward_workspace_bytes(self.dt, rows, self.d, self.f, self.d_out)
-            if need:
-                stream = dp._stream(stream)
-                ws = self._ws(need, self.device, self.index, stream)
+        ws, stream = self._scratch((rows, "backward"), stream, dp.dp_gated_backward_workspace_bytes, self.dt, rows, self.d, self.f,
+                                   0 if self.w_down is None else self.d_out)
         dp.dp_gated_backward(dy, self.w_down, self.d_out, gate, up, self.dt, rows, self.d, self.f, *self.weights, self.act, dgate, dup, dx, ws,
                              stream)
 

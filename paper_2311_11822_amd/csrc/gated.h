@@ -15,13 +15,14 @@ struct GatedArgs {
   void *dgate, *dup, *dx;                              // [rows, f], [rows, f], [rows, d] or null
   int rows, d, f, d_out;
   int act;
-  float* partial;                                      // dx: [parts, rows, d] where the contraction is dealt to several workgroups
+  float* partial;                                      // sums of tiles whose contraction is dealt to several workgroups
 };
 
 // The products: x with both weights; dy with w_down; dgate and dup with theirs.
 enum GatedPass { kForward, kHidden, kInput };
 dp_status launch_gated_tiles(const GatedArgs& a, dp_dtype dt, GatedPass pass, hipStream_t s);      // 16-bit types (gated_tiles.hip)
-size_t gated_input_workspace(int rows, int d, int f, int d_out);                                   // of their input gradients: `partial`
+size_t gated_tiles_workspace(GatedPass pass, int rows, int d, int f, int d_out);                   // bytes of `partial`
+size_t gated_workspace(dp_dtype dt, GatedPass pass, int rows, int d, int f, int d_out);            // of any type
 constexpr int kGatedFewRows = 64;
 dp_status launch_gated_few(const GatedArgs& a, dp_dtype dt, GatedPass pass, hipStream_t s);        // up to kGatedFewRows of them (gated_few.hip)
 dp_status launch_gated_forward(const GatedArgs& a, dp_dtype dt, hipStream_t s);

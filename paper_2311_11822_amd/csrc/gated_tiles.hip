@@ -74,6 +74,8 @@ struct Tiles {
   }
 };
 
+constexpr int kJoinSide = 128;       // of tiles that are dealt in parts
+
 template <int PASS, class S, int DT>
 __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) gated_tile_kernel(const GatedArgs a, const Tiles tiles) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds_raw[];
@@ -91,7 +93,7 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) gated_tile_kerne
   if constexpr (PASS == kInput) p.s[0] = {a.dgate, a.w_gate, nullptr};
   p.s[1] = PASS == kInput ? ProductSegment{a.dup, a.w_up, nullptr} : p.s[0];
   const int rest = tiles.count() - tiles.whole, id = grad_logical_tile(blockIdx.x, tiles.whole + rest * tiles.parts);
-  const bool dealt = PASS == kInput && id >= tiles.whole;
+  const bool dealt = S::BM == kJoinSide && id >= tiles.whole;
   const int part = dealt ? (id - tiles.whole) / rest : 0, tile = id - part * rest, shares = dealt ? tiles.parts : 1;
   int tm, tn;
   tiles.place(tile, tm, tn);
@@ -101,12 +103,22 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) gated_tile_kerne
   const int m0 = tm * S::BM, n = tn * (S::SETS ? S::BN / 2 : S::BN), n0[2] = {n, n};
   if (m0 >= p.M || n >= p.N) return;                   // of a large tile at the edge
   f32x4 acc[S::TM][S::TN];
+  // a part's sums: [row][column], of two sets one beside the other
+  float* const partial = a.partial + ((int64_t)part * rest + tile - tiles.whole) * (S::BM * S::BN);
+  auto keep = [&](int row, int col, int, const float (&v)[2][8], Nothing) {
+#pragma unroll
+    for (int set = 0; set < (S::SETS ? 2 : 1); ++set) {
+      f32x4* const to = reinterpret_cast<f32x4*>(partial + row * S::BN + set * (S::BN / 2) + col);
+      to[0] = f32x4{v[set][0], v[set][1], v[set][2], v[set][3]};
+      to[1] = f32x4{v[set][4], v[set][5], v[set][6], v[set][7]};
+    }
+  };
   auto place = [&](int row, int col) { return (int64_t)(m0 + row) * p.N + n + col; };
   auto inside = [&](int row, int col) { return m0 + row < p.M && n + col < p.N; };
   if constexpr (PASS == kHidden) {
     auto load = [&](int row, int col, int) {
       GateAndUp<DT> in;
-      if (inside(row, col)) {
+      if (!dealt && inside(row, col)) {
         in.gate.load(a.gate, place(row, col));
         in.up.load(a.up, place(row, col));
       }
@@ -114,6 +126,11 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) gated_tile_kerne
     };
     ProductAhead<S, false, decltype(load)> ahead(load);
     product_tile<S, DT == DP_F16>(p, m0, n0, lds0, acc);
+    if (dealt) {
+      NothingAhead<S, false> none(NoLoad{});
+      product_rows<S, false>(acc, lds0, none, keep);
+      return;
+    }
     with_activation(a.act, [&](auto act) {
       product_rows<S, false>(acc, lds0, ahead, [&](int row, int col, int, const float (&v)[2][8], GateAndUp<DT>& in) {
         if (inside(row, col)) gated_hidden_rows<decltype(act)::value, DT>(a, place(row, col), v[0], in);
@@ -122,6 +139,10 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) gated_tile_kerne
   } else if constexpr (PASS == kForward) {
     product_tile<S, DT == DP_F16>(p, m0, n0, lds0, acc);
     NothingAhead<S, true> ahead(NoLoad{});
+    if (dealt) {
+      product_rows<S, true>(acc, lds0, ahead, keep);
+      return;
+    }
     with_activation(a.act, [&](auto act) {
       product_rows<S, true>(acc, lds0, ahead, [&](int row, int col, int, const float (&v)[2][8], Nothing) {
         if (inside(row, col)) gated_forward_rows<decltype(act)::value, DT>(a, place(row, col), n + col, v);
@@ -130,14 +151,12 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) gated_tile_kerne
   } else {
     product_tile<S, DT == DP_F16>(p, m0, n0, lds0, acc);
     NothingAhead<S, false> ahead(NoLoad{});
+    if (dealt) {
+      product_rows<S, false>(acc, lds0, ahead, keep);
+      return;
+    }
     product_rows<S, false>(acc, lds0, ahead, [&](int row, int col, int, const float (&v)[2][8], Nothing) {
       if (!inside(row, col)) return;
-      if (dealt) {
-        f32x4* const to = reinterpret_cast<f32x4*>(a.partial + ((int64_t)part * rest + tile - tiles.whole) * (S::BM * S::BN) + row * S::BN + col);
-        to[0] = f32x4{v[0][0], v[0][1], v[0][2], v[0][3]};
-        to[1] = f32x4{v[0][4], v[0][5], v[0][6], v[0][7]};
-        return;
-      }
       Values<DT, 8> out;
       out.set(v[0]);
       out.store(a.dx, place(row, col));
@@ -145,25 +164,38 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) gated_tile_kerne
   }
 }
 
-// The parts' sums of the tiles from `whole` on, in their order: eight workgroups to a tile of 128 x 128, eight columns to a thread.
-constexpr int kJoinSide = 128;
-template <int DT>
-__global__ void __launch_bounds__(256) gated_join_kernel(const float* partial, void* dx, int rows, int d, const Tiles tiles) {
-  const int rest = tiles.count() - tiles.whole, t = blockIdx.x / 8, at = (blockIdx.x % 8 * 256 + threadIdx.x) * 8;
+// The parts' sums of the tiles from `whole` on, in their order, and what becomes of them: eight columns (of both sets) to a thread.
+template <int PASS, int DT>
+__global__ void __launch_bounds__(256) gated_join_kernel(const GatedArgs a, const Tiles tiles) {
+  constexpr int SETS = PASS == kForward ? 2 : 1, WIDTH = kJoinSide / SETS, GROUPS = kJoinSide * WIDTH / 2048;
+  const int rest = tiles.count() - tiles.whole, t = blockIdx.x / GROUPS, at = (blockIdx.x % GROUPS * 256 + threadIdx.x) * 8;
   int tm, tn;
   tiles.place(tiles.whole + t, tm, tn);
-  const int row = tm * kJoinSide + at / kJoinSide, col = tn * kJoinSide + at % kJoinSide;
-  if (row >= rows || col >= d) return;
-  float v[8] = {};
+  const int N = PASS == kInput ? a.d : a.f, row = tm * kJoinSide + at / WIDTH, col = tn * WIDTH + at % WIDTH;
+  if (row >= a.rows || col >= N) return;
+  const int64_t to = (int64_t)row * N + col;
+  float v[2][8] = {};
   for (int p = 0; p < tiles.parts; ++p) {
-    const f32x4* from = reinterpret_cast<const f32x4*>(partial + ((int64_t)p * rest + t) * (kJoinSide * kJoinSide) + at);
-    const f32x4 x = from[0], y = from[1];
+    const float* const from = a.partial + ((int64_t)p * rest + t) * (kJoinSide * kJoinSide) + at / WIDTH * kJoinSide + at % WIDTH;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] += x[k], v[4 + k] += y[k];
+    for (int set = 0; set < SETS; ++set) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(from + set * WIDTH), y = *reinterpret_cast<const f32x4*>(from + set * WIDTH + 4);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[set][k] += x[k], v[set][4 + k] += y[k];
+    }
   }
-  Values<DT, 8> out;
-  out.set(v);
-  out.store(dx, (int64_t)row * d + col);
+  if constexpr (PASS == kForward) {
+    with_activation(a.act, [&](auto act) { gated_forward_rows<decltype(act)::value, DT>(a, to, col, v); });
+  } else if constexpr (PASS == kHidden) {
+    GateAndUp<DT> in;
+    in.gate.load(a.gate, to);
+    in.up.load(a.up, to);
+    with_activation(a.act, [&](auto act) { gated_hidden_rows<decltype(act)::value, DT>(a, to, v[0], in); });
+  } else {
+    Values<DT, 8> out;
+    out.set(v[0]);
+    out.store(a.dx, to);
+  }
 }
 
 template <int PASS, class S>
@@ -189,12 +221,14 @@ dp_status launch_tiles(const GatedArgs& a, const Tiles& tiles, int64_t blocks, h
 // with all units full).  Both as measured, us, large and small: forward 4096 x 768 x 2048 30.0, 35.0; 1000 x 1024 x 2816 28.6, 20.5;
 // 4096 x 4096 x 11008 616, 743; hidden 4096 x 1280 x 3456 47.0, 54.1; 16384 x 768 x 2048 92, 90; 2048 x 1280 x 3456 39.4, 28.4; input 4096 x 4096 x
 // 11008 517, 752; 2048 x 4096 x 4096 145, 118.
-// Input gradients contract over 2 f and have few tiles: where small ones leave compute units idle their contraction is dealt to `parts`
-// workgroups, whose sums go through memory (4 bytes an element and part, there and back, at some 6 TB/s) and one more launch.  1, 2, 4, 8 and 16
-// parts, us: 128 x 768 x 2048 27.5, 15.9, 9.9, 7.9, 9.4; 256 x 4096 x 11008 162, 89, 55, 54, 81; 4096 x 1280 x 3456 95.0, 90.2, 94.4, 136, 229,
-// and 76.2 with 256 of its 320 tiles whole and the others, which would be a second one on some units, in four parts.
-// Few rows, there and on tiles (in parts), us: forward 64 x 1280 x 3456 9.7, 16.3; 32 x 4096 x 11008 54.6, 44.1; hidden 32 x 4096 x 11008 26.6, 37.6;
-// 64 x 12288 x 32768 407, 198; input 32 x 768 x 2048 3.3, 6.6; 16 x 4096 x 11008 27.9, 32.4; 64 x 4096 x 11008 62.1, 34.8.
+// Where small tiles leave compute units idle, as most input gradients', which contract over 2 f, their contraction is dealt to `parts`
+// workgroups, whose sums go through memory (4 bytes an element and part, there and back, at some 6 TB/s) and one more launch.  Input gradients in
+// 1, 2, 4, 8 and 16 parts, us: 128 x 768 x 2048 27.5, 15.9, 9.9, 7.9, 9.4; 256 x 4096 x 11008 162, 89, 55, 54, 81; 4096 x 1280 x 3456 95.0, 90.2,
+// 94.4, 136, 229, and 76.2 with 256 of its 320 tiles whole and the others, which would be a second one on some units, in four parts.  Other passes,
+// whole and in parts: forward 1014 x 7416 x 216 70, 24; 256 x 4096 x 1024 39, 20; hidden, d_out 4096, 1014 x 1024 35, 22.
+// Few rows, there and on tiles (in parts), us: forward 16 x 4096 x 2048 14.4, 17.8; 64 x 2048 x 4096 15.2, 17.7; 16 x 7424 x 768 26.3, 17.8;
+// 64 x 4096 x 4096 25.3, 21.8; hidden, d_out first, 16 x 8192 x 11008 35.6, 38.8; 64 x 2048 x 4096 10.9, 16.1; 64 x 7424 x 2048 22.5, 18.1; input,
+// 2 f last, 16 x 4096 x 16384 18.0, 23.1; 64 x 4096 x 2048 3.5, 9.5; 64 x 11008 x 4096 33.6, 20.5; 64 x 216 x 7424 18.9, 10.6.
 struct Choice {
   bool few;
   int64_t large, whole;             // large tiles; small ones, of what is left, that one workgroup has each
@@ -208,8 +242,11 @@ Choice choose(GatedPass pass, int rows, int d, int f, int d_out) {
   const int64_t all_large = tiles(256), all_small = tiles(128);
   Choice c = {false, all_large, 0, 1, 0};
   if (rows <= kGatedFewRows) {
-    const double products = (double)rows * (double)K * (double)N;
-    c.few = pass == kForward ? all_small < 160 : rows <= 16 || products <= (pass == kHidden ? 3e9 : 1.5e8);
+    const double weights = (double)stages * kProductTerms * (double)N;
+    if (pass == kForward)
+      c.few = K <= 4096 && (rows + 32) * weights <= 8e8;
+    else
+      c.few = (double)rows * rows * weights <= 4e10 && (pass == kHidden || rows * stages <= 4096);
     if (c.few) return c;
   }
   const float big_rest = pass == kForward ? 9.f : pass == kHidden ? 19.f : 8.f, mid_rest = pass == kHidden ? 13.f : 8.f;
@@ -240,11 +277,11 @@ Choice choose(GatedPass pass, int rows, int d, int f, int d_out) {
     if (large == all_large) continue;
     const int64_t total = large ? 4 * (all_large - large) : all_small;
     consider(large, total, 1);
-    if (pass == kInput)
-      for (int parts = 2; parts <= 64 && 4 * parts <= stages; ++parts) {
-        consider(large, 0, parts);
-        if (total > 256 && total % 256) consider(large, total / 256 * 256, parts);
-      }
+    for (const int parts : {2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64}) {
+      if (4 * parts > stages) break;
+      consider(large, 0, parts);
+      if (total > 256 && total % 256) consider(large, total / 256 * 256, parts);
+    }
   }
   return c;
 }
@@ -269,15 +306,15 @@ dp_status launch_pass(const GatedArgs& a, hipStream_t s) {
   tiles.parts = c.parts;
   st = launch_tiles<PASS, Mid, DT>(a, tiles, c.whole + c.dealt * c.parts, s);
   if (st != DP_OK || c.dealt == 0) return st;
-  gated_join_kernel<DT><<<dim3((unsigned)c.dealt * 8), 256, 0, s>>>(a.partial, a.dx, a.rows, a.d, tiles);
+  gated_join_kernel<PASS, DT><<<dim3((unsigned)c.dealt * (PASS == kForward ? 4 : 8)), 256, 0, s>>>(a, tiles);
   return hip_status(hipGetLastError());
 }
 
 }  // namespace
 
-size_t gated_input_workspace(int rows, int d, int f, int d_out) {
-  const Choice c = choose(kInput, rows, d, f, d_out);
-  return (size_t)c.parts * c.dealt * (kJoinSide * kJoinSide) * sizeof(float);
+size_t gated_tiles_workspace(GatedPass pass, int rows, int d, int f, int d_out) {
+  const Choice c = choose(pass, rows, d, f, d_out);
+  return c.few ? 0 : (size_t)c.parts * c.dealt * (kJoinSide * kJoinSide) * sizeof(float);
 }
 
 dp_status launch_gated_tiles(const GatedArgs& a, dp_dtype dt, GatedPass pass, hipStream_t s) {

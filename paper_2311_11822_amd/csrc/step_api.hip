@@ -93,6 +93,15 @@ dp_status gated_shape(dp_dtype dt, int rows, int d, int f, int d_out) {
   if (((int64_t)rows + 63) / 64 * ((std::max(d, f) + 63) / 64) > INT32_MAX || (int64_t)rows * f / 256 > INT32_MAX) return DP_ERR_UNSUPPORTED;
   return DP_OK;
 }
+// Both passes use the same memory, one after the other.
+size_t gated_backward_workspace(dp_dtype dt, int rows, int d, int f, int d_out, bool input) {
+  return std::max(d_out ? gated_workspace(dt, kHidden, rows, d, f, d_out) : 0, input ? gated_workspace(dt, kInput, rows, d, f, d_out) : 0);
+}
+dp_status scratch_ok(const void* ws, size_t ws_bytes, size_t need) {
+  if (need == 0) return DP_OK;
+  if (!ws || ws_bytes < need) return DP_ERR_WORKSPACE;
+  return aligned(ws, 16) ? DP_OK : DP_ERR_INVALID_ARG;
+}
 bool act_ok(dp_activation act) { return act >= DP_ACT_SILU && act <= DP_ACT_SIGMOID; }
 
 // Matrices of a step, as far as their sizes go.
@@ -244,14 +253,21 @@ dp_status dp_head_norm_backward(const dp_heads_shape* shape, dp_dtype dt, const 
   return launch_heads(a, dt, kNormGrad, static_cast<hipStream_t>(stream));
 }
 
+size_t dp_gated_workspace_bytes(dp_dtype dt, int rows, int d, int f) {
+  return gated_shape(dt, rows, d, f, d) == DP_OK ? gated_workspace(dt, kForward, rows, d, f, d) : 0;
+}
+
 dp_status dp_gated(const void* x, dp_dtype dt, int rows, int d, int f, const void* w_gate, const void* w_up, const void* b_gate,
-                   const void* b_up, dp_activation act, void* gate, void* up, void* h, void* stream) {
+                   const void* b_up, dp_activation act, void* gate, void* up, void* h, void* ws, size_t ws_bytes, void* stream) {
   const dp_status st = gated_shape(dt, rows, d, f, d);
   if (st != DP_OK) return st;
   if (!act_ok(act) || !there(x, dt) || !there(w_gate, dt) || !there(w_up, dt) || !there(h, dt) || !gate != !up) return DP_ERR_INVALID_ARG;
   for (const void* p : {b_gate, b_up, (const void*)gate, (const void*)up})
     if (!aligned(p, alignment(dt))) return DP_ERR_INVALID_ARG;
+  const dp_status scratch = scratch_ok(ws, ws_bytes, gated_workspace(dt, kForward, rows, d, f, d));
+  if (scratch != DP_OK) return scratch;
   GatedArgs a = {};
+  a.partial = static_cast<float*>(ws);
   a.x = x;
   a.w_gate = w_gate;
   a.w_up = w_up;
@@ -268,8 +284,8 @@ dp_status dp_gated(const void* x, dp_dtype dt, int rows, int d, int f, const voi
 }
 
 size_t dp_gated_backward_workspace_bytes(dp_dtype dt, int rows, int d, int f, int d_out) {
-  if (dt == DP_F32 || gated_shape(dt, rows, d, f, d_out) != DP_OK) return 0;
-  return gated_input_workspace(rows, d, f, d_out);
+  if (gated_shape(dt, rows, d, f, d_out == 0 ? d : d_out) != DP_OK) return 0;
+  return gated_backward_workspace(dt, rows, d, f, d_out, true);
 }
 
 dp_status dp_gated_backward(const void* dy, const void* w_down, int d_out, const void* gate, const void* up, dp_dtype dt, int rows, int d,
@@ -281,11 +297,8 @@ dp_status dp_gated_backward(const void* dy, const void* w_down, int d_out, const
   for (const void* p : {dy, gate, up, (const void*)dgate, (const void*)dup})
     if (!there(p, dt)) return DP_ERR_INVALID_ARG;
   if (dx && (!there(w_gate, dt) || !there(w_up, dt))) return DP_ERR_INVALID_ARG;
-  const size_t need = dx && dt != DP_F32 ? gated_input_workspace(rows, d, f, w_down ? d_out : d) : 0;
-  if (need) {
-    if (!ws || ws_bytes < need) return DP_ERR_WORKSPACE;
-    if (!aligned(ws, 16)) return DP_ERR_INVALID_ARG;
-  }
+  const dp_status scratch = scratch_ok(ws, ws_bytes, gated_backward_workspace(dt, rows, d, f, w_down ? d_out : 0, dx != nullptr));
+  if (scratch != DP_OK) return scratch;
   GatedArgs a = {};
   a.dy = dy;
   a.w_down = w_down;

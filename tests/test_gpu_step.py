@@ -267,8 +267,10 @@ GATED = [  # rows, d, f, d_out
     (4, 2056, 1000, 24), (31, 16, 4104, 16), (700, 1032, 264, 512),
     (2100, 72, 4104, 40), (2100, 4104, 136, 48), (1800, 520, 2600, 136),
     # whole rounds of large tiles and some more: forward, hidden and input
-    (4400, 328, 2184, 16), (4400, 40, 4360, 776), (4400, 4360, 520, 24)]
-GATED_F32 = GATED + [(1, 1, 1, 1), (5, 3, 7, 2), (111, 60, 161, 61), (130, 257, 65, 33), (64, 17, 129, 130)]
+    (4400, 328, 2184, 16), (4400, 40, 4360, 776), (4400, 4360, 520, 24),
+    # long contractions of few tiles
+    (200, 4104, 40, 3080), (1000, 7416, 216, 7416), (70, 520, 72, 4104), (40, 5000, 72, 5000), (2300, 2056, 776, 2056)]
+GATED_F32 = GATED + [(5, 1027, 33, 517), (300, 2001, 65, 1999), (1, 1, 1, 1), (5, 3, 7, 2), (111, 60, 161, 61), (130, 257, 65, 33), (64, 17, 129, 130)]
 GATED_CASES = [(d, *s) for d in DTYPES for s in (GATED_F32 if d == "f32" else [(r, 8 * -(-a // 8), b, 8 * -(-c // 8)) for r, a, b, c in GATED])]
 
 
@@ -450,8 +452,8 @@ def test_muon_other_polynomials(block):
 # ------------------------------------------------------------------------------------------------ as programs call them
 
 class Step:
-    """Every call of this file once, with the tensors that a program keeps: rotation, head norms, gated layers of many and of few rows, whose input
-    gradients' contraction is dealt to several workgroups or not, and updates of matrices of both kinds."""
+    """Every call of this file once, with the tensors that a program keeps: rotation, head norms, gated layers of many and of few rows, whose
+    contractions are dealt to several workgroups or not, and updates of matrices of both kinds."""
 
     def __init__(self, block, seed, T=150):
         self.gen = torch.Generator(device="cuda").manual_seed(seed)
@@ -466,19 +468,21 @@ class Step:
         turn = block.Rotary(self.q, self.k, self.q, self.k, **kw)
         self.w = [new(d, f), new(d, f), new(f, d)]
         gated = block.GatedFeedForward(*self.w, activation="gelu")
-        rows = [(new(n, d), [new(n, f) for _ in range(5)], new(n, d)) for n in (7, 90, 600)]
+        self.w += [new(2056, 40), new(2056, 40), new(40, 2056), *(new(*s, dt=torch.float32) for s in ((520, 96), (520, 96), (96, 520)))]
+        layers = [gated] * 3 + [block.GatedFeedForward(*self.w[3:6]), block.GatedFeedForward(*self.w[6:])]
+        rows = [(new(n, o.d, dt=o.dtype), [new(n, o.f, dt=o.dtype) for _ in range(5)], new(n, o.d, dt=o.dtype)) for o, n in zip(layers, (7, 90, 600, 90, 20))]
         self.p, self.g, self.m = ([torch.empty(s, device="cuda") for s in ((40, 24), (200, 136), (96, 300), (8, 8))] for _ in range(3))
         muon = block.Muon(self.p, self.g, self.m, 0.1)
-        self.objects, self.inputs = (norm, gated, muon), [self.x, self.dq, self.dk, *self.w, *[r[0] for r in rows], *self.g]
+        self.objects, self.inputs = (norm, gated, muon, *layers[3:]), [self.x, self.dq, self.dk, *self.w, *[r[0] for r in rows], *self.g]
         self.outputs = [self.q, self.k, self.kept, self.sq, *[t for r in rows for t in (*r[1], r[2])], *self.p, *self.m]
 
         def run():
             norm.forward(*views(self.x), self.q, self.k)
             turn.forward(self.q, self.k, self.q, self.k)
             norm.backward(*views(self.x), self.dq, self.dk, *views(self.dx), self.kept, self.sq)
-            for x, (gate, up, h, dgate, dup), dx in rows:
-                gated.forward(x, h, gate, up)
-                gated.backward(x, gate, up, dgate, dup, dx)
+            for layer, (x, (gate, up, h, dgate, dup), dx) in zip(layers, rows):
+                layer.forward(x, h, gate, up)
+                layer.backward(x, gate, up, dgate, dup, dx)
             muon.step(0.01)
         self.run = run
 
@@ -537,7 +541,7 @@ def test_steps_on_streams_at_once(block):
         steps[0].run()
     spans = sorted(captured + [(t.data_ptr(), t.data_ptr() + t.numel()) for t in used])
     torch.cuda.synchronize()
-    assert len(captured) >= 3 and all(a[1] <= b[0] for a, b in zip(spans, spans[1:]) if a != b)
+    assert len(captured) >= 8 and all(a[1] <= b[0] for a, b in zip(spans, spans[1:]) if a != b)
     for _ in range(6):
         for s in steps:
             for t, before in zip((*s.p, *s.m), s.state):

@@ -142,7 +142,8 @@ def test_heads_objects_refuse():
 
 # ------------------------------------------------------------------------------------------------ gated feed-forward layers
 
-GATED = dict(x=FAKE, dt=dp.DP_BF16, rows=4, d=16, f=24, w_gate=FAKE, w_up=FAKE, b_gate=None, b_up=None, act=0, gate=None, up=None, h=FAKE, stream=None)
+GATED = dict(x=FAKE, dt=dp.DP_BF16, rows=4, d=16, f=24, w_gate=FAKE, w_up=FAKE, b_gate=None, b_up=None, act=0, gate=None, up=None, h=FAKE, ws=None,
+             ws_bytes=0, stream=None)
 
 
 @pytest.mark.parametrize("change,status", [
@@ -167,13 +168,24 @@ def test_gated_backward_refuses(change, status):
 
 
 def test_gated_workspaces():
-    size = dp.dp_gated_backward_workspace_bytes
-    assert size(7, 4, 16, 24, 16) == 0 == size(dp.DP_BF16, 0, 16, 24, 16)
+    for size, args in ((dp.dp_gated_workspace_bytes, (4, 16, 24)), (dp.dp_gated_backward_workspace_bytes, (4, 16, 24, 16))):
+        assert size(7, *args) == 0 == size(dp.DP_BF16, 0, *args[1:])
+    # sums of both passes of backward fit; without w_down there is one
+    both, one = (dp.dp_gated_backward_workspace_bytes(dp.DP_BF16, 1000, 64, 216, k) for k in (7416, 0))
+    assert both > one
     # where a workspace is used it is asked for
-    for rows, d, f in ((1, 1280, 3456), (1, 16, 1 << 20), (1, 1 << 20, 16), (64, 768, 2048), (4096, 1280, 3456)):
-        n = dp.dp_gated_backward_workspace_bytes(dp.DP_F16, rows, d, f, d)
+    # where a workspace is used it is asked for
+    for dt, rows, d, f in [(dt, *sizes) for dt in (dp.DP_F32, dp.DP_BF16) for sizes in
+                           ((1, 1280, 3456), (1, 16, 1 << 20), (1, 1 << 20, 16), (64, 768, 2048), (1000, 7416, 216), (4096, 1280, 3456))]:
+        n = dp.dp_gated_workspace_bytes(dt, rows, d, f)
+        assert n > 0 or (rows, d, f) != (1000, 7416, 216)
         if n:
-            args = dict(GATED_BACK, rows=rows, d=d, f=f, d_out=d)
+            args = dict(GATED, dt=dt, rows=rows, d=d, f=f)
+            assert dp.lib.dp_gated(*changed(args, ws=FAKE, ws_bytes=n - 1)) == WS == dp.lib.dp_gated(*changed(args))
+            assert dp.lib.dp_gated(*changed(args, ws=FAKE + 4, ws_bytes=n)) == INV
+        n = dp.dp_gated_backward_workspace_bytes(dt, rows, d, f, d)
+        if n:
+            args = dict(GATED_BACK, dt=dt, rows=rows, d=d, f=f, d_out=d)
             assert dp.lib.dp_gated_backward(*changed(args, ws=FAKE, ws_bytes=n - 1)) == WS == dp.lib.dp_gated_backward(*changed(args))
             assert dp.lib.dp_gated_backward(*changed(args, ws=FAKE + 4, ws_bytes=n)) == INV
 
