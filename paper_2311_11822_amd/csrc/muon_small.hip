@@ -10,7 +10,7 @@ namespace dpbk {
 
 namespace {
 
-constexpr int kThreads = 512, kWaves = kThreads / 64, kLds = 160 * 1024 - 64;
+constexpr int kThreads = 512, kWaves = kThreads / 64, kPartBytes = kWaves * 1024, kLds = 160 * 1024 - 64 - kPartBytes;
 
 struct SmallGroup {
   int n, iterations, grad_dt, copy_dt;
@@ -23,6 +23,9 @@ __host__ __device__ inline int sixteens(int n) { return (n + 15) & ~15; }
 // Floats from one row to the next: 16-byte reads of sixteen rows fall on different banks.
 __host__ __device__ inline int pitch_of(int n) { return sixteens(n) + 4; }
 __host__ __device__ inline int64_t small_floats(int m, int n) { return (int64_t)sixteens(m) * (pitch_of(n) + 2 * pitch_of(m)); }
+
+// Whether waves share the tiles of A (one or four of them): 8 x 1000 56 us without, 39 with; 16 x 16 8.1 and 8.7.
+__host__ __device__ inline bool is_long(int m, int n) { return m <= 32 && n > 240; }
 
 __device__ __forceinline__ float value(const void* base, int dt, int64_t at) {
   if (dt == DP_F32) return static_cast<const float*>(base)[at];
@@ -45,9 +48,11 @@ __device__ __forceinline__ f32x4 rows_product(const float* p, const float* q, in
   return acc;
 }
 
+// LONG: some matrix's A has few tiles of a long contraction, which several waves share.
+template <bool LONG>
 __global__ void __launch_bounds__(kThreads) muon_small_kernel(const SmallGroup g) {
   extern __shared__ __align__(16) float lds[];
-  __shared__ float red[kWaves];
+  __shared__ float red[kWaves], part[LONG ? kWaves : 1][256];
   const MuonTensor& t = g.t[blockIdx.x];
   const bool turned = t.rows > t.cols;
   const int m = turned ? t.cols : t.rows, n = turned ? t.rows : t.cols, mp = sixteens(m), np = sixteens(n), px = pitch_of(n), pa = pitch_of(m);
@@ -73,16 +78,32 @@ __global__ void __launch_bounds__(kThreads) muon_small_kernel(const SmallGroup g
   const float norm = sqrtf(sum) + g.eps;
   for (int i = tid; i < mp * px; i += kThreads) X[i] = norm == 0.f ? 0.f : X[i] / norm;
   __syncthreads();
-  const int tiles = mp / 16;
+  const int tiles = mp / 16, shares = LONG && is_long(m, n) ? kWaves / (tiles * tiles) : 1, tile = wave / shares, share = wave - tile * shares;
+  const int begin = share * (np / 16) / shares * 16, end = (share + 1) * (np / 16) / shares * 16;
   for (int it = 0; it < g.iterations; ++it) {
     const float a = g.abc[it][0], b = g.abc[it][1], c = g.abc[it][2];
-    for (int k = wave; k < tiles * tiles; k += kWaves) {
+    for (int k = tile; k < tiles * tiles; k += kWaves) {
       const int i0 = k / tiles * 16, j0 = (k - k / tiles * tiles) * 16;
-      const f32x4 acc = rows_product(X, X, px, px, i0, j0, np, lane);
+      const f32x4 acc = rows_product(X + begin, X + begin, px, px, i0, j0, end - begin, lane);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) A[(i0 + 4 * (lane >> 4) + r) * pa + j0 + (lane & 15)] = acc[r];
+      for (int r = 0; r < 4; ++r) {
+        const int i = 4 * (lane >> 4) + r, j = lane & 15;
+        if (shares > 1)
+          part[wave][i * 16 + j] = acc[r];
+        else
+          A[(i0 + i) * pa + j0 + j] = acc[r];
+      }
     }
     __syncthreads();
+    if (shares > 1) {
+      for (int e = tid; e < tiles * tiles * 256; e += kThreads) {
+        const int k = e >> 8, i0 = k / tiles * 16, j0 = (k - k / tiles * tiles) * 16;
+        float s = 0.f;
+        for (int w = 0; w < shares; ++w) s += part[k * shares + w][e & 255];
+        A[(i0 + (e >> 4 & 15)) * pa + j0 + (e & 15)] = s;
+      }
+      __syncthreads();
+    }
     for (int k = wave; k < tiles * tiles; k += kWaves) {
       const int i0 = k / tiles * 16, j0 = (k - k / tiles * tiles) * 16;
       const f32x4 acc = rows_product(A, A, pa, pa, i0, j0, mp, lane);          // A is symmetric
@@ -128,6 +149,15 @@ __global__ void __launch_bounds__(kThreads) muon_small_kernel(const SmallGroup g
   }
 }
 
+template <bool LONG>
+dp_status launch(const SmallGroup& g, int64_t floats, hipStream_t s) {
+  static ReadyTable ready;
+  const dp_status st = allow_big_lds(muon_small_kernel<LONG>, kLds, ready);
+  if (st != DP_OK) return st;
+  muon_small_kernel<LONG><<<dim3((unsigned)g.n), kThreads, (size_t)floats * 4, s>>>(g);
+  return hip_status(hipGetLastError());
+}
+
 }  // namespace
 
 // One compute unit's fp32 matrix instructions take some 2 us to 2^20 multiply-adds of an iteration.
@@ -137,9 +167,6 @@ bool muon_is_small(int rows, int cols) {
 }
 
 dp_status launch_muon_small(const MuonTensor* tensors, int n, const MuonArgs& a, dp_dtype grad_dt, dp_dtype copy_dt, hipStream_t s) {
-  static ReadyTable ready;
-  const dp_status st = allow_big_lds(muon_small_kernel, kLds, ready);
-  if (st != DP_OK) return st;
   SmallGroup g = {};
   g.n = n;
   g.iterations = a.iterations;
@@ -152,12 +179,14 @@ dp_status launch_muon_small(const MuonTensor* tensors, int n, const MuonArgs& a,
   for (int k = 0; k < a.iterations; ++k)
     for (int i = 0; i < 3; ++i) g.abc[k][i] = (float)a.coefficients[3 * k + i];
   int64_t floats = 0;
+  bool any_long = false;
   for (int i = 0; i < n; ++i) {
     g.t[i] = tensors[i];
-    floats = std::max(floats, small_floats(std::min(tensors[i].rows, tensors[i].cols), std::max(tensors[i].rows, tensors[i].cols)));
+    const int rows = std::min(tensors[i].rows, tensors[i].cols), cols = std::max(tensors[i].rows, tensors[i].cols);
+    floats = std::max(floats, small_floats(rows, cols));
+    any_long = any_long || is_long(rows, cols);
   }
-  muon_small_kernel<<<dim3((unsigned)n), kThreads, (size_t)floats * 4, s>>>(g);
-  return hip_status(hipGetLastError());
+  return any_long ? launch<true>(g, floats, s) : launch<false>(g, floats, s);
 }
 
 }  // namespace dpbk
