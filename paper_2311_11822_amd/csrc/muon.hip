@@ -5,10 +5,13 @@
 //
 // Products as exact as fp32's at the rate of 16-bit ones: a value v is kept as two fp16 numbers, h = fp16(2^12 v) and l = fp16(2^12 v - h),
 // together within 2^-23 of v (2^-37 of 1 where v is next to nothing), and h h' + h l' + l h' is added up in fp32; l l', 2^-24 of it, is left
-// out.  A row is blocks of 32 columns, 32 h and 32 l, a line each (product.h).  2^12 keeps the halves of entries from 2^-15 up out of fp16's subnormal range; entries are bounded by singular
-// values, which the host has followed through the polynomials.  (fp32 matrix instructions have 1/16 of the 16-bit rate, a third of it 1/3.)
+// out.  A row is lines of 32 columns' h and l (product.h).  2^12 keeps the halves of entries from 2^-15 up out of fp16's subnormal range;
+// entries are bounded by singular values, which the host has followed through the polynomials.  (fp32 matrix instructions have 1/16 of the 16-bit
+// ones' rate, three products for one have 1/3.)
 // A, the square and the polynomial of A are symmetric: tiles on and above the diagonal are formed, and leave turned as well.
-// Matrices travel together: a launch does one step of up to 64 of them.
+// Matrices travel together: a launch does one step of up to 64 of them.  60 matrices of 768 x 768 to 768 x 2304 (85 M elements), us: momentum 190,
+// start 250, five times A 205, polynomial 127 and update 363, parameters 270; the elementwise passes move 3.2 GB, 650 us of a copy, the products are
+// 468 us an iteration at the rate of a large library product.
 #include <math.h>
 
 #include <algorithm>
@@ -41,6 +44,7 @@ struct Group {
   float beta, ahead, grad_scale, eps;
   float a, b, c;
   int from;                                          // x[from] is X, x[1 - from] what comes of it
+  float* sums;                                       // of A's tiles whose contraction is dealt to several workgroups
   Matrix t[kMuonGroup];
 };
 
@@ -177,12 +181,34 @@ __global__ void __launch_bounds__(kThreads) muon_apply_kernel(const Group g) {
 
 enum MuonStep { kGram, kPoly, kUpdate };
 
-// Tiles of one step.  Symmetric results: tile row by tile row from the diagonal on.
-template <int STEP, class S>
-__global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) muon_product_kernel(const Group g, int total) {
+// Eight values of a row as halves; col is a multiple of 8.
+__device__ __forceinline__ void put_halves(_Float16* out, int pitch, int row, int col, const float (&v)[8]) {
+  f16x8 h, l;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const Halves w(v[k]);
+    h[k] = w.h;
+    l[k] = w.l;
+  }
+  f16x8* const to = reinterpret_cast<f16x8*>(out + half_at(row, col, pitch));
+  to[0] = h;
+  to[4] = l;
+}
+
+// Where a symmetric result's tile lies: tile row by tile row from the diagonal on.
+__device__ __forceinline__ void place_above(int tiles_m, int rest, int& tm, int& tn) {
+  for (tm = 0; rest >= tiles_m - tm; ++tm) rest -= tiles_m - tm;
+  tn = tm + rest;
+}
+
+constexpr int kDealtSide = 128;                      // of tiles that are dealt in parts
+
+// Tiles of one step.  DEALT: each has `parts` workgroups, whose sums go to memory: [part][tile][row][column].
+template <int STEP, class S, bool DEALT>
+__global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) muon_product_kernel(const Group g, int total, int parts) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds_raw[];
   const unsigned lds0 = (unsigned)(uintptr_t)lds_raw;
-  const int logical = grad_logical_tile(blockIdx.x, total);
+  const int id = grad_logical_tile(blockIdx.x, DEALT ? total * parts : total), part = DEALT ? id / total : 0, logical = id - part * total;
   const Matrix& t = g.t[owner(g, logical)];
   const int m = imin(t.rows, t.cols), mp = blocks_of(m), np = blocks_of(imax(t.rows, t.cols));
   const int tiles_m = (m + S::BM - 1) / S::BM;
@@ -190,8 +216,7 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) muon_product_ker
   if constexpr (STEP == kUpdate) {
     grad_tile_of(tiles_m, (np + S::BN - 1) / S::BN, rest, tm, tn);
   } else {
-    for (tm = 0; rest >= tiles_m - tm; ++tm) rest -= tiles_m - tm;
-    tn = tm + rest;
+    place_above(tiles_m, rest, tm, tn);
   }
   const int m0 = tm * S::BM, n = tn * S::BN, n0[2] = {n, n};
   const _Float16 *a, *b;
@@ -214,23 +239,25 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) muon_product_ker
     p.K = p.lda = 2 * mp;
   }
   p.stages = p.K / kProductTerms;
+  if constexpr (DEALT) {
+    p.first = part * p.stages / parts;
+    p.stages = (part + 1) * p.stages / parts - p.first;
+  }
   p.s[0] = p.s[1] = {a, b, b};
   f32x4 acc[S::TM][S::TN];
   product_tile<S, true>(p, m0, n0, lds0, acc);
   _Float16* const out = STEP == kGram ? t.gram : STEP == kPoly ? t.poly : t.x[1 - g.from];
   const int pitch = STEP == kUpdate ? np : mp;
-  auto put = [&](int row, int col, const float (&v)[8]) {
-    f16x8 h, l;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const Halves w(v[k]);
-      h[k] = w.h;
-      l[k] = w.l;
-    }
-    f16x8* const to = reinterpret_cast<f16x8*>(out + half_at(row, col, pitch));
-    to[0] = h;
-    to[4] = l;
-  };
+  if constexpr (DEALT) {
+    float* const sums = g.sums + ((int64_t)part * total + logical) * (S::BM * S::BN);
+    NothingAhead<S, false> ahead(NoLoad{});
+    product_rows<S, false>(acc, lds0, ahead, [&](int row, int col, int, const float (&acc8)[2][8], Nothing) {
+      f32x4* const to = reinterpret_cast<f32x4*>(sums + row * S::BN + col);
+      to[0] = f32x4{acc8[0][0], acc8[0][1], acc8[0][2], acc8[0][3]};
+      to[1] = f32x4{acc8[0][4], acc8[0][5], acc8[0][6], acc8[0][7]};
+    });
+    return;
+  }
   // what is stored of eight values of the product
   auto finish = [&](int row, int col, const float (&acc8)[8], float (&v)[8]) {
     if constexpr (STEP == kPoly) {
@@ -249,7 +276,7 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) muon_product_ker
     if (r >= m || c >= pitch) return;
     float v[8];
     finish(r, c, acc8[0], v);
-    put(r, c, v);
+    put_halves(out, pitch, r, c, v);
   };
   if constexpr (STEP == kUpdate) {
     NothingAhead<S, false> ahead(NoLoad{});
@@ -261,10 +288,49 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) muon_product_ker
       if (r >= m || c >= mp) return;
       float v[8];
       finish(r, c, acc8, v);
-      put(r, c, v);
+      put_halves(out, pitch, r, c, v);
     };
     NothingAhead<S, false> ahead(NoLoad{});
     product_rows<S, false>(acc, lds0, ahead, store, tm != tn, across);
+  }
+}
+
+// The parts' sums of A's tiles, in their order: four workgroups to a tile, a square of 64 x 64 each.
+__global__ void __launch_bounds__(kThreads) muon_join_kernel(const Group g, int total, int parts) {
+  __shared__ float square[kSide][kSide + 1];
+  const int logical = blockIdx.x / 4, quarter = blockIdx.x % 4;
+  const Matrix& t = g.t[owner(g, logical)];
+  const int m = imin(t.rows, t.cols), pitch = blocks_of(m);
+  int tm, tn;
+  place_above((m + kDealtSide - 1) / kDealtSide, logical - (int)t.begin, tm, tn);
+  const int r0 = (quarter >> 1) * kSide, c0 = (quarter & 1) * kSide;
+  const float* const from = g.sums + (int64_t)logical * (kDealtSide * kDealtSide);
+#pragma unroll
+  for (int i = 0; i < kSide * kSide / 8 / kThreads; ++i) {
+    const int piece = threadIdx.x + i * kThreads, row = piece / 8, col = piece % 8 * 8;
+    float v[8] = {};
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p) {
+      const f32x4* const at = reinterpret_cast<const f32x4*>(from + (int64_t)p * total * (kDealtSide * kDealtSide) + (r0 + row) * kDealtSide + c0 + col);
+      const f32x4 x = at[0], y = at[1];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] += x[k], v[4 + k] += y[k];
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) square[row][col + k] = v[k] *= 1.f / kScale;
+    const int r = tm * kDealtSide + r0 + row, c = tn * kDealtSide + c0 + col;
+    if (r < m && c < pitch) put_halves(t.gram, pitch, r, c, v);
+  }
+  if (tm == tn) return;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kSide * kSide / 8 / kThreads; ++i) {         // below the diagonal
+    const int piece = threadIdx.x + i * kThreads, row = piece / 8, col = piece % 8 * 8;
+    const int r = tn * kDealtSide + c0 + row, c = tm * kDealtSide + r0 + col;
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = square[col + k][row];
+    if (r < m && c < pitch) put_halves(t.gram, pitch, r, c, v);
   }
 }
 
@@ -278,44 +344,74 @@ unsigned lay_out(Group& g, F workgroups) {
   return total;
 }
 
-template <int STEP, int SIDE>
-int64_t tiles_of(const Matrix& t) {
+template <int STEP, int SIDE, class T>
+int64_t tiles_of(const T& t) {
   const int64_t m = std::min(t.rows, t.cols), n = blocks_of(std::max(t.rows, t.cols)), tm = (m + SIDE - 1) / SIDE;
   return STEP == kUpdate ? tm * ((n + SIDE - 1) / SIDE) : tm * (tm + 1) / 2;
 }
 
-template <int STEP, class S>
-dp_status launch_product(Group& g, hipStream_t s) {
+// Large tiles or small ones, and of how many workgroups each.  256 large ones are resident, 2.2 us to a stage of 32 terms; 512 small ones, 1.2 us, or
+// 256 at 0.6; and what comes before and after a contraction.  Workgroups are dealt out in order, the longest first: a launch takes their sum over
+// those that are resident, and some of the longest besides.  A of few matrices, whose rows are long, has few tiles: their contraction is dealt to
+// `parts` workgroups, for one more launch and the sums' way through memory.  A step of one matrix, its contractions whole and in parts, us:
+// 768 x 2304 507, 352; 1280 x 3456 812, 615; 300 x 5000 672, 288; 8 x 4096 463, 158; 128 x 32768 3175, 299.
+struct StepChoice {
+  bool large;
+  int parts;
+  int64_t tiles;
+};
+template <int STEP, class T>
+StepChoice choose_step(const T* t, int n) {
+  constexpr float kBigStage = 2.2f, kBigRest = STEP == kUpdate ? 12.f : 30.f, kMidStage = 1.2f, kMidRest = STEP == kUpdate ? 10.f : 18.f;
+  int64_t big = 0, mid = 0, big_stages = 0, mid_stages = 0, longest = 0, shortest = INT64_MAX;
+  for (int i = 0; i < n; ++i) {
+    const int64_t stages = ((STEP == kGram ? std::max(t[i].rows, t[i].cols) : std::min(t[i].rows, t[i].cols)) + kHalfTerms - 1) / kHalfTerms;
+    big += tiles_of<STEP, 256>(t[i]);
+    mid += tiles_of<STEP, 128>(t[i]);
+    big_stages += stages * tiles_of<STEP, 256>(t[i]);
+    mid_stages += stages * tiles_of<STEP, 128>(t[i]);
+    longest = std::max(longest, stages);
+    shortest = std::min(shortest, stages);
+  }
+  auto cost = [&](int64_t tiles, int64_t tile_stages, float stage, float rest, float resident) {
+    const float one = (float)longest * stage + rest;
+    return (float)tiles <= resident ? one : ((float)tile_stages * stage + (float)tiles * rest) / resident + one / 2;
+  };
+  const float large = cost(big, big_stages, kBigStage, kBigRest, 256.f), small = mid <= 256 ? 0.6f * (float)longest + 7.f : cost(mid, mid_stages, kMidStage, kMidRest, 512.f);
+  StepChoice c = {large <= small, 1, mid};
+  if constexpr (STEP == kGram) {
+    float best = std::min(large, small);
+    for (const int parts : {2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+      const int64_t pieces = mid * parts;
+      if (pieces > 512 || 4 * parts > shortest) break;
+      const float dealt = (pieces <= 256 ? 0.6f : 1.2f) * (float)longest / parts + 13.f + 0.02f * (float)pieces;
+      if (dealt >= best) continue;
+      best = dealt;
+      c.large = false;
+      c.parts = parts;
+    }
+  }
+  return c;
+}
+
+template <int STEP, class S, bool DEALT = false>
+dp_status launch_product(Group& g, int parts, hipStream_t s) {
   static ReadyTable ready;
-  const dp_status st = allow_big_lds(muon_product_kernel<STEP, S>, S::LDS_BYTES, ready);
+  const dp_status st = allow_big_lds(muon_product_kernel<STEP, S, DEALT>, S::LDS_BYTES, ready);
   if (st != DP_OK) return st;
   const unsigned total = lay_out(g, [](const Matrix& t) { return tiles_of<STEP, S::BM>(t); });
-  muon_product_kernel<STEP, S><<<dim3(total), S::NT, S::LDS_BYTES, s>>>(g, (int)total);
+  muon_product_kernel<STEP, S, DEALT><<<dim3(total * parts), S::NT, S::LDS_BYTES, s>>>(g, (int)total, parts);
+  if constexpr (DEALT) muon_join_kernel<<<dim3(total * 4), kThreads, 0, s>>>(g, (int)total, parts);
   return hip_status(hipGetLastError());
 }
 
-// Large tiles or small ones: 256 of the former are resident, 1.5 us to a stage of 64 terms, 512 of the latter, 0.85 us; what comes before and after a
-// contraction is the same again for some stages.  Workgroups are dealt out in order, the longest first: a launch takes their sum over those that
-// are resident, and some of the longest besides.
 template <int STEP>
 dp_status launch_step(Group& g, hipStream_t s) {
   constexpr ProductB B = STEP == kUpdate ? kSplitColumns : kRowsOfTerms;
-  auto cost = [&](auto tiles, float stage, float rest, float resident) {
-    float sum = 0.f, longest = 0.f;
-    int64_t n = 0;
-    for (int i = 0; i < g.n; ++i) {
-      const Matrix& t = g.t[i];
-      const int k = STEP == kGram ? std::max(t.rows, t.cols) : std::min(t.rows, t.cols);
-      const float one = (float)((k + 31) / 32) * stage + rest;
-      sum += (float)tiles(t) * one;
-      longest = std::max(longest, one);
-      n += tiles(t);
-    }
-    return (float)n <= resident ? longest : sum / resident + longest / 2;
-  };
-  const float big = cost(tiles_of<STEP, 256>, 2.2f, STEP == kUpdate ? 12.f : 30.f, 256.f);
-  const float mid = cost(tiles_of<STEP, 128>, 1.2f, STEP == kUpdate ? 10.f : 18.f, 512.f);
-  return big <= mid ? launch_product<STEP, BigProduct<B, true>>(g, s) : launch_product<STEP, MidProduct<B, true>>(g, s);
+  const StepChoice c = choose_step<STEP>(g.t, g.n);
+  if constexpr (STEP == kGram)
+    if (c.parts > 1) return launch_product<STEP, MidProduct<B, true>, true>(g, c.parts, s);
+  return c.large ? launch_product<STEP, BigProduct<B, true>>(g, 1, s) : launch_product<STEP, MidProduct<B, true>>(g, 1, s);
 }
 
 // Bytes of a matrix's two X, A, polynomial and partial sums.
@@ -335,7 +431,8 @@ size_t matrix_bytes(int rows, int cols, size_t (&at)[5]) {
 size_t muon_workspace(const MuonTensor* tensors, int n) {
   size_t total = 0, at[5];
   for (int i = 0; i < n; ++i) total += matrix_bytes(tensors[i].rows, tensors[i].cols, at);
-  return total;
+  const StepChoice c = choose_step<kGram>(tensors, n);
+  return total + (c.parts > 1 ? (size_t)c.parts * c.tiles * (kDealtSide * kDealtSide) * sizeof(float) : 0);
 }
 
 dp_status launch_muon(const MuonTensor* tensors, int n, const MuonArgs& a, dp_dtype grad_dt, dp_dtype copy_dt, void* ws, hipStream_t s) {
@@ -373,6 +470,7 @@ dp_status launch_muon(const MuonTensor* tensors, int n, const MuonArgs& a, dp_dt
     t.parts = (int)((size + part_values(size) - 1) / part_values(size));
     base += bytes;
   }
+  g.sums = reinterpret_cast<float*>(base);
   auto launch = [&](auto kernel, unsigned total) {
     kernel<<<dim3(total), kThreads, 0, s>>>(g);
     return hip_status(hipGetLastError());
