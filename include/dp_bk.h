@@ -650,8 +650,8 @@ dp_status dp_gated_backward(const void* dy, const void* w_down, int d_out, const
  *                elements need no more than their own alignment.  rows and cols are at most 2^20, the shorter at most 2^16.
  *   coefficients HOST fp64 [iterations, 3]: a, b, c of each iteration, 1 to 32 of them.  Singular values, which start in [0, 1], may not leave
  *                |x| <= 15 on the way, nor A's polynomial (DP_ERR_UNSUPPORTED).
- *   ws           device scratch, >= dp_muon_workspace_bytes(...), 16-byte aligned: some 8 bytes an element of up to 64 matrices at a time and 8 of
- *                each shorter side squared
+ *   ws           device scratch, >= dp_muon_workspace_bytes(...), 16-byte aligned: some 8 bytes an element of up to 64 matrices at a time, 8 of
+ *                each shorter side squared, and up to 32 MiB where they are few
  * What is written, workspace included, overlaps nothing else: no matrix is named twice.
  * Matrices go in runs of up to 64, each of them a few launches whatever the number of its matrices.
  */

@@ -302,7 +302,8 @@ dp_status launch_f32_tiles(const GatedArgs& a, const F32Choice& c, hipStream_t s
   st = hip_status(hipGetLastError());
   if constexpr (W == 2) {
     if (st != DP_OK || c.parts == 1) return st;
-    gated_f32_join_kernel<PASS, S::SIDE><<<dim3(tiles * (S::SIDE * S::SIDE / kThreads / (PASS == kForward ? 2 : 1))), kThreads, 0, s>>>(a, c.tiles_m, c.tiles_n, c.parts);
+    constexpr unsigned GROUPS = S::SIDE * S::SIDE / kThreads / (PASS == kForward ? 2 : 1);
+    gated_f32_join_kernel<PASS, S::SIDE><<<dim3(tiles * GROUPS), kThreads, 0, s>>>(a, c.tiles_m, c.tiles_n, c.parts);
     st = hip_status(hipGetLastError());
   }
   return st;

@@ -377,7 +377,8 @@ StepChoice choose_step(const T* t, int n) {
     const float one = (float)longest * stage + rest;
     return (float)tiles <= resident ? one : ((float)tile_stages * stage + (float)tiles * rest) / resident + one / 2;
   };
-  const float large = cost(big, big_stages, kBigStage, kBigRest, 256.f), small = mid <= 256 ? 0.6f * (float)longest + 7.f : cost(mid, mid_stages, kMidStage, kMidRest, 512.f);
+  const float large = cost(big, big_stages, kBigStage, kBigRest, 256.f);
+  const float small = mid <= 256 ? 0.6f * (float)longest + 7.f : cost(mid, mid_stages, kMidStage, kMidRest, 512.f);
   StepChoice c = {large <= small, 1, mid};
   if constexpr (STEP == kGram) {
     float best = std::min(large, small);
@@ -476,7 +477,10 @@ dp_status launch_muon(const MuonTensor* tensors, int n, const MuonArgs& a, dp_dt
     return hip_status(hipGetLastError());
   };
   unsigned total = lay_out(g, [](const Matrix& t) { return t.parts; });
-  dp_status st = launch(grad_dt == DP_F32 ? muon_momentum_kernel<DP_F32> : grad_dt == DP_BF16 ? muon_momentum_kernel<DP_BF16> : muon_momentum_kernel<DP_F16>, total);
+  dp_status st = launch(grad_dt == DP_F32    ? muon_momentum_kernel<DP_F32>
+                        : grad_dt == DP_BF16 ? muon_momentum_kernel<DP_BF16>
+                                             : muon_momentum_kernel<DP_F16>,
+                        total);
   if (st != DP_OK) return st;
   auto squares = [](const Matrix& t, bool padded) {
     const int64_t m = std::min(t.rows, t.cols), c = std::max(t.rows, t.cols);

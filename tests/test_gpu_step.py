@@ -391,7 +391,8 @@ def muon_tolerance(shape):
 
 
 MUON_SHAPES = [[(1, 1)], [(1, 40), (40, 1), (2, 3)], [(16, 16), (24, 72), (72, 24), (65, 24), (24, 65)], [(128, 128), (129, 127), (127, 300), (260, 140)],
-               [(520, 300), (256, 1030)], [(33, 2000)] * 3 + [(2000, 33)] * 2, [(96, 100), (100, 96), (90, 113), (16, 600), (1, 1900)], [(64, 256), (250, 61)] + [(130, 70)] * 3, [(8, 9 + i) for i in range(131)], [(1300, 1100)], [(700, 2600)] * 14,
+               [(520, 300), (256, 1030)], [(33, 2000)] * 3 + [(2000, 33)] * 2, [(96, 100), (100, 96), (90, 113), (16, 600), (1, 1900)], [(64, 256), (250, 61)] + [(130, 70)] * 3,
+               [(8, 9 + i) for i in range(131)], [(1300, 1100)], [(700, 2600)] * 14,
                [(40, 4100)], [(300, 2500), (2500, 300), (130, 1030)], [(8, 5000), (5000, 16)]]          # A's contraction in parts
 
 
