@@ -631,7 +631,7 @@ dp_status dp_gated(const void* x, dp_dtype dt, int rows, int d, int f, const voi
  *   dh = dy w_down' (or given),  dgate = dh up act'(gate),  dup = dh act(gate),  dx = dgate w_gate' + dup w_up'  (of dgate and dup as stored)
  *   dy        device, [rows, d_out] of type dt, with w_down device [f, d_out];  or, w_down NULL, dh itself, [rows, f] (d_out is not looked at)
  *   gate, up  dp_gated's;  dgate, dup  device, [rows, f] of type dt; they may be gate and up, or one of them dh
- *   dx        device, [rows, d] of type dt, or NULL: not wanted (then the weights may be NULL)
+ *   dx        device, [rows, d] of type dt, or NULL: not wanted (then the weights may be NULL); like dgate and dup otherwise it overlaps nothing
  *   ws        device scratch, >= dp_gated_backward_workspace_bytes(...), 16-byte aligned; not used where the size is 0.  The size is for calls with
  *             dx or without; d_out = 0: with no w_down
  */
