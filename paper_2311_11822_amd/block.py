@@ -265,7 +265,10 @@ class _Heads:
                                     three(q_out), three(k_out), turns, position, length)
         self._check((q, k), self.in_strides)
         self._check((q_out, k_out), self.out_strides)
-        if dp.dp_head_norm_workspace_bytes(self.shape, self.dt) == 0:
+        # results as gradients would be; what is read may be broadcast (and has no gradients in its own layout then)
+        written = dp.heads_shape(B, T, H, 0 if k is None else k.shape[2], D, rotary, interleaved, amplitude, three(q_out), three(k_out),
+                                 three(q_out), three(k_out), turns, position, length)
+        if dp.dp_head_norm_workspace_bytes(written, self.dt) == 0 or (self.dt != dp.DP_F32 and any(st % 8 for t in (q, k) for st in three(t))):
             raise ValueError("sizes or strides that heads do not have")
         if self.index < 0:
             raise ValueError(f"tensors on a GPU, not {q.device}")

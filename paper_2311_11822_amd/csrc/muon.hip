@@ -168,7 +168,8 @@ __global__ void __launch_bounds__(kThreads) muon_apply_kernel(const Group g) {
     const int k = wave + i * WAVES, row = (turned ? c0 : r0) + k;
     if (row < t.rows && col < t.cols) {
       const int64_t at = (int64_t)row * t.cols + col;
-      const float w = fmaf(t.keep, param[i], -t.rate * (turned ? tile[lane][k] : tile[k][lane]));
+      float w = fmaf(t.keep, param[i], -t.rate * (turned ? tile[lane][k] : tile[k][lane]));
+      asm("" : "+v"(w));                              // the copy is the parameter rounded, not the sum (v_fma_mixlo_f16)
       t.param[at] = w;
       if constexpr (DT != DP_F32) {
         Values<DT, 1> v;

@@ -142,7 +142,8 @@ __global__ void __launch_bounds__(kThreads) muon_small_kernel(const SmallGroup g
   }
   for (int i = tid; i < size; i += kThreads) {
     const int row = i / t.cols, col = i - row * t.cols;
-    const float w = fmaf(t.keep, t.param[i], -t.rate * X[turned ? col * px + row : row * px + col]);
+    float w = fmaf(t.keep, t.param[i], -t.rate * X[turned ? col * px + row : row * px + col]);
+    asm("" : "+v"(w));                                // the copy is the parameter rounded, not the sum
     t.param[i] = w;
     if (g.copy_dt == DP_BF16) static_cast<__bf16*>(t.copy)[i] = (__bf16)w;
     if (g.copy_dt == DP_F16) static_cast<_Float16*>(t.copy)[i] = (_Float16)w;

@@ -4,7 +4,8 @@ CPU, at the sizes, layouts, positions and lengths where they can go wrong.
 Tolerances, relative in the 2-norm unless said otherwise.  U is half a unit in the last place of the storage type, relative to the
 value: what one rounding may err by.
   stored results     one rounding: U, and what the fp32 arithmetic before it errs by
-  FP32               2e-6: some ten fp32 operations in a row (each 2^-24 = 6e-8 at most), or a sum of up to 1000 products in fp32 (sqrt(1000) 2^-24);
+  FP32               2e-6: some ten fp32 operations in a row (each 2^-24 = 6e-8 at most), or a sum of up to 1000 products in fp32 (sqrt(1000) 2^-24;
+                     longer ones are sums of such sums);
                      an angle, a fraction of a turn rounded to fp32, is within 2 pi 2^-26 = 9.4e-8
 """
 import math
@@ -589,6 +590,52 @@ def test_gated_rows_and_columns_do_not_meet(block):
         dh[rows - 1] = math.nan
         bad.backward(dh, r(rows, f), r(rows, f), dgate, dup, dx)
         assert torch.isfinite(dx[:rows - 1]).all() and torch.isnan(dx[rows - 1]).all()
+
+
+def test_muon_more_matrices_than_travel_together(block):
+    """Two launches of each step, fp16 copies of matrices of both kinds, gradients that two matrices share."""
+    gen = torch.Generator().manual_seed(12)
+    shapes = [(100, 110)] * 66 + [(20, 30)] * 2
+    param = [torch.randn(s, generator=gen).cuda() for s in shapes]
+    shared = {s: torch.randn(s, generator=gen).cuda() for s in set(shapes)}
+    copy, before = [torch.empty(s, dtype=torch.float16, device="cuda") for s in shapes], [p.cpu().double() for p in param]
+    block.Muon(param, [shared[s] for s in shapes], [torch.zeros(s, device="cuda") for s in shapes], 0.5, copy, 2.0).step(0.25, 0.5)
+    x = {s: orthogonal(1.5 * shared[s].cpu().double()) for s in set(shapes)}
+    for p, c, b in zip(param, copy, before):
+        want = b * (1 - 0.25 * 0.5) - 0.25 * 2.0 * x[p.shape]
+        assert (p.cpu().double() - want).norm() <= 0.5 * muon_tolerance(p.shape) * x[p.shape].norm() + FP32 * want.norm()
+        assert torch.equal(c, p.half())
+
+
+def test_gated_one_bias(block):
+    for dtype, rows in (("bf16", 3), ("f16", 90), ("f32", 5)):
+        gen = torch.Generator().manual_seed(rows)
+        x, wg, wu = rand(gen, (rows, 64), dtype), rand(gen, (64, 40), dtype, 0.125), rand(gen, (64, 40), dtype, 0.125)
+        bias = rand(gen, (40,), dtype)
+        for biases in ((bias, None), (None, bias)):
+            layer = block.GatedFeedForward(wg.cuda(), wu.cuda(), None, *(None if b is None else b.cuda() for b in biases))
+            gate, up, h = (torch.empty((rows, 40), dtype=x.dtype, device="cuda") for _ in range(3))
+            layer.forward(x.cuda(), h, gate, up)
+            for got, w, b in zip((gate, up), (wg, wu), biases):
+                same(got, x.double() @ w.double() + (0 if b is None else b.double()), FP32, dtype)
+
+
+def test_heads_read_what_is_broadcast(block):
+    """One head of keys for all of them, one row of queries for all samples; results of their own."""
+    gen = torch.Generator().manual_seed(2)
+    q, k = rand(gen, (1, 5, 4, 32), "bf16").cuda().expand(3, 5, 4, 32), rand(gen, (3, 5, 1, 32), "bf16").cuda().expand(3, 5, 4, 32)
+    turns = block.rotary_turns(32)
+    out = [torch.empty((3, 5, 4, 32), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    block.Rotary(q, k, *out, turns.cuda()).forward(q, k, *out)
+    for x, y in zip((q, k), out):
+        assert rel(y, turn(x.cpu().double(), turns, False, 1.0, torch.arange(5).repeat(3, 1))) <= U["bf16"] + FP32
+    norm = block.HeadNorm(q, k, *out, turns=turns.cuda())
+    norm.forward(q, k, *out)
+    for x, y in zip((q, k), out):
+        unit = x.cpu().double() * (x.cpu().double().square().mean(-1, keepdim=True) + 1e-6) ** -0.5
+        assert rel(y, turn(unit, turns, False, 1.0, torch.arange(5).repeat(3, 1))) <= U["bf16"] + 4 * FP32
+    with pytest.raises(block.dp.DpError):                # gradients in the layout of what is broadcast
+        norm.backward(q, k, *out, q, k)
 
 
 def test_far_offsets(block):
