@@ -355,7 +355,7 @@ int64_t tiles_of(const T& t) {
 // 256 at 0.6; and what comes before and after a contraction.  Workgroups are dealt out in order, the longest first: a launch takes their sum over
 // those that are resident, and some of the longest besides.  A of few matrices, whose rows are long, has few tiles: their contraction is dealt to
 // `parts` workgroups, for one more launch and the sums' way through memory.  A step of one matrix, its contractions whole and in parts, us:
-// 768 x 2304 507, 352; 1280 x 3456 812, 615; 300 x 5000 672, 288; 8 x 4096 463, 158; 128 x 32768 3175, 299.
+// 768 x 2304 507, 352; 1280 x 3456 812, 615; 300 x 5000 671, 271; 8 x 4096 459, 152; 128 x 32768 3160, 285; 768 x 50264 5880, 1820.
 struct StepChoice {
   bool large;
   int parts;
@@ -383,10 +383,10 @@ StepChoice choose_step(const T* t, int n) {
   StepChoice c = {large <= small, 1, mid};
   if constexpr (STEP == kGram) {
     float best = std::min(large, small);
-    for (const int parts : {2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+    for (const int parts : {2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128}) {
       const int64_t pieces = mid * parts;
       if (pieces > 512 || 4 * parts > shortest) break;
-      const float dealt = (pieces <= 256 ? 0.6f : 1.2f) * (float)longest / parts + 13.f + 0.02f * (float)pieces;
+      const float dealt = (pieces <= 256 ? 0.6f : 1.2f) * (float)longest / parts + 13.f + 0.02f * (float)pieces + 0.3f * (float)parts;
       if (dealt >= best) continue;
       best = dealt;
       c.large = false;
