@@ -84,7 +84,7 @@ struct Unit {
 
 // A workgroup has one side (queries or keys) of a run of tokens; its row groups take rows in turn, the next one's values on their way while
 // one is worked on.  Bound by memory: gradients of 32760 tokens of 16 + 4 heads of 128 (335 MB) 71 us; a norm's backward pass of 4 x 2048 tokens of
-// 96 + 96 heads of 128 (1.2 GB) 250 us, 4.8 TB/s.  (Both sides' heads of a token in one workgroup: 419 us there, rows of two widths left
+// 96 + 96 heads of 128 (1.2 GB) 248 us, 4.9 TB/s.  (Both sides' heads of a token in one workgroup: 419 us there, rows of two widths left
 // lanes idle.)
 template <int DT, int VEC, int KIND>
 __global__ void __launch_bounds__(kThreads) heads_kernel(const HeadsArgs a) {
@@ -251,24 +251,28 @@ __global__ void __launch_bounds__(kThreads) heads_kernel(const HeadsArgs a) {
   }
 }
 
-// A workgroup to a sample: its chunks' sums, by parts that are added in their order, and the square of all of them.  374 chunks of 2 x 128 columns
-// take 10 us (14 with sixteen loads of a thread on their way).
-constexpr int kJoinThreads = 1024;
+// A workgroup to a sample: its chunks' sums, VEC columns to a thread, by parts that are added in their order, and the square of all of them.
+// 94 chunks of 2 x 128 columns of each of four samples 5 us, 1024 of one sample 7 (one column to a thread 11).
+constexpr int kJoinThreads = 1024, kJoinParts = 32;
+template <int VEC>
 __global__ void __launch_bounds__(kJoinThreads) heads_join_kernel(const HeadsArgs a) {
-  __shared__ float part[kJoinThreads], square[kJoinThreads / 64];
-  const int b = blockIdx.x, sides = a.heads[1] ? 2 : 1, columns = sides * a.D;             // up to 512
-  const int parts = kJoinThreads / columns, p = threadIdx.x / columns, c = threadIdx.x - p * columns, w = c >= a.D;
+  __shared__ __align__(16) float part[kJoinThreads * VEC];
+  __shared__ float square[kJoinThreads / 64];
+  const int b = blockIdx.x, sides = a.heads[1] ? 2 : 1, columns = sides * a.D, units = columns / VEC;           // up to 512 columns
+  const int parts = min(kJoinThreads / units, kJoinParts), p = threadIdx.x / units, c = (threadIdx.x - p * units) * VEC, w = c >= a.D;
   const HeadsPlan plan = a.plan[w];
-  float s = 0.f;
+  typedef __attribute__((ext_vector_type(VEC))) float Columns;
+  Columns s = {};
   if (p < parts) {
     const float* from = a.partial + (w ? (int64_t)a.B * a.plan[0].chunks * a.D : 0) + (int64_t)b * plan.chunks * a.D + (c - w * a.D);
 #pragma unroll 8
-    for (int k = p; k < plan.chunks; k += parts) s += from[(int64_t)k * a.D];
+    for (int k = p; k < plan.chunks; k += parts) s += *reinterpret_cast<const Columns*>(from + (int64_t)k * a.D);
+    *reinterpret_cast<Columns*>(part + p * columns + c) = s;
   }
-  part[threadIdx.x] = s;
   __syncthreads();
   float v = 0.f;
   if (threadIdx.x < columns) {
+#pragma unroll 8
     for (int k = 0; k < parts; ++k) v += part[k * columns + threadIdx.x];
     a.kept[(int64_t)b * columns + threadIdx.x] = v;
   }
@@ -342,7 +346,13 @@ dp_status launch_heads(HeadsArgs a, dp_dtype dt, HeadsKind kind, hipStream_t s) 
   for (int w = 0; w < 2; ++w) {
     if (w == 1) a.begin = blocks;
     if (!a.heads[w]) continue;
-    a.plan[w] = plan_side(a, w, kind == kNormGrad ? kHeadsGradChunks : kHeadsChunks);
+    // A norm's backward pass: pieces of eight values leave registers for three workgroups to a compute unit: one round of those, but for a side of half as many
+    // heads as the other, whose small chunks fill in.  Each side up to 768 workgroups and both together, us: 16 x 256 tokens, 12 + 12 heads of 64 16.0, 14.3;
+    // 8 x 512, 20 + 20 19.5, 17.9; 1 x 4096, 16 + 4 of 128 17.6, 19.1; pieces of four, 7 x 991, 2 + 2 of 152 15.3, 16.4.
+    const int others = a.heads[1 - w];
+    const bool apart = vec < 8 || 2 * a.heads[w] <= others;
+    const int share = apart ? kHeadsGradChunks : (int)((int64_t)kHeadsGradChunks * a.heads[w] / (a.heads[w] + others)) + 1;
+    a.plan[w] = plan_side(a, w, kind == kNormGrad ? share : kHeadsChunks);
     blocks += (unsigned)(a.B * a.plan[w].chunks);
     tokens = std::max(tokens, a.plan[w].block_tokens);
   }
@@ -365,7 +375,10 @@ dp_status launch_heads(HeadsArgs a, dp_dtype dt, HeadsKind kind, hipStream_t s) 
   else return DP_ERR_UNSUPPORTED;
 #undef DP_LAUNCH
   if (st != DP_OK || kind != kNormGrad || !a.kept) return st;
-  heads_join_kernel<<<dim3(a.B), kJoinThreads, 0, s>>>(a);
+  if (a.D % 4 == 0)
+    heads_join_kernel<4><<<dim3(a.B), kJoinThreads, 0, s>>>(a);
+  else
+    heads_join_kernel<1><<<dim3(a.B), kJoinThreads, 0, s>>>(a);
   return hip_status(hipGetLastError());
 }
 
