@@ -74,8 +74,6 @@ struct Tiles {
   }
 };
 
-constexpr int kJoinSide = 128;       // of tiles that are dealt in parts
-
 template <int PASS, class S, int DT>
 __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) gated_tile_kernel(const GatedArgs a, const Tiles tiles) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds_raw[];
@@ -93,7 +91,7 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) gated_tile_kerne
   if constexpr (PASS == kInput) p.s[0] = {a.dgate, a.w_gate, nullptr};
   p.s[1] = PASS == kInput ? ProductSegment{a.dup, a.w_up, nullptr} : p.s[0];
   const int rest = tiles.count() - tiles.whole, id = grad_logical_tile(blockIdx.x, tiles.whole + rest * tiles.parts);
-  const bool dealt = S::BM == kJoinSide && id >= tiles.whole;
+  const bool dealt = id >= tiles.whole;
   const int part = dealt ? (id - tiles.whole) / rest : 0, tile = id - part * rest, shares = dealt ? tiles.parts : 1;
   int tm, tn;
   tiles.place(tile, tm, tn);
@@ -165,18 +163,20 @@ __global__ void __launch_bounds__(S::NT, 163840 / S::LDS_BYTES) gated_tile_kerne
 }
 
 // The parts' sums of the tiles from `whole` on, in their order, and what becomes of them: eight columns (of both sets) to a thread.
-template <int PASS, int DT>
+template <int PASS, int SIDE>
+constexpr int kJoinGroups = SIDE * SIDE / (PASS == kForward ? 2 : 1) / 2048;      // workgroups to a tile
+template <int PASS, int SIDE, int DT>
 __global__ void __launch_bounds__(256) gated_join_kernel(const GatedArgs a, const Tiles tiles) {
-  constexpr int SETS = PASS == kForward ? 2 : 1, WIDTH = kJoinSide / SETS, GROUPS = kJoinSide * WIDTH / 2048;
+  constexpr int SETS = PASS == kForward ? 2 : 1, WIDTH = SIDE / SETS, GROUPS = kJoinGroups<PASS, SIDE>;
   const int rest = tiles.count() - tiles.whole, t = blockIdx.x / GROUPS, at = (blockIdx.x % GROUPS * 256 + threadIdx.x) * 8;
   int tm, tn;
   tiles.place(tiles.whole + t, tm, tn);
-  const int N = PASS == kInput ? a.d : a.f, row = tm * kJoinSide + at / WIDTH, col = tn * WIDTH + at % WIDTH;
+  const int N = PASS == kInput ? a.d : a.f, row = tm * SIDE + at / WIDTH, col = tn * WIDTH + at % WIDTH;
   if (row >= a.rows || col >= N) return;
   const int64_t to = (int64_t)row * N + col;
   float v[2][8] = {};
   for (int p = 0; p < tiles.parts; ++p) {
-    const float* const from = a.partial + ((int64_t)p * rest + t) * (kJoinSide * kJoinSide) + at / WIDTH * kJoinSide + at % WIDTH;
+    const float* const from = a.partial + ((int64_t)p * rest + t) * (SIDE * SIDE) + at / WIDTH * SIDE + at % WIDTH;
 #pragma unroll
     for (int set = 0; set < SETS; ++set) {
       const f32x4 x = *reinterpret_cast<const f32x4*>(from + set * WIDTH), y = *reinterpret_cast<const f32x4*>(from + set * WIDTH + 4);
@@ -221,18 +221,22 @@ dp_status launch_tiles(const GatedArgs& a, const Tiles& tiles, int64_t blocks, h
 // with all units full).  Both as measured, us, large and small: forward 4096 x 768 x 2048 30.0, 35.0; 1000 x 1024 x 2816 28.6, 20.5;
 // 4096 x 4096 x 11008 616, 743; hidden 4096 x 1280 x 3456 47.0, 54.1; 16384 x 768 x 2048 92, 90; 2048 x 1280 x 3456 39.4, 28.4; input 4096 x 4096 x
 // 11008 517, 752; 2048 x 4096 x 4096 145, 118.
-// Where small tiles leave compute units idle, as most input gradients', which contract over 2 f, their contraction is dealt to `parts`
+// Weights whose rows lie far apart (f from some 5000 values on, forward and input gradients) come later than small tiles have asked for them: 0.7 us
+// a stage alone, 1.1 to 1.2 two at a time; large ones, which need half as many bytes to a product, hardly feel it.
+// Where tiles leave compute units idle, as most input gradients', which contract over 2 f, their contraction is dealt to `parts`
 // workgroups, whose sums go through memory (4 bytes an element and part, there and back, at some 6 TB/s) and one more launch.  Input gradients in
-// 1, 2, 4, 8 and 16 parts, us: 128 x 768 x 2048 27.5, 15.9, 9.9, 7.9, 9.4; 256 x 4096 x 11008 162, 89, 55, 54, 81; 4096 x 1280 x 3456 95.0, 90.2,
-// 94.4, 136, 229, and 76.2 with 256 of its 320 tiles whole and the others, which would be a second one on some units, in four parts.  Other passes,
-// whole and in parts: forward 1014 x 7416 x 216 70, 24; 256 x 4096 x 1024 39, 20; hidden, d_out 4096, 1014 x 1024 35, 22.
+// 1, 2, 4, 8 and 16 parts of small tiles, us: 128 x 768 x 2048 27.5, 15.9, 9.9, 7.9, 9.4; 4096 x 1280 x 3456 95.0, 90.2, 94.4, 136, 229, and 76.2 with 256 of
+// its 320 tiles whole and the others, which would be a second one on some units, in four parts; 1014 x 4096 x 11008, weights from memory, 254, 211,
+// 223, 246, and of large ones 441, 238, 160, 183, 242; 512 x 4096 x 11008 120 in 4 parts of small tiles, 95 in 8 of large ones.  Other passes, whole and in
+// parts: forward 1014 x 7416 x 216 70, 24; 256 x 4096 x 1024 39, 20; 200 x 16384 x 8192 199 (small tiles), 147 (large ones); hidden, d_out 4096,
+// 1014 x 1024 35, 22.
 // Few rows, there and on tiles (in parts), us: forward 16 x 4096 x 2048 14.4, 17.8; 64 x 2048 x 4096 15.2, 17.7; 16 x 7424 x 768 26.3, 17.8;
 // 64 x 4096 x 4096 25.3, 21.8; hidden, d_out first, 16 x 8192 x 11008 35.6, 38.8; 64 x 2048 x 4096 10.9, 16.1; 64 x 7424 x 2048 22.5, 18.1; input,
 // 2 f last, 16 x 4096 x 16384 18.0, 23.1; 64 x 4096 x 2048 3.5, 9.5; 64 x 11008 x 4096 33.6, 20.5; 64 x 216 x 7424 18.9, 10.6.
 struct Choice {
   bool few;
-  int64_t large, whole;             // large tiles; small ones, of what is left, that one workgroup has each
-  int parts;                        // of the others
+  int64_t large, whole;             // large tiles and, of what is left, small ones that one workgroup has each
+  int parts, side;                  // of the others, whose sides these are
   int64_t dealt;                    // how many those are
 };
 Choice choose(GatedPass pass, int rows, int d, int f, int d_out) {
@@ -240,7 +244,7 @@ Choice choose(GatedPass pass, int rows, int d, int f, int d_out) {
   const int stages = (int)((K + kProductTerms - 1) / kProductTerms) * (pass == kInput ? 2 : 1);
   auto tiles = [&](int side) { return ((int64_t)rows + side - 1) / side * ((N * (pass == kForward ? 2 : 1) + side - 1) / side); };
   const int64_t all_large = tiles(256), all_small = tiles(128);
-  Choice c = {false, all_large, 0, 1, 0};
+  Choice c = {false, all_large, 0, 1, 128, 0};
   if (rows <= kGatedFewRows) {
     const double weights = (double)stages * kProductTerms * (double)N;
     if (pass == kForward)
@@ -250,27 +254,45 @@ Choice choose(GatedPass pass, int rows, int d, int f, int d_out) {
     if (c.few) return c;
   }
   const float big_rest = pass == kForward ? 9.f : pass == kHidden ? 19.f : 8.f, mid_rest = pass == kHidden ? 13.f : 8.f;
-  auto rounds = [&](int64_t large) { return (float)((large + 255) / 256) * (1.5f * stages + big_rest); };
+  const bool far = pass != kHidden && f >= 5120;
+  const float big_stage = far && pass == kForward ? 1.65f : 1.5f, mid_stage = !far ? 0.4f : pass == kForward ? 0.55f : 0.6f, alone = far ? 0.15f : 0.05f;
+  auto joined = [&](int parts, int64_t dealt, float tile_bytes) {
+    if (dealt == 0 || parts == 1) return 0.f;
+    const float bytes = (float)dealt * tile_bytes;                             // (hidden: its epilogue is the join's)
+    return (pass == kForward && far ? 8.f : 4.f) + (2 * parts + 0.5f) * bytes / (pass == kInput && far ? 4.5e6f : 6e6f) + (pass == kHidden ? 1.3e-6f * bytes : 0.f);
+  };
+  auto rounds = [&](int64_t large) { return (float)((large + 255) / 256) * (big_stage * stages + big_rest); };
   float best = rounds(all_large);
   auto consider = [&](int64_t large, int64_t whole, int parts) {
     const int64_t total = large ? 4 * (all_large - large) : all_small, dealt = total - whole, pieces = dealt * parts, n = whole + pieces;
-    float cost = large ? rounds(large) + 2.f : 0.f;
+    float cost = large ? rounds(large) - 6.f : 0.f;
     if (n > 768) {
-      cost += (0.9f + 0.0004f * stages) / 512.f * stages * (float)total;
+      cost += (far ? 1.1f : 0.9f + 0.0004f * stages) / 512.f * stages * (float)total;
     } else {
-      // a compute unit's workgroups: tile-stages at 0.4 us each, 0.05 more where one runs alone
+      // a compute unit's workgroups, and more where one runs alone
       const float longest = whole ? (float)stages : (float)stages / parts;
       const float all = (float)((whole + 255) / 256) * stages + (float)((pieces + 255) / 256) * stages / parts;
-      cost += 0.4f * all + 0.05f * std::max(0.f, 2.f * longest - all);
+      cost += mid_stage * all + alone * std::max(0.f, 2.f * longest - all);
     }
-    cost += std::max(1.f, (float)n / 512.f) * mid_rest;
-    if (dealt) cost += 4.f + (2 * parts + 0.5f) * ((float)dealt * 65536e-6f / 6.f);
+    cost += std::max(1.f, (float)n / 512.f) * ((float)whole * mid_rest + (float)pieces * 8.f) / (float)n;
+    cost += joined(parts, dealt, 65536.f);
     if (cost < best) {
       best = cost;
       c.large = large;
       c.whole = whole;
+      c.side = 128;
       c.parts = parts;
       c.dealt = dealt;
+    }
+  };
+  auto deal_large = [&](int parts) {
+    const float cost = big_stage * stages / parts + big_rest + joined(parts, all_large, 262144.f);
+    if (cost < best) {
+      best = cost;
+      c.large = c.whole = 0;
+      c.parts = parts;
+      c.side = 256;
+      c.dealt = all_large;
     }
   };
   for (const int64_t large : {(int64_t)0, all_large / 256 * 256}) {
@@ -281,6 +303,7 @@ Choice choose(GatedPass pass, int rows, int d, int f, int d_out) {
       if (4 * parts > stages) break;
       consider(large, 0, parts);
       if (total > 256 && total % 256) consider(large, total / 256 * 256, parts);
+      if (large == 0 && pass != kHidden && all_large * parts <= 256) deal_large(parts);
     }
   }
   return c;
@@ -294,27 +317,36 @@ dp_status launch_pass(const GatedArgs& a, hipStream_t s) {
   const Choice c = choose((GatedPass)PASS, a.rows, a.d, a.f, a.d_out);
   if (c.few) return launch_gated_few(a, (dp_dtype)DT, (GatedPass)PASS, s);
   Tiles tiles = grid_of<PASS, Big>(a, -1);
-  const int large = tiles.count();
+  const int all_large = tiles.count();
+  auto join = [&](auto side) {
+    const unsigned blocks = (unsigned)c.dealt * kJoinGroups<PASS, decltype(side)::value>;
+    gated_join_kernel<PASS, decltype(side)::value, DT><<<dim3(blocks), 256, 0, s>>>(a, tiles);
+    return hip_status(hipGetLastError());
+  };
   dp_status st = DP_OK;
   if (c.large > 0) {
-    tiles.whole = large;
+    tiles.whole = all_large;
     st = launch_tiles<PASS, Big, DT>(a, tiles, c.large, s);
   }
-  if (st != DP_OK || c.large == large) return st;
-  tiles = c.large > 0 ? grid_of<PASS, Big>(a, (int)c.large) : grid_of<PASS, Mid>(a, -1);
+  if (st != DP_OK || c.large == all_large) return st;
+  if (c.large > 0 || c.side == 128) tiles = c.large > 0 ? grid_of<PASS, Big>(a, (int)c.large) : grid_of<PASS, Mid>(a, -1);
   tiles.whole = (int)c.whole;
   tiles.parts = c.parts;
-  st = launch_tiles<PASS, Mid, DT>(a, tiles, c.whole + c.dealt * c.parts, s);
-  if (st != DP_OK || c.dealt == 0) return st;
-  gated_join_kernel<PASS, DT><<<dim3((unsigned)c.dealt * (PASS == kForward ? 4 : 8)), 256, 0, s>>>(a, tiles);
-  return hip_status(hipGetLastError());
+  const int64_t blocks = c.whole + c.dealt * c.parts;
+  if constexpr (PASS != kHidden)
+    if (c.side == 256) {
+      st = launch_tiles<PASS, Big, DT>(a, tiles, blocks, s);
+      return st == DP_OK ? join(std::integral_constant<int, 256>{}) : st;
+    }
+  st = launch_tiles<PASS, Mid, DT>(a, tiles, blocks, s);
+  return st == DP_OK && c.dealt > 0 ? join(std::integral_constant<int, 128>{}) : st;
 }
 
 }  // namespace
 
 size_t gated_tiles_workspace(GatedPass pass, int rows, int d, int f, int d_out) {
   const Choice c = choose(pass, rows, d, f, d_out);
-  return c.few ? 0 : (size_t)c.parts * c.dealt * (kJoinSide * kJoinSide) * sizeof(float);
+  return c.few ? 0 : (size_t)c.parts * c.dealt * (c.side * c.side) * sizeof(float);
 }
 
 dp_status launch_gated_tiles(const GatedArgs& a, dp_dtype dt, GatedPass pass, hipStream_t s) {

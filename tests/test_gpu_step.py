@@ -272,7 +272,9 @@ GATED = [  # rows, d, f, d_out
     # long contractions of few tiles
     (200, 4104, 40, 3080), (1000, 7416, 216, 7416), (70, 520, 72, 4104), (40, 5000, 72, 5000), (2300, 2056, 776, 2056),
     # of what whole rounds leave: forward, hidden
-    (2200, 2056, 4488, 24), (4200, 16, 3976, 2056)]
+    (2200, 2056, 4488, 24), (4200, 16, 3976, 2056),
+    # large tiles in parts, forward and input
+    (136, 6152, 5896, 16)]
 GATED_F32 = GATED + [(5, 1027, 33, 517), (300, 2001, 65, 1999), (1, 1, 1, 1), (5, 3, 7, 2), (111, 60, 161, 61), (130, 257, 65, 33), (64, 17, 129, 130)]
 GATED_CASES = [(d, *s) for d in DTYPES for s in (GATED_F32 if d == "f32" else [(r, 8 * -(-a // 8), b, 8 * -(-c // 8)) for r, a, b, c in GATED])]
 
