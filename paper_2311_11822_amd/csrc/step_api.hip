@@ -1,5 +1,6 @@
 // Entry points of what gated transformer blocks run besides: heads' rotation and norms, gated feed-forward layers, orthogonalised updates.
 // Arguments are checked here, on the host, before anything is launched.
+#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -142,7 +143,7 @@ bool muon_values_fit(const double* abc, int iterations) {
   double most = 1.;
   for (int k = 0; k < iterations; ++k) {
     const double a = abc[3 * k], b = abc[3 * k + 1], c = abc[3 * k + 2], end = most * most;
-    if (!isfinite(a) || !isfinite(b) || !isfinite(c) || end > kMuonMost) return false;
+    if (!(fabs(a) <= FLT_MAX && fabs(b) <= FLT_MAX && fabs(c) <= FLT_MAX && end <= kMuonMost)) return false;      // (kernels take fp32; NaN as well)
     double next = 0., poly = 0.;
     auto at = [&](double s) {                          // s = x^2
       if (!(s >= 0. && s <= end)) return;
@@ -152,14 +153,12 @@ bool muon_values_fit(const double* abc, int iterations) {
     };
     at(0.);
     at(end);
-    if (c != 0.) {
-      at(-b / (2. * c));                               // where the polynomial of A turns, and where x's does: a + 3 b s + 5 c s^2 = 0
-      const double root = sqrt(std::max(0., 9. * b * b - 20. * a * c));
-      at((-3. * b + root) / (10. * c));
-      at((-3. * b - root) / (10. * c));
-    } else if (b != 0.) {
-      at(-a / (3. * b));
-    }
+    // where the polynomial of A turns, and where x's does: a + 3 b s + 5 c s^2 = 0, by the sum of two terms of one sign, so that neither
+    // root is lost where c is next to nothing
+    if (c != 0.) at(-b / (2. * c));
+    const double q = -0.5 * (3. * b + copysign(sqrt(std::max(0., 9. * b * b - 20. * a * c)), b));
+    if (c != 0.) at(q / (5. * c));
+    if (q != 0.) at(a / q);
     if (!(poly <= kMuonMost && next <= kMuonMost)) return false;
     most = next * 1.001;                               // what rounding adds
   }

@@ -240,6 +240,20 @@ def test_muon_refuses_polynomials(abc):
     assert muon(abc=abc) == UNS
 
 
+# Polynomials whose turning points a plain quadratic formula loses: a next to vanishing leading coefficient; squares beyond 64 bits; and
+# coefficients that are finite in 64 bits alone.
+@pytest.mark.parametrize("abc", [((14.0, -14.0, 1e-17), (14.0, 0.0, 0.0)), ((14.0, -14.0, -1e-17), (14.0, 0.0, 0.0)), ((14.0, -14.0, 0.0), (14.0, 0.0, 0.0)),
+                                 ((1.0, 1.7e308, -1.7e308),), ((0.0, 0.0, 0.0), (1.0, 1e39, 0.0)), ((0.0, 0.0, 0.0), (1.0, 0.0, -1e39))])
+def test_muon_refuses_polynomials_at_their_turning_points(abc):
+    assert muon(abc=abc) == UNS
+
+
+def test_muon_takes_polynomials_that_fit():
+    """Up to the workspace's check: the usual ones, and such next to those that are refused."""
+    for abc in (((3.4445, -4.7750, 2.0315),) * 5, ((1.5, -0.5, 0.0),) * 12, ((1.5, -0.5, 1e-17),) * 12, ((14.0, -14.0, 1e-17),), ((0.0, 0.0, 0.0), (1.0, 1e30, 0.0))):
+        assert muon(abc=abc, ws=None) == WS, abc
+
+
 def test_muon_workspace_is_of_one_run():
     """Matrices go in runs of up to 64: the workspace is the largest run's."""
     one = [(None, None, None, None, 128, 160, 0.0, 1.0)]
