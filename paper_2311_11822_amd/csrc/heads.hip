@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(kThreads) heads_kernel(const HeadsArgs a) {
   const unsigned id = blockIdx.x - (w ? a.begin : 0);
   const int b = id / (unsigned)plan.chunks, chunk = id - b * plan.chunks, half = a.turn / 2, heads = a.heads[w];
   const int length = a.len ? min(max(a.len[b], 0), a.T) : a.T;
-  const int begin = min(chunk * plan.chunk_tokens, length), end = min(begin + plan.chunk_tokens, length);
+  const int begin = min(chunk * plan.chunk_tokens, length), end = begin + min(plan.chunk_tokens, length - begin);      // (up to 2^31 - 1)
   const HeadStrides in_stride = a.in_stride[w], out_stride = a.out_stride[w], dy_stride = a.dy_stride[w];
   Unit<VEC> unit[N];
   bool there[N][2];
@@ -144,8 +144,8 @@ __global__ void __launch_bounds__(kThreads) heads_kernel(const HeadsArgs a) {
         }
   };
 
-  for (int first = begin; first < end; first += plan.block_tokens) {
-    const int tokens = min(plan.block_tokens, end - first);
+  for (int done = 0; done < end - begin; done += plan.block_tokens) {
+    const int first = begin + done, tokens = min(plan.block_tokens, end - first);
     int token = group / heads, head = group - token * heads;
     Place x_at, dy_at, out_at;
     x_at.init(in_stride, b, first + token, head, token_step, head_step, heads);
@@ -154,7 +154,7 @@ __global__ void __launch_bounds__(kThreads) heads_kernel(const HeadsArgs a) {
     Row row;
     if (token < tokens) load(row, x_at.at, dy_at.at);
     if (half) {
-      if (first > begin) __syncthreads();              // the last ones' angles have been read
+      if (done > 0) __syncthreads();              // the last ones' angles have been read
       work_out_angles(a, b, first, tokens, angle);
       __syncthreads();
     }
@@ -318,9 +318,10 @@ HeadsPlan plan_side(const HeadsArgs& a, int w, int most) {
       plan.block_tokens = tokens;
     }
   }
-  const int64_t blocks = (int64_t)((a.T + plan.block_tokens - 1) / plan.block_tokens) * a.B;
-  plan.chunk_tokens = plan.block_tokens * (int)((blocks + most - 1) / most);
-  plan.chunks = (a.T + plan.chunk_tokens - 1) / plan.chunk_tokens;
+  // (in 64 bits: tokens are up to 2^31 - 1)
+  const int64_t blocks = ((int64_t)a.T + plan.block_tokens - 1) / plan.block_tokens * a.B;
+  plan.chunk_tokens = (int)std::min<int64_t>(plan.block_tokens * ((blocks + most - 1) / most), a.T);
+  plan.chunks = (int)(((int64_t)a.T + plan.chunk_tokens - 1) / plan.chunk_tokens);
   return plan;
 }
 
