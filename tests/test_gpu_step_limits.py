@@ -4,6 +4,8 @@ next to nothing, against 64-bit values on the CPU or values that are known.
 U is half a unit in the last place of the storage type, relative to the value.
 """
 import math
+import random
+from fractions import Fraction
 
 import pytest
 import torch
@@ -54,3 +56,39 @@ def test_head_norm_gradient_of_two_thousand_million_tokens(block):
     assert abs(sqnorm.item() - float(T) ** 2) <= 2 * 769 * U["f32"] * float(T) ** 2
     for s in slices(dy):                                 # of one column all of dx cancels
         assert (s.abs().max() <= 4 * U["f32"]).item()
+
+
+def check_angles(block, positions, turns):
+    """Pairs (1, 0) turn into cosine and sine.  The library functions are within four units in the last place (OpenCL's bound for them), the
+    angle's rest of a turn is added with two roundings: 5 units, 5 * 2^-23 of the value, whatever its size.  The reference takes a turn's
+    fraction from exact products, and its own cosines are within 1e-13."""
+    half, T = len(turns), len(positions)
+    q = torch.zeros(1, T, 1, 2 * half)
+    q[..., :half] = 1
+    q, out = q.cuda(), torch.empty((1, T, 1, 2 * half), device="cuda")
+    at = torch.tensor([positions], dtype=torch.int32, device="cuda")
+    plan = block.Rotary(q, None, out, None, torch.tensor(turns, dtype=torch.float64, device="cuda"), position=at)
+    sign = 1
+    for call in (plan.forward, plan.backward):
+        call(q, None, out, None)
+        got = out.cpu().double()[0, :, 0]
+        for t, p in enumerate(positions):
+            for i, turn in enumerate(turns):
+                f = Fraction(p) * Fraction(turn)
+                angle = 2 * math.pi * float(f - round(f))
+                for x, want in ((got[t, i].item(), math.cos(angle)), (got[t, half + i].item(), sign * math.sin(angle))):
+                    assert abs(x - want) <= 5 * 2.0 ** -23 * abs(want) + 1e-13, (p, turn, x, want)
+        sign = -1
+
+
+def test_angles_next_to_half_and_quarter_turns(block):
+    """Where sine or cosine are small, what an angle's fraction of a turn loses shows."""
+    rng = random.Random(1)
+    for whole in (0.5, -0.5, 0.25, 0.75, 0.125):
+        check_angles(block, [1, -1, 3], [whole + rng.choice((-1, 1)) * 2.0 ** -rng.uniform(4, 20) for _ in range(64)])
+
+
+def test_angles_at_far_positions(block):
+    rng = random.Random(2)
+    for lo, hi in ((-2 ** 31, -2 ** 31 + 2 ** 20), (2 ** 31 - 2 ** 20, 2 ** 31 - 1), (-2 ** 31, 2 ** 31 - 1), (0, 2 ** 20)):
+        check_angles(block, [rng.randint(lo, hi) for _ in range(60)] + [lo, hi], block.rotary_turns(64).tolist())
