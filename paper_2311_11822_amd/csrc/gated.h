@@ -31,8 +31,9 @@ dp_status launch_gated_backward(const GatedArgs& a, dp_dtype dt, hipStream_t s);
 // The gate's activation: its value and, where asked for, its slope.  All but relu are shares of their argument (sigmoid: the share itself).
 //
 // EXACT, for fp32 results: written with exp(-|v|), so that neither a share nor its complement is a difference.  For 16-bit ones some 2^-23 of 1 is
-// enough of a share, which takes half the instructions; gelu's is then Hastings' approximation of the normal distribution's tail (Abramowitz and
-// Stegun, 7.1.26: within 1.5e-7), whose exponential is its slope's as well.
+// enough of a share, which takes half the instructions (not of sigmoid's slope, which is all there is where the share is next to 1: as the exact one);
+// gelu's is then Hastings' approximation of the normal distribution's tail (Abramowitz and Stegun, 7.1.26: within 1.5e-7), whose exponential is its
+// slope's as well.
 template <int ACT, bool EXACT, bool SLOPE>
 __device__ __forceinline__ float activation(float x, float& slope) {
   constexpr float kLog2e = 1.44269504088896340736f;
@@ -67,6 +68,10 @@ __device__ __forceinline__ float activation(float x, float& slope) {
       const float e = expf(-fabsf(v)), r = 1.f / (1.f + e);
       share = v < 0.f ? e * r : r;
       rise = e * r * r * dv;                           // share (1 - share) dv
+    } else if constexpr (ACT == DP_ACT_SIGMOID && SLOPE) {
+      const float e = __builtin_amdgcn_exp2f(-kLog2e * fabsf(v)), r = __builtin_amdgcn_rcpf(1.f + e);
+      share = v < 0.f ? e * r : r;
+      rise = e * r * r;
     } else {
       share = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * v));
       rise = fmaf(-share, share, share) * dv;

@@ -92,3 +92,27 @@ def test_angles_at_far_positions(block):
     rng = random.Random(2)
     for lo, hi in ((-2 ** 31, -2 ** 31 + 2 ** 20), (2 ** 31 - 2 ** 20, 2 ** 31 - 1), (-2 ** 31, 2 ** 31 - 1), (0, 2 ** 20)):
         check_angles(block, [rng.randint(lo, hi) for _ in range(60)] + [lo, hi], block.rotary_turns(64).tolist())
+
+
+# ------------------------------------------------------------------------------------------------ gated feed-forward layers
+
+def given(block, act, dtype, gate):
+    """act'(gate) and act(gate) as the backward pass has them, of a row of gates: dh and up are ones."""
+    gate = gate.to(DTYPES[dtype])[None].cuda()
+    ones, eye = torch.ones_like(gate), torch.eye(gate.shape[1], dtype=gate.dtype, device="cuda")
+    slope, value = torch.empty_like(gate), torch.empty_like(gate)
+    block.GatedFeedForward(eye, eye, activation=act).backward(ones, gate, ones, slope, value)
+    return gate[0].cpu().double(), slope[0].cpu().double(), value[0].cpu().double()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_sigmoid_slope_of_gates_far_from_zero(block, dtype):
+    """s(x) (1 - s(x)), to a rounding also where s(x) is next to 1.  What comes before it is an exponential, whose argument's rounding is
+    |x| 2^-24 of it, a quotient and products: within (|x| + 16) 2^-24.  Subnormal fp16 numbers are 2^-24 apart."""
+    at = torch.cat([torch.linspace(-24, 24, 193, dtype=torch.float64), torch.tensor([-40.0, -30.0, 30.0, 40.0, 1.28, -1.28, 0.0], dtype=torch.float64)])
+    gate, slope, value = given(block, "sigmoid", dtype, at)
+    e = torch.exp(-gate.abs())
+    for got, want in ((slope, e / (1 + e) ** 2), (value, torch.where(gate < 0, e, 1.0) / (1 + e))):
+        tol = (U[dtype] + (gate.abs() + 16) * 2.0 ** -24) * want + (2.0 ** -25 if dtype == "f16" else 0)
+        off = ((got - want).abs() - tol).max().item()
+        assert off <= 0, (gate[((got - want).abs() - tol).argmax()].item(), off)
