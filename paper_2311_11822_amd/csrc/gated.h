@@ -61,7 +61,7 @@ __device__ __forceinline__ float activation(float x, float& slope) {
     if constexpr (ACT == DP_ACT_GELU_TANH) {           // 1 + tanh(u) = 2 share(2 u)
       constexpr float c = 1.59576912160573071176f, c3 = c * 0.044715f;
       v = x * fmaf(c3, x * x, c);
-      dv = fmaf(3.f * c3, x * x, c);
+      dv = fmaf(3.f * c3, fminf(x * x, 1e30f), c);     // (finite: it meets shares of zero)
     }
     float share, rise;
     if constexpr (EXACT) {

@@ -116,3 +116,14 @@ def test_sigmoid_slope_of_gates_far_from_zero(block, dtype):
         tol = (U[dtype] + (gate.abs() + 16) * 2.0 ** -24) * want + (2.0 ** -25 if dtype == "f16" else 0)
         off = ((got - want).abs() - tol).max().item()
         assert off <= 0, (gate[((got - want).abs() - tol).argmax()].item(), off)
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh", "relu", "sigmoid"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gated_largest_gates(block, dtype, act):
+    """Finite gates whose square is not: slopes and values are those of a step, without a rounding (a slope is at most one, dh and up are)."""
+    at = torch.tensor([1e13, 1e18, 1.9e19, 3e19, 1e20, 1e30, 3e38, 65504.0], dtype=torch.float64)
+    gate, slope, value = given(block, act, dtype, torch.cat([at, -at]))
+    step = (gate > 0).double()
+    assert torch.equal(slope, torch.zeros_like(step) if act == "sigmoid" else step), slope
+    assert torch.equal(value, step if act == "sigmoid" else gate * step), value
