@@ -13,7 +13,7 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = 4, kTerms = 32;         // terms of a stage: 128 bytes of a row
 
-// 16384 x 512 x 1024 forward: 325 us, 106 TFLOP/s (the library's product alone, without what comes of it: 135).
+// 16384 x 512 x 1024 forward: 320 us, 107 TFLOP/s (the library's product alone, without what comes of it: 135).
 // A tile of 32 W x 32 W by four waves of 16 W x 16 W.  Its columns: forward two sets of half as many, the gate's and up's, else those of one product.
 // Memory -> LDS without registers, 4 bytes a lane, so that no row need begin anywhere in particular: 256 loads of 256 bytes to 64 KiB of a
 // stage cost a hundredth of the matrix instructions' time, which is 16 times that of 16-bit ones.  Two stages: one is multiplied, one on its way.
@@ -88,11 +88,11 @@ __global__ void __launch_bounds__(kThreads, 2) gated_f32_kernel(const GatedArgs 
     for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_readfirstlane(r[i]);
     return r;
   };
-  auto ask = [&](int st, unsigned to) {
+  auto ask = [&](int st, unsigned to) __attribute__((always_inline)) {
     const int seg = PASS == kInput && st >= per ? 1 : 0, k = (st - seg * per) * kTerms;
     const char* const pa = static_cast<const char*>(PASS == kForward ? a.x : PASS == kHidden ? a.dy : seg ? a.dup : a.dgate);
     const char* const pb = static_cast<const char*>(PASS == kHidden ? a.w_down : seg ? a.w_up : a.w_gate);
-    auto rows = [&](const char* base, int row0, int row_end, unsigned pitch, unsigned lds) {
+    auto rows = [&](const char* base, int row0, int row_end, unsigned pitch, unsigned lds) __attribute__((always_inline)) {
       const i32x4 r = scalar(make_rsrc(base + (uint64_t)row0 * pitch + 4ull * k, st < end ? (unsigned)imax(imin(row_end - row0, S::SIDE), 0) * pitch : 0));
 #pragma unroll
       for (int l = 0; l < S::LOADS; ++l) {
@@ -119,26 +119,16 @@ __global__ void __launch_bounds__(kThreads, 2) gated_f32_kernel(const GatedArgs 
     }
   };
   f32x4 acc[W][W], sum[W][W];
-  auto begin = [&](f32x4 (&x)[W][W]) {
 #pragma unroll
-    for (int i = 0; i < W; ++i)
+  for (int i = 0; i < W; ++i)
 #pragma unroll
-      for (int k = 0; k < W; ++k) x[i][k] = f32x4{0.f, 0.f, 0.f, 0.f};
-  };
-  begin(acc);
-  begin(sum);
-  auto join = [&]() {
-#pragma unroll
-    for (int i = 0; i < W; ++i)
-#pragma unroll
-      for (int k = 0; k < W; ++k) sum[i][k] += acc[i][k];
-  };
+    for (int k = 0; k < W; ++k) sum[i][k] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int r16 = lane & 15, h = lane >> 4, wm = (wave >> 1) * 16 * W, wc = wave & 1;
   typedef __attribute__((address_space(3))) const f32x4* Four;
   typedef __attribute__((address_space(3))) const float* One;
   ask(first, lds0);
   landed();
-  for (int st = 0; st < end - first; ++st) {
+  auto stage = [&](int st, auto fresh) __attribute__((always_inline)) {
     const unsigned from = lds0 + (st & 1) * S::STAGE_BYTES;
     ask(first + st + 1, lds0 + (~st & 1) * S::STAGE_BYTES);
 #pragma unroll
@@ -165,15 +155,21 @@ __global__ void __launch_bounds__(kThreads, 2) gated_f32_kernel(const GatedArgs 
 #pragma unroll
         for (int x = 0; x < W; ++x)
 #pragma unroll
-          for (int y = 0; y < W; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[x][e], fb[y][e], acc[x][y], 0, 0, 0);
+          for (int y = 0; y < W; ++y)
+            acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[x][e], fb[y][e], fresh && ks + e == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : acc[x][y], 0, 0, 0);
     }
     landed();
-    if ((st & 7) == 7) {                               // sums of 256 terms, then of those: the error grows with the root of either number
-      join();
-      begin(acc);
-    }
+  };
+  // Sums of 64 terms, then of those: the error grows with the root of either number.  2048 terms 1.7e-7 off, chains of 256 2.9e-7 (and no faster:
+  // a chain begins from the zero that its first instructions take).
+  for (int st = 0; st < end - first; ++st) {
+    stage(st, std::true_type{});
+    if (++st < end - first) stage(st, std::false_type{});
+#pragma unroll
+    for (int i = 0; i < W; ++i)
+#pragma unroll
+      for (int k = 0; k < W; ++k) sum[i][k] += acc[i][k];
   }
-  join();
 
   // lane: column lane % 16 of a fragment; register r: row 4 (lane / 16) + r
   constexpr int COLS = SETS ? W / 2 : W;

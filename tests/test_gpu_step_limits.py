@@ -127,3 +127,29 @@ def test_gated_largest_gates(block, dtype, act):
     step = (gate > 0).double()
     assert torch.equal(slope, torch.zeros_like(step) if act == "sigmoid" else step), slope
     assert torch.equal(value, step if act == "sigmoid" else gate * step), value
+
+
+def chained(terms, chain=64):
+    """What fp32 sums of `terms` products in chains of 64, then of those, err by, of random signs: an addition's rounding is spread evenly over a unit in the
+    last place of the sum so far, 2^-23 / m of it, whose root mean square over mantissas m spread evenly in their logarithm is 0.7355 * 2^-23 / sqrt(12) = c; the
+    sum so far grows with the root of the terms, so a chain of n errs by c sqrt(n / 2) of it."""
+    return 0.7355 * 2.0 ** -23 / 12 ** 0.5 * (chain / 2 + terms / chain / 2) ** 0.5
+
+
+@pytest.mark.parametrize("rows,d,f", [(300, 2048, 128), (300, 216, 1024), (4096, 2048, 1024), (64, 768, 2048), (12, 520, 7416)])
+def test_gated_f32_sums_are_in_short_chains(block, rows, d, f):
+    """Within 1.15 times what chains of 64 err by (thousands of results leave its estimate within some percent); chains of 256 err by twice as much."""
+    gen = torch.Generator().manual_seed(rows + d)
+    r = lambda *s: torch.randn(s, generator=gen).cuda()  # noqa: E731
+    x, wg, wu, wd, dy = r(rows, d), r(d, f), r(d, f), r(f, d), r(rows, d)
+    gate, up, h, dgate, dup, dx = *(torch.empty((rows, f), device="cuda") for _ in range(5)), torch.empty_like(x)
+    layer = block.GatedFeedForward(wg, wu, wd, activation="relu")
+    layer.forward(x, h, gate, up)
+    rel = lambda a, b: ((a.double() - b).norm() / b.norm()).item()  # noqa: E731
+    for got, w in ((gate, wg), (up, wu)):
+        assert rel(got, x.double() @ w.double()) <= 1.15 * chained(d)
+    layer.backward(dy, torch.ones_like(gate), torch.ones_like(up), dgate, dup, dx)
+    # gate and up of 1: both are dh
+    for got in (dgate, dup):
+        assert rel(got, dy.double() @ wd.double().t()) <= 1.15 * chained(d)
+    assert rel(dx, dgate.double() @ wg.double().t() + dup.double() @ wu.double().t()) <= 1.15 * chained(2 * f)
