@@ -31,6 +31,12 @@ __device__ __forceinline__ float lanes_sum(float x, int lanes) {
   return x;
 }
 
+// Within one unit in the last place; the instruction itself takes subnormal numbers (eps of zero) for zeros.
+__device__ __forceinline__ float inverse_root(float x) {
+  const bool low = x < 0x1p-126f;
+  return __builtin_amdgcn_rsqf(low ? x * 0x1p64f : x) * (low ? 0x1p32f : 1.f);
+}
+
 // Cosine and sine of each pair at the tokens first .. first + n - 1 of sample b.  What counts of an angle is its fraction of a turn.  Whole
 // turns come off the exact product of position and turns, so the fraction is right to 2^-54 of a turn at any 32-bit position (off the product's
 // nearest 64-bit number: to 2^-25 near 2^31).  Its nearest fp32 number goes to the library's functions, and what that leaves, up to 2^-26 of a turn,
@@ -191,7 +197,7 @@ __global__ void __launch_bounds__(kThreads) heads_kernel(const HeadsArgs a) {
           for (int p = 0; p < 2; ++p)
 #pragma unroll
             for (int k = 0; k < VEC; ++k) square = fmaf(x[n][p][k], x[n][p][k], square);
-        r = __builtin_amdgcn_rsqf(lanes_sum(square, a.lanes) * width + a.eps);       // within one unit in the last place
+        r = inverse_root(lanes_sum(square, a.lanes) * width + a.eps);
       }
       if constexpr (GRAD) {
         float uh = 0.f;

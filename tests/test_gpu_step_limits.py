@@ -58,6 +58,27 @@ def test_head_norm_gradient_of_two_thousand_million_tokens(block):
         assert (s.abs().max() <= 4 * U["f32"]).item()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_head_norm_of_next_to_nothing(block, dtype):
+    """Rows whose mean square is a subnormal fp32 number, without eps: squares of 3e-20 are within 2^-150 of their 9e-40, 7.8e-7 of it, and so is each of
+    the eight sums and the mean; the root halves ten of these."""
+    gen = torch.Generator().manual_seed(1)
+    x = (torch.sign(torch.randn(1, 40, 2, 8, generator=gen)) * torch.empty(1, 40, 2, 8).uniform_(2.5e-20, 6e-20, generator=gen)).to(DTYPES[dtype])
+    x[0, 7], x[0, 8, 1] = 1.0, 1e18                       # beside ordinary rows
+    q, out, dy = x.cuda(), torch.empty_like(x, device="cuda"), torch.ones(x.shape, dtype=x.dtype)
+    norm = block.HeadNorm(q, None, out, None, eps=0.0)
+    norm.forward(q, None, out, None)
+    r = x.double().square().mean(-1, keepdim=True) ** -0.5
+    tol = U[dtype] + 5 * 2.0 ** -150 / 2.5e-20 ** 2 + 1e-6
+    assert ((out.cpu().double() - x.double() * r).abs() <= tol * (x.double() * r).abs()).all()
+    dx = torch.empty_like(q)
+    norm.backward(q, None, dy.cuda(), None, dx, None)
+    h = x.double() * r
+    want = r * (1 - h * h.mean(-1, keepdim=True))
+    # (relative to the root; two factors of it, and the difference that cancels)
+    assert ((dx.cpu().double() - want).abs() <= 4 * tol * r * (1 + h.abs() * h.abs().mean(-1, keepdim=True))).all()
+
+
 def check_angles(block, positions, turns):
     """Pairs (1, 0) turn into cosine and sine.  The library functions are within four units in the last place (OpenCL's bound for them), the
     angle's rest of a turn is added with two roundings: 5 units, 5 * 2^-23 of the value, whatever its size.  The reference takes a turn's
