@@ -174,3 +174,85 @@ def test_gated_f32_sums_are_in_short_chains(block, rows, d, f):
     for got in (dgate, dup):
         assert rel(got, dy.double() @ wd.double().t()) <= 1.15 * chained(d)
     assert rel(dx, dgate.double() @ wg.double().t() + dup.double() @ wu.double().t()) <= 1.15 * chained(2 * f)
+
+
+# ------------------------------------------------------------------------------------------------ as programs call them
+
+def test_graphs_and_eager_calls_of_the_same_objects(block):
+    """Two graphs and eager calls on two streams, all of the same objects: no graph's scratch is another's or an eager call's, nor does one eager stream's
+    touch the other's; and both at once leave what each alone does."""
+    from test_gpu_step import Step
+    s = Step(block, 7)
+    s.fill()
+    used = []
+    for o in s.objects:
+        inner = o._ws
+        o._ws = lambda *args, inner=inner: used.append(inner(*args)) or used[-1]
+    streams, held = [torch.cuda.Stream(), torch.cuda.Stream()], []
+
+    def spans():
+        found = {(t.data_ptr(), t.data_ptr() + t.numel()) for t in used}
+        held.extend(used)                                # an eager call's stays while others are made
+        del used[:]
+        return found
+
+    def eager(stream):
+        with torch.cuda.stream(stream):
+            s.run()
+        torch.cuda.synchronize()
+        return spans()
+
+    graphs, groups = [], []
+    for stream in streams:
+        eager(stream)                                    # grows the workspaces
+        groups.append(eager(stream))
+    for stream in streams:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            s.run()
+        graphs.append(graph)
+        found = {(t.data_ptr(), t.data_ptr() + t.numel()) for t in used}
+        del used[:]                                      # the pool's, and the graph's
+        groups.append(found)
+    assert groups[0] == eager(streams[0]) and groups[1] == eager(streams[1])      # an object's own from call to call
+    assert all(len(g) >= 2 for g in groups)
+    for i, a in enumerate(groups):
+        for b in groups[:i]:
+            assert all(x[1] <= y[0] or y[1] <= x[0] for x in a for y in b)
+    # what is not updated in place, by a graph on one stream beside eager calls on the other: same inputs, same results
+    norm, gated, _, *layers = s.objects
+    x = [torch.randn((n, o.d), device="cuda").to(o.dtype) for o, n in zip((gated, *layers), (600, 90, 20))]
+    sets = [[[torch.empty((t.shape[0], o.f), dtype=o.dtype, device="cuda") for _ in range(5)] + [torch.empty_like(t)] for o, t in zip((gated, *layers), x)]
+            for _ in range(3)]
+    kept = [(torch.empty_like(s.kept), torch.empty_like(s.sq), torch.empty_like(s.dx)) for _ in range(3)]
+    views = lambda t: (t[:, :, :6], t[:, :, 6:7])  # noqa: E731
+
+    def calls(k):
+        norm.backward(*views(s.x), s.dq, s.dk, *views(kept[k][2]), *kept[k][:2])
+        for o, t, (gate, up, h, dgate, dup, dx) in zip((gated, *layers), x, sets[k]):
+            o.forward(t, h, gate, up)
+            o.backward(t if o.w_down is not None else h, gate, up, dgate, dup, dx)
+
+    def results(k):
+        return [*views(kept[k][2]), *kept[k][:2], *[t for group in sets[k] for t in group]]
+
+    calls(0)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(streams[1]):
+        calls(2)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=streams[0]):
+        calls(1)
+    for _ in range(6):
+        for k in (1, 2):
+            for t in results(k):
+                t.fill_(7.0)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(streams[0]):
+            graph.replay()
+        with torch.cuda.stream(streams[1]):
+            calls(2)
+        torch.cuda.synchronize()
+        for k in (1, 2):
+            assert all(torch.equal(a, b) for a, b in zip(results(k), results(0)))
