@@ -641,6 +641,15 @@ dp_status dp_gated_backward(const void* dy, const void* w_down, int d_out, const
                             size_t ws_bytes, void* stream);
 
 /*
+ * Host query (no GPU): how a pass of a gated layer is launched, so that a test can pin the kernels that it means to run.
+ *   pass      0: forward; 1: dgate and dup from dy and w_down (d_out is looked at here alone); 2: dx
+ *   launches  HOST, [6]: the kernel (0: tiles of 16-bit types, 256 x 256 and 128 x 128; 1: few rows; 2: tiles of fp32, 128 x 128 and 64 x 64); large tiles
+ *             of one workgroup each; small ones (where there are large ones too, of what those leave); tiles whose contraction several workgroups
+ *             share; how many; the side of these
+ */
+dp_status dp_gated_launches(dp_dtype dt, int rows, int d, int f, int d_out, int pass, int32_t* launches);
+
+/*
  * One step of an optimizer that orthogonalises its update, over many matrices, in place:
  *   g = grad_scale grad;  m = beta m + g;  u = g + beta m (nesterov = 1) or m;  X = u / (||u||_F + eps);
  *   `iterations` times  X <- a X + b A X + c A^2 X,  A = X X'  (on the shorter side);

@@ -119,6 +119,7 @@ _PROTOS = {
     "dp_gated": (_i, [_vp, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
     "dp_gated_backward_workspace_bytes": (_sz, [_i, _i, _i, _i, _i]),
     "dp_gated_backward": (_i, [_vp, _vp, _i, _vp, _vp, _i, _i, _i, _i, _vp, _vp, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "dp_gated_launches": (_i, [_i, _i, _i, _i, _i, _i, _vp]),
     "dp_muon_workspace_bytes": (_sz, [C.POINTER(dp_muon_tensor), _i]),
     "dp_muon_multi": (_i, [C.POINTER(dp_muon_tensor), _i, _i, _i, C.c_double, C.c_double, _i, C.c_double, C.c_double, C.POINTER(C.c_double), _i,
                           _vp, _sz, _vp]),
@@ -469,6 +470,13 @@ def dp_gated_backward_workspace_bytes(dt, rows, d, f, d_out) -> int:
 
 def dp_gated_backward(dy, w_down, d_out, gate, up, dt, rows, d, f, w_gate, w_up, act, dgate, dup, dx, ws=None, stream=None) -> None:
     _call("dp_gated_backward", dy, w_down, d_out, gate, up, dt, rows, d, f, w_gate, w_up, act, dgate, dup, dx, ws, _nbytes(ws), stream)
+
+
+def dp_gated_launches(dt, rows, d, f, d_out, which) -> dict:
+    """How a pass (0: forward, 1: hidden gradients, 2: input gradients) is launched (host function)."""
+    out = (C.c_int32 * 6)()
+    _check(lib.dp_gated_launches(dt, rows, d, f, d_out, which, out), "dp_gated_launches")
+    return dict(zip(("kernel", "large", "small", "dealt", "parts", "side"), out))
 
 
 def muon_tensors(tensors: Sequence) -> "C.Array[dp_muon_tensor]":

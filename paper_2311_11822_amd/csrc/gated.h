@@ -21,6 +21,15 @@ struct GatedArgs {
 // The products: x with both weights; dy with w_down; dgate and dup with theirs.
 enum GatedPass { kForward, kHidden, kInput };
 dp_status launch_gated_tiles(const GatedArgs& a, dp_dtype dt, GatedPass pass, hipStream_t s);      // 16-bit types (gated_tiles.hip)
+// How a pass is launched: the kernel, its tiles of one workgroup each, large and small, and those that several share.
+enum GatedKernel { kGatedTiles16 = 0, kGatedFew = 1, kGatedTiles32 = 2 };
+struct GatedLaunches {
+  int kernel;
+  int64_t large, small, dealt;
+  int parts, side;                                     // of the dealt ones
+};
+GatedLaunches gated_tiles_launches(GatedPass pass, int rows, int d, int f, int d_out);
+GatedLaunches gated_launches(dp_dtype dt, GatedPass pass, int rows, int d, int f, int d_out);
 size_t gated_tiles_workspace(GatedPass pass, int rows, int d, int f, int d_out);                   // bytes of `partial`
 size_t gated_workspace(dp_dtype dt, GatedPass pass, int rows, int d, int f, int d_out);            // of any type
 constexpr int kGatedFewRows = 64;

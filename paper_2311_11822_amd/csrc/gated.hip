@@ -313,6 +313,13 @@ dp_status launch_f32(const GatedArgs& a, hipStream_t s) {
 
 }  // namespace
 
+GatedLaunches gated_launches(dp_dtype dt, GatedPass pass, int rows, int d, int f, int d_out) {
+  if (dt != DP_F32) return gated_tiles_launches(pass, rows, d, f, d_out);
+  const F32Choice c = choose_f32(pass, rows, d, f, d_out);
+  const int64_t tiles = (int64_t)c.tiles_m * c.tiles_n;
+  return {kGatedTiles32, c.large ? tiles : 0, !c.large && c.parts == 1 ? tiles : 0, c.parts > 1 ? tiles : 0, c.parts > 1 ? c.parts : 0, c.parts > 1 ? 64 : 0};
+}
+
 size_t gated_workspace(dp_dtype dt, GatedPass pass, int rows, int d, int f, int d_out) {
   if (dt != DP_F32) return gated_tiles_workspace(pass, rows, d, f, d_out);
   const F32Choice c = choose_f32(pass, rows, d, f, d_out);

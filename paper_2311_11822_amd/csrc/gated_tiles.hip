@@ -344,6 +344,12 @@ dp_status launch_pass(const GatedArgs& a, hipStream_t s) {
 
 }  // namespace
 
+GatedLaunches gated_tiles_launches(GatedPass pass, int rows, int d, int f, int d_out) {
+  const Choice c = choose(pass, rows, d, f, d_out);
+  if (c.few) return {kGatedFew, 0, 0, 0, 0, 0};
+  return {kGatedTiles16, c.large, c.whole, c.dealt, c.dealt ? c.parts : 0, c.dealt ? c.side : 0};
+}
+
 size_t gated_tiles_workspace(GatedPass pass, int rows, int d, int f, int d_out) {
   const Choice c = choose(pass, rows, d, f, d_out);
   return c.few ? 0 : (size_t)c.parts * c.dealt * (c.side * c.side) * sizeof(float);

@@ -317,6 +317,16 @@ dp_status dp_gated_backward(const void* dy, const void* w_down, int d_out, const
   return launch_gated_backward(a, dt, static_cast<hipStream_t>(stream));
 }
 
+dp_status dp_gated_launches(dp_dtype dt, int rows, int d, int f, int d_out, int pass, int32_t* launches) {
+  const dp_status st = gated_shape(dt, rows, d, f, pass == kHidden ? d_out : d);
+  if (st != DP_OK) return st;
+  if (pass < kForward || pass > kInput || !launches) return DP_ERR_INVALID_ARG;
+  const GatedLaunches l = gated_launches(dt, (GatedPass)pass, rows, d, f, d_out);
+  const int64_t all[6] = {l.kernel, l.large, l.small, l.dealt, l.parts, l.side};
+  for (int i = 0; i < 6; ++i) launches[i] = (int32_t)std::min<int64_t>(all[i], INT32_MAX);
+  return DP_OK;
+}
+
 size_t dp_muon_workspace_bytes(const dp_muon_tensor* tensors, int n_tensors) {
   if (muon_sizes(tensors, n_tensors) != DP_OK) return 0;
   size_t most = 0;
