@@ -673,6 +673,12 @@ typedef struct {
   float weight_decay, scale;
 } dp_muon_tensor;
 size_t dp_muon_workspace_bytes(const dp_muon_tensor* tensors, int n_tensors);
+/*
+ * Host query (no GPU): how such a step is launched, so that a test can pin the kernels that it means to run; rows and cols are looked at alone.
+ *   launches  HOST, [7]: matrices that one workgroup holds each; of the first run of others, for A, its polynomial and the update, the side of tiles
+ *             and the workgroups that share one (0: there are none)
+ */
+dp_status dp_muon_launches(const dp_muon_tensor* tensors, int n_tensors, int32_t* launches);
 dp_status dp_muon_multi(const dp_muon_tensor* tensors, int n_tensors, dp_dtype grad_dt, dp_dtype copy_dt, double lr, double beta, int nesterov,
                         double grad_scale, double eps, const double* coefficients, int iterations, void* ws, size_t ws_bytes, void* stream);
 

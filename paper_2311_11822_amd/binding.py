@@ -121,6 +121,7 @@ _PROTOS = {
     "dp_gated_backward": (_i, [_vp, _vp, _i, _vp, _vp, _i, _i, _i, _i, _vp, _vp, _i, _vp, _vp, _vp, _vp, _sz, _vp]),
     "dp_gated_launches": (_i, [_i, _i, _i, _i, _i, _i, _vp]),
     "dp_muon_workspace_bytes": (_sz, [C.POINTER(dp_muon_tensor), _i]),
+    "dp_muon_launches": (_i, [C.POINTER(dp_muon_tensor), _i, _vp]),
     "dp_muon_multi": (_i, [C.POINTER(dp_muon_tensor), _i, _i, _i, C.c_double, C.c_double, _i, C.c_double, C.c_double, C.POINTER(C.c_double), _i,
                           _vp, _sz, _vp]),
     "dp_ghost_tile_order": (C.c_int64, [_i, _i, _vp, _vp, _vp, _vp, C.c_int64]),
@@ -490,6 +491,14 @@ def muon_tensors(tensors: Sequence) -> "C.Array[dp_muon_tensor]":
 def dp_muon_workspace_bytes(tensors) -> int:
     arr = tensors if isinstance(tensors, C.Array) else muon_tensors(tensors)
     return lib.dp_muon_workspace_bytes(arr, len(arr))
+
+
+def dp_muon_launches(tensors) -> dict:
+    """How a step of these is launched: matrices of one workgroup, and (side, workgroups) of the others' tiles in each product (host function)."""
+    arr = tensors if isinstance(tensors, C.Array) else muon_tensors(tensors)
+    out = (C.c_int32 * 7)()
+    _check(lib.dp_muon_launches(arr, len(arr), out), "dp_muon_launches")
+    return dict(held=out[0], square=(out[1], out[2]), polynomial=(out[3], out[4]), update=(out[5], out[6]))
 
 
 def dp_muon_multi(tensors, grad_dt, copy_dt, lr, beta, nesterov, grad_scale, eps, coefficients, ws, stream=None) -> None:

@@ -31,6 +31,10 @@ struct MuonArgs {
 bool muon_is_small(int rows, int cols);
 dp_status launch_muon_small(const MuonTensor* tensors, int n, const MuonArgs& a, dp_dtype grad_dt, dp_dtype copy_dt, hipStream_t s);
 // Of one run of up to kMuonGroup matrices.
+struct MuonLaunches {
+  int side, parts;                                     // of a step's tiles, and the workgroups that share one
+};
+void muon_launches(const MuonTensor* tensors, int n, MuonLaunches (&steps)[3]);                     // A, its polynomial, the update
 size_t muon_workspace(const MuonTensor* tensors, int n);
 dp_status launch_muon(const MuonTensor* tensors, int n, const MuonArgs& a, dp_dtype grad_dt, dp_dtype copy_dt, void* ws, hipStream_t s);
 

@@ -430,6 +430,11 @@ size_t matrix_bytes(int rows, int cols, size_t (&at)[5]) {
 
 }  // namespace
 
+void muon_launches(const MuonTensor* tensors, int n, MuonLaunches (&steps)[3]) {
+  const StepChoice c[3] = {choose_step<kGram>(tensors, n), choose_step<kPoly>(tensors, n), choose_step<kUpdate>(tensors, n)};
+  for (int i = 0; i < 3; ++i) steps[i] = {c[i].large ? 256 : kDealtSide, c[i].parts};
+}
+
 size_t muon_workspace(const MuonTensor* tensors, int n) {
   size_t total = 0, at[5];
   for (int i = 0; i < n; ++i) total += matrix_bytes(tensors[i].rows, tensors[i].cols, at);

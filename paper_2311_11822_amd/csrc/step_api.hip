@@ -337,6 +337,25 @@ size_t dp_muon_workspace_bytes(const dp_muon_tensor* tensors, int n_tensors) {
   return most;
 }
 
+dp_status dp_muon_launches(const dp_muon_tensor* tensors, int n_tensors, int32_t* launches) {
+  const dp_status st = muon_sizes(tensors, n_tensors);
+  if (st != DP_OK) return st;
+  if (!launches) return DP_ERR_INVALID_ARG;
+  std::fill(launches, launches + 7, 0);
+  int runs = 0;
+  muon_runs(tensors, n_tensors, [&](const MuonTensor* run, int n, bool small) {
+    if (small) {
+      launches[0] += n;
+    } else if (++runs == 1) {
+      MuonLaunches steps[3];
+      muon_launches(run, n, steps);
+      for (int i = 0; i < 3; ++i) launches[1 + 2 * i] = steps[i].side, launches[2 + 2 * i] = steps[i].parts;
+    }
+    return DP_OK;
+  });
+  return DP_OK;
+}
+
 dp_status dp_muon_multi(const dp_muon_tensor* tensors, int n_tensors, dp_dtype grad_dt, dp_dtype copy_dt, double lr, double beta, int nesterov,
                         double grad_scale, double eps, const double* coefficients, int iterations, void* ws, size_t ws_bytes, void* stream) {
   if (!dtype_ok(grad_dt) || !dtype_ok(copy_dt) || !coefficients || iterations < 1 || iterations > kMuonMostIterations) return DP_ERR_INVALID_ARG;
