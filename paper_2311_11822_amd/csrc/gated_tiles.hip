@@ -221,8 +221,12 @@ dp_status launch_tiles(const GatedArgs& a, const Tiles& tiles, int64_t blocks, h
 // with all units full).  Both as measured, us, large and small: forward 4096 x 768 x 2048 30.0, 35.0; 1000 x 1024 x 2816 28.6, 20.5;
 // 4096 x 4096 x 11008 616, 743; hidden 4096 x 1280 x 3456 47.0, 54.1; 16384 x 768 x 2048 92, 90; 2048 x 1280 x 3456 39.4, 28.4; input 4096 x 4096 x
 // 11008 517, 752; 2048 x 4096 x 4096 145, 118.
-// Weights whose rows lie far apart (f from some 5000 values on, forward and input gradients) come later than small tiles have asked for them: 0.7 us
-// a stage alone, 1.1 to 1.2 two at a time; large ones, which need half as many bytes to a product, hardly feel it.
+// Weights that come from memory arrive later than small tiles have asked for them: 0.7 us a stage alone, 1.1 to 1.2 two at a time; large ones, which
+// need half as many bytes to a product, hardly feel it.  Where they come from is not known here; the forward pass and input gradients take these costs
+// (`far`) from f = 5120 on, where what they lose if a cache has the weights after all meets what they win if none has.  The other costs and these, us,
+// from memory and, behind the semicolon, from caches: input gradients 1014 x 2048 x 4096 58.7, 51.8; 43.7, 45.9.  x 4608 64.9, 58.8; 48.1, 53.3.
+// x 5112 76.3, 67.8; 62.0, 60.3.  x 5120 71.8, 61.8; 52.5, 56.6.  x 6144 83.0, 66.6; 61.9, 61.8.  2048 x 4096 x 4096 137, 128; 123, 123.  x 5120 173, 155;
+// 154, 148.  Forward 1014 x 2048 x 4096 47.0, 47.9; 40.2, 40.4.  x 5120 65.2, 55.0; 54.5, 52.3.  (Rows of 5112 values begin inside of lines, at any rule.)
 // Where tiles leave compute units idle, as most input gradients', which contract over 2 f, their contraction is dealt to `parts`
 // workgroups, whose sums go through memory (4 bytes an element and part, there and back, at some 6 TB/s) and one more launch.  Input gradients in
 // 1, 2, 4, 8 and 16 parts of small tiles, us: 128 x 768 x 2048 27.5, 15.9, 9.9, 7.9, 9.4; 4096 x 1280 x 3456 95.0, 90.2, 94.4, 136, 229, and 76.2 with 256 of
@@ -230,9 +234,10 @@ dp_status launch_tiles(const GatedArgs& a, const Tiles& tiles, int64_t blocks, h
 // 223, 246, and of large ones 441, 238, 160, 183, 242; 512 x 4096 x 11008 120 in 4 parts of small tiles, 95 in 8 of large ones.  Other passes, whole and in
 // parts: forward 1014 x 7416 x 216 70, 24; 256 x 4096 x 1024 39, 20; 200 x 16384 x 8192 199 (small tiles), 147 (large ones); hidden, d_out 4096,
 // 1014 x 1024 35, 22.
-// Few rows, there and on tiles (in parts), us: forward 16 x 4096 x 2048 14.4, 17.8; 64 x 2048 x 4096 15.2, 17.7; 16 x 7424 x 768 26.3, 17.8;
-// 64 x 4096 x 4096 25.3, 21.8; hidden, d_out first, 16 x 8192 x 11008 35.6, 38.8; 64 x 2048 x 4096 10.9, 16.1; 64 x 7424 x 2048 22.5, 18.1; input,
-// 2 f last, 16 x 4096 x 16384 18.0, 23.1; 64 x 4096 x 2048 3.5, 9.5; 64 x 11008 x 4096 33.6, 20.5; 64 x 216 x 7424 18.9, 10.6.
+// Few rows, there and on tiles (in parts), weights from caches, us: forward 16 x 4096 x 2048 14.4, 17.8; 64 x 2048 x 4096 15.2, 17.7; 16 x 7424 x 768
+// 26.3, 17.8; 64 x 4096 x 4096 25.3, 21.8 (from memory 63 or 64 x 2048 x 4096 20.7, 20.6, x 4096 x 2048 33.6, 21.2: the rule ends between those rows);
+// hidden, d_out first, 16 x 8192 x 11008 35.6, 38.8; 64 x 2048 x 4096 10.9, 16.1; 64 x 7424 x 2048 22.5, 18.1; input, 2 f last, 16 x 4096 x 16384 18.0,
+// 23.1; 64 x 4096 x 2048 3.5, 9.5; 64 x 11008 x 4096 33.6, 20.5; 64 x 216 x 7424 18.9, 10.6.
 struct Choice {
   bool few;
   int64_t large, whole;             // large tiles and, of what is left, small ones that one workgroup has each
