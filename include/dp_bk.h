@@ -618,7 +618,8 @@ dp_status dp_head_norm_backward(const dp_heads_shape* shape, dp_dtype dt, const 
  *   h         device, [rows, f] of type dt
  *   ws        device scratch, >= dp_gated_workspace_bytes(...), 16-byte aligned; not used where the size is 0
  * For 16-bit types d and f are multiples of 8 and arrays 16-byte aligned (DP_F32: 4-byte).  d and f are at most 2^20.  Results overlap nothing.
- * act: silu x s(x), s the logistic function; gelu x Phi(x); gelu_tanh its form by tanh; relu; sigmoid s(x).
+ * act: silu x s(x), s the logistic function; gelu x Phi(x); gelu_tanh its form by tanh; relu; sigmoid s(x).  For 16-bit types Phi(x) is within 1.5e-7
+ * (where it is below 1e-10 itself, at x < -6.5, from 0.5 % of it on), s(x) within 2^-22.
  */
 typedef enum { DP_ACT_SILU = 0, DP_ACT_GELU = 1, DP_ACT_GELU_TANH = 2, DP_ACT_RELU = 3, DP_ACT_SIGMOID = 4 } dp_activation;
 size_t dp_gated_workspace_bytes(dp_dtype dt, int rows, int d, int f);
